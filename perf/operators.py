@@ -307,8 +307,8 @@ def _own_grouped_bw(s):
     c, st = s.case, _stream()
     a, b, G, e, t = c["d_in"], c["d_out"], c["groups"], _SIZE[c["dtype"]], T[c["dtype"]]
     ws, ws_bytes = _workspace(s, B.fg_linear_grouped_backward_workspace_bytes(t, s.k, G, a, b)) if s.ws is None else (s.ws, s.ws.numel())
-    B.fg_linear_grouped_backward(s.x, len(s.x), a * e, t, None, s.dh, b * e, s.h, b * e if s.h is not None else 0, s.n, s.order, s.offsets, s.k, G,
-                                 a, b, s.w, s.dx, a * _SIZE[c["out"]], T[c["out"]], s.dw, s.db, ws, ws_bytes, st)
+    B.fg_linear_grouped_backward(s.x, len(s.x), a * e, t, None, s.dh, b * e, t, s.h, b * e if s.h is not None else 0, s.n, s.order, s.offsets, s.k,
+                                 G, a, b, s.w, s.dx, a * _SIZE[c["out"]], T[c["out"]], s.dw, s.db, ws, ws_bytes, st)
     return dict(dx=s.dx, dw=s.dw, db=s.db)
 
 
@@ -316,7 +316,8 @@ def _own_norm(s):
     B, T = _lib()
     c = s.case
     d, e = c["d"], _SIZE[c["dtype"]]
-    B.fg_residual_norm(s.x, d * e, s.residual, d * e if s.residual is not None else 0, T[c["dtype"]], s.rows, s.n_rows, s.k, s.n, d, s.p, s.key,
+    t = T[c["dtype"]]
+    B.fg_residual_norm(s.x, d * e, t, s.residual, d * e if s.residual is not None else 0, t, s.rows, s.n_rows, s.k, s.n, d, s.p, s.key,
                        s.w, _EPS, s.sum, d * e, s.y, d * _SIZE[c["out"]], T[c["out"]], s.scale, s.rstd, _stream())
     out = dict(sum=s.sum, rstd=s.rstd, y=s.y)
     return dict(out, scale=s.scale) if s.scale is not None else out
@@ -327,8 +328,9 @@ def _own_norm_bw(s):
     c = s.case
     d, e = c["d"], _SIZE[c["dtype"]]
     ws, ws_bytes = _workspace(s, B.fg_residual_norm_backward_workspace_bytes(s.k, d)) if s.ws is None else (s.ws, s.ws.numel())
-    B.fg_residual_norm_backward(s.dy, d * e, s.sum, d * e, T[c["dtype"]], s.rstd, s.w, s.dsum_in, d * e if s.dsum_in is not None else 0, s.rows,
-                                s.n_rows, s.k, s.n, d, s.p, s.key, s.dsum, d * e, s.dx, d * e if s.p else 0, s.dw, ws, ws_bytes, _stream())
+    t = T[c["dtype"]]
+    B.fg_residual_norm_backward(s.dy, d * e, t, s.sum, d * e, t, s.rstd, s.w, s.dsum_in, d * e if s.dsum_in is not None else 0, s.rows, s.n_rows,
+                                s.k, s.n, d, s.p, s.key, s.dsum, d * e, s.dx, d * e if s.p else 0, s.dw, ws, ws_bytes, _stream())
     return dict(dsum=s.dsum, dx=s.dx, dw=s.dw) if s.p else dict(dsum=s.dsum, dw=s.dw)
 
 
