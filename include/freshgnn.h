@@ -54,7 +54,9 @@ enum {
     FG_ERR_HIP = 6          /* the HIP runtime reported an error (message in fg_last_error) */
 };
 
-typedef enum { FG_F32 = 0, FG_F16 = 1, FG_BF16 = 2 } fg_dtype_t;
+/* FG_E4M3: 8 bits (1 sign, 4 exponent, 3 mantissa; finite values up to 448, no infinities), with a float scale per row beside it: a row's
+ * values are its 8-bit values times its scale. Only the calls that name it take it. */
+typedef enum { FG_F32 = 0, FG_F16 = 1, FG_BF16 = 2, FG_E4M3 = 3 } fg_dtype_t;
 
 typedef struct fg_cache fg_cache_t; /* opaque: the historical embedding caches C^(1..L-1) of one model */
 
@@ -787,6 +789,134 @@ typedef struct fg_weight_grad_layer {
 size_t fg_backward_weights_all_workspace_bytes(fg_dtype_t compute_dtype, int32_t n_layers, const fg_weight_grad_layer_t* layers);
 fg_status_t fg_backward_weights_all(fg_dtype_t compute_dtype, int32_t n_layers, const fg_weight_grad_layer_t* layers, void* ws_dev,
                                     size_t ws_bytes, void* stream);
+
+/*
+ * ---- Layers with a weight matrix per node type, and what stands between two layers ----
+ * For relational models (the paper's R-GCN on the heterogeneous MAG240M, Section 7.5): the nodes have types ("groups"), and the dense
+ * update of a row takes its group's weights. fg_group_rows sorts a layer's listed rows by group on the device, fg_linear_grouped
+ * multiplies, fg_linear_grouped_backward gives the gradients. fg_residual_norm, fg_dropout and their backward passes are the element-wise part of a deeper
+ * model's layer. All of them work by position, on the rows listed (no position twice), as the calls above: rows that are not listed are neither
+ * read nor written.
+ *
+ * fg_group_rows: the listed positions r = rows[k], k < *n_rows_dev, sorted by their group, stably (in list order within a group):
+ *   order[offsets[g] .. offsets[g + 1]) = the positions of group g = groups[v], v = ids[r] (ids NULL: v = r)
+ *   groups_dev [n_table]                int32 group of every node (or, ids NULL, of every position)
+ *   ids_dev [n_positions]               int32 node ids by position, or NULL
+ *   rows_dev, n_rows_dev, max_rows      the list (NULL: 0 .. count-1), its device-side count (NULL: max_rows) and bound
+ *   n_groups                            1 .. FG_MAX_GROUPS
+ *   order_dev [max_rows]                out, int32; entries at and beyond offsets[n_groups] are left as they were
+ *   offsets_dev [n_groups + 1]          out, int64; offsets[n_groups] = rows that have a group
+ *   ws_dev, ws_bytes                    device workspace, >= fg_group_rows_workspace_bytes(max_rows, n_groups), 16-byte aligned
+ * Positions outside [0, n_positions), ids outside [0, n_table) and groups outside [0, n_groups) are left out. One launch for up to 8192
+ * rows, else two. The result does not depend on the order in which threads run.
+ */
+#define FG_MAX_GROUPS 1024
+size_t fg_group_rows_workspace_bytes(int64_t max_rows, int32_t n_groups);
+fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int32_t* ids_dev, int64_t n_positions, const int32_t* rows_dev,
+                          const int64_t* n_rows_dev, int64_t max_rows, int32_t n_groups, int32_t* order_dev, int64_t* offsets_dev, void* ws_dev,
+                          size_t ws_bytes, void* stream);
+
+/*
+ * Dense update with a weight matrix per group, for the positions in `order`:
+ *   h_out[r, :] = act( x[s, :] . W[g] + bias[g, :] ),  r = order[k], offsets[g] <= k < offsets[g + 1],  s = src_ids[r] (NULL: s = r)
+ *   x, x_rows, x_stride, dtype          the rows, FG_F32, FG_F16, FG_BF16 or FG_E4M3, byte stride; with src_ids a table read by row number
+ *   x_scale [x_rows]                    FG_E4M3: a row's scale (fg_residual_norm, fg_quantize_rows); else NULL
+ *   src_ids_dev [n_out]                 int32 rows of x by position, or NULL
+ *   order_dev, offsets_dev, n_groups    as fg_group_rows leaves them (order NULL: position k itself, rows that lie sorted by group);
+ *                                       at most max_rows entries are taken; no position twice
+ *   W                                   [n_groups x d_in x d_out] row-major, the type of x; FG_E4M3: [n_groups x d_out x d_in], each matrix
+ *                                       transposed, with w_scale [n_groups x d_out], as fg_quantize_rows makes them of the transposed matrices
+ *   bias [n_groups x d_out]             float, or NULL;  relu != 0: act = ReLU
+ *   h_out, n_out, out_stride            rows of out_dtype (FG_F32, FG_F16 or FG_BF16; FG_F32 for FG_F32 rows) by position
+ * Products: fp32 rows as in fg_linear (from exact three-way bf16 splits, fp32 sums; same input domain); the narrower types are multiplied
+ * as they are. Sums in fp32, one rounding to out_dtype. d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types);
+ * x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
+ * [0, x_rows) are skipped.
+ */
+fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const float* x_scale, const int32_t* src_ids_dev,
+                              const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                              int32_t d_out, const void* W, const float* w_scale, const float* bias, int32_t relu, void* h_out, int64_t n_out,
+                              int64_t out_stride, fg_dtype_t out_dtype, void* stream);
+
+/*
+ * The gradients of fg_linear_grouped:
+ *   dz[k, :] = dh[r, :] * (h[r, :] > 0), r = order[k]     (h = the layer's output; NULL = no activation)
+ *   dx[r, :] = dz[k, :] . W[g]^T                           (by position; with src_ids that of the row the position took)
+ *   dW[g] = sum over the group's k of x[s, :]^T . dz[k, :]  ([n_groups x d_in x d_out] float; zeros for a group without rows)
+ *   db[g, :] = sum over the group's k of dz[k, :]           ([n_groups x d_out] float)
+ *   x, W, dtype, src_ids, order, offsets   as in the forward call (not FG_E4M3); x, dW, db and dx, W may be NULL where the result is not wanted
+ *   dh, dh_stride, dh_dtype             dL/dh by position, n rows of d_out values, FG_F32 or `dtype`; fp32 gradients of 16-bit rows are
+ *                                       rounded to `dtype` after the mask, as in fg_layer_backward_bf16 (db sums the unrounded ones)
+ *   h, h_stride                         rows of `dtype` by position
+ *   dx, dx_stride, dx_dtype             FG_F32 or `dtype`
+ *   ws_dev, ws_bytes                    >= fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned
+ * An entry that the forward call skips has no part in any of the sums and gets no dx. fp32 sums within at most 4096 rows, fp64 across them;
+ * no atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out * sizeof(dtype) a multiple of 16.
+ */
+size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out);
+fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev, const void* dh,
+                                       int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, int64_t n, const int32_t* order_dev,
+                                       const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out, const void* W,
+                                       void* dx, int64_t dx_stride, fg_dtype_t dx_dtype, float* dw_dev, float* db_dev, void* ws_dev,
+                                       size_t ws_bytes, void* stream);
+
+/*
+ * Dropout. Element (r, c), r the position, c the column, is kept or not by (key, r, c) alone, so the mask is computed again wherever it is
+ * needed and never stored: draw c % 4 (16 bits, the lowest first) of w(w(mix(key), r), c / 4), with w and mix as in fg_sample_block, is at
+ * least T = floor(p * 65536 + 1/2). A kept element is multiplied by 65536 / (65536 - T), one that is not becomes 0 whatever it was.
+ *   out[r, :] = dropout(x[r, :]),  r = rows[k], k < *n_rows_dev       (rows NULL: r = k)
+ *   x, x_stride, dtype                  n rows of d values by position, FG_F32, FG_F16 or FG_BF16; out the same type; out may be x
+ *   p in [0, 1]                         resolved to multiples of 2^-16; p = 1 drops everything
+ * The gradient of the call is the same call on the gradient. Any d; pointers and strides aligned to the element.
+ */
+fg_status_t fg_dropout(const void* x, int64_t x_stride, fg_dtype_t dtype, const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows,
+                       int64_t n, int32_t d, float p, uint64_t key, void* out, int64_t out_stride, void* stream);
+
+/*
+ * Residual sum and root-mean-square norm between two layers, for the positions listed (r = rows[k]; rows NULL: r = k):
+ *   s = residual[r, :] + dropout(x[r, :])                  (residual NULL: s = dropout(x); p and key as in fg_dropout; p = 0: none)
+ *   rstd[r] = 1 / sqrt(mean(s^2) + eps)
+ *   y[r, :] = s * rstd[r] * weight                         (weight [d] float, or NULL: ones)
+ *   sum_out[r, :] = s
+ *   x, dtype                            n rows of d values by position, FG_F32, FG_F16 or FG_BF16
+ *   residual, sum_out, sum_dtype        n rows each, `dtype` or FG_F32; either may be NULL; sum_out may be residual
+ *   y, y_dtype                          `dtype`, FG_F32, or FG_E4M3 with y_scale [n] (else NULL): with a = the largest |y| of the row, at least
+ *                                       2^-100, y_scale[r] = a / 448 and the 8-bit values are y * (448 * (1 / a)), every step in fp32, rounded to nearest even. A NaN becomes a
+ *                                       NaN; a row with an infinity has an infinite scale, its values are NaN.
+ *   rstd_out [n]                        float, or NULL
+ * s is formed in fp32 and rounded once into sum_out; norm and y are those of the unrounded s. The sum of squares is carried in fp64. d up to
+ * FG_MAX_NORM_DIM; pointers and strides aligned to the element. At most 16 bytes at a time are read wherever a row begins.
+ */
+#define FG_MAX_NORM_DIM 16384
+fg_status_t fg_residual_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, const void* residual, int64_t residual_stride, fg_dtype_t sum_dtype,
+                             const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows, int64_t n, int32_t d, float p, uint64_t key,
+                             const float* weight, float eps, void* sum_out, int64_t sum_stride, void* y, int64_t y_stride, fg_dtype_t y_dtype,
+                             float* y_scale, float* rstd_out, void* stream);
+
+/*
+ * The gradients of fg_residual_norm, from dy and, for what the sum itself went on to, dsum_in:
+ *   t = dy[r, :] * weight,  xh = sum[r, :] * rstd[r]
+ *   dsum_out[r, :] = dsum_in[r, :] + rstd[r] * (t - xh * mean(t * xh))     (dsum_in NULL: nothing added): the gradient of the residual
+ *   dx[r, :] = dropout(dsum_out[r, :] before its rounding)                 (the forward call's p and key; NULL: not wanted, as where p = 0)
+ *   dw = sum over the listed rows of dy[r, :] * xh                         ([d] float; NULL: not wanted)
+ *   dy, dsum_in, dsum_out, dx, grad_dtype   n rows of d values by position, FG_F32, FG_F16 or FG_BF16; dsum_out may be dsum_in or dy, dx may be dy
+ *   sum, sum_dtype                      the forward call's sum_out, FG_F32, FG_F16 or FG_BF16;  rstd [n] its rstd_out
+ *   ws_dev, ws_bytes                    >= fg_residual_norm_backward_workspace_bytes(max_rows, d), 16-byte aligned (not needed without dw)
+ * mean(t * xh) in fp64, dw in fp32 within and fp64 across groups of rows; no atomics, results do not depend on scheduling.
+ */
+size_t fg_residual_norm_backward_workspace_bytes(int64_t max_rows, int32_t d);
+fg_status_t fg_residual_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* sum, int64_t sum_stride,
+                                      fg_dtype_t sum_dtype, const float* rstd, const float* weight, const void* dsum_in, int64_t dsum_in_stride,
+                                      const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows, int64_t n, int32_t d, float p,
+                                      uint64_t key, void* dsum_out, int64_t dsum_stride, void* dx, int64_t dx_stride, float* dw_dev, void* ws_dev,
+                                      size_t ws_bytes, void* stream);
+
+/*
+ * Rows in 8 bits with a scale each, as fg_residual_norm writes y: q[i, :] = e4m3(x[i, :] * (448 * (1 / a))), scale[i] = a / 448, i < n_rows. For weights: the
+ * rows of all transposed matrices in one call. x FG_F32, FG_F16 or FG_BF16; d up to FG_MAX_NORM_DIM; pointers and strides aligned to the element.
+ */
+fg_status_t fg_quantize_rows(const void* x, int64_t x_stride, fg_dtype_t dtype, int64_t n_rows, int32_t d, void* q, int64_t q_stride, float* scale,
+                             void* stream);
 
 /*
  * ---- One iteration in one call ----

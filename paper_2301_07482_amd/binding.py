@@ -11,10 +11,11 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfreshgnn.so")
 
 FG_OK, FG_ERR_INVALID_ARG, FG_ERR_SHAPE, FG_ERR_DTYPE, FG_ERR_STATE, FG_ERR_OOM, FG_ERR_HIP = range(7)
-FG_F32, FG_F16, FG_BF16 = 0, 1, 2
+FG_F32, FG_F16, FG_BF16, FG_E4M3 = 0, 1, 2, 3
 FG_WS_LOOKUP_PRUNE, FG_WS_CACHE_UPDATE, FG_WS_EXPORT = 0, 1, 2
 FG_TABLE_HBM_STREAMED, FG_TABLE_HOST_MAPPED, FG_TABLE_HBM_REUSED = 0, 1, 2
-DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2}
+DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2, FG_E4M3: 1}
+FG_MAX_GROUPS, FG_MAX_NORM_DIM = 1024, 16384
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2301_07482_amd.build` (needs hipcc); "
@@ -84,6 +85,19 @@ SIGNATURES = {
     "fg_layer_backward_weights_bf16_workspace_bytes": (_sz, [_i64, _i32, _i32]),
     "fg_layer_backward_weights_bf16": (_i32, [_p, _i32, _i64, _i32, _p, _i64, _p, _i64, _p, _i64, _i32, _p, _p, _i64, _i32, _i32, _p, _p,
                                               _p, _sz, _p]),
+    "fg_group_rows_workspace_bytes": (_sz, [_i64, _i32]),
+    "fg_group_rows": (_i32, [_p, _i64, _p, _i64, _p, _p, _i64, _i32, _p, _p, _p, _sz, _p]),
+    "fg_linear_grouped": (_i32, [_p, _i64, _i64, _i32, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _i32, _p, _i64, _i64, _i32, _p]),
+    "fg_linear_grouped_backward_workspace_bytes": (_sz, [_i32, _i64, _i32, _i32, _i32]),
+    "fg_linear_grouped_backward": (_i32, [_p, _i64, _i64, _i32, _p, _p, _i64, _i32, _p, _i64, _i64, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _i64,
+                                          _i32, _p, _p, _p, _sz, _p]),
+    "fg_dropout": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _i64, _p]),
+    "fg_residual_norm": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _f, _p, _i64, _p, _i64, _i32, _p, _p,
+                                _p]),
+    "fg_residual_norm_backward_workspace_bytes": (_sz, [_i64, _i32]),
+    "fg_residual_norm_backward": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _p, _i64, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _i64, _p,
+                                         _i64, _p, _p, _sz, _p]),
+    "fg_quantize_rows": (_i32, [_p, _i64, _i32, _i64, _i32, _p, _i64, _p, _p]),
 }
 
 
@@ -491,6 +505,57 @@ def fg_backward_weights_all_workspace_bytes(compute_dtype, layers):
 
 def fg_backward_weights_all(compute_dtype, layers, ws, ws_bytes, stream=None):
     _check(_lib.fg_backward_weights_all(compute_dtype, len(layers), layers, ptr(ws), ws_bytes, stream))
+
+
+def fg_group_rows_workspace_bytes(max_rows, n_groups):
+    return int(_lib.fg_group_rows_workspace_bytes(max_rows, n_groups))
+
+
+def fg_group_rows(groups, n_table, ids, n_positions, rows, n_rows, max_rows, n_groups, order, offsets, ws, ws_bytes, stream=None):
+    _check(_lib.fg_group_rows(ptr(groups), n_table, ptr(ids), n_positions, ptr(rows), ptr(n_rows), max_rows, n_groups, ptr(order), ptr(offsets),
+                              ptr(ws), ws_bytes, stream))
+
+
+def fg_linear_grouped(x, x_rows, x_stride, dtype, x_scale, src_ids, order, offsets, max_rows, n_groups, d_in, d_out, W, w_scale, bias, relu, h_out,
+                      n_out, out_stride, out_dtype, stream=None):
+    _check(_lib.fg_linear_grouped(ptr(x), x_rows, x_stride, dtype, ptr(x_scale), ptr(src_ids), ptr(order), ptr(offsets), max_rows, n_groups, d_in,
+                                  d_out, ptr(W), ptr(w_scale), ptr(bias), relu, ptr(h_out), n_out, out_stride, out_dtype, stream))
+
+
+def fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out):
+    return int(_lib.fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out))
+
+
+def fg_linear_grouped_backward(x, x_rows, x_stride, dtype, src_ids, dh, dh_stride, dh_dtype, h, h_stride, n, order, offsets, max_rows, n_groups,
+                               d_in, d_out, W, dx, dx_stride, dx_dtype, dw, db, ws, ws_bytes, stream=None):
+    _check(_lib.fg_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(h), h_stride, n,
+                                           ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), ptr(dx), dx_stride, dx_dtype, ptr(dw),
+                                           ptr(db), ptr(ws), ws_bytes, stream))
+
+
+def fg_dropout(x, x_stride, dtype, rows, n_rows, max_rows, n, d, p, key, out, out_stride, stream=None):
+    _check(_lib.fg_dropout(ptr(x), x_stride, dtype, ptr(rows), ptr(n_rows), max_rows, n, d, p, key, ptr(out), out_stride, stream))
+
+
+def fg_residual_norm(x, x_stride, dtype, residual, residual_stride, sum_dtype, rows, n_rows, max_rows, n, d, p, key, weight, eps, sum_out, sum_stride,
+                     y, y_stride, y_dtype, y_scale, rstd_out, stream=None):
+    _check(_lib.fg_residual_norm(ptr(x), x_stride, dtype, ptr(residual), residual_stride, sum_dtype, ptr(rows), ptr(n_rows), max_rows, n, d, p, key,
+                                 ptr(weight), eps, ptr(sum_out), sum_stride, ptr(y), y_stride, y_dtype, ptr(y_scale), ptr(rstd_out), stream))
+
+
+def fg_residual_norm_backward_workspace_bytes(max_rows, d):
+    return int(_lib.fg_residual_norm_backward_workspace_bytes(max_rows, d))
+
+
+def fg_residual_norm_backward(dy, dy_stride, grad_dtype, sum_, sum_stride, sum_dtype, rstd, weight, dsum_in, dsum_in_stride, rows, n_rows, max_rows, n,
+                              d, p, key, dsum_out, dsum_stride, dx, dx_stride, dw, ws, ws_bytes, stream=None):
+    _check(_lib.fg_residual_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(sum_), sum_stride, sum_dtype, ptr(rstd), ptr(weight), ptr(dsum_in),
+                                          dsum_in_stride, ptr(rows), ptr(n_rows), max_rows, n, d, p, key, ptr(dsum_out), dsum_stride, ptr(dx),
+                                          dx_stride, ptr(dw), ptr(ws), ws_bytes, stream))
+
+
+def fg_quantize_rows(x, x_stride, dtype, n_rows, d, q, q_stride, scale, stream=None):
+    _check(_lib.fg_quantize_rows(ptr(x), x_stride, dtype, n_rows, d, ptr(q), q_stride, ptr(scale), stream))
 
 
 _POINTER_FIELDS = {}

@@ -101,6 +101,14 @@ static inline int fg_dtype_size(fg_dtype_t t) { return t == FG_F32 ? 4 : (t == F
 
 constexpr int FG_SCAN_BLOCK = 1024;  // elements (= threads) per block in the compaction kernels
 
+// The counter-based generator of this library: the SplitMix64 output function, and word `counter` of the stream `key`.
+__host__ __device__ inline uint64_t fg_mix64(uint64_t x) {
+    x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
+    x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+    return x ^ (x >> 31);
+}
+__host__ __device__ inline uint64_t fg_word64(uint64_t key, uint64_t counter) { return fg_mix64(key + (counter + 1ull) * 0x9E3779B97F4A7C15ull); }
+
 static inline int64_t fg_ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static inline size_t fg_align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -42,15 +42,6 @@ constexpr uint32_t SMP_LINE = 8;                        // entries of the table 
 constexpr uint32_t SMP_LOST = 0x80000000u;              // in `entry`: the slot's node was there with a smaller number
 constexpr int SMP_DRAW_THREADS = 256;                   // small workgroups: one that has finished makes room at once
 
-__host__ __device__ inline uint64_t smp_mix(uint64_t x) {
-    x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
-    x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
-    return x ^ (x >> 31);
-}
-__host__ __device__ inline uint64_t smp_word(uint64_t key, uint64_t counter) {
-    return smp_mix(key + (counter + 1ull) * 0x9E3779B97F4A7C15ull);
-}
-
 struct SmpArgs {
     const int64_t* indptr;
     const int32_t* indices;
@@ -143,8 +134,8 @@ __device__ __forceinline__ uint32_t smp_insert(const SmpArgs& A, int32_t node, u
 
 // Where in a row of d entries the draws of node v start: the common turn of its strata and the word its draws are derived from.
 __device__ __forceinline__ void smp_row(const SmpArgs& A, int32_t v, int64_t d, uint64_t& word, int64_t& turn) {
-    word = smp_word(A.key_l, (uint64_t)v);
-    const double u = (double)(smp_word(word, (uint64_t)A.fanout) >> 11) * (1.0 / 9007199254740992.0);
+    word = fg_word64(A.key_l, (uint64_t)v);
+    const double u = (double)(fg_word64(word, (uint64_t)A.fanout) >> 11) * (1.0 / 9007199254740992.0);
     turn = (int64_t)(u * (double)d);
     if (turn > d - 1) turn = d - 1;
 }
@@ -155,7 +146,7 @@ __device__ __forceinline__ int32_t smp_draw(const SmpArgs& A, int32_t v, int64_t
     if (j >= f || j >= d) return -1;
     int64_t slot = j;
     if (d > f) {
-        const double u = (double)(smp_word(word, (uint64_t)j) >> 11) * (1.0 / 9007199254740992.0);
+        const double u = (double)(fg_word64(word, (uint64_t)j) >> 11) * (1.0 / 9007199254740992.0);
         if (d < (1 << 26)) {      // in 32 bits: (j + 1) * d is below 2^31
             const uint32_t a = (uint32_t)j * (uint32_t)d, first = a / (uint32_t)f, width = (a + (uint32_t)d) / (uint32_t)f - first;
             uint32_t inside = (uint32_t)(u * (double)width);
@@ -1151,7 +1142,7 @@ fg_status_t smp_launch(const char* who, const int64_t* indptr, const int32_t* in
             A.rows_per = smp_slots(y.max_rows, y.fanout) * SMP_THREADS / y.fanout;
             A.draw_blocks = (int32_t)fg_ceil_div(y.max_rows, SMP_DRAW_THREADS / y.fanout);
             A.own_blocks = (int32_t)fg_ceil_div(y.max_rows, SMP_DRAW_THREADS);
-            A.key_l = smp_word(smp_mix(key), (uint64_t)y.layer);
+            A.key_l = fg_word64(fg_mix64(key), (uint64_t)y.layer);
             A.row_start = y.row_start_dev;
             A.row_end = y.row_end_dev;
             A.col = y.col_dev;
