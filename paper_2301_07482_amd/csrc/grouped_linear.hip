@@ -72,6 +72,8 @@ __device__ __forceinline__ void put_value(int type, char* p, int64_t i, float v)
 }
 __device__ __forceinline__ float rounded(int type, float v) { return type == FG_F32 ? v : type == FG_BF16 ? (float)(__bf16)v : (float)(_Float16)v; }
 
+enum { GL_A_SOURCE = 0, GL_A_POSITION = 1, GL_A_ENTRY = 2 };      // rows of the left operand: by x row, by position, packed in entry order
+
 struct GlArgs {
     Groups G;
     const char *x, *W, *h, *dh;
@@ -81,6 +83,10 @@ struct GlArgs {
     const int32_t* src_ids;
     char* out;
     float *dw, *db;
+    // the matrix core kernels: out[r, 0:N] = a[., 0:K] . B, K and N whichever way round the call has them
+    const char* a;
+    int64_t a_stride;
+    int a_by, K, N;
 };
 // position and row of x of entry k; -1: skipped
 __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, int32_t& r, int32_t& s) {
@@ -184,6 +190,282 @@ __global__ __launch_bounds__(GL_THREADS) void grouped_weights_kernel(GlArgs A) {
     if (A.db && m0 == 0 && t < GL_TILE && n0 + t < A.d_out) A.db[(int64_t)g * A.d_out + n0 + t] = (float)sum;
 }
 
+// ---- 16- and 8-bit products on the matrix cores ----
+//
+// A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 128 bytes of a row (64 halfwords, 128 bytes of 8 bits). The
+// operands of a step go from memory straight to LDS (global_load_lds, 16 bytes a lane): two buffers, step s + 2 sets out when step s
+// has been multiplied, so a load has a whole step of arithmetic to arrive in. A lane's place in LDS is fixed by the instruction (base + 16
+// bytes per lane), so the exchange of 16-byte pieces that keeps the operand reads off each other's banks is made on the side of memory: piece c
+// of LDS row m holds piece c ^ (m & 7) of the row. B is either read the same way (rows of W along K: gradients, 8 bits), or its rows are k and
+// transposed on the way out of LDS (ds_read_b64_tr_b16), with the 64-byte windows of a row exchanged so that the four rows a read takes a
+// window of lie in different banks.
+// Every lane's address is valid: a row or column that does not exist reads the first one there is (its products go to outputs that are
+// not stored), pieces beyond K are read from 16 bytes of zeros, both operands'.
+//
+// The waits are counted by hand: the compiler knows nothing of these loads (it would wait for all of them before every LDS read).
+__device__ __attribute__((aligned(16))) unsigned int gl_zero[4];
+
+typedef float gl_f32x16 __attribute__((ext_vector_type(16)));
+typedef int gl_i32x8 __attribute__((ext_vector_type(8)));
+typedef short gl_s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void load_to_lds(const char* from, unsigned int lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+// all loads but the N youngest have arrived, in every wavefront
+template <int N>
+__device__ __forceinline__ void arrived() {
+    static_assert(N == 0 || N == 4 || N == 8, "");
+    if constexpr (N == 0)
+        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    else if constexpr (N == 4)
+        asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
+    else
+        asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
+}
+// every wavefront has read what it needs of the buffer
+__device__ __forceinline__ void read_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// 8-bit products. The 8-bit matrix instructions do not add up in fp32: they drop bits of products that are much smaller than the largest of
+// the same instruction (measured against exact sums: 1.3e-5 of the result's norm for normally distributed rows, 6e-5 for rows whose values
+// spread over e^2; the 64-deep and the 16-deep one alike). Beside the 2e-3 of an output in 16 bits that is nothing and they are twice as fast;
+// for an output in fp32 (WIDE) the operands become bf16, which holds every 8-bit value, and are multiplied as such: 3e-7.
+template <int T, bool WIDE>
+__device__ __forceinline__ gl_f32x16 mfma(const fg_u32x4* a, const fg_u32x4* b, gl_f32x16 c) {
+    if constexpr (T == FG_BF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
+    else if constexpr (T == FG_F16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(fg_f16x8, a[0]), __builtin_bit_cast(fg_f16x8, b[0]), c, 0, 0, 0);
+    else if constexpr (WIDE) {
+        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[1]), __builtin_bit_cast(fg_bf16x8, b[1]), c, 0, 0, 0);
+    } else {      // (the block scales of the instruction are 2^0)
+        const gl_i32x8 av = {(int)a[0][0], (int)a[0][1], (int)a[0][2], (int)a[0][3], (int)a[1][0], (int)a[1][1], (int)a[1][2], (int)a[1][3]};
+        const gl_i32x8 bv = {(int)b[0][0], (int)b[0][1], (int)b[0][2], (int)b[0][3], (int)b[1][0], (int)b[1][1], (int)b[1][2], (int)b[1][3]};
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
+    }
+}
+// sixteen 8-bit values as twice eight bf16
+__device__ __forceinline__ void widen(fg_u32x4 v, fg_u32x4 (&out)[2]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        out[i / 2][(i & 1) * 2] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.f, false));
+        out[i / 2][(i & 1) * 2 + 1] = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[i], 1.f, true));
+    }
+}
+
+constexpr int GL_STEP = 128;      // bytes of K per step
+constexpr size_t gl_lds_bytes(int bm, int bn, int waves) {
+    return (size_t)2 * (bm + bn) * GL_STEP + (size_t)bm * 8;      // (the epilogue's blocks, 32 rows of a wavefront's columns in fp32, fit in the operands' space)
+}
+
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN, bool WIDE>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
+    constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
+    constexpr int E = T == FG_E4M3 ? 1 : 2, BK = GL_STEP / E;
+    constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / 8 / WAVES, B_LOADS = BN / 8 / WAVES, LOADS = A_LOADS + B_LOADS;
+    constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
+    constexpr int DEEP = T == FG_E4M3 && !WIDE ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
+    constexpr int PARTS = T == FG_E4M3 ? 2 : 1;                                          // 16-byte registers of it
+    constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
+    static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
+    static_assert(A_LOADS * 8 * WAVES == BM && B_LOADS * 8 * WAVES == BN, "whole loads");
+    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
+    int32_t *pos = (int32_t*)(gl_lds + 2 * STAGE), *src = pos + BM;
+
+    // the column tiles of a row tile lie on one XCD (workgroup ids are dealt round-robin to the eight of them): the rows come from memory once
+    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
+    int g;
+    int64_t k0, k1;
+    if (!find_tile(A.G, (int64_t)(j / A.tiles_n) * 8 + xcd, BM, g, k0, k1)) return;
+    const int n0 = (j % A.tiles_n) * BN;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int K = A.K, N = A.N;
+    for (int m = t; m < BM; m += THREADS) {
+        int32_t r, s;
+        entry(A, k0 + m, k1, r, s);
+        pos[m] = r;
+        src[m] = r < 0 ? -1 : (A.a_by == GL_A_SOURCE ? s : A.a_by == GL_A_POSITION ? r : (int32_t)(k0 + m));
+    }
+    __syncthreads();
+
+    // this lane's loads of a step: rows 8 (wave + WAVES i) + lane / 8 of A (and of B along K), piece lane % 8 exchanged
+    const char* pa[A_LOADS];
+    const char* pb[B_LOADS];
+    int kb[B_LOADS];      // first element of K (of the step) that a load of B holds; B_KN: its row
+    const int a_piece = (lane & 7) ^ (lane >> 3);      // row & 7 is lane / 8
+    const int ka = a_piece * (16 / E);
+    const char* const zero = (const char*)gl_zero;
+#pragma unroll
+    for (int i = 0; i < A_LOADS; ++i) {
+        const int32_t r = src[8 * (wave + WAVES * i) + (lane >> 3)];
+        pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + a_piece * 16;
+    }
+    auto b_window = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };      // what a row's windows are exchanged by (BN = 64: it has two)
+    const char* w0 = A.W + (int64_t)g * K * N * E;
+#pragma unroll
+    for (int i = 0; i < B_LOADS; ++i) {
+        if constexpr (B_KN) {
+            const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
+            const int c = n0 + (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
+            kb[i] = row;
+            pb[i] = w0 + ((int64_t)row * N + (c < N ? c : 0)) * E;
+        } else {
+            const int c = n0 + 8 * (wave + WAVES * i) + (lane >> 3);
+            kb[i] = ka;
+            pb[i] = w0 + (int64_t)(c < N ? c : 0) * K * E + a_piece * 16;
+        }
+    }
+    const int64_t b_step = B_KN ? (int64_t)BK * N * E : GL_STEP;
+    const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
+    const int steps = (K + BK - 1) / BK;
+    auto load_step = [&](int s) {
+        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * STAGE + wave * 1024);
+        const int left = K - s * BK;      // elements of K that the step has
+        if (left >= BK) {
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) load_to_lds(pa[i], to + i * WAVES * 1024);
+#pragma unroll
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds(pb[i], to + BM * GL_STEP + i * WAVES * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) load_to_lds(ka < left ? pa[i] : zero, to + i * WAVES * 1024);
+#pragma unroll
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds(kb[i] < left ? pb[i] : zero, to + BM * GL_STEP + i * WAVES * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) pa[i] += GL_STEP;
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) pb[i] += b_step;
+    };
+
+    const int l32 = lane & 31, half = lane >> 5;
+    const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * WN;
+    gl_f32x16 acc[MB][NB];
+#pragma unroll
+    for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+    const int swap = (l32 & 7) << 4;
+    const int place = (lane >> 2) & 3;
+    const int b_in = (8 * half + place) * B_ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto multiply = [&](int s) {
+        const char* As = gl_lds + (s & 1) * STAGE + (wm + l32) * GL_STEP;
+        const char* Bs = gl_lds + (s & 1) * STAGE + BM * GL_STEP;
+#pragma unroll
+        for (int kk = 0; kk < SUB; ++kk) {
+            fg_u32x4 av[MB][PARTS], bv[NB][PARTS];
+#pragma unroll
+            for (int q = 0; q < DEEP; ++q) {
+                const int at = (((kk * DEEP + q) * 2 + half) << 4) ^ swap;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) av[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + at);
+                if constexpr (!B_KN)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) bv[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + at);
+            }
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) widen(av[mb][0], av[mb]);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) widen(bv[nb][0], bv[nb]);
+            }
+            if constexpr (B_KN)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+                    const char* from = Bs + kk * 16 * B_ROW + b_in + ((((wn >> 5) + nb) ^ b_window(place)) << 6);
+                    const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from);
+                    const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 4 * B_ROW));
+                    bv[nb][0] = __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(av[mb], bv[nb], acc[mb][nb]);
+        }
+    };
+
+    load_step(0);
+    if (steps > 1) load_step(1);
+    for (int s = 0; s < steps; ++s) {
+        if (s + 1 < steps)
+            arrived<LOADS>();
+        else
+            arrived<0>();
+        multiply(s);
+        read_done();
+        if (s + 2 < steps) load_step(s + 2);
+    }
+
+    // Epilogue: 32 rows of the wavefront's columns at a time through LDS (its own part: no barrier), so that the rows are written 16 bytes
+    // at a time. Accumulator element i of a block is its row 8 * (i / 4) + 4 * half + i % 4, column l32.
+    constexpr int LD = WN + 4;
+    static_assert(WAVES * 32 * LD * 4 <= 2 * STAGE, "the blocks fit in the operands' space");
+    float* blk = (float*)gl_lds + wave * 32 * LD;
+    constexpr int LPR = WN / 8, RPP = 64 / LPR;      // lanes per row (eight columns each), rows per pass
+    const int c0 = n0 + wn + (lane % LPR) * 8;
+    const bool c_in = c0 < N;                        // N is a multiple of 8
+    float bias[8], ws[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        bias[e] = A.bias && c_in ? A.bias[(int64_t)g * N + c0 + e] : 0.f;
+        ws[e] = T == FG_E4M3 && c_in ? A.w_scale[(int64_t)g * N + c0 + e] : 1.f;
+    }
+#pragma unroll
+    for (int mb = 0; mb < MB; ++mb) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) blk[(8 * (i >> 2) + 4 * half + (i & 3)) * LD + nb * 32 + l32] = acc[mb][nb][i];
+#pragma unroll
+        for (int p = 0; p < 32 / RPP; ++p) {
+            const int m = p * RPP + lane / LPR;
+            const int32_t r = pos[wm + mb * 32 + m];
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = blk[m * LD + (lane % LPR) * 8 + e];
+            if (r < 0 || !c_in) continue;
+            const float xs = T == FG_E4M3 ? A.x_scale[src[wm + mb * 32 + m]] : 1.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (T == FG_E4M3) v[e] *= xs * ws[e];
+                v[e] += bias[e];
+                if (A.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
+            }
+            char* to = A.out + (int64_t)r * A.out_stride;
+            if (A.out_type == FG_F32)
+                fg_store_piece<FG_F32>(to + (int64_t)c0 * 4, v, 8);
+            else if (A.out_type == FG_BF16)
+                fg_store_piece<FG_BF16>(to + (int64_t)c0 * 2, v, 8);
+            else
+                fg_store_piece<FG_F16>(to + (int64_t)c0 * 2, v, 8);
+        }
+    }
+}
+
+template <int T, int BM, int BN, int WM, int WN, bool B_KN, bool WIDE>
+fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
+    A.tiles_n = (int)fg_ceil_div(A.N, BN);
+    const int64_t row_tiles_ = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
+    const int64_t grid = fg_ceil_div(row_tiles_, 8) * 8 * A.tiles_n;
+    if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN, WIDE>), dim3((unsigned)grid), dim3(64 * WM * WN), gl_lds_bytes(BM, BN, WM * WN), st, A);
+    FG_LAUNCH_CHECK("grouped_tile_kernel");
+    return FG_OK;
+}
+// out[r, :] = a[., :] . B for the entries of every group (A.a, a_stride, a_by, K, N, W, out, ... are set)
+template <int T, bool B_KN, bool WIDE>
+fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
+    const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
+    if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, B_KN, WIDE>(who, A, st);
+    const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
+    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, B_KN, WIDE>(who, A, st);
+    return tile_launch<T, 64, 64, 2, 2, B_KN, WIDE>(who, A, st);
+}
+
 fg_status_t check_groups(const char* who, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out,
                          fg_dtype_t dtype, int64_t x_rows, int64_t n) {
     const int e = dtype == FG_E4M3 ? 1 : fg_dtype_size(dtype);
@@ -237,6 +519,11 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     A.x = (const char*)x, A.W = (const char*)W, A.x_rows = x_rows, A.x_stride = x_stride, A.n = n_out, A.out_stride = out_stride;
     A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu, A.tiles_n = (int)fg_ceil_div(d_out, GL_TILE);
     A.x_scale = x_scale, A.w_scale = w_scale, A.bias = bias, A.src_ids = src_ids_dev, A.out = (char*)h_out;
+    A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
+    if (dtype == FG_BF16) return tile_product<FG_BF16, true, false>(who, A, (hipStream_t)stream);
+    if (dtype == FG_F16) return tile_product<FG_F16, true, false>(who, A, (hipStream_t)stream);
+    if (dtype == FG_E4M3 && out_dtype == FG_F32) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
+    if (dtype == FG_E4M3) return tile_product<FG_E4M3, false, false>(who, A, (hipStream_t)stream);
     const int64_t grid = row_tiles(max_rows, n_groups, GL_TILE) * A.tiles_n;
     if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
     hipLaunchKernelGGL((grouped_linear_kernel<false>), dim3((unsigned)grid), dim3(GL_THREADS), 0, (hipStream_t)stream, A);
