@@ -87,6 +87,11 @@ struct GlArgs {
     const char* a;
     int64_t a_stride;
     int a_by, K, N;
+    // gradients: dz in entry order (or NULL: dh serves as it is) and its row stride, column sums by tile, parts of dW and who makes them
+    char* dz;
+    int64_t dz_stride;
+    float *db_part, *dw_part;
+    int shares, min_share;
 };
 // position and row of x of entry k; -1: skipped
 __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, int32_t& r, int32_t& s) {
@@ -466,6 +471,311 @@ fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
     return tile_launch<T, 64, 64, 2, 2, B_KN, WIDE>(who, A, st);
 }
 
+// ---- gradients of 16-bit rows ----
+//
+// dz in entry order, in the rows' type, and its column sums by tiles of GZ_ROWS entries of one group (db is their sum). What it costs,
+// reading dh and h and writing dz, both products save again: they read dz alone, in the order of the entries.
+constexpr int GZ_ROWS = 64, GZ_THREADS = 256;
+
+template <int T, int D>
+__global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
+    constexpr int E = T == FG_F32 ? 4 : 2, DE = D == FG_F32 ? 4 : 2;
+    __shared__ int32_t pos[GZ_ROWS];
+    __shared__ float sums[GZ_THREADS * 8];
+    int g;
+    int64_t k0, k1;
+    if (!find_tile(A.G, blockIdx.x, GZ_ROWS, g, k0, k1)) return;
+    const int t = threadIdx.x;
+    if (t < GZ_ROWS) {
+        int32_t s;
+        entry(A, k0 + t, k1, pos[t], s);
+    }
+    __syncthreads();
+    const int rows = (int)(k1 - k0), pieces = (A.d_out + 7) / 8;
+    int side = 1;      // rows side by side
+    while (side * 2 * pieces <= GZ_THREADS) side *= 2;
+    const int width = GZ_THREADS / side;      // threads of a row
+    for (int p0 = 0; p0 < pieces; p0 += width) {
+        const int p = p0 + t % width, c = p * 8;
+        float sum[8] = {};
+        if (p < pieces) {
+#pragma unroll 4
+            for (int m = t / width; m < rows; m += side) {
+                const int32_t r = pos[m];
+                float z[8] = {};
+                if (r >= 0) {
+                    fg_piece_values<D>(fg_load_piece<D>(A.dh + r * A.dh_stride + (int64_t)c * DE, A.d_out - c), z);
+                    if (A.h) {
+                        float h[8];
+                        fg_piece_values<T>(fg_load_piece<T>(A.h + r * A.h_stride + (int64_t)c * E, A.d_out - c), h);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = h[e] > 0.f ? z[e] : 0.f;
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += z[e];
+                if (A.dz) fg_store_piece<T>(A.dz + ((k0 + m) * A.d_out + c) * E, z, A.d_out - c);
+            }
+        }
+        if (A.db_part) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sums[t * 8 + e] = sum[e];
+            __syncthreads();
+            for (int i = t; i < width * 8; i += GZ_THREADS) {
+                float v = 0.f;
+                for (int q = 0; q < side; ++q) v += sums[q * width * 8 + i];
+                if (p0 * 8 + i < A.d_out) A.db_part[(int64_t)blockIdx.x * A.d_out + p0 * 8 + i] = v;
+            }
+        }
+    }
+}
+
+// db[g, c] = sum over the group's tiles, in fp64; 32 columns a workgroup
+__global__ __launch_bounds__(GZ_THREADS) void grouped_db_kernel(GlArgs A) {
+    __shared__ double red[GZ_THREADS];
+    const int blocks = (A.d_out + 31) / 32, g = blockIdx.x / blocks;
+    const int c = (blockIdx.x % blocks) * 32 + (threadIdx.x & 31);
+    int64_t first = 0;
+    for (int i = fg_lane(); i < g; i += 64) {
+        const int64_t from = group_offset(A.G, i), to = group_offset(A.G, i + 1);
+        first += to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
+    }
+    for (int off = 32; off > 0; off >>= 1) first += __shfl_xor(first, off, 64);
+    const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
+    const int64_t tiles = to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
+    double s = 0.0;
+    if (c < A.d_out)
+#pragma unroll 8
+        for (int64_t i = threadIdx.x >> 5; i < tiles; i += GZ_THREADS / 32) s += (double)A.db_part[(first + i) * A.d_out + c];
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 32 && c < A.d_out) {
+        for (int q = 1; q < GZ_THREADS / 32; ++q) s += red[threadIdx.x + 32 * q];
+        A.db[(int64_t)g * A.d_out + c] = (float)s;
+    }
+}
+
+// dW = x^T . dz of every group: a contraction over the group's rows, whose number the device alone knows, with BM x BN tiles of the result.
+// The work is a line of steps of GW_ROWS entries, group by group, tile by tile, and cut into equal shares for the workgroups there
+// are: all of them end together however the groups are sized. A workgroup writes a tile that lies wholly in its share, and leaves its
+// part of one that does not (the first and the last of its share) in a slot of its own; a second launch adds those up, in order.
+// Both operands have the contraction index in front, rows of x and of dz: they go to LDS as they lie and are transposed on the way out.
+constexpr int GW_ROWS = 64, GW_LIST = 4096;
+
+struct Share {
+    int64_t total, per;      // steps of all groups; of a workgroup
+};
+// steps of the groups before `upto` (lanes of a wavefront together)
+__device__ __forceinline__ int64_t steps_before(const Groups& G, int upto) {
+    int64_t n = 0;
+    for (int i = fg_lane(); i < upto; i += 64) {
+        const int64_t from = group_offset(G, i), to = group_offset(G, i + 1);
+        n += to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
+    }
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    return n;
+}
+__device__ __forceinline__ Share share_of(const GlArgs& A, int tiles) {
+    Share s;
+    s.total = steps_before(A.G, A.G.n_groups) * tiles;
+    s.per = (s.total + A.shares - 1) / A.shares;
+    if (s.per < A.min_share) s.per = A.min_share;
+    return s;
+}
+
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N>
+__global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(GlArgs A) {
+    constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
+    constexpr int STAGE = GW_ROWS * (BM + BN) * 2, A_LOADS = GW_ROWS * BM * 2 / 1024 / WAVES, B_LOADS = GW_ROWS * BN * 2 / 1024 / WAVES, LOADS = A_LOADS + B_LOADS;
+    constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32;
+    static_assert(BM == BN, "a lane's pieces of x and of dz lie in the same rows");
+    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
+    int32_t* list = (int32_t*)(gl_lds + 2 * STAGE);      // rows of x of the next entries, -1: skipped
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int tiles_m = (A.d_in + BM - 1) / BM, tiles_n = (A.d_out + BN - 1) / BN, tiles = tiles_m * tiles_n;
+    const Share S = share_of(A, tiles);
+    int64_t at = blockIdx.x * S.per;
+    const int64_t end = at + S.per < S.total ? at + S.per : S.total;
+    if (at >= end) return;
+
+    const int l32 = lane & 31, half = lane >> 5, place = (lane >> 2) & 3;
+    const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * (BN / WAVES_N);
+    constexpr int ROW = BM * 2, ROW_PIECES = ROW / 16;
+    const int in_row = (8 * half + place) * ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
+    const char* const zero = (const char*)gl_zero;
+
+    int g = 0;
+    int64_t before = 0;      // steps (times tiles) of the groups before g
+    while (at < end) {       // uniform over the workgroup
+        int64_t from, to, steps_g;
+        for (;; ++g) {
+            from = group_offset(A.G, g);
+            to = group_offset(A.G, g + 1);
+            steps_g = to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
+            if (at < before + steps_g * tiles) break;
+            before += steps_g * tiles;
+        }
+        const int tile = (int)((at - before) / steps_g);
+        const int64_t first = at - before - tile * steps_g;                   // step of the tile
+        const int64_t last = first + (end - at) < steps_g ? first + (end - at) : steps_g;
+        const int steps = (int)(last - first);
+        const int64_t k0 = from + first * GW_ROWS, k1 = from + last * GW_ROWS < to ? from + last * GW_ROWS : to;
+        const int m0 = (tile / tiles_n) * BM, n0 = (tile % tiles_n) * BN;
+
+        // this lane's pieces of a step: rows row[i], column pieces of the tile (a column that does not exist reads the first: not stored)
+        int64_t ca[A_LOADS], cb[B_LOADS];
+        int row[A_LOADS];
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int p = 64 * (wave + WAVES * i) + lane, slot = p % ROW_PIECES;
+            row[i] = p / ROW_PIECES;
+            const int c = (((slot >> 2) ^ (row[i] & 3)) * 4 + (slot & 3)) * 8;
+            ca[i] = (m0 + c < A.d_in ? m0 + c : 0) * 2;
+            cb[i] = (n0 + c < A.d_out ? n0 + c : 0) * 2;
+        }
+        auto fill = [&](int64_t k) {      // entries k .. k + GW_LIST
+            for (int i = t; i < GW_LIST; i += THREADS) {
+                int32_t r = -1, s = -1;
+                entry(A, k + i, k1, r, s);
+                list[i] = s;
+            }
+            __syncthreads();
+        };
+        auto load_step = [&](int s) {
+            const unsigned int dst = __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * STAGE + wave * 1024);
+            const int64_t k = k0 + (int64_t)s * GW_ROWS;
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) {
+                const int32_t x_row = list[(s * GW_ROWS) % GW_LIST + row[i]];
+                const int64_t z_row = A.dz ? k + row[i] : x_row;      // without dz: dh by position, which is the row of x
+                const char *pa = A.x + x_row * A.x_stride + ca[i], *pb = (A.dz ? A.dz : A.dh) + z_row * A.dz_stride + cb[i];
+                load_to_lds(x_row >= 0 ? pa : zero, dst + i * WAVES * 1024);
+                load_to_lds(x_row >= 0 ? pb : zero, dst + GW_ROWS * BM * 2 + i * WAVES * 1024);
+            }
+        };
+        gl_f32x16 acc[MB][NB];
+#pragma unroll
+        for (int a = 0; a < MB; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
+        auto fragment = [&](const char* p) -> fg_u32x4 {
+            typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+            const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
+            const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROW));
+            return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        auto multiply = [&](int s) {
+            const char* As = gl_lds + (s & 1) * STAGE + in_row;
+            const char* Bs = As + GW_ROWS * BM * 2;
+            fg_u32x4 av[2][MB], bv[2][NB];
+            auto read = [&](int kk, int set) {
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) av[set][mb] = fragment(As + kk * 16 * ROW + ((((wm >> 5) + mb) ^ place) << 6));
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) bv[set][nb] = fragment(Bs + kk * 16 * ROW + ((((wn >> 5) + nb) ^ place) << 6));
+            };
+            read(0, 0);
+#pragma unroll
+            for (int kk = 0; kk < GW_ROWS / 16; ++kk) {      // the next operands are on their way while these are multiplied
+                if (kk + 1 < GW_ROWS / 16) read(kk + 1, (kk + 1) & 1);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, false>(&av[kk & 1][mb], &bv[kk & 1][nb], acc[mb][nb]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+
+        fill(k0);
+        load_step(0);
+        if (steps > 1) load_step(1);
+        for (int s = 0; s < steps; ++s) {
+            if (s + 1 < steps)
+                arrived<LOADS>();
+            else
+                arrived<0>();
+            multiply(s);
+            read_done();
+            if (s + 2 < steps) {
+                if ((s + 2) % (GW_LIST / GW_ROWS) == 0) fill(k0 + (int64_t)(s + 2) * GW_ROWS);
+                load_step(s + 2);
+            }
+        }
+        // a whole tile is the result; a part goes to this workgroup's slot 0 (the tile began before the share) or 1
+        const bool whole = first == 0 && last == steps_g;
+        float* to_part = A.dw_part + (int64_t)(2 * blockIdx.x + (at == blockIdx.x * S.per ? 0 : 1)) * BM * BN;
+        float* to_dw = A.dw + (int64_t)g * A.d_in * A.d_out;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int m = wm + mb * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    const int c = wn + nb * 32 + l32;
+                    if (!whole)
+                        to_part[m * BN + c] = acc[mb][nb][i];
+                    else if (m0 + m < A.d_in && n0 + c < A.d_out)
+                        to_dw[(int64_t)(m0 + m) * A.d_out + n0 + c] = acc[mb][nb][i];
+                }
+            }
+        at += steps;
+        __syncthreads();      // the list may be filled again
+    }
+}
+
+// The tiles that several workgroups have parts of, and zeros for groups without rows: GW_PARTS workgroups a tile
+constexpr int GW_PARTS = 16;
+template <int BM, int BN>
+__global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
+    const int tiles_n = (A.d_out + BN - 1) / BN, tiles = (A.d_in + BM - 1) / BM * tiles_n;
+    const int part = blockIdx.x % GW_PARTS, unit = blockIdx.x / GW_PARTS, tile = unit % tiles, g = unit / tiles;
+    const Share S = share_of(A, tiles);
+    const int64_t before = steps_before(A.G, g) * tiles;
+    const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
+    const int64_t steps_g = to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
+    const int64_t t0 = before + tile * steps_g, t1 = t0 + steps_g;
+    const int64_t w0 = steps_g ? t0 / S.per : 0, w1 = steps_g ? (t1 - 1) / S.per : -1;
+    if (steps_g && w0 == w1) return;      // one workgroup has written it
+    const int m0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
+    for (int i = threadIdx.x * 4; i < BM * BN / GW_PARTS; i += GZ_THREADS * 4) {
+        const int e = part * (BM * BN / GW_PARTS) + i, m = m0 + e / BN, c = n0 + e % BN;
+        if (m >= A.d_in || c >= A.d_out) continue;      // d_out is a multiple of 4
+        double s[4] = {};
+        for (int64_t w = w0; w <= w1; ++w) {
+            const float4 v = *(const float4*)(A.dw_part + (2 * w + (t0 <= w * S.per ? 0 : 1)) * BM * BN + e);
+            s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
+        }
+        *(float4*)(A.dw + ((int64_t)g * A.d_in + m) * A.d_out + c) = float4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+    }
+}
+
+// The workspace of a backward call: dz, column sums by tile, parts of dW
+struct BwPlan {
+    bool dz;
+    int bm, shares;
+    size_t dz_bytes, db_bytes, dw_bytes;
+    size_t total() const { return dz_bytes + db_bytes + dw_bytes + 16; }
+};
+// (sized for the masked call, which needs dz, at every size: a workspace for max_rows serves fewer rows too)
+BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
+    BwPlan P;
+    P.dz = true;
+    P.bm = d_in > 128 || d_out > 128 ? 256 : 128;
+    const int64_t tiles = fg_ceil_div(d_in, P.bm) * fg_ceil_div(d_out, P.bm);
+    const int64_t steps = (max_rows / GW_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * tiles;
+    const int most = P.bm == 256 ? 256 : 512;      // as many as run at once
+    P.shares = steps < 1 ? 1 : (int)(steps < most ? steps : most);
+    P.dz_bytes = fg_align_up((size_t)max_rows * d_out * e, 256);
+    P.db_bytes = fg_align_up((size_t)(max_rows / GZ_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * d_out * 4, 256);
+    P.dw_bytes = (size_t)2 * P.shares * P.bm * P.bm * 4;
+    return P;
+}
+
 fg_status_t check_groups(const char* who, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out,
                          fg_dtype_t dtype, int64_t x_rows, int64_t n) {
     const int e = dtype == FG_E4M3 ? 1 : fg_dtype_size(dtype);
@@ -494,6 +804,50 @@ fg_status_t check_matrix(const char* who, const char* what, const void* p, int64
 
 // tiles of rows at most: every group may end in one that is partly filled
 int64_t row_tiles(int64_t max_rows, int n_groups, int size) { return max_rows / size + (n_groups < max_rows ? n_groups : max_rows); }
+
+template <int T>
+fg_status_t backward_16_of(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
+    const BwPlan P = bw_plan(A.G.max_rows, A.G.n_groups, A.d_in, A.d_out, 2);
+    char* ws = (char*)ws_dev;
+    const bool pack = A.h || A.dh_type != T || A.src_ids;      // otherwise dh, by position as x is, serves as it lies
+    A.dz = work && pack && (A.out || A.dw) ? ws : nullptr;
+    A.dz_stride = A.dz ? (int64_t)A.d_out * 2 : A.dh_stride;
+    A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
+    A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
+    if (A.dz || A.db_part) {
+        const unsigned grid = (unsigned)row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS);
+        if (A.dh_type == T)
+            hipLaunchKernelGGL((grouped_dz_kernel<T, T>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
+        else
+            hipLaunchKernelGGL((grouped_dz_kernel<T, FG_F32>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
+        FG_LAUNCH_CHECK("grouped_dz_kernel");
+    }
+    if (A.db) {
+        hipLaunchKernelGGL(grouped_db_kernel, dim3((unsigned)(A.G.n_groups * fg_ceil_div(A.d_out, 32))), dim3(GZ_THREADS), 0, st, A);
+        FG_LAUNCH_CHECK("grouped_db_kernel");
+    }
+    if (A.out && work) {
+        A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
+        FG_TRY((tile_product<T, false, false>(who, A, st)));
+    }
+    if (A.dw) {
+        A.shares = P.shares, A.min_share = 1;
+        const int64_t tiles = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * GW_PARTS;
+        if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
+        if (P.bm == 256) {
+            hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), dim3((unsigned)P.shares), dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
+            hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256>), dim3((unsigned)tiles), dim3(GZ_THREADS), 0, st, A);
+        } else {
+            hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), dim3((unsigned)P.shares), dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
+            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128>), dim3((unsigned)tiles), dim3(GZ_THREADS), 0, st, A);
+        }
+        FG_LAUNCH_CHECK("grouped_dw_kernel");
+    }
+    return FG_OK;
+}
+fg_status_t backward_16(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
+    return A.type == FG_BF16 ? backward_16_of<FG_BF16>(who, A, work, st, ws_dev) : backward_16_of<FG_F16>(who, A, work, st, ws_dev);
+}
 
 }  // namespace
 
@@ -533,7 +887,7 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
     if (!fg_dtype_size(dtype) || max_rows < 0 || max_rows > INT32_MAX || n_groups < 1 || n_groups > FG_MAX_GROUPS || d_in <= 0 || d_out <= 0) return 0;
-    return 16;
+    return bw_plan(max_rows, n_groups, d_in, d_out, fg_dtype_size(dtype)).total();
 }
 
 extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
@@ -567,6 +921,7 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.type = dtype, A.dh_type = dh_dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
     A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = dw_dev, A.db = db_dev;
     hipStream_t st = (hipStream_t)stream;
+    if (dtype != FG_F32) return backward_16(who, A, work, st, ws_dev);
     if (dx && work) {
         A.tiles_n = (int)fg_ceil_div(d_in, GL_TILE);
         const int64_t grid = row_tiles(max_rows, n_groups, GL_TILE) * A.tiles_n;
