@@ -7,9 +7,6 @@
 
 namespace {
 
-constexpr int GL_THREADS = 256;
-constexpr int GL_TILE = 64, GL_K = 16;
-
 struct Groups {
     const int32_t* order;      // NULL: position k itself
     const int64_t* offsets;
@@ -48,30 +45,6 @@ __device__ __forceinline__ bool find_tile(const Groups& G, int64_t tile, int siz
     return false;
 }
 
-template <int T>
-__device__ __forceinline__ float value_at(const char* p, int64_t i) {
-    if constexpr (T == FG_F32)
-        return ((const float*)p)[i];
-    else if constexpr (T == FG_BF16)
-        return __uint_as_float((unsigned int)((const unsigned short*)p)[i] << 16);
-    else if constexpr (T == FG_F16)
-        return (float)((const _Float16*)p)[i];
-    else
-        return __builtin_amdgcn_cvt_f32_fp8((int)((const unsigned char*)p)[i], 0);
-}
-__device__ __forceinline__ float value_of(int type, const char* p, int64_t i) {
-    return type == FG_F32 ? value_at<FG_F32>(p, i) : type == FG_BF16 ? value_at<FG_BF16>(p, i) : type == FG_F16 ? value_at<FG_F16>(p, i) : value_at<FG_E4M3>(p, i);
-}
-__device__ __forceinline__ void put_value(int type, char* p, int64_t i, float v) {
-    if (type == FG_F32)
-        ((float*)p)[i] = v;
-    else if (type == FG_BF16)
-        ((__bf16*)p)[i] = (__bf16)v;
-    else
-        ((_Float16*)p)[i] = (_Float16)v;
-}
-__device__ __forceinline__ float rounded(int type, float v) { return type == FG_F32 ? v : type == FG_BF16 ? (float)(__bf16)v : (float)(_Float16)v; }
-
 enum { GL_A_SOURCE = 0, GL_A_POSITION = 1, GL_A_ENTRY = 2 };      // rows of the left operand: by x row, by position, packed in entry order
 
 struct GlArgs {
@@ -102,99 +75,6 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
     if (r >= 0) s = A.src_ids ? A.src_ids[r] : r;
     if (s < 0 || s >= A.x_rows) r = s = -1;
 }
-__device__ __forceinline__ float dz_at(const GlArgs& A, int32_t r, int c, bool round) {
-    float v = value_of(A.dh_type, A.dh + r * A.dh_stride, c);
-    if (A.h && !(value_of(A.type, A.h + r * A.h_stride, c) > 0.f)) v = 0.f;
-    return round ? rounded(A.type, v) : v;
-}
-
-// BACK false: h_out; true: dx
-template <bool BACK>
-__global__ __launch_bounds__(GL_THREADS) void grouped_linear_kernel(GlArgs A) {
-    __shared__ float a[GL_K][GL_TILE + 4], b[GL_K][GL_TILE + 4];
-    __shared__ int32_t pos[GL_TILE], src[GL_TILE];
-    int g;
-    int64_t k0, k1;
-    if (!find_tile(A.G, blockIdx.x / A.tiles_n, GL_TILE, g, k0, k1)) return;
-    const int n0 = (int)(blockIdx.x % A.tiles_n) * GL_TILE;
-    const int K = BACK ? A.d_out : A.d_in, N = BACK ? A.d_in : A.d_out;
-    const int t = threadIdx.x;
-    if (t < GL_TILE) entry(A, k0 + t, k1, pos[t], src[t]);
-    __syncthreads();
-    const int64_t w0 = (int64_t)g * A.d_in * A.d_out;
-    float acc[4][4] = {};
-    const int tm = (t / 16) * 4, tn = (t % 16) * 4;
-    for (int kk = 0; kk < K; kk += GL_K) {
-        for (int i = t; i < GL_K * GL_TILE; i += GL_THREADS) {
-            const int m = i / GL_K, k = kk + i % GL_K;
-            float v = 0.f;
-            if (pos[m] >= 0 && k < K) v = BACK ? dz_at(A, pos[m], k, true) : value_of(A.type, A.x + src[m] * A.x_stride, k);
-            a[i % GL_K][m] = v;
-            const int c = n0 + m;
-            const bool by_column = BACK || A.type == FG_E4M3;      // W has the contraction index behind
-            b[i % GL_K][m] = c < N && k < K ? value_of(A.type, A.W, w0 + (by_column ? (int64_t)c * K + k : (int64_t)k * N + c)) : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < GL_K; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += a[k][tm + i] * b[k][tn + j];
-        __syncthreads();
-    }
-    for (int i = 0; i < 4; ++i) {
-        const int32_t r = pos[tm + i];
-        if (r < 0) continue;
-        for (int j = 0; j < 4; ++j) {
-            const int c = n0 + tn + j;
-            if (c >= N) continue;
-            float v = acc[i][j];
-            if (!BACK) {
-                if (A.x_scale) v *= A.x_scale[src[tm + i]] * A.w_scale[(int64_t)g * A.d_out + c];
-                if (A.bias) v += A.bias[(int64_t)g * A.d_out + c];
-                if (A.relu) v = v < 0.f ? 0.f : v;
-            }
-            put_value(A.out_type, A.out + r * A.out_stride, c, v);
-        }
-    }
-}
-
-// dW and db: a workgroup per group and tile of dW
-__global__ __launch_bounds__(GL_THREADS) void grouped_weights_kernel(GlArgs A) {
-    __shared__ float a[GL_K][GL_TILE + 4], b[GL_K][GL_TILE + 4], bz[GL_K][GL_TILE + 4];
-    const int tiles_m = (A.d_in + GL_TILE - 1) / GL_TILE;
-    const int g = blockIdx.x / (tiles_m * A.tiles_n), tile = blockIdx.x % (tiles_m * A.tiles_n);
-    const int m0 = tile / A.tiles_n * GL_TILE, n0 = tile % A.tiles_n * GL_TILE;
-    const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
-    const int t = threadIdx.x, tm = (t / 16) * 4, tn = (t % 16) * 4;
-    double acc[4][4] = {}, sum = 0.0;
-    for (int64_t kk = from; kk < to; kk += GL_K) {
-        for (int i = t; i < GL_K * GL_TILE; i += GL_THREADS) {
-            const int k = i / GL_TILE, c = i % GL_TILE;
-            int32_t r, s;
-            entry(A, kk + k, to, r, s);
-            a[k][c] = r >= 0 && m0 + c < A.d_in && A.dw ? value_of(A.type, A.x + s * A.x_stride, m0 + c) : 0.f;
-            b[k][c] = r >= 0 && n0 + c < A.d_out ? dz_at(A, r, n0 + c, true) : 0.f;
-            bz[k][c] = r >= 0 && n0 + c < A.d_out ? dz_at(A, r, n0 + c, false) : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < GL_K; ++k)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] += (double)a[k][tm + i] * (double)b[k][tn + j];
-        if (t < GL_TILE)
-            for (int k = 0; k < GL_K; ++k) sum += (double)bz[k][t];
-        __syncthreads();
-    }
-    if (A.dw)
-        for (int i = 0; i < 4; ++i)
-            for (int j = 0; j < 4; ++j)
-                if (m0 + tm + i < A.d_in && n0 + tn + j < A.d_out)
-                    A.dw[((int64_t)g * A.d_in + m0 + tm + i) * A.d_out + n0 + tn + j] = (float)acc[i][j];
-    if (A.db && m0 == 0 && t < GL_TILE && n0 + t < A.d_out) A.db[(int64_t)g * A.d_out + n0 + t] = (float)sum;
-}
-
 // ---- 16- and 8-bit products on the matrix cores ----
 //
 // A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 128 bytes of a row (64 halfwords, 128 bytes of 8 bits). The
@@ -567,18 +447,18 @@ struct Share {
     int64_t total, per;      // steps of all groups; of a workgroup
 };
 // steps of the groups before `upto` (lanes of a wavefront together)
-__device__ __forceinline__ int64_t steps_before(const Groups& G, int upto) {
+__device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int rows) {
     int64_t n = 0;
     for (int i = fg_lane(); i < upto; i += 64) {
         const int64_t from = group_offset(G, i), to = group_offset(G, i + 1);
-        n += to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
+        n += to > from ? (to - from + rows - 1) / rows : 0;
     }
     for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
     return n;
 }
-__device__ __forceinline__ Share share_of(const GlArgs& A, int tiles) {
+__device__ __forceinline__ Share share_of(const GlArgs& A, int tiles, int rows) {
     Share s;
-    s.total = steps_before(A.G, A.G.n_groups) * tiles;
+    s.total = steps_before(A.G, A.G.n_groups, rows) * tiles;
     s.per = (s.total + A.shares - 1) / A.shares;
     if (s.per < A.min_share) s.per = A.min_share;
     return s;
@@ -594,7 +474,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
     int32_t* list = (int32_t*)(gl_lds + 2 * STAGE);      // rows of x of the next entries, -1: skipped
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int tiles_m = (A.d_in + BM - 1) / BM, tiles_n = (A.d_out + BN - 1) / BN, tiles = tiles_m * tiles_n;
-    const Share S = share_of(A, tiles);
+    const Share S = share_of(A, tiles, GW_ROWS);
     int64_t at = blockIdx.x * S.per;
     const int64_t end = at + S.per < S.total ? at + S.per : S.total;
     if (at >= end) return;
@@ -636,6 +516,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
             cb[i] = (n0 + c < A.d_out ? n0 + c : 0) * 2;
         }
         auto fill = [&](int64_t k) {      // entries k .. k + GW_LIST
+#pragma unroll 2
             for (int i = t; i < GW_LIST; i += THREADS) {
                 int32_t r = -1, s = -1;
                 entry(A, k + i, k1, r, s);
@@ -709,14 +590,16 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
         const bool whole = first == 0 && last == steps_g;
         float* to_part = A.dw_part + (int64_t)(2 * blockIdx.x + (at == blockIdx.x * S.per ? 0 : 1)) * BM * BN;
         float* to_dw = A.dw + (int64_t)g * A.d_in * A.d_out;
+        int m_first = wm + 4 * half, c_first = wn + l32;      // (addresses are formed here: hoisted out of the loops they take registers those have not got)
+        asm volatile("" : "+v"(m_first), "+v"(c_first));
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int m = wm + mb * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
+                const int m = m_first + mb * 32 + 8 * (i >> 2) + (i & 3);
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) {
-                    const int c = wn + nb * 32 + l32;
+                    const int c = c_first + nb * 32;
                     if (!whole)
                         to_part[m * BN + c] = acc[mb][nb][i];
                     else if (m0 + m < A.d_in && n0 + c < A.d_out)
@@ -730,14 +613,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
 
 // The tiles that several workgroups have parts of, and zeros for groups without rows: GW_PARTS workgroups a tile
 constexpr int GW_PARTS = 16;
-template <int BM, int BN>
+template <int BM, int BN, int ROWS>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
     const int tiles_n = (A.d_out + BN - 1) / BN, tiles = (A.d_in + BM - 1) / BM * tiles_n;
     const int part = blockIdx.x % GW_PARTS, unit = blockIdx.x / GW_PARTS, tile = unit % tiles, g = unit / tiles;
-    const Share S = share_of(A, tiles);
-    const int64_t before = steps_before(A.G, g) * tiles;
+    const Share S = share_of(A, tiles, ROWS);
+    const int64_t before = steps_before(A.G, g, ROWS) * tiles;
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
-    const int64_t steps_g = to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
+    const int64_t steps_g = to > from ? (to - from + ROWS - 1) / ROWS : 0;
     const int64_t t0 = before + tile * steps_g, t1 = t0 + steps_g;
     const int64_t w0 = steps_g ? t0 / S.per : 0, w1 = steps_g ? (t1 - 1) / S.per : -1;
     if (steps_g && w0 == w1) return;      // one workgroup has written it
@@ -754,6 +637,318 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
     }
 }
 
+// ---- fp32 ----
+//
+// Every product of two fp32 values is formed on the bf16 matrix cores from the exact split of both into three bf16 terms (x1 = bf16(x), x2 =
+// bf16(x - x1), x3 = bf16(x - x1 - x2)): the six products a_i * b_j with i + j <= 4, the leading ones in a running sum of their own, as in
+// fg_linear. A workgroup owns a TILE x TILE tile of the result and walks the contraction in steps of GF_K: a thread loads 16 bytes of
+// an operand's row, splits them and writes each term's bf16 values to LDS as they lie. An operand whose rows lie along the contraction (KC)
+// is read from there 16 bytes a lane, one whose rows lie across it (KN: W of the forward product; x and dz of the weight gradients) is
+// transposed on the way out. One buffer and two barriers a step; the loads of the next step are in flight while a step is multiplied, and the
+// two workgroups of a compute unit fill each other's waits.
+constexpr int GF_THREADS = 256, GF_K = 32;
+constexpr size_t gf_lds_bytes(int tile) { return (size_t)2 * 3 * tile * GF_K * 2; }
+typedef float gf_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 gf_bf16x2 __attribute__((ext_vector_type(2)));
+
+// four values -> two words of each of their three terms
+__device__ __forceinline__ void split4(fg_u32x4 v, fg_u32x2 (&u)[3]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        gf_f32x2 x = {__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])};
+#pragma unroll
+        for (int term = 0; term < 3; ++term) {
+            u[term][p] = __builtin_bit_cast(unsigned int, __builtin_convertvector(x, gf_bf16x2));
+            x = gf_f32x2{x[0] - __uint_as_float(u[term][p] << 16), x[1] - __uint_as_float(u[term][p] & 0xFFFF0000u)};
+        }
+    }
+}
+
+// One operand: TILE rows (KC) or columns (KN) by GF_K
+template <int TILE, bool KN>
+struct F32Operand {
+    static constexpr int LOADS = TILE * GF_K / 4 / GF_THREADS, TERM = TILE * GF_K * 2, ROW = KN ? TILE * 2 : GF_K * 2;
+    static constexpr int PER_ROW = KN ? TILE / 4 : GF_K / 4, ROWS = GF_THREADS / PER_ROW;      // pieces of a row; rows of a pass
+    // windows of 64 bytes are exchanged so that the four rows of a transposing read lie in different banks
+    static __device__ __forceinline__ int window(int row) { return TILE >= 128 ? row & 3 : (row >> 1) & 1; }
+    static __device__ __forceinline__ int row_of(int t, int i) { return t / PER_ROW + ROWS * i; }
+    static __device__ __forceinline__ int place(int t, int i) {      // bytes from the term's first
+        const int row = row_of(t, i), p = t % PER_ROW;
+        return KN ? row * ROW + (((p >> 3) ^ window(row)) << 6) + (p & 7) * 8 : row * ROW + (((p >> 1) ^ ((row >> 1) & 3)) << 4) + (p & 1) * 8;
+    }
+    static __device__ __forceinline__ void put(char* lds, int t, int i, fg_u32x4 v) {
+        fg_u32x2 u[3];
+        split4(v, u);
+        char* to = lds + place(t, i);
+#pragma unroll
+        for (int term = 0; term < 3; ++term) *(fg_u32x2*)(to + term * TERM) = u[term];
+    }
+    // rows (columns) first .. first + 31, k = 16 kk + 8 half + 0..7
+    static __device__ __forceinline__ fg_u32x4 fragment(const char* lds, int first, int kk, int lane) {
+        const int l32 = lane & 31, half = lane >> 5;
+        if constexpr (!KN) {
+            const int row = first + l32;
+            return *(const fg_u32x4*)(lds + row * ROW + (((2 * kk + half) ^ ((row >> 1) & 3)) << 4));
+        } else {
+            typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+            const int place = (lane >> 2) & 3;
+            const char* p = lds + (16 * kk + 8 * half + place) * ROW + (((first >> 5) ^ window(place)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+            const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
+            const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROW));
+            return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
+
+// A wavefront's part of the tile: TILE / 2 by TILE / 2, as 32 x 32 blocks
+template <int TILE>
+struct F32Sums {
+    static constexpr int B = TILE / 64;
+    gl_f32x16 lead[B][B], rest[B][B];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int a = 0; a < B; ++a)
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) lead[a][b][i] = rest[a][b][i] = 0.f;
+    }
+};
+template <int TILE, bool A_KN, bool B_KN>
+__device__ __forceinline__ void f32_multiply(const char* lds, int wm, int wn, int lane, F32Sums<TILE>& S) {
+    typedef F32Operand<TILE, A_KN> OA;
+    typedef F32Operand<TILE, B_KN> OB;
+    constexpr int NB = F32Sums<TILE>::B;
+    constexpr int TA[5] = {2, 0, 1, 1, 0}, TB[5] = {0, 2, 1, 0, 1};      // smallest products first
+#pragma unroll
+    for (int kk = 0; kk < GF_K / 16; ++kk) {
+        fg_u32x4 a[NB][3], b[NB][3];
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+                a[i][term] = OA::fragment(lds + term * OA::TERM, wm + 32 * i, kk, lane);
+                b[i][term] = OB::fragment(lds + 3 * OA::TERM + term * OB::TERM, wn + 32 * i, kk, lane);
+            }
+#pragma unroll
+        for (int e = 0; e < 5; ++e)
+#pragma unroll
+            for (int i = 0; i < NB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) S.rest[i][j] = mfma<FG_BF16, false>(&a[i][TA[e]], &b[j][TB[e]], S.rest[i][j]);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) S.lead[i][j] = mfma<FG_BF16, false>(&a[i][0], &b[j][0], S.lead[i][j]);
+    }
+}
+
+template <int TILE, bool B_KN>
+__global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_kernel(GlArgs A) {
+    typedef F32Operand<TILE, false> OA;
+    typedef F32Operand<TILE, B_KN> OB;
+    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
+    __shared__ int32_t pos[TILE], src[TILE];
+    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;      // column tiles of a row tile on one XCD
+    int g;
+    int64_t k0, k1;
+    if (!find_tile(A.G, (int64_t)(j / A.tiles_n) * 8 + xcd, TILE, g, k0, k1)) return;
+    const int n0 = (j % A.tiles_n) * TILE;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int K = A.K, N = A.N;
+    if (t < TILE) {
+        int32_t r, s;
+        entry(A, k0 + t, k1, r, s);
+        pos[t] = r;
+        src[t] = r < 0 ? -1 : (A.a_by == GL_A_SOURCE ? s : A.a_by == GL_A_POSITION ? r : (int32_t)(k0 + t));
+    }
+    __syncthreads();
+    // (a row or column that does not exist reads the first one there is, a k beyond K the first: zeroed when they are written to LDS)
+    const float* pa[OA::LOADS];
+    const int ka = (t % OA::PER_ROW) * 4;
+#pragma unroll
+    for (int i = 0; i < OA::LOADS; ++i) {
+        const int32_t r = src[OA::row_of(t, i)];
+        pa[i] = (const float*)(A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride);
+    }
+    const float* w0 = (const float*)A.W + (int64_t)g * K * N;
+    const float* pb[OB::LOADS];
+    const int pb_c = (t % OB::PER_ROW) * 4;      // column (KN) or k (KC) of the thread's pieces
+#pragma unroll
+    for (int i = 0; i < OB::LOADS; ++i) {
+        const int row = OB::row_of(t, i);
+        if constexpr (B_KN)
+            pb[i] = w0 + (n0 + pb_c < N ? n0 + pb_c : 0);
+        else
+            pb[i] = w0 + (int64_t)(n0 + row < N ? n0 + row : 0) * K;
+    }
+    fg_u32x4 ra[OA::LOADS], rb[OB::LOADS];
+    auto load = [&](int k) {
+        const int kk = k + ka < K ? k + ka : 0;
+#pragma unroll
+        for (int i = 0; i < OA::LOADS; ++i) ra[i] = *(const fg_u32x4*)(pa[i] + kk);
+#pragma unroll
+        for (int i = 0; i < OB::LOADS; ++i) {
+            if constexpr (B_KN) {
+                const int row = k + OB::row_of(t, i);
+                rb[i] = *(const fg_u32x4*)(pb[i] + (int64_t)(row < K ? row : 0) * N);
+            } else {
+                rb[i] = *(const fg_u32x4*)(pb[i] + (k + pb_c < K ? k + pb_c : 0));
+            }
+        }
+    };
+    auto store = [&](int k) {
+        const fg_u32x4 none = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int i = 0; i < OA::LOADS; ++i) OA::put(gl_lds, t, i, k + ka < K ? ra[i] : none);
+#pragma unroll
+        for (int i = 0; i < OB::LOADS; ++i) OB::put(gl_lds + 3 * OA::TERM, t, i, k + (B_KN ? OB::row_of(t, i) : pb_c) < K ? rb[i] : none);
+    };
+    const int wm = (wave >> 1) * (TILE / 2), wn = (wave & 1) * (TILE / 2);
+    F32Sums<TILE> S;
+    S.clear();
+    load(0);
+    for (int k = 0; k < K; k += GF_K) {
+        store(k);
+        __syncthreads();
+        load(k + GF_K);      // beyond K: valid addresses, not used
+        __builtin_amdgcn_sched_barrier(0);
+        f32_multiply<TILE, false, B_KN>(gl_lds, wm, wn, lane, S);
+        __syncthreads();
+    }
+    // accumulator element i of a block is its row 8 * (i / 4) + 4 * half + i % 4, column l32
+    const int l32 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < F32Sums<TILE>::B; ++b) {
+        const int c = n0 + wn + 32 * b + l32;
+        if (c >= N) continue;
+        const double bias = A.bias ? (double)A.bias[(int64_t)g * N + c] : 0.0;
+#pragma unroll
+        for (int a = 0; a < F32Sums<TILE>::B; ++a)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int32_t r = pos[wm + 32 * a + 8 * (i >> 2) + 4 * half + (i & 3)];
+                if (r < 0) continue;
+                float v = (float)((double)S.lead[a][b][i] + (double)S.rest[a][b][i] + bias);
+                if (A.relu) v = v < 0.f ? 0.f : v;
+                *(float*)(A.out + (int64_t)r * A.out_stride + (int64_t)c * 4) = v;
+            }
+    }
+}
+
+// out[r, :] = a[., :] . B in fp32 (as tile_product)
+template <bool B_KN>
+fg_status_t f32_product(const char* who, GlArgs& A, hipStream_t st) {
+    const int tile = A.G.max_rows / 128 * fg_ceil_div(A.N, 128) >= 256 && A.N > 64 ? 128 : 64;
+    A.tiles_n = (int)fg_ceil_div(A.N, tile);
+    const int64_t rows = A.G.max_rows / tile + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
+    const int64_t grid = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
+    if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
+    if (tile == 128)
+        hipLaunchKernelGGL((grouped_f32_kernel<128, B_KN>), dim3((unsigned)grid), dim3(GF_THREADS), gf_lds_bytes(128), st, A);
+    else
+        hipLaunchKernelGGL((grouped_f32_kernel<64, B_KN>), dim3((unsigned)grid), dim3(GF_THREADS), gf_lds_bytes(64), st, A);
+    FG_LAUNCH_CHECK("grouped_f32_kernel");
+    return FG_OK;
+}
+
+// dW in fp32: the shares of grouped_dw_kernel, steps of GF_K entries, 128 x 128 tiles
+__global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A) {
+    constexpr int TILE = 128;
+    typedef F32Operand<TILE, true> OP;
+    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
+    int32_t* list = (int32_t*)(gl_lds + gf_lds_bytes(TILE));
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int tiles_n = (A.d_out + TILE - 1) / TILE, tiles = (A.d_in + TILE - 1) / TILE * tiles_n;
+    const Share S = share_of(A, tiles, GF_K);
+    int64_t at = blockIdx.x * S.per;
+    const int64_t end = at + S.per < S.total ? at + S.per : S.total;
+    const int wm = (wave >> 1) * (TILE / 2), wn = (wave & 1) * (TILE / 2);
+    int g = 0;
+    int64_t before = 0;
+    while (at < end) {      // uniform over the workgroup
+        int64_t from, to, steps_g;
+        for (;; ++g) {
+            from = group_offset(A.G, g);
+            to = group_offset(A.G, g + 1);
+            steps_g = to > from ? (to - from + GF_K - 1) / GF_K : 0;
+            if (at < before + steps_g * tiles) break;
+            before += steps_g * tiles;
+        }
+        const int tile = (int)((at - before) / steps_g);
+        const int64_t first = at - before - tile * steps_g;
+        const int64_t last = first + (end - at) < steps_g ? first + (end - at) : steps_g;
+        const int steps = (int)(last - first);
+        const int64_t k0 = from + first * GF_K, k1 = from + last * GF_K < to ? from + last * GF_K : to;
+        const int m0 = (tile / tiles_n) * TILE, n0 = (tile % tiles_n) * TILE;
+        const int c = (t % OP::PER_ROW) * 4;
+        const int64_t ca = (m0 + c < A.d_in ? m0 + c : 0) * 4, cb = (n0 + c < A.d_out ? n0 + c : 0) * 4;
+        fg_u32x4 ra[OP::LOADS], rb[OP::LOADS];
+        bool in[OP::LOADS];
+        auto fill = [&](int64_t k) {
+#pragma unroll 2
+            for (int i = t; i < GW_LIST; i += GF_THREADS) {
+                int32_t r = -1, s = -1;
+                entry(A, k + i, k1, r, s);
+                list[i] = s;
+            }
+            __syncthreads();
+        };
+        auto load = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < OP::LOADS; ++i) {
+                const int32_t x_row = list[(s * GF_K) % GW_LIST + OP::row_of(t, i)];
+                in[i] = x_row >= 0;
+                const int64_t xr = in[i] ? x_row : 0, zr = in[i] ? (A.dz ? k0 + (int64_t)s * GF_K + OP::row_of(t, i) : xr) : 0;
+                ra[i] = *(const fg_u32x4*)(A.x + xr * A.x_stride + ca);
+                rb[i] = *(const fg_u32x4*)((A.dz ? A.dz : A.dh) + zr * A.dz_stride + cb);
+            }
+        };
+        auto store = [&]() {
+            const fg_u32x4 none = {0u, 0u, 0u, 0u};
+#pragma unroll
+            for (int i = 0; i < OP::LOADS; ++i) {
+                OP::put(gl_lds, t, i, in[i] ? ra[i] : none);
+                OP::put(gl_lds + 3 * OP::TERM, t, i, in[i] ? rb[i] : none);
+            }
+        };
+        F32Sums<TILE> C;
+        C.clear();
+        fill(k0);
+        load(0);
+        for (int s = 0; s < steps; ++s) {
+            store();
+            if (s + 1 < steps && (s + 1) % (GW_LIST / GF_K) == 0) fill(k0 + (int64_t)(s + 1) * GF_K);      // (the list's last entries have been taken)
+            __syncthreads();
+            if (s + 1 < steps) load(s + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            f32_multiply<TILE, true, true>(gl_lds, wm, wn, lane, C);
+            __syncthreads();
+        }
+        const bool whole = first == 0 && last == steps_g;
+        float* to_part = A.dw_part + (int64_t)(2 * blockIdx.x + (at == blockIdx.x * S.per ? 0 : 1)) * TILE * TILE;
+        float* to_dw = A.dw + (int64_t)g * A.d_in * A.d_out;
+        int m_first = wm + 4 * (lane >> 5), n_first = wn + (lane & 31);      // (formed here, as above)
+        asm volatile("" : "+v"(m_first), "+v"(n_first));
+#pragma unroll
+        for (int a = 0; a < F32Sums<TILE>::B; ++a)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int m = m_first + 32 * a + 8 * (i >> 2) + (i & 3);
+#pragma unroll
+                for (int b = 0; b < F32Sums<TILE>::B; ++b) {
+                    const int n = n_first + 32 * b;
+                    const float v = C.lead[a][b][i] + C.rest[a][b][i];
+                    if (!whole)
+                        to_part[m * TILE + n] = v;
+                    else if (m0 + m < A.d_in && n0 + n < A.d_out)
+                        to_dw[(int64_t)(m0 + m) * A.d_out + n0 + n] = v;
+                }
+            }
+        at += steps;
+    }
+}
+
 // The workspace of a backward call: dz, column sums by tile, parts of dW
 struct BwPlan {
     bool dz;
@@ -765,9 +960,9 @@ struct BwPlan {
 BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
     BwPlan P;
     P.dz = true;
-    P.bm = d_in > 128 || d_out > 128 ? 256 : 128;
+    P.bm = e == 2 && (d_in > 128 || d_out > 128) ? 256 : 128;
     const int64_t tiles = fg_ceil_div(d_in, P.bm) * fg_ceil_div(d_out, P.bm);
-    const int64_t steps = (max_rows / GW_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * tiles;
+    const int64_t steps = (max_rows / (e == 4 ? GF_K : GW_ROWS) + (n_groups < max_rows ? n_groups : max_rows)) * tiles;
     const int most = P.bm == 256 ? 256 : 512;      // as many as run at once
     P.shares = steps < 1 ? 1 : (int)(steps < most ? steps : most);
     P.dz_bytes = fg_align_up((size_t)max_rows * d_out * e, 256);
@@ -806,12 +1001,13 @@ fg_status_t check_matrix(const char* who, const char* what, const void* p, int64
 int64_t row_tiles(int64_t max_rows, int n_groups, int size) { return max_rows / size + (n_groups < max_rows ? n_groups : max_rows); }
 
 template <int T>
-fg_status_t backward_16_of(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
-    const BwPlan P = bw_plan(A.G.max_rows, A.G.n_groups, A.d_in, A.d_out, 2);
+fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
+    constexpr int E = T == FG_F32 ? 4 : 2;
+    const BwPlan P = bw_plan(A.G.max_rows, A.G.n_groups, A.d_in, A.d_out, E);
     char* ws = (char*)ws_dev;
     const bool pack = A.h || A.dh_type != T || A.src_ids;      // otherwise dh, by position as x is, serves as it lies
     A.dz = work && pack && (A.out || A.dw) ? ws : nullptr;
-    A.dz_stride = A.dz ? (int64_t)A.d_out * 2 : A.dh_stride;
+    A.dz_stride = A.dz ? (int64_t)A.d_out * E : A.dh_stride;
     A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
     A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
     if (A.dz || A.db_part) {
@@ -828,25 +1024,29 @@ fg_status_t backward_16_of(const char* who, GlArgs& A, bool work, hipStream_t st
     }
     if (A.out && work) {
         A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
-        FG_TRY((tile_product<T, false, false>(who, A, st)));
+        if constexpr (T == FG_F32)
+            FG_TRY(f32_product<false>(who, A, st));
+        else
+            FG_TRY((tile_product<T, false, false>(who, A, st)));
     }
     if (A.dw) {
         A.shares = P.shares, A.min_share = 1;
-        const int64_t tiles = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * GW_PARTS;
-        if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
-        if (P.bm == 256) {
-            hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), dim3((unsigned)P.shares), dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
-            hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256>), dim3((unsigned)tiles), dim3(GZ_THREADS), 0, st, A);
+        const int64_t sums = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * GW_PARTS;
+        if (sums > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
+        const dim3 grid((unsigned)P.shares), sum_grid((unsigned)sums);
+        if constexpr (T == FG_F32) {
+            hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), gf_lds_bytes(128) + GW_LIST * 4, st, A);
+            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GF_K>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+        } else if (P.bm == 256) {
+            hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
+            hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
         } else {
-            hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), dim3((unsigned)P.shares), dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
-            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128>), dim3((unsigned)tiles), dim3(GZ_THREADS), 0, st, A);
+            hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
+            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
         }
         FG_LAUNCH_CHECK("grouped_dw_kernel");
     }
     return FG_OK;
-}
-fg_status_t backward_16(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
-    return A.type == FG_BF16 ? backward_16_of<FG_BF16>(who, A, work, st, ws_dev) : backward_16_of<FG_F16>(who, A, work, st, ws_dev);
 }
 
 }  // namespace
@@ -871,18 +1071,14 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     GlArgs A = {};
     A.G = {order_dev, offsets_dev, max_rows, n_groups};
     A.x = (const char*)x, A.W = (const char*)W, A.x_rows = x_rows, A.x_stride = x_stride, A.n = n_out, A.out_stride = out_stride;
-    A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu, A.tiles_n = (int)fg_ceil_div(d_out, GL_TILE);
+    A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu;
     A.x_scale = x_scale, A.w_scale = w_scale, A.bias = bias, A.src_ids = src_ids_dev, A.out = (char*)h_out;
     A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
     if (dtype == FG_BF16) return tile_product<FG_BF16, true, false>(who, A, (hipStream_t)stream);
     if (dtype == FG_F16) return tile_product<FG_F16, true, false>(who, A, (hipStream_t)stream);
     if (dtype == FG_E4M3 && out_dtype == FG_F32) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
     if (dtype == FG_E4M3) return tile_product<FG_E4M3, false, false>(who, A, (hipStream_t)stream);
-    const int64_t grid = row_tiles(max_rows, n_groups, GL_TILE) * A.tiles_n;
-    if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
-    hipLaunchKernelGGL((grouped_linear_kernel<false>), dim3((unsigned)grid), dim3(GL_THREADS), 0, (hipStream_t)stream, A);
-    FG_LAUNCH_CHECK("grouped_linear_kernel");
-    return FG_OK;
+    return f32_product<true>(who, A, (hipStream_t)stream);
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
@@ -920,21 +1116,7 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     A.x = (const char*)x, A.W = (const char*)W, A.h = (const char*)h, A.dh = (const char*)dh, A.x_rows = x_rows, A.x_stride = x_stride, A.h_stride = h_stride;
     A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.type = dtype, A.dh_type = dh_dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
     A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = dw_dev, A.db = db_dev;
-    hipStream_t st = (hipStream_t)stream;
-    if (dtype != FG_F32) return backward_16(who, A, work, st, ws_dev);
-    if (dx && work) {
-        A.tiles_n = (int)fg_ceil_div(d_in, GL_TILE);
-        const int64_t grid = row_tiles(max_rows, n_groups, GL_TILE) * A.tiles_n;
-        if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
-        hipLaunchKernelGGL((grouped_linear_kernel<true>), dim3((unsigned)grid), dim3(GL_THREADS), 0, st, A);
-        FG_LAUNCH_CHECK("grouped_linear_kernel");
-    }
-    if (dw_dev || db_dev) {
-        A.tiles_n = (int)fg_ceil_div(d_out, GL_TILE);
-        const int64_t grid = n_groups * A.tiles_n * fg_ceil_div(d_in, GL_TILE);
-        if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
-        hipLaunchKernelGGL(grouped_weights_kernel, dim3((unsigned)grid), dim3(GL_THREADS), 0, st, A);
-        FG_LAUNCH_CHECK("grouped_weights_kernel");
-    }
-    return FG_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dtype == FG_F32) return backward<FG_F32>(who, A, work, st, ws_dev);
+    return dtype == FG_BF16 ? backward<FG_BF16>(who, A, work, st, ws_dev) : backward<FG_F16>(who, A, work, st, ws_dev);
 }
