@@ -77,13 +77,16 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 }
 // ---- 16- and 8-bit products on the matrix cores ----
 //
-// A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 128 bytes of a row (64 halfwords, 128 bytes of 8 bits). The
-// operands of a step go from memory straight to LDS (global_load_lds, 16 bytes a lane): two buffers, step s + 2 sets out when step s
-// has been multiplied, so a load has a whole step of arithmetic to arrive in. A lane's place in LDS is fixed by the instruction (base + 16
-// bytes per lane), so the exchange of 16-byte pieces that keeps the operand reads off each other's banks is made on the side of memory: piece c
-// of LDS row m holds piece c ^ (m & 7) of the row. B is either read the same way (rows of W along K: gradients, 8 bits), or its rows are k and
-// transposed on the way out of LDS (ds_read_b64_tr_b16), with the 64-byte windows of a row exchanged so that the four rows a read takes a
-// window of lie in different banks.
+// A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 64 bytes of a row (32 halfwords, 64 values of 8 bits). The
+// operands of a step go from memory straight to LDS (global_load_lds, 16 bytes a lane) into a ring of four buffers, so that a load has three
+// steps of arithmetic to arrive in. A wavefront reads the operands of its next matrix instructions from LDS while it issues the current
+// ones, over the end of a step too: there it waits for its loads of the next step, meets the others, and sends the loads of the fourth step
+// ahead into the buffer that all have then read. One barrier a step.
+// A lane's place in LDS is fixed by the instruction (base + 16 bytes per lane), so the exchange of 16-byte pieces that keeps the operand reads
+// off each other's banks is made on the side of memory: piece c of LDS row m holds piece c ^ (m / 4 & 3) of the row (a 16-byte read takes
+// the lanes in groups of sixteen: 0-3, 12-15, 20-23, 24-27 and so on; 256 bytes of banks). B is either read the same way (rows of W along K:
+// gradients, 8 bits), or its rows are k and transposed on the way out of LDS (ds_read_b64_tr_b16), with the 64-byte windows of a row exchanged so
+// that the four rows a read takes a window of lie in different banks.
 // Every lane's address is valid: a row or column that does not exist reads the first one there is (its products go to outputs that are
 // not stored), pieces beyond K are read from 16 bytes of zeros, both operands'.
 //
@@ -97,19 +100,11 @@ typedef short gl_s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void load_to_lds(const char* from, unsigned int lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
-// all loads but the N youngest have arrived, in every wavefront
+// Every wavefront's loads but the N youngest of each have arrived, and all have what they have read from LDS before
 template <int N>
 __device__ __forceinline__ void arrived() {
-    static_assert(N == 0 || N == 4 || N == 8, "");
-    if constexpr (N == 0)
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-    else if constexpr (N == 4)
-        asm volatile("s_waitcnt vmcnt(4)\n\ts_barrier" ::: "memory");
-    else
-        asm volatile("s_waitcnt vmcnt(8)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
-// every wavefront has read what it needs of the buffer
-__device__ __forceinline__ void read_done() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // 8-bit products. The 8-bit matrix instructions do not add up in fp32: they drop bits of products that are much smaller than the largest of
 // the same instruction (measured against exact sums: 1.3e-5 of the result's norm for normally distributed rows, 6e-5 for rows whose values
@@ -139,24 +134,24 @@ __device__ __forceinline__ void widen(fg_u32x4 v, fg_u32x4 (&out)[2]) {
     }
 }
 
-constexpr int GL_STEP = 128;      // bytes of K per step
-constexpr size_t gl_lds_bytes(int bm, int bn, int waves) {
-    return (size_t)2 * (bm + bn) * GL_STEP + (size_t)bm * 8;      // (the epilogue's blocks, 32 rows of a wavefront's columns in fp32, fit in the operands' space)
+constexpr int GL_STEP = 64;      // bytes of K per step
+constexpr size_t gl_lds_bytes(int bm, int bn, int ring) {
+    return (size_t)ring * (bm + bn) * GL_STEP + (size_t)bm * 8;      // (the epilogue's blocks, 32 rows of a wavefront's columns in fp32, fit in the operands' space)
 }
 
-template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N, int RING, bool B_KN, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int E = T == FG_E4M3 ? 1 : 2, BK = GL_STEP / E;
-    constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / 8 / WAVES, B_LOADS = BN / 8 / WAVES, LOADS = A_LOADS + B_LOADS;
+    constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / 16 / WAVES, B_LOADS = BN / 16 / WAVES, LOADS = A_LOADS + B_LOADS;
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
     constexpr int DEEP = T == FG_E4M3 && !WIDE ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
     constexpr int PARTS = T == FG_E4M3 ? 2 : 1;                                          // 16-byte registers of it
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
-    static_assert(A_LOADS * 8 * WAVES == BM && B_LOADS * 8 * WAVES == BN, "whole loads");
+    static_assert(A_LOADS * 16 * WAVES == BM && B_LOADS * 16 * WAVES == BN, "whole loads");
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
-    int32_t *pos = (int32_t*)(gl_lds + 2 * STAGE), *src = pos + BM;
+    int32_t *pos = (int32_t*)(gl_lds + RING * STAGE), *src = pos + BM;
 
     // the column tiles of a row tile lie on one XCD (workgroup ids are dealt round-robin to the eight of them): the rows come from memory once
     const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
@@ -174,16 +169,16 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     }
     __syncthreads();
 
-    // this lane's loads of a step: rows 8 (wave + WAVES i) + lane / 8 of A (and of B along K), piece lane % 8 exchanged
+    // this lane's loads of a step: rows 16 (wave + WAVES i) + lane / 4 of A (and of B along K), piece lane % 4 exchanged
     const char* pa[A_LOADS];
     const char* pb[B_LOADS];
     int kb[B_LOADS];      // first element of K (of the step) that a load of B holds; B_KN: its row
-    const int a_piece = (lane & 7) ^ (lane >> 3);      // row & 7 is lane / 8
+    const int a_piece = (lane & 3) ^ ((lane >> 4) & 3);
     const int ka = a_piece * (16 / E);
     const char* const zero = (const char*)gl_zero;
 #pragma unroll
     for (int i = 0; i < A_LOADS; ++i) {
-        const int32_t r = src[8 * (wave + WAVES * i) + (lane >> 3)];
+        const int32_t r = src[16 * (wave + WAVES * i) + (lane >> 2)];
         pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + a_piece * 16;
     }
     auto b_window = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };      // what a row's windows are exchanged by (BN = 64: it has two)
@@ -196,7 +191,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             kb[i] = row;
             pb[i] = w0 + ((int64_t)row * N + (c < N ? c : 0)) * E;
         } else {
-            const int c = n0 + 8 * (wave + WAVES * i) + (lane >> 3);
+            const int c = n0 + 16 * (wave + WAVES * i) + (lane >> 2);
             kb[i] = ka;
             pb[i] = w0 + (int64_t)(c < N ? c : 0) * K * E + a_piece * 16;
         }
@@ -205,7 +200,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
     const int steps = (K + BK - 1) / BK;
     auto load_step = [&](int s) {
-        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * STAGE + wave * 1024);
+        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)s % RING * STAGE + wave * 1024);
         const int left = K - s * BK;      // elements of K that the step has
         if (left >= BK) {
 #pragma unroll
@@ -233,62 +228,90 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
-    const int swap = (l32 & 7) << 4;
+    const int swap = ((l32 >> 2) & 3) << 4;
     const int place = (lane >> 2) & 3;
     const int b_in = (8 * half + place) * B_ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-    auto multiply = [&](int s) {
-        const char* As = gl_lds + (s & 1) * STAGE + (wm + l32) * GL_STEP;
-        const char* Bs = gl_lds + (s & 1) * STAGE + BM * GL_STEP;
+    struct Operands {
+        fg_u32x4 a[MB][PARTS], b[NB][PARTS];
+    };
+    auto read = [&](int s, int kk, Operands& F) {
+        const char* As = gl_lds + (unsigned)s % RING * STAGE + (wm + l32) * GL_STEP;
+        const char* Bs = gl_lds + (unsigned)s % RING * STAGE + BM * GL_STEP;
 #pragma unroll
-        for (int kk = 0; kk < SUB; ++kk) {
-            fg_u32x4 av[MB][PARTS], bv[NB][PARTS];
+        for (int q = 0; q < DEEP; ++q) {
+            const int at = (((kk * DEEP + q) * 2 + half) << 4) ^ swap;
 #pragma unroll
-            for (int q = 0; q < DEEP; ++q) {
-                const int at = (((kk * DEEP + q) * 2 + half) << 4) ^ swap;
+            for (int mb = 0; mb < MB; ++mb) F.a[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + at);
+            if constexpr (!B_KN)
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) av[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + at);
-                if constexpr (!B_KN)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) bv[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + at);
-            }
-            if constexpr (WIDE) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) widen(av[mb][0], av[mb]);
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) widen(bv[nb][0], bv[nb]);
-            }
-            if constexpr (B_KN)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) {
-                    typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
-                    const char* from = Bs + kk * 16 * B_ROW + b_in + ((((wn >> 5) + nb) ^ b_window(place)) << 6);
-                    const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from);
-                    const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 4 * B_ROW));
-                    bv[nb][0] = __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                }
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(av[mb], bv[nb], acc[mb][nb]);
+                for (int nb = 0; nb < NB; ++nb) F.b[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + at);
         }
+        if constexpr (B_KN)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+                const char* from = Bs + kk * 16 * B_ROW + b_in + ((((wn >> 5) + nb) ^ b_window(place)) << 6);
+                const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from);
+                const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 4 * B_ROW));
+                F.b[nb][0] = __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+    };
+    auto multiply = [&](Operands& F) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) widen(F.a[mb][0], F.a[mb]);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) widen(F.b[nb][0], F.b[nb]);
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.a[mb], F.b[nb], acc[mb][nb]);
+    };
+    // the last operands of step s are multiplied while the first of step s + 1 are read
+    auto next_step = [&](int s, Operands& now, Operands& next) {
+        if (s + 1 < steps) {
+            if (s + RING - 1 < steps)
+                arrived<(RING - 2) * LOADS>();
+            else if (RING > 3 && s + 2 < steps)
+                arrived<LOADS>();
+            else
+                arrived<0>();
+            if (s + RING < steps) load_step(s + RING);
+            read(s + 1, 0, next);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(now);
+        __builtin_amdgcn_sched_barrier(0);
     };
 
-    load_step(0);
-    if (steps > 1) load_step(1);
-    for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps)
-            arrived<LOADS>();
-        else
-            arrived<0>();
-        multiply(s);
-        read_done();
-        if (s + 2 < steps) load_step(s + 2);
+    for (int s = 0; s < RING && s < steps; ++s) load_step(s);
+    if (steps >= RING)
+        arrived<(RING - 1) * LOADS>();
+    else
+        arrived<0>();
+    Operands F0, F1;
+    read(0, 0, F0);
+    if constexpr (SUB == 2) {
+        for (int s = 0; s < steps; ++s) {
+            read(s, 1, F1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(F0);
+            __builtin_amdgcn_sched_barrier(0);
+            next_step(s, F1, F0);
+        }
+    } else {
+        for (int s = 0; s < steps; s += 2) {
+            next_step(s, F0, F1);
+            if (s + 1 < steps) next_step(s + 1, F1, F0);
+        }
     }
+    __syncthreads();
 
     // Epilogue: 32 rows of the wavefront's columns at a time through LDS (its own part: no barrier), so that the rows are written 16 bytes
     // at a time. Accumulator element i of a block is its row 8 * (i / 4) + 4 * half + i % 4, column l32.
     constexpr int LD = WN + 4;
-    static_assert(WAVES * 32 * LD * 4 <= 2 * STAGE, "the blocks fit in the operands' space");
+    static_assert(WAVES * 32 * LD * 4 <= RING * STAGE, "the blocks fit in the operands' space");
     float* blk = (float*)gl_lds + wave * 32 * LD;
     constexpr int LPR = WN / 8, RPP = 64 / LPR;      // lanes per row (eight columns each), rows per pass
     const int c0 = n0 + wn + (lane % LPR) * 8;
@@ -331,28 +354,39 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     }
 }
 
-template <int T, int BM, int BN, int WM, int WN, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WM, int WN, int RING, bool B_KN, bool WIDE>
 fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
     A.tiles_n = (int)fg_ceil_div(A.N, BN);
     const int64_t row_tiles_ = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t grid = fg_ceil_div(row_tiles_, 8) * 8 * A.tiles_n;
     if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
-    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN, WIDE>), dim3((unsigned)grid), dim3(64 * WM * WN), gl_lds_bytes(BM, BN, WM * WN), st, A);
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, RING, B_KN, WIDE>), dim3((unsigned)grid), dim3(64 * WM * WN), gl_lds_bytes(BM, BN, RING), st, A);
     FG_LAUNCH_CHECK("grouped_tile_kernel");
     return FG_OK;
 }
 // out[r, :] = a[., :] . B for the entries of every group (A.a, a_stride, a_by, K, N, W, out, ... are set)
 template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
-    const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
-    if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, B_KN, WIDE>(who, A, st);
+    const int64_t large = (A.G.max_rows / 128) * fg_ceil_div(A.N, 256);
+    if (large >= 512 && A.N > 128) return tile_launch<T, 128, 256, 1, 4, 3, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, B_KN, WIDE>(who, A, st);
-    return tile_launch<T, 64, 64, 2, 2, B_KN, WIDE>(who, A, st);
+    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 4, B_KN, WIDE>(who, A, st);
+    return tile_launch<T, 64, 64, 2, 2, 4, B_KN, WIDE>(who, A, st);
 }
 
-// ---- gradients of 16-bit rows ----
-//
+// ---- gradients ----
+
+// steps of the groups before `upto` (lanes of a wavefront together)
+__device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int rows) {
+    int64_t n = 0;
+    for (int i = fg_lane(); i < upto; i += 64) {
+        const int64_t from = group_offset(G, i), to = group_offset(G, i + 1);
+        n += to > from ? (to - from + rows - 1) / rows : 0;
+    }
+    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
+    return n;
+}
+
 // dz in entry order, in the rows' type, and its column sums by tiles of GZ_ROWS entries of one group (db is their sum). What it costs,
 // reading dh and h and writing dz, both products save again: they read dz alone, in the order of the entries.
 constexpr int GZ_ROWS = 64, GZ_THREADS = 256;
@@ -394,7 +428,7 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += z[e];
-                if (A.dz) fg_store_piece<T>(A.dz + ((k0 + m) * A.d_out + c) * E, z, A.d_out - c);
+            if (A.dz) fg_store_piece<T>(A.dz + (k0 + m) * A.dz_stride + (int64_t)c * E, z, A.d_out - c);
             }
         }
         if (A.db_part) {
@@ -411,29 +445,26 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
     }
 }
 
-// db[g, c] = sum over the group's tiles, in fp64; 32 columns a workgroup
-__global__ __launch_bounds__(GZ_THREADS) void grouped_db_kernel(GlArgs A) {
-    __shared__ double red[GZ_THREADS];
+// db[g, c] = sum over the group's tiles, in fp64; 32 columns a workgroup, 32 runs of tiles side by side
+constexpr int DB_THREADS = 1024;
+__global__ __launch_bounds__(DB_THREADS) void grouped_db_kernel(GlArgs A) {
+    __shared__ double red[DB_THREADS];
     const int blocks = (A.d_out + 31) / 32, g = blockIdx.x / blocks;
     const int c = (blockIdx.x % blocks) * 32 + (threadIdx.x & 31);
-    int64_t first = 0;
-    for (int i = fg_lane(); i < g; i += 64) {
-        const int64_t from = group_offset(A.G, i), to = group_offset(A.G, i + 1);
-        first += to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
-    }
-    for (int off = 32; off > 0; off >>= 1) first += __shfl_xor(first, off, 64);
+    const int64_t first = steps_before(A.G, g, GZ_ROWS);
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
     const int64_t tiles = to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
     double s = 0.0;
     if (c < A.d_out)
 #pragma unroll 8
-        for (int64_t i = threadIdx.x >> 5; i < tiles; i += GZ_THREADS / 32) s += (double)A.db_part[(first + i) * A.d_out + c];
+        for (int64_t i = threadIdx.x >> 5; i < tiles; i += DB_THREADS / 32) s += (double)A.db_part[(first + i) * A.d_out + c];
     red[threadIdx.x] = s;
     __syncthreads();
-    if (threadIdx.x < 32 && c < A.d_out) {
-        for (int q = 1; q < GZ_THREADS / 32; ++q) s += red[threadIdx.x + 32 * q];
-        A.db[(int64_t)g * A.d_out + c] = (float)s;
+    for (int n = DB_THREADS / 64; n >= 1; n >>= 1) {      // halves of the runs
+        if ((int)threadIdx.x < 32 * n) red[threadIdx.x] += red[threadIdx.x + 32 * n];
+        __syncthreads();
     }
+    if (threadIdx.x < 32 && c < A.d_out) A.db[(int64_t)g * A.d_out + c] = (float)red[threadIdx.x];
 }
 
 // dW = x^T . dz of every group: a contraction over the group's rows, whose number the device alone knows, with BM x BN tiles of the result.
@@ -446,16 +477,6 @@ constexpr int GW_ROWS = 64, GW_LIST = 4096;
 struct Share {
     int64_t total, per;      // steps of all groups; of a workgroup
 };
-// steps of the groups before `upto` (lanes of a wavefront together)
-__device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int rows) {
-    int64_t n = 0;
-    for (int i = fg_lane(); i < upto; i += 64) {
-        const int64_t from = group_offset(G, i), to = group_offset(G, i + 1);
-        n += to > from ? (to - from + rows - 1) / rows : 0;
-    }
-    for (int off = 32; off > 0; off >>= 1) n += __shfl_xor(n, off, 64);
-    return n;
-}
 __device__ __forceinline__ Share share_of(const GlArgs& A, int tiles, int rows) {
     Share s;
     s.total = steps_before(A.G, A.G.n_groups, rows) * tiles;
@@ -515,9 +536,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
             ca[i] = (m0 + c < A.d_in ? m0 + c : 0) * 2;
             cb[i] = (n0 + c < A.d_out ? n0 + c : 0) * 2;
         }
-        auto fill = [&](int64_t k) {      // entries k .. k + GW_LIST
+        auto fill = [&](int64_t k) {      // entries k .. k + GW_LIST, as far as whole steps need them
+            const int need = (int)(k1 - k < GW_LIST ? (k1 - k + GW_ROWS - 1) / GW_ROWS * GW_ROWS : GW_LIST);
 #pragma unroll 2
-            for (int i = t; i < GW_LIST; i += THREADS) {
+            for (int i = t; i < need; i += THREADS) {
                 int32_t r = -1, s = -1;
                 entry(A, k + i, k1, r, s);
                 list[i] = s;
@@ -580,7 +602,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
             else
                 arrived<0>();
             multiply(s);
-            read_done();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // every wavefront has read what it needs of the buffer
             if (s + 2 < steps) {
                 if ((s + 2) % (GW_LIST / GW_ROWS) == 0) fill(k0 + (int64_t)(s + 2) * GW_ROWS);
                 load_step(s + 2);
@@ -611,12 +633,17 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
     }
 }
 
-// The tiles that several workgroups have parts of, and zeros for groups without rows: GW_PARTS workgroups a tile
-constexpr int GW_PARTS = 16;
+// The tiles that several workgroups have parts of, and zeros for groups without rows. A workgroup takes VALUES values of a tile; where those are
+// fewer than its threads can hold, runs of the parts lie side by side (a small result has many parts: 14 tiles of 128 x 128 in 512 shares 27 us
+// with 1024 values and the parts one after the other, 7 with 256 values).
+constexpr int ds_values(int bm) { return bm == 256 ? 4096 : 256; }
 template <int BM, int BN, int ROWS>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
+    constexpr int VALUES = ds_values(BM), RUNS = VALUES < GZ_THREADS * 4 ? GZ_THREADS * 4 / VALUES : 1, SIDE = GZ_THREADS / RUNS, PARTS = BM * BN / VALUES;
+    __shared__ double red[RUNS][SIDE * 4];
     const int tiles_n = (A.d_out + BN - 1) / BN, tiles = (A.d_in + BM - 1) / BM * tiles_n;
-    const int part = blockIdx.x % GW_PARTS, unit = blockIdx.x / GW_PARTS, tile = unit % tiles, g = unit / tiles;
+    const int part = blockIdx.x % PARTS, unit = blockIdx.x / PARTS, tile = unit % tiles, g = unit / tiles;
+    if (tile / tiles_n * BM + part * VALUES / BN >= A.d_in) return;      // its rows do not exist
     const Share S = share_of(A, tiles, ROWS);
     const int64_t before = steps_before(A.G, g, ROWS) * tiles;
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
@@ -624,16 +651,28 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
     const int64_t t0 = before + tile * steps_g, t1 = t0 + steps_g;
     const int64_t w0 = steps_g ? t0 / S.per : 0, w1 = steps_g ? (t1 - 1) / S.per : -1;
     if (steps_g && w0 == w1) return;      // one workgroup has written it
-    const int m0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
-    for (int i = threadIdx.x * 4; i < BM * BN / GW_PARTS; i += GZ_THREADS * 4) {
-        const int e = part * (BM * BN / GW_PARTS) + i, m = m0 + e / BN, c = n0 + e % BN;
-        if (m >= A.d_in || c >= A.d_out) continue;      // d_out is a multiple of 4
+    const int run = threadIdx.x / SIDE, at = (threadIdx.x % SIDE) * 4;
+#pragma unroll
+    for (int i = 0; i < VALUES; i += SIDE * 4) {
+        const int e = part * VALUES + i + at, m = tile / tiles_n * BM + e / BN, c = tile % tiles_n * BN + e % BN;
         double s[4] = {};
-        for (int64_t w = w0; w <= w1; ++w) {
+#pragma unroll 4
+        for (int64_t w = w0 + run; w <= w1; w += RUNS) {
             const float4 v = *(const float4*)(A.dw_part + (2 * w + (t0 <= w * S.per ? 0 : 1)) * BM * BN + e);
             s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
         }
-        *(float4*)(A.dw + ((int64_t)g * A.d_in + m) * A.d_out + c) = float4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+        if constexpr (RUNS > 1) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) red[run][at + q] = s[q];
+            __syncthreads();
+            if (run == 0)
+#pragma unroll
+                for (int q = 1; q < RUNS; ++q)
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) s[f] += red[q][at + f];
+        }
+        if (run == 0 && m < A.d_in && c < A.d_out)      // d_out is a multiple of 4
+            *(float4*)(A.dw + ((int64_t)g * A.d_in + m) * A.d_out + c) = float4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
     }
 }
 
@@ -674,7 +713,7 @@ struct F32Operand {
     static __device__ __forceinline__ int row_of(int t, int i) { return t / PER_ROW + ROWS * i; }
     static __device__ __forceinline__ int place(int t, int i) {      // bytes from the term's first
         const int row = row_of(t, i), p = t % PER_ROW;
-        return KN ? row * ROW + (((p >> 3) ^ window(row)) << 6) + (p & 7) * 8 : row * ROW + (((p >> 1) ^ ((row >> 1) & 3)) << 4) + (p & 1) * 8;
+        return KN ? row * ROW + (((p >> 3) ^ window(row)) << 6) + (p & 7) * 8 : row * ROW + (((p >> 1) ^ ((row >> 2) & 3)) << 4) + (p & 1) * 8;
     }
     static __device__ __forceinline__ void put(char* lds, int t, int i, fg_u32x4 v) {
         fg_u32x2 u[3];
@@ -688,7 +727,7 @@ struct F32Operand {
         const int l32 = lane & 31, half = lane >> 5;
         if constexpr (!KN) {
             const int row = first + l32;
-            return *(const fg_u32x4*)(lds + row * ROW + (((2 * kk + half) ^ ((row >> 1) & 3)) << 4));
+            return *(const fg_u32x4*)(lds + row * ROW + (((2 * kk + half) ^ ((row >> 2) & 3)) << 4));
         } else {
             typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
             const int place = (lane >> 2) & 3;
@@ -886,8 +925,9 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
         fg_u32x4 ra[OP::LOADS], rb[OP::LOADS];
         bool in[OP::LOADS];
         auto fill = [&](int64_t k) {
+            const int need = (int)(k1 - k < GW_LIST ? (k1 - k + GF_K - 1) / GF_K * GF_K : GW_LIST);
 #pragma unroll 2
-            for (int i = t; i < GW_LIST; i += GF_THREADS) {
+            for (int i = t; i < need; i += GF_THREADS) {
                 int32_t r = -1, s = -1;
                 entry(A, k + i, k1, r, s);
                 list[i] = s;
@@ -949,6 +989,12 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
     }
 }
 
+// Bytes between the rows of dz. Tiles read the same columns of many rows at a time: rows a multiple of 512 bytes apart meet in few of the memory's
+// channels (66 k rows of 1024 bf16 x 1024 columns: 186 us at 2048 bytes, 159 at 2432), so such rows get 384 bytes more.
+int64_t dz_row(int d_out, int e) {
+    const int64_t row = (int64_t)d_out * e;
+    return row % 512 ? row : row + 384;
+}
 // The workspace of a backward call: dz, column sums by tile, parts of dW
 struct BwPlan {
     bool dz;
@@ -965,7 +1011,7 @@ BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
     const int64_t steps = (max_rows / (e == 4 ? GF_K : GW_ROWS) + (n_groups < max_rows ? n_groups : max_rows)) * tiles;
     const int most = P.bm == 256 ? 256 : 512;      // as many as run at once
     P.shares = steps < 1 ? 1 : (int)(steps < most ? steps : most);
-    P.dz_bytes = fg_align_up((size_t)max_rows * d_out * e, 256);
+    P.dz_bytes = fg_align_up((size_t)max_rows * dz_row(d_out, e), 256);
     P.db_bytes = fg_align_up((size_t)(max_rows / GZ_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * d_out * 4, 256);
     P.dw_bytes = (size_t)2 * P.shares * P.bm * P.bm * 4;
     return P;
@@ -1007,7 +1053,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     char* ws = (char*)ws_dev;
     const bool pack = A.h || A.dh_type != T || A.src_ids;      // otherwise dh, by position as x is, serves as it lies
     A.dz = work && pack && (A.out || A.dw) ? ws : nullptr;
-    A.dz_stride = A.dz ? (int64_t)A.d_out * E : A.dh_stride;
+    A.dz_stride = A.dz ? dz_row(A.d_out, E) : A.dh_stride;
     A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
     A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
     if (A.dz || A.db_part) {
@@ -1019,7 +1065,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
         FG_LAUNCH_CHECK("grouped_dz_kernel");
     }
     if (A.db) {
-        hipLaunchKernelGGL(grouped_db_kernel, dim3((unsigned)(A.G.n_groups * fg_ceil_div(A.d_out, 32))), dim3(GZ_THREADS), 0, st, A);
+        hipLaunchKernelGGL(grouped_db_kernel, dim3((unsigned)(A.G.n_groups * fg_ceil_div(A.d_out, 32))), dim3(DB_THREADS), 0, st, A);
         FG_LAUNCH_CHECK("grouped_db_kernel");
     }
     if (A.out && work) {
@@ -1031,7 +1077,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     }
     if (A.dw) {
         A.shares = P.shares, A.min_share = 1;
-        const int64_t sums = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * GW_PARTS;
+        const int64_t sums = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm / ds_values(P.bm));
         if (sums > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
         const dim3 grid((unsigned)P.shares), sum_grid((unsigned)sums);
         if constexpr (T == FG_F32) {
