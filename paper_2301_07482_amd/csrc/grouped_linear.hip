@@ -2,6 +2,8 @@
 //
 // The rows of a group lie behind each other in `order`; how many there are is known on the device only. The grid is sized for the
 // bound (every group may leave one tile partly filled), and a workgroup finds its group and its rows from the offsets.
+#include <type_traits>
+
 #include "row_types.h"
 #include "scan.h"
 
@@ -18,14 +20,15 @@ __device__ __forceinline__ int64_t group_offset(const Groups& G, int g) {
     return o < 0 ? 0 : (o > G.max_rows ? G.max_rows : o);
 }
 // tile number `tile` of rows (`size` of one group each): its group and its entries [k0, k1); false: there are fewer tiles
-__device__ __forceinline__ bool find_tile(const Groups& G, int64_t tile, int size, int& group, int64_t& k0, int64_t& k1) {
+template <typename OffsetOf>
+__device__ __forceinline__ bool find_tile(const Groups& G, const OffsetOf& offset, int64_t tile, int size, int& group, int64_t& k0, int64_t& k1) {
     int64_t before = 0;
     for (int base = 0; base < G.n_groups; base += 64) {
         const int g = base + fg_lane();
         int64_t from = 0, to = 0;
         if (g < G.n_groups) {
-            from = group_offset(G, g);
-            to = group_offset(G, g + 1);
+            from = offset(g);
+            to = offset(g + 1);
         }
         const int tiles = to > from ? (int)((to - from + size - 1) / size) : 0;
         const int incl = fg_wave_scan(tiles);
@@ -43,6 +46,9 @@ __device__ __forceinline__ bool find_tile(const Groups& G, int64_t tile, int siz
         before += __shfl(incl, 63, 64);
     }
     return false;
+}
+__device__ __forceinline__ bool find_tile(const Groups& G, int64_t tile, int size, int& group, int64_t& k0, int64_t& k1) {
+    return find_tile(G, [&](int g) { return group_offset(G, g); }, tile, size, group, k0, k1);
 }
 
 enum { GL_A_SOURCE = 0, GL_A_POSITION = 1, GL_A_ENTRY = 2 };      // rows of the left operand: by x row, by position, packed in entry order
@@ -92,14 +98,27 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 //
 // The waits are counted by hand: the compiler knows nothing of these loads (it would wait for all of them before every LDS read).
 __device__ __attribute__((aligned(16))) unsigned int gl_zero[4];
+// where the lanes of a store write that have nothing to write (never read)
+__device__ __attribute__((aligned(16))) unsigned int gl_sink[4 * 64];
 
 typedef float gl_f32x16 __attribute__((ext_vector_type(16)));
 typedef int gl_i32x8 __attribute__((ext_vector_type(8)));
 typedef short gl_s16x4 __attribute__((ext_vector_type(4)));
 
+// an address that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p) {
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    return (const char*)(uintptr_t)(((uint64_t)(unsigned int)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned int)__builtin_amdgcn_readfirstlane((int)v));
+}
+// the same from such an address and an offset below 2^31
+__device__ __forceinline__ void load_to_lds(const char* base, unsigned int offset, unsigned int lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+}
 __device__ __forceinline__ void load_to_lds(const char* from, unsigned int lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
+// A store that is counted by hand as well: it is issued whatever the lanes have to write
+__device__ __forceinline__ void store_16(char* to, fg_u32x4 v) { asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 1" ::"v"(to), "v"(v) : "memory"); }
 // Every wavefront's loads but the N youngest of each have arrived, and all have what they have read from LDS before
 template <int N>
 __device__ __forceinline__ void arrived() {
@@ -120,8 +139,8 @@ __device__ __forceinline__ gl_f32x16 mfma(const fg_u32x4* a, const fg_u32x4* b, 
         c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[1]), __builtin_bit_cast(fg_bf16x8, b[1]), c, 0, 0, 0);
     } else {      // (the block scales of the instruction are 2^0)
-        const gl_i32x8 av = {(int)a[0][0], (int)a[0][1], (int)a[0][2], (int)a[0][3], (int)a[1][0], (int)a[1][1], (int)a[1][2], (int)a[1][3]};
-        const gl_i32x8 bv = {(int)b[0][0], (int)b[0][1], (int)b[0][2], (int)b[0][3], (int)b[1][0], (int)b[1][1], (int)b[1][2], (int)b[1][3]};
+        const gl_i32x8 av = __builtin_bit_cast(gl_i32x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        const gl_i32x8 bv = __builtin_bit_cast(gl_i32x8, __builtin_shufflevector(b[0], b[1], 0, 1, 2, 3, 4, 5, 6, 7));
         return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
     }
 }
@@ -134,101 +153,155 @@ __device__ __forceinline__ void widen(fg_u32x4 v, fg_u32x4 (&out)[2]) {
     }
 }
 
-constexpr int GL_STEP = 64;      // bytes of K per step
-constexpr size_t gl_lds_bytes(int bm, int bn, int ring) {
-    return (size_t)ring * (bm + bn) * GL_STEP + (size_t)bm * 8;      // (the epilogue's blocks, 32 rows of a wavefront's columns in fp32, fit in the operands' space)
+constexpr int GL_STEP = 128, GL_PIECES = GL_STEP / 16, GL_ROWS = 1024 / GL_STEP;      // bytes of K per step; 16-byte pieces of a row; rows of a load
+constexpr int EP_BLOCK = 16 * 128;      // bytes of an epilogue's block
+// the operands' ring, the epilogue's blocks, what belongs to a tile (twice), the offsets
+constexpr size_t gl_lds_bytes(int bm, int bn, int waves, int ring, bool eight, int n_groups) {
+    return (size_t)ring * (bm + bn) * GL_STEP + (size_t)waves * EP_BLOCK + (size_t)2 * (8 * bm + 4 * bn + (eight ? 4 * (bm + bn) : 32)) + (size_t)(n_groups + 1) * 4;
 }
+// max(v, 0), a NaN stays one
+__device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise_maximum(v, 0.f); }
 
 template <int T, int BM, int BN, int WAVES_M, int WAVES_N, int RING, bool B_KN, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int E = T == FG_E4M3 ? 1 : 2, BK = GL_STEP / E;
-    constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / 16 / WAVES, B_LOADS = BN / 16 / WAVES, LOADS = A_LOADS + B_LOADS;
+    constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / GL_ROWS / WAVES, B_LOADS = BN / GL_ROWS / WAVES, LOADS = A_LOADS + B_LOADS;
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
     constexpr int DEEP = T == FG_E4M3 && !WIDE ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
     constexpr int PARTS = T == FG_E4M3 ? 2 : 1;                                          // 16-byte registers of it
+    constexpr bool AHEAD = PARTS == 1 || BM < 256;                                        // (two sets of the long operands do not fit the registers)
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
-    static_assert(A_LOADS * 16 * WAVES == BM && B_LOADS * 16 * WAVES == BN, "whole loads");
+    static_assert(A_LOADS * GL_ROWS * WAVES == BM && B_LOADS * GL_ROWS * WAVES == BN, "whole loads");
+    // LDS: the ring; the epilogue's blocks; what belongs to a tile, for the current one and the next; the offsets of the groups
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
-    int32_t *pos = (int32_t*)(gl_lds + RING * STAGE), *src = pos + BM;
-
-    // the column tiles of a row tile lie on one XCD (workgroup ids are dealt round-robin to the eight of them): the rows come from memory once
-    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;
-    int g;
-    int64_t k0, k1;
-    if (!find_tile(A.G, (int64_t)(j / A.tiles_n) * 8 + xcd, BM, g, k0, k1)) return;
-    const int n0 = (j % A.tiles_n) * BN;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int K = A.K, N = A.N;
-    for (int m = t; m < BM; m += THREADS) {
-        int32_t r, s;
-        entry(A, k0 + m, k1, r, s);
-        pos[m] = r;
-        src[m] = r < 0 ? -1 : (A.a_by == GL_A_SOURCE ? s : A.a_by == GL_A_POSITION ? r : (int32_t)(k0 + m));
-    }
+    struct TileData {
+        int32_t pos[BM], src[BM];      // position and row of A of every row, -1: none
+        float x_scale[T == FG_E4M3 ? BM : 4], bias[BN], w_scale[T == FG_E4M3 ? BN : 4];
+    };
+    char* const blocks = gl_lds + RING * STAGE;
+    TileData* data = (TileData*)(blocks + WAVES * EP_BLOCK);
+    int32_t* offsets = (int32_t*)(data + 2);
+    for (int i = t; i <= A.G.n_groups; i += THREADS) offsets[i] = (int32_t)group_offset(A.G, i);
     __syncthreads();
 
-    // this lane's loads of a step: rows 16 (wave + WAVES i) + lane / 4 of A (and of B along K), piece lane % 4 exchanged
-    const char* pa[A_LOADS];
-    const char* pb[B_LOADS];
-    int kb[B_LOADS];      // first element of K (of the step) that a load of B holds; B_KN: its row
-    const int a_piece = (lane & 3) ^ ((lane >> 4) & 3);
-    const int ka = a_piece * (16 / E);
-    const char* const zero = (const char*)gl_zero;
-#pragma unroll
-    for (int i = 0; i < A_LOADS; ++i) {
-        const int32_t r = src[16 * (wave + WAVES * i) + (lane >> 2)];
-        pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + a_piece * 16;
-    }
-    auto b_window = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };      // what a row's windows are exchanged by (BN = 64: it has two)
-    const char* w0 = A.W + (int64_t)g * K * N * E;
-#pragma unroll
-    for (int i = 0; i < B_LOADS; ++i) {
-        if constexpr (B_KN) {
-            const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
-            const int c = n0 + (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
-            kb[i] = row;
-            pb[i] = w0 + ((int64_t)row * N + (c < N ? c : 0)) * E;
-        } else {
-            const int c = n0 + 16 * (wave + WAVES * i) + (lane >> 2);
-            kb[i] = ka;
-            pb[i] = w0 + (int64_t)(c < N ? c : 0) * K * E + a_piece * 16;
+    const int K = A.K, N = A.N;
+    // The column tiles of a row tile lie on one XCD (workgroup ids are dealt round-robin to the eight of them): the rows come from memory
+    // once. A workgroup takes every (workgroups of an XCD)-th of its XCD's tiles.
+    const int xcd = blockIdx.x & 7, j_step = gridDim.x >> 3;
+    struct Tile {
+        int g, n0, k0, k1;
+    };
+    auto find = [&](int j, Tile& F) -> bool {
+        int g = 0;
+        int64_t k0 = 0, k1 = 0;
+        const bool there = find_tile(A.G, [&](int i) { return (int64_t)offsets[i]; }, (int64_t)(j / A.tiles_n) * 8 + xcd, BM, g, k0, k1);
+        F.g = __builtin_amdgcn_readfirstlane(g);
+        F.k0 = __builtin_amdgcn_readfirstlane((int)k0);
+        F.k1 = __builtin_amdgcn_readfirstlane((int)k1);
+        F.n0 = (j % A.tiles_n) * BN;
+        return __builtin_amdgcn_readfirstlane(there);
+    };
+    // What belongs to a tile comes in three reads that depend on each other, a value to a thread: entry, row, scale of the row
+    static_assert(THREADS >= BM && THREADS >= BN, "a thread for every row and column");
+    int32_t e_pos = -1, e_src = -1;
+    float e_scale = 0.f, e_bias = 0.f, e_w_scale = 0.f;
+    auto fetch_entry = [&](const Tile& F) {
+        const int k = F.k0 + t, c = F.n0 + t;
+        e_pos = t < BM && k < F.k1 ? (A.G.order ? A.G.order[k] : k) : -1;
+        if (t < BN && c < N) {
+            if (A.bias) e_bias = A.bias[(int64_t)F.g * N + c];
+            if constexpr (T == FG_E4M3) e_w_scale = A.w_scale[(int64_t)F.g * N + c];
         }
-    }
+    };
+    auto fetch_source = [&]() {
+        if (e_pos < 0 || e_pos >= A.n) e_pos = -1;
+        e_src = e_pos >= 0 && A.src_ids ? A.src_ids[e_pos] : e_pos;
+    };
+    auto fetch_scale = [&](const Tile& F) {
+        if (e_src < 0 || e_src >= A.x_rows) e_pos = e_src = -1;
+        if constexpr (T == FG_E4M3) e_scale = e_src >= 0 ? A.x_scale[e_src] : 0.f;
+        if (e_src >= 0 && A.a_by != GL_A_SOURCE) e_src = A.a_by == GL_A_POSITION ? e_pos : F.k0 + t;
+    };
+    auto keep = [&](TileData& D) {
+        if (t < BM) {
+            D.pos[t] = e_pos;
+            D.src[t] = e_src;
+            if constexpr (T == FG_E4M3) D.x_scale[t] = e_scale;
+        }
+        if (t < BN) {
+            D.bias[t] = e_bias;
+            if constexpr (T == FG_E4M3) D.w_scale[t] = e_w_scale;
+        }
+        __syncthreads();
+    };
+
+    int j = blockIdx.x >> 3;
+    Tile cur, next = {};
+    if (!find(j, cur)) return;
+    fetch_entry(cur);
+    fetch_source();
+    fetch_scale(cur);
+    keep(data[0]);
+
+    // this lane's loads of a step: rows 8 (wave + WAVES i) + lane / 8 of A (and of B along K), piece lane % 8 exchanged
+    const char* pa[A_LOADS];
+    const char* w_at = nullptr;      // the step's first weight, and this lane's pieces from there
+    unsigned int pb[B_LOADS];
+    auto exchanged = [](int row) { return (row >> 1) & (GL_PIECES - 1); };
+    const int a_row = GL_ROWS * wave + lane / GL_PIECES, a_piece = (lane % GL_PIECES) ^ exchanged(a_row), ka = a_piece * (16 / E);
+    static_assert(GL_ROWS * WAVES % (2 * GL_PIECES) == 0, "the same exchange for all loads of a lane");
+    const char* const zero = (const char*)gl_zero;
+    auto b_window = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };      // what a row's windows are exchanged by (BN = 64: it has two)
+    auto begin = [&](const Tile& F, const TileData& D) {
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) {
+            const int32_t r = D.src[a_row + GL_ROWS * WAVES * i];
+            pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + a_piece * 16;
+        }
+        w_at = A.W + ((int64_t)F.g * N + (B_KN ? 0 : F.n0)) * K * E;      // (a column tile begins below N)
+#pragma unroll
+        for (int i = 0; i < B_LOADS; ++i) {
+            if constexpr (B_KN) {
+                const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
+                const int c = F.n0 + (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
+                pb[i] = (unsigned int)(row * N + (c < N ? c : 0)) * E;
+            } else {
+                const int c = F.n0 + a_row + GL_ROWS * WAVES * i;
+                pb[i] = (unsigned int)(c < N ? c - F.n0 : 0) * K * E + a_piece * 16;
+            }
+        }
+    };
     const int64_t b_step = B_KN ? (int64_t)BK * N * E : GL_STEP;
     const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
     const int steps = (K + BK - 1) / BK;
     auto load_step = [&](int s) {
         const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)s % RING * STAGE + wave * 1024);
         const int left = K - s * BK;      // elements of K that the step has
+        const char* const w = uniform(w_at);
         if (left >= BK) {
 #pragma unroll
             for (int i = 0; i < A_LOADS; ++i) load_to_lds(pa[i], to + i * WAVES * 1024);
 #pragma unroll
-            for (int i = 0; i < B_LOADS; ++i) load_to_lds(pb[i], to + BM * GL_STEP + i * WAVES * 1024);
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds(w, pb[i], to + BM * GL_STEP + i * WAVES * 1024);
         } else {
 #pragma unroll
             for (int i = 0; i < A_LOADS; ++i) load_to_lds(ka < left ? pa[i] : zero, to + i * WAVES * 1024);
 #pragma unroll
-            for (int i = 0; i < B_LOADS; ++i) load_to_lds(kb[i] < left ? pb[i] : zero, to + BM * GL_STEP + i * WAVES * 1024);
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds((B_KN ? (64 * (wave + WAVES * i) + lane) / B_ROW_PIECES : ka) < left ? w_at + pb[i] : zero, to + BM * GL_STEP + i * WAVES * 1024);
         }
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) pa[i] += GL_STEP;
-#pragma unroll
-        for (int i = 0; i < B_LOADS; ++i) pb[i] += b_step;
+        w_at += b_step;
     };
 
     const int l32 = lane & 31, half = lane >> 5;
     const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * WN;
     gl_f32x16 acc[MB][NB];
-#pragma unroll
-    for (int a = 0; a < MB; ++a)
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
-    const int swap = ((l32 >> 2) & 3) << 4;
+    const int swap = exchanged(l32) << 4;
+    static_assert(RING == 2 && SUB % 2 == 0, "one step ahead; the operands' two sets in turn");
     const int place = (lane >> 2) & 3;
     const int b_in = (8 * half + place) * B_ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     struct Operands {
@@ -266,112 +339,188 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.a[mb], F.b[nb], acc[mb][nb]);
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], F.a[mb], acc[mb][nb]);
     };
-    // the last operands of step s are multiplied while the first of step s + 1 are read
-    auto next_step = [&](int s, Operands& now, Operands& next) {
-        if (s + 1 < steps) {
-            if (s + RING - 1 < steps)
-                arrived<(RING - 2) * LOADS>();
-            else if (RING > 3 && s + 2 < steps)
-                arrived<LOADS>();
-            else
-                arrived<0>();
-            if (s + RING < steps) load_step(s + RING);
-            read(s + 1, 0, next);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(now);
-        __builtin_amdgcn_sched_barrier(0);
+    // The stores of a tile are younger than the next one's first two steps' loads: those are waited for with the stores left on their way
+    constexpr int STORES = MB * NB * 2;
+    static_assert(LOADS + 2 * STORES < 64, "as many as can be counted");
+    int stores = 0;      // 0, STORES or 2 * STORES
+    auto arrived_first = [&](auto loads) {
+        constexpr int N = decltype(loads)::value;
+        if (stores == 0)
+            arrived<N>();
+        else if (stores == STORES)
+            arrived<N + STORES>();
+        else
+            arrived<N + 2 * STORES>();
     };
-
-    for (int s = 0; s < RING && s < steps; ++s) load_step(s);
-    if (steps >= RING)
-        arrived<(RING - 1) * LOADS>();
-    else
-        arrived<0>();
+    // One step: its operands are read one set ahead of the matrix instructions; the last set is multiplied while the first of the next step
+    // is read. LAST: there is no next step, LOAD: there is one after it, whose loads set out.
     Operands F0, F1;
-    read(0, 0, F0);
-    if constexpr (SUB == 2) {
-        for (int s = 0; s < steps; ++s) {
-            read(s, 1, F1);
+    auto step = [&](int s, auto last, auto load) {
+        constexpr bool LAST = decltype(last)::value, LOAD = decltype(load)::value;
+#pragma unroll
+        for (int kk = 0; kk < SUB; ++kk) {
+            Operands &now = AHEAD && (kk & 1) ? F1 : F0, &ahead = AHEAD && !(kk & 1) ? F1 : F0;
+            if (kk + 1 < SUB) {
+                if (AHEAD) read(s, kk + 1, ahead);
+            } else if (!LAST) {
+                if (s == 0)
+                    arrived_first(std::integral_constant<int, 0>());
+                else
+                    arrived<0>();
+                if (LOAD) load_step(s + 2);
+                if (AHEAD) read(s + 1, 0, ahead);
+            }
             __builtin_amdgcn_sched_barrier(0);
-            multiply(F0);
+            multiply(now);
             __builtin_amdgcn_sched_barrier(0);
-            next_step(s, F1, F0);
+            if (!AHEAD && kk + 1 < SUB) read(s, kk + 1, F0);
+            if (!AHEAD && kk + 1 == SUB && !LAST) read(s + 1, 0, F0);
         }
-    } else {
-        for (int s = 0; s < steps; s += 2) {
-            next_step(s, F0, F1);
-            if (s + 1 < steps) next_step(s + 1, F1, F0);
-        }
-    }
-    __syncthreads();
+    };
 
-    // Epilogue: 32 rows of the wavefront's columns at a time through LDS (its own part: no barrier), so that the rows are written 16 bytes
-    // at a time. Accumulator element i of a block is its row 8 * (i / 4) + 4 * half + i % 4, column l32.
-    constexpr int LD = WN + 4;
-    static_assert(WAVES * 32 * LD * 4 <= RING * STAGE, "the blocks fit in the operands' space");
-    float* blk = (float*)gl_lds + wave * 32 * LD;
-    constexpr int LPR = WN / 8, RPP = 64 / LPR;      // lanes per row (eight columns each), rows per pass
-    const int c0 = n0 + wn + (lane % LPR) * 8;
-    const bool c_in = c0 < N;                        // N is a multiple of 8
-    float bias[8], ws[8];
+    // The products are formed as (B^T . A^T): element i of a 32 x 32 block is column 8 * (i / 4) + 4 * half + i % 4 of its row l32, so a lane holds
+    // four adjacent columns of a row. Blocks of 16 rows by 128 bytes go through LDS (a wavefront's own part: no barrier), so that a store writes
+    // whole lines. Pieces of 16 bytes are exchanged by the row, as the operands'.
+    auto write = [&](const Tile& F, const TileData& D) {
+        int lane = t & 63;      // (addresses are formed here: hoisted out of the loops they take registers those have not got)
+        asm volatile("" : "+v"(lane));
+        const int l32 = lane & 31, half = lane >> 5;
+        char* const sink = (char*)gl_sink + lane * 16;
+        char* const blk = blocks + wave * EP_BLOCK;
+        constexpr int ROW16 = WN * 2;      // bytes of a row of the block in a 16-bit type; 128 of fp32
+        auto swapped = [](int row, int row_bytes) { return row_bytes == 128 ? (row >> 1) & 7 : (row >> 2) & 3; };
+        // rows 16 * part .. of block row mb, columns from n0 + cl on
+        auto put_out = [&](int mb, int part, int cl, int element, int row_bytes) {
+            const int lanes = row_bytes / 16, piece = lane % lanes, c = F.n0 + cl + piece * (16 / element);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        bias[e] = A.bias && c_in ? A.bias[(int64_t)g * N + c0 + e] : 0.f;
-        ws[e] = T == FG_E4M3 && c_in ? A.w_scale[(int64_t)g * N + c0 + e] : 1.f;
-    }
+            for (int p = 0; p < row_bytes / 64; ++p) {
+                const int row = p * (64 / lanes) + lane / lanes;
+                const fg_u32x4 w = *(const fg_u32x4*)(blk + row * row_bytes + ((piece ^ swapped(row, row_bytes)) << 4));
+                const int32_t r = c < N ? D.pos[wm + mb * 32 + part * 16 + row] : -1;
+                store_16(r >= 0 ? A.out + (int64_t)r * A.out_stride + (int64_t)c * element : sink, w);
+            }
+        };
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
+        for (int mb = 0; mb < MB; ++mb) {
+            asm volatile("" ::: "memory");      // (what is read from LDS below stays in LDS until then)
+            const float xs = T == FG_E4M3 ? D.x_scale[wm + mb * 32 + l32] : 1.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if constexpr (T == FG_E4M3) {
+                        const int cl = wn + nb * 32 + 8 * q + 4 * half;
+                        const float4 b = *(const float4*)(D.bias + cl), ws = *(const float4*)(D.w_scale + cl);
+                        gl_f32x16& v = acc[mb][nb];
+                        v[4 * q] = v[4 * q] * (xs * ws.x) + b.x, v[4 * q + 1] = v[4 * q + 1] * (xs * ws.y) + b.y;
+                        v[4 * q + 2] = v[4 * q + 2] * (xs * ws.z) + b.z, v[4 * q + 3] = v[4 * q + 3] * (xs * ws.w) + b.w;
+                    }
+                    if (A.relu)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[mb][nb][4 * q + e] = relu_of(acc[mb][nb][4 * q + e]);
+                }
+            const int row = l32 & 15;
+            if (A.out_type == FG_F32) {
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        if ((l32 >> 4) == part)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const gl_f32x16& v = acc[mb][nb];
+                                *(fg_u32x4*)(blk + row * 128 + (((2 * q + half) ^ swapped(row, 128)) << 4)) =
+                                    fg_u32x4{__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
+                            }
+                        put_out(mb, part, wn + nb * 32, 4, 128);
+                    }
+            } else {
+                fg_u32x2 w[NB][4];
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float v[4] = {acc[mb][nb][4 * q], acc[mb][nb][4 * q + 1], acc[mb][nb][4 * q + 2], acc[mb][nb][4 * q + 3]};
+                        w[nb][q] = A.out_type == FG_BF16 ? fg_to_words<FG_BF16>(v) : fg_to_words<FG_F16>(v);
+                    }
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    if ((l32 >> 4) == part)
+#pragma unroll
+                        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) *(fg_u32x2*)(blk + row * ROW16 + (((nb * 4 + q) ^ swapped(row, ROW16)) << 4) + half * 8) = w[nb][q];
+                    put_out(mb, part, wn, 2, ROW16);
+                }
+            }
+        }
+    };
+
+    begin(cur, data[0]);
+    load_step(0);
+    if (steps > 1) load_step(1);
+    for (int which = 0;; which ^= 1) {
+        const bool more = find(j + j_step, next);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) blk[(8 * (i >> 2) + 4 * half + (i & 3)) * LD + nb * 32 + l32] = acc[mb][nb][i];
+            for (int q = 0; q < 4; ++q) {      // (8-bit products are scaled before the bias is added)
+                float4 b = {0.f, 0.f, 0.f, 0.f};
+                if constexpr (T != FG_E4M3) b = *(const float4*)(data[which].bias + wn + nb * 32 + 8 * q + 4 * half);
 #pragma unroll
-        for (int p = 0; p < 32 / RPP; ++p) {
-            const int m = p * RPP + lane / LPR;
-            const int32_t r = pos[wm + mb * 32 + m];
-            float v[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = blk[m * LD + (lane % LPR) * 8 + e];
-            if (r < 0 || !c_in) continue;
-            const float xs = T == FG_E4M3 ? A.x_scale[src[wm + mb * 32 + m]] : 1.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if constexpr (T == FG_E4M3) v[e] *= xs * ws[e];
-                v[e] += bias[e];
-                if (A.relu) v[e] = v[e] < 0.f ? 0.f : v[e];
+                for (int mb = 0; mb < MB; ++mb) acc[mb][nb][4 * q] = b.x, acc[mb][nb][4 * q + 1] = b.y, acc[mb][nb][4 * q + 2] = b.z, acc[mb][nb][4 * q + 3] = b.w;
             }
-            char* to = A.out + (int64_t)r * A.out_stride;
-            if (A.out_type == FG_F32)
-                fg_store_piece<FG_F32>(to + (int64_t)c0 * 4, v, 8);
-            else if (A.out_type == FG_BF16)
-                fg_store_piece<FG_BF16>(to + (int64_t)c0 * 2, v, 8);
-            else
-                fg_store_piece<FG_F16>(to + (int64_t)c0 * 2, v, 8);
+        if (steps > 1)
+            arrived_first(std::integral_constant<int, LOADS>());
+        else
+            arrived<0>();
+        read(0, 0, F0);
+        // what belongs to the next tile is read behind this one's last loads (the waits for it are for everything in front of it)
+        int s = 0;
+        for (; s + 2 < steps; ++s) step(s, std::false_type(), std::true_type());
+        if (more) fetch_entry(next);
+        if (steps > 1) step(s++, std::false_type(), std::false_type());
+        if (more) fetch_source();
+        step(s, std::true_type(), std::false_type());
+        if (more) fetch_scale(next);
+        // the next tile's first loads are on their way while this one is written
+        if (more) {
+            keep(data[which ^ 1]);      // (every wavefront has read what it needs of the ring)
+            begin(next, data[which ^ 1]);
+            load_step(0);
+            if (steps > 1) load_step(1);
         }
+        write(cur, data[which]);
+        if (!more) break;
+        stores = A.out_type == FG_F32 ? 2 * STORES : STORES;
+        cur = next;
+        j += j_step;
     }
 }
 
-template <int T, int BM, int BN, int WM, int WN, int RING, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WM, int WN, int RING, int PER_CU, bool B_KN, bool WIDE>
 fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
     A.tiles_n = (int)fg_ceil_div(A.N, BN);
-    const int64_t row_tiles_ = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
-    const int64_t grid = fg_ceil_div(row_tiles_, 8) * 8 * A.tiles_n;
-    if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
-    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, RING, B_KN, WIDE>), dim3((unsigned)grid), dim3(64 * WM * WN), gl_lds_bytes(BM, BN, RING), st, A);
+    const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
+    const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
+    if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
+    const int64_t at_once = 256 * PER_CU;
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, RING, B_KN, WIDE>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
+                       gl_lds_bytes(BM, BN, WM * WN, RING, T == FG_E4M3, A.G.n_groups), st, A);
     FG_LAUNCH_CHECK("grouped_tile_kernel");
     return FG_OK;
 }
 // out[r, :] = a[., :] . B for the entries of every group (A.a, a_stride, a_by, K, N, W, out, ... are set)
 template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
-    const int64_t large = (A.G.max_rows / 128) * fg_ceil_div(A.N, 256);
-    if (large >= 512 && A.N > 128) return tile_launch<T, 128, 256, 1, 4, 3, B_KN, WIDE>(who, A, st);
+    const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
+    if constexpr (T != FG_E4M3)
+        if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 4, B_KN, WIDE>(who, A, st);
-    return tile_launch<T, 64, 64, 2, 2, 4, B_KN, WIDE>(who, A, st);
+    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
+    return tile_launch<T, 64, 64, 2, 2, 2, 4, B_KN, WIDE>(who, A, st);
 }
 
 // ---- gradients ----

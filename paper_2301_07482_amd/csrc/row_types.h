@@ -11,7 +11,9 @@ typedef fg_u32x4 fg_u32x4_any __attribute__((aligned(2)));
 typedef fg_u32x4 fg_u32x4_word __attribute__((aligned(4)));
 typedef fg_u32x2 fg_u32x2_any __attribute__((aligned(1)));
 typedef float fg_f32x8 __attribute__((ext_vector_type(8)));
-typedef float fg_f32x2 __attribute__((ext_vector_type(2)));
+typedef float fg_f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 fg_bf16x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 fg_f16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 fg_bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 fg_f16x8 __attribute__((ext_vector_type(8)));
 
@@ -78,35 +80,51 @@ __device__ __forceinline__ void fg_piece_values(const fg_piece<T>& v, float (&f)
 }
 // nearest even
 template <int T>
+__device__ __forceinline__ fg_piece<T> fg_to_piece(const float (&f)[8]) {
+    fg_piece<T> v;
+    if constexpr (T == FG_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v.a[i] = __float_as_uint(f[i]);
+            v.b[i] = __float_as_uint(f[i + 4]);
+        }
+    } else {
+        const fg_f32x8 w = {f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
+        if constexpr (T == FG_BF16)
+            v.a = __builtin_bit_cast(fg_u32x4, __builtin_convertvector(w, fg_bf16x8));
+        else
+            v.a = __builtin_bit_cast(fg_u32x4, __builtin_convertvector(w, fg_f16x8));
+    }
+    return v;
+}
+// four values to a 16-bit type, nearest even
+template <int T>
+__device__ __forceinline__ fg_u32x2 fg_to_words(const float (&f)[4]) {
+    const fg_f32x4 w = {f[0], f[1], f[2], f[3]};
+    if constexpr (T == FG_BF16)
+        return __builtin_bit_cast(fg_u32x2, __builtin_convertvector(w, fg_bf16x4));
+    else
+        return __builtin_bit_cast(fg_u32x2, __builtin_convertvector(w, fg_f16x4));
+}
+template <int T>
 __device__ __forceinline__ void fg_store_piece(char* p, const float (&f)[8], int left) {
+    const fg_piece<T> v = fg_to_piece<T>(f);
     if constexpr (T == FG_F32) {
         if (left >= 8) {
-            fg_u32x4 a, b;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                a[i] = __float_as_uint(f[i]);
-                b[i] = __float_as_uint(f[i + 4]);
-            }
-            *(fg_u32x4_word*)p = a;
-            *(fg_u32x4_word*)(p + 16) = b;
+            *(fg_u32x4_word*)p = v.a;
+            *(fg_u32x4_word*)(p + 16) = v.b;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < left) ((float*)p)[i] = f[i];
         }
     } else {
-        const fg_f32x8 w = {f[0], f[1], f[2], f[3], f[4], f[5], f[6], f[7]};
-        fg_u32x4 a;
-        if constexpr (T == FG_BF16)
-            a = __builtin_bit_cast(fg_u32x4, __builtin_convertvector(w, fg_bf16x8));
-        else
-            a = __builtin_bit_cast(fg_u32x4, __builtin_convertvector(w, fg_f16x8));
         if (left >= 8) {
-            *(fg_u32x4_any*)p = a;
+            *(fg_u32x4_any*)p = v.a;
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < left) ((unsigned short*)p)[i] = (unsigned short)(a[i / 2] >> (16 * (i & 1)));
+                if (i < left) ((unsigned short*)p)[i] = (unsigned short)(v.a[i / 2] >> (16 * (i & 1)));
         }
     }
 }
