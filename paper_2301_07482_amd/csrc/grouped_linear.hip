@@ -66,11 +66,11 @@ struct GlArgs {
     const char* a;
     int64_t a_stride;
     int a_by, K, N;
-    // gradients: dz in entry order (or NULL: dh serves as it is) and its row stride, column sums by tile, parts of dW and who makes them
+    // gradients: dz in entry order (or NULL: dh serves as it is) and its row stride, column sums by tile, parts of dW and the ranges of rows they are made of
     char* dz;
     int64_t dz_stride;
     float *db_part, *dw_part;
-    int shares, min_share;
+    int ranges;
 };
 // position and row of x of entry k; -1: skipped
 __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, int32_t& r, int32_t& s) {
@@ -617,74 +617,108 @@ __global__ __launch_bounds__(DB_THREADS) void grouped_db_kernel(GlArgs A) {
 }
 
 // dW = x^T . dz of every group: a contraction over the group's rows, whose number the device alone knows, with BM x BN tiles of the result.
-// The work is a line of steps of GW_ROWS entries, group by group, tile by tile, and cut into equal shares for the workgroups there
-// are: all of them end together however the groups are sized. A workgroup writes a tile that lies wholly in its share, and leaves its
-// part of one that does not (the first and the last of its share) in a slot of its own; a second launch adds those up, in order.
+// The rows are a line of steps of ROWS entries, group by group, cut into equal ranges; a workgroup takes one tile along one range, so
+// that all of them end together however the groups are sized, and those of one range (on one XCD) read the same rows at the same time: from
+// its L2 but for the first. A group that lies wholly in a range is a result; of one that does not (the first and the last of a range) the
+// workgroup leaves its part in a slot of its own, and a second launch adds those up, in order.
 // Both operands have the contraction index in front, rows of x and of dz: they go to LDS as they lie and are transposed on the way out.
 constexpr int GW_ROWS = 64, GW_LIST = 4096;
 
 struct Share {
-    int64_t total, per;      // steps of all groups; of a workgroup
+    int64_t total, per;      // steps of all groups; of a range
 };
-__device__ __forceinline__ Share share_of(const GlArgs& A, int tiles, int rows) {
+__device__ __forceinline__ Share share_of(const GlArgs& A, int rows) {
     Share s;
-    s.total = steps_before(A.G, A.G.n_groups, rows) * tiles;
-    s.per = (s.total + A.shares - 1) / A.shares;
-    if (s.per < A.min_share) s.per = A.min_share;
+    s.total = steps_before(A.G, A.G.n_groups, rows);
+    s.per = (s.total + A.ranges - 1) / A.ranges;
     return s;
 }
+// range and tile of this workgroup: consecutive ones on one XCD
+__device__ __forceinline__ bool range_and_tile(const GlArgs& A, int tiles, int& range, int& tile) {
+    const int per_xcd = (int)gridDim.x >> 3, unit = ((int)blockIdx.x & 7) * per_xcd + ((int)blockIdx.x >> 3);
+    range = unit / tiles;
+    tile = unit % tiles;
+    return range < A.ranges;
+}
+// walks the groups of a range: group g's steps [first, last) of its steps_g lie in it, entries [k0, k1)
+struct RangeWalk {
+    int64_t at, end, before;
+    int g;
+    int64_t steps_g, first, last, k0, k1;
+    __device__ __forceinline__ bool next(const Groups& G, int rows) {
+        if (at >= end) return false;
+        int64_t from, to;
+        for (;; ++g) {
+            from = group_offset(G, g);
+            to = group_offset(G, g + 1);
+            steps_g = to > from ? (to - from + rows - 1) / rows : 0;
+            if (at < before + steps_g) break;
+            before += steps_g;
+        }
+        first = at - before;
+        last = first + (end - at) < steps_g ? first + (end - at) : steps_g;
+        k0 = from + first * rows;
+        k1 = from + last * rows < to ? from + last * rows : to;
+        return true;
+    }
+};
 
 template <int T, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
-    constexpr int STAGE = GW_ROWS * (BM + BN) * 2, A_LOADS = GW_ROWS * BM * 2 / 1024 / WAVES, B_LOADS = GW_ROWS * BN * 2 / 1024 / WAVES, LOADS = A_LOADS + B_LOADS;
-    constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32;
-    static_assert(BM == BN, "a lane's pieces of x and of dz lie in the same rows");
+    constexpr int STAGE = GW_ROWS * (BM + BN) * 2, LOADS = GW_ROWS * BM * 2 / 1024 / WAVES;      // of either operand
+    constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, SUB = GW_ROWS / 16;
+    static_assert(BM == BN && SUB % 2 == 0, "a lane's pieces of x and of dz lie in the same rows; the operands' two sets in turn");
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
     int32_t* list = (int32_t*)(gl_lds + 2 * STAGE);      // rows of x of the next entries, -1: skipped
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int tiles_m = (A.d_in + BM - 1) / BM, tiles_n = (A.d_out + BN - 1) / BN, tiles = tiles_m * tiles_n;
-    const Share S = share_of(A, tiles, GW_ROWS);
-    int64_t at = blockIdx.x * S.per;
-    const int64_t end = at + S.per < S.total ? at + S.per : S.total;
-    if (at >= end) return;
+    int range, tile;
+    if (!range_and_tile(A, tiles, range, tile)) return;
+    const Share S = share_of(A, GW_ROWS);
+    RangeWalk W = {range * S.per, (range + 1) * S.per < S.total ? (range + 1) * S.per : S.total, 0, 0};
 
     const int l32 = lane & 31, half = lane >> 5, place = (lane >> 2) & 3;
     const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * (BN / WAVES_N);
-    constexpr int ROW = BM * 2, ROW_PIECES = ROW / 16;
+    const int m0 = (tile / tiles_n) * BM, n0 = (tile % tiles_n) * BN;
+    constexpr int ROW = BM * 2, ROW_PIECES = ROW / 16, ROWS_A_LOAD = 1024 / ROW;
     const int in_row = (8 * half + place) * ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
     const char* const zero = (const char*)gl_zero;
+    // this lane's pieces of a step: rows row0 + ROWS_A_LOAD * WAVES * i, one piece of 8 columns (columns that do not exist read the first: not stored)
+    const int row0 = ROWS_A_LOAD * wave + lane / ROW_PIECES, slot = lane % ROW_PIECES;
+    static_assert(ROWS_A_LOAD * WAVES % 4 == 0, "the same exchange for all loads of a lane");
+    const int col = (((slot >> 2) ^ (row0 & 3)) * 4 + (slot & 3)) * 8;
+    const int ca = (m0 + col < A.d_in ? m0 + col : 0) * 2, cb = (n0 + col < A.d_out ? n0 + col : 0) * 2;
 
-    int g = 0;
-    int64_t before = 0;      // steps (times tiles) of the groups before g
-    while (at < end) {       // uniform over the workgroup
-        int64_t from, to, steps_g;
-        for (;; ++g) {
-            from = group_offset(A.G, g);
-            to = group_offset(A.G, g + 1);
-            steps_g = to > from ? (to - from + GW_ROWS - 1) / GW_ROWS : 0;
-            if (at < before + steps_g * tiles) break;
-            before += steps_g * tiles;
-        }
-        const int tile = (int)((at - before) / steps_g);
-        const int64_t first = at - before - tile * steps_g;                   // step of the tile
-        const int64_t last = first + (end - at) < steps_g ? first + (end - at) : steps_g;
-        const int steps = (int)(last - first);
-        const int64_t k0 = from + first * GW_ROWS, k1 = from + last * GW_ROWS < to ? from + last * GW_ROWS : to;
-        const int m0 = (tile / tiles_n) * BM, n0 = (tile % tiles_n) * BN;
-
-        // this lane's pieces of a step: rows row[i], column pieces of the tile (a column that does not exist reads the first: not stored)
-        int64_t ca[A_LOADS], cb[B_LOADS];
-        int row[A_LOADS];
+    gl_f32x16 acc[MB][NB];
+    struct Operands {
+        fg_u32x4 a[MB], b[NB];
+    };
+    auto fragment = [&](const char* p) -> fg_u32x4 {
+        typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+        const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
+        const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROW));
+        return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto read = [&](int s, int kk, Operands& F) {
+        const char* As = gl_lds + (s & 1) * STAGE + in_row + kk * 16 * ROW;
+        const char* Bs = As + GW_ROWS * BM * 2;
 #pragma unroll
-        for (int i = 0; i < A_LOADS; ++i) {
-            const int p = 64 * (wave + WAVES * i) + lane, slot = p % ROW_PIECES;
-            row[i] = p / ROW_PIECES;
-            const int c = (((slot >> 2) ^ (row[i] & 3)) * 4 + (slot & 3)) * 8;
-            ca[i] = (m0 + c < A.d_in ? m0 + c : 0) * 2;
-            cb[i] = (n0 + c < A.d_out ? n0 + c : 0) * 2;
-        }
+        for (int mb = 0; mb < MB; ++mb) F.a[mb] = fragment(As + ((((wm >> 5) + mb) ^ place) << 6));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) F.b[nb] = fragment(Bs + ((((wn >> 5) + nb) ^ place) << 6));
+    };
+    auto multiply = [&](const Operands& F) {
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, false>(&F.a[mb], &F.b[nb], acc[mb][nb]);
+    };
+
+    for (; W.next(A.G, GW_ROWS); W.at += W.last - W.first) {      // uniform over the workgroup
+        const int steps = (int)(W.last - W.first);
+        const int64_t k0 = W.k0, k1 = W.k1;
         auto fill = [&](int64_t k) {      // entries k .. k + GW_LIST, as far as whole steps need them
             const int need = (int)(k1 - k < GW_LIST ? (k1 - k + GW_ROWS - 1) / GW_ROWS * GW_ROWS : GW_LIST);
 #pragma unroll 2
@@ -695,72 +729,68 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
             }
             __syncthreads();
         };
+        int32_t x_row[LOADS];
+        auto read_rows = [&](int s) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) x_row[i] = list[(s * GW_ROWS) % GW_LIST + row0 + ROWS_A_LOAD * WAVES * i];
+        };
         auto load_step = [&](int s) {
             const unsigned int dst = __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * STAGE + wave * 1024);
             const int64_t k = k0 + (int64_t)s * GW_ROWS;
 #pragma unroll
-            for (int i = 0; i < A_LOADS; ++i) {
-                const int32_t x_row = list[(s * GW_ROWS) % GW_LIST + row[i]];
-                const int64_t z_row = A.dz ? k + row[i] : x_row;      // without dz: dh by position, which is the row of x
-                const char *pa = A.x + x_row * A.x_stride + ca[i], *pb = (A.dz ? A.dz : A.dh) + z_row * A.dz_stride + cb[i];
-                load_to_lds(x_row >= 0 ? pa : zero, dst + i * WAVES * 1024);
-                load_to_lds(x_row >= 0 ? pb : zero, dst + GW_ROWS * BM * 2 + i * WAVES * 1024);
+            for (int i = 0; i < LOADS; ++i) {
+                const int64_t z_row = A.dz ? k + row0 + ROWS_A_LOAD * WAVES * i : x_row[i];      // without dz: dh by position, which is the row of x
+                const char *pa = A.x + x_row[i] * A.x_stride + ca, *pb = (A.dz ? A.dz : A.dh) + z_row * A.dz_stride + cb;
+                load_to_lds(x_row[i] >= 0 ? pa : zero, dst + i * WAVES * 1024);
+                load_to_lds(x_row[i] >= 0 ? pb : zero, dst + GW_ROWS * BM * 2 + i * WAVES * 1024);
             }
         };
-        gl_f32x16 acc[MB][NB];
 #pragma unroll
         for (int a = 0; a < MB; ++a)
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[a][b][i] = 0.f;
-        auto fragment = [&](const char* p) -> fg_u32x4 {
-            typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
-            const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
-            const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROW));
-            return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        auto multiply = [&](int s) {
-            const char* As = gl_lds + (s & 1) * STAGE + in_row;
-            const char* Bs = As + GW_ROWS * BM * 2;
-            fg_u32x4 av[2][MB], bv[2][NB];
-            auto read = [&](int kk, int set) {
+        fill(k0);
+        read_rows(0);
+        load_step(0);
+        if (steps > 1) {
+            read_rows(1);
+            load_step(1);
+            arrived<2 * LOADS>();
+        } else {
+            arrived<0>();
+        }
+        // as in grouped_tile_kernel: one barrier a step, behind the reads of its last operands
+        Operands F0, F1;
+        read(0, 0, F0);
+        for (int s = 0; s < steps; ++s) {
+            const bool load = s + 2 < steps;
+            if (load && (s + 2) % (GW_LIST / GW_ROWS) != 0) read_rows(s + 2);
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) av[set][mb] = fragment(As + kk * 16 * ROW + ((((wm >> 5) + mb) ^ place) << 6));
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) bv[set][nb] = fragment(Bs + kk * 16 * ROW + ((((wn >> 5) + nb) ^ place) << 6));
-            };
-            read(0, 0);
-#pragma unroll
-            for (int kk = 0; kk < GW_ROWS / 16; ++kk) {      // the next operands are on their way while these are multiplied
-                if (kk + 1 < GW_ROWS / 16) read(kk + 1, (kk + 1) & 1);
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-                    for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, false>(&av[kk & 1][mb], &bv[kk & 1][nb], acc[mb][nb]);
+            for (int kk = 0; kk < SUB; ++kk) {
+                Operands &now = kk & 1 ? F1 : F0, &ahead = kk & 1 ? F0 : F1;
+                if (kk + 1 < SUB) {
+                    read(s, kk + 1, ahead);
+                } else if (s + 1 < steps) {
+                    arrived<0>();
+                    if (load) {
+                        if ((s + 2) % (GW_LIST / GW_ROWS) == 0) {
+                            fill(k0 + (int64_t)(s + 2) * GW_ROWS);
+                            read_rows(s + 2);
+                        }
+                        load_step(s + 2);
+                    }
+                    read(s + 1, 0, ahead);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(now);
                 __builtin_amdgcn_sched_barrier(0);
             }
-        };
-
-        fill(k0);
-        load_step(0);
-        if (steps > 1) load_step(1);
-        for (int s = 0; s < steps; ++s) {
-            if (s + 1 < steps)
-                arrived<LOADS>();
-            else
-                arrived<0>();
-            multiply(s);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // every wavefront has read what it needs of the buffer
-            if (s + 2 < steps) {
-                if ((s + 2) % (GW_LIST / GW_ROWS) == 0) fill(k0 + (int64_t)(s + 2) * GW_ROWS);
-                load_step(s + 2);
-            }
         }
-        // a whole tile is the result; a part goes to this workgroup's slot 0 (the tile began before the share) or 1
-        const bool whole = first == 0 && last == steps_g;
-        float* to_part = A.dw_part + (int64_t)(2 * blockIdx.x + (at == blockIdx.x * S.per ? 0 : 1)) * BM * BN;
-        float* to_dw = A.dw + (int64_t)g * A.d_in * A.d_out;
+        const bool whole = W.first == 0 && W.last == W.steps_g;
+        float* to_part = A.dw_part + ((int64_t)(2 * range + (W.at == range * S.per ? 0 : 1)) * tiles + tile) * BM * BN;
+        float* to_dw = A.dw + (int64_t)W.g * A.d_in * A.d_out;
         int m_first = wm + 4 * half, c_first = wn + l32;      // (addresses are formed here: hoisted out of the loops they take registers those have not got)
         asm volatile("" : "+v"(m_first), "+v"(c_first));
 #pragma unroll
@@ -777,8 +807,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
                         to_dw[(int64_t)(m0 + m) * A.d_out + n0 + c] = acc[mb][nb][i];
                 }
             }
-        at += steps;
-        __syncthreads();      // the list may be filled again
+        __syncthreads();      // the list and the buffers may be filled again
     }
 }
 
@@ -793,11 +822,11 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
     const int tiles_n = (A.d_out + BN - 1) / BN, tiles = (A.d_in + BM - 1) / BM * tiles_n;
     const int part = blockIdx.x % PARTS, unit = blockIdx.x / PARTS, tile = unit % tiles, g = unit / tiles;
     if (tile / tiles_n * BM + part * VALUES / BN >= A.d_in) return;      // its rows do not exist
-    const Share S = share_of(A, tiles, ROWS);
-    const int64_t before = steps_before(A.G, g, ROWS) * tiles;
+    const Share S = share_of(A, ROWS);
+    const int64_t t0 = steps_before(A.G, g, ROWS);
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
     const int64_t steps_g = to > from ? (to - from + ROWS - 1) / ROWS : 0;
-    const int64_t t0 = before + tile * steps_g, t1 = t0 + steps_g;
+    const int64_t t1 = t0 + steps_g;
     const int64_t w0 = steps_g ? t0 / S.per : 0, w1 = steps_g ? (t1 - 1) / S.per : -1;
     if (steps_g && w0 == w1) return;      // one workgroup has written it
     const int run = threadIdx.x / SIDE, at = (threadIdx.x % SIDE) * 4;
@@ -807,7 +836,7 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
         double s[4] = {};
 #pragma unroll 4
         for (int64_t w = w0 + run; w <= w1; w += RUNS) {
-            const float4 v = *(const float4*)(A.dw_part + (2 * w + (t0 <= w * S.per ? 0 : 1)) * BM * BN + e);
+            const float4 v = *(const float4*)(A.dw_part + ((2 * w + (t0 <= w * S.per ? 0 : 1)) * tiles + tile) * BM * BN + e);
             s[0] += v.x, s[1] += v.y, s[2] += v.z, s[3] += v.w;
         }
         if constexpr (RUNS > 1) {
@@ -1040,7 +1069,7 @@ fg_status_t f32_product(const char* who, GlArgs& A, hipStream_t st) {
     return FG_OK;
 }
 
-// dW in fp32: the shares of grouped_dw_kernel, steps of GF_K entries, 128 x 128 tiles
+// dW in fp32: the ranges of grouped_dw_kernel, steps of GF_K entries, 128 x 128 tiles
 __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A) {
     constexpr int TILE = 128;
     typedef F32Operand<TILE, true> OP;
@@ -1048,27 +1077,15 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
     int32_t* list = (int32_t*)(gl_lds + gf_lds_bytes(TILE));
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int tiles_n = (A.d_out + TILE - 1) / TILE, tiles = (A.d_in + TILE - 1) / TILE * tiles_n;
-    const Share S = share_of(A, tiles, GF_K);
-    int64_t at = blockIdx.x * S.per;
-    const int64_t end = at + S.per < S.total ? at + S.per : S.total;
+    int range, tile;
+    if (!range_and_tile(A, tiles, range, tile)) return;
+    const Share S = share_of(A, GF_K);
+    RangeWalk W = {range * S.per, (range + 1) * S.per < S.total ? (range + 1) * S.per : S.total, 0, 0};
     const int wm = (wave >> 1) * (TILE / 2), wn = (wave & 1) * (TILE / 2);
-    int g = 0;
-    int64_t before = 0;
-    while (at < end) {      // uniform over the workgroup
-        int64_t from, to, steps_g;
-        for (;; ++g) {
-            from = group_offset(A.G, g);
-            to = group_offset(A.G, g + 1);
-            steps_g = to > from ? (to - from + GF_K - 1) / GF_K : 0;
-            if (at < before + steps_g * tiles) break;
-            before += steps_g * tiles;
-        }
-        const int tile = (int)((at - before) / steps_g);
-        const int64_t first = at - before - tile * steps_g;
-        const int64_t last = first + (end - at) < steps_g ? first + (end - at) : steps_g;
-        const int steps = (int)(last - first);
-        const int64_t k0 = from + first * GF_K, k1 = from + last * GF_K < to ? from + last * GF_K : to;
-        const int m0 = (tile / tiles_n) * TILE, n0 = (tile % tiles_n) * TILE;
+    const int m0 = (tile / tiles_n) * TILE, n0 = (tile % tiles_n) * TILE;
+    for (; W.next(A.G, GF_K); W.at += W.last - W.first) {      // uniform over the workgroup
+        const int steps = (int)(W.last - W.first);
+        const int64_t k0 = W.k0, k1 = W.k1;
         const int c = (t % OP::PER_ROW) * 4;
         const int64_t ca = (m0 + c < A.d_in ? m0 + c : 0) * 4, cb = (n0 + c < A.d_out ? n0 + c : 0) * 4;
         fg_u32x4 ra[OP::LOADS], rb[OP::LOADS];
@@ -1114,9 +1131,9 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
             f32_multiply<TILE, true, true>(gl_lds, wm, wn, lane, C);
             __syncthreads();
         }
-        const bool whole = first == 0 && last == steps_g;
-        float* to_part = A.dw_part + (int64_t)(2 * blockIdx.x + (at == blockIdx.x * S.per ? 0 : 1)) * TILE * TILE;
-        float* to_dw = A.dw + (int64_t)g * A.d_in * A.d_out;
+        const bool whole = W.first == 0 && W.last == W.steps_g;
+        float* to_part = A.dw_part + ((int64_t)(2 * range + (W.at == range * S.per ? 0 : 1)) * tiles + tile) * TILE * TILE;
+        float* to_dw = A.dw + (int64_t)W.g * A.d_in * A.d_out;
         int m_first = wm + 4 * (lane >> 5), n_first = wn + (lane & 31);      // (formed here, as above)
         asm volatile("" : "+v"(m_first), "+v"(n_first));
 #pragma unroll
@@ -1134,7 +1151,6 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
                         to_dw[(int64_t)(m0 + m) * A.d_out + n0 + n] = v;
                 }
             }
-        at += steps;
     }
 }
 
@@ -1147,7 +1163,7 @@ int64_t dz_row(int d_out, int e) {
 // The workspace of a backward call: dz, column sums by tile, parts of dW
 struct BwPlan {
     bool dz;
-    int bm, shares;
+    int bm, ranges, grid;      // tile, ranges of rows, workgroups of the weight gradients
     size_t dz_bytes, db_bytes, dw_bytes;
     size_t total() const { return dz_bytes + db_bytes + dw_bytes + 16; }
 };
@@ -1157,12 +1173,16 @@ BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
     P.dz = true;
     P.bm = e == 2 && (d_in > 128 || d_out > 128) ? 256 : 128;
     const int64_t tiles = fg_ceil_div(d_in, P.bm) * fg_ceil_div(d_out, P.bm);
-    const int64_t steps = (max_rows / (e == 4 ? GF_K : GW_ROWS) + (n_groups < max_rows ? n_groups : max_rows)) * tiles;
-    const int most = P.bm == 256 ? 256 : 512;      // as many as run at once
-    P.shares = steps < 1 ? 1 : (int)(steps < most ? steps : most);
+    // as many ranges as give every place on the chip a tile; of more tiles than places two ranges where that leaves fewer of them idle
+    const int64_t steps = max_rows / (e == 4 ? GF_K : GW_ROWS) + (n_groups < max_rows ? n_groups : max_rows), places = P.bm == 256 ? 256 : 512;
+    int64_t ranges = places / tiles;
+    if (ranges < 1) ranges = fg_ceil_div(2 * tiles, places) < 2 * fg_ceil_div(tiles, places) ? 2 : 1;
+    if (ranges > steps) ranges = steps < 1 ? 1 : steps;
+    P.ranges = (int)ranges;
+    P.grid = (int)(fg_ceil_div(ranges * tiles, 8) * 8);
     P.dz_bytes = fg_align_up((size_t)max_rows * dz_row(d_out, e), 256);
     P.db_bytes = fg_align_up((size_t)(max_rows / GZ_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * d_out * 4, 256);
-    P.dw_bytes = (size_t)2 * P.shares * P.bm * P.bm * 4;
+    P.dw_bytes = P.ranges > 1 ? (size_t)2 * P.ranges * tiles * P.bm * P.bm * 4 : 0;
     return P;
 }
 
@@ -1225,10 +1245,10 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
             FG_TRY((tile_product<T, false, false>(who, A, st)));
     }
     if (A.dw) {
-        A.shares = P.shares, A.min_share = 1;
+        A.ranges = P.ranges;
         const int64_t sums = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm / ds_values(P.bm));
         if (sums > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
-        const dim3 grid((unsigned)P.shares), sum_grid((unsigned)sums);
+        const dim3 grid((unsigned)P.grid), sum_grid((unsigned)sums);
         if constexpr (T == FG_F32) {
             hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), gf_lds_bytes(128) + GW_LIST * 4, st, A);
             hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GF_K>), sum_grid, dim3(GZ_THREADS), 0, st, A);
