@@ -125,10 +125,11 @@ __device__ __forceinline__ void arrived() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// 8-bit products. The 8-bit matrix instructions do not add up in fp32: they drop bits of products that are much smaller than the largest of
-// the same instruction (measured against exact sums: 1.3e-5 of the result's norm for normally distributed rows, 6e-5 for rows whose values
-// spread over e^2; the 64-deep and the 16-deep one alike). Beside the 2e-3 of an output in 16 bits that is nothing and they are twice as fast;
-// for an output in fp32 (WIDE) the operands become bf16, which holds every 8-bit value, and are multiplied as such: 3e-7.
+// 8-bit products. The 8-bit matrix instructions add groups of eight adjacent products with 13 bits below the largest of the group (measured: of 2^16
+// and 1 in one group the 1 is lost, in two groups it is not; the sums are off by up to 1.5e-4 of the largest product), the groups in fp32. An
+// output in bf16, which is rounded to 2^-8, takes that for twice the rate: 1.3e-5 of the result's norm for normally distributed rows, 6e-5 for rows
+// whose values spread over e^2, beside 1.7e-3 of the rounding. For the other outputs (WIDE) the operands become bf16, which holds every 8-bit
+// value, and are multiplied as such, in fp32 throughout: 1e-7.
 template <int T, bool WIDE>
 __device__ __forceinline__ gl_f32x16 mfma(const fg_u32x4* a, const fg_u32x4* b, gl_f32x16 c) {
     if constexpr (T == FG_BF16)
@@ -170,7 +171,6 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
     constexpr int DEEP = T == FG_E4M3 && !WIDE ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
     constexpr int PARTS = T == FG_E4M3 ? 2 : 1;                                          // 16-byte registers of it
-    constexpr bool AHEAD = PARTS == 1 || BM < 256;                                        // (two sets of the long operands do not fit the registers)
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
     static_assert(A_LOADS * GL_ROWS * WAVES == BM && B_LOADS * GL_ROWS * WAVES == BN, "whole loads");
@@ -361,22 +361,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         constexpr bool LAST = decltype(last)::value, LOAD = decltype(load)::value;
 #pragma unroll
         for (int kk = 0; kk < SUB; ++kk) {
-            Operands &now = AHEAD && (kk & 1) ? F1 : F0, &ahead = AHEAD && !(kk & 1) ? F1 : F0;
+            Operands &now = kk & 1 ? F1 : F0, &ahead = kk & 1 ? F0 : F1;
             if (kk + 1 < SUB) {
-                if (AHEAD) read(s, kk + 1, ahead);
+                read(s, kk + 1, ahead);
             } else if (!LAST) {
                 if (s == 0)
                     arrived_first(std::integral_constant<int, 0>());
                 else
                     arrived<0>();
                 if (LOAD) load_step(s + 2);
-                if (AHEAD) read(s + 1, 0, ahead);
+                read(s + 1, 0, ahead);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply(now);
             __builtin_amdgcn_sched_barrier(0);
-            if (!AHEAD && kk + 1 < SUB) read(s, kk + 1, F0);
-            if (!AHEAD && kk + 1 == SUB && !LAST) read(s + 1, 0, F0);
         }
     };
 
@@ -516,7 +514,7 @@ fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
 template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
-    if constexpr (T != FG_E4M3)
+    if constexpr (T != FG_E4M3 || WIDE)      // (two sets of the 8-bit instruction's long operands do not fit the registers of a 256 x 256 tile)
         if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
     if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
@@ -1291,7 +1289,7 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
     if (dtype == FG_BF16) return tile_product<FG_BF16, true, false>(who, A, (hipStream_t)stream);
     if (dtype == FG_F16) return tile_product<FG_F16, true, false>(who, A, (hipStream_t)stream);
-    if (dtype == FG_E4M3 && out_dtype == FG_F32) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
+    if (dtype == FG_E4M3 && out_dtype != FG_BF16) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
     if (dtype == FG_E4M3) return tile_product<FG_E4M3, false, false>(who, A, (hipStream_t)stream);
     return f32_product<true>(who, A, (hipStream_t)stream);
 }

@@ -229,6 +229,93 @@ def test_linear_grouped(B, dtype, out, n, n_groups, d_in, d_out, options):
     assert np.array_equal(bad, order)
 
 
+def large(dtype, out, n, n_groups, d_in, d_out, options=""):
+    """A call whose tiles are several to a workgroup, on the GPU in fp64 (products of contiguous operands)."""
+    g = torch.Generator(device="cuda").manual_seed(n + d_in + d_out)
+    kw = dict(device="cuda", generator=g)
+    rows = torch.randperm(n, **kw)[:n - n // 7]
+    types = torch.randint(0, n_groups, (len(rows),), **kw).sort()
+    order = rows[torch.argsort(torch.rand(len(rows), **kw))].int()
+    offsets = torch.searchsorted(types.values, torch.arange(n_groups + 1, device="cuda"))
+    src = torch.randint(0, n, (n,), **kw).int() if "src" in options else None
+    x = torch.randn(n, d_in, **kw)
+    W = torch.randn(n_groups, d_in, d_out, **kw) / math.sqrt(d_in)
+    return order, offsets, src, x, W, torch.randn(n_groups, d_out, **kw)
+
+
+LARGE = [  # tiles of 256, 128 and 64 rows, one step of the contraction and several, whole steps and parts of one
+    ("bf16", "bf16", 33_500, 3, 64, 264, "src relu"), ("bf16", "f32", 70_001, 2, 72, 256, ""), ("f16", "f16", 40_000, 5, 200, 512, "src"),
+    ("f16", "f32", 36_000, 40, 136, 264, "relu"), ("bf16", "bf16", 33_100, 4, 328, 520, ""), ("bf16", "bf16", 70_500, 3, 40, 128, "relu"), ("f16", "f16", 71_000, 9, 264, 72, "src"),
+    ("bf16", "f32", 72_000, 2, 64, 64, ""), ("f16", "f16", 90_000, 1024, 136, 40, "src relu"), ("bf16", "bf16", 130_000, 1, 8, 16, ""),
+    ("e4m3", "bf16", 70_000, 3, 128, 256, "src relu"), ("e4m3", "f32", 40_000, 4, 272, 512, "relu"), ("e4m3", "bf16", 36_000, 7, 400, 264, ""), ("e4m3", "f16", 90_000, 2, 16, 48, ""),
+    ("f32", "f32", 50_000, 3, 100, 256, "src relu"), ("f32", "f32", 34_000, 60, 36, 132, ""), ("f32", "f32", 70_000, 2, 260, 64, "relu"),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype, out, n, n_groups, d_in, d_out, options", LARGE)
+def test_linear_grouped_of_many_rows(B, dtype, out, n, n_groups, d_in, d_out, options):
+    order, offsets, src, x, W, bias = large(dtype, out, n, n_groups, d_in, d_out, options)
+    relu = "relu" in options
+    xs = ws = None
+    if dtype == "e4m3":
+        xq, xs = R.quantise(x)
+        wq, ws = R.quantise(W.transpose(1, 2).contiguous().reshape(n_groups * d_out, d_in))
+        x64, W64 = xq.double() * xs.double()[:, None], (wq.double() * ws.double()[:, None]).reshape(n_groups, d_out, d_in).transpose(1, 2).contiguous()
+        x, W = xq.to(torch.float8_e4m3fn), wq.to(torch.float8_e4m3fn)
+    else:
+        x, W = x.to(T[dtype]), W.to(T[dtype])
+        x64, W64 = x.double(), W.double()
+    h = torch.full((n, d_out), -77.0, dtype=T[out], device="cuda")
+    # twice, the second time over the first one's results: nothing may depend on what was there
+    for _ in range(2):
+        B.fg_linear_grouped(x, n, stride(x), code(B, dtype), xs, src, order, offsets, len(order), n_groups, d_in, d_out, W, ws, bias, int(relu), h, n, stride(h),
+                            code(B, out))
+    torch.cuda.synchronize()
+    want, size = torch.full((n, d_out), -77.0, dtype=torch.float64, device="cuda"), torch.zeros(n, d_out, dtype=torch.float64, device="cuda")
+    at = offsets.tolist()
+    for g in range(n_groups):
+        pos = order[at[g]:at[g + 1]].long()
+        a = x64[src[pos].long() if src is not None else pos]
+        v = torch.mm(a, W64[g]) + bias[g].double()
+        want[pos] = v.clamp_min(0) if relu else v
+        size[pos] = torch.mm(a.abs(), W64[g].abs()) + bias[g].double().abs()
+    close(h, want, (d_in + 8) * 2.0 ** -23 * size + HALF[out] * want.abs() + TINY[out], f"{dtype} {n} x {d_in} x {d_out}")
+
+
+@gpu
+@pytest.mark.parametrize("dtype, out, n, n_groups, d_in, d_out", [("bf16", "bf16", 40_000, 3, 264, 136), ("f16", "f32", 70_000, 2, 256, 64), ("bf16", "f32", 33_500, 40, 520, 264),
+                                                                   ("f32", "f32", 45_000, 3, 88, 256), ("bf16", "bf16", 50_000, 1, 64, 64), ("f16", "f16", 9_000, 300, 72, 40),
+                                                                   ("f32", "f32", 33_000, 5, 132, 400)])
+def test_linear_grouped_backward_of_many_rows(B, dtype, out, n, n_groups, d_in, d_out):
+    order, offsets, _, x, W, _ = large(dtype, out, n, n_groups, d_in, d_out)
+    x, W = x.to(T[dtype]), W.to(T[dtype])
+    dh, h = torch.randn(n, d_out, device="cuda").to(T[dtype]), torch.randn(n, d_out, device="cuda").to(T[dtype])
+    dx = torch.full((n, d_in), -77.0, dtype=T[out], device="cuda")
+    dw, db = torch.full((n_groups, d_in, d_out), -77.0, device="cuda"), torch.full((n_groups, d_out), -77.0, device="cuda")
+    ws = torch.full((B.fg_linear_grouped_backward_workspace_bytes(code(B, dtype), len(order), n_groups, d_in, d_out),), 255, dtype=torch.uint8, device="cuda")
+    for mask in (h, None):
+        for _ in range(2):
+            B.fg_linear_grouped_backward(x, n, stride(x), code(B, dtype), None, dh, stride(dh), code(B, dtype), mask, stride(h) if mask is not None else 0, n, order, offsets,
+                                         len(order), n_groups, d_in, d_out, W, dx, stride(dx), code(B, out), dw, db, ws, ws.numel())
+        torch.cuda.synchronize()
+        z = dh.double() if mask is None else torch.where(h > 0, dh.double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+        at = offsets.tolist()
+        for g in range(n_groups):
+            pos = order[at[g]:at[g + 1]].long()
+            zg, xg, wt = z[pos], x[pos].double(), W[g].double().T.contiguous()
+            want = torch.mm(zg, wt)
+            close(dx[pos], want, (d_out + 8) * 2.0 ** -23 * torch.mm(zg.abs(), wt.abs()) + HALF[out] * want.abs() + TINY[out], "dx")
+            # rows' sums in fp32: a rounding of 2^-24 of the running sum a row at most, granted twice as everywhere here
+            rows = len(pos) + 16
+            xt = xg.T.contiguous()
+            want = torch.mm(xt, zg)
+            close(dw[g], want, rows * 2.0 ** -23 * torch.mm(xt.abs(), zg.abs()) + 2.0 ** -24 * want.abs(), "dW")
+            close(db[g], zg.sum(0), rows * 2.0 ** -23 * zg.abs().sum(0), "db")
+            if len(pos) > 2000:      # and as near as sums of independent roundings are: the square root of that
+                assert float((dw[g].double() - want).norm() / want.norm()) < 2e-6
+
+
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "e4m3"])
 def test_linear_grouped_skips_what_is_out_of_range(B, dtype):
