@@ -154,6 +154,33 @@ __device__ __forceinline__ void widen(fg_u32x4 v, fg_u32x4 (&out)[2]) {
     }
 }
 
+typedef float gf_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 gf_bf16x2 __attribute__((ext_vector_type(2)));
+
+// four values -> two words of each of their three terms
+__device__ __forceinline__ void split4(fg_u32x4 v, fg_u32x2 (&u)[3]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+        gf_f32x2 x = {__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])};
+#pragma unroll
+        for (int term = 0; term < 3; ++term) {
+            u[term][p] = __builtin_bit_cast(unsigned int, __builtin_convertvector(x, gf_bf16x2));
+            x = gf_f32x2{x[0] - __uint_as_float(u[term][p] << 16), x[1] - __uint_as_float(u[term][p] & 0xFFFF0000u)};
+        }
+    }
+}
+
+// eight values -> their three terms
+__device__ __forceinline__ void split8(const fg_u32x4 (&v)[2], fg_u32x4 (&u)[3]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        fg_u32x2 w[3];
+        split4(v[h], w);
+#pragma unroll
+        for (int term = 0; term < 3; ++term) u[term][2 * h] = w[term][0], u[term][2 * h + 1] = w[term][1];
+    }
+}
+
 constexpr int GL_STEP = 128, GL_PIECES = GL_STEP / 16, GL_ROWS = 1024 / GL_STEP;      // bytes of K per step; 16-byte pieces of a row; rows of a load
 constexpr int EP_BLOCK = 16 * 128;      // bytes of an epilogue's block
 // the operands' ring, the epilogue's blocks, what belongs to a tile (twice), the offsets
@@ -166,11 +193,11 @@ __device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise
 template <int T, int BM, int BN, int WAVES_M, int WAVES_N, int RING, bool B_KN, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
-    constexpr int E = T == FG_E4M3 ? 1 : 2, BK = GL_STEP / E;
+    constexpr int E = T == FG_E4M3 ? 1 : T == FG_F32 ? 4 : 2, BK = GL_STEP / E;
     constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / GL_ROWS / WAVES, B_LOADS = BN / GL_ROWS / WAVES, LOADS = A_LOADS + B_LOADS;
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
-    constexpr int DEEP = T == FG_E4M3 && !WIDE ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
-    constexpr int PARTS = T == FG_E4M3 ? 2 : 1;                                          // 16-byte registers of it
+    constexpr int DEEP = T == FG_F32 || (T == FG_E4M3 && !WIDE) ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
+    constexpr int PARTS = T == FG_E4M3 || T == FG_F32 ? 2 : 1;                                          // 16-byte registers of it
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
     static_assert(A_LOADS * GL_ROWS * WAVES == BM && B_LOADS * GL_ROWS * WAVES == BN, "whole loads");
@@ -254,7 +281,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     const int a_row = GL_ROWS * wave + lane / GL_PIECES, a_piece = (lane % GL_PIECES) ^ exchanged(a_row), ka = a_piece * (16 / E);
     static_assert(GL_ROWS * WAVES % (2 * GL_PIECES) == 0, "the same exchange for all loads of a lane");
     const char* const zero = (const char*)gl_zero;
-    auto b_window = [](int row) { return BN >= 128 ? row & 3 : (row >> 1) & 1; };      // what a row's windows are exchanged by (BN = 64: it has two)
+    // what a row's windows are exchanged by (BN = 64: it has two); fp32: windows of 128 bytes, so that the halves of a wavefront, four rows apart, read
+    // different banks
+    auto b_window = [](int row) { return T == FG_F32 ? (row >> 2) & 1 : BN >= 128 ? row & 3 : (row >> 1) & 1; };
     auto begin = [&](const Tile& F, const TileData& D) {
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) {
@@ -266,7 +295,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         for (int i = 0; i < B_LOADS; ++i) {
             if constexpr (B_KN) {
                 const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
-                const int c = F.n0 + (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
+                const int c = F.n0 + (T == FG_F32 ? (((slot >> 3) ^ b_window(row)) * 8 + (slot & 7)) * 4 : (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8);
                 pb[i] = (unsigned int)(row * N + (c < N ? c : 0)) * E;
             } else {
                 const int c = F.n0 + a_row + GL_ROWS * WAVES * i;
@@ -299,7 +328,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 
     const int l32 = lane & 31, half = lane >> 5;
     const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * WN;
-    gl_f32x16 acc[MB][NB];
+    gl_f32x16 acc[MB][NB], rest[T == FG_F32 ? MB : 1][T == FG_F32 ? NB : 1];      // fp32: the leading products, the others
     const int swap = exchanged(l32) << 4;
     static_assert(RING == 2 && SUB % 2 == 0, "one step ahead; the operands' two sets in turn");
     const int place = (lane >> 2) & 3;
@@ -319,7 +348,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) F.b[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + at);
         }
-        if constexpr (B_KN)
+        if constexpr (B_KN && T == FG_F32)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                const char* from = Bs + (kk * 16 + 4 * half) * B_ROW + ((((wn >> 5) + nb) ^ half) << 7) + l32 * 4;      // (k as the pieces of A lie)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) F.b[nb][e >> 2][e & 3] = *(const unsigned int*)(from + (e + (e & 4)) * B_ROW);
+            }
+        else if constexpr (B_KN)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
                 typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
@@ -330,6 +366,24 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             }
     };
     auto multiply = [&](Operands& F) {
+        if constexpr (T == FG_F32) {
+            fg_u32x4 a[MB][3];
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) split8(F.a[mb], a[mb]);
+            constexpr int TA[5] = {2, 0, 1, 1, 0}, TB[5] = {0, 2, 1, 0, 1};      // smallest products first
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                fg_u32x4 b[3];
+                split8(F.b[nb], b);
+#pragma unroll
+                for (int e = 0; e < 5; ++e)
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) rest[mb][nb] = mfma<FG_BF16, false>(&b[TB[e]], &a[mb][TA[e]], rest[mb][nb]);
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb) acc[mb][nb] = mfma<FG_BF16, false>(&b[0], &a[mb][0], acc[mb][nb]);
+            }
+            return;
+        }
         if constexpr (WIDE) {
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) widen(F.a[mb][0], F.a[mb]);
@@ -339,7 +393,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], F.a[mb], acc[mb][nb]);
+            for (int nb = 0; nb < NB; ++nb)
+                if constexpr (T != FG_F32) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], F.a[mb], acc[mb][nb]);
     };
     // The stores of a tile are younger than the next one's first two steps' loads: those are waited for with the stores left on their way
     constexpr int STORES = MB * NB * 2;
@@ -408,6 +463,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
+                    if constexpr (T == FG_F32)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[mb][nb][4 * q + e] += rest[mb][nb][4 * q + e];
                     if constexpr (T == FG_E4M3) {
                         const int cl = wn + nb * 32 + 8 * q + 4 * half;
                         const float4 b = *(const float4*)(D.bias + cl), ws = *(const float4*)(D.w_scale + cl);
@@ -468,7 +526,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
                 float4 b = {0.f, 0.f, 0.f, 0.f};
                 if constexpr (T != FG_E4M3) b = *(const float4*)(data[which].bias + wn + nb * 32 + 8 * q + 4 * half);
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) acc[mb][nb][4 * q] = b.x, acc[mb][nb][4 * q + 1] = b.y, acc[mb][nb][4 * q + 2] = b.z, acc[mb][nb][4 * q + 3] = b.w;
+                for (int mb = 0; mb < MB; ++mb) {
+                    if constexpr (T == FG_F32)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) rest[mb][nb][4 * q + e] = 0.f;
+                    acc[mb][nb][4 * q] = b.x, acc[mb][nb][4 * q + 1] = b.y, acc[mb][nb][4 * q + 2] = b.z, acc[mb][nb][4 * q + 3] = b.w;
+                }
             }
         if (steps > 1)
             arrived_first(std::integral_constant<int, LOADS>());
@@ -514,7 +577,7 @@ fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
 template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
-    if constexpr (T != FG_E4M3 || WIDE)      // (two sets of the 8-bit instruction's long operands do not fit the registers of a 256 x 256 tile)
+    if constexpr (T != FG_F32 && (T != FG_E4M3 || WIDE))      // (fp32 has two sums; two sets of the 8-bit instruction's long operands do not fit the registers of a 256 x 256 tile)
         if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
     if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
@@ -863,22 +926,6 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
 // two workgroups of a compute unit fill each other's waits.
 constexpr int GF_THREADS = 256, GF_K = 32;
 constexpr size_t gf_lds_bytes(int tile) { return (size_t)2 * 3 * tile * GF_K * 2; }
-typedef float gf_f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 gf_bf16x2 __attribute__((ext_vector_type(2)));
-
-// four values -> two words of each of their three terms
-__device__ __forceinline__ void split4(fg_u32x4 v, fg_u32x2 (&u)[3]) {
-#pragma unroll
-    for (int p = 0; p < 2; ++p) {
-        gf_f32x2 x = {__uint_as_float(v[2 * p]), __uint_as_float(v[2 * p + 1])};
-#pragma unroll
-        for (int term = 0; term < 3; ++term) {
-            u[term][p] = __builtin_bit_cast(unsigned int, __builtin_convertvector(x, gf_bf16x2));
-            x = gf_f32x2{x[0] - __uint_as_float(u[term][p] << 16), x[1] - __uint_as_float(u[term][p] & 0xFFFF0000u)};
-        }
-    }
-}
-
 // One operand: TILE rows (KC) or columns (KN) by GF_K
 template <int TILE, bool KN>
 struct F32Operand {
@@ -956,115 +1003,6 @@ __device__ __forceinline__ void f32_multiply(const char* lds, int wm, int wn, in
 #pragma unroll
             for (int j = 0; j < NB; ++j) S.lead[i][j] = mfma<FG_BF16, false>(&a[i][0], &b[j][0], S.lead[i][j]);
     }
-}
-
-template <int TILE, bool B_KN>
-__global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_kernel(GlArgs A) {
-    typedef F32Operand<TILE, false> OA;
-    typedef F32Operand<TILE, B_KN> OB;
-    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
-    __shared__ int32_t pos[TILE], src[TILE];
-    const int xcd = blockIdx.x & 7, j = blockIdx.x >> 3;      // column tiles of a row tile on one XCD
-    int g;
-    int64_t k0, k1;
-    if (!find_tile(A.G, (int64_t)(j / A.tiles_n) * 8 + xcd, TILE, g, k0, k1)) return;
-    const int n0 = (j % A.tiles_n) * TILE;
-    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int K = A.K, N = A.N;
-    if (t < TILE) {
-        int32_t r, s;
-        entry(A, k0 + t, k1, r, s);
-        pos[t] = r;
-        src[t] = r < 0 ? -1 : (A.a_by == GL_A_SOURCE ? s : A.a_by == GL_A_POSITION ? r : (int32_t)(k0 + t));
-    }
-    __syncthreads();
-    // (a row or column that does not exist reads the first one there is, a k beyond K the first: zeroed when they are written to LDS)
-    const float* pa[OA::LOADS];
-    const int ka = (t % OA::PER_ROW) * 4;
-#pragma unroll
-    for (int i = 0; i < OA::LOADS; ++i) {
-        const int32_t r = src[OA::row_of(t, i)];
-        pa[i] = (const float*)(A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride);
-    }
-    const float* w0 = (const float*)A.W + (int64_t)g * K * N;
-    const float* pb[OB::LOADS];
-    const int pb_c = (t % OB::PER_ROW) * 4;      // column (KN) or k (KC) of the thread's pieces
-#pragma unroll
-    for (int i = 0; i < OB::LOADS; ++i) {
-        const int row = OB::row_of(t, i);
-        if constexpr (B_KN)
-            pb[i] = w0 + (n0 + pb_c < N ? n0 + pb_c : 0);
-        else
-            pb[i] = w0 + (int64_t)(n0 + row < N ? n0 + row : 0) * K;
-    }
-    fg_u32x4 ra[OA::LOADS], rb[OB::LOADS];
-    auto load = [&](int k) {
-        const int kk = k + ka < K ? k + ka : 0;
-#pragma unroll
-        for (int i = 0; i < OA::LOADS; ++i) ra[i] = *(const fg_u32x4*)(pa[i] + kk);
-#pragma unroll
-        for (int i = 0; i < OB::LOADS; ++i) {
-            if constexpr (B_KN) {
-                const int row = k + OB::row_of(t, i);
-                rb[i] = *(const fg_u32x4*)(pb[i] + (int64_t)(row < K ? row : 0) * N);
-            } else {
-                rb[i] = *(const fg_u32x4*)(pb[i] + (k + pb_c < K ? k + pb_c : 0));
-            }
-        }
-    };
-    auto store = [&](int k) {
-        const fg_u32x4 none = {0u, 0u, 0u, 0u};
-#pragma unroll
-        for (int i = 0; i < OA::LOADS; ++i) OA::put(gl_lds, t, i, k + ka < K ? ra[i] : none);
-#pragma unroll
-        for (int i = 0; i < OB::LOADS; ++i) OB::put(gl_lds + 3 * OA::TERM, t, i, k + (B_KN ? OB::row_of(t, i) : pb_c) < K ? rb[i] : none);
-    };
-    const int wm = (wave >> 1) * (TILE / 2), wn = (wave & 1) * (TILE / 2);
-    F32Sums<TILE> S;
-    S.clear();
-    load(0);
-    for (int k = 0; k < K; k += GF_K) {
-        store(k);
-        __syncthreads();
-        load(k + GF_K);      // beyond K: valid addresses, not used
-        __builtin_amdgcn_sched_barrier(0);
-        f32_multiply<TILE, false, B_KN>(gl_lds, wm, wn, lane, S);
-        __syncthreads();
-    }
-    // accumulator element i of a block is its row 8 * (i / 4) + 4 * half + i % 4, column l32
-    const int l32 = lane & 31, half = lane >> 5;
-#pragma unroll
-    for (int b = 0; b < F32Sums<TILE>::B; ++b) {
-        const int c = n0 + wn + 32 * b + l32;
-        if (c >= N) continue;
-        const double bias = A.bias ? (double)A.bias[(int64_t)g * N + c] : 0.0;
-#pragma unroll
-        for (int a = 0; a < F32Sums<TILE>::B; ++a)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int32_t r = pos[wm + 32 * a + 8 * (i >> 2) + 4 * half + (i & 3)];
-                if (r < 0) continue;
-                float v = (float)((double)S.lead[a][b][i] + (double)S.rest[a][b][i] + bias);
-                if (A.relu) v = v < 0.f ? 0.f : v;
-                *(float*)(A.out + (int64_t)r * A.out_stride + (int64_t)c * 4) = v;
-            }
-    }
-}
-
-// out[r, :] = a[., :] . B in fp32 (as tile_product)
-template <bool B_KN>
-fg_status_t f32_product(const char* who, GlArgs& A, hipStream_t st) {
-    const int tile = A.G.max_rows / 128 * fg_ceil_div(A.N, 128) >= 256 && A.N > 64 ? 128 : 64;
-    A.tiles_n = (int)fg_ceil_div(A.N, tile);
-    const int64_t rows = A.G.max_rows / tile + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
-    const int64_t grid = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
-    if (grid > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
-    if (tile == 128)
-        hipLaunchKernelGGL((grouped_f32_kernel<128, B_KN>), dim3((unsigned)grid), dim3(GF_THREADS), gf_lds_bytes(128), st, A);
-    else
-        hipLaunchKernelGGL((grouped_f32_kernel<64, B_KN>), dim3((unsigned)grid), dim3(GF_THREADS), gf_lds_bytes(64), st, A);
-    FG_LAUNCH_CHECK("grouped_f32_kernel");
-    return FG_OK;
 }
 
 // dW in fp32: the ranges of grouped_dw_kernel, steps of GF_K entries, 128 x 128 tiles
@@ -1237,10 +1175,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     }
     if (A.out && work) {
         A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
-        if constexpr (T == FG_F32)
-            FG_TRY(f32_product<false>(who, A, st));
-        else
-            FG_TRY((tile_product<T, false, false>(who, A, st)));
+        FG_TRY((tile_product<T, false, false>(who, A, st)));
     }
     if (A.dw) {
         A.ranges = P.ranges;
@@ -1291,7 +1226,7 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     if (dtype == FG_F16) return tile_product<FG_F16, true, false>(who, A, (hipStream_t)stream);
     if (dtype == FG_E4M3 && out_dtype != FG_BF16) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
     if (dtype == FG_E4M3) return tile_product<FG_E4M3, false, false>(who, A, (hipStream_t)stream);
-    return f32_product<true>(who, A, (hipStream_t)stream);
+    return tile_product<FG_F32, true, false>(who, A, (hipStream_t)stream);
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
