@@ -336,18 +336,18 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     struct Operands {
         fg_u32x4 a[MB][PARTS], b[NB][PARTS];
     };
-    auto read = [&](int s, int kk, Operands& F) {
+    auto read_a = [&](int s, int kk, int mb, Operands& F) {
         const char* As = gl_lds + (unsigned)s % RING * STAGE + (wm + l32) * GL_STEP;
+#pragma unroll
+        for (int q = 0; q < DEEP; ++q) F.a[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + ((((kk * DEEP + q) * 2 + half) << 4) ^ swap));
+    };
+    auto read_b = [&](int s, int kk, Operands& F) {
         const char* Bs = gl_lds + (unsigned)s % RING * STAGE + BM * GL_STEP;
+        if constexpr (!B_KN)
 #pragma unroll
-        for (int q = 0; q < DEEP; ++q) {
-            const int at = (((kk * DEEP + q) * 2 + half) << 4) ^ swap;
+            for (int q = 0; q < DEEP; ++q)
 #pragma unroll
-            for (int mb = 0; mb < MB; ++mb) F.a[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + at);
-            if constexpr (!B_KN)
-#pragma unroll
-                for (int nb = 0; nb < NB; ++nb) F.b[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + at);
-        }
+                for (int nb = 0; nb < NB; ++nb) F.b[nb][q] = *(const fg_u32x4*)(Bs + (wn + nb * 32 + l32) * GL_STEP + ((((kk * DEEP + q) * 2 + half) << 4) ^ swap));
         if constexpr (B_KN && T == FG_F32)
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
@@ -364,6 +364,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
                 const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 4 * B_ROW));
                 F.b[nb][0] = __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
             }
+    };
+    auto multiply_row = [&](const Operands& F, int mb) {
+        if constexpr (T != FG_F32) {
+            fg_u32x4 a[2];
+            if constexpr (WIDE) widen(F.a[mb][0], a);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], WIDE ? a : F.a[mb], acc[mb][nb]);
+        }
     };
     auto multiply = [&](Operands& F) {
         if constexpr (T == FG_F32) {
@@ -382,19 +390,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
                 for (int mb = 0; mb < MB; ++mb) acc[mb][nb] = mfma<FG_BF16, false>(&b[0], &a[mb][0], acc[mb][nb]);
             }
-            return;
         }
-        if constexpr (WIDE) {
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) widen(F.a[mb][0], F.a[mb]);
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb) widen(F.b[nb][0], F.b[nb]);
-        }
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-                if constexpr (T != FG_F32) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], F.a[mb], acc[mb][nb]);
     };
     // The stores of a tile are younger than the next one's first two steps' loads: those are waited for with the stores left on their way
     constexpr int STORES = MB * NB * 2;
@@ -409,27 +405,42 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         else
             arrived<N + 2 * STORES>();
     };
-    // One step: its operands are read one set ahead of the matrix instructions; the last set is multiplied while the first of the next step
-    // is read. LAST: there is no next step, LOAD: there is one after it, whose loads set out.
+    // One step: its operands are read one set ahead of the matrix instructions, a row of blocks of them before each row is multiplied; the last set is
+    // multiplied while the first of the next step is read. LAST: there is no next step, LOAD: there is one after it, whose loads set out.
     Operands F0, F1;
     auto step = [&](int s, auto last, auto load) {
         constexpr bool LAST = decltype(last)::value, LOAD = decltype(load)::value;
 #pragma unroll
         for (int kk = 0; kk < SUB; ++kk) {
+            if (LAST && kk > 0 && kk * (BK / SUB) >= K - s * BK) break;      // (nothing but zeros beyond K)
             Operands &now = kk & 1 ? F1 : F0, &ahead = kk & 1 ? F0 : F1;
-            if (kk + 1 < SUB) {
-                read(s, kk + 1, ahead);
-            } else if (!LAST) {
+            const bool more = kk + 1 < SUB || !LAST;
+            const int to_s = kk + 1 < SUB ? s : s + 1, to_kk = kk + 1 < SUB ? kk + 1 : 0;
+            if (kk + 1 == SUB && !LAST) {
                 if (s == 0)
                     arrived_first(std::integral_constant<int, 0>());
                 else
                     arrived<0>();
                 if (LOAD) load_step(s + 2);
-                read(s + 1, 0, ahead);
             }
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(now);
-            __builtin_amdgcn_sched_barrier(0);
+            if (more) read_b(to_s, to_kk, ahead);
+            if constexpr (WIDE)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) widen(now.b[nb][0], now.b[nb]);
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) {
+                if (more) read_a(to_s, to_kk, mb, ahead);
+                if constexpr (T != FG_F32) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply_row(now, mb);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if constexpr (T == FG_F32) {
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(now);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
 
@@ -537,7 +548,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             arrived_first(std::integral_constant<int, LOADS>());
         else
             arrived<0>();
-        read(0, 0, F0);
+        read_b(0, 0, F0);
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) read_a(0, 0, mb, F0);
         // what belongs to the next tile is read behind this one's last loads (the waits for it are for everything in front of it)
         int s = 0;
         for (; s + 2 < steps; ++s) step(s, std::false_type(), std::true_type());
