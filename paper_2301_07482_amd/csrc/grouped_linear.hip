@@ -71,6 +71,7 @@ struct GlArgs {
     int64_t dz_stride;
     float *db_part, *dw_part;
     int ranges;
+    int sums;                 // workgroups that sum parts of dW
 };
 // position and row of x of entry k; -1: skipped
 __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, int32_t& r, int32_t& s) {
@@ -668,26 +669,25 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
     }
 }
 
-// db[g, c] = sum over the group's tiles, in fp64; 32 columns a workgroup, 32 runs of tiles side by side
-constexpr int DB_THREADS = 1024;
-__global__ __launch_bounds__(DB_THREADS) void grouped_db_kernel(GlArgs A) {
-    __shared__ double red[DB_THREADS];
-    const int blocks = (A.d_out + 31) / 32, g = blockIdx.x / blocks;
-    const int c = (blockIdx.x % blocks) * 32 + (threadIdx.x & 31);
+// db[g, c] = sum over the group's tiles, in fp64; DB_COLUMNS columns a workgroup, DB_RUNS runs of tiles side by side
+constexpr int DB_COLUMNS = 8, DB_RUNS = GZ_THREADS / DB_COLUMNS;
+__device__ __forceinline__ void sum_db(const GlArgs& A, int block, double* red) {
+    const int blocks = (A.d_out + DB_COLUMNS - 1) / DB_COLUMNS, g = block / blocks;
+    const int c = (block % blocks) * DB_COLUMNS + ((int)threadIdx.x % DB_COLUMNS);
     const int64_t first = steps_before(A.G, g, GZ_ROWS);
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
     const int64_t tiles = to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
     double s = 0.0;
     if (c < A.d_out)
 #pragma unroll 8
-        for (int64_t i = threadIdx.x >> 5; i < tiles; i += DB_THREADS / 32) s += (double)A.db_part[(first + i) * A.d_out + c];
+        for (int64_t i = threadIdx.x / DB_COLUMNS; i < tiles; i += DB_RUNS) s += (double)A.db_part[(first + i) * A.d_out + c];
     red[threadIdx.x] = s;
     __syncthreads();
-    for (int n = DB_THREADS / 64; n >= 1; n >>= 1) {      // halves of the runs
-        if ((int)threadIdx.x < 32 * n) red[threadIdx.x] += red[threadIdx.x + 32 * n];
+    for (int n = GZ_THREADS / 2; n >= DB_COLUMNS; n >>= 1) {      // halves of the runs
+        if ((int)threadIdx.x < n) red[threadIdx.x] += red[threadIdx.x + n];
         __syncthreads();
     }
-    if (threadIdx.x < 32 && c < A.d_out) A.db[(int64_t)g * A.d_out + c] = (float)red[threadIdx.x];
+    if (threadIdx.x < DB_COLUMNS && c < A.d_out) A.db[(int64_t)g * A.d_out + c] = (float)red[threadIdx.x];
 }
 
 // dW = x^T . dz of every group: a contraction over the group's rows, whose number the device alone knows, with BM x BN tiles of the result.
@@ -887,12 +887,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
 
 // The tiles that several workgroups have parts of, and zeros for groups without rows. A workgroup takes VALUES values of a tile; where those are
 // fewer than its threads can hold, runs of the parts lie side by side (a small result has many parts: 14 tiles of 128 x 128 in 512 shares 27 us
-// with 1024 values and the parts one after the other, 7 with 256 values).
+// with 1024 values and the parts one after the other, 7 with 256 values). The workgroups behind those sum db: a launch of their own cost 5 us.
 constexpr int ds_values(int bm) { return bm == 256 ? 4096 : 256; }
 template <int BM, int BN, int ROWS>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
     constexpr int VALUES = ds_values(BM), RUNS = VALUES < GZ_THREADS * 4 ? GZ_THREADS * 4 / VALUES : 1, SIDE = GZ_THREADS / RUNS, PARTS = BM * BN / VALUES;
     __shared__ double red[RUNS][SIDE * 4];
+    static_assert(sizeof(red) >= GZ_THREADS * sizeof(double), "a value of every thread");
+    if ((int)blockIdx.x >= A.sums) return sum_db(A, (int)blockIdx.x - A.sums, &red[0][0]);
     const int tiles_n = (A.d_out + BN - 1) / BN, tiles = (A.d_in + BM - 1) / BM * tiles_n;
     const int part = blockIdx.x % PARTS, unit = blockIdx.x / PARTS, tile = unit % tiles, g = unit / tiles;
     if (tile / tiles_n * BM + part * VALUES / BN >= A.d_in) return;      // its rows do not exist
@@ -1104,7 +1106,7 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
 }
 
 // Bytes between the rows of dz. Tiles read the same columns of many rows at a time: rows a multiple of 512 bytes apart meet in few of the memory's
-// channels (66 k rows of 1024 bf16 x 1024 columns: 186 us at 2048 bytes, 159 at 2432), so such rows get 384 bytes more.
+// channels (66 k rows of 1024 bf16 x 1024 columns: 167 us at 2048 bytes, 160 at 2432), so such rows get 384 bytes more.
 int64_t dz_row(int d_out, int e) {
     const int64_t row = (int64_t)d_out * e;
     return row % 512 ? row : row + 384;
@@ -1182,31 +1184,28 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
             hipLaunchKernelGGL((grouped_dz_kernel<T, FG_F32>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
         FG_LAUNCH_CHECK("grouped_dz_kernel");
     }
-    if (A.db) {
-        hipLaunchKernelGGL(grouped_db_kernel, dim3((unsigned)(A.G.n_groups * fg_ceil_div(A.d_out, 32))), dim3(DB_THREADS), 0, st, A);
-        FG_LAUNCH_CHECK("grouped_db_kernel");
-    }
     if (A.out && work) {
         A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
         FG_TRY((tile_product<T, false, false>(who, A, st)));
     }
-    if (A.dw) {
-        A.ranges = P.ranges;
-        const int64_t sums = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm / ds_values(P.bm));
-        if (sums > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
-        const dim3 grid((unsigned)P.grid), sum_grid((unsigned)sums);
-        if constexpr (T == FG_F32) {
-            hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), gf_lds_bytes(128) + GW_LIST * 4, st, A);
-            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GF_K>), sum_grid, dim3(GZ_THREADS), 0, st, A);
-        } else if (P.bm == 256) {
-            hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
-            hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
-        } else {
-            hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
-            hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
-        }
-        FG_LAUNCH_CHECK("grouped_dw_kernel");
+    if (!A.dw && !A.db) return FG_OK;
+    A.ranges = P.ranges;
+    const int64_t sums = A.dw ? fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm / ds_values(P.bm)) : 0;
+    const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
+    if (sums + db_blocks > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
+    A.sums = (int)sums;
+    const dim3 grid((unsigned)P.grid), sum_grid((unsigned)(sums + db_blocks));
+    if constexpr (T == FG_F32) {
+        if (A.dw) hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), gf_lds_bytes(128) + GW_LIST * 4, st, A);
+        hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GF_K>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+    } else if (P.bm == 256) {
+        if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
+        hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+    } else {
+        if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
+        hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
     }
+    FG_LAUNCH_CHECK("grouped_dw_kernel");
     return FG_OK;
 }
 
