@@ -82,15 +82,17 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
     if (r >= 0) s = A.src_ids ? A.src_ids[r] : r;
     if (s < 0 || s >= A.x_rows) r = s = -1;
 }
-// ---- 16- and 8-bit products on the matrix cores ----
+// ---- products on the matrix cores ----
 //
-// A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 64 bytes of a row (32 halfwords, 64 values of 8 bits). The
-// operands of a step go from memory straight to LDS (global_load_lds, 16 bytes a lane) into a ring of four buffers, so that a load has three
-// steps of arithmetic to arrive in. A wavefront reads the operands of its next matrix instructions from LDS while it issues the current
-// ones, over the end of a step too: there it waits for its loads of the next step, meets the others, and sends the loads of the fourth step
-// ahead into the buffer that all have then read. One barrier a step.
+// A workgroup owns a BM x BN tile of one group's rows; K is walked in steps of 128 bytes of a row (32 floats, 64 halfwords, 128 values of 8
+// bits: narrower pieces of a row come at a lower rate, 64 bytes a step measured 8 % slower). The operands of a step go from memory straight to
+// LDS (global_load_lds, 16 bytes a lane) into one of two buffers. A wavefront reads the operands of its next matrix instructions from LDS
+// while it issues the current ones, over the end of a step too: there it waits for its loads of the next step, meets the others, and sends the
+// loads of the step after that into the buffer that all have then read. One barrier a step. A ring of three or four half as deep
+// buffers was no faster: a step's arithmetic is longer than a load. Workgroups stay and go from tile to tile; the first loads of the next tile
+// are on their way while a tile is written.
 // A lane's place in LDS is fixed by the instruction (base + 16 bytes per lane), so the exchange of 16-byte pieces that keeps the operand reads
-// off each other's banks is made on the side of memory: piece c of LDS row m holds piece c ^ (m / 4 & 3) of the row (a 16-byte read takes
+// off each other's banks is made on the side of memory: piece c of LDS row m holds piece c ^ (m / 2 & 7) of the row (a 16-byte read takes
 // the lanes in groups of sixteen: 0-3, 12-15, 20-23, 24-27 and so on; 256 bytes of banks). B is either read the same way (rows of W along K:
 // gradients, 8 bits), or its rows are k and transposed on the way out of LDS (ds_read_b64_tr_b16), with the 64-byte windows of a row exchanged so
 // that the four rows a read takes a window of lie in different banks.
@@ -98,6 +100,17 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 // not stored), pieces beyond K are read from 16 bytes of zeros, both operands'.
 //
 // The waits are counted by hand: the compiler knows nothing of these loads (it would wait for all of them before every LDS read).
+//
+// fp32: every product of two values is formed on the bf16 matrix cores from the exact split of both into three bf16 terms (x1 = bf16(x), x2 =
+// bf16(x - x1), x3 = bf16(x - x1 - x2)): the six products a_i * b_j with i + j <= 4, the leading ones in a running sum of their own, as in
+// fg_linear. The values lie in LDS as they are and are split as they are read: the split costs about the vector instructions that the
+// products cost matrix instructions.
+//
+// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 98 us
+// (1.26 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
+// 2.0 us for the 1.15 us that its matrix instructions take by themselves and the 0.85 us that LDS is busy with them; tiles of 256 x 256 on four
+// wavefronts, with a third fewer LDS reads, took 1010 us instead of 702 (nothing fills the waits of a lone wavefront), tiles of 128 x 256 two
+// to a compute unit 12 % longer.
 __device__ __attribute__((aligned(16))) unsigned int gl_zero[4];
 // where the lanes of a store write that have nothing to write (never read)
 __device__ __attribute__((aligned(16))) unsigned int gl_sink[4 * 64];
@@ -588,13 +601,21 @@ fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
     return FG_OK;
 }
 // out[r, :] = a[., :] . B for the entries of every group (A.a, a_stride, a_by, K, N, W, out, ... are set)
+//
+// The largest tile that there are as many of as compute units, and that the columns and an average group more than half fill. Both sides in us
+// (K = N = 256 unless said, 4 groups):
+//   256 against 128, bf16: 65536 rows 18.6 | 20.0, 32768 rows 16.6 | 13.1; N = 128 17.8 | 12.9; 193 rows a group 30.3 | 31.2, 128 rows a group 32.7 | 25.5
+//   128 against 64: 16384 rows bf16 9.6 | 11.1, fp32 21.4 | 22.5, 8 bits 8.5 | 9.5; 8192 rows 8.7 | 7.1, 20.1 | 13.7, 7.9 | 6.0; N = 64 fp32 32.6 | 22.7;
+//                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 56 | 61; 64 rows a group 43 | 53, 134 | 115, 66 | 46
+// No 256 x 256 tile for fp32, whose two sums do not fit the registers, nor with the 8-bit instructions, whose long operands fit them only one row
+// of blocks at a time: 65536 x 1024 x 1024 149 us a pass against 151.
 template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
-    const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256);
-    if constexpr (T != FG_F32 && (T != FG_E4M3 || WIDE))      // (fp32 has two sums; two sets of the 8-bit instruction's long operands do not fit the registers of a 256 x 256 tile)
-        if (large >= 256 && A.N > 128) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
+    const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
+    if constexpr (T != FG_F32 && (T != FG_E4M3 || WIDE))
+        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
+    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
     return tile_launch<T, 64, 64, 2, 2, 2, 4, B_KN, WIDE>(who, A, st);
 }
 
@@ -611,8 +632,9 @@ __device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int r
     return n;
 }
 
-// dz in entry order, in the rows' type, and its column sums by tiles of GZ_ROWS entries of one group (db is their sum). What it costs,
-// reading dh and h and writing dz, both products save again: they read dz alone, in the order of the entries.
+// dz in entry order, in the rows' type, and its column sums by tiles of GZ_ROWS entries of one group (db is their sum). The products then
+// read dz alone, straight to LDS; a mask on the way there would take both matrices through registers, twice. Bound by memory: 58982 x 1024
+// bf16 72 us (5.0 TB/s, the rate of a copy), 43352 x 256 fp32 23 us (5.7, part of it from the last-level cache).
 constexpr int GZ_ROWS = 64, GZ_THREADS = 256;
 
 template <int T, int D>
@@ -885,13 +907,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
     }
 }
 
-// The tiles that several workgroups have parts of, and zeros for groups without rows. A workgroup takes VALUES values of a tile; where those are
-// fewer than its threads can hold, runs of the parts lie side by side (a small result has many parts: 14 tiles of 128 x 128 in 512 shares 27 us
-// with 1024 values and the parts one after the other, 7 with 256 values). The workgroups behind those sum db: a launch of their own cost 5 us.
-constexpr int ds_values(int bm) { return bm == 256 ? 4096 : 256; }
-template <int BM, int BN, int ROWS>
+// The tiles that several workgroups have parts of, and zeros for groups without rows. A workgroup takes VALUES values of a tile: 4096 if that
+// gives 512 workgroups, else 256, with runs of the parts side by side (a small result has many parts: 14 tiles of 128 x 128 from 512 ranges 27 us
+// with 1024 values and the parts one after the other, 7 with 256; 100 groups of 4 tiles, a part or two each, with 256 39 us more than with 4096).
+// The workgroups behind those sum db: a launch of their own cost 5 us.
+constexpr int DS_MANY = 4096, DS_FEW = 256;
+template <int BM, int BN, int ROWS, int VALUES>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
-    constexpr int VALUES = ds_values(BM), RUNS = VALUES < GZ_THREADS * 4 ? GZ_THREADS * 4 / VALUES : 1, SIDE = GZ_THREADS / RUNS, PARTS = BM * BN / VALUES;
+    constexpr int RUNS = VALUES < GZ_THREADS * 4 ? GZ_THREADS * 4 / VALUES : 1, SIDE = GZ_THREADS / RUNS, PARTS = BM * BN / VALUES;
     __shared__ double red[RUNS][SIDE * 4];
     static_assert(sizeof(red) >= GZ_THREADS * sizeof(double), "a value of every thread");
     if ((int)blockIdx.x >= A.sums) return sum_db(A, (int)blockIdx.x - A.sums, &red[0][0]);
@@ -932,100 +955,42 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
 
 // ---- fp32 ----
 //
-// Every product of two fp32 values is formed on the bf16 matrix cores from the exact split of both into three bf16 terms (x1 = bf16(x), x2 =
-// bf16(x - x1), x3 = bf16(x - x1 - x2)): the six products a_i * b_j with i + j <= 4, the leading ones in a running sum of their own, as in
-// fg_linear. A workgroup owns a TILE x TILE tile of the result and walks the contraction in steps of GF_K: a thread loads 16 bytes of
-// an operand's row, splits them and writes each term's bf16 values to LDS as they lie. An operand whose rows lie along the contraction (KC)
-// is read from there 16 bytes a lane, one whose rows lie across it (KN: W of the forward product; x and dz of the weight gradients) is
-// transposed on the way out. One buffer and two barriers a step; the loads of the next step are in flight while a step is multiplied, and the
-// two workgroups of a compute unit fill each other's waits.
-constexpr int GF_THREADS = 256, GF_K = 32;
-constexpr size_t gf_lds_bytes(int tile) { return (size_t)2 * 3 * tile * GF_K * 2; }
-// One operand: TILE rows (KC) or columns (KN) by GF_K
-template <int TILE, bool KN>
-struct F32Operand {
-    static constexpr int LOADS = TILE * GF_K / 4 / GF_THREADS, TERM = TILE * GF_K * 2, ROW = KN ? TILE * 2 : GF_K * 2;
-    static constexpr int PER_ROW = KN ? TILE / 4 : GF_K / 4, ROWS = GF_THREADS / PER_ROW;      // pieces of a row; rows of a pass
-    // windows of 64 bytes are exchanged so that the four rows of a transposing read lie in different banks
-    static __device__ __forceinline__ int window(int row) { return TILE >= 128 ? row & 3 : (row >> 1) & 1; }
-    static __device__ __forceinline__ int row_of(int t, int i) { return t / PER_ROW + ROWS * i; }
-    static __device__ __forceinline__ int place(int t, int i) {      // bytes from the term's first
-        const int row = row_of(t, i), p = t % PER_ROW;
-        return KN ? row * ROW + (((p >> 3) ^ window(row)) << 6) + (p & 7) * 8 : row * ROW + (((p >> 1) ^ ((row >> 2) & 3)) << 4) + (p & 1) * 8;
-    }
-    static __device__ __forceinline__ void put(char* lds, int t, int i, fg_u32x4 v) {
-        fg_u32x2 u[3];
-        split4(v, u);
-        char* to = lds + place(t, i);
+// dW in fp32: the products as above, from terms that are split before they go to LDS (values that are split as they are read, which
+// needs no registers for loads on their way, took 129 us a backward call instead of 110: here every value of both operands is read by
+// two wavefronts). A workgroup owns a TILE x TILE tile of the result and walks the contraction in steps of GF_K: a thread loads 16 bytes of
+// an operand's row, splits them and writes each term's bf16 values to LDS as they lie; they are transposed on the way out. One buffer and two
+// barriers a step; the loads of the next step are in flight while a step is multiplied, and the two workgroups of a compute unit fill each
+// other's waits. 43352 x 88 x 256: 36 us.
+constexpr int GF_THREADS = 256, GF_K = 32, GF_TILE = 128, GF_BLOCKS = GF_TILE / 64;      // 32 x 32 blocks of a wavefront, both ways
+// one operand in LDS: three terms of GF_K rows
+constexpr int GF_ROW = GF_TILE * 2, GF_TERM = GF_K * GF_ROW;
+constexpr int GF_PER_ROW = GF_TILE / 4, GF_ROWS = GF_THREADS / GF_PER_ROW, GF_LOADS = GF_K / GF_ROWS;      // pieces of a row; rows of a pass; passes
+constexpr size_t GF_LDS_BYTES = 2 * 3 * GF_TERM;
+__device__ __forceinline__ int gf_row_of(int t, int i) { return t / GF_PER_ROW + GF_ROWS * i; }
+// windows of 64 bytes are exchanged so that the four rows of a transposing read lie in different banks
+__device__ __forceinline__ void gf_put(char* lds, int t, int i, fg_u32x4 v) {
+    const int row = gf_row_of(t, i), piece = t % GF_PER_ROW;
+    fg_u32x2 u[3];
+    split4(v, u);
+    char* to = lds + row * GF_ROW + (((piece >> 3) ^ (row & 3)) << 6) + (piece & 7) * 8;
 #pragma unroll
-        for (int term = 0; term < 3; ++term) *(fg_u32x2*)(to + term * TERM) = u[term];
-    }
-    // rows (columns) first .. first + 31, k = 16 kk + 8 half + 0..7
-    static __device__ __forceinline__ fg_u32x4 fragment(const char* lds, int first, int kk, int lane) {
-        const int l32 = lane & 31, half = lane >> 5;
-        if constexpr (!KN) {
-            const int row = first + l32;
-            return *(const fg_u32x4*)(lds + row * ROW + (((2 * kk + half) ^ ((row >> 2) & 3)) << 4));
-        } else {
-            typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
-            const int place = (lane >> 2) & 3;
-            const char* p = lds + (16 * kk + 8 * half + place) * ROW + (((first >> 5) ^ window(place)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-            const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
-            const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * ROW));
-            return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        }
-    }
-};
-
-// A wavefront's part of the tile: TILE / 2 by TILE / 2, as 32 x 32 blocks
-template <int TILE>
-struct F32Sums {
-    static constexpr int B = TILE / 64;
-    gl_f32x16 lead[B][B], rest[B][B];
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int a = 0; a < B; ++a)
-#pragma unroll
-            for (int b = 0; b < B; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) lead[a][b][i] = rest[a][b][i] = 0.f;
-    }
-};
-template <int TILE, bool A_KN, bool B_KN>
-__device__ __forceinline__ void f32_multiply(const char* lds, int wm, int wn, int lane, F32Sums<TILE>& S) {
-    typedef F32Operand<TILE, A_KN> OA;
-    typedef F32Operand<TILE, B_KN> OB;
-    constexpr int NB = F32Sums<TILE>::B;
-    constexpr int TA[5] = {2, 0, 1, 1, 0}, TB[5] = {0, 2, 1, 0, 1};      // smallest products first
-#pragma unroll
-    for (int kk = 0; kk < GF_K / 16; ++kk) {
-        fg_u32x4 a[NB][3], b[NB][3];
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int term = 0; term < 3; ++term) {
-                a[i][term] = OA::fragment(lds + term * OA::TERM, wm + 32 * i, kk, lane);
-                b[i][term] = OB::fragment(lds + 3 * OA::TERM + term * OB::TERM, wn + 32 * i, kk, lane);
-            }
-#pragma unroll
-        for (int e = 0; e < 5; ++e)
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) S.rest[i][j] = mfma<FG_BF16, false>(&a[i][TA[e]], &b[j][TB[e]], S.rest[i][j]);
-#pragma unroll
-        for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) S.lead[i][j] = mfma<FG_BF16, false>(&a[i][0], &b[j][0], S.lead[i][j]);
-    }
+    for (int term = 0; term < 3; ++term) *(fg_u32x2*)(to + term * GF_TERM) = u[term];
+}
+// columns first .. first + 31, k = 16 kk + 8 half + 0..7
+__device__ __forceinline__ fg_u32x4 gf_fragment(const char* lds, int first, int kk, int lane) {
+    typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+    const int half = lane >> 5, place = (lane >> 2) & 3;
+    const char* p = lds + (16 * kk + 8 * half + place) * GF_ROW + (((first >> 5) ^ place) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p);
+    const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(p + 4 * GF_ROW));
+    return __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // dW in fp32: the ranges of grouped_dw_kernel, steps of GF_K entries, 128 x 128 tiles
 __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A) {
-    constexpr int TILE = 128;
-    typedef F32Operand<TILE, true> OP;
+    constexpr int TILE = GF_TILE, B = GF_BLOCKS;
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
-    int32_t* list = (int32_t*)(gl_lds + gf_lds_bytes(TILE));
+    int32_t* list = (int32_t*)(gl_lds + GF_LDS_BYTES);
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int tiles_n = (A.d_out + TILE - 1) / TILE, tiles = (A.d_in + TILE - 1) / TILE * tiles_n;
     int range, tile;
@@ -1037,10 +1002,10 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
     for (; W.next(A.G, GF_K); W.at += W.last - W.first) {      // uniform over the workgroup
         const int steps = (int)(W.last - W.first);
         const int64_t k0 = W.k0, k1 = W.k1;
-        const int c = (t % OP::PER_ROW) * 4;
+        const int c = (t % GF_PER_ROW) * 4;
         const int64_t ca = (m0 + c < A.d_in ? m0 + c : 0) * 4, cb = (n0 + c < A.d_out ? n0 + c : 0) * 4;
-        fg_u32x4 ra[OP::LOADS], rb[OP::LOADS];
-        bool in[OP::LOADS];
+        fg_u32x4 ra[GF_LOADS], rb[GF_LOADS];
+        bool in[GF_LOADS];
         auto fill = [&](int64_t k) {
             const int need = (int)(k1 - k < GW_LIST ? (k1 - k + GF_K - 1) / GF_K * GF_K : GW_LIST);
 #pragma unroll 2
@@ -1053,10 +1018,10 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
         };
         auto load = [&](int s) {
 #pragma unroll
-            for (int i = 0; i < OP::LOADS; ++i) {
-                const int32_t x_row = list[(s * GF_K) % GW_LIST + OP::row_of(t, i)];
+            for (int i = 0; i < GF_LOADS; ++i) {
+                const int32_t x_row = list[(s * GF_K) % GW_LIST + gf_row_of(t, i)];
                 in[i] = x_row >= 0;
-                const int64_t xr = in[i] ? x_row : 0, zr = in[i] ? (A.dz ? k0 + (int64_t)s * GF_K + OP::row_of(t, i) : xr) : 0;
+                const int64_t xr = in[i] ? x_row : 0, zr = in[i] ? (A.dz ? k0 + (int64_t)s * GF_K + gf_row_of(t, i) : xr) : 0;
                 ra[i] = *(const fg_u32x4*)(A.x + xr * A.x_stride + ca);
                 rb[i] = *(const fg_u32x4*)((A.dz ? A.dz : A.dh) + zr * A.dz_stride + cb);
             }
@@ -1064,13 +1029,42 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
         auto store = [&]() {
             const fg_u32x4 none = {0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int i = 0; i < OP::LOADS; ++i) {
-                OP::put(gl_lds, t, i, in[i] ? ra[i] : none);
-                OP::put(gl_lds + 3 * OP::TERM, t, i, in[i] ? rb[i] : none);
+            for (int i = 0; i < GF_LOADS; ++i) {
+                gf_put(gl_lds, t, i, in[i] ? ra[i] : none);
+                gf_put(gl_lds + 3 * GF_TERM, t, i, in[i] ? rb[i] : none);
             }
         };
-        F32Sums<TILE> C;
-        C.clear();
+        gl_f32x16 lead[B][B], rest[B][B];
+#pragma unroll
+        for (int i = 0; i < B; ++i)
+#pragma unroll
+            for (int j = 0; j < B; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) lead[i][j][e] = rest[i][j][e] = 0.f;
+        auto multiply = [&]() {
+            constexpr int TA[5] = {2, 0, 1, 1, 0}, TB[5] = {0, 2, 1, 0, 1};      // smallest products first
+#pragma unroll
+            for (int kk = 0; kk < GF_K / 16; ++kk) {
+                fg_u32x4 a[B][3], b[B][3];
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+#pragma unroll
+                    for (int term = 0; term < 3; ++term) {
+                        a[i][term] = gf_fragment(gl_lds + term * GF_TERM, wm + 32 * i, kk, lane);
+                        b[i][term] = gf_fragment(gl_lds + (3 + term) * GF_TERM, wn + 32 * i, kk, lane);
+                    }
+#pragma unroll
+                for (int e = 0; e < 5; ++e)
+#pragma unroll
+                    for (int i = 0; i < B; ++i)
+#pragma unroll
+                        for (int j = 0; j < B; ++j) rest[i][j] = mfma<FG_BF16, false>(&a[i][TA[e]], &b[j][TB[e]], rest[i][j]);
+#pragma unroll
+                for (int i = 0; i < B; ++i)
+#pragma unroll
+                    for (int j = 0; j < B; ++j) lead[i][j] = mfma<FG_BF16, false>(&a[i][0], &b[j][0], lead[i][j]);
+            }
+        };
         fill(k0);
         load(0);
         for (int s = 0; s < steps; ++s) {
@@ -1079,7 +1073,7 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
             __syncthreads();
             if (s + 1 < steps) load(s + 1);
             __builtin_amdgcn_sched_barrier(0);
-            f32_multiply<TILE, true, true>(gl_lds, wm, wn, lane, C);
+            multiply();
             __syncthreads();
         }
         const bool whole = W.first == 0 && W.last == W.steps_g;
@@ -1088,14 +1082,14 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
         int m_first = wm + 4 * (lane >> 5), n_first = wn + (lane & 31);      // (formed here, as above)
         asm volatile("" : "+v"(m_first), "+v"(n_first));
 #pragma unroll
-        for (int a = 0; a < F32Sums<TILE>::B; ++a)
+        for (int a = 0; a < B; ++a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int m = m_first + 32 * a + 8 * (i >> 2) + (i & 3);
 #pragma unroll
-                for (int b = 0; b < F32Sums<TILE>::B; ++b) {
+                for (int b = 0; b < B; ++b) {
                     const int n = n_first + 32 * b;
-                    const float v = C.lead[a][b][i] + C.rest[a][b][i];
+                    const float v = lead[a][b][i] + rest[a][b][i];
                     if (!whole)
                         to_part[m * TILE + n] = v;
                     else if (m0 + m < A.d_in && n0 + n < A.d_out)
@@ -1113,27 +1107,40 @@ int64_t dz_row(int d_out, int e) {
 }
 // The workspace of a backward call: dz, column sums by tile, parts of dW
 struct BwPlan {
-    bool dz;
     int bm, ranges, grid;      // tile, ranges of rows, workgroups of the weight gradients
     size_t dz_bytes, db_bytes, dw_bytes;
     size_t total() const { return dz_bytes + db_bytes + dw_bytes + 16; }
 };
-// (sized for the masked call, which needs dz, at every size: a workspace for max_rows serves fewer rows too)
-BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
-    BwPlan P;
-    P.dz = true;
-    P.bm = e == 2 && (d_in > 128 || d_out > 128) ? 256 : 128;
-    const int64_t tiles = fg_ceil_div(d_in, P.bm) * fg_ceil_div(d_out, P.bm);
-    // as many ranges as give every place on the chip a tile; of more tiles than places two ranges where that leaves fewer of them idle
-    const int64_t steps = max_rows / (e == 4 ? GF_K : GW_ROWS) + (n_groups < max_rows ? n_groups : max_rows), places = P.bm == 256 ? 256 : 512;
+// Ranges of rows for bm x bm tiles. As many as give every place on the chip a tile; of more tiles than places two ranges where that leaves fewer of
+// them idle. But a part of a tile that is written and read again costs what reading its operands for bm rows costs: a range has DW_MIN_ROWS rows
+// at least, where that leaves DW_MIN_GROUPS workgroups (dW alone, bf16, 4096 x 256 x 256: 18 us, 21 with shorter ranges; 2000 x 64 x 64: 19 | 14).
+constexpr int DW_MIN_ROWS = 128, DW_MIN_GROUPS = 64;
+int dw_ranges(int64_t max_rows, int n_groups, int64_t tiles, int bm, int e) {
+    const int rows = e == 4 ? GF_K : GW_ROWS;
+    const int64_t steps = max_rows / rows + (n_groups < max_rows ? n_groups : max_rows), places = bm == 256 ? 256 : 512;
     int64_t ranges = places / tiles;
     if (ranges < 1) ranges = fg_ceil_div(2 * tiles, places) < 2 * fg_ceil_div(tiles, places) ? 2 : 1;
-    if (ranges > steps) ranges = steps < 1 ? 1 : steps;
-    P.ranges = (int)ranges;
-    P.grid = (int)(fg_ceil_div(ranges * tiles, 8) * 8);
+    const int64_t few = DW_MIN_GROUPS / tiles < steps ? DW_MIN_GROUPS / tiles : steps, most = fg_ceil_div(steps * rows, DW_MIN_ROWS);
+    if (ranges > (most > few ? most : few)) ranges = most > few ? most : few;
+    return ranges < 1 ? 1 : (int)ranges;
+}
+// (sized for the masked call, which needs dz, at every size, and for both tiles: a workspace for max_rows serves fewer rows too)
+BwPlan bw_plan(int64_t max_rows, int n_groups, int d_in, int d_out, int e) {
+    BwPlan P;
+    P.dw_bytes = 0;
+    for (int bm = 128; bm <= (e == 2 ? 256 : 128); bm *= 2) {
+        const int64_t tiles = fg_ceil_div(d_in, bm) * fg_ceil_div(d_out, bm);
+        // tiles of 256 x 256 take half the reads, and their parts twice the writes: from 2048 rows a place on (bf16, 4 groups, us, 256 | 128: 65536 x 1024 x
+        // 1024, 4096 rows, 160 | 189; 20000 x 2048 x 2048 172 | 212; 65536 x 512 x 512, 1024 rows, 69 | 63; 4096 x 1024 x 1024, 256 rows, 43 | 35)
+        if (bm == 256 && max_rows * tiles < 2048 * 256) break;
+        P.bm = bm;
+        P.ranges = dw_ranges(max_rows, n_groups, tiles, bm, e);
+        P.grid = (int)(fg_ceil_div(P.ranges * tiles, 8) * 8);
+        const size_t bytes = P.ranges > 1 ? (size_t)2 * P.ranges * tiles * bm * bm * 4 : 0;
+        if (bytes > P.dw_bytes) P.dw_bytes = bytes;
+    }
     P.dz_bytes = fg_align_up((size_t)max_rows * dz_row(d_out, e), 256);
     P.db_bytes = fg_align_up((size_t)(max_rows / GZ_ROWS + (n_groups < max_rows ? n_groups : max_rows)) * d_out * 4, 256);
-    P.dw_bytes = P.ranges > 1 ? (size_t)2 * P.ranges * tiles * P.bm * P.bm * 4 : 0;
     return P;
 }
 
@@ -1166,6 +1173,10 @@ fg_status_t check_matrix(const char* who, const char* what, const void* p, int64
 // tiles of rows at most: every group may end in one that is partly filled
 int64_t row_tiles(int64_t max_rows, int n_groups, int size) { return max_rows / size + (n_groups < max_rows ? n_groups : max_rows); }
 
+template <int BM, int ROWS, int VALUES>
+void launch_sum(const GlArgs& A, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((grouped_dw_sum_kernel<BM, BM, ROWS, VALUES>), grid, dim3(GZ_THREADS), 0, st, A);
+}
 template <int T>
 fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void* ws_dev) {
     constexpr int E = T == FG_F32 ? 4 : 2;
@@ -1190,20 +1201,22 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     }
     if (!A.dw && !A.db) return FG_OK;
     A.ranges = P.ranges;
-    const int64_t sums = A.dw ? fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm / ds_values(P.bm)) : 0;
+    const int64_t results = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm);
+    const bool many = results / DS_MANY >= 512;
+    const int64_t sums = A.dw ? results / (many ? DS_MANY : DS_FEW) : 0;
     const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
     if (sums + db_blocks > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
     A.sums = (int)sums;
     const dim3 grid((unsigned)P.grid), sum_grid((unsigned)(sums + db_blocks));
     if constexpr (T == FG_F32) {
-        if (A.dw) hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), gf_lds_bytes(128) + GW_LIST * 4, st, A);
-        hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GF_K>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+        if (A.dw) hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), GF_LDS_BYTES + GW_LIST * 4, st, A);
+        many ? launch_sum<128, GF_K, DS_MANY>(A, sum_grid, st) : launch_sum<128, GF_K, DS_FEW>(A, sum_grid, st);
     } else if (P.bm == 256) {
         if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
-        hipLaunchKernelGGL((grouped_dw_sum_kernel<256, 256, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+        many ? launch_sum<256, GW_ROWS, DS_MANY>(A, sum_grid, st) : launch_sum<256, GW_ROWS, DS_FEW>(A, sum_grid, st);
     } else {
         if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
-        hipLaunchKernelGGL((grouped_dw_sum_kernel<128, 128, GW_ROWS>), sum_grid, dim3(GZ_THREADS), 0, st, A);
+        many ? launch_sum<128, GW_ROWS, DS_MANY>(A, sum_grid, st) : launch_sum<128, GW_ROWS, DS_FEW>(A, sum_grid, st);
     }
     FG_LAUNCH_CHECK("grouped_dw_kernel");
     return FG_OK;

@@ -118,9 +118,10 @@ def test_refusals(B):
 
 
 def test_workspaces_of_a_bound_serve_every_smaller_call(B):
-    sizes = sorted({*range(0, 400), *range(4000, 4200), *range(8100, 8300), *range(16300, 16500), 30000, 70000, 10 ** 6, 3 * 10 ** 6, 10 ** 7})
+    sizes = sorted({*range(0, 400), *range(4000, 4200), *range(8100, 8300), *range(16300, 16500), *range(30000, 70000, 1000), 70000, 10 ** 6, 3 * 10 ** 6, 10 ** 7})
     for need in (lambda n: B.fg_group_rows_workspace_bytes(n, 37), lambda n: B.fg_residual_norm_backward_workspace_bytes(n, 88),
-                 *(lambda n, t=t, g=g: B.fg_linear_grouped_backward_workspace_bytes(t, n, g, 96, 256) for t in (0, 1, 2) for g in (1, 5, 300))):
+                 *(lambda n, t=t, g=g, a=a, b=b: B.fg_linear_grouped_backward_workspace_bytes(t, n, g, a, b) for t in (0, 1, 2) for g in (1, 5, 300)
+                   for a, b in ((96, 256), (264, 520), (1024, 1024), (2048, 4096), (4096, 4096), (8, 65536)))):
         got = [need(n) for n in sizes]
         assert got == sorted(got) and min(got) >= 0
 
@@ -286,7 +287,8 @@ def test_linear_grouped_of_many_rows(B, dtype, out, n, n_groups, d_in, d_out, op
 @gpu
 @pytest.mark.parametrize("dtype, out, n, n_groups, d_in, d_out", [("bf16", "bf16", 40_000, 3, 264, 136), ("f16", "f32", 70_000, 2, 256, 64), ("bf16", "f32", 33_500, 40, 520, 264),
                                                                    ("f32", "f32", 45_000, 3, 88, 256), ("bf16", "bf16", 50_000, 1, 64, 64), ("f16", "f16", 9_000, 300, 72, 40),
-                                                                   ("f32", "f32", 33_000, 5, 132, 400)])
+                                                                   ("f32", "f32", 33_000, 5, 132, 400), ("bf16", "bf16", 66_000, 5, 520, 520),
+                                                                   ("f16", "f32", 30_000, 3, 1160, 1032)])
 def test_linear_grouped_backward_of_many_rows(B, dtype, out, n, n_groups, d_in, d_out):
     order, offsets, _, x, W, _ = large(dtype, out, n, n_groups, d_in, d_out)
     x, W = x.to(T[dtype]), W.to(T[dtype])
@@ -391,7 +393,7 @@ def test_linear_grouped_backward(B, dtype, dh_type, dx_type, n, n_groups, d_in, 
     out = got_dx.cpu()
     close(out[pos, :d_in], dx, (d_out + 8) * 2.0 ** -23 * dxs + HALF[dx_type] * dx.abs() + TINY[dx_type], "dx")
     assert bool((out[np.setdiff1d(np.arange(n), pos)] == -77).all()) and bool((out[:, d_in:] == -77).all())
-    rows = torch.from_numpy(np.diff(offsets)).double().clamp(max=4096) + 16      # sums of at most 4096 rows in fp32, those in fp64
+    rows = torch.from_numpy(np.diff(offsets)).double().clamp(max=4096) + 16      # a range of rows, at these sizes fewer than 4096, in fp32, the ranges in fp64
     close(dw.cpu(), dW, rows[:, None, None] * 2.0 ** -23 * dWs + 2.0 ** -24 * dW.abs(), "dW")
     close(gb.cpu(), db, rows[:, None] * 2.0 ** -23 * dbs + 2.0 ** -24 * db.abs(), "db")
     assert n_groups <= 2 or not bool(dw[1].any()), "a group without rows has a zero gradient"
