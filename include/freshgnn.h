@@ -807,7 +807,7 @@ fg_status_t fg_backward_weights_all(fg_dtype_t compute_dtype, int32_t n_layers, 
  *   order_dev [max_rows]                out, int32; entries at and beyond offsets[n_groups] are left as they were
  *   offsets_dev [n_groups + 1]          out, int64; offsets[n_groups] = rows that have a group
  *   ws_dev, ws_bytes                    device workspace, >= fg_group_rows_workspace_bytes(max_rows, n_groups), 16-byte aligned
- * Positions outside [0, n_positions), ids outside [0, n_table) and groups outside [0, n_groups) are left out. One launch for up to 8192
+ * Positions outside [0, n_positions), ids outside [0, n_table) and groups outside [0, n_groups) are left out. One launch for up to 6144
  * rows, else two. The result does not depend on the order in which threads run.
  */
 #define FG_MAX_GROUPS 1024
@@ -823,7 +823,7 @@ fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int3
  *   x_scale [x_rows]                    FG_E4M3: a row's scale (fg_residual_norm, fg_quantize_rows); else NULL
  *   src_ids_dev [n_out]                 int32 rows of x by position, or NULL
  *   order_dev, offsets_dev, n_groups    as fg_group_rows leaves them (order NULL: position k itself, rows that lie sorted by group);
- *                                       at most max_rows entries are taken; no position twice
+ *                                       at most max_rows entries are taken, up to FG_MAX_GROUPED_ROWS; no position twice
  *   W                                   [n_groups x d_in x d_out] row-major, the type of x; FG_E4M3: [n_groups x d_out x d_in], each matrix
  *                                       transposed, with w_scale [n_groups x d_out], as fg_quantize_rows makes them of the transposed matrices
  *   bias [n_groups x d_out]             float, or NULL;  relu != 0: act = ReLU
@@ -834,6 +834,7 @@ fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int3
  * x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
  * [0, x_rows) are skipped.
  */
+#define FG_MAX_GROUPED_ROWS 536870912
 fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const float* x_scale, const int32_t* src_ids_dev,
                               const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
                               int32_t d_out, const void* W, const float* w_scale, const float* bias, int32_t relu, void* h_out, int64_t n_out,

@@ -99,6 +99,8 @@ static inline int fg_dtype_size(fg_dtype_t t) { return t == FG_F32 ? 4 : (t == F
         if (e_ != hipSuccess) FG_FAIL(FG_ERR_HIP, "launch of %s failed: %s", name, hipGetErrorString(e_)); \
     } while (0)
 
+constexpr int64_t FG_MAX_GRID = 1 << 24;      // workgroups of 256 threads: fewer than that many, 2^32 threads is what a launch takes
+
 constexpr int FG_SCAN_BLOCK = 1024;  // elements (= threads) per block in the compaction kernels
 
 // The counter-based generator of this library: the SplitMix64 output function, and word `counter` of the stream `key`.

@@ -5,13 +5,16 @@
 // wavefront has counted so far (LDS, one row of counters per wavefront: no atomics, so the order is the list's). Two scans, over the
 // wavefronts and over the groups, turn the counts into places. Up to ONE_ROWS rows are one workgroup and one launch; else the first
 // launch leaves every workgroup's counts and every row's group and rank, and in the second each workgroup adds up the counts of those before it.
+// What it costs is latency, three or four reads that depend on each other to a launch: 256 rows 3.9 us, 54067 rows 5.1 + 6.5, 368640 rows
+// 13 + 9.5 (their 12 bytes a row read and 8 written would take 1.5 us). One launch against two, us, 4 groups: 256 rows 4.2 | 6.4, 4000 5.8 | 7.4, 6000
+// 6.8 | 7.6, 8192 8.0 | 7.7; 100 groups: 4000 7.4 | 9.2, 6000 9.4 | 9.3, 8192 11.4 | 9.9.
 #include "common.h"
 #include "scan.h"
 
 namespace {
 
 constexpr int GR_THREADS = 1024, GR_WAVES = GR_THREADS / 64;
-constexpr int GR_AHEAD = 8;                          // rows of a lane whose reads (list, id, group) are in flight together
+constexpr int GR_AHEAD = 6;                          // rows of a lane whose reads (list, id, group) are in flight together
 constexpr int64_t ONE_ROWS = GR_THREADS * GR_AHEAD;
 constexpr int64_t GR_MAX_BLOCKS = 512;               // a workgroup reads the counts of all of them
 constexpr int GR_RANK_BITS = 22;                     // of a row within its wavefront's run; the 10 bits above hold the group

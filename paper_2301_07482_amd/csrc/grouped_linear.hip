@@ -72,6 +72,7 @@ struct GlArgs {
     float *db_part, *dw_part;
     int ranges;
     int sums;                 // workgroups that sum parts of dW
+    int64_t db_tiles;         // tiles that have column sums
 };
 // position and row of x of entry k; -1: skipped
 __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, int32_t& r, int32_t& s) {
@@ -698,7 +699,8 @@ __device__ __forceinline__ void sum_db(const GlArgs& A, int block, double* red) 
     const int c = (block % blocks) * DB_COLUMNS + ((int)threadIdx.x % DB_COLUMNS);
     const int64_t first = steps_before(A.G, g, GZ_ROWS);
     const int64_t from = group_offset(A.G, g), to = group_offset(A.G, g + 1);
-    const int64_t tiles = to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
+    int64_t tiles = to > from ? (to - from + GZ_ROWS - 1) / GZ_ROWS : 0;
+    if (tiles > A.db_tiles - first) tiles = A.db_tiles - first;      // (offsets that do not ascend)
     double s = 0.0;
     if (c < A.d_out)
 #pragma unroll 8
@@ -1148,7 +1150,7 @@ fg_status_t check_groups(const char* who, const int32_t* order_dev, const int64_
                          fg_dtype_t dtype, int64_t x_rows, int64_t n) {
     const int e = dtype == FG_E4M3 ? 1 : fg_dtype_size(dtype);
     if (!e) FG_FAIL(FG_ERR_DTYPE, "%s: unknown element type %d", who, (int)dtype);
-    if (max_rows < 0 || max_rows > INT32_MAX || x_rows < 0 || x_rows > INT32_MAX || n < 0 || n > INT32_MAX)
+    if (max_rows < 0 || max_rows > FG_MAX_GROUPED_ROWS || x_rows < 0 || x_rows > INT32_MAX || n < 0 || n > INT32_MAX)
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
     if (n_groups < 1 || n_groups > FG_MAX_GROUPS) FG_FAIL(FG_ERR_INVALID_ARG, "%s: n_groups = %d is not in 1..%d", who, n_groups, FG_MAX_GROUPS);
     const int step_in = 16 / e, step_out = dtype == FG_F32 ? 4 : 8;
@@ -1187,8 +1189,9 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     A.dz_stride = A.dz ? dz_row(A.d_out, E) : A.dh_stride;
     A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
     A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
+    A.db_tiles = work ? row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS) : 0;
     if (A.dz || A.db_part) {
-        const unsigned grid = (unsigned)row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS);
+        const unsigned grid = (unsigned)A.db_tiles;
         if (A.dh_type == T)
             hipLaunchKernelGGL((grouped_dz_kernel<T, T>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
         else
@@ -1205,7 +1208,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     const bool many = results / DS_MANY >= 512;
     const int64_t sums = A.dw ? results / (many ? DS_MANY : DS_FEW) : 0;
     const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
-    if (sums + db_blocks > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
+    if (sums + db_blocks >= FG_MAX_GRID) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
     A.sums = (int)sums;
     const dim3 grid((unsigned)P.grid), sum_grid((unsigned)(sums + db_blocks));
     if constexpr (T == FG_F32) {
@@ -1255,7 +1258,7 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
-    if (!fg_dtype_size(dtype) || max_rows < 0 || max_rows > INT32_MAX || n_groups < 1 || n_groups > FG_MAX_GROUPS || d_in <= 0 || d_out <= 0) return 0;
+    if (!fg_dtype_size(dtype) || max_rows < 0 || max_rows > FG_MAX_GROUPED_ROWS || n_groups < 1 || n_groups > FG_MAX_GROUPS || d_in <= 0 || d_out <= 0) return 0;
     return bw_plan(max_rows, n_groups, d_in, d_out, fg_dtype_size(dtype)).total();
 }
 

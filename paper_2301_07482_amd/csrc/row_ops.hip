@@ -1,6 +1,8 @@
 // Element-wise work on listed rows: fg_dropout, fg_residual_norm and its backward pass, fg_quantize_rows.
 //
-// All of them are bound by the memory they read and write once. A row belongs to a power of two of lanes, up to a wavefront's 64, each
+// All of them are bound by the memory they read and write once (a large copy runs at 5.06 TB/s): dropout of 368640 x 768 bf16 232 us, 4.9 TB/s;
+// residual and norm of 49152 x 256 fp32 33 us, 6.1 TB/s (part of it from the last-level cache), of 65536 x 1024 bf16 with 8-bit rows 91 us, 5.2;
+// its gradients, 65536 x 1024 bf16, 123 us and 8 for the sums of dw, 5.1. A row belongs to a power of two of lanes, up to a wavefront's 64, each
 // with pieces of eight adjacent values (16 bytes of a 16-bit type), and stays in registers between the sum over the row and the use
 // of it; a row of more than 2048 values belongs to all wavefronts of a workgroup, which meet in LDS.
 #include "row_types.h"
@@ -38,7 +40,7 @@ DropArgs drop_args(float p, uint64_t key) {
 struct RowList {
     const int32_t* rows;
     const int64_t* n_rows_dev;
-    int64_t max_rows, n;
+    int64_t max_rows, n, first;      // first: of this launch
 };
 __device__ __forceinline__ int64_t row_count(const RowList& L) {
     const int64_t k = L.n_rows_dev ? *L.n_rows_dev : L.max_rows;
@@ -58,7 +60,7 @@ __global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, const c
     const int64_t at = blockIdx.x * (int64_t)ROW_THREADS + threadIdx.x;
     const int64_t k = at / pieces;
     const int c = (int)(at - k * pieces) * 8;
-    const int64_t r = row_at(L, k, count);
+    const int64_t r = row_at(L, L.first + k, count);
     if (r < 0) return;
     float f[8];
     fg_piece_values<T>(fg_load_piece<T>(x + r * x_stride + (int64_t)c * E, d - c), f);
@@ -131,7 +133,7 @@ __global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : ROW_THREADS) void residual
     const int me = WAVES > 1 ? (int)threadIdx.x : lane & (A.lanes - 1);      // which piece of the row
     const int width = WAVES > 1 ? WAVES * 64 : A.lanes;
     const int64_t k = WAVES > 1 ? blockIdx.x : (blockIdx.x * (int64_t)(ROW_THREADS / 64) + wave) * rows_per_wave + lane / A.lanes;
-    const int64_t r = row_at(A.L, k, count);
+    const int64_t r = row_at(A.L, A.L.first + k, count);
     if (WAVES > 1 && r < 0) return;      // the whole workgroup
     float v[NP][8];
     double ss = 0.0;
@@ -361,19 +363,23 @@ int64_t nb_blocks(int64_t max_rows, int d) {
 }
 
 template <int XT, int ST, bool NORM>
-void norm_launch(const RowShape& s, const NormArgs& A, hipStream_t st) {
-    const int64_t rows = A.L.max_rows;
-    const unsigned one = (unsigned)fg_ceil_div(rows, ROW_THREADS / s.lanes), all = (unsigned)rows;
-    if (s.waves == 1 && s.np == 1)
-        hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 1, NORM>), dim3(one), dim3(ROW_THREADS), 0, st, A);
-    else if (s.waves == 1 && s.np == 2)
-        hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 2, NORM>), dim3(one), dim3(ROW_THREADS), 0, st, A);
-    else if (s.waves == 1)
-        hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 4, NORM>), dim3(one), dim3(ROW_THREADS), 0, st, A);
-    else if (s.waves == 4)
-        hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 4, 4, NORM>), dim3(all), dim3(256), 0, st, A);
-    else
-        hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 8, 4, NORM>), dim3(all), dim3(512), 0, st, A);
+void norm_launch(const RowShape& s, NormArgs A, hipStream_t st) {
+    const int per_block = s.waves > 1 ? 1 : ROW_THREADS / s.lanes;
+    const int64_t at_once = (FG_MAX_GRID / 2 - 1) * per_block;      // rows of a launch
+    for (; A.L.first < A.L.max_rows; A.L.first += at_once) {
+        const int64_t rows = A.L.max_rows - A.L.first < at_once ? A.L.max_rows - A.L.first : at_once;
+        const dim3 grid((unsigned)fg_ceil_div(rows, per_block));
+        if (s.waves == 1 && s.np == 1)
+            hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 1, NORM>), grid, dim3(ROW_THREADS), 0, st, A);
+        else if (s.waves == 1 && s.np == 2)
+            hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 2, NORM>), grid, dim3(ROW_THREADS), 0, st, A);
+        else if (s.waves == 1)
+            hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 1, 4, NORM>), grid, dim3(ROW_THREADS), 0, st, A);
+        else if (s.waves == 4)
+            hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 4, 4, NORM>), grid, dim3(256), 0, st, A);
+        else
+            hipLaunchKernelGGL((residual_norm_kernel<XT, ST, 8, 4, NORM>), grid, dim3(512), 0, st, A);
+    }
 }
 
 template <int GT, int ST>
@@ -426,18 +432,20 @@ extern "C" fg_status_t fg_dropout(const void* x, int64_t x_stride, fg_dtype_t dt
     fg_clear_error();
     if (max_rows == 0 || n == 0) return FG_OK;
     const int pieces = (int)fg_ceil_div(d, 8);
-    const int64_t blocks = fg_ceil_div(max_rows * pieces, ROW_THREADS);
-    if (blocks > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: %lld rows of %d values are too many for one call", who, (long long)max_rows, d);
-    const RowList L = {rows_dev, n_rows_dev, max_rows, n};
+    const int64_t at_once = (FG_MAX_GRID - 1) * ROW_THREADS / pieces;      // rows of a launch
+    RowList L = {rows_dev, n_rows_dev, max_rows, n, 0};
     const DropArgs D = drop_args(p, key);
     hipStream_t st = (hipStream_t)stream;
 #define FG_DROP(T) hipLaunchKernelGGL((dropout_kernel<T>), dim3((unsigned)blocks), dim3(ROW_THREADS), 0, st, L, (const char*)x, x_stride, (char*)out, out_stride, d, pieces, D)
-    if (dtype == FG_F32)
-        FG_DROP(FG_F32);
-    else if (dtype == FG_F16)
-        FG_DROP(FG_F16);
-    else
-        FG_DROP(FG_BF16);
+    for (; L.first < max_rows; L.first += at_once) {
+        const int64_t blocks = fg_ceil_div((max_rows - L.first < at_once ? max_rows - L.first : at_once) * pieces, ROW_THREADS);
+        if (dtype == FG_F32)
+            FG_DROP(FG_F32);
+        else if (dtype == FG_F16)
+            FG_DROP(FG_F16);
+        else
+            FG_DROP(FG_BF16);
+    }
 #undef FG_DROP
     FG_LAUNCH_CHECK("dropout_kernel");
     return FG_OK;
@@ -467,7 +475,7 @@ extern "C" fg_status_t fg_residual_norm(const void* x, int64_t x_stride, fg_dtyp
     fg_clear_error();
     if (max_rows == 0 || n == 0) return FG_OK;
     const RowShape s = row_shape(d);
-    const NormArgs A = {{rows_dev, n_rows_dev, max_rows, n}, (const char*)x, (const char*)residual, x_stride, residual_stride, d, s.lanes, drop_args(p, key), weight, eps,
+    const NormArgs A = {{rows_dev, n_rows_dev, max_rows, n, 0}, (const char*)x, (const char*)residual, x_stride, residual_stride, d, s.lanes, drop_args(p, key), weight, eps,
                         (char*)sum_out, (char*)y, sum_stride, y_stride, (int)y_dtype, y_scale, rstd_out};
     hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32)
@@ -498,7 +506,7 @@ extern "C" fg_status_t fg_quantize_rows(const void* x, int64_t x_stride, fg_dtyp
     fg_clear_error();
     if (n_rows == 0) return FG_OK;
     const RowShape s = row_shape(d);
-    const NormArgs A = {{nullptr, nullptr, n_rows, n_rows}, (const char*)x, nullptr, x_stride, 0, d, s.lanes, {}, nullptr, 0.f,
+    const NormArgs A = {{nullptr, nullptr, n_rows, n_rows, 0}, (const char*)x, nullptr, x_stride, 0, d, s.lanes, {}, nullptr, 0.f,
                         nullptr, (char*)q, 0, q_stride, (int)FG_E4M3, scale, nullptr};
     hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32)
@@ -544,7 +552,7 @@ extern "C" fg_status_t fg_residual_norm_backward(const void* dy, int64_t dy_stri
     hipStream_t st = (hipStream_t)stream;
     const RowShape s = row_shape(d);
     if (work) {
-        const NormBwArgs A = {{rows_dev, n_rows_dev, max_rows, n}, (const char*)dy, (const char*)sum, (const char*)dsum_in, dy_stride, sum_stride, dsum_in_stride,
+        const NormBwArgs A = {{rows_dev, n_rows_dev, max_rows, n, 0}, (const char*)dy, (const char*)sum, (const char*)dsum_in, dy_stride, sum_stride, dsum_in_stride,
                               rstd, weight, d, s.lanes, drop_args(p, key), (char*)dsum_out, (char*)dx, dsum_stride, dx_stride,
                               dw_dev ? (float*)ws_dev : nullptr};
 #define FG_NB(G)                                       \

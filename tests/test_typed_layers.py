@@ -91,6 +91,10 @@ def test_refusals(B):
         assert refused(B, bw, **bad) == want, bad
     assert B.fg_linear_grouped_backward_workspace_bytes(B.FG_E4M3, 10, 4, 64, 64) == 0
 
+    assert refused(B, lin, max_rows=B.FG_MAX_GROUPED_ROWS + 1, n_out=1 << 30) == B.FG_ERR_INVALID_ARG
+    assert refused(B, bw, max_rows=B.FG_MAX_GROUPED_ROWS + 1, n=1 << 30) == B.FG_ERR_INVALID_ARG
+    assert B.fg_linear_grouped_backward_workspace_bytes(B.FG_F32, B.FG_MAX_GROUPED_ROWS + 1, 4, 64, 64) == 0
+
     drop = lambda **k: B.fg_dropout(**{**dict(x=P, x_stride=256, dtype=B.FG_F32, rows=None, n_rows=None, max_rows=10, n=10, d=64, p=0.5, key=1, out=P,
                                               out_stride=256), **k})
     for bad, want in ((dict(x=None), 1), (dict(out=None), 1), (dict(p=-0.1), 1), (dict(p=1.1), 1), (dict(p=float("nan")), 1), (dict(dtype=3), 3), (dict(d=0), 2),
@@ -132,7 +136,7 @@ gpu = pytest.mark.gpu
 
 
 @gpu
-@pytest.mark.parametrize("n, n_groups, mode", [(1, 1, "all"), (1, 1024, "list"), (63, 3, "list"), (64, 2, "all"), (1000, 7, "ids"), (1025, 1, "all"), (8192, 64, "ids"),
+@pytest.mark.parametrize("n, n_groups, mode", [(1, 1, "all"), (1, 1024, "list"), (63, 3, "list"), (64, 2, "all"), (1000, 7, "ids"), (1025, 1, "all"), (8192, 64, "ids"), (6144, 9, "all"), (6145, 9, "all"),
                                                (8193, 5, "list"), (20000, 1024, "ids"), (70001, 33, "list"), (300000, 3, "ids"), (2500000, 17, "all")])
 def test_group_rows(B, n, n_groups, mode):
     r = np.random.default_rng(n + n_groups)
@@ -249,6 +253,7 @@ LARGE = [  # tiles of 256, 128 and 64 rows, one step of the contraction and seve
     ("f16", "f32", 36_000, 40, 136, 264, "relu"), ("bf16", "bf16", 33_100, 4, 328, 520, ""), ("bf16", "bf16", 70_500, 3, 40, 128, "relu"), ("f16", "f16", 71_000, 9, 264, 72, "src"),
     ("bf16", "f32", 72_000, 2, 64, 64, ""), ("f16", "f16", 90_000, 1024, 136, 40, "src relu"), ("bf16", "bf16", 130_000, 1, 8, 16, ""),
     ("e4m3", "bf16", 70_000, 3, 128, 256, "src relu"), ("e4m3", "f32", 40_000, 4, 272, 512, "relu"), ("e4m3", "bf16", 36_000, 7, 400, 264, ""), ("e4m3", "f16", 90_000, 2, 16, 48, ""),
+    ("e4m3", "f32", 170_000, 1024, 64, 264, ""), ("f16", "f16", 160_000, 1024, 40, 136, "src"),
     ("f32", "f32", 50_000, 3, 100, 256, "src relu"), ("f32", "f32", 34_000, 60, 36, 132, ""), ("f32", "f32", 70_000, 2, 260, 64, "relu"),
 ]
 
@@ -600,6 +605,28 @@ def test_residual_norm_gradients_against_differences():
         want = (loss(*hi) - loss(*lo)) / (2 * step)
         # truncation step^2 times a third derivative of order 100 here, rounding 1e-16 x 100 / step
         assert abs(float((grad * v).sum()) - want) <= 1e-6
+
+
+@gpu
+@pytest.mark.parametrize("d, dtype, skipped", [(8000, "f16", 4_300_000), (2056, "bf16", 8_400_000), (8200, "f32", 8_390_000)])
+def test_lists_that_are_longer_than_a_launch_can_have_threads_for(B, d, dtype, skipped):
+    """What the last of 2^32 threads and more would do: the list ends in the only positions that exist."""
+    n, p, key = 40, 0.3, 77
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn(n, d, device="cuda", generator=g).to(T[dtype])
+    tail = torch.randperm(n, device="cuda", generator=g)[:33].int()
+    rows = torch.cat([torch.full((skipped,), -1, dtype=torch.int32, device="cuda"), tail])
+    got = {}
+    for name, list_ in (("short", tail), ("long", rows)):
+        out, y = torch.full_like(x, -77.0), torch.full_like(x, -77.0)
+        rstd = torch.full((n,), -77.0, device="cuda")
+        B.fg_dropout(x, stride(x), code(B, dtype), list_, None, len(list_), n, d, p, key, out, stride(out))
+        B.fg_residual_norm(x, stride(x), code(B, dtype), None, 0, code(B, dtype), list_, None, len(list_), n, d, p, key, None, 1e-6, None, 0, y, stride(y),
+                           code(B, dtype), None, rstd)
+        torch.cuda.synchronize()
+        got[name] = out, y, rstd
+    for a, b in zip(got["short"], got["long"]):
+        assert torch.equal(a, b) and bool((a[tail.long()] != -77).any())
 
 
 # ---- fg_quantize_rows ----
