@@ -634,9 +634,12 @@ __device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int r
 }
 
 // dz in entry order, in the rows' type, and its column sums by tiles of GZ_ROWS entries of one group (db is their sum). The products then
-// read dz alone, straight to LDS; a mask on the way there would take both matrices through registers, twice. Bound by memory: 58982 x 1024
-// bf16 72 us (5.0 TB/s, the rate of a copy), 43352 x 256 fp32 23 us (5.7, part of it from the last-level cache).
-constexpr int GZ_ROWS = 64, GZ_THREADS = 256;
+// read dz alone, straight to LDS; a mask on the way there would take both matrices through registers, twice (for one tile of columns of x it was tried in
+// the fp32 weight gradients, with dz and db's sums as by-products: 102.9 us a backward call against 103.5). Bound by memory: 58982 x 1024
+// bf16 72 us (5.0 TB/s, the rate of a copy), 43352 x 256 fp32 23 us (5.7, part of it from the last-level cache). Few rows are bound by latency:
+// hence 256 columns to a workgroup and four rows' reads on their way together (2000 x 1000 bf16 5 us more than dx alone takes; 20 with all the
+// columns in one workgroup, row after row).
+constexpr int GZ_ROWS = 64, GZ_THREADS = 256, GZ_COLUMNS = 256;
 
 template <int T, int D>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
@@ -652,43 +655,51 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
         entry(A, k0 + t, k1, pos[t], s);
     }
     __syncthreads();
-    const int rows = (int)(k1 - k0), pieces = (A.d_out + 7) / 8;
-    int side = 1;      // rows side by side
+    // this workgroup's columns, and how many rows of them its threads have side by side
+    const int first = (int)blockIdx.y * (GZ_COLUMNS / 8), rows = (int)(k1 - k0);
+    const int pieces = (A.d_out + 7) / 8 - first < GZ_COLUMNS / 8 ? (A.d_out + 7) / 8 - first : GZ_COLUMNS / 8;
+    int side = GZ_THREADS / (GZ_COLUMNS / 8);
     while (side * 2 * pieces <= GZ_THREADS) side *= 2;
-    const int width = GZ_THREADS / side;      // threads of a row
-    for (int p0 = 0; p0 < pieces; p0 += width) {
-        const int p = p0 + t % width, c = p * 8;
-        float sum[8] = {};
-        if (p < pieces) {
-#pragma unroll 4
-            for (int m = t / width; m < rows; m += side) {
-                const int32_t r = pos[m];
-                float z[8] = {};
-                if (r >= 0) {
-                    fg_piece_values<D>(fg_load_piece<D>(A.dh + r * A.dh_stride + (int64_t)c * DE, A.d_out - c), z);
-                    if (A.h) {
-                        float h[8];
-                        fg_piece_values<T>(fg_load_piece<T>(A.h + r * A.h_stride + (int64_t)c * E, A.d_out - c), h);
+    const int width = GZ_THREADS / side, p = t % width, c = (first + p) * 8, left = A.d_out - c;
+    float sum[8] = {};
+    if (p < pieces) {
+        constexpr int AHEAD = 4;      // rows whose reads are on their way together
+        for (int m0 = t / width; m0 < rows; m0 += AHEAD * side) {
+            fg_piece<D> pz[AHEAD];
+            fg_piece<T> ph[AHEAD];
+            int32_t r[AHEAD];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] = h[e] > 0.f ? z[e] : 0.f;
-                    }
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = m0 + u * side;
+                r[u] = m < rows ? pos[m] : -1;
+                if (r[u] >= 0) pz[u] = fg_load_piece<D>(A.dh + r[u] * A.dh_stride + (int64_t)c * DE, left);
+                if (r[u] >= 0 && A.h) ph[u] = fg_load_piece<T>(A.h + r[u] * A.h_stride + (int64_t)c * E, left);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = m0 + u * side;
+                float z[8] = {};
+                if (r[u] >= 0) fg_piece_values<D>(pz[u], z);
+                if (r[u] >= 0 && A.h) {
+                    float h[8];
+                    fg_piece_values<T>(ph[u], h);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = h[e] > 0.f ? z[e] : 0.f;
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) sum[e] += z[e];
-            if (A.dz) fg_store_piece<T>(A.dz + (k0 + m) * A.dz_stride + (int64_t)c * E, z, A.d_out - c);
+                if (A.dz && m < rows) fg_store_piece<T>(A.dz + (k0 + m) * A.dz_stride + (int64_t)c * E, z, left);
             }
         }
-        if (A.db_part) {
-            __syncthreads();
+    }
+    if (!A.db_part) return;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sums[t * 8 + e] = sum[e];
-            __syncthreads();
-            for (int i = t; i < width * 8; i += GZ_THREADS) {
-                float v = 0.f;
-                for (int q = 0; q < side; ++q) v += sums[q * width * 8 + i];
-                if (p0 * 8 + i < A.d_out) A.db_part[(int64_t)blockIdx.x * A.d_out + p0 * 8 + i] = v;
-            }
-        }
+    for (int e = 0; e < 8; ++e) sums[t * 8 + e] = sum[e];
+    __syncthreads();
+    for (int i = t; i < width * 8; i += GZ_THREADS) {
+        float v = 0.f;
+        for (int q = 0; q < side; ++q) v += sums[q * width * 8 + i];
+        if (first * 8 + i < A.d_out && i < GZ_COLUMNS) A.db_part[(int64_t)blockIdx.x * A.d_out + first * 8 + i] = v;
     }
 }
 
@@ -1115,8 +1126,9 @@ struct BwPlan {
 };
 // Ranges of rows for bm x bm tiles. As many as give every place on the chip a tile; of more tiles than places two ranges where that leaves fewer of
 // them idle. But a part of a tile that is written and read again costs what reading its operands for bm rows costs: a range has DW_MIN_ROWS rows
-// at least, where that leaves DW_MIN_GROUPS workgroups (dW alone, bf16, 4096 x 256 x 256: 18 us, 21 with shorter ranges; 2000 x 64 x 64: 19 | 14).
-constexpr int DW_MIN_ROWS = 128, DW_MIN_GROUPS = 64;
+// at least, where that leaves DW_MIN_GROUPS workgroups. (dW alone, us: bf16, 4096 x 256 x 256, 18 with such ranges, 21 with shorter ones; fp32, 2000 x
+// 256 x 256 in 40 groups 33 with 256 workgroups, 48 with 64; 8000 x 64 x 64 in 100 groups 44 and 58.)
+constexpr int DW_MIN_ROWS = 128, DW_MIN_GROUPS = 256;
 int dw_ranges(int64_t max_rows, int n_groups, int64_t tiles, int bm, int e) {
     const int rows = e == 4 ? GF_K : GW_ROWS;
     const int64_t steps = max_rows / rows + (n_groups < max_rows ? n_groups : max_rows), places = bm == 256 ? 256 : 512;
@@ -1191,11 +1203,11 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
     A.db_tiles = work ? row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS) : 0;
     if (A.dz || A.db_part) {
-        const unsigned grid = (unsigned)A.db_tiles;
+        const dim3 grid((unsigned)A.db_tiles, (unsigned)fg_ceil_div(A.d_out, GZ_COLUMNS));
         if (A.dh_type == T)
-            hipLaunchKernelGGL((grouped_dz_kernel<T, T>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
+            hipLaunchKernelGGL((grouped_dz_kernel<T, T>), grid, dim3(GZ_THREADS), 0, st, A);
         else
-            hipLaunchKernelGGL((grouped_dz_kernel<T, FG_F32>), dim3(grid), dim3(GZ_THREADS), 0, st, A);
+            hipLaunchKernelGGL((grouped_dz_kernel<T, FG_F32>), grid, dim3(GZ_THREADS), 0, st, A);
         FG_LAUNCH_CHECK("grouped_dz_kernel");
     }
     if (A.out && work) {
