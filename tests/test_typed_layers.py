@@ -680,6 +680,33 @@ OUTPUTS = ("order", "offsets", "h", "sum", "y", "rstd", "dres", "dh", "dgain", "
 
 
 @gpu
+@pytest.mark.parametrize("bound", [0, 1, 300, 9000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_is_listed(B, dtype, bound):
+    """A count of zero on the device under any bound: sums are zeros, nothing else is touched."""
+    n, G, d = max(bound, 4), 3, 64
+    x, zero = torch.randn(n, d, device="cuda").to(T[dtype]), torch.zeros(1, dtype=torch.int64, device="cuda")
+    c = code(B, dtype)
+    order = torch.full((max(bound, 1),), -77, dtype=torch.int32, device="cuda")
+    offsets = torch.full((G + 1,), -77, dtype=torch.int64, device="cuda")
+    ws = torch.full((1 << 26,), 255, dtype=torch.uint8, device="cuda")      # more than any of the calls needs
+    B.fg_group_rows(torch.zeros(n, dtype=torch.int32, device="cuda"), n, None, n, None, zero, bound, G, order, offsets, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert bool((order == -77).all()) and bool((offsets == 0).all())
+    W, h, dx = torch.randn(G, d, d, device="cuda").to(T[dtype]), torch.full_like(x, -77.0), torch.full_like(x, -77.0)
+    B.fg_linear_grouped(x, n, stride(x), c, None, None, order, offsets, bound, G, d, d, W, None, None, 1, h, n, stride(h), c)
+    dw, db = torch.full((G, d, d), -77.0, device="cuda"), torch.full((G, d), -77.0, device="cuda")
+    B.fg_linear_grouped_backward(x, n, stride(x), c, None, x, stride(x), c, x, stride(x), n, order, offsets, bound, G, d, d, W, dx, stride(dx), c, dw, db, ws, ws.numel())
+    y, rstd, gw = torch.full_like(x, -77.0), torch.full((n,), -77.0, device="cuda"), torch.full((d,), -77.0, device="cuda")
+    B.fg_dropout(x, stride(x), c, None, zero, bound, n, d, 0.5, 1, y, stride(y))
+    B.fg_residual_norm(x, stride(x), c, None, 0, c, None, zero, bound, n, d, 0.5, 1, None, 1e-6, None, 0, y, stride(y), c, None, rstd)
+    B.fg_residual_norm_backward(x, stride(x), c, x, stride(x), c, rstd, None, None, 0, None, zero, bound, n, d, 0.5, 1, y, stride(y), None, 0, gw, ws, ws.numel())
+    torch.cuda.synchronize()
+    assert all(bool((t == -77).all()) for t in (h, dx, y, rstd))
+    assert all(not bool(t.any()) for t in (dw, db, gw))
+
+
+@gpu
 def test_a_typed_layer_and_its_gradients(B):
     """The calls one behind the other, as a training step makes them, against automatic differentiation in 64 bits."""
     n, G, a, b, p, key = 700, 4, 52, 88, 0.3, 4242
