@@ -198,14 +198,14 @@ __device__ __forceinline__ void split8(const fg_u32x4 (&v)[2], fg_u32x4 (&u)[3])
 
 constexpr int GL_STEP = 128, GL_PIECES = GL_STEP / 16, GL_ROWS = 1024 / GL_STEP;      // bytes of K per step; 16-byte pieces of a row; rows of a load
 constexpr int EP_BLOCK = 16 * 128;      // bytes of an epilogue's block
-// the operands' ring, the epilogue's blocks, what belongs to a tile (twice), the offsets
-constexpr size_t gl_lds_bytes(int bm, int bn, int waves, int ring, bool eight, int n_groups) {
-    return (size_t)ring * (bm + bn) * GL_STEP + (size_t)waves * EP_BLOCK + (size_t)2 * (8 * bm + 4 * bn + (eight ? 4 * (bm + bn) : 32)) + (size_t)(n_groups + 1) * 4;
+// the operands' two buffers, the epilogue's blocks, what belongs to a tile (twice), the offsets
+constexpr size_t gl_lds_bytes(int bm, int bn, int waves, bool eight, int n_groups) {
+    return (size_t)2 * (bm + bn) * GL_STEP + (size_t)waves * EP_BLOCK + (size_t)2 * (8 * bm + 4 * bn + (eight ? 4 * (bm + bn) : 32)) + (size_t)(n_groups + 1) * 4;
 }
 // max(v, 0), a NaN stays one
 __device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise_maximum(v, 0.f); }
 
-template <int T, int BM, int BN, int WAVES_M, int WAVES_N, int RING, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN, bool WIDE>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int E = T == FG_E4M3 ? 1 : T == FG_F32 ? 4 : 2, BK = GL_STEP / E;
@@ -216,14 +216,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
     static_assert(A_LOADS * GL_ROWS * WAVES == BM && B_LOADS * GL_ROWS * WAVES == BN, "whole loads");
-    // LDS: the ring; the epilogue's blocks; what belongs to a tile, for the current one and the next; the offsets of the groups
+    // LDS: two steps' operands; the epilogue's blocks; what belongs to a tile, for the current one and the next; the offsets of the groups
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     struct TileData {
         int32_t pos[BM], src[BM];      // position and row of A of every row, -1: none
         float x_scale[T == FG_E4M3 ? BM : 4], bias[BN], w_scale[T == FG_E4M3 ? BN : 4];
     };
-    char* const blocks = gl_lds + RING * STAGE;
+    char* const blocks = gl_lds + 2 * STAGE;
     TileData* data = (TileData*)(blocks + WAVES * EP_BLOCK);
     int32_t* offsets = (int32_t*)(data + 2);
     for (int i = t; i <= A.G.n_groups; i += THREADS) offsets[i] = (int32_t)group_offset(A.G, i);
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds;
     const int steps = (K + BK - 1) / BK;
     auto load_step = [&](int s) {
-        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (unsigned)s % RING * STAGE + wave * 1024);
+        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + (s & 1) * STAGE + wave * 1024);
         const int left = K - s * BK;      // elements of K that the step has
         const char* const w = uniform(w_at);
         if (left >= BK) {
@@ -345,19 +345,21 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     const int wm = (wave / WAVES_N) * (BM / WAVES_M), wn = (wave % WAVES_N) * WN;
     gl_f32x16 acc[MB][NB], rest[T == FG_F32 ? MB : 1][T == FG_F32 ? NB : 1];      // fp32: the leading products, the others
     const int swap = exchanged(l32) << 4;
-    static_assert(RING == 2 && SUB % 2 == 0, "one step ahead; the operands' two sets in turn");
+    static_assert(SUB % 2 == 0, "the operands' two sets in turn");
+    static_assert(WN <= 64, "a row of a wavefront's columns in 16 bits fits a row of the epilogue's block");
+    static_assert(2 * STAGE + WAVES * EP_BLOCK + 2 * sizeof(TileData) + 4 == gl_lds_bytes(BM, BN, WAVES, T == FG_E4M3, 0), "what the launch asks for");
     const int place = (lane >> 2) & 3;
     const int b_in = (8 * half + place) * B_ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     struct Operands {
         fg_u32x4 a[MB][PARTS], b[NB][PARTS];
     };
     auto read_a = [&](int s, int kk, int mb, Operands& F) {
-        const char* As = gl_lds + (unsigned)s % RING * STAGE + (wm + l32) * GL_STEP;
+        const char* As = gl_lds + (s & 1) * STAGE + (wm + l32) * GL_STEP;
 #pragma unroll
         for (int q = 0; q < DEEP; ++q) F.a[mb][q] = *(const fg_u32x4*)(As + mb * 32 * GL_STEP + ((((kk * DEEP + q) * 2 + half) << 4) ^ swap));
     };
     auto read_b = [&](int s, int kk, Operands& F) {
-        const char* Bs = gl_lds + (unsigned)s % RING * STAGE + BM * GL_STEP;
+        const char* Bs = gl_lds + (s & 1) * STAGE + BM * GL_STEP;
         if constexpr (!B_KN)
 #pragma unroll
             for (int q = 0; q < DEEP; ++q)
@@ -589,15 +591,15 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     }
 }
 
-template <int T, int BM, int BN, int WM, int WN, int RING, int PER_CU, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN, bool WIDE>
 fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
     A.tiles_n = (int)fg_ceil_div(A.N, BN);
     const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
     if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
     const int64_t at_once = 256 * PER_CU;
-    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, RING, B_KN, WIDE>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
-                       gl_lds_bytes(BM, BN, WM * WN, RING, T == FG_E4M3, A.G.n_groups), st, A);
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN, WIDE>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
+                       gl_lds_bytes(BM, BN, WM * WN, T == FG_E4M3, A.G.n_groups), st, A);
     FG_LAUNCH_CHECK("grouped_tile_kernel");
     return FG_OK;
 }
@@ -614,10 +616,10 @@ template <int T, bool B_KN, bool WIDE>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
     if constexpr (T != FG_F32 && (T != FG_E4M3 || WIDE))
-        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 2, 1, B_KN, WIDE>(who, A, st);
+        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN, WIDE>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, 2, B_KN, WIDE>(who, A, st);
-    return tile_launch<T, 64, 64, 2, 2, 2, 4, B_KN, WIDE>(who, A, st);
+    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN, WIDE>(who, A, st);
+    return tile_launch<T, 64, 64, 2, 2, 4, B_KN, WIDE>(who, A, st);
 }
 
 // ---- gradients ----
