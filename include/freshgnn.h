@@ -829,8 +829,7 @@ fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int3
  *   bias [n_groups x d_out]             float, or NULL;  relu != 0: act = ReLU
  *   h_out, n_out, out_stride            rows of out_dtype (FG_F32, FG_F16 or FG_BF16; FG_F32 for FG_F32 rows) by position
  * Products: fp32 rows as in fg_linear (from exact three-way bf16 splits, fp32 sums; same input domain); the narrower types are multiplied
- * as they are. Sums in fp32, one rounding to out_dtype; FG_E4M3 rows with FG_BF16 outputs take the 8-bit matrix instructions, which drop what is below
- * 2^-13 of the largest of eight adjacent products. d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types);
+ * as they are (8 bits as the bf16 values they are). Sums in fp32, one rounding to out_dtype. d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types);
  * x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
  * [0, x_rows) are skipped.
  */

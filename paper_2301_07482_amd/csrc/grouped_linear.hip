@@ -107,8 +107,8 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 // fg_linear. The values lie in LDS as they are and are split as they are read: the split costs about the vector instructions that the
 // products cost matrix instructions.
 //
-// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 98 us
-// (1.26 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
+// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 120 us
+// (1.03 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
 // 2.0 us for the 1.15 us that its matrix instructions take by themselves and the 0.85 us that LDS is busy with them; tiles of 256 x 256 on four
 // wavefronts, with a third fewer LDS reads, took 1010 us instead of 702 (nothing fills the waits of a lone wavefront), tiles of 128 x 256 two
 // to a compute unit 12 % longer.
@@ -117,7 +117,6 @@ __device__ __attribute__((aligned(16))) unsigned int gl_zero[4];
 __device__ __attribute__((aligned(16))) unsigned int gl_sink[4 * 64];
 
 typedef float gl_f32x16 __attribute__((ext_vector_type(16)));
-typedef int gl_i32x8 __attribute__((ext_vector_type(8)));
 typedef short gl_s16x4 __attribute__((ext_vector_type(4)));
 
 // an address that is the same in all lanes, in scalar registers
@@ -140,25 +139,17 @@ __device__ __forceinline__ void arrived() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// 8-bit products. The 8-bit matrix instructions add groups of eight adjacent products with 13 bits below the largest of the group (measured: of 2^16
-// and 1 in one group the 1 is lost, in two groups it is not; the sums are off by up to 1.5e-4 of the largest product), the groups in fp32. An
-// output in bf16, which is rounded to 2^-8, takes that for twice the rate: 1.3e-5 of the result's norm for normally distributed rows, 6e-5 for rows
-// whose values spread over e^2, beside 1.7e-3 of the rounding. For the other outputs (WIDE) the operands become bf16, which holds every 8-bit
-// value, and are multiplied as such, in fp32 throughout: 1e-7.
-template <int T, bool WIDE>
+// 8-bit values become bf16, which holds every one of them, and are multiplied as such (two instructions to an operand's 16 bytes), with sums in fp32
+// throughout. The 8-bit matrix instructions are not used: they add groups of eight adjacent products with 13 bits below the largest of the group
+// (measured: of 2^16 and 1 in one group the 1 is lost), so that of a row with a large value in every eight the others are lost, and where the large
+// products cancel nothing of the result is right. They would take 84 us instead of 120 for 58982 x 1024 x 1024 to bf16 with 16 groups.
+template <int T>
 __device__ __forceinline__ gl_f32x16 mfma(const fg_u32x4* a, const fg_u32x4* b, gl_f32x16 c) {
-    if constexpr (T == FG_BF16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
-    else if constexpr (T == FG_F16)
+    if constexpr (T == FG_F16)
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(fg_f16x8, a[0]), __builtin_bit_cast(fg_f16x8, b[0]), c, 0, 0, 0);
-    else if constexpr (WIDE) {
-        c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[1]), __builtin_bit_cast(fg_bf16x8, b[1]), c, 0, 0, 0);
-    } else {      // (the block scales of the instruction are 2^0)
-        const gl_i32x8 av = __builtin_bit_cast(gl_i32x8, __builtin_shufflevector(a[0], a[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        const gl_i32x8 bv = __builtin_bit_cast(gl_i32x8, __builtin_shufflevector(b[0], b[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, c, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
-    }
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[0]), __builtin_bit_cast(fg_bf16x8, b[0]), c, 0, 0, 0);
+    if constexpr (T == FG_E4M3) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(fg_bf16x8, a[1]), __builtin_bit_cast(fg_bf16x8, b[1]), c, 0, 0, 0);
+    return c;
 }
 // sixteen 8-bit values as twice eight bf16
 __device__ __forceinline__ void widen(fg_u32x4 v, fg_u32x4 (&out)[2]) {
@@ -205,13 +196,13 @@ constexpr size_t gl_lds_bytes(int bm, int bn, int waves, bool eight, int n_group
 // max(v, 0), a NaN stays one
 __device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise_maximum(v, 0.f); }
 
-template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int E = T == FG_E4M3 ? 1 : T == FG_F32 ? 4 : 2, BK = GL_STEP / E;
     constexpr int STAGE = (BM + BN) * GL_STEP, A_LOADS = BM / GL_ROWS / WAVES, B_LOADS = BN / GL_ROWS / WAVES, LOADS = A_LOADS + B_LOADS;
     constexpr int MB = BM / WAVES_M / 32, NB = BN / WAVES_N / 32, WN = BN / WAVES_N;
-    constexpr int DEEP = T == FG_F32 || (T == FG_E4M3 && !WIDE) ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
+    constexpr int DEEP = T == FG_F32 ? 2 : 1, SUB = GL_STEP / 32 / DEEP;      // 16-byte pieces of a lane's operand; operands per step
     constexpr int PARTS = T == FG_E4M3 || T == FG_F32 ? 2 : 1;                                          // 16-byte registers of it
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
@@ -385,9 +376,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     auto multiply_row = [&](const Operands& F, int mb) {
         if constexpr (T != FG_F32) {
             fg_u32x4 a[2];
-            if constexpr (WIDE) widen(F.a[mb][0], a);
+            if constexpr (T == FG_E4M3) widen(F.a[mb][0], a);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, WIDE>(F.b[nb], WIDE ? a : F.a[mb], acc[mb][nb]);
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T>(F.b[nb], T == FG_E4M3 ? a : F.a[mb], acc[mb][nb]);
         }
     };
     auto multiply = [&](Operands& F) {
@@ -403,9 +394,9 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
                 for (int e = 0; e < 5; ++e)
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) rest[mb][nb] = mfma<FG_BF16, false>(&b[TB[e]], &a[mb][TA[e]], rest[mb][nb]);
+                    for (int mb = 0; mb < MB; ++mb) rest[mb][nb] = mfma<FG_BF16>(&b[TB[e]], &a[mb][TA[e]], rest[mb][nb]);
 #pragma unroll
-                for (int mb = 0; mb < MB; ++mb) acc[mb][nb] = mfma<FG_BF16, false>(&b[0], &a[mb][0], acc[mb][nb]);
+                for (int mb = 0; mb < MB; ++mb) acc[mb][nb] = mfma<FG_BF16>(&b[0], &a[mb][0], acc[mb][nb]);
             }
         }
     };
@@ -441,7 +432,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
                 if (LOAD) load_step(s + 2);
             }
             if (more) read_b(to_s, to_kk, ahead);
-            if constexpr (WIDE)
+            if constexpr (T == FG_E4M3)
 #pragma unroll
                 for (int nb = 0; nb < NB; ++nb) widen(now.b[nb][0], now.b[nb]);
 #pragma unroll
@@ -591,14 +582,14 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     }
 }
 
-template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN, bool WIDE>
+template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN>
 fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
     A.tiles_n = (int)fg_ceil_div(A.N, BN);
     const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
     if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
     const int64_t at_once = 256 * PER_CU;
-    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN, WIDE>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
                        gl_lds_bytes(BM, BN, WM * WN, T == FG_E4M3, A.G.n_groups), st, A);
     FG_LAUNCH_CHECK("grouped_tile_kernel");
     return FG_OK;
@@ -607,19 +598,19 @@ fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
 //
 // The largest tile that there are as many of as compute units, and that the columns and an average group more than half fill. Both sides in us
 // (K = N = 256 unless said, 4 groups):
-//   256 against 128, bf16: 65536 rows 18.6 | 20.0, 32768 rows 16.6 | 13.1; N = 128 17.8 | 12.9; 193 rows a group 30.3 | 31.2, 128 rows a group 32.7 | 25.5
-//   128 against 64: 16384 rows bf16 9.6 | 11.1, fp32 21.4 | 22.5, 8 bits 8.5 | 9.5; 8192 rows 8.7 | 7.1, 20.1 | 13.7, 7.9 | 6.0; N = 64 fp32 32.6 | 22.7;
-//                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 56 | 61; 64 rows a group 43 | 53, 134 | 115, 66 | 46
-// No 256 x 256 tile for fp32, whose two sums do not fit the registers, nor with the 8-bit instructions, whose long operands fit them only one row
-// of blocks at a time: 65536 x 1024 x 1024 149 us a pass against 151.
-template <int T, bool B_KN, bool WIDE>
+//   256 against 128, bf16: 65536 rows 18.6 | 20.0, 32768 rows 16.6 | 13.1; N = 128 17.8 | 12.9; 193 rows a group 30.3 | 31.2, 128 rows a group 32.7 | 25.5;
+//                   8 bits: 65536 rows 20.3 | 21.0, K = N = 1024 121 | 136, 32768 rows 16.9 | 12.2; N = 128 17.4 | 12.3; 193 rows a group 33.7 | 30.2, 128 rows a group 36.0 | 25.4
+//   128 against 64: 16384 rows bf16 9.6 | 11.1, fp32 21.4 | 22.5, 8 bits 9.3 | 10.2; 8192 rows 8.7 | 7.1, 20.1 | 13.7, 8.6 | 6.5; N = 64 fp32 32.6 | 22.7;
+//                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 62 | 65; 64 rows a group 43 | 53, 134 | 115, 72 | 49
+// No 256 x 256 tile for fp32, whose two sums do not fit the registers.
+template <int T, bool B_KN>
 fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
-    if constexpr (T != FG_F32 && (T != FG_E4M3 || WIDE))
-        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN, WIDE>(who, A, st);
+    if constexpr (T != FG_F32)
+        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN>(who, A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN, WIDE>(who, A, st);
-    return tile_launch<T, 64, 64, 2, 2, 4, B_KN, WIDE>(who, A, st);
+    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN>(who, A, st);
+    return tile_launch<T, 64, 64, 2, 2, 4, B_KN>(who, A, st);
 }
 
 // ---- gradients ----
@@ -824,7 +815,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T, false>(&F.a[mb], &F.b[nb], acc[mb][nb]);
+            for (int nb = 0; nb < NB; ++nb) acc[mb][nb] = mfma<T>(&F.a[mb], &F.b[nb], acc[mb][nb]);
     };
 
     for (; W.next(A.G, GW_ROWS); W.at += W.last - W.first) {      // uniform over the workgroup
@@ -1073,11 +1064,11 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
 #pragma unroll
                     for (int i = 0; i < B; ++i)
 #pragma unroll
-                        for (int j = 0; j < B; ++j) rest[i][j] = mfma<FG_BF16, false>(&a[i][TA[e]], &b[j][TB[e]], rest[i][j]);
+                        for (int j = 0; j < B; ++j) rest[i][j] = mfma<FG_BF16>(&a[i][TA[e]], &b[j][TB[e]], rest[i][j]);
 #pragma unroll
                 for (int i = 0; i < B; ++i)
 #pragma unroll
-                    for (int j = 0; j < B; ++j) lead[i][j] = mfma<FG_BF16, false>(&a[i][0], &b[j][0], lead[i][j]);
+                    for (int j = 0; j < B; ++j) lead[i][j] = mfma<FG_BF16>(&a[i][0], &b[j][0], lead[i][j]);
             }
         };
         fill(k0);
@@ -1214,7 +1205,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     }
     if (A.out && work) {
         A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
-        FG_TRY((tile_product<T, false, false>(who, A, st)));
+        FG_TRY((tile_product<T, false>(who, A, st)));
     }
     if (!A.dw && !A.db) return FG_OK;
     A.ranges = P.ranges;
@@ -1264,11 +1255,10 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu;
     A.x_scale = x_scale, A.w_scale = w_scale, A.bias = bias, A.src_ids = src_ids_dev, A.out = (char*)h_out;
     A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
-    if (dtype == FG_BF16) return tile_product<FG_BF16, true, false>(who, A, (hipStream_t)stream);
-    if (dtype == FG_F16) return tile_product<FG_F16, true, false>(who, A, (hipStream_t)stream);
-    if (dtype == FG_E4M3 && out_dtype != FG_BF16) return tile_product<FG_E4M3, false, true>(who, A, (hipStream_t)stream);
-    if (dtype == FG_E4M3) return tile_product<FG_E4M3, false, false>(who, A, (hipStream_t)stream);
-    return tile_product<FG_F32, true, false>(who, A, (hipStream_t)stream);
+    if (dtype == FG_BF16) return tile_product<FG_BF16, true>(who, A, (hipStream_t)stream);
+    if (dtype == FG_F16) return tile_product<FG_F16, true>(who, A, (hipStream_t)stream);
+    if (dtype == FG_E4M3) return tile_product<FG_E4M3, false>(who, A, (hipStream_t)stream);
+    return tile_product<FG_F32, true>(who, A, (hipStream_t)stream);
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {

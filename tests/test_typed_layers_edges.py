@@ -1,0 +1,45 @@
+"""The calls of a typed layer where one kind of input decides: 8-bit rows whose products differ by many orders of magnitude, entries that are
+skipped in the gradients, lists longer than a launch, limits. Tolerances as in tests/test_typed_layers.py: a sum of K products in fp32 is granted
+K steps of 2^-23 of the sum of the products' magnitudes, a result half a step of its type."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_typed_layers import HALF, T, TINY, B, close, code, cuda, gpu, refused, stride  # noqa: F401 (B: the fixture)
+
+
+def e4m3(v):
+    q = v.to(torch.float8_e4m3fn)
+    assert torch.equal(q.to(v.dtype), v), "values that 8 bits hold"
+    return q
+
+
+# ---- 8-bit rows ----
+
+@gpu
+@pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("signs", ["alternating", "equal", "random"])
+@pytest.mark.parametrize("n, n_groups, d_in, d_out", [(150, 3, 64, 40), (300, 2, 400, 136), (34_000, 3, 80, 264), (68_000, 2, 64, 512)])
+def test_8_bit_rows_with_one_large_value_in_eight(B, n, n_groups, d_in, d_out, signs, out):
+    """A feature in eight whose products are 2^13 times the others' and more, as outlying features of activations are. Where the large products
+    cancel, what is left is made of the small ones."""
+    g = torch.Generator(device="cuda").manual_seed(n + d_in)
+    kw = dict(device="cuda", generator=g)
+    pick = lambda *s: 2.0 ** torch.randint(-1, 3, s, **kw).float() * (1 - 2 * torch.randint(0, 2, s, **kw)).float()
+    x, W = pick(n, d_in), pick(n_groups, d_out, d_in)
+    eighth = torch.arange(0, d_in, 8, device="cuda") + 3
+    sign = {"alternating": 1 - 2 * (torch.arange(len(eighth), device="cuda") % 2), "equal": torch.ones(len(eighth), device="cuda"),
+            "random": 1 - 2 * torch.randint(0, 2, (n, len(eighth)), **kw)}[signs].float()
+    x[:, eighth], W[:, :, eighth] = 256.0 * sign.expand(n, -1), 256.0
+    xs, ws = torch.rand(n, **kw) * 2.0 ** -7, torch.rand(n_groups * d_out, **kw) * 2.0 ** -7
+    types = torch.randint(0, n_groups, (n,), **kw).sort()
+    offsets = torch.searchsorted(types.values, torch.arange(n_groups + 1, device="cuda"))
+    order = torch.randperm(n, **kw).int()
+    h = torch.full((n, d_out), -77.0, dtype=T[out], device="cuda")
+    B.fg_linear_grouped(e4m3(x), n, d_in, B.FG_E4M3, xs, None, order, offsets, n, n_groups, d_in, d_out, e4m3(W), ws, None, 0, h, n, stride(h), code(B, out))
+    torch.cuda.synchronize()
+    for k in range(n_groups):
+        pos = order[int(offsets[k]):int(offsets[k + 1])].long()
+        a, w = x[pos].double() * xs[pos].double()[:, None], (W[k].double() * ws.view(n_groups, -1)[k].double()[:, None]).T.contiguous()
+        want, size = torch.mm(a, w), torch.mm(a.abs(), w.abs())
+        close(h[pos], want, (d_in + 8) * 2.0 ** -23 * size + HALF[out] * want.abs() + TINY[out], f"{signs} {out}")
