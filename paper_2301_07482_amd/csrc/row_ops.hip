@@ -53,12 +53,13 @@ __device__ __forceinline__ int64_t row_at(const RowList& L, int64_t k, int64_t c
 }
 
 template <int T>
-__global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, const char* x, int64_t x_stride, char* out, int64_t out_stride, int d,
-                                                              int pieces, DropArgs D) {
+__global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, int64_t rows, const char* x, int64_t x_stride, char* out,
+                                                              int64_t out_stride, int d, int pieces, DropArgs D) {
     constexpr int E = T == FG_F32 ? 4 : 2;
     const int64_t count = row_count(L);
     const int64_t at = blockIdx.x * (int64_t)ROW_THREADS + threadIdx.x;
     const int64_t k = at / pieces;
+    if (k >= rows) return;      // the next launch's (x may be out: a row that two launches take is dropped twice)
     const int c = (int)(at - k * pieces) * 8;
     const int64_t r = row_at(L, L.first + k, count);
     if (r < 0) return;
@@ -436,9 +437,9 @@ extern "C" fg_status_t fg_dropout(const void* x, int64_t x_stride, fg_dtype_t dt
     RowList L = {rows_dev, n_rows_dev, max_rows, n, 0};
     const DropArgs D = drop_args(p, key);
     hipStream_t st = (hipStream_t)stream;
-#define FG_DROP(T) hipLaunchKernelGGL((dropout_kernel<T>), dim3((unsigned)blocks), dim3(ROW_THREADS), 0, st, L, (const char*)x, x_stride, (char*)out, out_stride, d, pieces, D)
+#define FG_DROP(T) hipLaunchKernelGGL((dropout_kernel<T>), dim3((unsigned)blocks), dim3(ROW_THREADS), 0, st, L, rows, (const char*)x, x_stride, (char*)out, out_stride, d, pieces, D)
     for (; L.first < max_rows; L.first += at_once) {
-        const int64_t blocks = fg_ceil_div((max_rows - L.first < at_once ? max_rows - L.first : at_once) * pieces, ROW_THREADS);
+        const int64_t rows = max_rows - L.first < at_once ? max_rows - L.first : at_once, blocks = fg_ceil_div(rows * pieces, ROW_THREADS);
         if (dtype == FG_F32)
             FG_DROP(FG_F32);
         else if (dtype == FG_F16)

@@ -43,3 +43,22 @@ def test_8_bit_rows_with_one_large_value_in_eight(B, n, n_groups, d_in, d_out, s
         a, w = x[pos].double() * xs[pos].double()[:, None], (W[k].double() * ws.view(n_groups, -1)[k].double()[:, None]).T.contiguous()
         want, size = torch.mm(a, w), torch.mm(a.abs(), w.abs())
         close(h[pos], want, (d_in + 8) * 2.0 ** -23 * size + HALF[out] * want.abs() + TINY[out], f"{signs} {out}")
+
+
+# ---- dropout ----
+
+@gpu
+def test_dropout_in_place_of_a_list_longer_than_a_launch(B):
+    """Every row is dropped once: the row at the place where a launch ends and the next one begins, too."""
+    n, d, p, key, dtype = 40, 8000, 0.3, 77, "f16"
+    at = ((1 << 24) - 1) * 256 // (d // 8)      # rows of a launch: 2^32 threads less 256, 1000 to a row
+    x = torch.randn(n, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(d)).to(T[dtype])
+    listed = torch.tensor([5, 11, 7], dtype=torch.int32, device="cuda")
+    rows = torch.full((at + 40,), -1, dtype=torch.int32, device="cuda")
+    rows[at - 1], rows[at], rows[at + 1] = 5, 11, 7
+    got = {}
+    for name, list_ in (("short", listed), ("long", rows)):
+        got[name] = x.clone()
+        B.fg_dropout(got[name], stride(x), code(B, dtype), list_, None, len(list_), n, d, p, key, got[name], stride(x))
+    torch.cuda.synchronize()
+    assert torch.equal(got["short"], got["long"]) and not torch.equal(got["short"], x)
