@@ -107,8 +107,8 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 // fg_linear. The values lie in LDS as they are and are split as they are read: the split costs about the vector instructions that the
 // products cost matrix instructions.
 //
-// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 120 us
-// (1.03 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
+// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 122 us
+// (1.01 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
 // 2.0 us for the 1.15 us that its matrix instructions take by themselves and the 0.85 us that LDS is busy with them; tiles of 256 x 256 on four
 // wavefronts, with a third fewer LDS reads, took 1010 us instead of 702 (nothing fills the waits of a lone wavefront), tiles of 128 x 256 two
 // to a compute unit 12 % longer.
@@ -192,6 +192,11 @@ constexpr int EP_BLOCK = 16 * 128;      // bytes of an epilogue's block
 // the operands' two buffers, the epilogue's blocks, what belongs to a tile (twice), the offsets
 constexpr size_t gl_lds_bytes(int bm, int bn, int waves, bool eight, int n_groups) {
     return (size_t)2 * (bm + bn) * GL_STEP + (size_t)waves * EP_BLOCK + (size_t)2 * (8 * bm + 4 * bn + (eight ? 4 * (bm + bn) : 32)) + (size_t)(n_groups + 1) * 4;
+}
+// A sum of 8-bit products times the scales of its row and its column, the smaller one first: the scales' own product may overflow where the sum is zero, or
+// lose its bits below the normal numbers where the sum is large (a scale of rows is 2^-109 and more). An infinity or a NaN in either shows.
+__device__ __forceinline__ float scaled(float v, float a, float b) {
+    return v * __builtin_elementwise_minimum(a, b) * __builtin_elementwise_maximum(a, b);
 }
 // max(v, 0), a NaN stays one
 __device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise_maximum(v, 0.f); }
@@ -489,8 +494,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
                         const int cl = wn + nb * 32 + 8 * q + 4 * half;
                         const float4 b = *(const float4*)(D.bias + cl), ws = *(const float4*)(D.w_scale + cl);
                         gl_f32x16& v = acc[mb][nb];
-                        v[4 * q] = v[4 * q] * (xs * ws.x) + b.x, v[4 * q + 1] = v[4 * q + 1] * (xs * ws.y) + b.y;
-                        v[4 * q + 2] = v[4 * q + 2] * (xs * ws.z) + b.z, v[4 * q + 3] = v[4 * q + 3] * (xs * ws.w) + b.w;
+                        v[4 * q] = scaled(v[4 * q], xs, ws.x) + b.x, v[4 * q + 1] = scaled(v[4 * q + 1], xs, ws.y) + b.y;
+                        v[4 * q + 2] = scaled(v[4 * q + 2], xs, ws.z) + b.z, v[4 * q + 3] = scaled(v[4 * q + 3], xs, ws.w) + b.w;
                     }
                     if (A.relu)
 #pragma unroll

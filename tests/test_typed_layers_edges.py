@@ -45,6 +45,32 @@ def test_8_bit_rows_with_one_large_value_in_eight(B, n, n_groups, d_in, d_out, s
         close(h[pos], want, (d_in + 8) * 2.0 ** -23 * size + HALF[out] * want.abs() + TINY[out], f"{signs} {out}")
 
 
+@gpu
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("x_scale, w_scale", [(1.37 * 2.0 ** 100, 1.61 * 2.0 ** 40), (1.37 * 2.0 ** 40, 1.61 * 2.0 ** 100), (1.37 * 2.0 ** -100, 1.61 * 2.0 ** -45),
+                                              (1.37 * 2.0 ** -45, 1.61 * 2.0 ** -100), (1.37 * 2.0 ** 110, 1.61 * 2.0 ** -30), (1.37 * 2.0 ** -30, 1.61 * 2.0 ** 110)])
+def test_8_bit_rows_with_scales_far_from_one(B, x_scale, w_scale, out):
+    """The product of the two scales may leave fp32 where the result does not: sums of zeros, and sums that are far from one the other way."""
+    n, a, b = 70, 64, 24
+    g = torch.Generator().manual_seed(7)
+    x = torch.randint(1, 8, (n, a), generator=g).float() * 64
+    x[:35] = 0
+    w = torch.randint(1, 8, (b, a), generator=g).float() * 64
+    if x_scale * w_scale > 2.0 ** 127:
+        x[35:] = 0
+    bias = torch.randn(1, b, generator=g)
+    if x_scale * w_scale < 1:
+        bias.zero_()
+    xs, ws = torch.full((n,), x_scale), torch.full((b,), w_scale)
+    h = torch.full((n, b), -77.0, dtype=T[out], device="cuda")
+    B.fg_linear_grouped(e4m3(x).cuda(), n, a, B.FG_E4M3, xs.cuda(), None, None, torch.tensor([0, n], device="cuda"), n, 1, a, b, e4m3(w).cuda(), ws.cuda(), bias.cuda(), 0, h, n,
+                        stride(h), code(B, out))
+    torch.cuda.synchronize()
+    want = (x.double() @ w.double().T) * float(xs[0]) * float(ws[0]) + bias.double()      # (whole numbers below 2^24: the sum is exact)
+    # four roundings: the two scales' products, the bias, the type
+    close(h.cpu(), want, 2.0 ** -22 * (want.abs() + bias.double().abs()) + HALF[out] * want.abs(), f"{x_scale:g} {w_scale:g} {out}")
+
+
 # ---- dropout ----
 
 @gpu
