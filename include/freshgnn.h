@@ -848,7 +848,7 @@ fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, f
  *   x, W, dtype, src_ids, order, offsets   as in the forward call (not FG_E4M3); x, dW, db and dx, W may be NULL where the result is not wanted
  *   dh, dh_stride, dh_dtype             dL/dh by position, n rows of d_out values, FG_F32 or `dtype`; fp32 gradients of 16-bit rows are
  *                                       rounded to `dtype` after the mask, as in fg_layer_backward_bf16 (db sums the unrounded ones)
- *   h, h_stride                         rows of `dtype` by position
+ *   h, h_stride, h_dtype                rows by position, of the type they were written in (the forward call's out_dtype)
  *   dx, dx_stride, dx_dtype             FG_F32 or `dtype`
  *   ws_dev, ws_bytes                    >= fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned
  * An entry that the forward call skips has no part in any of the sums and gets no dx. dW: the rows are cut into equal ranges, as many as
@@ -857,8 +857,8 @@ fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, f
  */
 size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out);
 fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev, const void* dh,
-                                       int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, int64_t n, const int32_t* order_dev,
-                                       const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out, const void* W,
+                                       int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, fg_dtype_t h_dtype, int64_t n,
+                                       const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out, const void* W,
                                        void* dx, int64_t dx_stride, fg_dtype_t dx_dtype, float* dw_dev, float* db_dev, void* ws_dev,
                                        size_t ws_bytes, void* stream);
 

@@ -15,6 +15,7 @@ FG_F32, FG_F16, FG_BF16, FG_E4M3 = 0, 1, 2, 3
 FG_WS_LOOKUP_PRUNE, FG_WS_CACHE_UPDATE, FG_WS_EXPORT = 0, 1, 2
 FG_TABLE_HBM_STREAMED, FG_TABLE_HOST_MAPPED, FG_TABLE_HBM_REUSED = 0, 1, 2
 DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2, FG_E4M3: 1}
+_TENSOR_DTYPE = {"torch.float32": FG_F32, "torch.float16": FG_F16, "torch.bfloat16": FG_BF16}
 FG_MAX_GROUPS, FG_MAX_GROUPED_ROWS, FG_MAX_NORM_DIM = 1024, 1 << 29, 16384
 
 if not os.path.exists(LIB_PATH):
@@ -89,8 +90,8 @@ SIGNATURES = {
     "fg_group_rows": (_i32, [_p, _i64, _p, _i64, _p, _p, _i64, _i32, _p, _p, _p, _sz, _p]),
     "fg_linear_grouped": (_i32, [_p, _i64, _i64, _i32, _p, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _p, _i32, _p, _i64, _i64, _i32, _p]),
     "fg_linear_grouped_backward_workspace_bytes": (_sz, [_i32, _i64, _i32, _i32, _i32]),
-    "fg_linear_grouped_backward": (_i32, [_p, _i64, _i64, _i32, _p, _p, _i64, _i32, _p, _i64, _i64, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _i64,
-                                          _i32, _p, _p, _p, _sz, _p]),
+    "fg_linear_grouped_backward": (_i32, [_p, _i64, _i64, _i32, _p, _p, _i64, _i32, _p, _i64, _i32, _i64, _p, _p, _i64, _i32, _i32, _i32, _p, _p,
+                                          _i64, _i32, _p, _p, _p, _sz, _p]),
     "fg_dropout": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _i64, _p]),
     "fg_residual_norm": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _f, _p, _i64, _p, _i64, _i32, _p, _p,
                                 _p]),
@@ -527,9 +528,12 @@ def fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, 
 
 
 def fg_linear_grouped_backward(x, x_rows, x_stride, dtype, src_ids, dh, dh_stride, dh_dtype, h, h_stride, n, order, offsets, max_rows, n_groups,
-                               d_in, d_out, W, dx, dx_stride, dx_dtype, dw, db, ws, ws_bytes, stream=None):
-    _check(_lib.fg_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(h), h_stride, n,
-                                           ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), ptr(dx), dx_stride, dx_dtype, ptr(dw),
+                               d_in, d_out, W, dx, dx_stride, dx_dtype, dw, db, ws, ws_bytes, stream=None, h_dtype=None):
+    """h_dtype None: the type of the tensor h, of an address that of the rows."""
+    if h_dtype is None:
+        h_dtype = _TENSOR_DTYPE.get(str(getattr(h, "dtype", "")), dtype)
+    _check(_lib.fg_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(h), h_stride,
+                                           h_dtype, n, ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), ptr(dx), dx_stride, dx_dtype, ptr(dw),
                                            ptr(db), ptr(ws), ws_bytes, stream))
 
 

@@ -46,7 +46,7 @@ extern "C" fg_status_t fg_set_tuning(const char* key, int64_t value) {
 
 extern "C" const char* fg_last_error(void) { return g_err; }
 
-extern "C" int32_t fg_version(void) { return 400; }  // 0.4.0: typed layers (fg_group_rows, fg_linear_grouped*, fg_residual_norm*, fg_dropout, fg_quantize_rows, FG_E4M3); 0.3.1: fg_linear_ids; 0.3.0: device-side layer sizes (two structs grew a field), backward for GCN and mixed precision, fg_linear_wt, fg_lookup_prune_static
+extern "C" int32_t fg_version(void) { return 401; }  // 0.4.1: fg_linear_grouped_backward has an argument for the type of h; 0.4.0: typed layers (fg_group_rows, fg_linear_grouped*, fg_residual_norm*, fg_dropout, fg_quantize_rows, FG_E4M3); 0.3.1: fg_linear_ids; 0.3.0: device-side layer sizes (two structs grew a field), backward for GCN and mixed precision, fg_linear_wt, fg_lookup_prune_static
 
 extern "C" size_t fg_workspace_bytes(fg_ws_kind_t kind, int64_t n, int64_t reserved) {
     (void)reserved;

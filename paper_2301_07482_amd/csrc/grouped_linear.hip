@@ -57,7 +57,7 @@ struct GlArgs {
     Groups G;
     const char *x, *W, *h, *dh;
     int64_t x_rows, x_stride, h_stride, dh_stride, n, out_stride;
-    int type, dh_type, out_type, d_in, d_out, relu, tiles_n;
+    int type, dh_type, h_type, out_type, d_in, d_out, relu, tiles_n;
     const float *x_scale, *w_scale, *bias;
     const int32_t* src_ids;
     char* out;
@@ -639,9 +639,10 @@ __device__ __forceinline__ int64_t steps_before(const Groups& G, int upto, int r
 // columns in one workgroup, row after row).
 constexpr int GZ_ROWS = 64, GZ_THREADS = 256, GZ_COLUMNS = 256;
 
-template <int T, int D>
+// T: the rows' type, D: that of dh, H: that of h
+template <int T, int D, int H>
 __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
-    constexpr int E = T == FG_F32 ? 4 : 2, DE = D == FG_F32 ? 4 : 2;
+    constexpr int E = T == FG_F32 ? 4 : 2, DE = D == FG_F32 ? 4 : 2, HE = H == FG_F32 ? 4 : 2;
     __shared__ int32_t pos[GZ_ROWS];
     __shared__ float sums[GZ_THREADS * 8];
     int g;
@@ -664,14 +665,14 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
         constexpr int AHEAD = 4;      // rows whose reads are on their way together
         for (int m0 = t / width; m0 < rows; m0 += AHEAD * side) {
             fg_piece<D> pz[AHEAD];
-            fg_piece<T> ph[AHEAD];
+            fg_piece<H> ph[AHEAD];
             int32_t r[AHEAD];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
                 const int m = m0 + u * side;
                 r[u] = m < rows ? pos[m] : -1;
                 if (r[u] >= 0) pz[u] = fg_load_piece<D>(A.dh + r[u] * A.dh_stride + (int64_t)c * DE, left);
-                if (r[u] >= 0 && A.h) ph[u] = fg_load_piece<T>(A.h + r[u] * A.h_stride + (int64_t)c * E, left);
+                if (r[u] >= 0 && A.h) ph[u] = fg_load_piece<H>(A.h + r[u] * A.h_stride + (int64_t)c * HE, left);
             }
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
@@ -680,7 +681,7 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
                 if (r[u] >= 0) fg_piece_values<D>(pz[u], z);
                 if (r[u] >= 0 && A.h) {
                     float h[8];
-                    fg_piece_values<T>(ph[u], h);
+                    fg_piece_values<H>(ph[u], h);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) z[e] = h[e] > 0.f ? z[e] : 0.f;
                 }
@@ -1185,6 +1186,10 @@ fg_status_t check_matrix(const char* who, const char* what, const void* p, int64
 // tiles of rows at most: every group may end in one that is partly filled
 int64_t row_tiles(int64_t max_rows, int n_groups, int size) { return max_rows / size + (n_groups < max_rows ? n_groups : max_rows); }
 
+template <int T, int D, int H>
+void launch_dz(const GlArgs& A, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((grouped_dz_kernel<T, D, H>), grid, dim3(GZ_THREADS), 0, st, A);
+}
 template <int BM, int ROWS, int VALUES>
 void launch_sum(const GlArgs& A, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((grouped_dw_sum_kernel<BM, BM, ROWS, VALUES>), grid, dim3(GZ_THREADS), 0, st, A);
@@ -1202,10 +1207,12 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     A.db_tiles = work ? row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS) : 0;
     if (A.dz || A.db_part) {
         const dim3 grid((unsigned)A.db_tiles, (unsigned)fg_ceil_div(A.d_out, GZ_COLUMNS));
-        if (A.dh_type == T)
-            hipLaunchKernelGGL((grouped_dz_kernel<T, T>), grid, dim3(GZ_THREADS), 0, st, A);
+        if constexpr (T == FG_F32)
+            launch_dz<T, T, T>(A, grid, st);
+        else if (A.dh_type == T)
+            A.h_type == FG_F32 ? launch_dz<T, T, FG_F32>(A, grid, st) : A.h_type == FG_F16 ? launch_dz<T, T, FG_F16>(A, grid, st) : launch_dz<T, T, FG_BF16>(A, grid, st);
         else
-            hipLaunchKernelGGL((grouped_dz_kernel<T, FG_F32>), grid, dim3(GZ_THREADS), 0, st, A);
+            A.h_type == FG_F32 ? launch_dz<T, FG_F32, FG_F32>(A, grid, st) : A.h_type == FG_F16 ? launch_dz<T, FG_F32, FG_F16>(A, grid, st) : launch_dz<T, FG_F32, FG_BF16>(A, grid, st);
         FG_LAUNCH_CHECK("grouped_dz_kernel");
     }
     if (A.out && work) {
@@ -1272,8 +1279,8 @@ extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, i
 }
 
 extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
-                                                  const void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, int64_t n,
-                                                  const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups,
+                                                  const void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, fg_dtype_t h_dtype,
+                                                  int64_t n,                                                   const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups,
                                                   int32_t d_in, int32_t d_out, const void* W, void* dx, int64_t dx_stride, fg_dtype_t dx_dtype,
                                                   float* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes, void* stream) {
     const char* who = "fg_linear_grouped_backward";
@@ -1281,12 +1288,13 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     FG_TRY(check_groups(who, order_dev, offsets_dev, max_rows, n_groups, d_in, d_out, dtype, x_rows, n));
     const int e = fg_dtype_size(dtype);
     if (dh_dtype != dtype && dh_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dh is of the type of x or fp32", who);
+    if (h && (!fg_dtype_size(h_dtype) || (dtype == FG_F32 && h_dtype != FG_F32))) FG_FAIL(FG_ERR_DTYPE, "%s: h is of a type that the layer's output can have", who);
     if (dx && dx_dtype != dtype && dx_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dx is of the type of x or fp32", who);
     if (!dx && !dw_dev && !db_dev) FG_FAIL(FG_ERR_INVALID_ARG, "%s: none of dx, dw and db is wanted", who);
     const bool work = max_rows > 0 && n > 0 && x_rows > 0;
     if (work) {
         FG_TRY(check_matrix(who, "dh", dh, dh_stride, (int64_t)d_out * fg_dtype_size(dh_dtype)));
-        if (h) FG_TRY(check_matrix(who, "h", h, h_stride, (int64_t)d_out * e));
+        if (h) FG_TRY(check_matrix(who, "h", h, h_stride, (int64_t)d_out * fg_dtype_size(h_dtype)));
         if (dw_dev) FG_TRY(check_matrix(who, "x", x, x_stride, (int64_t)d_in * e));
         if (dx) FG_TRY(check_matrix(who, "dx", dx, dx_stride, (int64_t)d_in * fg_dtype_size(dx_dtype)));
         if (dx) FG_TRY(check_matrix(who, "W", W, 0, 0));
@@ -1299,7 +1307,7 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     GlArgs A = {};
     A.G = {order_dev, offsets_dev, work ? max_rows : 0, n_groups};
     A.x = (const char*)x, A.W = (const char*)W, A.h = (const char*)h, A.dh = (const char*)dh, A.x_rows = x_rows, A.x_stride = x_stride, A.h_stride = h_stride;
-    A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.type = dtype, A.dh_type = dh_dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
+    A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.type = dtype, A.dh_type = dh_dtype, A.h_type = h ? h_dtype : dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
     A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = dw_dev, A.db = db_dev;
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32) return backward<FG_F32>(who, A, work, st, ws_dev);

@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_typed_layers import HALF, T, TINY, B, close, code, cuda, gpu, refused, stride  # noqa: F401 (B: the fixture)
+from tests import typed_reference as R
+from tests.test_typed_layers import HALF, T, TINY, B, close, code, cuda, gpu, layout, matrix, refused, stride  # noqa: F401 (B: the fixture)
 
 
 def e4m3(v):
@@ -88,3 +89,46 @@ def test_dropout_in_place_of_a_list_longer_than_a_launch(B):
         B.fg_dropout(got[name], stride(x), code(B, dtype), list_, None, len(list_), n, d, p, key, got[name], stride(x))
     torch.cuda.synchronize()
     assert torch.equal(got["short"], got["long"]) and not torch.equal(got["short"], x)
+
+
+# ---- gradients ----
+
+def test_refusals_of_the_output_s_type(B):
+    P = 4096
+    bw = lambda **k: B.fg_linear_grouped_backward(**{**dict(x=P, x_rows=10, x_stride=256, dtype=B.FG_BF16, src_ids=None, dh=P, dh_stride=256, dh_dtype=B.FG_BF16,
+                                                            h=P, h_stride=128, n=10, order=P, offsets=P, max_rows=10, n_groups=4, d_in=64, d_out=64, W=P,
+                                                            dx=P, dx_stride=256, dx_dtype=B.FG_F32, dw=P, db=P, ws=P, ws_bytes=1 << 40, h_dtype=B.FG_BF16), **k})
+    for bad, want in ((dict(h_dtype=B.FG_E4M3), 3), (dict(h_dtype=7), 3), (dict(h_dtype=B.FG_F32), 2), (dict(dtype=B.FG_F32, dh_dtype=B.FG_F32), 3),
+                      (dict(h_dtype=B.FG_F16, h_stride=112), 2)):
+        assert refused(B, bw, **bad) == want, bad
+
+
+@gpu
+@pytest.mark.parametrize("dtype, out, dh_type", [("bf16", "f32", "bf16"), ("bf16", "f32", "f32"), ("bf16", "f16", "bf16"), ("bf16", "f16", "f32"), ("f16", "f32", "f16"),
+                                                 ("f16", "f32", "f32"), ("f16", "bf16", "f16"), ("f16", "bf16", "f32"), ("bf16", "bf16", "f32"), ("f32", "f32", "f32")])
+@pytest.mark.parametrize("named", [True, False])
+def test_gradients_of_a_relu_layer_by_the_type_of_its_output(B, dtype, out, dh_type, named):
+    """The mask is h > 0 of the rows as the forward call wrote them, in each type that it writes; what has no sign to speak of among them too."""
+    n, G, a, b = 400, 3, 64, 72
+    r = np.random.default_rng(17)
+    order, offsets = layout(r, n, G, 0.9)
+    x, W, dh = matrix(r, n, a, dtype), torch.from_numpy(r.standard_normal((G, a, b)) / 8).to(T[dtype]), matrix(r, n, b, dh_type)
+    bias = torch.from_numpy(r.standard_normal((G, b))).float().cuda()
+    od, fd, xd, Wd = torch.from_numpy(order).cuda(), torch.from_numpy(offsets).cuda(), x.cuda(), W.cuda()
+    h = torch.full((n, b + 8), -77.0, dtype=T[out], device="cuda")
+    B.fg_linear_grouped(xd, n, stride(xd), code(B, dtype), None, None, od, fd, len(order), G, a, b, Wd, None, bias, 1, h, n, stride(h), code(B, out))
+    low = torch.finfo(T[out]).smallest_normal
+    h[:5, :6] = torch.tensor([0.0, -0.0, float("nan"), low, -low, low / 8], device="cuda").to(T[out])
+    h[5:9, :2] = torch.tensor([float("inf"), -float("inf")], device="cuda").to(T[out])
+    rounds = T[dtype] if dtype != "f32" and dh_type == "f32" else None
+    (dx, dxs), (dW, dWs), (db, dbs) = R.grouped_linear_backward(x, W, dh, h.cpu()[:, :b], order.tolist(), offsets.tolist(), None, rounds)
+    gx, gw, gb = torch.full((n, a), -77.0, device="cuda"), torch.full((G, a, b), -77.0, device="cuda"), torch.full((G, b), -77.0, device="cuda")
+    ws = torch.zeros(B.fg_linear_grouped_backward_workspace_bytes(code(B, dtype), len(order), G, a, b), dtype=torch.uint8, device="cuda")
+    dhd = dh.cuda()
+    B.fg_linear_grouped_backward(xd, n, stride(xd), code(B, dtype), None, dhd, stride(dhd), code(B, dh_type), h, stride(h), n, od, fd, len(order), G, a, b, Wd, gx, 4 * a,
+                                 B.FG_F32, gw, gb, ws, ws.numel(), **(dict(h_dtype=code(B, out)) if named else {}))
+    torch.cuda.synchronize()
+    pos = order.astype(np.int64)
+    close(gx.cpu()[pos], dx, (b + 8) * 2.0 ** -23 * dxs + HALF["f32"] * dx.abs(), "dx")
+    close(gw.cpu(), dW, (len(order) + 16) * 2.0 ** -23 * dWs, "dW")
+    close(gb.cpu(), db, (len(order) + 16) * 2.0 ** -23 * dbs, "db")
