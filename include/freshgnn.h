@@ -853,7 +853,8 @@ fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, f
  *   ws_dev, ws_bytes                    >= fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned
  * An entry that the forward call skips has no part in any of the sums and gets no dx. dW: the rows are cut into equal ranges, as many as
  * keep the chip busy (512 over the result's number of tiles of 128 x 128, 256 over that of 256 x 256 where those are used; one or two from there
- * on), fp32 sums within a range, fp64 across ranges; db the same with 64 rows. No atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out * sizeof(dtype) a multiple of 16.
+ * on), fp32 sums within a range, fp64 across ranges; db the same with 64 rows. No atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out * sizeof(dtype) a multiple of 16. A dW of about
+ * 2^36 values, with d_in and d_out rounded up to 256, and more is refused.
  */
 size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out);
 fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev, const void* dh,

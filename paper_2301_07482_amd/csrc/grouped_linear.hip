@@ -588,11 +588,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 }
 
 template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN>
-fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
+fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
     A.tiles_n = (int)fg_ceil_div(A.N, BN);
     const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
-    if (tiles > INT32_MAX) FG_FAIL(FG_ERR_SHAPE, "%s: too many rows and columns for one call", who);
+    // (a workgroup's number of a tile is one of its XCD's, and a step beyond: (2^23 + 2^10) rows of tiles x 2^10 / 8 fit 31 bits)
+    static_assert((FG_MAX_GROUPED_ROWS / 64 + FG_MAX_GROUPS + 8) * (int64_t)(65536 / 64) / 8 + 256 * 4 < INT32_MAX, "tiles of an XCD fit an int");
     const int64_t at_once = 256 * PER_CU;
     hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
                        gl_lds_bytes(BM, BN, WM * WN, T == FG_E4M3, A.G.n_groups), st, A);
@@ -609,13 +610,13 @@ fg_status_t tile_launch(const char* who, GlArgs& A, hipStream_t st) {
 //                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 62 | 65; 64 rows a group 43 | 53, 134 | 115, 72 | 49
 // No 256 x 256 tile for fp32, whose two sums do not fit the registers.
 template <int T, bool B_KN>
-fg_status_t tile_product(const char* who, GlArgs& A, hipStream_t st) {
+fg_status_t tile_product(GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
     if constexpr (T != FG_F32)
-        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN>(who, A, st);
+        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN>(A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN>(who, A, st);
-    return tile_launch<T, 64, 64, 2, 2, 4, B_KN>(who, A, st);
+    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN>(A, st);
+    return tile_launch<T, 64, 64, 2, 2, 4, B_KN>(A, st);
 }
 
 // ---- gradients ----
@@ -1205,6 +1206,12 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
     A.dw_part = (float*)(ws + P.dz_bytes + P.db_bytes);
     A.db_tiles = work ? row_tiles(A.G.max_rows, A.G.n_groups, GZ_ROWS) : 0;
+    // the launch of the sums: what it cannot hold is refused before anything is launched
+    const int64_t results = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm);
+    const bool many = results / DS_MANY >= 512;
+    const int64_t sums = A.dw ? results / (many ? DS_MANY : DS_FEW) : 0;
+    const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
+    if (sums + db_blocks >= FG_MAX_GRID) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
     if (A.dz || A.db_part) {
         const dim3 grid((unsigned)A.db_tiles, (unsigned)fg_ceil_div(A.d_out, GZ_COLUMNS));
         if constexpr (T == FG_F32)
@@ -1217,15 +1224,10 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     }
     if (A.out && work) {
         A.a = A.dz ? A.dz : A.dh, A.a_stride = A.dz_stride, A.a_by = A.dz ? GL_A_ENTRY : GL_A_POSITION, A.K = A.d_out, A.N = A.d_in;
-        FG_TRY((tile_product<T, false>(who, A, st)));
+        FG_TRY((tile_product<T, false>(A, st)));
     }
     if (!A.dw && !A.db) return FG_OK;
     A.ranges = P.ranges;
-    const int64_t results = fg_ceil_div(A.d_in, P.bm) * fg_ceil_div(A.d_out, P.bm) * A.G.n_groups * (P.bm * P.bm);
-    const bool many = results / DS_MANY >= 512;
-    const int64_t sums = A.dw ? results / (many ? DS_MANY : DS_FEW) : 0;
-    const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
-    if (sums + db_blocks >= FG_MAX_GRID) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
     A.sums = (int)sums;
     const dim3 grid((unsigned)P.grid), sum_grid((unsigned)(sums + db_blocks));
     if constexpr (T == FG_F32) {
@@ -1267,10 +1269,10 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu;
     A.x_scale = x_scale, A.w_scale = w_scale, A.bias = bias, A.src_ids = src_ids_dev, A.out = (char*)h_out;
     A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
-    if (dtype == FG_BF16) return tile_product<FG_BF16, true>(who, A, (hipStream_t)stream);
-    if (dtype == FG_F16) return tile_product<FG_F16, true>(who, A, (hipStream_t)stream);
-    if (dtype == FG_E4M3) return tile_product<FG_E4M3, false>(who, A, (hipStream_t)stream);
-    return tile_product<FG_F32, true>(who, A, (hipStream_t)stream);
+    if (dtype == FG_BF16) return tile_product<FG_BF16, true>(A, (hipStream_t)stream);
+    if (dtype == FG_F16) return tile_product<FG_F16, true>(A, (hipStream_t)stream);
+    if (dtype == FG_E4M3) return tile_product<FG_E4M3, false>(A, (hipStream_t)stream);
+    return tile_product<FG_F32, true>(A, (hipStream_t)stream);
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {

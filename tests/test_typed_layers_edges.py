@@ -93,6 +93,15 @@ def test_dropout_in_place_of_a_list_longer_than_a_launch(B):
 
 # ---- gradients ----
 
+def test_a_call_is_refused_before_anything_is_launched(B):
+    """Weight gradients that one launch cannot sum; without a GPU a launch would end the call with another error."""
+    P = 4096
+    for dtype in (B.FG_F32, B.FG_BF16):
+        for n in (10, 0):
+            assert refused(B, B.fg_linear_grouped_backward, P, n, 1 << 20, dtype, None, P, 1 << 20, dtype, P, 1 << 20, n, P, P, 1000, 1024, 65536, 65536, P, P, 1 << 20, dtype, P, P, P,
+                           1 << 62) == B.FG_ERR_SHAPE
+
+
 def test_refusals_of_the_output_s_type(B):
     P = 4096
     bw = lambda **k: B.fg_linear_grouped_backward(**{**dict(x=P, x_rows=10, x_stride=256, dtype=B.FG_BF16, src_ids=None, dh=P, dh_stride=256, dh_dtype=B.FG_BF16,
