@@ -16,7 +16,7 @@ FG_WS_LOOKUP_PRUNE, FG_WS_CACHE_UPDATE, FG_WS_EXPORT = 0, 1, 2
 FG_TABLE_HBM_STREAMED, FG_TABLE_HOST_MAPPED, FG_TABLE_HBM_REUSED = 0, 1, 2
 DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2, FG_E4M3: 1}
 _TENSOR_DTYPE = {"torch.float32": FG_F32, "torch.float16": FG_F16, "torch.bfloat16": FG_BF16}
-FG_MAX_GROUPS, FG_MAX_GROUPED_ROWS, FG_MAX_NORM_DIM = 1024, 1 << 29, 16384
+FG_MAX_GROUPS, FG_MAX_GROUPED_ROWS, FG_MAX_GROUPED_DIM, FG_MAX_NORM_DIM = 1024, 1 << 29, 65536, 16384
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2301_07482_amd.build` (needs hipcc); "

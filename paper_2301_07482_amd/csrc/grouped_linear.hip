@@ -57,7 +57,7 @@ struct GlArgs {
     Groups G;
     const char *x, *W, *h, *dh;
     int64_t x_rows, x_stride, h_stride, dh_stride, n, out_stride;
-    int type, dh_type, h_type, out_type, d_in, d_out, relu, tiles_n;
+    int dh_type, h_type, out_type, d_in, d_out, relu, tiles_n;
     const float *x_scale, *w_scale, *bias;
     const int32_t* src_ids;
     char* out;
@@ -593,7 +593,7 @@ fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
     const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
     // (a workgroup's number of a tile is one of its XCD's, and a step beyond: (2^23 + 2^10) rows of tiles x 2^10 / 8 fit 31 bits)
-    static_assert((FG_MAX_GROUPED_ROWS / 64 + FG_MAX_GROUPS + 8) * (int64_t)(65536 / 64) / 8 + 256 * 4 < INT32_MAX, "tiles of an XCD fit an int");
+    static_assert((FG_MAX_GROUPED_ROWS / 64 + FG_MAX_GROUPS + 8) * (int64_t)(FG_MAX_GROUPED_DIM / 64) / 8 + 256 * 4 < INT32_MAX, "tiles of an XCD fit an int");
     const int64_t at_once = 256 * PER_CU;
     hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
                        gl_lds_bytes(BM, BN, WM * WN, T == FG_E4M3, A.G.n_groups), st, A);
@@ -1166,8 +1166,8 @@ fg_status_t check_groups(const char* who, const int32_t* order_dev, const int64_
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
     if (n_groups < 1 || n_groups > FG_MAX_GROUPS) FG_FAIL(FG_ERR_INVALID_ARG, "%s: n_groups = %d is not in 1..%d", who, n_groups, FG_MAX_GROUPS);
     const int step_in = 16 / e, step_out = dtype == FG_F32 ? 4 : 8;
-    if (d_in <= 0 || d_in % step_in || d_out <= 0 || d_out % step_out || d_in > 65536 || d_out > 65536)
-        FG_FAIL(FG_ERR_SHAPE, "%s: d_in = %d must be a multiple of %d and d_out = %d of %d for this type, 65536 at most", who, d_in, step_in, d_out, step_out);
+    if (d_in <= 0 || d_in % step_in || d_out <= 0 || d_out % step_out || d_in > FG_MAX_GROUPED_DIM || d_out > FG_MAX_GROUPED_DIM)
+        FG_FAIL(FG_ERR_SHAPE, "%s: d_in = %d must be a multiple of %d and d_out = %d of %d for this type, %d at most", who, d_in, step_in, d_out, step_out, FG_MAX_GROUPED_DIM);
     if (!offsets_dev || ((uintptr_t)offsets_dev & 7) || ((uintptr_t)order_dev & 3))
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: offsets must not be NULL, and order and offsets aligned to their elements", who);
     return FG_OK;
@@ -1266,7 +1266,7 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
     GlArgs A = {};
     A.G = {order_dev, offsets_dev, max_rows, n_groups};
     A.x = (const char*)x, A.W = (const char*)W, A.x_rows = x_rows, A.x_stride = x_stride, A.n = n_out, A.out_stride = out_stride;
-    A.type = dtype, A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu;
+    A.out_type = out_dtype, A.d_in = d_in, A.d_out = d_out, A.relu = relu;
     A.x_scale = x_scale, A.w_scale = w_scale, A.bias = bias, A.src_ids = src_ids_dev, A.out = (char*)h_out;
     A.a = (const char*)x, A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.K = d_in, A.N = d_out;
     if (dtype == FG_BF16) return tile_product<FG_BF16, true>(A, (hipStream_t)stream);
@@ -1276,7 +1276,9 @@ extern "C" fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t 
 }
 
 extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
-    if (!fg_dtype_size(dtype) || max_rows < 0 || max_rows > FG_MAX_GROUPED_ROWS || n_groups < 1 || n_groups > FG_MAX_GROUPS || d_in <= 0 || d_out <= 0) return 0;
+    if (!fg_dtype_size(dtype) || max_rows < 0 || max_rows > FG_MAX_GROUPED_ROWS || n_groups < 1 || n_groups > FG_MAX_GROUPS || d_in <= 0 || d_in > FG_MAX_GROUPED_DIM ||
+        d_out <= 0 || d_out > FG_MAX_GROUPED_DIM)
+        return 0;
     return bw_plan(max_rows, n_groups, d_in, d_out, fg_dtype_size(dtype)).total();
 }
 
@@ -1309,7 +1311,7 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     GlArgs A = {};
     A.G = {order_dev, offsets_dev, work ? max_rows : 0, n_groups};
     A.x = (const char*)x, A.W = (const char*)W, A.h = (const char*)h, A.dh = (const char*)dh, A.x_rows = x_rows, A.x_stride = x_stride, A.h_stride = h_stride;
-    A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.type = dtype, A.dh_type = dh_dtype, A.h_type = h ? h_dtype : dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
+    A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.dh_type = dh_dtype, A.h_type = h ? h_dtype : dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
     A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = dw_dev, A.db = db_dev;
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32) return backward<FG_F32>(who, A, work, st, ws_dev);

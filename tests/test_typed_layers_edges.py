@@ -15,6 +15,23 @@ def e4m3(v):
     return q
 
 
+# ---- limits ----
+
+def test_widths_beyond_the_limit_are_refused(B):
+    """As the header names it; the workspace query knows the same limit."""
+    P, stride_ = 4096, 1 << 20
+    most = B.FG_MAX_GROUPED_DIM
+    for dtype in (B.FG_F32, B.FG_F16, B.FG_BF16, B.FG_E4M3):
+        scale = P if dtype == B.FG_E4M3 else None
+        for a, b in ((most + 16, 64), (64, most + 16)):
+            assert refused(B, B.fg_linear_grouped, P, 10, stride_, dtype, scale, None, P, P, 10, 4, a, b, P, scale, None, 0, P, 10, stride_, B.FG_F32) == B.FG_ERR_SHAPE
+            if dtype != B.FG_E4M3:
+                assert refused(B, B.fg_linear_grouped_backward, P, 10, stride_, dtype, None, P, stride_, dtype, None, 0, 10, P, P, 10, 4, a, b, P, P, stride_, dtype, P, P, P,
+                               1 << 62) == B.FG_ERR_SHAPE
+                assert B.fg_linear_grouped_backward_workspace_bytes(dtype, 10, 4, a, b) == 0
+                assert B.fg_linear_grouped_backward_workspace_bytes(dtype, 10, 4, min(a, most), min(b, most)) > 0
+
+
 # ---- 8-bit rows ----
 
 @gpu
@@ -141,3 +158,44 @@ def test_gradients_of_a_relu_layer_by_the_type_of_its_output(B, dtype, out, dh_t
     close(gx.cpu()[pos], dx, (b + 8) * 2.0 ** -23 * dxs + HALF["f32"] * dx.abs(), "dx")
     close(gw.cpu(), dW, (len(order) + 16) * 2.0 ** -23 * dWs, "dW")
     close(gb.cpu(), db, (len(order) + 16) * 2.0 ** -23 * dbs, "db")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "e4m3"])
+@pytest.mark.parametrize("a, b", [(65536, 24), (32, 65536)])
+def test_the_widest_rows(B, dtype, a, b):
+    n, G = 70, 2
+    g = torch.Generator(device="cuda").manual_seed(a)
+    kw = dict(device="cuda", generator=g)
+    offsets, order = torch.tensor([0, 30, n - 5], device="cuda"), torch.randperm(n, **kw).int()
+    x, W = torch.randn(n, a, **kw), torch.randn(G, a, b, **kw) / 8
+    out = "f32"
+    xs = ws = None
+    if dtype == "e4m3":
+        (xq, xs), (wq, ws) = R.quantise(x), R.quantise(W.transpose(1, 2).contiguous().reshape(G * b, a))
+        x64, W64 = xq.double() * xs.double()[:, None], (wq.double() * ws.double()[:, None]).reshape(G, b, a).transpose(1, 2).contiguous()
+        x, W = e4m3(xq), e4m3(wq)
+    else:
+        x, W = x.to(T[dtype]), W.to(T[dtype])
+        x64, W64 = x.double(), W.double()
+    h = torch.full((n, b), -77.0, device="cuda")
+    B.fg_linear_grouped(x, n, stride(x), code(B, dtype), xs, None, order, offsets, n, G, a, b, W, ws, None, 0, h, n, 4 * b, B.FG_F32)
+    if dtype != "e4m3":
+        dh = torch.randn(n, b, **kw).to(T[dtype])
+        dx, dw, db = torch.full((n, a), -77.0, device="cuda"), torch.full((G, a, b), -77.0, device="cuda"), torch.full((G, b), -77.0, device="cuda")
+        space = torch.zeros(B.fg_linear_grouped_backward_workspace_bytes(code(B, dtype), n, G, a, b), dtype=torch.uint8, device="cuda")
+        B.fg_linear_grouped_backward(x, n, stride(x), code(B, dtype), None, dh, stride(dh), code(B, dtype), h, 4 * b, n, order, offsets, n, G, a, b, W, dx, 4 * a, B.FG_F32, dw, db,
+                                     space, space.numel())
+    torch.cuda.synchronize()
+    for k in range(G):
+        pos = order[int(offsets[k]):int(offsets[k + 1])].long()
+        want, size = torch.mm(x64[pos], W64[k]), torch.mm(x64[pos].abs(), W64[k].abs())
+        close(h[pos], want, (a + 8) * 2.0 ** -23 * size + HALF[out] * want.abs(), "h")
+        if dtype != "e4m3":
+            z, wt, xt = torch.where(h[pos] > 0, dh[pos].double(), torch.zeros((), dtype=torch.float64, device="cuda")), W64[k].T.contiguous(), x64[pos].T.contiguous()
+            want = torch.mm(z, wt)
+            close(dx[pos], want, (b + 8) * 2.0 ** -23 * torch.mm(z.abs(), wt.abs()) + HALF[out] * want.abs(), "dx")
+            close(dw[k], torch.mm(xt, z), (len(pos) + 16) * 2.0 ** -23 * torch.mm(xt.abs(), z.abs()), "dW")
+            close(db[k], z.sum(0), (len(pos) + 16) * 2.0 ** -23 * z.abs().sum(0), "db")
+    rest = order[int(offsets[G]):].long()
+    assert bool((h[rest] == -77).all()) and (dtype == "e4m3" or bool((dx[rest] == -77).all()))
