@@ -124,12 +124,15 @@ __device__ __forceinline__ const char* uniform(const char* p) {
     const uint64_t v = (uint64_t)(uintptr_t)p;
     return (const char*)(uintptr_t)(((uint64_t)(unsigned int)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (unsigned int)__builtin_amdgcn_readfirstlane((int)v));
 }
-// the same from such an address and an offset below 2^31
+// 16 bytes a lane from memory to LDS, from such an address and an offset below 2^31, or from an address of the lane's own. M0, which holds the place in LDS, is not
+// the statement's to change (the compiler takes no such register as overwritten): it is put back.
 __device__ __forceinline__ void load_to_lds(const char* base, unsigned int offset, unsigned int lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory");
+    unsigned int was;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0" : "=&s"(was) : "s"(lds), "v"(offset), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds(const char* from, unsigned int lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+    unsigned int was;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0" : "=&s"(was) : "s"(lds), "v"(from) : "memory");
 }
 // A store that is counted by hand as well: it is issued whatever the lanes have to write
 __device__ __forceinline__ void store_16(char* to, fg_u32x4 v) { asm volatile("global_store_dwordx4 %0, %1, off\n\ts_nop 1" ::"v"(to), "v"(v) : "memory"); }

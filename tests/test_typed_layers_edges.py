@@ -1,6 +1,10 @@
 """The calls of a typed layer where one kind of input decides: 8-bit rows whose products differ by many orders of magnitude, entries that are
 skipped in the gradients, lists longer than a launch, limits. Tolerances as in tests/test_typed_layers.py: a sum of K products in fp32 is granted
 K steps of 2^-23 of the sum of the products' magnitudes, a result half a step of its type."""
+import glob
+import os
+import re
+
 import numpy as np
 import pytest
 import torch
@@ -30,6 +34,23 @@ def test_widths_beyond_the_limit_are_refused(B):
                                1 << 62) == B.FG_ERR_SHAPE
                 assert B.fg_linear_grouped_backward_workspace_bytes(dtype, 10, 4, a, b) == 0
                 assert B.fg_linear_grouped_backward_workspace_bytes(dtype, 10, 4, min(a, most), min(b, most)) > 0
+
+
+# ---- statements the compiler does not see into ----
+
+def test_statements_that_write_m0_put_it_back():
+    """M0 cannot be named as overwritten, so that a statement has to leave it as it was."""
+    found = 0
+    for path in sorted(glob.glob(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2301_07482_amd", "csrc", "*"))):
+        for text in re.findall(r'asm\s*(?:volatile)?\s*\(\s*"((?:[^"\\]|\\.)*)"', open(path).read()):
+            lines = [line.strip() for line in re.split(r"\\n|\\t|;", text) if line.strip()]
+            if not any(re.match(r"s_mov_b32 m0,", line) for line in lines):
+                assert "m0" not in text, (path, text)
+                continue
+            found += 1
+            kept = re.match(r"s_mov_b32 (%\d), m0$", lines[0])
+            assert kept and lines[-1] == f"s_mov_b32 m0, {kept.group(1)}", (path, text)
+    assert found
 
 
 # ---- 8-bit rows ----
