@@ -220,3 +220,95 @@ def test_the_widest_rows(B, dtype, a, b):
             close(db[k], z.sum(0), (len(pos) + 16) * 2.0 ** -23 * z.abs().sum(0), "db")
     rest = order[int(offsets[G]):].long()
     assert bool((h[rest] == -77).all()) and (dtype == "e4m3" or bool((dx[rest] == -77).all()))
+
+
+def guarded(shape, dtype, fill=-77.0, guard=64):
+    """A tensor with sentinels around it (16-byte aligned): (the whole, the part that calls get)."""
+    count = int(np.prod(shape))
+    whole = torch.full((guard + count + guard,), fill, dtype=dtype, device="cuda")
+    return whole, whole[guard:guard + count].view(shape)
+
+
+def untouched(whole, fill=-77.0, guard=64):
+    return bool((whole[:guard] == fill).all()) and bool((whole[-guard:] == fill).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype, n, a, b", [("f32", 150, 64, 64), ("bf16", 150, 64, 64), ("f16", 150, 72, 40), ("f32", 9_000, 36, 132), ("bf16", 9_000, 264, 136), ("bf16", 40_000, 520, 520)])
+@pytest.mark.parametrize("masked", [True, False])
+@pytest.mark.parametrize("with_src", [True, False])
+def test_gradients_skip_what_the_forward_call_skips(B, dtype, n, a, b, masked, with_src):
+    """Bad positions, bad rows, entries beyond the bound: no part in dx, dW or db, though the rows they would take are NaN."""
+    r = np.random.default_rng(n + a + masked)
+    G = 3
+    order, offsets = layout(r, n, G, 0.9)
+    x_rows = 2 * n if with_src else n - 4
+    src = r.integers(0, x_rows, n).astype(np.int32) if with_src else None
+    entries = order.copy()
+    skipped = set(r.choice(len(order), 12, replace=False).tolist())
+    for i, k in enumerate(sorted(skipped)):
+        if with_src and i % 2:
+            src[order[k]] = (-1, x_rows, -2 ** 31, 2 ** 31 - 1)[i // 2 % 4]
+        else:
+            entries[k] = (-1, n, -2 ** 31, 2 ** 31 - 1)[i // 2 % 4]
+    if not with_src:
+        skipped |= {k for k in range(len(order)) if order[k] >= x_rows}
+    bound = len(order) - 30
+    taken = [k for k in range(bound) if k not in skipped]
+    members = [[int(order[k]) for k in taken if offsets[g] <= k < offsets[g + 1]] for g in range(G)]
+    good, at = [p for m in members for p in m], np.cumsum([0] + [len(m) for m in members]).tolist()
+    x, dh, h = matrix(r, max(x_rows, n), a, dtype), matrix(r, n, b, dtype), matrix(r, n, b, dtype)
+    W = torch.from_numpy(r.standard_normal((G, a, b)) / 8).to(T[dtype])
+    (dx, dxs), (dW, dWs), (db, dbs) = R.grouped_linear_backward(x, W, dh, h if masked else None, good, at, src.tolist() if with_src else None)
+    used = np.array([src[p] if with_src else p for p in good])
+    x[np.setdiff1d(np.arange(len(x)), used)] = float("nan")
+    rest = np.setdiff1d(np.arange(n), good)
+    dh[rest], h[rest] = float("nan"), float("nan")
+    xd, dhd, hd, Wd = x.cuda(), dh.cuda(), h.cuda(), W.cuda()
+    (gx_all, gx), (gw_all, gw), (gb_all, gb) = guarded((n, a), torch.float32), guarded((G, a, b), torch.float32), guarded((G, b), torch.float32)
+    size = B.fg_linear_grouped_backward_workspace_bytes(code(B, dtype), bound, G, a, b)
+    ws_all, ws = guarded((size,), torch.uint8, 0xAB, 4096)
+    B.fg_linear_grouped_backward(xd, x_rows, stride(xd), code(B, dtype), cuda(torch.from_numpy(src)) if with_src else None, dhd, stride(dhd), code(B, dtype), hd if masked else None,
+                                 stride(hd) if masked else 0, n, torch.from_numpy(entries).cuda(), torch.from_numpy(offsets).cuda(), bound, G, a, b, Wd, gx, 4 * a, B.FG_F32, gw, gb,
+                                 ws, size)
+    torch.cuda.synchronize()
+    close(gx.cpu()[good], dx, (b + 8) * 2.0 ** -23 * dxs + HALF["f32"] * dx.abs(), "dx")
+    rows = (np.diff(at).max() + 16) * 2.0 ** -23
+    close(gw.cpu(), dW, rows * dWs + 2.0 ** -24 * dW.abs(), "dW")
+    close(gb.cpu(), db, rows * dbs + 2.0 ** -24 * db.abs(), "db")
+    assert bool((gx.cpu()[rest] == -77).all())
+    assert all(untouched(w) for w in (gx_all, gw_all, gb_all)) and untouched(ws_all, 0xAB, 4096)
+
+
+@gpu
+@pytest.mark.parametrize("dtype, n, a, b", [("f32", 300, 64, 64), ("bf16", 300, 64, 64), ("f32", 9_000, 132, 260), ("f16", 20_000, 264, 136)])
+@pytest.mark.parametrize("masked", [True, False])
+@pytest.mark.parametrize("shape", ["falling", "overlapping", "beyond", "negative"])
+def test_offsets_that_do_not_ascend_stay_in_bounds(B, dtype, n, a, b, masked, shape):
+    """Not what fg_group_rows leaves: no memory but the call's own is touched. A group whose end lies before its begin has no rows, and as long as no entry has two
+    groups, the other groups' weight gradients are those of their entries."""
+    r = np.random.default_rng(n + a)
+    at = {"falling": [0, n, n // 2, n // 3, 0], "overlapping": [0, n - 7, 30, n, n // 2, n], "beyond": [0, n // 2, n + 1000, 2 ** 40, n + 5], "negative": [-5, -2 ** 40, n // 3, n, n]}[shape]
+    G = len(at) - 1
+    order = r.permutation(n).astype(np.int32)
+    x, dh, h = matrix(r, n, a, dtype), matrix(r, n, b, dtype), matrix(r, n, b, dtype)
+    W = torch.from_numpy(r.standard_normal((G, a, b)) / 8).to(T[dtype])
+    xd, dhd, hd, Wd, od, fd = x.cuda(), dh.cuda(), h.cuda(), W.cuda(), torch.from_numpy(order).cuda(), torch.tensor(at, dtype=torch.int64, device="cuda")
+    (h_all, out), (gx_all, gx), (gw_all, gw), (gb_all, gb) = (guarded(s, torch.float32) for s in ((n, b), (n, a), (G, a, b), (G, b)))
+    size = B.fg_linear_grouped_backward_workspace_bytes(code(B, dtype), n, G, a, b)
+    ws_all, ws = guarded((size,), torch.uint8, 0xAB, 4096)
+    B.fg_linear_grouped(xd, n, stride(xd), code(B, dtype), None, None, od, fd, n, G, a, b, Wd, None, None, 0, out, n, 4 * b, B.FG_F32)
+    B.fg_linear_grouped_backward(xd, n, stride(xd), code(B, dtype), None, dhd, stride(dhd), code(B, dtype), hd if masked else None, stride(hd) if masked else 0, n, od, fd, n, G, a,
+                                 b, Wd, gx, 4 * a, B.FG_F32, gw, gb, ws, size)
+    torch.cuda.synchronize()
+    assert all(untouched(w) for w in (h_all, gx_all, gw_all, gb_all)) and untouched(ws_all, 0xAB, 4096)
+    if shape == "overlapping":
+        return
+    inside = [min(max(o, 0), n) for o in at]
+    for g in range(G):
+        pos = order[inside[g]:max(inside[g], inside[g + 1])].astype(np.int64)
+        z = dh[pos].double()
+        if masked:
+            z = torch.where(h[pos] > 0, z, torch.zeros((), dtype=torch.float64))
+        xs = x[pos].double().T
+        close(gw[g].cpu(), xs @ z, (len(pos) + 16) * 2.0 ** -23 * (xs.abs() @ z.abs()), f"dW of group {g}")
