@@ -312,3 +312,103 @@ def test_offsets_that_do_not_ascend_stay_in_bounds(B, dtype, n, a, b, masked, sh
             z = torch.where(h[pos] > 0, z, torch.zeros((), dtype=torch.float64))
         xs = x[pos].double().T
         close(gw[g].cpu(), xs @ z, (len(pos) + 16) * 2.0 ** -23 * (xs.abs() @ z.abs()), f"dW of group {g}")
+
+
+# ---- memory ----
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_that_lie_further_apart_than_32_bits_count(B, dtype):
+    """Row strides of 64 MB: the last rows' offsets are beyond 2^32. Results as with packed rows, bit for bit."""
+    n, G, a, b, p, key = 70, 2, 64, 64, 0.3, 9
+    r = np.random.default_rng(5)
+    size, row = T[dtype].itemsize, (1 << 26) + 16
+    c = code(B, dtype)
+    order, offsets = layout(r, n, G, 0.9)
+    od, fd = torch.from_numpy(order).cuda(), torch.from_numpy(offsets).cuda()
+    src = torch.from_numpy(r.permutation(n).astype(np.int32)).cuda()
+    W, values = torch.from_numpy(r.standard_normal((G, a, b)) / 8).to(T[dtype]).cuda(), {k: matrix(r, n, a, dtype).cuda() for k in ("x", "dh", "h", "res")}
+    ws = torch.zeros(max(B.fg_linear_grouped_backward_workspace_bytes(c, n, G, a, b), B.fg_residual_norm_backward_workspace_bytes(n, a)), dtype=torch.uint8, device="cuda")
+
+    def far(v):
+        t = torch.empty(n * row // size, dtype=v.dtype, device="cuda").as_strided(v.shape, (row // size, 1))
+        return t.copy_(v)
+
+    results = []
+    for place in (lambda v: v.clone(), far):
+        t = {k: place(v) for k, v in values.items()}
+        o = {k: place(torch.full_like(values["x"], -77.0)) for k in ("out", "dx", "drop", "sum", "y", "dsum", "dres")}
+        dw, db, rstd, gain = (torch.zeros(s, device="cuda") for s in ((G, a, b), (G, b), (n,), (a,)))
+        B.fg_linear_grouped(t["x"], n, stride(t["x"]), c, None, src, od, fd, len(order), G, a, b, W, None, None, 0, o["out"], n, stride(o["out"]), c)
+        B.fg_linear_grouped_backward(t["x"], n, stride(t["x"]), c, src, t["dh"], stride(t["dh"]), c, t["h"], stride(t["h"]), n, od, fd, len(order), G, a, b, W, o["dx"],
+                                     stride(o["dx"]), c, dw, db, ws, ws.numel())
+        B.fg_dropout(t["x"], stride(t["x"]), c, od, None, len(order), n, a, p, key, o["drop"], stride(o["drop"]))
+        B.fg_residual_norm(t["x"], stride(t["x"]), c, t["res"], stride(t["res"]), c, od, None, len(order), n, a, p, key, None, 1e-6, o["sum"], stride(o["sum"]), o["y"],
+                           stride(o["y"]), c, None, rstd)
+        B.fg_residual_norm_backward(t["dh"], stride(t["dh"]), c, o["sum"], stride(o["sum"]), c, rstd, None, t["res"], stride(t["res"]), od, None, len(order), n, a, p, key,
+                                    o["dsum"], stride(o["dsum"]), o["dres"], stride(o["dres"]), gain, ws, ws.numel())
+        torch.cuda.synchronize()
+        results.append([v.clone(memory_format=torch.contiguous_format) for v in (*o.values(), dw, db, rstd, gain)])
+        del t, o
+    for near, away in zip(*results):
+        assert torch.equal(near, away) and bool((near != -77).any())
+
+
+@gpu
+def test_16_and_8_bit_layers_captured(B):
+    """A serving step in 8 bits and a training step in bf16 with an fp32 sum, captured with one workspace and replayed with new inputs between eager calls."""
+    n, G, a, b, p, key = 900, 4, 128, 136, 0.25, 11
+    c = B.FG_BF16
+    z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype, device="cuda")
+    bf = torch.bfloat16
+
+    def inputs(seed):
+        r = np.random.default_rng(seed)
+        f = lambda *s: torch.from_numpy(r.standard_normal(s)).to(bf).cuda()
+        return dict(types=torch.from_numpy(r.integers(0, G, n).astype(np.int32)).cuda(), x=f(n, a), W=f(G, a, b) / 8, dy=f(n, b), res=torch.from_numpy(r.standard_normal((n, b))).float().cuda(),
+                    Wt=f(G, b, a), n_rows=torch.tensor([n - seed], device="cuda"))
+
+    def outputs():
+        return dict(order=z(n, dtype=torch.int32), offsets=z(G + 1, dtype=torch.int64), q=z(n, a, dtype=torch.float8_e4m3fn), qs=z(n), wq=z(G, b, a, dtype=torch.float8_e4m3fn), wqs=z(G, b),
+                    served=z(n, b, dtype=bf), h=z(n, b), sum=z(n, b), y=z(n, b, dtype=torch.float8_e4m3fn), ys=z(n), rstd=z(n), dres=z(n, b), dh=z(n, b), gain=z(b), dx=z(n, a, dtype=bf),
+                    dW=z(G, a, b), db=z(G, b))
+
+    def steps(t, o, ws):
+        st = torch.cuda.current_stream().cuda_stream
+        B.fg_group_rows(t["types"], n, None, n, None, t["n_rows"], n, G, o["order"], o["offsets"], ws, ws.numel(), st)
+        B.fg_quantize_rows(t["x"], 2 * a, c, n, a, o["q"], a, o["qs"], st)
+        B.fg_quantize_rows(t["Wt"], 2 * a, c, G * b, a, o["wq"], a, o["wqs"], st)
+        B.fg_linear_grouped(o["q"], n, a, B.FG_E4M3, o["qs"], None, o["order"], o["offsets"], n, G, a, b, o["wq"], o["wqs"], None, 1, o["served"], n, 2 * b, c, st)
+        B.fg_linear_grouped(t["x"], n, 2 * a, c, None, None, o["order"], o["offsets"], n, G, a, b, t["W"], None, None, 1, o["h"], n, 4 * b, B.FG_F32, st)
+        B.fg_residual_norm(o["h"], 4 * b, B.FG_F32, t["res"], 4 * b, B.FG_F32, None, t["n_rows"], n, n, b, p, key, None, 1e-6, o["sum"], 4 * b, o["y"], b, B.FG_E4M3, o["ys"],
+                           o["rstd"], st)
+        B.fg_residual_norm_backward(t["res"], 4 * b, B.FG_F32, o["sum"], 4 * b, B.FG_F32, o["rstd"], None, None, 0, None, t["n_rows"], n, n, b, p, key, o["dres"], 4 * b, o["dh"],
+                                    4 * b, o["gain"], ws, ws.numel(), st)
+        B.fg_linear_grouped_backward(t["x"], n, 2 * a, c, None, o["dh"], 4 * b, B.FG_F32, o["h"], 4 * b, n, o["order"], o["offsets"], n, G, a, b, t["W"], o["dx"], 2 * a, c, o["dW"],
+                                     o["db"], ws, ws.numel(), st)
+
+    space = lambda: z(max(B.fg_group_rows_workspace_bytes(n, G), B.fg_residual_norm_backward_workspace_bytes(n, b), B.fg_linear_grouped_backward_workspace_bytes(c, n, G, a, b)),
+                      dtype=torch.uint8)
+    data = [inputs(1), inputs(200)]
+    want = []
+    for d in data:
+        want.append(outputs())
+        steps(d, want[-1], space())
+    torch.cuda.synchronize()
+    assert all(bool((w["served"].float() != 0).any()) and bool((w["dW"] != 0).any()) for w in want)
+    t, o, ws = inputs(3), outputs(), space()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        steps(t, o, ws)
+    for i in (0, 1, 1, 0, 1):
+        for k, v in data[i].items():
+            t[k].copy_(v)
+        for v in o.values():
+            v.view(torch.uint8).zero_()
+        g.replay()
+        steps(data[1 - i], outputs(), space())      # an eager call between the replays
+        torch.cuda.synchronize()
+        for k, v in o.items():
+            assert torch.equal(v.view(torch.uint8), want[i][k].view(torch.uint8)), (i, k)
