@@ -795,8 +795,8 @@ fg_status_t fg_backward_weights_all(fg_dtype_t compute_dtype, int32_t n_layers, 
  * For relational models (the paper's R-GCN on the heterogeneous MAG240M, Section 7.5): the nodes have types ("groups"), and the dense
  * update of a row takes its group's weights. fg_group_rows sorts a layer's listed rows by group on the device, fg_linear_grouped
  * multiplies, fg_linear_grouped_backward gives the gradients. fg_residual_norm, fg_dropout and their backward passes are the element-wise part of a deeper
- * model's layer. All of them work by position, on the rows listed (no position twice), as the calls above: rows that are not listed are neither
- * read nor written.
+ * model's layer. All of them work by position, on the rows listed (no position twice), as the calls above: rows that are not listed are not
+ * written, and nothing that is depends on them.
  *
  * fg_group_rows: the listed positions r = rows[k], k < *n_rows_dev, sorted by their group, stably (in list order within a group):
  *   order[offsets[g] .. offsets[g + 1]) = the positions of group g = groups[v], v = ids[r] (ids NULL: v = r)
@@ -852,7 +852,8 @@ fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, f
  *                                       rounded to `dtype` after the mask, as in fg_layer_backward_bf16 (db sums the unrounded ones)
  *   h, h_stride, h_dtype                rows by position, of the type they were written in (the forward call's out_dtype)
  *   dx, dx_stride, dx_dtype             FG_F32 or `dtype`
- *   ws_dev, ws_bytes                    >= fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned
+ *   ws_dev, ws_bytes                    >= fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned, as are
+ *                                       the arrays of values and their strides
  * An entry that the forward call skips has no part in any of the sums and gets no dx. dW: the rows are cut into equal ranges, as many as
  * keep the chip busy (512 over the result's number of tiles of 128 x 128, 256 over that of 256 x 256 where those are used; one or two from there
  * on), fp32 sums within a range, fp64 across ranges; db the same with 64 rows. No atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out * sizeof(dtype) a multiple of 16. A dW of about

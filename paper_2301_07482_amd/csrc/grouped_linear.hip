@@ -107,8 +107,8 @@ __device__ __forceinline__ void entry(const GlArgs& A, int64_t k, int64_t k1, in
 // fg_linear. The values lie in LDS as they are and are split as they are read: the split costs about the vector instructions that the
 // products cost matrix instructions.
 //
-// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 122 us
-// (1.01 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
+// Measured: 368640 x 768 x 1024 fp16 710 us (0.82 PFLOP/s, 1.07 at K = 4096; a large library product 1.31), 58982 x 1024 x 1024 8 bits to bf16 130 us
+// (0.95 PFLOP/s), 54067 x 100 x 256 fp32 39 us (2.0 TB/s of its bytes), 256 x 64 x 64 fp32 6 us (latency). What bounds the large ones: the loop runs at
 // 2.0 us for the 1.15 us that its matrix instructions take by themselves and the 0.85 us that LDS is busy with them; tiles of 256 x 256 on four
 // wavefronts, with a third fewer LDS reads, took 1010 us instead of 702 (nothing fills the waits of a lone wavefront), tiles of 128 x 256 two
 // to a compute unit 12 % longer.
@@ -611,7 +611,8 @@ fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
 //                   8 bits: 65536 rows 20.3 | 21.0, K = N = 1024 121 | 136, 32768 rows 16.9 | 12.2; N = 128 17.4 | 12.3; 193 rows a group 33.7 | 30.2, 128 rows a group 36.0 | 25.4
 //   128 against 64: 16384 rows bf16 9.6 | 11.1, fp32 21.4 | 22.5, 8 bits 9.3 | 10.2; 8192 rows 8.7 | 7.1, 20.1 | 13.7, 8.6 | 6.5; N = 64 fp32 32.6 | 22.7;
 //                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 62 | 65; 64 rows a group 43 | 53, 134 | 115, 72 | 49
-// No 256 x 256 tile for fp32, whose two sums do not fit the registers.
+// No 256 x 256 tile for fp32, whose two sums do not fit the registers. (PER_CU: of four of the 64 x 64 tile
+// LDS holds three, and of two of the 128 x 128 tile in 8 bits one above 767 groups; the others start as those end.)
 template <int T, bool B_KN>
 fg_status_t tile_product(GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
