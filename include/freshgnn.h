@@ -829,9 +829,8 @@ fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int3
  *   bias [n_groups x d_out]             float, or NULL;  relu != 0: act = ReLU
  *   h_out, n_out, out_stride            rows of out_dtype (FG_F32, FG_F16 or FG_BF16; FG_F32 for FG_F32 rows) by position
  * Products: fp32 rows as in fg_linear (from exact three-way bf16 splits, fp32 sums; same input domain); the narrower types are multiplied
- * as they are (8 bits as the bf16 values they are). Sums in fp32, one rounding to out_dtype. d_in and d_out up to
- * FG_MAX_GROUPED_DIM (8-bit rows wider than FG_MAX_NORM_DIM are the caller's own), d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types);
- * x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
+ * as they are (8 bits as the bf16 values they are). Sums in fp32, one rounding to out_dtype. d_in and d_out up to FG_MAX_GROUPED_DIM (8-bit rows
+ * wider than FG_MAX_NORM_DIM are the caller's own), d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types); x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
  * [0, x_rows) are skipped.
  */
 #define FG_MAX_GROUPED_ROWS 536870912
@@ -856,13 +855,14 @@ fg_status_t fg_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, f
  *                                       the arrays of values and their strides
  * An entry that the forward call skips has no part in any of the sums and gets no dx. dW: the rows are cut into equal ranges, as many as
  * keep the chip busy (512 over the result's number of tiles of 128 x 128, 256 over that of 256 x 256 where those are used; one or two from there
- * on), fp32 sums within a range, fp64 across ranges; db the same with 64 rows. No atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out * sizeof(dtype) a multiple of 16. A dW of about
- * 2^36 values, with d_in and d_out rounded up to 256, and more is refused.
+ * on), fp32 sums within a range, fp64 across ranges; db the same with 64 rows. No atomics, results do not depend on scheduling. Sizes and alignment as for fg_linear_grouped, d_out *
+ * sizeof(dtype) a multiple of 16. A dW of about 2^36 values, with d_in and d_out rounded up to 256, and more is refused.
  */
 size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out);
 fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev, const void* dh,
                                        int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, fg_dtype_t h_dtype, int64_t n,
-                                       const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out, const void* W,
+                                       const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                                       int32_t d_out, const void* W,
                                        void* dx, int64_t dx_stride, fg_dtype_t dx_dtype, float* dw_dev, float* db_dev, void* ws_dev,
                                        size_t ws_bytes, void* stream);
 

@@ -611,8 +611,8 @@ fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
 //                   8 bits: 65536 rows 20.3 | 21.0, K = N = 1024 121 | 136, 32768 rows 16.9 | 12.2; N = 128 17.4 | 12.3; 193 rows a group 33.7 | 30.2, 128 rows a group 36.0 | 25.4
 //   128 against 64: 16384 rows bf16 9.6 | 11.1, fp32 21.4 | 22.5, 8 bits 9.3 | 10.2; 8192 rows 8.7 | 7.1, 20.1 | 13.7, 8.6 | 6.5; N = 64 fp32 32.6 | 22.7;
 //                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 62 | 65; 64 rows a group 43 | 53, 134 | 115, 72 | 49
-// No 256 x 256 tile for fp32, whose two sums do not fit the registers. (PER_CU: of four of the 64 x 64 tile
-// LDS holds three, and of two of the 128 x 128 tile in 8 bits one above 767 groups; the others start as those end.)
+// No 256 x 256 tile for fp32, whose two sums do not fit the registers. (PER_CU: of four workgroups of the 64 x 64 tile LDS holds three, and of two
+// of the 128 x 128 tile in 8 bits one above 767 groups; the others start as those end.)
 template <int T, bool B_KN>
 fg_status_t tile_product(GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
@@ -1288,7 +1288,7 @@ extern "C" size_t fg_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, i
 
 extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
                                                   const void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, const void* h, int64_t h_stride, fg_dtype_t h_dtype,
-                                                  int64_t n,                                                   const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups,
+                                                  int64_t n, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups,
                                                   int32_t d_in, int32_t d_out, const void* W, void* dx, int64_t dx_stride, fg_dtype_t dx_dtype,
                                                   float* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes, void* stream) {
     const char* who = "fg_linear_grouped_backward";
