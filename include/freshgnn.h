@@ -830,7 +830,8 @@ fg_status_t fg_group_rows(const int32_t* groups_dev, int64_t n_table, const int3
  *   h_out, n_out, out_stride            rows of out_dtype (FG_F32, FG_F16 or FG_BF16; FG_F32 for FG_F32 rows) by position
  * Products: fp32 rows as in fg_linear (from exact three-way bf16 splits, fp32 sums; same input domain); the narrower types are multiplied
  * as they are (8 bits as the bf16 values they are). Sums in fp32, one rounding to out_dtype. d_in and d_out up to FG_MAX_GROUPED_DIM (8-bit rows
- * wider than FG_MAX_NORM_DIM are the caller's own), d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types); x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
+ * wider than FG_MAX_NORM_DIM are the caller's own), d_in * sizeof(dtype) a multiple of 16, d_out a multiple of 4 (8 for the narrower types);
+ * x, W, h_out and the strides 16-byte aligned, bias and the scales 4-byte. Entries with a position outside [0, n_out) or a row outside
  * [0, x_rows) are skipped.
  */
 #define FG_MAX_GROUPED_ROWS 536870912
