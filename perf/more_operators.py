@@ -1,0 +1,434 @@
+"""The operators of a student block, as they are measured: each case one pass through one of them. A student learns a trained graph model's
+answers and is served without the graph: rows of the feature table, a few dense blocks, classes.
+
+  gated     a gated feed-forward layer: both projections, the activation and the product (`fg_gated_linear_grouped`): forward, with the
+            projections kept for training or without
+  gated_bw  its gradients: rows, weights, biases (`fg_gated_linear_grouped_backward`)
+  gnorm     group norm with an activation over the rows of each graph of a batch, or of each node type (`fg_group_norm`): forward
+  gnorm_bw  its gradients: rows, gain, offset (`fg_group_norm_backward`)
+  distill   the loss against a teacher's stored top logits and the hard labels, and its gradient (`fg_distill_loss`)
+
+Widths and row counts are those of the repository's workloads (`fg_inputs.workload`), of its ragged cases, or generic: listed rows
+(`listed_share` of the positions) of a layer, in ascending order. The layers with a weight matrix per type are measured with one type, which
+tensor operations multiply in one product.
+"""
+import math
+
+import torch
+
+own = False
+
+_TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+_SIZE = {"f32": 4, "f16": 2, "bf16": 2}
+_EPS = 1e-5
+
+
+def listed():
+    return [
+        # serving: the rows of a handful of requests through a layer of the small model and of the wide one; launches and latency decide
+        dict(name="gated_few_f32", op="gated", dtype="f32", out="f32", act="silu", n=5, listed_share=1.0, d_in=64, d_out=256, table=0, keep=False),
+        dict(name="gated_few_bf16", op="gated", dtype="bf16", out="bf16", act="silu", n=16, listed_share=1.0, d_in=1024, d_out=1024, table=0, keep=False),
+        # a training step's first layer over the raw fp16 features of the widest graph, read from the table by node id
+        dict(name="gated_table_f16", op="gated", dtype="f16", out="f16", act="gelu", n=409_600, listed_share=0.9, d_in=768, d_out=1024, table=1_000_000,
+             keep=True),
+        # gradients of a user's own small model (88 columns are no multiple of a tile), and of the wide mixed-precision one
+        dict(name="gated_bw_f32", op="gated_bw", dtype="f32", act="silu", n=51_003, listed_share=0.85, d_in=88, d_out=256),
+        dict(name="gated_bw_bf16", op="gated_bw", dtype="bf16", act="silu", n=65_536, listed_share=0.9, d_in=1024, d_out=1024),
+        # many small graphs to a batch, and a layer of a hidden width whose rows have a few types
+        dict(name="gnorm_graphs_f32", op="gnorm", dtype="f32", act="relu", n=31_744, parts=1024, gathered=False, d=100, channel_groups=5),
+        dict(name="gnorm_types_bf16", op="gnorm", dtype="bf16", act="silu", n=65_536, parts=4, gathered=True, d=1024, channel_groups=32),
+        dict(name="gnorm_bw_few", op="gnorm_bw", dtype="f32", act="gelu", n=777, parts=9, gathered=False, d=88, channel_groups=8),
+        dict(name="gnorm_bw_bf16", op="gnorm_bw", dtype="bf16", act="silu", n=65_536, parts=4, gathered=True, d=1024, channel_groups=32),
+        # the smallest workload's seeds; the seeds of a step with the hidden width's classes; many classes (the items of a recommender)
+        dict(name="distill_few", op="distill", dtype="f32", n=256, listed_share=1.0, d=64, k=8, temperature=2.0, alpha=0.5, table=10_000),
+        dict(name="distill_f32", op="distill", dtype="f32", n=67_584, listed_share=0.8, d=256, k=16, temperature=4.0, alpha=0.9, table=1_000_000),
+        dict(name="distill_many_bf16", op="distill", dtype="bf16", n=8192, listed_share=1.0, d=50_003, k=32, temperature=2.0, alpha=0.5, table=1_000_000),
+    ]
+
+
+def draw(rng):
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    op = rng.choice(["gated", "gated", "gated_bw", "gated_bw", "gnorm", "gnorm_bw", "distill", "distill"])
+    dtype, share = rng.choice(["f32", "f16", "bf16"]), round(rng.uniform(0.5, 1.0), 3)
+    if op in ("gated", "gated_bw"):
+        step = {"f32": 4, "f16": 8, "bf16": 8}[dtype]
+        width = lambda: step * max(1, log_int(32, 1024) // step)
+        case = dict(op=op, dtype=dtype, act=rng.choice(["silu", "gelu", "relu", "sigmoid"]), n=log_int(1, 100_000), listed_share=share, d_in=width(), d_out=width())
+        if op == "gated":
+            return dict(case, out=rng.choice(["f32", dtype]), table=rng.choice([0, 300_000]), keep=rng.random() < 0.5)
+        return case
+    if op in ("gnorm", "gnorm_bw"):
+        groups, n = rng.choice([1, 2, 5, 8, 32]), log_int(1, 200_000)
+        d = groups * max(1, log_int(16, 2048) // groups)
+        n = max(1, min(n, 60_000_000 // d))
+        acts = ["none", "silu", "gelu", "sigmoid"] + (["relu"] if op == "gnorm" else [])      # (a gradient at ReLU's corner is one of two)
+        if rng.random() < 0.5:
+            return dict(op=op, dtype=dtype, act=rng.choice(acts), n=n, parts=log_int(1, 16), gathered=True, d=d, channel_groups=groups)
+        return dict(op=op, dtype=dtype, act=rng.choice(acts), n=n, parts=max(1, n // log_int(4, 1000)), gathered=False, d=d, channel_groups=rng.choice([groups, d]))
+    d = log_int(8, 50_000)
+    return dict(op=op, dtype=dtype, n=max(1, min(log_int(1, 100_000), 300_000_000 // d)), listed_share=share, d=d, k=min(d, rng.choice([1, 4, 8, 16, 50, 64])),
+                temperature=rng.choice([1.0, 2.0, 4.0, 2.5]), alpha=rng.choice([0.5, 0.9, 1.0]), table=rng.choice([20_000, 500_000]))
+
+
+class _State:
+    pass
+
+
+def _count(case):
+    return max(1, int(case["n"] * case.get("listed_share", 1.0)))
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda").manual_seed(int(seed))
+    kw = dict(device="cuda", generator=gen)
+    s = _State()
+    s.case, s.n = case, case["n"]
+    op, n, t = case["op"], case["n"], _TYPES[case["dtype"]]
+    s.k = k = _count(case)
+    s.rows = torch.randperm(n, **kw)[:k].sort().values.int() if k < n else None
+    s.ws = None      # the workspace: laid out by the first call, kept as a program keeps it
+    if op in ("gated", "gated_bw"):
+        a, b = case["d_in"], case["d_out"]
+        s.offsets = torch.tensor([0, k], dtype=torch.int64, device="cuda")      # one type
+        table = case.get("table", 0)
+        s.ids = torch.randint(0, table, (n,), **kw).int() if table else None
+        s.x = torch.randn(table or n, a, **kw).to(t)
+        s.w = ((torch.rand(1, a, 2 * b, **kw) * 2 - 1) * math.sqrt(6.0 / (a + b))).to(t)
+        s.bias = torch.randn(1, 2 * b, **kw) * 0.1
+        if op == "gated":
+            s.h = torch.zeros(n, b, dtype=_TYPES[case["out"]], device="cuda")
+            s.z = torch.zeros(n, 2 * b, dtype=t, device="cuda") if case["keep"] else None
+        else:
+            s.z = (s.x @ s.w[0] + s.bias).to(t)      # the forward call's projections
+            s.dh = torch.randn(n, b, **kw).to(t)
+            s.dx = torch.zeros(n, a, dtype=t, device="cuda")
+            s.dw, s.db = torch.zeros(1, a, 2 * b, dtype=t, device="cuda"), torch.zeros(1, 2 * b, device="cuda")
+    elif op in ("gnorm", "gnorm_bw"):
+        d, parts = case["d"], case["parts"]
+        if case["gathered"]:      # a few frequent types, many rare ones; most positions listed, sorted by type
+            types = torch.multinomial(1.0 / torch.arange(1, parts + 1, device="cuda").float(), n, replacement=True, generator=gen)
+            types = torch.where(torch.rand(n, **kw) < 0.1, parts, types)
+            s.order = torch.sort(types, stable=True).indices.int()
+            s.offsets = (types[:, None] < torch.arange(parts + 1, device="cuda")).sum(0)
+        else:                     # graphs that lie behind each other, of uneven sizes, some of them empty
+            s.order, s.offsets = None, torch.zeros(parts + 1, dtype=torch.int64, device="cuda")
+            s.offsets[1:-1], s.offsets[-1] = torch.randint(0, n + 1, (parts - 1,), **kw).sort().values, n
+        level = torch.randn(d, **kw)      # columns of different level and spread
+        s.x = (torch.randn(n, d, **kw) * torch.exp(0.5 * torch.randn(d, **kw)) + level).to(t)
+        s.w, s.b = 1 + 0.1 * torch.randn(d, **kw), 0.1 * torch.randn(d, **kw)
+        if op == "gnorm":
+            s.y = torch.zeros(n, d, dtype=t, device="cuda")
+            s.mean, s.rstd = (torch.zeros(parts, case["channel_groups"], device="cuda") for _ in range(2))
+        else:
+            _, s.mean, s.rstd = _statistics(s, s.x[_entries(s)].float())      # the forward call's
+            s.dy = torch.randn(n, d, **kw).to(t)
+            s.dx = torch.zeros(n, d, dtype=t, device="cuda")
+            s.dw, s.db = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+    else:
+        d, top, table = case["d"], case["k"], case["table"]
+        s.h = (3 * torch.randn(n, d, **kw)).to(t)
+        s.ids = torch.randint(0, table, (n,), **kw).int()
+        step = torch.randint(1, max(2, d // top + 1), (table, 1), **kw)
+        s.top_idx = ((torch.randint(0, d, (table, 1), **kw) + step * torch.arange(top, device="cuda")) % d).int()      # distinct classes
+        s.top_val = (4 * torch.randn(table, top, **kw)).sort(1, descending=True).values.half()
+        s.top_idx[torch.rand(table, top, **kw) < 0.02] = -1      # nodes with fewer than k stored logits, a few without any, ...
+        s.top_idx[torch.rand(table, **kw) < 0.01] = -1
+        s.labels = torch.randint(0, d, (n,), **kw).int()
+        s.labels[torch.rand(n, **kw) < 0.5] = -1                 # ... and without a label
+        s.weight, s.scale = torch.rand(n, **kw) + 0.5, 1.0 if case["dtype"] != "f16" else 64.0
+        s.loss = torch.zeros(n, device="cuda")
+        s.dh = torch.zeros(n, d, dtype=t, device="cuda")
+    return s
+
+
+def run(state):
+    return (_own if own else _plain)[state.case["op"]](state)
+
+
+# ---- plain forms ----
+
+def _listed_rows(s):
+    return s.rows if s.rows is not None else torch.arange(s.n, device="cuda", dtype=torch.int32)
+
+
+def _act(name, u):
+    if name == "none":
+        return u
+    if name == "relu":
+        return u.clamp_min(0)
+    if name == "gelu":
+        return 0.5 * u * (1 + torch.erf(u * math.sqrt(0.5)))
+    s = 1 / (1 + torch.exp(-u))
+    return u * s if name == "silu" else s
+
+
+def _slope(name, u):
+    if name == "none":
+        return torch.ones_like(u)
+    if name == "relu":
+        return (u > 0).to(u.dtype)
+    if name == "gelu":
+        return 0.5 * (1 + torch.erf(u * math.sqrt(0.5))) + u * torch.exp(-0.5 * u * u) * math.sqrt(0.5 / math.pi)
+    s = 1 / (1 + torch.exp(-u))
+    return s * (1 + u * (1 - s)) if name == "silu" else s * (1 - s)
+
+
+def _placed(like, rows, v):
+    out = torch.zeros_like(like)
+    out[rows] = v.to(like.dtype)
+    return out
+
+
+def _plain_gated(s):
+    pos, b = _listed_rows(s), s.case["d_out"]
+    x = s.x[pos if s.ids is None else s.ids[pos]].float()
+    z = x @ s.w[0].float() + s.bias[0]
+    h = _placed(s.h, pos, _act(s.case["act"], z[:, :b]) * z[:, b:])
+    return dict(h=h, z=_placed(s.z, pos, z)) if s.case["keep"] else h
+
+
+def _plain_gated_bw(s):
+    pos, b, act = _listed_rows(s), s.case["d_out"], s.case["act"]
+    z, dh = s.z[pos].float(), s.dh[pos].float()
+    u, v = z[:, :b], z[:, b:]
+    dz = torch.cat([dh * v * _slope(act, u), dh * _act(act, u)], 1)
+    dx = _placed(s.dx, pos, dz @ s.w[0].float().T)
+    dw = (s.x[pos].float().T @ dz).to(s.dw.dtype)
+    return dict(dx=dx, dw=dw[None], db=dz.sum(0, dtype=torch.float64).float()[None])
+
+
+def _entries(s):
+    """Positions in the order of their parts, as far as they belong to one."""
+    return torch.arange(s.n, device="cuda") if s.order is None else s.order[:s.offsets[-1]].long()
+
+
+def _part_of(s, count):
+    return torch.searchsorted(s.offsets[1:], torch.arange(count, device="cuda"), right=True)
+
+
+def _part_means(s, v):
+    """[parts, channel groups]: the mean of v [entries, channel groups, channels] over a part's entries and a group's channels, in 64 bits."""
+    upto = torch.zeros(v.shape[1], len(v) + 1, dtype=torch.float64, device="cuda")      # running sums over the entries
+    torch.cumsum(v.sum(2, dtype=torch.float64).T.contiguous(), 1, out=upto[:, 1:])
+    sums = (upto[:, s.offsets[1:]] - upto[:, s.offsets[:-1]]).T
+    size = (s.offsets[1:] - s.offsets[:-1]).clamp_min(1) * v.shape[2]
+    return sums / size[:, None]
+
+
+def _statistics(s, x):
+    """Normalised rows, and every part's and channel group's mean and reciprocal deviation."""
+    x, part = x.reshape(len(x), s.case["channel_groups"], -1), _part_of(s, len(x))
+    mean = _part_means(s, x).float()
+    c = x - mean[part][:, :, None]
+    rstd = torch.rsqrt(_part_means(s, c.square()).float() + _EPS)
+    return (c * rstd[part][:, :, None]).reshape(len(x), -1), mean, rstd
+
+
+def _plain_gnorm(s):
+    pos = _entries(s)
+    xh, mean, rstd = _statistics(s, s.x[pos].float())
+    return dict(y=_placed(s.y, pos, _act(s.case["act"], xh * s.w + s.b)), mean=mean, rstd=rstd)
+
+
+def _plain_gnorm_bw(s):
+    pos = _entries(s)
+    part, split = _part_of(s, len(pos)), (len(pos), s.case["channel_groups"], -1)
+    rstd = s.rstd[part][:, :, None]
+    xh = ((s.x[pos].float().reshape(split) - s.mean[part][:, :, None]) * rstd).reshape(len(pos), -1)
+    t = s.dy[pos].float() * _slope(s.case["act"], xh * s.w + s.b)
+    q, xg = (t * s.w).reshape(split), xh.reshape(split)
+    dx = rstd * (q - _part_means(s, q).float()[part][:, :, None] - xg * _part_means(s, q * xg).float()[part][:, :, None])
+    return dict(dx=_placed(s.dx, pos, dx.reshape(len(pos), -1)), dw=(t * xh).sum(0, dtype=torch.float64).float(), db=t.sum(0, dtype=torch.float64).float())
+
+
+def _plain_distill(s):
+    rows, c = _listed_rows(s), s.case
+    T, alpha = c["temperature"], c["alpha"]
+    z, ids = s.h[rows].float(), s.ids[rows]
+    idx, y, weight = s.top_idx[ids].long(), s.labels[rows].long(), s.weight[rows]
+    there, labelled = idx >= 0, y >= 0
+    taught, idx, y = there.any(1), idx.clamp_min(0), y.clamp_min(0)[:, None]
+    # the teacher's distribution over its stored classes
+    v = torch.where(there, s.top_val[ids].float() / T, -math.inf)
+    v = v - torch.where(taught, v.amax(1), 0)[:, None]
+    log_p = v - v.exp().sum(1, keepdim=True).log()
+    p = torch.where(there, log_p.exp(), 0)
+    # the student's at the temperature, and as it is
+    hard, zt = z - z.amax(1, keepdim=True), (z - z.amax(1, keepdim=True)) / T
+    log_soft, log_hard = zt.exp().sum(1, dtype=torch.float64).log().float(), hard.exp().sum(1, dtype=torch.float64).log().float()
+    kl = torch.where(there, p * (log_p - zt.gather(1, idx) + log_soft[:, None]), 0).sum(1)
+    xent = torch.where(labelled, log_hard - hard.gather(1, y)[:, 0], 0)
+    loss = weight * (alpha * T * T * kl + (1 - alpha) * xent)
+    grad = (alpha * T * taught)[:, None] * (zt - log_soft[:, None]).exp() + ((1 - alpha) * labelled)[:, None] * (hard - log_hard[:, None]).exp()
+    grad.scatter_add_(1, idx, -alpha * T * p)
+    grad.scatter_add_(1, y, ((alpha - 1) * labelled)[:, None])
+    return dict(loss=_placed(s.loss, rows, loss), dh=_placed(s.dh, rows, grad * (s.scale * weight)[:, None]))
+
+
+_plain = dict(gated=_plain_gated, gated_bw=_plain_gated_bw, gnorm=_plain_gnorm, gnorm_bw=_plain_gnorm_bw, distill=_plain_distill)
+
+
+# ---- the framework's calls ----
+
+def _lib():
+    from paper_2301_07482_amd import binding
+    return (binding, {"f32": binding.FG_F32, "f16": binding.FG_F16, "bf16": binding.FG_BF16},
+            {"none": binding.FG_ACT_NONE, "relu": binding.FG_ACT_RELU, "silu": binding.FG_ACT_SILU, "gelu": binding.FG_ACT_GELU,
+             "sigmoid": binding.FG_ACT_SIGMOID})
+
+
+def _stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _workspace(s, need):
+    if s.ws is None:
+        s.ws = torch.zeros(max(need(), 16), dtype=torch.uint8, device="cuda")
+    return s.ws, s.ws.numel()
+
+
+def _own_gated(s):
+    B, T, A = _lib()
+    c = s.case
+    a, b, e = c["d_in"], c["d_out"], _SIZE[c["dtype"]]
+    B.fg_gated_linear_grouped(s.x, len(s.x), a * e, T[c["dtype"]], s.ids, s.rows, s.offsets, s.k, 1, a, b, s.w, s.bias, A[c["act"]], s.h, s.n,
+                              b * _SIZE[c["out"]], T[c["out"]], s.z, 2 * b * e if s.z is not None else 0, _stream())
+    return dict(h=s.h, z=s.z) if c["keep"] else s.h
+
+
+def _own_gated_bw(s):
+    B, T, A = _lib()
+    c = s.case
+    a, b, e, t = c["d_in"], c["d_out"], _SIZE[c["dtype"]], T[c["dtype"]]
+    ws, ws_bytes = _workspace(s, lambda: B.fg_gated_linear_grouped_backward_workspace_bytes(t, s.k, 1, a, b))
+    B.fg_gated_linear_grouped_backward(s.x, len(s.x), a * e, t, None, s.dh, b * e, t, s.z, 2 * b * e, s.n, s.rows, s.offsets, s.k, 1, a, b, s.w, A[c["act"]],
+                                       s.dx, a * e, t, s.dw, t, s.db, ws, ws_bytes, _stream())
+    return dict(dx=s.dx, dw=s.dw, db=s.db)
+
+
+def _own_gnorm(s):
+    B, T, A = _lib()
+    c = s.case
+    d, e, t, parts, groups = c["d"], _SIZE[c["dtype"]], T[c["dtype"]], c["parts"], c["channel_groups"]
+    ws, ws_bytes = _workspace(s, lambda: B.fg_group_norm_workspace_bytes(s.n, parts, d, groups))
+    B.fg_group_norm(s.x, d * e, t, s.order, s.offsets, s.n, parts, s.n, d, groups, s.w, s.b, _EPS, A[c["act"]], s.y, d * e, t, s.mean, s.rstd, ws, ws_bytes,
+                    _stream())
+    return dict(y=s.y, mean=s.mean, rstd=s.rstd)
+
+
+def _own_gnorm_bw(s):
+    B, T, A = _lib()
+    c = s.case
+    d, e, t, parts, groups = c["d"], _SIZE[c["dtype"]], T[c["dtype"]], c["parts"], c["channel_groups"]
+    ws, ws_bytes = _workspace(s, lambda: B.fg_group_norm_backward_workspace_bytes(s.n, parts, d, groups))
+    B.fg_group_norm_backward(s.dy, d * e, t, s.x, d * e, t, s.mean, s.rstd, s.w, s.b, A[c["act"]], s.order, s.offsets, s.n, parts, s.n, d, groups,
+                             s.dx, d * e, s.dw, s.db, ws, ws_bytes, _stream())
+    return dict(dx=s.dx, dw=s.dw, db=s.db)
+
+
+def _own_distill(s):
+    B, T, _ = _lib()
+    c = s.case
+    stride = c["d"] * _SIZE[c["dtype"]]
+    B.fg_distill_loss(s.h, stride, T[c["dtype"]], s.rows, None, s.k, s.n, c["d"], s.ids, s.top_idx, s.top_val, T["f16"], c["table"], c["k"], s.labels,
+                      c["temperature"], c["alpha"], s.weight, s.scale, s.loss, s.dh, stride, T[c["dtype"]], _stream())
+    return dict(loss=s.loss, dh=s.dh)
+
+
+_own = dict(gated=_own_gated, gated_bw=_own_gated_bw, gnorm=_own_gnorm, gnorm_bw=_own_gnorm_bw, distill=_own_distill)
+
+
+# ---- what a pass cannot do without ----
+
+def work(case):
+    k, op, e = _count(case), case["op"], _SIZE[case["dtype"]]
+    lists = 4 * k if k < case["n"] else 0
+    if op in ("gated", "gated_bw"):
+        a, b = case["d_in"], case["d_out"]
+        if op == "gated":
+            rows = k * (a * e + b * _SIZE[case["out"]] + (2 * b * e if case["keep"] else 0))
+            return dict(bytes=rows + 2 * a * b * e + 8 * b + lists + (4 * k if case["table"] else 0), flops=4 * k * a * b)
+        return dict(bytes=k * e * (2 * a + 3 * b) + 4 * a * b * e + 8 * b + lists, flops=8 * k * a * b)
+    if op in ("gnorm", "gnorm_bw"):
+        n, d = case["n"] * (0.9 if case["gathered"] else 1.0), case["d"]
+        small = 8 * (case["parts"] + 1) + 8 * case["parts"] * case["channel_groups"] + (4 * n if case["gathered"] else 0) + 8 * d
+        if op == "gnorm":
+            return dict(bytes=int(2 * n * d * e + small), flops=int(9 * n * d))
+        return dict(bytes=int(3 * n * d * e + small + 8 * d), flops=int(20 * n * d))
+    d, top = case["d"], case["k"]
+    return dict(bytes=2 * k * d * e + k * (6 * top + 16) + lists, flops=8 * k * d)
+
+
+# ---- the definitions in 64 bits ----
+
+def _act_exact(name, u):
+    """The activation and its slope."""
+    if name == "none":
+        return u, torch.ones_like(u)
+    if name == "relu":
+        return torch.relu(u), torch.heaviside(u, torch.zeros((), dtype=u.dtype, device=u.device))
+    if name == "gelu":
+        share = torch.special.ndtr(u)
+        return u * share, share + u * torch.exp(-u * u / 2) / math.sqrt(2 * math.pi)
+    g = torch.sigmoid(u)
+    return (u * g, g + u * g * (1 - g)) if name == "silu" else (g, g * (1 - g))
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    op = case["op"]
+    rows = torch.arange(s.n, device="cuda") if s.rows is None else s.rows.long()
+    place = lambda v, at=rows: torch.zeros(s.n, *v.shape[1:], dtype=torch.float64, device="cuda").index_copy_(0, at, v)
+    if op in ("gated", "gated_bw"):
+        w, b, act = s.w[0].double(), case["d_out"], case["act"]
+        if op == "gated":
+            z = torch.addmm(s.bias[0].double(), s.x[rows if s.ids is None else s.ids.long()[rows]].double(), w)
+            h = place(_act_exact(act, z[:, :b])[0] * z[:, b:])
+            return dict(h=h, z=place(z)) if case["keep"] else h
+        (f, slope), v, dh = _act_exact(act, s.z[rows, :b].double()), s.z[rows, b:].double(), s.dh[rows].double()
+        du, dv = dh * v * slope, dh * f
+        dx = torch.mm(du, w[:, :b].T.contiguous()) + torch.mm(dv, w[:, b:].T.contiguous())
+        xt = s.x[rows].double().T.contiguous()
+        return dict(dx=place(dx), dw=torch.hstack([torch.mm(xt, du), torch.mm(xt, dv)])[None], db=torch.hstack([du.sum(0), dv.sum(0)])[None])
+    if op in ("gnorm", "gnorm_bw"):
+        at = s.offsets.tolist()
+        entries = torch.arange(s.n, device="cuda") if s.order is None else s.order.long()
+        y, mean, rstd = torch.zeros(s.n, case["d"], dtype=torch.float64, device="cuda"), torch.zeros_like(s.mean, dtype=torch.float64), torch.zeros_like(s.rstd, dtype=torch.float64)
+        if op == "gnorm_bw":
+            dw, db = torch.zeros_like(s.dw, dtype=torch.float64), torch.zeros_like(s.db, dtype=torch.float64)
+        split = (case["channel_groups"], case["d"] // case["channel_groups"])
+        w, b = s.w.double().view(split), s.b.double().view(split)
+        for g in range(case["parts"]):
+            pos = entries[at[g]:at[g + 1]]
+            if not len(pos):
+                rstd[g] = _EPS ** -0.5
+                continue
+            x = s.x[pos].double().view(-1, *split)
+            if op == "gnorm":
+                mean[g] = x.mean((0, 2))
+                rstd[g] = (x.var((0, 2), correction=0) + _EPS) ** -0.5
+                y[pos] = _act_exact(case["act"], (x - mean[g][:, None]) * rstd[g][:, None] * w + b)[0].flatten(1)
+                continue
+            r = s.rstd[g].double()[:, None]
+            xh = (x - s.mean[g].double()[:, None]) * r
+            t = s.dy[pos].double().view_as(xh) * _act_exact(case["act"], xh * w + b)[1]
+            dw += (t * xh).sum(0).flatten()
+            db += t.sum(0).flatten()
+            q = t * w
+            y[pos] = (r * (q - q.mean((0, 2))[:, None] - xh * (q * xh).mean((0, 2))[:, None])).flatten(1)
+        return dict(y=y, mean=mean, rstd=rstd) if op == "gnorm" else dict(dx=y, dw=dw, db=db)
+    T, alpha, ids = case["temperature"], case["alpha"], s.ids[rows].long()
+    z = s.h[rows].double()
+    soft, hard = torch.log_softmax(z / T, 1), torch.log_softmax(z, 1)
+    idx, y = s.top_idx[ids].long(), s.labels[rows].long()
+    p = torch.softmax(torch.where(idx < 0, -1e30, s.top_val[ids].double() / T), 1) * (idx >= 0)
+    taught, labelled = p.sum(1) > 0, y >= 0
+    kl = (torch.special.xlogy(p, p) - p * soft.gather(1, idx.clamp(min=0))).sum(1)
+    loss = alpha * T * T * kl - (1 - alpha) * labelled * hard.gather(1, y.clamp(min=0)[:, None])[:, 0]
+    weight = s.weight[rows].double()
+    P = torch.zeros_like(z).scatter_add_(1, idx.clamp(min=0), p)
+    Y = torch.zeros_like(z).scatter_(1, y.clamp(min=0)[:, None], labelled.double()[:, None])
+    grad = alpha * T * (soft.exp() * taught[:, None] - P) + (1 - alpha) * (hard.exp() * labelled[:, None] - Y)
+    return dict(loss=place(weight * loss), dh=place(grad * (s.scale * weight)[:, None]))
