@@ -926,6 +926,121 @@ fg_status_t fg_quantize_rows(const void* x, int64_t x_stride, fg_dtype_t dtype, 
                              void* stream);
 
 /*
+ * ---- A student's block: gated feed-forward layers, group norm, and the loss against a teacher's top logits ----
+ * For models that learn a trained graph model's answers and are served without the graph: rows of the feature table, a few dense blocks, classes.
+ * They work by position on listed rows or on groups of rows, as the calls above.
+ */
+typedef enum {
+    FG_ACT_NONE = 0,
+    FG_ACT_RELU = 1,
+    FG_ACT_SILU = 2,   /* u / (1 + e^-u) */
+    FG_ACT_GELU = 3,   /* u * Phi(u), Phi the normal distribution function */
+    FG_ACT_SIGMOID = 4 /* 1 / (1 + e^-u) */
+} fg_act_t;
+
+/*
+ * Gated feed-forward layer with weights per group: two projections of a row, one of them activated, multiplied with each other.
+ *   z[r, :] = x[s, :] . W[g] + bias[g, :]                   2 * d_out values: u, the gate's, then v; r, g and s as in fg_linear_grouped
+ *   h_out[r, :] = act(u) * v
+ *   W                                   [n_groups x d_in x 2*d_out] row-major, the type of x: a row holds the gate's d_out weights, then the others
+ *   bias [n_groups x 2*d_out]           float, or NULL
+ *   h_out, out_dtype                    n_out rows of d_out values by position, `dtype` or FG_F32
+ *   z_out                               n_out rows of 2 * d_out values of `dtype` by position, which the gradients need; NULL: not wanted
+ * All else as in fg_linear_grouped without 8-bit rows: types FG_F32, FG_F16 and FG_BF16, products and sums (h is formed from the unrounded z and
+ * rounded once), limits (2 * d_out up to FG_MAX_GROUPED_DIM), alignment, entries that are skipped.
+ */
+fg_status_t fg_gated_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
+                                    const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                                    int32_t d_out, const void* W, const float* bias, fg_act_t act, void* h_out, int64_t n_out, int64_t out_stride,
+                                    fg_dtype_t out_dtype, void* z_out, int64_t z_stride, void* stream);
+
+/*
+ * The gradients of fg_gated_linear_grouped:
+ *   dz[k, :] = (dh[r, :] * v * act'(u), dh[r, :] * act(u)),  (u, v) = z[r, :], r = order[k]      (ReLU's slope at 0 is 0)
+ *   dx[r, :] = dz[k, :] . W[g]^T                            (by position; with src_ids that of the row the position took)
+ *   dW[g] = sum over the group's k of x[s, :]^T . dz[k, :]  ([n_groups x d_in x 2*d_out]; zeros for a group without rows)
+ *   db[g, :] = sum over the group's k of dz[k, :]           ([n_groups x 2*d_out] float)
+ *   dh, dh_dtype                        n rows of d_out values by position, FG_F32 or `dtype`
+ *   z                                   n rows of 2 * d_out values of `dtype` by position: the forward call's z_out
+ *   dx, dx_dtype                        FG_F32 or `dtype`;  dw, dw_dtype: FG_F32 or `dtype`;  any of dx, dw and db may be NULL
+ * dz is formed in fp32 and, for 16-bit rows, rounded to `dtype` for the products (db sums the unrounded values), as in fg_linear_grouped_backward,
+ * whose sums these are: fp32 within a range of rows, fp64 across ranges, one rounding to dw_dtype; results do not depend on scheduling.
+ *   ws_dev, ws_bytes                    >= fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out), 16-byte aligned
+ * d_in * sizeof(dtype) and d_out * sizeof(dtype) are multiples of 16; arrays of values and their strides are 16-byte aligned.
+ */
+size_t fg_gated_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out);
+fg_status_t fg_gated_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
+                                             const void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, const void* z, int64_t z_stride, int64_t n,
+                                             const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                                             int32_t d_out, const void* W, fg_act_t act, void* dx, int64_t dx_stride, fg_dtype_t dx_dtype, void* dw_dev,
+                                             fg_dtype_t dw_dtype, float* db_dev, void* ws_dev, size_t ws_bytes, void* stream);
+
+/*
+ * Group norm with an activation, channels last: the values of a group's rows (a graph of a batch, a node type) in each of channel_groups
+ * equal blocks of adjacent columns are normalised together.
+ *   mean, rstd [g, j] = mean and 1 / sqrt(variance + eps) of x[r, c] over r = order[k], offsets[g] <= k < offsets[g + 1], c in block j
+ *   y[r, c] = act((x[r, c] - mean[g, j]) * rstd[g, j] * weight[c] + bias[c])
+ *   x, dtype                            n rows of d values by position, FG_F32, FG_F16 or FG_BF16;  y of `dtype` or FG_F32; y may be x
+ *   order_dev, offsets_dev, n_groups    as fg_group_rows leaves them (order NULL: position k itself); at most max_rows entries are taken, no position
+ *                                       twice, offsets ascend; up to FG_MAX_NORM_GROUPS groups
+ *   channel_groups                      divides d: 1 (all columns together) .. d (every column by itself)
+ *   weight, bias [d]                    float, or NULL: ones, zeros
+ *   mean_out, rstd_out [n_groups x channel_groups]   float, which the gradients need; NULL: not wanted
+ *   ws_dev, ws_bytes                    >= fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
+ * The variance is that of the values at hand (divided by their number). A group without rows has mean 0 and rstd 1 / sqrt(eps). Sums in fp64 of the
+ * distances from the group's first value of the block, so that a large level takes nothing from the variance; no atomics, results do not
+ * depend on scheduling. Entries with a position outside [0, n) are left out. d up to FG_MAX_NORM_DIM; pointers and strides aligned to the
+ * element.
+ */
+#define FG_MAX_NORM_GROUPS 1048576
+size_t fg_group_norm_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups);
+fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows,
+                          int32_t n_groups, int64_t n, int32_t d, int32_t channel_groups, const float* weight, const float* bias, float eps,
+                          fg_act_t act, void* y, int64_t y_stride, fg_dtype_t y_dtype, float* mean_out, float* rstd_out, void* ws_dev, size_t ws_bytes,
+                          void* stream);
+
+/*
+ * The gradients of fg_group_norm:
+ *   xh = (x[r, c] - mean[g, j]) * rstd[g, j],  t = dy[r, c] * act'(xh * weight[c] + bias[c])      (ReLU's slope at 0 is 0)
+ *   dx[r, c] = rstd[g, j] * (t * weight[c] - m1 - xh * m2),  m1, m2 = the means of t * weight and t * weight * xh over the group's rows and block j
+ *   dw[c] = sum over all groups' rows of t * xh,  db[c] = that of t      ([d] float; NULL: not wanted)
+ *   dy, dx, grad_dtype                  n rows of d values by position, FG_F32, FG_F16 or FG_BF16; dx may be dy
+ *   x, mean, rstd, ...                  as in the forward call (mean, rstd its mean_out, rstd_out)
+ *   ws_dev, ws_bytes                    >= fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
+ * Means in fp64; dw and db in fp32 within and fp64 across ranges of rows; results do not depend on scheduling.
+ */
+size_t fg_group_norm_backward_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups);
+fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* x, int64_t x_stride, fg_dtype_t dtype,
+                                   const float* mean, const float* rstd, const float* weight, const float* bias, fg_act_t act,
+                                   const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int64_t n, int32_t d,
+                                   int32_t channel_groups, void* dx, int64_t dx_stride, float* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes,
+                                   void* stream);
+
+/*
+ * Loss of a student against a teacher's stored top logits and against labels, and its gradient, for the rows listed (r = rows[k]; NULL: r = k):
+ *   p = softmax of top_val[v, j] / temperature over the k stored entries of node v = ids[r] (NULL: v = r) whose class top_idx[v, j] lies in [0, d)
+ *   q_T = softmax(h[r, :] / temperature), q = softmax(h[r, :])
+ *   loss[r] = weight[r] * (alpha * temperature^2 * sum_j p_j * (log p_j - log q_T[c_j]) - (1 - alpha) * log q[labels[r]])
+ *   dh[r, c] = grad_scale * weight[r] * (alpha * temperature * (q_T[c] - sum of the p_j with c_j = c) + (1 - alpha) * (q[c] - [c = labels[r]]))
+ *   h, dtype                            n rows of d logits by position, FG_F32, FG_F16 or FG_BF16
+ *   ids_dev [n]                         int32 node ids by position, or NULL
+ *   top_idx_dev [table_rows x k]        int32 classes, top_val_dev the same of FG_F32, FG_F16 or FG_BF16; k = 0: no teacher (both NULL); up to FG_MAX_TOP
+ *   labels_dev [n]                      int32 by position, or NULL: no labels
+ *   weight_dev [n]                      float by position, or NULL: ones
+ *   loss_out [n]                        float by position; NULL: not wanted
+ *   dh, dh_dtype                        n rows by position, `dtype` or FG_F32; NULL: not wanted; dh may be h (of one type)
+ * A row without a teacher (no entry with a class in [0, d) and a value above -infinity, a node outside [0, table_rows), alpha = 0) has no first term, one without a
+ * label in [0, d) (or with alpha = 1) no second; a row with neither has loss 0 and gradient 0 whatever its logits. A class that is stored twice has
+ * the sum of both. A logit of -infinity is a class that cannot be chosen: no gradient, an infinite loss if the teacher or the label has it.
+ * Exponentials and gradients in fp32, sums in fp64 across a row's lanes. pointers and strides aligned to the element, any d.
+ */
+#define FG_MAX_TOP 64
+fg_status_t fg_distill_loss(const void* h, int64_t h_stride, fg_dtype_t dtype, const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows,
+                            int64_t n, int32_t d, const int32_t* ids_dev, const int32_t* top_idx_dev, const void* top_val_dev, fg_dtype_t top_dtype,
+                            int64_t table_rows, int32_t k, const int32_t* labels_dev, float temperature, float alpha, const float* weight_dev,
+                            float grad_scale, float* loss_out, void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, void* stream);
+
+/*
  * ---- One iteration in one call ----
  * fg_path_run queues the launches of one iteration on call->stream (and P->side) in the order a training loop makes the calls above:
  * the row copy that is still due, top-down pass, fetch, loader, layers, loss and backward pass, weight gradients, cache update. The

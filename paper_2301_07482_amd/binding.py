@@ -17,6 +17,8 @@ FG_TABLE_HBM_STREAMED, FG_TABLE_HOST_MAPPED, FG_TABLE_HBM_REUSED = 0, 1, 2
 DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2, FG_E4M3: 1}
 _TENSOR_DTYPE = {"torch.float32": FG_F32, "torch.float16": FG_F16, "torch.bfloat16": FG_BF16}
 FG_MAX_GROUPS, FG_MAX_GROUPED_ROWS, FG_MAX_GROUPED_DIM, FG_MAX_NORM_DIM = 1024, 1 << 29, 65536, 16384
+FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU, FG_ACT_SIGMOID = range(5)
+FG_MAX_NORM_GROUPS, FG_MAX_TOP = 1 << 20, 64
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2301_07482_amd.build` (needs hipcc); "
@@ -99,6 +101,16 @@ SIGNATURES = {
     "fg_residual_norm_backward": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _p, _i64, _p, _p, _i64, _i64, _i32, _f, C.c_uint64, _p, _i64, _p,
                                          _i64, _p, _p, _sz, _p]),
     "fg_quantize_rows": (_i32, [_p, _i64, _i32, _i64, _i32, _p, _i64, _p, _p]),
+    "fg_gated_linear_grouped": (_i32, [_p, _i64, _i64, _i32, _p, _p, _p, _i64, _i32, _i32, _i32, _p, _p, _i32, _p, _i64, _i64, _i32, _p, _i64, _p]),
+    "fg_gated_linear_grouped_backward_workspace_bytes": (_sz, [_i32, _i64, _i32, _i32, _i32]),
+    "fg_gated_linear_grouped_backward": (_i32, [_p, _i64, _i64, _i32, _p, _p, _i64, _i32, _p, _i64, _i64, _p, _p, _i64, _i32, _i32, _i32, _p, _i32, _p,
+                                                _i64, _i32, _p, _i32, _p, _p, _sz, _p]),
+    "fg_group_norm_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "fg_group_norm": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i32, _i64, _i32, _i32, _p, _p, _f, _i32, _p, _i64, _i32, _p, _p, _p, _sz, _p]),
+    "fg_group_norm_backward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
+    "fg_group_norm_backward": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _p, _p, _i32, _p, _p, _i64, _i32, _i64, _i32, _i32, _p, _i64, _p, _p, _p,
+                                      _sz, _p]),
+    "fg_distill_loss": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i64, _i32, _p, _p, _p, _i32, _i64, _i32, _p, _f, _f, _p, _f, _p, _p, _i64, _i32, _p]),
 }
 
 
@@ -560,6 +572,51 @@ def fg_residual_norm_backward(dy, dy_stride, grad_dtype, sum_, sum_stride, sum_d
 
 def fg_quantize_rows(x, x_stride, dtype, n_rows, d, q, q_stride, scale, stream=None):
     _check(_lib.fg_quantize_rows(ptr(x), x_stride, dtype, n_rows, d, ptr(q), q_stride, ptr(scale), stream))
+
+
+def fg_gated_linear_grouped(x, x_rows, x_stride, dtype, src_ids, order, offsets, max_rows, n_groups, d_in, d_out, W, bias, act, h_out, n_out, out_stride,
+                            out_dtype, z_out, z_stride, stream=None):
+    _check(_lib.fg_gated_linear_grouped(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W),
+                                        ptr(bias), act, ptr(h_out), n_out, out_stride, out_dtype, ptr(z_out), z_stride, stream))
+
+
+def fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out):
+    return int(_lib.fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out))
+
+
+def fg_gated_linear_grouped_backward(x, x_rows, x_stride, dtype, src_ids, dh, dh_stride, dh_dtype, z, z_stride, n, order, offsets, max_rows, n_groups, d_in,
+                                     d_out, W, act, dx, dx_stride, dx_dtype, dw, dw_dtype, db, ws, ws_bytes, stream=None):
+    _check(_lib.fg_gated_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(z), z_stride, n,
+                                                 ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), act, ptr(dx), dx_stride, dx_dtype,
+                                                 ptr(dw), dw_dtype, ptr(db), ptr(ws), ws_bytes, stream))
+
+
+def fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups):
+    return int(_lib.fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups))
+
+
+def fg_group_norm(x, x_stride, dtype, order, offsets, max_rows, n_groups, n, d, channel_groups, weight, bias, eps, act, y, y_stride, y_dtype, mean_out,
+                  rstd_out, ws, ws_bytes, stream=None):
+    _check(_lib.fg_group_norm(ptr(x), x_stride, dtype, ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(weight), ptr(bias), eps,
+                              act, ptr(y), y_stride, y_dtype, ptr(mean_out), ptr(rstd_out), ptr(ws), ws_bytes, stream))
+
+
+def fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups):
+    return int(_lib.fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups))
+
+
+def fg_group_norm_backward(dy, dy_stride, grad_dtype, x, x_stride, dtype, mean, rstd, weight, bias, act, order, offsets, max_rows, n_groups, n, d,
+                           channel_groups, dx, dx_stride, dw, db, ws, ws_bytes, stream=None):
+    _check(_lib.fg_group_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(x), x_stride, dtype, ptr(mean), ptr(rstd), ptr(weight), ptr(bias), act,
+                                       ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(dx), dx_stride, ptr(dw), ptr(db),
+                                       ptr(ws), ws_bytes, stream))
+
+
+def fg_distill_loss(h, h_stride, dtype, rows, n_rows, max_rows, n, d, ids, top_idx, top_val, top_dtype, table_rows, k, labels, temperature, alpha, weight,
+                    grad_scale, loss_out, dh, dh_stride, dh_dtype, stream=None):
+    _check(_lib.fg_distill_loss(ptr(h), h_stride, dtype, ptr(rows), ptr(n_rows), max_rows, n, d, ptr(ids), ptr(top_idx), ptr(top_val), top_dtype,
+                                table_rows, k, ptr(labels), temperature, alpha, ptr(weight), grad_scale, ptr(loss_out), ptr(dh), dh_stride, dh_dtype,
+                                stream))
 
 
 _POINTER_FIELDS = {}

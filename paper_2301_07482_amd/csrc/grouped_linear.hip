@@ -1,9 +1,10 @@
-// fg_linear_grouped and its gradients: the dense update with a weight matrix per group of rows.
+// fg_linear_grouped, fg_gated_linear_grouped and their gradients: dense updates with a weight matrix per group of rows.
 //
 // The rows of a group lie behind each other in `order`; how many there are is known on the device only. The grid is sized for the
 // bound (every group may leave one tile partly filled), and a workgroup finds its group and its rows from the offsets.
 #include <type_traits>
 
+#include "activation.h"
 #include "row_types.h"
 #include "scan.h"
 
@@ -61,7 +62,13 @@ struct GlArgs {
     const float *x_scale, *w_scale, *bias;
     const int32_t* src_ids;
     char* out;
-    float *dw, *db;
+    char* dw;
+    float* db;
+    int dw_type;
+    // gated layers: the two projections by position, what activates the first (N and d_out are those of both together)
+    char* z;
+    int64_t z_stride;
+    int act;
     // the matrix core kernels: out[r, 0:N] = a[., 0:K] . B, K and N whichever way round the call has them
     const char* a;
     int64_t a_stride;
@@ -204,7 +211,9 @@ __device__ __forceinline__ float scaled(float v, float a, float b) {
 // max(v, 0), a NaN stays one
 __device__ __forceinline__ float relu_of(float v) { return __builtin_elementwise_maximum(v, 0.f); }
 
-template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN>
+// GATED: a tile's columns are BN / 2 of the gate's and the same ones of the other projection, 32 of each in turn, so that a wavefront has both of an
+// output value in the same registers of two blocks; the epilogue activates, multiplies and writes the product.
+template <int T, int BM, int BN, int WAVES_M, int WAVES_N, bool B_KN, bool GATED = false>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int E = T == FG_E4M3 ? 1 : T == FG_F32 ? 4 : 2, BK = GL_STEP / E;
@@ -214,6 +223,7 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     constexpr int PARTS = T == FG_E4M3 || T == FG_F32 ? 2 : 1;                                          // 16-byte registers of it
     constexpr int B_ROW = BN * E, B_ROW_PIECES = B_ROW / 16;                      // B_KN: bytes of a row of k
     static_assert(!B_KN || T != FG_E4M3, "8-bit weights lie along K");
+    static_assert(!GATED || (B_KN && NB == 2), "gate and projection side by side in a wavefront");
     static_assert(A_LOADS * GL_ROWS * WAVES == BM && B_LOADS * GL_ROWS * WAVES == BN, "whole loads");
     // LDS: two steps' operands; the epilogue's blocks; what belongs to a tile, for the current one and the next; the offsets of the groups
     extern __shared__ __attribute__((aligned(16))) char gl_lds[];
@@ -242,17 +252,25 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         F.g = __builtin_amdgcn_readfirstlane(g);
         F.k0 = __builtin_amdgcn_readfirstlane((int)k0);
         F.k1 = __builtin_amdgcn_readfirstlane((int)k1);
-        F.n0 = (j % A.tiles_n) * BN;
+        F.n0 = (j % A.tiles_n) * (GATED ? BN / 2 : BN);
         return __builtin_amdgcn_readfirstlane(there);
+    };
+    // column of the weights of a tile's column c, `none` where there is none
+    auto column = [&](const Tile& F, int c, int none) -> int {
+        if constexpr (GATED) {
+            const int o = F.n0 + (c >> 6) * 32 + (c & 31);
+            return o < N / 2 ? o + (c & 32 ? N / 2 : 0) : none;
+        }
+        return F.n0 + c < N ? F.n0 + c : none;
     };
     // What belongs to a tile comes in three reads that depend on each other, a value to a thread: entry, row, scale of the row
     static_assert(THREADS >= BM && THREADS >= BN, "a thread for every row and column");
     int32_t e_pos = -1, e_src = -1;
     float e_scale = 0.f, e_bias = 0.f, e_w_scale = 0.f;
     auto fetch_entry = [&](const Tile& F) {
-        const int k = F.k0 + t, c = F.n0 + t;
+        const int k = F.k0 + t, c = column(F, t, -1);
         e_pos = t < BM && k < F.k1 ? (A.G.order ? A.G.order[k] : k) : -1;
-        if (t < BN && c < N) {
+        if (t < BN && c >= 0) {
             if (A.bias) e_bias = A.bias[(int64_t)F.g * N + c];
             if constexpr (T == FG_E4M3) e_w_scale = A.w_scale[(int64_t)F.g * N + c];
         }
@@ -309,8 +327,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         for (int i = 0; i < B_LOADS; ++i) {
             if constexpr (B_KN) {
                 const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
-                const int c = F.n0 + (T == FG_F32 ? (((slot >> 3) ^ b_window(row)) * 8 + (slot & 7)) * 4 : (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8);
-                pb[i] = (unsigned int)(row * N + (c < N ? c : 0)) * E;
+                const int c = T == FG_F32 ? (((slot >> 3) ^ b_window(row)) * 8 + (slot & 7)) * 4 : (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
+                pb[i] = (unsigned int)(row * N + column(F, c, 0)) * E;
             } else {
                 const int c = F.n0 + a_row + GL_ROWS * WAVES * i;
                 pb[i] = (unsigned int)(c < N ? c - F.n0 : 0) * K * E + a_piece * 16;
@@ -409,12 +427,20 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         }
     };
     // The stores of a tile are younger than the next one's first two steps' loads: those are waited for with the stores left on their way
-    constexpr int STORES = MB * NB * 2;
-    static_assert(LOADS + 2 * STORES < 64, "as many as can be counted");
-    int stores = 0;      // 0, STORES or 2 * STORES
+    // (gated: STORES for a block of 16-bit values in each row of blocks, up to six of them)
+    constexpr int STORES = GATED ? MB * 2 : MB * NB * 2;
+    static_assert(LOADS + (GATED ? T == FG_F32 ? 6 : 4 : 2) * STORES < 64, "as many as can be counted");
+    int stores = 0;      // a multiple of STORES
     auto arrived_first = [&](auto loads) {
         constexpr int N = decltype(loads)::value;
-        if (stores == 0)
+        if (GATED && stores > 2 * STORES) {
+            if (T == FG_F32)
+                arrived<N + 6 * STORES>();
+            else if (stores == 3 * STORES)
+                arrived<N + 3 * STORES>();
+            else
+                arrived<N + 4 * STORES>();
+        } else if (stores == 0)
             arrived<N>();
         else if (stores == STORES)
             arrived<N + STORES>();
@@ -541,6 +567,65 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
         }
     };
 
+    // a block of 32 x 32 values to 32 columns from `c0` of the rows of block row mb
+    auto write_block = [&](const TileData& D, int mb, const gl_f32x16& v, int type, char* out, int64_t stride, int c0, int columns) {
+        int lane = t & 63;
+        asm volatile("" : "+v"(lane));
+        const int l32 = lane & 31, half = lane >> 5;
+        char* const sink = (char*)gl_sink + lane * 16;
+        char* const blk = blocks + wave * EP_BLOCK;
+        asm volatile("" ::: "memory");      // (as in `write`)
+        if (type == FG_F32) {
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                if ((l32 >> 4) == part)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *(fg_u32x4*)(blk + (l32 & 15) * 128 + (((2 * q + half) ^ ((l32 >> 1) & 7)) << 4)) =
+                            fg_u32x4{__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const int row = p * 8 + lane / 8, piece = lane % 8, c = c0 + piece * 4;
+                    const fg_u32x4 w = *(const fg_u32x4*)(blk + row * 128 + ((piece ^ ((row >> 1) & 7)) << 4));
+                    const int32_t r = c < columns ? D.pos[wm + mb * 32 + part * 16 + row] : -1;
+                    store_16(r >= 0 ? out + (int64_t)r * stride + (int64_t)c * 4 : sink, w);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float f[4] = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                *(fg_u32x2*)(blk + l32 * 64 + ((q ^ ((l32 >> 2) & 3)) << 4) + half * 8) = type == FG_BF16 ? fg_to_words<FG_BF16>(f) : fg_to_words<FG_F16>(f);
+            }
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                const int row = p * 16 + lane / 4, piece = lane % 4, c = c0 + piece * 8;
+                const fg_u32x4 w = *(const fg_u32x4*)(blk + row * 64 + ((piece ^ ((row >> 2) & 3)) << 4));
+                const int32_t r = c < columns ? D.pos[wm + mb * 32 + row] : -1;
+                store_16(r >= 0 ? out + (int64_t)r * stride + (int64_t)c * 2 : sink, w);
+            }
+        }
+    };
+    auto write_gated = [&](const Tile& F, const TileData& D) {
+        const int c0 = F.n0 + wn / 2, columns = N / 2;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) {
+            if constexpr (T == FG_F32)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[mb][nb][e] += rest[mb][nb][e];
+            if (A.z)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) write_block(D, mb, acc[mb][nb], T, A.z + (int64_t)nb * columns * E, A.z_stride, c0, columns);
+            fg_with_act(A.act, [&](auto act) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[mb][0][e] = fg_act<decltype(act)::value>(acc[mb][0][e]) * acc[mb][NB - 1][e];
+            });
+            write_block(D, mb, acc[mb][0], A.out_type, A.out, A.out_stride, c0, columns);
+        }
+    };
+
     begin(cur, data[0]);
     load_step(0);
     if (steps > 1) load_step(1);
@@ -582,23 +667,27 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             load_step(0);
             if (steps > 1) load_step(1);
         }
-        write(cur, data[which]);
+        if constexpr (GATED)
+            write_gated(cur, data[which]);
+        else
+            write(cur, data[which]);
         if (!more) break;
         stores = A.out_type == FG_F32 ? 2 * STORES : STORES;
+        if (GATED && A.z) stores += (T == FG_F32 ? 4 : 2) * STORES;
         cur = next;
         j += j_step;
     }
 }
 
-template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN>
+template <int T, int BM, int BN, int WM, int WN, int PER_CU, bool B_KN, bool GATED = false>
 fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
-    A.tiles_n = (int)fg_ceil_div(A.N, BN);
+    A.tiles_n = (int)(GATED ? fg_ceil_div(A.N / 2, BN / 2) : fg_ceil_div(A.N, BN));
     const int64_t rows = A.G.max_rows / BM + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
     const int64_t tiles = fg_ceil_div(rows, 8) * 8 * A.tiles_n;
     // (a workgroup's number of a tile is one of its XCD's, and a step beyond: (2^23 + 2^10) rows of tiles x 2^10 / 8 fit 31 bits)
     static_assert((FG_MAX_GROUPED_ROWS / 64 + FG_MAX_GROUPS + 8) * (int64_t)(FG_MAX_GROUPED_DIM / 64) / 8 + 256 * 4 < INT32_MAX, "tiles of an XCD fit an int");
     const int64_t at_once = 256 * PER_CU;
-    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
+    hipLaunchKernelGGL((grouped_tile_kernel<T, BM, BN, WM, WN, B_KN, GATED>), dim3((unsigned)(tiles < at_once ? tiles : at_once)), dim3(64 * WM * WN),
                        gl_lds_bytes(BM, BN, WM * WN, T == FG_E4M3, A.G.n_groups), st, A);
     FG_LAUNCH_CHECK("grouped_tile_kernel");
     return FG_OK;
@@ -613,13 +702,14 @@ fg_status_t tile_launch(GlArgs& A, hipStream_t st) {
 //                   77 rows a group bf16 37 | 73, fp32 112 | 156, 8 bits 62 | 65; 64 rows a group 43 | 53, 134 | 115, 72 | 49
 // No 256 x 256 tile for fp32, whose two sums do not fit the registers. (PER_CU: of four workgroups of the 64 x 64 tile LDS holds three, and of two
 // of the 128 x 128 tile in 8 bits one above 767 groups; the others start as those end.)
-template <int T, bool B_KN>
+template <int T, bool B_KN, bool GATED = false>
 fg_status_t tile_product(GlArgs& A, hipStream_t st) {
     const int64_t large = (A.G.max_rows / 256) * fg_ceil_div(A.N, 256), groups = A.G.n_groups;
     if constexpr (T != FG_F32)
-        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN>(A, st);
+        if (large >= 256 && A.N > 128 && A.G.max_rows > 128 * groups) return tile_launch<T, 256, 256, 2, 4, 1, B_KN, GATED>(A, st);
     const int64_t mid = (A.G.max_rows / 128) * fg_ceil_div(A.N, 128);
-    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN>(A, st);
+    if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN, GATED>(A, st);
+    if constexpr (GATED) return tile_launch<T, 64, 64, 2, 1, 4, B_KN, GATED>(A, st);
     return tile_launch<T, 64, 64, 2, 2, 4, B_KN>(A, st);
 }
 
@@ -707,6 +797,92 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dz_kernel(GlArgs A) {
     }
 }
 
+// dz of a gated layer, both halves of a row, with their column sums. D: the type of dh
+template <int T, int D>
+__global__ __launch_bounds__(GZ_THREADS) void grouped_gated_dz_kernel(GlArgs A) {
+    constexpr int E = T == FG_F32 ? 4 : 2, DE = D == FG_F32 ? 4 : 2;
+    __shared__ int32_t pos[GZ_ROWS];
+    __shared__ float sums[GZ_THREADS * 16];
+    int g;
+    int64_t k0, k1;
+    if (!find_tile(A.G, blockIdx.x, GZ_ROWS, g, k0, k1)) return;
+    const int t = threadIdx.x, d = A.d_out / 2;
+    if (t < GZ_ROWS) {
+        int32_t s;
+        entry(A, k0 + t, k1, pos[t], s);
+    }
+    __syncthreads();
+    // as in grouped_dz_kernel
+    const int first = (int)blockIdx.y * (GZ_COLUMNS / 8), rows = (int)(k1 - k0);
+    const int pieces = (d + 7) / 8 - first < GZ_COLUMNS / 8 ? (d + 7) / 8 - first : GZ_COLUMNS / 8;
+    int side = GZ_THREADS / (GZ_COLUMNS / 8);
+    while (side * 2 * pieces <= GZ_THREADS) side *= 2;
+    const int width = GZ_THREADS / side, p = t % width, c = (first + p) * 8, left = d - c;
+    float sum[2][8] = {};
+    if (p < pieces) {
+        constexpr int AHEAD = 2;      // rows whose reads are on their way together
+        for (int m0 = t / width; m0 < rows; m0 += AHEAD * side) {
+            fg_piece<D> ph[AHEAD];
+            fg_piece<T> pu[AHEAD], pv[AHEAD];
+            int32_t r[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = m0 + u * side;
+                r[u] = m < rows ? pos[m] : -1;
+                if (r[u] >= 0) {
+                    const char* z = A.z + r[u] * A.z_stride + (int64_t)c * E;
+                    ph[u] = fg_load_piece<D>(A.dh + r[u] * A.dh_stride + (int64_t)c * DE, left);
+                    pu[u] = fg_load_piece<T>(z, left);
+                    pv[u] = fg_load_piece<T>(z + (int64_t)d * E, left);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int m = m0 + u * side;
+                float du[8] = {}, dv[8] = {};
+                if (r[u] >= 0) {
+                    float a[8], v[8], dh[8];
+                    fg_piece_values<T>(pu[u], a);
+                    fg_piece_values<T>(pv[u], v);
+                    fg_piece_values<D>(ph[u], dh);
+                    fg_with_act(A.act, [&](auto act) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            float f, slope;
+                            fg_act_slope<decltype(act)::value>(a[e], f, slope);
+                            du[e] = dh[e] * v[e] * slope;
+                            dv[e] = dh[e] * f;
+                        }
+                    });
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        sum[0][e] += du[e];
+                        sum[1][e] += dv[e];
+                    }
+                }
+                if (A.dz && m < rows) {
+                    char* to = A.dz + (k0 + m) * A.dz_stride + (int64_t)c * E;
+                    fg_store_piece<T>(to, du, left);
+                    fg_store_piece<T>(to + (int64_t)d * E, dv, left);
+                }
+            }
+        }
+    }
+    if (!A.db_part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        sums[t * 8 + e] = sum[0][e];
+        sums[GZ_THREADS * 8 + t * 8 + e] = sum[1][e];
+    }
+    __syncthreads();
+    for (int i = t; i < 2 * width * 8; i += GZ_THREADS) {
+        const int half = i / (width * 8), at = i % (width * 8);
+        float v = 0.f;
+        for (int q = 0; q < side; ++q) v += sums[half * GZ_THREADS * 8 + q * width * 8 + at];
+        if (first * 8 + at < d && at < GZ_COLUMNS) A.db_part[(int64_t)blockIdx.x * A.d_out + half * d + first * 8 + at] = v;
+    }
+}
+
 // db[g, c] = sum over the group's tiles, in fp64; DB_COLUMNS columns a workgroup, DB_RUNS runs of tiles side by side
 constexpr int DB_COLUMNS = 8, DB_RUNS = GZ_THREADS / DB_COLUMNS;
 __device__ __forceinline__ void sum_db(const GlArgs& A, int block, double* red) {
@@ -775,6 +951,11 @@ struct RangeWalk {
         return true;
     }
 };
+
+// a value in 16 bits, to nearest even
+__device__ __forceinline__ unsigned short narrow(int type, float v) {
+    return type == FG_BF16 ? __builtin_bit_cast(unsigned short, (__bf16)v) : __builtin_bit_cast(unsigned short, (_Float16)v);
+}
 
 template <int T, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(GlArgs A) {
@@ -903,7 +1084,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
         }
         const bool whole = W.first == 0 && W.last == W.steps_g;
         float* to_part = A.dw_part + ((int64_t)(2 * range + (W.at == range * S.per ? 0 : 1)) * tiles + tile) * BM * BN;
-        float* to_dw = A.dw + (int64_t)W.g * A.d_in * A.d_out;
+        float* to_dw = (float*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
+        unsigned short* to_narrow = (unsigned short*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
         int m_first = wm + 4 * half, c_first = wn + l32;      // (addresses are formed here: hoisted out of the loops they take registers those have not got)
         asm volatile("" : "+v"(m_first), "+v"(c_first));
 #pragma unroll
@@ -916,8 +1098,13 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
                     const int c = c_first + nb * 32;
                     if (!whole)
                         to_part[m * BN + c] = acc[mb][nb][i];
-                    else if (m0 + m < A.d_in && n0 + c < A.d_out)
-                        to_dw[(int64_t)(m0 + m) * A.d_out + n0 + c] = acc[mb][nb][i];
+                    else if (m0 + m < A.d_in && n0 + c < A.d_out) {
+                        const int64_t at = (int64_t)(m0 + m) * A.d_out + n0 + c;
+                        if (A.dw_type == FG_F32)
+                            to_dw[at] = acc[mb][nb][i];
+                        else
+                            to_narrow[at] = narrow(T, acc[mb][nb][i]);
+                    }
                 }
             }
         __syncthreads();      // the list and the buffers may be filled again
@@ -965,8 +1152,14 @@ __global__ __launch_bounds__(GZ_THREADS) void grouped_dw_sum_kernel(GlArgs A) {
 #pragma unroll
                     for (int f = 0; f < 4; ++f) s[f] += red[q][at + f];
         }
-        if (run == 0 && m < A.d_in && c < A.d_out)      // d_out is a multiple of 4
-            *(float4*)(A.dw + ((int64_t)g * A.d_in + m) * A.d_out + c) = float4{(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+        if (run == 0 && m < A.d_in && c < A.d_out) {      // d_out is a multiple of 4
+            const int64_t at = ((int64_t)g * A.d_in + m) * A.d_out + c;
+            const float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+            if (A.dw_type == FG_F32)
+                *(float4*)((float*)A.dw + at) = float4{v[0], v[1], v[2], v[3]};
+            else
+                *(fg_u32x2*)((unsigned short*)A.dw + at) = A.dw_type == FG_BF16 ? fg_to_words<FG_BF16>(v) : fg_to_words<FG_F16>(v);
+        }
     }
 }
 
@@ -1095,7 +1288,7 @@ __global__ __launch_bounds__(GF_THREADS, 2) void grouped_f32_dw_kernel(GlArgs A)
         }
         const bool whole = W.first == 0 && W.last == W.steps_g;
         float* to_part = A.dw_part + ((int64_t)(2 * range + (W.at == range * S.per ? 0 : 1)) * tiles + tile) * TILE * TILE;
-        float* to_dw = A.dw + (int64_t)W.g * A.d_in * A.d_out;
+        float* to_dw = (float*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
         int m_first = wm + 4 * (lane >> 5), n_first = wn + (lane & 31);      // (formed here, as above)
         asm volatile("" : "+v"(m_first), "+v"(n_first));
 #pragma unroll
@@ -1176,6 +1369,15 @@ fg_status_t check_groups(const char* who, const int32_t* order_dev, const int64_
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: offsets must not be NULL, and order and offsets aligned to their elements", who);
     return FG_OK;
 }
+fg_status_t check_gated(const char* who, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out,
+                        fg_dtype_t dtype, int64_t x_rows, int64_t n, fg_act_t act) {
+    if (!fg_dtype_size(dtype)) FG_FAIL(FG_ERR_DTYPE, "%s: element type %d is not one of fp32, fp16 and bf16", who, (int)dtype);
+    const int step = 16 / fg_dtype_size(dtype);
+    if (d_out <= 0 || d_out % step || d_out > FG_MAX_GROUPED_DIM / 2)
+        FG_FAIL(FG_ERR_SHAPE, "%s: d_out = %d must be a multiple of %d for this type, %d at most", who, d_out, step, FG_MAX_GROUPED_DIM / 2);
+    if (!fg_act_known(act)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: unknown activation %d", who, (int)act);
+    return check_groups(who, order_dev, offsets_dev, max_rows, n_groups, d_in, 2 * d_out, dtype, x_rows, n);
+}
 fg_status_t check_matrix(const char* who, const char* what, const void* p, int64_t stride, int64_t row_bytes) {
     if (!p) FG_FAIL(FG_ERR_INVALID_ARG, "%s: %s must not be NULL", who, what);
     if (stride < row_bytes) FG_FAIL(FG_ERR_SHAPE, "%s: the stride of %s is smaller than its row", who, what);
@@ -1195,6 +1397,10 @@ template <int T, int D, int H>
 void launch_dz(const GlArgs& A, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((grouped_dz_kernel<T, D, H>), grid, dim3(GZ_THREADS), 0, st, A);
 }
+template <int T, int D>
+void launch_gated_dz(const GlArgs& A, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((grouped_gated_dz_kernel<T, D>), grid, dim3(GZ_THREADS), 0, st, A);
+}
 template <int BM, int ROWS, int VALUES>
 void launch_sum(const GlArgs& A, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((grouped_dw_sum_kernel<BM, BM, ROWS, VALUES>), grid, dim3(GZ_THREADS), 0, st, A);
@@ -1204,7 +1410,7 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     constexpr int E = T == FG_F32 ? 4 : 2;
     const BwPlan P = bw_plan(A.G.max_rows, A.G.n_groups, A.d_in, A.d_out, E);
     char* ws = (char*)ws_dev;
-    const bool pack = A.h || A.dh_type != T || A.src_ids;      // otherwise dh, by position as x is, serves as it lies
+    const bool pack = A.z || A.h || A.dh_type != T || A.src_ids;      // otherwise dh, by position as x is, serves as it lies
     A.dz = work && pack && (A.out || A.dw) ? ws : nullptr;
     A.dz_stride = A.dz ? dz_row(A.d_out, E) : A.dh_stride;
     A.db_part = work && A.db ? (float*)(ws + P.dz_bytes) : nullptr;
@@ -1217,8 +1423,10 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
     const int64_t db_blocks = A.db ? A.G.n_groups * fg_ceil_div(A.d_out, DB_COLUMNS) : 0;
     if (sums + db_blocks >= FG_MAX_GRID) FG_FAIL(FG_ERR_SHAPE, "%s: too many groups and columns for one call", who);
     if (A.dz || A.db_part) {
-        const dim3 grid((unsigned)A.db_tiles, (unsigned)fg_ceil_div(A.d_out, GZ_COLUMNS));
-        if constexpr (T == FG_F32)
+        const dim3 grid((unsigned)A.db_tiles, (unsigned)fg_ceil_div(A.z ? A.d_out / 2 : A.d_out, GZ_COLUMNS));
+        if (A.z)
+            A.dh_type == T ? launch_gated_dz<T, T>(A, grid, st) : launch_gated_dz<T, FG_F32>(A, grid, st);
+        else if constexpr (T == FG_F32)
             launch_dz<T, T, T>(A, grid, st);
         else if (A.dh_type == T)
             A.h_type == FG_F32 ? launch_dz<T, T, FG_F32>(A, grid, st) : A.h_type == FG_F16 ? launch_dz<T, T, FG_F16>(A, grid, st) : launch_dz<T, T, FG_BF16>(A, grid, st);
@@ -1316,7 +1524,74 @@ extern "C" fg_status_t fg_linear_grouped_backward(const void* x, int64_t x_rows,
     A.G = {order_dev, offsets_dev, work ? max_rows : 0, n_groups};
     A.x = (const char*)x, A.W = (const char*)W, A.h = (const char*)h, A.dh = (const char*)dh, A.x_rows = x_rows, A.x_stride = x_stride, A.h_stride = h_stride;
     A.dh_stride = dh_stride, A.n = n, A.out_stride = dx_stride, A.dh_type = dh_dtype, A.h_type = h ? h_dtype : dtype, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = d_out;
-    A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = dw_dev, A.db = db_dev;
+    A.src_ids = src_ids_dev, A.out = (char*)dx, A.dw = (char*)dw_dev, A.dw_type = FG_F32, A.db = db_dev;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dtype == FG_F32) return backward<FG_F32>(who, A, work, st, ws_dev);
+    return dtype == FG_BF16 ? backward<FG_BF16>(who, A, work, st, ws_dev) : backward<FG_F16>(who, A, work, st, ws_dev);
+}
+
+extern "C" fg_status_t fg_gated_linear_grouped(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
+                                               const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                                               int32_t d_out, const void* W, const float* bias, fg_act_t act, void* h_out, int64_t n_out,
+                                               int64_t out_stride, fg_dtype_t out_dtype, void* z_out, int64_t z_stride, void* stream) {
+    const char* who = "fg_gated_linear_grouped";
+    FG_TRY(check_gated(who, order_dev, offsets_dev, max_rows, n_groups, d_in, d_out, dtype, x_rows, n_out, act));
+    const int e = fg_dtype_size(dtype);
+    if (out_dtype != dtype && out_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: h is of the type of x or fp32", who);
+    if (((uintptr_t)bias | (uintptr_t)src_ids_dev) & 3) FG_FAIL(FG_ERR_INVALID_ARG, "%s: bias and ids must be aligned to their elements", who);
+    if (max_rows > 0 && n_out > 0 && x_rows > 0) {
+        FG_TRY(check_matrix(who, "x", x, x_stride, (int64_t)d_in * e));
+        FG_TRY(check_matrix(who, "h_out", h_out, out_stride, (int64_t)d_out * fg_dtype_size(out_dtype)));
+        if (z_out) FG_TRY(check_matrix(who, "z_out", z_out, z_stride, (int64_t)2 * d_out * e));
+        FG_TRY(check_matrix(who, "W", W, 0, 0));
+    }
+    fg_clear_error();
+    if (max_rows == 0 || n_out == 0 || x_rows == 0) return FG_OK;
+    GlArgs A = {};
+    A.G = {order_dev, offsets_dev, max_rows, n_groups};
+    A.x = A.a = (const char*)x, A.x_rows = x_rows, A.x_stride = A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.W = (const char*)W, A.bias = bias, A.src_ids = src_ids_dev;
+    A.n = n_out, A.out = (char*)h_out, A.out_stride = out_stride, A.out_type = out_dtype, A.z = (char*)z_out, A.z_stride = z_stride, A.act = act;
+    A.d_in = A.K = d_in, A.d_out = A.N = 2 * d_out;
+    if (dtype == FG_BF16) return tile_product<FG_BF16, true, true>(A, (hipStream_t)stream);
+    if (dtype == FG_F16) return tile_product<FG_F16, true, true>(A, (hipStream_t)stream);
+    return tile_product<FG_F32, true, true>(A, (hipStream_t)stream);
+}
+
+extern "C" size_t fg_gated_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
+    if (d_out <= 0 || d_out > FG_MAX_GROUPED_DIM / 2) return 0;
+    return fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, 2 * d_out);
+}
+
+extern "C" fg_status_t fg_gated_linear_grouped_backward(const void* x, int64_t x_rows, int64_t x_stride, fg_dtype_t dtype, const int32_t* src_ids_dev,
+                                                        const void* dh, int64_t dh_stride, fg_dtype_t dh_dtype, const void* z, int64_t z_stride, int64_t n,
+                                                        const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int32_t d_in,
+                                                        int32_t d_out, const void* W, fg_act_t act, void* dx, int64_t dx_stride, fg_dtype_t dx_dtype,
+                                                        void* dw_dev, fg_dtype_t dw_dtype, float* db_dev, void* ws_dev, size_t ws_bytes, void* stream) {
+    const char* who = "fg_gated_linear_grouped_backward";
+    FG_TRY(check_gated(who, order_dev, offsets_dev, max_rows, n_groups, d_in, d_out, dtype, x_rows, n, act));
+    const int e = fg_dtype_size(dtype);
+    if (dh_dtype != dtype && dh_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dh is of the type of x or fp32", who);
+    if (dx && dx_dtype != dtype && dx_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dx is of the type of x or fp32", who);
+    if (dw_dev && dw_dtype != dtype && dw_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dw is of the type of x or fp32", who);
+    if (!dx && !dw_dev && !db_dev) FG_FAIL(FG_ERR_INVALID_ARG, "%s: none of dx, dw and db is wanted", who);
+    const bool work = max_rows > 0 && n > 0 && x_rows > 0;
+    if (work) {
+        FG_TRY(check_matrix(who, "dh", dh, dh_stride, (int64_t)d_out * fg_dtype_size(dh_dtype)));
+        FG_TRY(check_matrix(who, "z", z, z_stride, (int64_t)2 * d_out * e));
+        if (dw_dev) FG_TRY(check_matrix(who, "x", x, x_stride, (int64_t)d_in * e));
+        if (dx) FG_TRY(check_matrix(who, "dx", dx, dx_stride, (int64_t)d_in * fg_dtype_size(dx_dtype)));
+        if (dx) FG_TRY(check_matrix(who, "W", W, 0, 0));
+    }
+    if (((uintptr_t)dw_dev | (uintptr_t)db_dev) & 15 || ((uintptr_t)src_ids_dev & 3)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: dw and db must be 16-byte aligned", who);
+    const size_t need = fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out);
+    if (!ws_dev || ((uintptr_t)ws_dev & 15)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: the workspace must be 16-byte aligned device memory", who);
+    if (ws_bytes < need) FG_FAIL(FG_ERR_SHAPE, "%s: workspace of %zu bytes, %zu are needed", who, ws_bytes, need);
+    fg_clear_error();
+    GlArgs A = {};
+    A.G = {order_dev, offsets_dev, work ? max_rows : 0, n_groups};
+    A.x = (const char*)x, A.W = (const char*)W, A.dh = (const char*)dh, A.x_rows = x_rows, A.x_stride = x_stride, A.dh_stride = dh_stride, A.dh_type = dh_dtype;
+    A.z = (char*)z, A.z_stride = z_stride, A.act = act, A.n = n, A.out = (char*)dx, A.out_stride = dx_stride, A.out_type = dx_dtype, A.d_in = d_in, A.d_out = 2 * d_out;
+    A.src_ids = src_ids_dev, A.dw = (char*)dw_dev, A.dw_type = dw_dtype, A.db = db_dev;
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32) return backward<FG_F32>(who, A, work, st, ws_dev);
     return dtype == FG_BF16 ? backward<FG_BF16>(who, A, work, st, ws_dev) : backward<FG_F16>(who, A, work, st, ws_dev);

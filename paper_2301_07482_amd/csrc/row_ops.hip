@@ -5,6 +5,7 @@
 // its gradients, 65536 x 1024 bf16, 123 us and 8 for the sums of dw, 5.1. A row belongs to a power of two of lanes, up to a wavefront's 64, each
 // with pieces of eight adjacent values (16 bytes of a 16-bit type), and stays in registers between the sum over the row and the use
 // of it; a row of more than 2048 values belongs to all wavefronts of a workgroup, which meet in LDS.
+#include "row_list.h"
 #include "row_types.h"
 
 namespace {
@@ -36,22 +37,6 @@ DropArgs drop_args(float p, uint64_t key) {
     return D;
 }
 
-// rows listed
-struct RowList {
-    const int32_t* rows;
-    const int64_t* n_rows_dev;
-    int64_t max_rows, n, first;      // first: of this launch
-};
-__device__ __forceinline__ int64_t row_count(const RowList& L) {
-    const int64_t k = L.n_rows_dev ? *L.n_rows_dev : L.max_rows;
-    return k < 0 ? 0 : (k > L.max_rows ? L.max_rows : k);
-}
-__device__ __forceinline__ int64_t row_at(const RowList& L, int64_t k, int64_t count) {
-    if (k >= count) return -1;
-    const int64_t r = L.rows ? L.rows[k] : k;
-    return r < 0 || r >= L.n ? -1 : r;
-}
-
 template <int T>
 __global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, int64_t rows, const char* x, int64_t x_stride, char* out,
                                                               int64_t out_stride, int d, int pieces, DropArgs D) {
@@ -67,43 +52,6 @@ __global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, int64_t
     fg_piece_values<T>(fg_load_piece<T>(x + r * x_stride + (int64_t)c * E, d - c), f);
     if (D.threshold) drop_piece(D, fg_word64(D.base, (uint64_t)r), c, f);
     fg_store_piece<T>(out + r * out_stride + (int64_t)c * E, f, d - c);
-}
-
-// sum or maximum over the lanes of a row
-__device__ __forceinline__ double lanes_sum(double v, int lanes) {
-    for (int off = lanes >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
-__device__ __forceinline__ float lanes_max(float v, int lanes) {
-    for (int off = lanes >> 1; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
-}
-// the same over the wavefronts of a workgroup that share a row
-template <int WAVES>
-__device__ __forceinline__ double row_sum(double v, int lanes, double* lds) {
-    v = lanes_sum(v, lanes);
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += lds[w];
-    }
-    return v;
-}
-template <int WAVES>
-__device__ __forceinline__ float row_max(float v, int lanes, double* lds) {
-    v = lanes_max(v, lanes);
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = (float)lds[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, (float)lds[w]);
-    }
-    return v;
 }
 
 struct NormArgs {
@@ -398,25 +346,6 @@ void norm_bw_launch(const RowShape& s, const NormBwArgs& A, hipStream_t st) {
     else
         hipLaunchKernelGGL((residual_norm_backward_kernel<GT, ST, 8, 4>), dim3(grid), dim3(512), 0, st, A);
 }
-
-fg_status_t check_rows(const char* who, const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows, int64_t n, int32_t d) {
-    if (max_rows < 0 || max_rows > INT32_MAX || n < 0 || n > INT32_MAX) FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
-    if (d <= 0) FG_FAIL(FG_ERR_SHAPE, "%s: d = %d must be positive", who, d);
-    if (!rows_dev && max_rows > n) FG_FAIL(FG_ERR_SHAPE, "%s: max_rows = %lld without a list, but n = %lld rows", who, (long long)max_rows, (long long)n);
-    if (((uintptr_t)rows_dev & 3) || ((uintptr_t)n_rows_dev & 7)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: the list or its count is not aligned", who);
-    return FG_OK;
-}
-// one array of n rows: type, stride and alignment
-fg_status_t check_array(const char* who, const char* what, const void* p, int64_t stride, int element, int32_t d) {
-    if (stride < (int64_t)d * element) FG_FAIL(FG_ERR_SHAPE, "%s: the stride of %s is smaller than its row", who, what);
-    if (((uintptr_t)p | (uintptr_t)stride) & (uintptr_t)(element - 1)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: %s or its stride is not aligned to its element", who, what);
-    return FG_OK;
-}
-#define FG_TRY(expr)                     \
-    do {                                 \
-        const fg_status_t s_ = (expr);   \
-        if (s_ != FG_OK) return s_;      \
-    } while (0)
 
 }  // namespace
 
