@@ -989,8 +989,8 @@ fg_status_t fg_gated_linear_grouped_backward(const void* x, int64_t x_rows, int6
  *   ws_dev, ws_bytes                    >= fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
  * The variance is that of the values at hand (divided by their number). A group without rows has mean 0 and rstd 1 / sqrt(eps). Sums in fp64 of the
  * distances from the group's first value of the block, so that a large level takes nothing from the variance; no atomics, results do not
- * depend on scheduling. Entries with a position outside [0, n) are left out. d up to FG_MAX_NORM_DIM; pointers and strides aligned to the
- * element.
+ * depend on scheduling. Entries with a position outside [0, n) are left out. d from 8 up to FG_MAX_NORM_DIM; pointers and strides aligned to
+ * the element.
  */
 #define FG_MAX_NORM_GROUPS 1048576
 size_t fg_group_norm_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups);

@@ -3,7 +3,7 @@
 // The entries of all groups are a line that is cut into chunks of rows. A group of few rows belongs to the chunk it begins in and is done there:
 // one pass for the sums, one for the result, whose rows come from the caches. A group of many rows is split along the chunks' ends: every chunk leaves the
 // sums of its part, a second launch joins them, a third goes over the rows again. A workgroup takes a chunk and a tile of whole blocks of columns; a
-// thread has pieces of eight adjacent columns and every side-th row. Which chunk a group lies in is found from the offsets, on the device.
+// thread has pieces of eight adjacent columns (whole ones: the last of a tile overlaps the one before it) and every so many-th row. Which chunk a group lies in is found from the offsets, on the device.
 #include "activation.h"
 #include "row_list.h"
 #include "row_types.h"
@@ -12,13 +12,15 @@
 namespace {
 
 constexpr int GN_THREADS = 256, GN_WAVES = GN_THREADS / 64, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 1024, GN_FEW_VALUES = 65536, GN_MAX_PIECES = 8;
+constexpr int GN_PLACES = 768, GN_FEW_WORKGROUPS = 128, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
+constexpr int GN_AHEAD = 4, GN_AHEAD_BW = 2;      // rows whose reads are on their way together
 
 struct GnArgs {
     const int32_t* order;      // NULL: position k itself
     const int64_t* offsets;
-    int64_t max_rows, n, rows, long_rows;      // rows of a chunk; a group of more rows than long_rows is split
-    int n_groups, d, block, blocks, tile_blocks, width;      // columns of a block, blocks of a row, blocks of a tile, lanes of a row's tile
+    int64_t max_rows, n;
+    unsigned int rows, long_rows;      // rows of a chunk; a group of more rows than long_rows is split
+    int n_groups, d, block, blocks, width, pieces;      // columns of a block, blocks of a row, lanes of a row's tile and pieces of a lane
     const char *x, *dy;
     int64_t x_stride, dy_stride, out_stride;
     const float *weight, *bias;
@@ -29,55 +31,51 @@ struct GnArgs {
     double* part;            // [chunks][2][blocks][3]: the sums of a chunk's parts of a group that began before it, and of one that begins in it
     int32_t* info;           // [chunks][2]: those groups, -1: none
     float* joined;           // [chunks][blocks][2]: what the parts of the group that begins in the chunk come to
+    int join_there;          // ... has been left there by a launch of its own
+    int64_t chunks;
+    int joins;               // workgroups that join
     float* columns;          // [chunks][2][d]: sums for dw and db, or NULL
+    float *dw, *db;
 };
 
-__device__ __forceinline__ int64_t offset_of(const GnArgs& A, int g) {
+// entries are counted in 32 bits (a call has fewer than 2^31, a step beyond them fits)
+__device__ __forceinline__ unsigned int offset_of(const GnArgs& A, int g) {
     const int64_t o = A.offsets[g];
-    return o < 0 ? 0 : (o > A.max_rows ? A.max_rows : o);
+    return (unsigned int)(o < 0 ? 0 : (o > A.max_rows ? A.max_rows : o));
 }
-// the first group that begins at `target` or beyond (lanes of a wavefront together, 64 offsets at a time)
-__device__ __forceinline__ int first_from(const GnArgs& A, int64_t target) {
-    int lo = 0, hi = A.n_groups;
-    while (lo < hi) {
-        const int step = (hi - lo + 63) / 64;
-        const int64_t i = lo + (int64_t)fg_lane() * step;
-        const int before = __popcll(__ballot(i < hi && offset_of(A, i < hi ? (int)i : lo) < target));
-        if (before == 0) return lo;
-        const int64_t end = lo + (int64_t)before * step;
-        lo += (before - 1) * step + 1;
-        hi = end < hi ? (int)end : hi;
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// A group with no more than 62 others behind it that begin before `target`, and all groups before it do (lanes of a wavefront together)
+__device__ __forceinline__ int near(const GnArgs& A, unsigned int target) {
+    int lo = 0, hi = A.n_groups;      // the first that does not lies in [lo, hi]
+    while (hi - lo > 62) {
+        const int step = (hi - lo + 63) / 64, i = lo + fg_lane() * step;
+        const int before = uniform(__popcll(__ballot(i < hi && offset_of(A, i < hi ? i : lo) < target)));
+        const int end = lo + before * step;
+        lo += before ? (before - 1) * step + 1 : 0;
+        hi = before == 0 ? lo : (end < hi ? end : hi);
     }
-    return lo;
+    return lo > 0 ? lo - 1 : 0;
 }
 enum { GN_WHOLE, GN_GOES_ON, GN_BEGINS };
-// The parts of groups that belong to a chunk, in order, the same in all wavefronts.
+// The parts of groups that belong to a chunk, in order, the same in all wavefronts: of the group that began before it, if that is split, and of
+// those that begin in it.
 struct Walk {
     const GnArgs& A;
-    int64_t c0, c1, from, to;      // entries of the chunk; of the group that this lane looks at
-    int first, base;
-    unsigned long long mask;       // lanes whose groups are still to come
-    __device__ __forceinline__ Walk(const GnArgs& args, int64_t chunk) : A(args) {
+    unsigned int c0, c1, from, to;      // entries of the chunk; of the group that this lane looks at
+    int base;
+    unsigned long long mask;            // lanes whose groups are still to come
+    __device__ __forceinline__ Walk(const GnArgs& args, unsigned int chunk) : A(args) {
         c0 = chunk * A.rows;
         c1 = c0 + A.rows;
-        first = first_from(A, c0);
-        base = first - 64;
+        base = near(A, c0) - 64;
         mask = 0;
-        from = to = c0;
+        from = 0;
+        to = 0;
     }
     // The next part: group, first entry and end, which of the three. empty(group): by one lane of the first wavefront, for every group without entries that
     // lies here
     template <typename Empty>
-    __device__ __forceinline__ bool next(int& g, int64_t& k0, int64_t& k1, int& which, const Empty& empty) {
-        if (base == first - 64 && first > 0) {      // the group that began before the chunk
-            g = --first;
-            base = first - 63;
-            k0 = c0;
-            const int64_t begin = offset_of(A, g), end = offset_of(A, g + 1);
-            k1 = end < c1 ? end : c1;
-            which = GN_GOES_ON;
-            if (begin < c0 && end > c0 && end - begin > A.long_rows) return true;
-        }
+    __device__ __forceinline__ bool next(int& g, unsigned int& k0, unsigned int& k1, int& which, const Empty& empty) {
         while (!mask) {
             if (__ballot(from >= c1)) return false;
             base += 64;
@@ -90,20 +88,20 @@ struct Walk {
             }
             const bool here = from >= c0 && from < c1;
             if (here && to <= from && fg_wave() == 0) empty(i);
-            mask = __ballot(here && to > from);
+            mask = __ballot((here && to > from) || (from < c0 && to > c0 && to - from > A.long_rows));
         }
         const int l = __ffsll((long long)mask) - 1;
         mask &= mask - 1;
         g = base + l;
-        k0 = __shfl((long long)from, l, 64);
-        k1 = __shfl((long long)to, l, 64);
-        which = k1 - k0 > A.long_rows ? GN_BEGINS : GN_WHOLE;
-        if (which == GN_BEGINS && k1 > c1) k1 = c1;
+        const unsigned int first = (unsigned int)__builtin_amdgcn_readlane((int)from, l), end = (unsigned int)__builtin_amdgcn_readlane((int)to, l);
+        which = first < c0 ? GN_GOES_ON : end - first > A.long_rows ? GN_BEGINS : GN_WHOLE;
+        k0 = first < c0 ? c0 : first;
+        k1 = which != GN_WHOLE && end > c1 ? c1 : end;
         return true;
     }
 };
-__device__ __forceinline__ int64_t position(const GnArgs& A, int64_t k) {
-    const int64_t r = A.order ? A.order[k] : k;
+__device__ __forceinline__ int position(const GnArgs& A, unsigned int k) {
+    const int r = A.order ? A.order[k] : (int)k;
     return r < 0 || r >= A.n ? -1 : r;
 }
 
@@ -113,8 +111,8 @@ struct Tile {
 };
 __device__ __forceinline__ Tile tile_of(const GnArgs& A) {
     Tile T;
-    T.block0 = (int)blockIdx.y * A.tile_blocks;
-    T.n_blocks = A.blocks - T.block0 < A.tile_blocks ? A.blocks - T.block0 : A.tile_blocks;
+    T.block0 = (int)((int64_t)blockIdx.y * A.blocks / gridDim.y);      // (even tiles: none of fewer than a piece's columns)
+    T.n_blocks = (int)((int64_t)(blockIdx.y + 1) * A.blocks / gridDim.y) - T.block0;
     T.c0 = T.block0 * A.block;
     T.cols = T.n_blocks * A.block;
     T.p = (int)threadIdx.x % A.width;
@@ -123,24 +121,50 @@ __device__ __forceinline__ Tile tile_of(const GnArgs& A) {
     return T;
 }
 
+// A thread's i-th piece of eight columns. The last one of a tile ends where the tile does: its first `twice` columns are the neighbour's, who has them in
+// the sums and writes them.
+struct Piece {
+    int c, twice;
+    bool there;
+};
+__device__ __forceinline__ Piece piece_of(const GnArgs& A, const Tile& T, int i) {
+    const int c = (T.p + A.width * i) * 8;
+    Piece P;
+    P.there = c < T.cols;
+    P.c = c + 8 <= T.cols ? c : T.cols - 8;
+    P.twice = P.there ? c - P.c : 8;
+    return P;
+}
+// all eight values, wherever the row begins
+template <int T>
+__device__ __forceinline__ fg_piece<T> load_piece(const char* row, int c) {
+    return fg_load_piece<T>(row + (int64_t)c * (T == FG_F32 ? 4 : 2), 8);
+}
+template <int T>
+__device__ __forceinline__ void store_piece(char* row, const Piece& P, const float (&f)[8]) {
+    char* to = row + (int64_t)P.c * (T == FG_F32 ? 4 : 2);
+    if (P.twice == 0) return fg_store_piece<T>(to, f, 8);
+    const fg_piece<T> v = fg_to_piece<T>(f);
+#pragma unroll
+    for (int e = 1; e < 8; ++e)
+        if (e >= P.twice) {
+            if constexpr (T == FG_F32)
+                ((float*)to)[e] = f[e];
+            else
+                ((unsigned short*)to)[e] = (unsigned short)(v.a[e / 2] >> (16 * (e & 1)));
+        }
+}
+
 struct Scratch {
     double wave[GN_WAVES][2 * GN_COLUMNS];      // sums of a wavefront's rows, by column
-    double sums[GN_COLUMNS][2];                 // of a block
-    float stats[GN_COLUMNS][2];
+    float from[GN_COLUMNS];                     // what they are measured from
+    float stats[GN_COLUMNS][2];                 // of a block: mean and rstd, or the gradient's two means
     int rows[GN_WAVES];
 };
-__device__ __forceinline__ int workgroup_rows(Scratch& S, int rows, int width) {
-    for (int off = 32; off > 0; off >>= 1) rows += __shfl_xor(rows, off, 64);
-    if (fg_lane() == 0) S.rows[fg_wave()] = rows;
-    __syncthreads();
-    int all = 0;
-#pragma unroll
-    for (int w = 0; w < GN_WAVES; ++w) all += S.rows[w];
-    return all / width;
-}
-// s[e], q[e] of the thread's columns (MANY) or s[0], q[0] of all it has seen: the sums of every block in S.sums (after the caller's next barrier)
-template <bool MANY>
-__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, Scratch& S, double (&s)[MANY ? 8 : 1], double (&q)[MANY ? 8 : 1]) {
+// The sums s[e], q[e] of a thread's columns (MANY) or s[0], q[0] of all it has seen, over the rows that a wavefront has side by side, and the number of rows;
+// they are there after the workgroup's next barrier.
+template <bool MANY, typename V>
+__device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows) {
     constexpr int N = MANY ? 8 : 1;
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -148,49 +172,59 @@ __device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, Scrat
             s[e] += __shfl_xor(s[e], off, 64);
             q[e] += __shfl_xor(q[e], off, 64);
         }
+    for (int off = 32; off > 0; off >>= 1) rows += __shfl_xor(rows, off, 64);
+    if (fg_lane() == 0) S.rows[fg_wave()] = rows;
     if constexpr (MANY) {
-        if (fg_lane() < A.width && T.p * 8 < T.cols)
+        const Piece P = piece_of(A, T, 0);
+        if (fg_lane() < A.width)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (T.p * 8 + e < T.cols) {
-                    S.wave[fg_wave()][T.p * 8 + e] = s[e];
-                    S.wave[fg_wave()][GN_COLUMNS + T.p * 8 + e] = q[e];
+                if (e >= P.twice) {
+                    S.wave[fg_wave()][P.c + e] = (double)s[e];
+                    S.wave[fg_wave()][GN_COLUMNS + P.c + e] = (double)q[e];
                 }
-        __syncthreads();
+    } else if (fg_lane() == 0) {
+        S.wave[fg_wave()][0] = (double)s[0], S.wave[fg_wave()][GN_COLUMNS] = (double)q[0];
+    }
+}
+__device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch& S) {
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < GN_WAVES; ++w) all += S.rows[w];
+    return all / A.width;      // (every lane of a row has counted it)
+}
+// done(block of the tile, s, q) by one thread of every block, of the sums over its columns; column(c, s, q) makes of a column's what is to be added
+template <bool MANY, typename Column, typename Done>
+__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const Scratch& S, const Column& column, const Done& done) {
+    const auto both = [&](int c, double& a, double& b) {
+        double s = 0.0, q = 0.0;
+#pragma unroll
+        for (int w = 0; w < GN_WAVES; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
+        column(c, s, q);
+        a += s, b += q;
+    };
+    double a = 0.0, b = 0.0;
+    if constexpr (MANY) {
         int lanes = 1;      // of a block
         while (lanes < 64 && lanes * 2 * T.n_blocks <= GN_THREADS) lanes *= 2;
         const int j = (int)threadIdx.x / lanes, l = (int)threadIdx.x % lanes;
-        double a = 0.0, b = 0.0;
         if (j < T.n_blocks)
-            for (int c = j * A.block + l; c < (j + 1) * A.block; c += lanes)
-#pragma unroll
-                for (int w = 0; w < GN_WAVES; ++w) {
-                    a += S.wave[w][c];
-                    b += S.wave[w][GN_COLUMNS + c];
-                }
+            for (int c = j * A.block + l; c < (j + 1) * A.block; c += lanes) both(c, a, b);
         for (int off = lanes >> 1; off > 0; off >>= 1) {
             a += __shfl_xor(a, off, 64);
             b += __shfl_xor(b, off, 64);
         }
-        if (j < T.n_blocks && l == 0) S.sums[j][0] = a, S.sums[j][1] = b;
-    } else {
-        if (fg_lane() == 0) S.wave[fg_wave()][0] = s[0], S.wave[fg_wave()][1] = q[0];
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            double a = 0.0, b = 0.0;
-#pragma unroll
-            for (int w = 0; w < GN_WAVES; ++w) a += S.wave[w][0], b += S.wave[w][1];
-            S.sums[0][0] = a, S.sums[0][1] = b;
-        }
+        if (j < T.n_blocks && l == 0) done(j, a, b);
+    } else if (threadIdx.x == 0) {
+        both(0, a, b);
+        done(0, a, b);
     }
 }
-__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, const Scratch& S, int64_t chunk, int which, int rows) {
-    for (int j = threadIdx.x; j < T.n_blocks; j += GN_THREADS) {
-        double* to = A.part + ((chunk * 2 + (which == GN_BEGINS)) * A.blocks + T.block0 + j) * 3;
-        to[0] = S.sums[j][0], to[1] = S.sums[j][1], to[2] = (double)rows;
-    }
+__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, unsigned int chunk, int which, int j, double s, double q, int rows) {
+    double* to = A.part + ((int64_t)(chunk * 2 + (which == GN_BEGINS)) * A.blocks + T.block0 + j) * 3;
+    to[0] = s, to[1] = q, to[2] = (double)rows;
 }
-__device__ __forceinline__ void note(const GnArgs& A, int64_t chunk, int goes_on, int begins) {
+__device__ __forceinline__ void note(const GnArgs& A, unsigned int chunk, int goes_on, int begins) {
     if (threadIdx.x == 0 && blockIdx.y == 0 && A.info) A.info[chunk * 2] = goes_on, A.info[chunk * 2 + 1] = begins;
 }
 __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
@@ -200,13 +234,18 @@ __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
 }
 // what a block's values are measured from: its first value in the group's first row (0 where that row does not exist)
 __device__ __forceinline__ float level(const GnArgs& A, int type, int g, int block) {
-    const int64_t r = position(A, offset_of(A, g));
-    return r >= 0 ? element(A.x + r * A.x_stride, type, (int64_t)block * A.block) : 0.f;
+    const int r = position(A, offset_of(A, g));
+    return r >= 0 ? element(A.x + (int64_t)r * A.x_stride, type, (int64_t)block * A.block) : 0.f;
 }
 __device__ __forceinline__ void mean_rstd(const GnArgs& A, float from, double s, double q, double rows, float& mean, float& rstd) {
     const double size = rows > 0.0 ? rows * A.block : 1.0, m = s / size, v = q / size - m * m;
     mean = (float)((double)from + m);
     rstd = (float)(1.0 / sqrt((v > 0.0 || !(v == v) ? v : 0.0) + (double)A.eps));
+}
+__device__ __forceinline__ void put_statistics(const GnArgs& A, const Tile& T, int g, int j, float mean, float rstd) {
+    const int64_t at = (int64_t)g * A.blocks + T.block0 + j;
+    if (A.mean) A.mean[at] = mean;
+    if (A.rstd) A.rstd[at] = rstd;
 }
 __device__ __forceinline__ void activate(int act, float (&u)[8]) {
     fg_with_act(act, [&](auto which) {
@@ -227,130 +266,156 @@ __device__ __forceinline__ void slopes(int act, float (&u)[8]) {
 __device__ __forceinline__ void affine(const GnArgs& A, const Tile& T, int c, float (&w)[8], float (&b)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[e] = 1.f, b[e] = 0.f;
-    if (A.weight) fg_piece_values<FG_F32>(fg_load_piece<FG_F32>((const char*)(A.weight + T.c0 + c), T.cols - c), w);
-    if (A.bias) fg_piece_values<FG_F32>(fg_load_piece<FG_F32>((const char*)(A.bias + T.c0 + c), T.cols - c), b);
+    if (A.weight) fg_piece_values<FG_F32>(load_piece<FG_F32>((const char*)A.weight, T.c0 + c), w);
+    if (A.bias) fg_piece_values<FG_F32>(load_piece<FG_F32>((const char*)A.bias, T.c0 + c), b);
 }
 
-// y of the entries [k0, k1) with the blocks' mean and rstd in S.stats
+// The rows of the entries [k0, k1) that this thread has, AHEAD at a time: load(set, row or -1) for all of them, then use(set, row) for each that exists; `now`: the rows of the last sets.
+// The next positions are fetched beside the rows.
+template <int AHEAD, typename Load, typename Use>
+__device__ __forceinline__ void for_rows(const GnArgs& A, const Tile& T, unsigned int k0, unsigned int k1, int (&now)[AHEAD], const Load& load, const Use& use) {
+    int r[AHEAD];
+    const auto fetch = [&](unsigned int k) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) r[u] = k + u * T.sides < k1 ? position(A, k + u * T.sides) : -1;
+    };
+    fetch(k0 + T.side);
+    for (unsigned int k = k0 + T.side; k < k1; k += AHEAD * T.sides) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            now[u] = r[u];
+            load(u, now[u]);
+        }
+        fetch(k + AHEAD * T.sides);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (now[u] >= 0) use(u, now[u]);
+    }
+}
+
+// y of the entries [k0, k1) with the blocks' mean and rstd in S.stats. held: the sets `now`, v are all of them and there already
 template <int T_, bool MANY>
-__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch& S, int64_t k0, int64_t k1) {
-    constexpr int E = T_ == FG_F32 ? 4 : 2, AHEAD = 4;
-    for (int c = T.p * 8; c < T.cols; c += A.width * 8) {
-        float w[8], b[8], mean[8], rstd[8];
-        affine(A, T, c, w, b);
+__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
+                                          fg_piece<T_> (&v)[GN_AHEAD]) {
+    for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
+        const Piece P = piece_of(A, T, i);
+        if (!P.there) break;
+        float w[8], b[8], mean[8];
+        affine(A, T, P.c, w, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = MANY && c + e < T.cols ? (c + e) / A.block : 0;
-            mean[e] = S.stats[j][0], rstd[e] = S.stats[j][1];
+            const int j = MANY ? (P.c + e) / A.block : 0;
+            mean[e] = S.stats[j][0], w[e] *= S.stats[j][1];
         }
-        for (int64_t k = k0 + T.side; k < k1; k += AHEAD * T.sides) {
-            int64_t r[AHEAD];
-            fg_piece<T_> v[AHEAD];
+        const auto finish = [&](int u, int r) {
+            float f[8];
+            fg_piece_values<T_>(v[u], f);
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) r[u] = k + u * T.sides < k1 ? position(A, k + u * T.sides) : -1;
+            for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean[e]) * w[e] + b[e];
+            activate(A.act, f);
+            char* to = A.out + (int64_t)r * A.out_stride;
+            if (A.out_type == FG_F32)
+                store_piece<FG_F32>(to + T.c0 * 4, P, f);
+            else if constexpr (T_ != FG_F32)
+                store_piece<T_>(to + T.c0 * 2, P, f);
+        };
+        if (held) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (r[u] >= 0) v[u] = fg_load_piece<T_>(A.x + r[u] * A.x_stride + (int64_t)(T.c0 + c) * E, T.cols - c);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (r[u] < 0) continue;
-                float f[8];
-                fg_piece_values<T_>(v[u], f);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean[e]) * rstd[e] * w[e] + b[e];
-                activate(A.act, f);
-                char* to = A.out + r[u] * A.out_stride;
-                if (A.out_type == FG_F32)
-                    fg_store_piece<FG_F32>(to + (int64_t)(T.c0 + c) * 4, f, T.cols - c);
-                else if constexpr (T_ != FG_F32)
-                    fg_store_piece<T_>(to + (int64_t)(T.c0 + c) * 2, f, T.cols - c);
-            }
+            for (int u = 0; u < GN_AHEAD; ++u)
+                if (now[u] >= 0) finish(u, now[u]);
+        } else {
+            for_rows<GN_AHEAD>(
+                A, T, k0, k1, now,
+                [&](int u, int r) {
+                    if (r >= 0) v[u] = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
+                },
+                finish);
         }
     }
 }
 
 template <int T_, bool MANY>
-__global__ __launch_bounds__(GN_THREADS) void group_norm_kernel(GnArgs A) {
-    constexpr int E = T_ == FG_F32 ? 4 : 2, N = MANY ? 8 : 1, AHEAD = 4;
+__global__ __launch_bounds__(GN_THREADS, 3) void group_norm_kernel(GnArgs A) {
+    constexpr int N = MANY ? 8 : 1;
     __shared__ Scratch S;
     const Tile T = tile_of(A);
-    const int64_t chunk = blockIdx.x;
+    const unsigned int chunk = blockIdx.x;
     int goes_on = -1, begins = -1, g, which;
-    int64_t k0, k1;
+    unsigned int k0, k1;
     const auto empty = [&](int i) {
-        for (int j = 0; j < T.n_blocks; ++j) {
-            const int64_t at = (int64_t)i * A.blocks + T.block0 + j;
-            if (A.mean) A.mean[at] = 0.f;
-            if (A.rstd) A.rstd[at] = (float)(1.0 / sqrt((double)A.eps));
-        }
+        for (int j = 0; j < T.n_blocks; ++j) put_statistics(A, T, i, j, 0.f, (float)(1.0 / sqrt((double)A.eps)));
     };
     for (Walk W(A, chunk); W.next(g, k0, k1, which, empty);) {
         double s[N] = {}, q[N] = {};
-        int rows = 0;
-        for (int c = T.p * 8; c == T.p * 8 || c < T.cols; c += A.width * 8) {
+        int rows = 0, now[GN_AHEAD];
+        fg_piece<T_> v[GN_AHEAD];
+        const bool held = k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);      // (all of a group's rows at once: they are read once)
+#pragma unroll
+        for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
+        // a column's values are measured from its first one (MANY), all columns' from the block's
+        const int first = position(A, which == GN_GOES_ON ? offset_of(A, g) : k0);
+        const float common = !MANY && first >= 0 ? element(A.x + (int64_t)first * A.x_stride, T_, T.c0) : 0.f;
+        for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
+            const Piece P = piece_of(A, T, i);
             float from[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) from[e] = c + e < T.cols ? level(A, T_, g, T.block0 + (MANY ? (c + e) / A.block : 0)) : 0.f;
-            for (int64_t k = k0 + T.side; k < k1; k += AHEAD * T.sides) {
-                int64_t r[AHEAD];
-                fg_piece<T_> v[AHEAD];
+            for (int e = 0; e < 8; ++e) from[e] = common;
+            if (MANY && first >= 0) fg_piece_values<T_>(load_piece<T_>(A.x + (int64_t)first * A.x_stride, T.c0 + P.c), from);
+            if (MANY && T.side == 0)
 #pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    r[u] = k + u * T.sides < k1 ? position(A, k + u * T.sides) : -1;
-                    rows += r[u] >= 0 && c == T.p * 8;
-                    if (c >= T.cols) r[u] = -1;
-                }
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u)
-                    if (r[u] >= 0) v[u] = fg_load_piece<T_>(A.x + r[u] * A.x_stride + (int64_t)(T.c0 + c) * E, T.cols - c);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) {
-                    if (r[u] < 0) continue;
+                for (int e = 0; e < 8; ++e)
+                    if (e >= P.twice) S.from[P.c + e] = from[e];
+            for_rows<GN_AHEAD>(
+                A, T, k0, k1, now,
+                [&](int u, int r) {
+                    rows += r >= 0 && i == 0;
+                    if (r >= 0) v[u] = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
+                },
+                [&](int u, int) {
                     float f[8];
                     fg_piece_values<T_>(v[u], f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        const double x = c + e < T.cols ? (double)f[e] - (double)from[e] : 0.0;
+                        const double x = MANY || e >= P.twice ? (double)f[e] - (double)from[e] : 0.0;      // (MANY: a neighbour's columns are not left in the sums)
                         s[MANY ? e : 0] += x;
                         q[MANY ? e : 0] += x * x;
                     }
-                }
-            }
+                });
         }
-        rows = workgroup_rows(S, rows, A.width);
-        block_sums<MANY>(A, T, S, s, q);
+        leave_sums<MANY>(A, T, S, s, q, rows);
         __syncthreads();
-        if (which == GN_WHOLE) {
-            for (int j = threadIdx.x; j < T.n_blocks; j += GN_THREADS) {
+        rows = rows_of(A, S);
+        block_sums<MANY>(
+            A, T, S,
+            [&](int c, double& a, double& b) {      // from the column's level to the block's
+                if constexpr (MANY) {
+                    const double up = (double)S.from[c] - (double)S.from[c / A.block * A.block];
+                    b += up * (2.0 * a + rows * up);
+                    a += rows * up;
+                }
+            },
+            [&](int j, double a, double b) {
+                if (which != GN_WHOLE) return write_part(A, T, chunk, which, j, a, b, rows);
                 float mean, rstd;
-                mean_rstd(A, level(A, T_, g, T.block0 + j), S.sums[j][0], S.sums[j][1], (double)rows, mean, rstd);
+                mean_rstd(A, MANY ? S.from[j * A.block] : common, a, b, (double)rows, mean, rstd);
                 S.stats[j][0] = mean, S.stats[j][1] = rstd;
-                const int64_t at = (int64_t)g * A.blocks + T.block0 + j;
-                if (A.mean) A.mean[at] = mean;
-                if (A.rstd) A.rstd[at] = rstd;
-            }
-            __syncthreads();
-            normalise<T_, MANY>(A, T, S, k0, k1);
-        } else {
-            write_part(A, T, S, chunk, which, rows);
+                put_statistics(A, T, g, j, mean, rstd);
+            });
+        __syncthreads();      // (the sums have been read: the next group's may be left there, and its statistics behind the next barrier)
+        if (which == GN_WHOLE)
+            normalise<T_, MANY>(A, T, S, k0, k1, held, now, v);
+        else
             (which == GN_BEGINS ? begins : goes_on) = g;
-        }
-        __syncthreads();      // the scratch may be used again
     }
     note(A, chunk, goes_on, begins);
 }
 
-// The parts of every split group, added up in order: a wavefront to a block of columns. BACKWARD: the two means of the gradient
-template <int T_, bool BACKWARD>
-__global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
-    const int64_t chunk = blockIdx.x;
-    const int j = (int)blockIdx.y * GN_WAVES + fg_wave();
-    const int g = A.info[chunk * 2 + 1];
-    if (g < 0 || j >= A.blocks) return;
-    const int64_t last = (offset_of(A, g + 1) - 1) / A.rows;
-    double s = 0.0, q = 0.0, rows = 0.0;
-    for (int64_t c = chunk + fg_lane(); c <= last; c += 64) {
-        const double* p = A.part + ((c * 2 + (c == chunk)) * A.blocks + j) * 3;
+// the sums of all parts of the split group that begins in a chunk, in order: lanes of a wavefront together
+__device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin, int block, double& s, double& q, double& rows) {
+    const unsigned int last = (offset_of(A, g + 1) - 1) / A.rows;
+    s = q = rows = 0.0;
+    for (unsigned int c = begin + fg_lane(); c <= last; c += 64) {
+        const double* p = A.part + ((int64_t)(c * 2 + (c == begin)) * A.blocks + block) * 3;
         s += p[0], q += p[1], rows += p[2];
     }
     for (int off = 32; off > 0; off >>= 1) {
@@ -358,29 +423,72 @@ __global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
         q += __shfl_xor(q, off, 64);
         rows += __shfl_xor(rows, off, 64);
     }
-    if (fg_lane() != 0) return;
-    float* to = A.joined + (chunk * A.blocks + j) * 2;
+}
+// what the parts come to, and the forward call's results
+template <int T_, bool BACKWARD>
+__device__ __forceinline__ void joined(const GnArgs& A, int g, unsigned int begin, int block, bool write, float& a, float& b) {
+    double s, q, rows;
+    join(A, g, begin, block, s, q, rows);
     if constexpr (BACKWARD) {
         const double size = rows > 0.0 ? rows * A.block : 1.0;
-        to[0] = (float)(s / size), to[1] = (float)(q / size);
+        a = (float)(s / size), b = (float)(q / size);
     } else {
-        mean_rstd(A, level(A, T_, g, j), s, q, rows, to[0], to[1]);
-        if (A.mean) A.mean[(int64_t)g * A.blocks + j] = to[0];
-        if (A.rstd) A.rstd[(int64_t)g * A.blocks + j] = to[1];
+        mean_rstd(A, level(A, T_, g, block), s, q, rows, a, b);
+        if (write && fg_lane() == 0) {
+            if (A.mean) A.mean[(int64_t)g * A.blocks + block] = a;
+            if (A.rstd) A.rstd[(int64_t)g * A.blocks + block] = b;
+        }
     }
 }
+// dw and db: the chunks' sums added up in fp64, in order; 32 columns a workgroup, eight runs of chunks side by side
+__device__ __forceinline__ void column_sums(const GnArgs& A, int block, double* red) {
+    const int c = block * 32 + ((int)threadIdx.x & 31);
+    double s = 0.0;
+    if (c < 2 * A.d)
+#pragma unroll 8
+        for (int64_t i = threadIdx.x >> 5; i < A.chunks; i += GN_THREADS / 32) s += (double)A.columns[i * 2 * A.d + c];
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.x < 32 && c < 2 * A.d) {
+        for (int i = 1; i < GN_THREADS / 32; ++i) s += red[threadIdx.x + 32 * i];
+        float* to = c < A.d ? A.dw : A.db;
+        if (to) to[c < A.d ? c : c - A.d] = (float)s;
+    }
+}
+// The launch between the two passes, a wavefront to a block of columns of every split group. The workgroups behind those sum dw and db
+template <int T_, bool BACKWARD>
+__global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
+    __shared__ double red[BACKWARD ? GN_THREADS : 1];
+    if (BACKWARD && (int)blockIdx.x >= A.joins) return column_sums(A, (int)blockIdx.x - A.joins, red);
+    const int per_chunk = (A.blocks + GN_WAVES - 1) / GN_WAVES;
+    const unsigned int chunk = blockIdx.x / per_chunk;
+    const int j = (int)(blockIdx.x % per_chunk) * GN_WAVES + fg_wave();
+    const int g = A.info[chunk * 2 + 1];
+    if (g < 0 || j >= A.blocks) return;
+    float a, b;
+    joined<T_, BACKWARD>(A, g, chunk, j, true, a, b);
+    if (fg_lane() == 0) *(float2*)(A.joined + ((int64_t)chunk * A.blocks + j) * 2) = float2{a, b};
+}
 
-// a chunk's parts of split groups: f(group, first entry, end) with what the join has left in S.stats
-template <typename F>
+// a chunk's parts of split groups: f(group, first entry, end) with what their parts come to in S.stats
+template <int T_, bool BACKWARD, typename F>
 __device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scratch& S, const F& f) {
-    const int64_t chunk = blockIdx.x, c0 = chunk * A.rows, c1 = c0 + A.rows;
+    const unsigned int chunk = gridDim.x - 1 - blockIdx.x, c0 = chunk * A.rows, c1 = c0 + A.rows;      // the last chunks' rows are the likeliest to be cached
     for (int which = 0; which < 2; ++which) {
         const int g = A.info[chunk * 2 + which];
         if (g < 0) continue;
-        const int64_t from = offset_of(A, g), to = offset_of(A, g + 1), begin = from / A.rows;
-        for (int j = threadIdx.x; j < T.n_blocks; j += GN_THREADS) {
-            const float* p = A.joined + (begin * A.blocks + T.block0 + j) * 2;
-            S.stats[j][0] = p[0], S.stats[j][1] = p[1];
+        const unsigned int from = offset_of(A, g), to = offset_of(A, g + 1), begin = from / A.rows;
+        if (A.join_there) {
+            for (int j = threadIdx.x; j < T.n_blocks; j += GN_THREADS) {
+                const float* p = A.joined + ((int64_t)begin * A.blocks + T.block0 + j) * 2;
+                S.stats[j][0] = p[0], S.stats[j][1] = p[1];
+            }
+        } else {
+            for (int j = fg_wave(); j < T.n_blocks; j += GN_WAVES) {
+                float a, b;
+                joined<T_, BACKWARD>(A, g, begin, T.block0 + j, which == 1, a, b);
+                if (fg_lane() == 0) S.stats[j][0] = a, S.stats[j][1] = b;
+            }
         }
         __syncthreads();
         f(g, from > c0 ? from : c0, to < c1 ? to : c1);
@@ -388,206 +496,260 @@ __device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scra
     }
 }
 template <int T_, bool MANY>
-__global__ __launch_bounds__(GN_THREADS) void group_norm_apply_kernel(GnArgs A) {
+__global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs A) {
     __shared__ Scratch S;
     const Tile T = tile_of(A);
-    split_parts(A, T, S, [&](int, int64_t k0, int64_t k1) { normalise<T_, MANY>(A, T, S, k0, k1); });
+    split_parts<T_, false>(A, T, S, [&](int, unsigned int k0, unsigned int k1) {
+        int now[GN_AHEAD];
+        fg_piece<T_> v[GN_AHEAD];
+        normalise<T_, MANY>(A, T, S, k0, k1, false, now, v);
+    });
 }
 
 // ---- gradients ----
 
-// xh, t and q = t * weight of a piece
-__device__ __forceinline__ void gradient_terms(const GnArgs& A, const float (&mean)[8], const float (&rstd)[8], const float (&w)[8], const float (&b)[8], float (&xh)[8],
-                                               float (&t)[8]) {
-    float slope[8];
+// A thread's piece of the columns: what the gradients need of them
+struct GradColumns {
+    float mean[8], rstd[8], w[8], b[8];
+};
+template <bool MANY>
+__device__ __forceinline__ void grad_columns(const GnArgs& A, const Tile& T, int g, int c, GradColumns& C) {
+    affine(A, T, c, C.w, C.b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        xh[e] = (xh[e] - mean[e]) * rstd[e];
-        slope[e] = xh[e] * w[e] + b[e];
+        const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY ? (c + e) / A.block : 0);
+        C.mean[e] = A.mean[at], C.rstd[e] = A.rstd[at];
     }
-    slopes(A.act, slope);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] *= slope[e];
 }
-// f(piece, columns left, xh, t, w, rstd, row) for every piece of the entries [k0, k1) that this thread has, by columns
-template <int X, int G, bool MANY, int NP, typename F>
-__device__ __forceinline__ void gradient_pass(const GnArgs& A, const Tile& T, int g, int64_t k0, int64_t k1, const F& f) {
-    constexpr int XE = X == FG_F32 ? 4 : 2, GE = G == FG_F32 ? 4 : 2, AHEAD = 2;
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int c = (T.p + A.width * i) * 8;
-        if (c >= T.cols) continue;
-        float w[8], b[8], mean[8], rstd[8];
-        affine(A, T, c, w, b);
+// rows on their way, or held
+template <int X, int G>
+struct GradRows {
+    int now[GN_AHEAD_BW];
+    fg_piece<X> x[GN_AHEAD_BW];
+    fg_piece<G> dy[GN_AHEAD_BW];
+};
+// use(row, xh, t) for every row of the entries [k0, k1) that this thread has; held: R has all of them already
+template <int X, int G, typename Use>
+__device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, int c, const GradColumns& C, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R,
+                                              const Use& use) {
+    const auto terms = [&](int u, int r) {
+        float xh[8], t[8], slope[8];
+        fg_piece_values<X>(R.x[u], xh);
+        fg_piece_values<G>(R.dy[u], t);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY && c + e < T.cols ? (c + e) / A.block : 0);
-            mean[e] = A.mean[at], rstd[e] = A.rstd[at];
+            xh[e] = (xh[e] - C.mean[e]) * C.rstd[e];
+            slope[e] = xh[e] * C.w[e] + C.b[e];
         }
-        for (int64_t k = k0 + T.side; k < k1; k += AHEAD * T.sides) {
-            int64_t r[AHEAD];
-            fg_piece<X> vx[AHEAD];
-            fg_piece<G> vg[AHEAD];
+        slopes(A.act, slope);
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) r[u] = k + u * T.sides < k1 ? position(A, k + u * T.sides) : -1;
+        for (int e = 0; e < 8; ++e) t[e] *= slope[e];
+        use(r, xh, t);
+    };
+    if (held) {
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-                if (r[u] >= 0) {
-                    vx[u] = fg_load_piece<X>(A.x + r[u] * A.x_stride + (int64_t)(T.c0 + c) * XE, T.cols - c);
-                    vg[u] = fg_load_piece<G>(A.dy + r[u] * A.dy_stride + (int64_t)(T.c0 + c) * GE, T.cols - c);
-                }
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (r[u] < 0) continue;
-                float xh[8], t[8];
-                fg_piece_values<X>(vx[u], xh);
-                fg_piece_values<G>(vg[u], t);
-                gradient_terms(A, mean, rstd, w, b, xh, t);
-                f(i, c, xh, t, w, rstd, r[u]);
-            }
-        }
+        for (int u = 0; u < GN_AHEAD_BW; ++u)
+            if (R.now[u] >= 0) terms(u, R.now[u]);
+    } else {
+        for_rows<GN_AHEAD_BW>(
+            A, T, k0, k1, R.now,
+            [&](int u, int r) {
+                if (r < 0) return;
+                R.x[u] = load_piece<X>(A.x + (int64_t)r * A.x_stride, T.c0 + c);
+                R.dy[u] = load_piece<G>(A.dy + (int64_t)r * A.dy_stride, T.c0 + c);
+            },
+            terms);
     }
 }
 // dx of the entries [k0, k1) with the blocks' two means in S.stats
-template <int X, int G, bool MANY, int NP>
-__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch& S, int g, int64_t k0, int64_t k1) {
-    gradient_pass<X, G, MANY, NP>(A, T, g, k0, k1, [&](int, int c, const float(&xh)[8], float(&t)[8], const float(&w)[8], const float(&rstd)[8], int64_t r) {
+template <int X, int G, bool MANY>
+__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch& S, int g, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R) {
+    for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
+        const Piece P = piece_of(A, T, i);
+        if (!P.there) break;
+        GradColumns C;
+        grad_columns<MANY>(A, T, g, P.c, C);
+        float m1[8], m2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = MANY && c + e < T.cols ? (c + e) / A.block : 0;
-            t[e] = rstd[e] * (t[e] * w[e] - S.stats[j][0] - xh[e] * S.stats[j][1]);
+            const int j = MANY ? (P.c + e) / A.block : 0;
+            m1[e] = S.stats[j][0], m2[e] = S.stats[j][1];
         }
-        fg_store_piece<G>(A.out + r * A.out_stride + (int64_t)(T.c0 + c) * (G == FG_F32 ? 4 : 2), t, T.cols - c);
-    });
+        gradient_rows<X, G>(A, T, P.c, C, k0, k1, held, R, [&](int r, const float(&xh)[8], float(&t)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = C.rstd[e] * (t[e] * C.w[e] - m1[e] - xh[e] * m2[e]);
+            store_piece<G>(A.out + (int64_t)r * A.out_stride + T.c0 * (G == FG_F32 ? 4 : 2), P, t);
+        });
+    }
 }
 
+// The first pass: a group's sums of t and t * xh by column, which give its two means and dw and db. MANY: the columns' sums over a group's rows
+// meet in LDS, a thread to a column adds them up over the chunk's groups. Else (NP pieces a thread) a thread keeps its columns' sums over all of
+// the chunk's rows, and those of a group over its columns beside them.
 template <int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(GN_THREADS) void group_norm_backward_kernel(GnArgs A) {
-    constexpr int N = MANY ? 8 : 1;
+__global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backward_kernel(GnArgs A) {
     __shared__ Scratch S;
     const Tile T = tile_of(A);
-    const int64_t chunk = blockIdx.x;
+    const unsigned int chunk = blockIdx.x;
     int goes_on = -1, begins = -1, g, which;
-    int64_t k0, k1;
-    float dw[NP][8] = {}, db[NP][8] = {};
+    unsigned int k0, k1;
+    const int mine = (int)threadIdx.x;      // MANY: the column whose sums this thread has
+    double dw = 0.0, db = 0.0;
+    float dw_piece[MANY ? 1 : NP][8] = {}, db_piece[MANY ? 1 : NP][8] = {};
     for (Walk W(A, chunk); W.next(g, k0, k1, which, [](int) {});) {
-        double s[N] = {}, q[N] = {};
-        int rows = 0;
-        for (int64_t k = k0 + T.side; k < k1; k += T.sides) rows += position(A, k) >= 0;
-        gradient_pass<X, G, MANY, NP>(A, T, g, k0, k1, [&](int i, int c, const float(&xh)[8], const float(&t)[8], const float(&w)[8], const float(&)[8], int64_t) {
+        GradRows<X, G> R;
+        const bool held = k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (c + e >= T.cols) continue;
-                const float a = t[e] * w[e];
-                s[MANY ? e : 0] += (double)a;
-                q[MANY ? e : 0] += (double)a * (double)xh[e];
-                dw[i][e] += t[e] * xh[e];
-                db[i][e] += t[e];
+        for (int u = 0; u < GN_AHEAD_BW; ++u) R.now[u] = -1;
+        int rows = 0;
+        for (unsigned int k = k0 + T.side; k < k1; k += T.sides) rows += position(A, k) >= 0;
+        if constexpr (MANY) {
+            float s[8] = {}, q[8] = {};
+            const Piece P = piece_of(A, T, 0);
+            if (P.there) {
+                GradColumns C;
+                grad_columns<true>(A, T, g, P.c, C);
+                gradient_rows<X, G>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * xh[e];
+                });
             }
-        });
-        rows = workgroup_rows(S, rows, A.width);
-        block_sums<MANY>(A, T, S, s, q);
-        __syncthreads();
-        if (which == GN_WHOLE) {
-            const double size = rows > 0 ? (double)rows * A.block : 1.0;
-            for (int j = threadIdx.x; j < T.n_blocks; j += GN_THREADS) S.stats[j][0] = (float)(S.sums[j][0] / size), S.stats[j][1] = (float)(S.sums[j][1] / size);
-            __syncthreads();
-            input_gradient<X, G, MANY, NP>(A, T, S, g, k0, k1);
+            leave_sums<true>(A, T, S, s, q, rows);
         } else {
-            write_part(A, T, S, chunk, which, rows);
-            (which == GN_BEGINS ? begins : goes_on) = g;
+            double s[1] = {}, q[1] = {};
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const Piece P = piece_of(A, T, i);
+                if (P.there) {
+                    GradColumns C;
+                    grad_columns<false>(A, T, g, P.c, C);
+                    gradient_rows<X, G>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (e < P.twice) continue;
+                            const double a = (double)(t[e] * C.w[e]);
+                            s[0] += a, q[0] += a * (double)xh[e];
+                            dw_piece[i][e] += t[e] * xh[e], db_piece[i][e] += t[e];
+                        }
+                    });
+                }
+            }
+            leave_sums<false>(A, T, S, s, q, rows);
         }
         __syncthreads();
+        rows = rows_of(A, S);
+        if (MANY && mine < T.cols)
+#pragma unroll
+            for (int w = 0; w < GN_WAVES; ++w) db += S.wave[w][mine], dw += S.wave[w][GN_COLUMNS + mine];
+        block_sums<MANY>(
+            A, T, S,
+            [&](int c, double& a, double& b) {
+                if constexpr (MANY) {
+                    const double w = A.weight ? (double)A.weight[T.c0 + c] : 1.0;
+                    a *= w, b *= w;
+                }
+            },
+            [&](int j, double a, double b) {
+                if (which != GN_WHOLE) return write_part(A, T, chunk, which, j, a, b, rows);
+                const double size = rows > 0 ? (double)rows * A.block : 1.0;
+                S.stats[j][0] = (float)(a / size), S.stats[j][1] = (float)(b / size);
+            });
+        __syncthreads();
+        if (which == GN_WHOLE)
+            input_gradient<X, G, MANY>(A, T, S, g, k0, k1, held, R);
+        else
+            (which == GN_BEGINS ? begins : goes_on) = g;
     }
     note(A, chunk, goes_on, begins);
     if (!A.columns) return;
-    // the rows that were walked side by side: their column sums meet in LDS
-    float* const to = A.columns + chunk * 2 * A.d + T.c0;
-    float* const meet = (float*)S.wave;      // [side][width * 8]
-    static_assert(sizeof(S.wave) >= GN_THREADS * 8 * sizeof(float), "eight columns of every thread");
+    float* const to = A.columns + (int64_t)chunk * 2 * A.d + T.c0;
+    if constexpr (MANY) {
+        if (mine < T.cols) to[mine] = (float)dw, to[A.d + mine] = (float)db;
+    } else {
+        float* const meet = (float*)S.wave;      // [side][width * 8]
+        static_assert(sizeof(S.wave) >= GN_THREADS * 8 * sizeof(float), "eight columns of every thread");
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        if (T.sides == 1) {
+        for (int which_sum = 0; which_sum < 2; ++which_sum) {
+            if (T.sides == 1) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const int c = (T.p + A.width * i) * 8;
-                if (c < T.cols) fg_store_piece<FG_F32>((char*)(to + which * A.d + c), which ? db[i] : dw[i], T.cols - c);
+                for (int i = 0; i < NP; ++i) {
+                    const Piece P = piece_of(A, T, i);
+                    if (P.there) store_piece<FG_F32>((char*)(to + which_sum * A.d), P, which_sum ? db_piece[i] : dw_piece[i]);
+                }
+            } else {      // rows side by side (NP is 1 then): their sums meet in LDS
+                const Piece P = piece_of(A, T, 0);
+                __syncthreads();
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e >= P.twice) meet[T.side * A.width * 8 + P.c + e] = which_sum ? db_piece[0][e] : dw_piece[0][e];
+                __syncthreads();
+                for (int c = threadIdx.x; c < T.cols; c += GN_THREADS) {
+                    float v = 0.f;
+                    for (int i = 0; i < T.sides; ++i) v += meet[i * A.width * 8 + c];
+                    to[which_sum * A.d + c] = v;
+                }
             }
-        } else {      // (NP is 1 where rows lie side by side)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) meet[threadIdx.x * 8 + e] = which ? db[0][e] : dw[0][e];
-            __syncthreads();
-            for (int c = threadIdx.x; c < T.cols; c += GN_THREADS) {
-                float v = 0.f;
-                for (int i = 0; i < T.sides; ++i) v += meet[i * A.width * 8 + c];
-                to[which * A.d + c] = v;
-            }
-            __syncthreads();
         }
     }
 }
-template <int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(GN_THREADS) void group_norm_backward_apply_kernel(GnArgs A) {
+// The second pass, on split groups
+template <int X, int G, bool MANY>
+__global__ __launch_bounds__(GN_THREADS, 3) void group_norm_backward_apply_kernel(GnArgs A) {
     __shared__ Scratch S;
     const Tile T = tile_of(A);
-    split_parts(A, T, S, [&](int g, int64_t k0, int64_t k1) { input_gradient<X, G, MANY, NP>(A, T, S, g, k0, k1); });
-}
-// dw and db: the chunks' sums added up in fp64, in order; 32 columns a workgroup, eight runs of chunks side by side
-__global__ __launch_bounds__(GN_THREADS) void group_norm_columns_kernel(const float* __restrict__ columns, int64_t chunks, int d, float* dw, float* db) {
-    __shared__ double red[GN_THREADS];
-    const int c = blockIdx.x * 32 + (threadIdx.x & 31);
-    double s = 0.0;
-    if (c < 2 * d)
-#pragma unroll 8
-        for (int64_t b = threadIdx.x >> 5; b < chunks; b += GN_THREADS / 32) s += (double)columns[b * 2 * d + c];
-    red[threadIdx.x] = s;
-    __syncthreads();
-    if (threadIdx.x < 32 && c < 2 * d) {
-        for (int i = 1; i < GN_THREADS / 32; ++i) s += red[threadIdx.x + 32 * i];
-        float* to = c < d ? dw : db;
-        if (to) to[c < d ? c : c - d] = (float)s;
-    }
+    split_parts<X, true>(A, T, S, [&](int g, unsigned int k0, unsigned int k1) {
+        GradRows<X, G> R;
+        input_gradient<X, G, MANY>(A, T, S, g, k0, k1, false, R);
+    });
 }
 
-// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block; chunks of rows so that there are about four workgroups to a
-// compute unit, with four rows a thread at least. A group whose values in a tile are up to GN_FEW_VALUES is not split.
+// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block; chunks of rows, with two rows a thread at least, so that
+// all workgroups are on the chip at once, three to a compute unit (a fourth of them in a second turn took as long as all the others). Where that leaves
+// compute units without work, tiles of fewer blocks, and a chunk to each of them. A group whose values in a tile are up to GN_FEW_VALUES is not split.
 struct Plan {
-    int tile_blocks, tiles, width, pieces;
-    int64_t rows, chunks, most_chunks, long_rows;
-    bool split;
+    int tiles, tile_blocks, width, pieces;
+    int64_t rows, chunks, long_rows;
+    bool split, join_there;
 };
 Plan plan_of(int64_t max_rows, int d, int blocks) {
     Plan P;
     const int block = d / blocks, per_tile = GN_COLUMNS / block;
-    P.tile_blocks = per_tile < 1 ? 1 : (per_tile < blocks ? per_tile : blocks);
-    P.tiles = (int)fg_ceil_div(blocks, P.tile_blocks);
-    const int cols = P.tile_blocks * block, pieces = (int)fg_ceil_div(cols, 8);
-    P.width = 1;
-    while (P.width < pieces && P.width < GN_THREADS) P.width *= 2;
+    P.tiles = (int)fg_ceil_div(blocks, per_tile < 1 ? 1 : per_tile);
+    int cols, pieces;
+    int64_t places, least;
+    for (;; P.tiles *= 2) {
+        P.tile_blocks = (int)fg_ceil_div(blocks, P.tiles);
+        cols = P.tile_blocks * block, pieces = (int)fg_ceil_div(cols, 8);
+        P.width = 1;
+        while (P.width < pieces && P.width < GN_THREADS) P.width *= 2;
+        places = GN_PLACES / P.tiles, least = 2 * (GN_THREADS / P.width);
+        if (P.tiles * 2 > blocks || blocks / (P.tiles * 2) * block < 8 || (max_rows / least + 1) * P.tiles > GN_FEW_WORKGROUPS) break;
+    }
     P.pieces = (int)fg_ceil_div(pieces, P.width);
-    const int64_t places = GN_PLACES / P.tiles, least = 4 * (GN_THREADS / P.width);
-    const int64_t even = fg_ceil_div(max_rows, places);
+    const int64_t even = max_rows / places + 1;
     P.rows = even > least ? even : least;
+    const int64_t spread = max_rows * P.tiles / 256 + 2;      // few rows: the groups' beginnings spread over the chip
+    if (spread < P.rows) P.rows = spread;
     P.chunks = max_rows / P.rows + 1;
-    P.most_chunks = (max_rows / least < places ? max_rows / least : places) + 1;
     P.long_rows = P.rows > GN_FEW_VALUES / cols ? P.rows : GN_FEW_VALUES / cols;
     P.split = P.long_rows < max_rows;
+    P.join_there = P.chunks * P.tile_blocks > GN_JOIN_HERE;
     return P;
 }
 static_assert(FG_MAX_NORM_DIM <= GN_THREADS * 8 * GN_MAX_PIECES && FG_MAX_NORM_DIM / GN_COLUMNS * 2 <= GN_PLACES, "pieces of a row; tiles");
 
-// (by the most chunks that a call of up to so many rows has: a workspace for max_rows serves fewer rows too)
+// A workspace for max_rows serves fewer rows too: by the most chunks that a call can have
 struct Space {
     size_t part, info, joined, columns;
     size_t total() const { return part + info + joined + columns + 16; }
 };
 Space space_of(int64_t max_rows, int d, int blocks, bool backward) {
-    const Plan P = plan_of(max_rows, d, blocks);
+    const int64_t chunks = max_rows < GN_PLACES ? max_rows + 1 : GN_PLACES;      // (two rows to a chunk at least, and no more chunks than places)
     Space W = {};
-    W.part = fg_align_up((size_t)P.most_chunks * 2 * blocks * 3 * 8, 256);
-    W.info = fg_align_up((size_t)P.most_chunks * 2 * 4, 256);
-    W.joined = fg_align_up((size_t)P.most_chunks * blocks * 2 * 4, 256);
-    if (backward) W.columns = (size_t)P.most_chunks * 2 * d * 4;
+    W.part = fg_align_up((size_t)chunks * 2 * blocks * 3 * 8, 256);
+    W.info = fg_align_up((size_t)chunks * 2 * 4, 256);
+    W.joined = fg_align_up((size_t)chunks * blocks * 2 * 4, 256);
+    if (backward) W.columns = (size_t)chunks * 2 * d * 4;
     return W;
 }
 
@@ -595,7 +757,7 @@ fg_status_t check_norm(const char* who, const int32_t* order_dev, const int64_t*
                        int32_t channel_groups, fg_act_t act) {
     FG_TRY(check_rows(who, nullptr, nullptr, 0, n, d));
     if (max_rows < 0 || max_rows > INT32_MAX) FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
-    if (d > FG_MAX_NORM_DIM) FG_FAIL(FG_ERR_SHAPE, "%s: d = %d is more than %d", who, d, FG_MAX_NORM_DIM);
+    if (d < 8 || d > FG_MAX_NORM_DIM) FG_FAIL(FG_ERR_SHAPE, "%s: d = %d is not in 8..%d", who, d, FG_MAX_NORM_DIM);
     if (n_groups < 1 || n_groups > FG_MAX_NORM_GROUPS) FG_FAIL(FG_ERR_INVALID_ARG, "%s: n_groups = %d is not in 1..%d", who, n_groups, FG_MAX_NORM_GROUPS);
     if (channel_groups < 1 || channel_groups > d || d % channel_groups) FG_FAIL(FG_ERR_SHAPE, "%s: %d groups do not divide d = %d columns", who, channel_groups, d);
     if (!fg_act_known(act)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: unknown activation %d", who, (int)act);
@@ -611,38 +773,35 @@ fg_status_t check_space(const char* who, const void* ws_dev, size_t ws_bytes, si
 GnArgs args_of(const Plan& P, const Space& W, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int64_t n, int32_t d,
                int32_t blocks, void* ws_dev) {
     GnArgs A = {};
-    A.order = order_dev, A.offsets = offsets_dev, A.max_rows = max_rows, A.n = n, A.rows = P.rows, A.long_rows = P.long_rows;
-    A.n_groups = n_groups, A.d = d, A.block = d / blocks, A.blocks = blocks, A.tile_blocks = P.tile_blocks, A.width = P.width;
+    A.order = order_dev, A.offsets = offsets_dev, A.max_rows = max_rows, A.n = n, A.rows = (unsigned int)P.rows, A.long_rows = (unsigned int)P.long_rows;
+    A.n_groups = n_groups, A.d = d, A.block = d / blocks, A.blocks = blocks, A.width = P.width, A.pieces = P.pieces;
     char* ws = (char*)ws_dev;
     A.part = (double*)ws;
     A.info = P.split ? (int32_t*)(ws + W.part) : nullptr;
+    A.chunks = P.chunks;
     A.joined = (float*)(ws + W.part + W.info);
     A.columns = (float*)(ws + W.part + W.info + W.joined);
     return A;
 }
 
-template <int T>
+// workgroups that join the parts of split groups, and those that sum dw and db
+int joins_of(const Plan& P, const GnArgs& A) { return (int)(P.chunks * fg_ceil_div(A.blocks, GN_WAVES)); }
+int sum_blocks(const GnArgs& A) { return A.columns ? (int)fg_ceil_div(2 * A.d, 32) : 0; }
+
+template <int T, bool MANY>
 void forward(const Plan& P, const GnArgs& A, hipStream_t st) {
-    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles), joins((unsigned)P.chunks, (unsigned)fg_ceil_div(A.blocks, GN_WAVES));
-    const bool many = P.tile_blocks > 1;
-    if (many)
-        hipLaunchKernelGGL((group_norm_kernel<T, true>), grid, dim3(GN_THREADS), 0, st, A);
-    else
-        hipLaunchKernelGGL((group_norm_kernel<T, false>), grid, dim3(GN_THREADS), 0, st, A);
+    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles);
+    hipLaunchKernelGGL((group_norm_kernel<T, MANY>), grid, dim3(GN_THREADS), 0, st, A);
     if (!P.split) return;
-    hipLaunchKernelGGL((group_norm_join_kernel<T, false>), joins, dim3(GN_THREADS), 0, st, A);
-    if (many)
-        hipLaunchKernelGGL((group_norm_apply_kernel<T, true>), grid, dim3(GN_THREADS), 0, st, A);
-    else
-        hipLaunchKernelGGL((group_norm_apply_kernel<T, false>), grid, dim3(GN_THREADS), 0, st, A);
+    if (A.joins) hipLaunchKernelGGL((group_norm_join_kernel<T, false>), dim3((unsigned)A.joins), dim3(GN_THREADS), 0, st, A);
+    hipLaunchKernelGGL((group_norm_apply_kernel<T, MANY>), grid, dim3(GN_THREADS), 0, st, A);
 }
 template <int X, int G, bool MANY, int NP>
 void backward_pass(const Plan& P, const GnArgs& A, hipStream_t st) {
-    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles), joins((unsigned)P.chunks, (unsigned)fg_ceil_div(A.blocks, GN_WAVES));
+    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles);
     hipLaunchKernelGGL((group_norm_backward_kernel<X, G, MANY, NP>), grid, dim3(GN_THREADS), 0, st, A);
-    if (!P.split) return;
-    hipLaunchKernelGGL((group_norm_join_kernel<X, true>), joins, dim3(GN_THREADS), 0, st, A);
-    hipLaunchKernelGGL((group_norm_backward_apply_kernel<X, G, MANY, NP>), grid, dim3(GN_THREADS), 0, st, A);
+    if (const int sums = A.joins + sum_blocks(A)) hipLaunchKernelGGL((group_norm_join_kernel<X, true>), dim3((unsigned)sums), dim3(GN_THREADS), 0, st, A);
+    if (P.split) hipLaunchKernelGGL((group_norm_backward_apply_kernel<X, G, MANY>), grid, dim3(GN_THREADS), 0, st, A);
 }
 template <int X, int G>
 void backward(const Plan& P, const GnArgs& A, hipStream_t st) {
@@ -657,7 +816,7 @@ void backward(const Plan& P, const GnArgs& A, hipStream_t st) {
 }  // namespace
 
 extern "C" size_t fg_group_norm_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups) {
-    if (max_rows < 0 || max_rows > INT32_MAX || n_groups < 1 || n_groups > FG_MAX_NORM_GROUPS || d <= 0 || d > FG_MAX_NORM_DIM || channel_groups < 1 || channel_groups > d ||
+    if (max_rows < 0 || max_rows > INT32_MAX || n_groups < 1 || n_groups > FG_MAX_NORM_GROUPS || d < 8 || d > FG_MAX_NORM_DIM || channel_groups < 1 || channel_groups > d ||
         d % channel_groups)
         return 0;
     return space_of(max_rows, d, channel_groups, false).total();
@@ -686,13 +845,15 @@ extern "C" fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t
     GnArgs A = args_of(P, W, order_dev, offsets_dev, max_rows, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.out = (char*)y, A.out_stride = y_stride, A.out_type = y_dtype, A.weight = weight, A.bias = bias, A.eps = eps, A.act = act;
     A.mean = mean_out, A.rstd = rstd_out;
+    A.join_there = P.join_there, A.joins = P.split && P.join_there ? joins_of(P, A) : 0;
     const hipStream_t st = (hipStream_t)stream;
+    const bool many = P.tile_blocks > 1;
     if (dtype == FG_F32)
-        forward<FG_F32>(P, A, st);
+        many ? forward<FG_F32, true>(P, A, st) : forward<FG_F32, false>(P, A, st);
     else if (dtype == FG_F16)
-        forward<FG_F16>(P, A, st);
+        many ? forward<FG_F16, true>(P, A, st) : forward<FG_F16, false>(P, A, st);
     else
-        forward<FG_BF16>(P, A, st);
+        many ? forward<FG_BF16, true>(P, A, st) : forward<FG_BF16, false>(P, A, st);
     FG_LAUNCH_CHECK("group_norm_kernel");
     return FG_OK;
 }
@@ -726,7 +887,10 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     GnArgs A = args_of(P, W, order_dev, offsets_dev, work ? max_rows : 0, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.dy = (const char*)dy, A.dy_stride = dy_stride, A.out = (char*)dx, A.out_stride = dx_stride, A.weight = weight, A.bias = bias;
     A.act = act, A.mean = const_cast<float*>(mean), A.rstd = const_cast<float*>(rstd);
+    A.dw = dw_dev, A.db = db_dev;
     if (!dw_dev && !db_dev) A.columns = nullptr;
+    A.join_there = 1, A.joins = work && P.split ? joins_of(P, A) : 0;      // (beside the sums of dw and db)
+    if (!work) A.chunks = 0;
     const hipStream_t st = (hipStream_t)stream;
 #define FG_GN(X) (grad_dtype == FG_F32 ? backward<X, FG_F32>(P, A, st) : grad_dtype == FG_F16 ? backward<X, FG_F16>(P, A, st) : backward<X, FG_BF16>(P, A, st))
     if (work) {
@@ -739,9 +903,9 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
         FG_LAUNCH_CHECK("group_norm_backward_kernel");
     }
 #undef FG_GN
-    if (dw_dev || db_dev) {
-        hipLaunchKernelGGL(group_norm_columns_kernel, dim3((unsigned)fg_ceil_div(2 * d, 32)), dim3(GN_THREADS), 0, st, A.columns, work ? P.chunks : 0, d, dw_dev, db_dev);
-        FG_LAUNCH_CHECK("group_norm_columns_kernel");
+    if (!work && A.columns) {
+        hipLaunchKernelGGL((group_norm_join_kernel<FG_F32, true>), dim3((unsigned)sum_blocks(A)), dim3(GN_THREADS), 0, st, A);
+        FG_LAUNCH_CHECK("group_norm_join_kernel");
     }
     return FG_OK;
 }

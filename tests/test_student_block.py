@@ -101,7 +101,7 @@ def test_group_norm_refusals(B):
                                                  ws_bytes=1 << 40), **k})
     for bad, want in ((dict(x=None), 1), (dict(y=None), 1), (dict(offsets=None), 1), (dict(offsets=P + 4), 1), (dict(order=P + 2), 1), (dict(ws=None), 1), (dict(ws=P + 8), 1),
                       (dict(ws_bytes=8), 2), (dict(max_rows=-1), 1), (dict(max_rows=1 << 31), 1), (dict(n=-1), 1), (dict(n_groups=0), 1), (dict(n_groups=B.FG_MAX_NORM_GROUPS + 1), 1),
-                      (dict(d=0), 2), (dict(d=B.FG_MAX_NORM_DIM + 1, channel_groups=1, x_stride=1 << 20, y_stride=1 << 20), 2), (dict(channel_groups=0), 2),
+                      (dict(d=0), 2), (dict(d=7, channel_groups=1), 2), (dict(d=B.FG_MAX_NORM_DIM + 1, channel_groups=1, x_stride=1 << 20, y_stride=1 << 20), 2), (dict(channel_groups=0), 2),
                       (dict(channel_groups=7), 2), (dict(channel_groups=128), 2), (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1), (dict(act=5), 1), (dict(dtype=3), 3),
                       (dict(y_dtype=B.FG_BF16), 3), (dict(y_dtype=3), 3), (dict(x_stride=252), 2), (dict(y_stride=16), 2), (dict(x=P + 2), 1), (dict(y=P + 1), 1),
                       (dict(weight=P + 2), 1), (dict(bias=P + 1), 1), (dict(mean_out=P + 1), 1), (dict(rstd_out=P + 2), 1), (dict(y=P, y_stride=512), 1),
@@ -137,7 +137,7 @@ def test_distill_refusals(B):
 
 def test_workspaces_of_a_bound_serve_every_smaller_call(B):
     sizes = sorted({*range(0, 400), *range(1000, 1100), *range(4000, 4200), *range(16300, 16500), *range(30000, 300000, 1000), 10 ** 6, 3 * 10 ** 6, 10 ** 7, 2 ** 31 - 1})
-    for d, blocks in ((1, 1), (8, 1), (88, 8), (100, 5), (100, 100), (256, 32), (1024, 32), (1024, 1), (1024, 1024), (4096, 2), (16384, 1), (16384, 16384), (1500, 3)):
+    for d, blocks in ((9, 1), (8, 8), (88, 8), (100, 5), (100, 100), (256, 32), (1024, 32), (1024, 1), (1024, 1024), (4096, 2), (16384, 1), (16384, 16384), (1500, 3)):
         for need in (B.fg_group_norm_workspace_bytes, B.fg_group_norm_backward_workspace_bytes):
             got = [need(n, 37, d, blocks) for n in sizes]
             assert got == sorted(got) and min(got) > 0
@@ -388,7 +388,7 @@ def test_gated_linear_of_no_rows(B):
 # ---- group norm ----
 
 NORM = [  # dtype, out, n, groups, d, channel groups, act, options
-    ("f32", "f32", 1, 1, 1, 1, "none", ""), ("f32", "f32", 1, 1, 8, 2, "silu", ""), ("f32", "f32", 777, 9, 88, 8, "gelu", ""), ("f32", "f32", 3000, 100, 100, 5, "relu", "empty"),
+    ("f32", "f32", 1, 1, 9, 1, "none", ""), ("f32", "f32", 1, 1, 8, 2, "silu", ""), ("bf16", "bf16", 50, 3, 8827, 1261, "silu", "gather"), ("f32", "f32", 777, 9, 88, 8, "gelu", ""), ("f32", "f32", 3000, 100, 100, 5, "relu", "empty"),
     ("f32", "f32", 2000, 3, 100, 100, "silu", "gather"), ("f32", "f32", 500, 4, 89, 1, "sigmoid", "gather pad noaffine"), ("f32", "f32", 9000, 2, 256, 32, "silu", "gather level"),
     ("bf16", "bf16", 700, 6, 256, 8, "silu", "gather pad"), ("bf16", "f32", 400, 3, 35, 7, "none", "empty"), ("bf16", "bf16", 5000, 2, 1024, 32, "silu", "gather"),
     ("f16", "f16", 6000, 5000, 64, 4, "gelu", "empty"), ("f16", "f32", 300, 2, 514, 2, "silu", "gather level pad"), ("f16", "f16", 90, 2, 4096, 1, "relu", ""),
