@@ -1004,7 +1004,7 @@ fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, con
  *   xh = (x[r, c] - mean[g, j]) * rstd[g, j],  t = dy[r, c] * act'(xh * weight[c] + bias[c])      (ReLU's slope at 0 is 0)
  *   dx[r, c] = rstd[g, j] * (t * weight[c] - m1 - xh * m2),  m1, m2 = the means of t * weight and t * weight * xh over the group's rows and block j
  *   dw[c] = sum over all groups' rows of t * xh,  db[c] = that of t      ([d] float; NULL: not wanted)
- *   dy, dx, grad_dtype                  n rows of d values by position, FG_F32, FG_F16 or FG_BF16; dx may be dy
+ *   dy, dx, grad_dtype                  n rows of d values by position, FG_F32 or `dtype`; dx may be dy
  *   x, mean, rstd, ...                  as in the forward call (mean, rstd its mean_out, rstd_out)
  *   ws_dev, ws_bytes                    >= fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
  * Means in fp64; dw and db in fp32 within and fp64 across ranges of rows; results do not depend on scheduling.

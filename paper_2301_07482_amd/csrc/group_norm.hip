@@ -1,9 +1,9 @@
 // fg_group_norm and its gradients: rows of a group (a graph, a node type), normalised over the rows and blocks of adjacent columns, with an activation.
 //
-// The entries of all groups are a line that is cut into chunks of rows. A group of few rows belongs to the chunk it begins in and is done there:
-// one pass for the sums, one for the result, whose rows come from the caches. A group of many rows is split along the chunks' ends: every chunk leaves the
-// sums of its part, a second launch joins them, a third goes over the rows again. A workgroup takes a chunk and a tile of whole blocks of columns; a
-// thread has pieces of eight adjacent columns (whole ones: the last of a tile overlaps the one before it) and every so many-th row. Which chunk a group lies in is found from the offsets, on the device.
+// A group of few rows belongs to one workgroup (of four wavefronts, or of one where the groups are small): a pass for the sums, a pass for the result, whose rows come
+// from registers where the group is small enough, else from the caches. A group of many rows is split: the entries of all groups are a line that is cut into
+// chunks of rows, every chunk's workgroup leaves the sums of its part, a second launch goes over the rows again with what all parts come to. A workgroup takes a tile of
+// whole blocks of columns; a thread has pieces of eight adjacent columns (whole ones: the last of a tile overlaps the one before it) and every so many-th row.
 #include "activation.h"
 #include "row_list.h"
 #include "row_types.h"
@@ -11,8 +11,8 @@
 
 namespace {
 
-constexpr int GN_THREADS = 256, GN_WAVES = GN_THREADS / 64, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 768, GN_FEW_WORKGROUPS = 128, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
+constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
+constexpr int GN_PLACES = 768, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
 constexpr int GN_AHEAD = 4, GN_AHEAD_BW = 2;      // rows whose reads are on their way together
 
 struct GnArgs {
@@ -20,6 +20,8 @@ struct GnArgs {
     const int64_t* offsets;
     int64_t max_rows, n;
     unsigned int rows, long_rows;      // rows of a chunk; a group of more rows than long_rows is split
+    unsigned int block_inverse;        // 2^32 / block, rounded up
+    int chunks, workers;               // workgroups of a tile that look for parts of split groups in a chunk each, and those that take whole groups
     int n_groups, d, block, blocks, width, pieces;      // columns of a block, blocks of a row, lanes of a row's tile and pieces of a lane
     const char *x, *dy;
     int64_t x_stride, dy_stride, out_stride;
@@ -32,9 +34,8 @@ struct GnArgs {
     int32_t* info;           // [chunks][2]: those groups, -1: none
     float* joined;           // [chunks][blocks][2]: what the parts of the group that begins in the chunk come to
     int join_there;          // ... has been left there by a launch of its own
-    int64_t chunks;
     int joins;               // workgroups that join
-    float* columns;          // [chunks][2][d]: sums for dw and db, or NULL
+    float* columns;          // [workers + chunks][2][d]: sums for dw and db, or NULL
     float *dw, *db;
 };
 
@@ -57,25 +58,44 @@ __device__ __forceinline__ int near(const GnArgs& A, unsigned int target) {
     return lo > 0 ? lo - 1 : 0;
 }
 enum { GN_WHOLE, GN_GOES_ON, GN_BEGINS };
-// The parts of groups that belong to a chunk, in order, the same in all wavefronts: of the group that began before it, if that is split, and of
-// those that begin in it.
+// What a workgroup of a tile has to do: the parts of split groups in its chunk (of one that began before it, of one that begins in it), or every so many-th group
+// that is not split. The same in all wavefronts.
 struct Walk {
     const GnArgs& A;
-    unsigned int c0, c1, from, to;      // entries of the chunk; of the group that this lane looks at
-    int base;
+    bool by_chunk;
+    unsigned int c0, c1, from, to;      // entries of the chunk; of the group that this lane looks at, or of the next group
+    int base;                           // the first lane's group, or the next group
     unsigned long long mask;            // lanes whose groups are still to come
-    __device__ __forceinline__ Walk(const GnArgs& args, unsigned int chunk) : A(args) {
-        c0 = chunk * A.rows;
-        c1 = c0 + A.rows;
-        base = near(A, c0) - 64;
+    __device__ __forceinline__ Walk(const GnArgs& args, int number) : A(args) {
+        by_chunk = number >= A.workers;
         mask = 0;
-        from = 0;
-        to = 0;
+        from = to = 0;
+        if (by_chunk) {
+            c0 = (number - A.workers) * A.rows;
+            c1 = c0 + A.rows;
+            base = near(A, c0) - 64;
+        } else {
+            base = number;
+            look();
+        }
     }
-    // The next part: group, first entry and end, which of the three. empty(group): by one lane of the first wavefront, for every group without entries that
-    // lies here
-    template <typename Empty>
-    __device__ __forceinline__ bool next(int& g, unsigned int& k0, unsigned int& k1, int& which, const Empty& empty) {
+    __device__ __forceinline__ void look() {
+        if (base >= A.n_groups) return;
+        from = offset_of(A, base);
+        to = offset_of(A, base + 1);
+    }
+    // The next part: group, first entry and end, which of the three
+    __device__ __forceinline__ bool next(int& g, unsigned int& k0, unsigned int& k1, int& which) {
+        if (!by_chunk) {
+            for (;;) {
+                if (base >= A.n_groups) return false;
+                g = base, k0 = from, k1 = to > from ? to : from;
+                base += A.workers;
+                look();      // (its offsets are on their way meanwhile)
+                which = GN_WHOLE;
+                if (k1 - k0 <= A.long_rows) return true;
+            }
+        }
         while (!mask) {
             if (__ballot(from >= c1)) return false;
             base += 64;
@@ -86,17 +106,15 @@ struct Walk {
                 from = offset_of(A, i);
                 to = offset_of(A, i + 1);
             }
-            const bool here = from >= c0 && from < c1;
-            if (here && to <= from && fg_wave() == 0) empty(i);
-            mask = __ballot((here && to > from) || (from < c0 && to > c0 && to - from > A.long_rows));
+            mask = __ballot(from < c1 && to > c0 && to > from && to - from > A.long_rows);
         }
         const int l = __ffsll((long long)mask) - 1;
         mask &= mask - 1;
         g = base + l;
         const unsigned int first = (unsigned int)__builtin_amdgcn_readlane((int)from, l), end = (unsigned int)__builtin_amdgcn_readlane((int)to, l);
-        which = first < c0 ? GN_GOES_ON : end - first > A.long_rows ? GN_BEGINS : GN_WHOLE;
+        which = first < c0 ? GN_GOES_ON : GN_BEGINS;
         k0 = first < c0 ? c0 : first;
-        k1 = which != GN_WHOLE && end > c1 ? c1 : end;
+        k1 = end < c1 ? end : c1;
         return true;
     }
 };
@@ -109,15 +127,16 @@ __device__ __forceinline__ int position(const GnArgs& A, unsigned int k) {
 struct Tile {
     int c0, cols, block0, n_blocks, p, side, sides;      // columns, blocks; piece and row of the thread, rows side by side
 };
+template <int TH>
 __device__ __forceinline__ Tile tile_of(const GnArgs& A) {
     Tile T;
-    T.block0 = (int)((int64_t)blockIdx.y * A.blocks / gridDim.y);      // (even tiles: none of fewer than a piece's columns)
-    T.n_blocks = (int)((int64_t)(blockIdx.y + 1) * A.blocks / gridDim.y) - T.block0;
+    T.block0 = (int)((int64_t)blockIdx.x * A.blocks / gridDim.x);      // (even tiles: none of fewer than a piece's columns)
+    T.n_blocks = (int)((int64_t)(blockIdx.x + 1) * A.blocks / gridDim.x) - T.block0;
     T.c0 = T.block0 * A.block;
     T.cols = T.n_blocks * A.block;
     T.p = (int)threadIdx.x % A.width;
     T.side = (int)threadIdx.x / A.width;
-    T.sides = GN_THREADS / A.width;
+    T.sides = TH / A.width;
     return T;
 }
 
@@ -155,16 +174,17 @@ __device__ __forceinline__ void store_piece(char* row, const Piece& P, const flo
         }
 }
 
+template <int TH>
 struct Scratch {
-    double wave[GN_WAVES][2 * GN_COLUMNS];      // sums of a wavefront's rows, by column
+    double wave[TH / 64][2 * GN_COLUMNS];      // sums of a wavefront's rows, by column
     float from[GN_COLUMNS];                     // what they are measured from
     float stats[GN_COLUMNS][2];                 // of a block: mean and rstd, or the gradient's two means
-    int rows[GN_WAVES];
+    int rows[TH / 64];
 };
 // The sums s[e], q[e] of a thread's columns (MANY) or s[0], q[0] of all it has seen, over the rows that a wavefront has side by side, and the number of rows;
 // they are there after the workgroup's next barrier.
-template <bool MANY, typename V>
-__device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows) {
+template <int TH, bool MANY, typename V>
+__device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch<TH>& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows) {
     constexpr int N = MANY ? 8 : 1;
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -187,60 +207,79 @@ __device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scrat
         S.wave[fg_wave()][0] = (double)s[0], S.wave[fg_wave()][GN_COLUMNS] = (double)q[0];
     }
 }
-__device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch& S) {
+template <int TH>
+__device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch<TH>& S) {
     int all = 0;
 #pragma unroll
-    for (int w = 0; w < GN_WAVES; ++w) all += S.rows[w];
+    for (int w = 0; w < TH / 64; ++w) all += S.rows[w];
     return all / A.width;      // (every lane of a row has counted it)
 }
 // done(block of the tile, s, q) by one thread of every block, of the sums over its columns; column(c, s, q) makes of a column's what is to be added
-template <bool MANY, typename Column, typename Done>
-__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const Scratch& S, const Column& column, const Done& done) {
+template <int TH, bool MANY, typename Column, typename Done>
+__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const Scratch<TH>& S, const Column& column, const Done& done) {
     const auto both = [&](int c, double& a, double& b) {
         double s = 0.0, q = 0.0;
 #pragma unroll
-        for (int w = 0; w < GN_WAVES; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
+        for (int w = 0; w < TH / 64; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
         column(c, s, q);
         a += s, b += q;
     };
     double a = 0.0, b = 0.0;
     if constexpr (MANY) {
         int lanes = 1;      // of a block
-        while (lanes < 64 && lanes * 2 * T.n_blocks <= GN_THREADS) lanes *= 2;
-        const int j = (int)threadIdx.x / lanes, l = (int)threadIdx.x % lanes;
-        if (j < T.n_blocks)
-            for (int c = j * A.block + l; c < (j + 1) * A.block; c += lanes) both(c, a, b);
-        for (int off = lanes >> 1; off > 0; off >>= 1) {
-            a += __shfl_xor(a, off, 64);
-            b += __shfl_xor(b, off, 64);
+        while (lanes < 64 && lanes * 2 * T.n_blocks <= TH) lanes *= 2;
+        for (int j0 = 0; j0 < T.n_blocks; j0 += TH / lanes) {
+            const int j = j0 + (int)threadIdx.x / lanes, l = (int)threadIdx.x % lanes;
+            a = b = 0.0;
+            if (j < T.n_blocks)
+                for (int c = j * A.block + l; c < (j + 1) * A.block; c += lanes) both(c, a, b);
+            for (int off = lanes >> 1; off > 0; off >>= 1) {
+                a += __shfl_xor(a, off, 64);
+                b += __shfl_xor(b, off, 64);
+            }
+            if (j < T.n_blocks && l == 0) done(j, a, b);
         }
-        if (j < T.n_blocks && l == 0) done(j, a, b);
     } else if (threadIdx.x == 0) {
         both(0, a, b);
         done(0, a, b);
     }
 }
-__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, unsigned int chunk, int which, int j, double s, double q, int rows) {
+__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, int chunk, int which, int j, double s, double q, int rows) {
     double* to = A.part + ((int64_t)(chunk * 2 + (which == GN_BEGINS)) * A.blocks + T.block0 + j) * 3;
     to[0] = s, to[1] = q, to[2] = (double)rows;
 }
-__device__ __forceinline__ void note(const GnArgs& A, unsigned int chunk, int goes_on, int begins) {
-    if (threadIdx.x == 0 && blockIdx.y == 0 && A.info) A.info[chunk * 2] = goes_on, A.info[chunk * 2 + 1] = begins;
+__device__ __forceinline__ void note(const GnArgs& A, int chunk, int goes_on, int begins) {
+    if (threadIdx.x == 0 && blockIdx.x == 0 && chunk >= 0) A.info[chunk * 2] = goes_on, A.info[chunk * 2 + 1] = begins;
 }
 __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
     if (type == FG_F32) return ((const float*)p)[i];
     const unsigned short v = ((const unsigned short*)p)[i];
     return type == FG_BF16 ? __uint_as_float((unsigned int)v << 16) : (float)__builtin_bit_cast(_Float16, v);
 }
+// the block of a tile's column
+__device__ __forceinline__ int block_of(const GnArgs& A, int c) { return A.block == 1 ? c : (int)__umulhi((unsigned int)c, A.block_inverse); }
 // what a block's values are measured from: its first value in the group's first row (0 where that row does not exist)
 __device__ __forceinline__ float level(const GnArgs& A, int type, int g, int block) {
     const int r = position(A, offset_of(A, g));
     return r >= 0 ? element(A.x + (int64_t)r * A.x_stride, type, (int64_t)block * A.block) : 0.f;
 }
+// 1 / x and 1 / sqrt(x) to within a few steps of 2^-52: the hardware's estimates and Newton's steps (a division and a root take longer than the rest of a
+// small group's statistics)
+__device__ __forceinline__ double reciprocal(double x) {
+    double r = __builtin_amdgcn_rcp(x);
+    r = fma(fma(-x, r, 1.0), r, r);
+    return fma(fma(-x, r, 1.0), r, r);
+}
+__device__ __forceinline__ double reciprocal_root(double x) {
+    double r = __builtin_amdgcn_rsq(x);
+    if (!(x > 0.0 && x < INFINITY)) return r;
+    r = fma(fma(-x * r, r, 1.0), 0.5 * r, r);
+    return fma(fma(-x * r, r, 1.0), 0.5 * r, r);
+}
 __device__ __forceinline__ void mean_rstd(const GnArgs& A, float from, double s, double q, double rows, float& mean, float& rstd) {
-    const double size = rows > 0.0 ? rows * A.block : 1.0, m = s / size, v = q / size - m * m;
+    const double per = reciprocal(rows > 0.0 ? rows * A.block : 1.0), m = s * per, v = q * per - m * m;
     mean = (float)((double)from + m);
-    rstd = (float)(1.0 / sqrt((v > 0.0 || !(v == v) ? v : 0.0) + (double)A.eps));
+    rstd = (float)reciprocal_root((v > 0.0 || !(v == v) ? v : 0.0) + (double)A.eps);
 }
 __device__ __forceinline__ void put_statistics(const GnArgs& A, const Tile& T, int g, int j, float mean, float rstd) {
     const int64_t at = (int64_t)g * A.blocks + T.block0 + j;
@@ -294,8 +333,8 @@ __device__ __forceinline__ void for_rows(const GnArgs& A, const Tile& T, unsigne
 }
 
 // y of the entries [k0, k1) with the blocks' mean and rstd in S.stats. held: the sets `now`, v are all of them and there already
-template <int T_, bool MANY>
-__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
+template <int TH, int T_, bool MANY>
+__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch<TH>& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
                                           fg_piece<T_> (&v)[GN_AHEAD]) {
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
@@ -304,7 +343,7 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
         affine(A, T, P.c, w, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = MANY ? (P.c + e) / A.block : 0;
+            const int j = MANY ? block_of(A, P.c + e) : 0;
             mean[e] = S.stats[j][0], w[e] *= S.stats[j][1];
         }
         const auto finish = [&](int u, int r) {
@@ -334,18 +373,19 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
     }
 }
 
-template <int T_, bool MANY>
-__global__ __launch_bounds__(GN_THREADS, 3) void group_norm_kernel(GnArgs A) {
+template <int TH, int T_, bool MANY>
+__global__ __launch_bounds__(TH, 3) void group_norm_kernel(GnArgs A) {
     constexpr int N = MANY ? 8 : 1;
-    __shared__ Scratch S;
-    const Tile T = tile_of(A);
-    const unsigned int chunk = blockIdx.x;
+    __shared__ Scratch<TH> S;
+    const Tile T = tile_of<TH>(A);
+    const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
     unsigned int k0, k1;
-    const auto empty = [&](int i) {
-        for (int j = 0; j < T.n_blocks; ++j) put_statistics(A, T, i, j, 0.f, (float)(1.0 / sqrt((double)A.eps)));
-    };
-    for (Walk W(A, chunk); W.next(g, k0, k1, which, empty);) {
+    for (Walk W(A, blockIdx.y); W.next(g, k0, k1, which);) {
+        if (k0 == k1) {      // a group without rows
+            for (int j = threadIdx.x; j < T.n_blocks; j += TH) put_statistics(A, T, g, j, 0.f, (float)reciprocal_root((double)A.eps));
+            continue;
+        }
         double s[N] = {}, q[N] = {};
         int rows = 0, now[GN_AHEAD];
         fg_piece<T_> v[GN_AHEAD];
@@ -382,14 +422,14 @@ __global__ __launch_bounds__(GN_THREADS, 3) void group_norm_kernel(GnArgs A) {
                     }
                 });
         }
-        leave_sums<MANY>(A, T, S, s, q, rows);
+        leave_sums<TH, MANY>(A, T, S, s, q, rows);
         __syncthreads();
         rows = rows_of(A, S);
-        block_sums<MANY>(
+        block_sums<TH, MANY>(
             A, T, S,
             [&](int c, double& a, double& b) {      // from the column's level to the block's
                 if constexpr (MANY) {
-                    const double up = (double)S.from[c] - (double)S.from[c / A.block * A.block];
+                    const double up = (double)S.from[c] - (double)S.from[block_of(A, c) * A.block];
                     b += up * (2.0 * a + rows * up);
                     a += rows * up;
                 }
@@ -403,7 +443,7 @@ __global__ __launch_bounds__(GN_THREADS, 3) void group_norm_kernel(GnArgs A) {
             });
         __syncthreads();      // (the sums have been read: the next group's may be left there, and its statistics behind the next barrier)
         if (which == GN_WHOLE)
-            normalise<T_, MANY>(A, T, S, k0, k1, held, now, v);
+            normalise<TH, T_, MANY>(A, T, S, k0, k1, held, now, v);
         else
             (which == GN_BEGINS ? begins : goes_on) = g;
     }
@@ -430,8 +470,8 @@ __device__ __forceinline__ void joined(const GnArgs& A, int g, unsigned int begi
     double s, q, rows;
     join(A, g, begin, block, s, q, rows);
     if constexpr (BACKWARD) {
-        const double size = rows > 0.0 ? rows * A.block : 1.0;
-        a = (float)(s / size), b = (float)(q / size);
+        const double per = reciprocal(rows > 0.0 ? rows * A.block : 1.0);
+        a = (float)(s * per), b = (float)(q * per);
     } else {
         mean_rstd(A, level(A, T_, g, block), s, q, rows, a, b);
         if (write && fg_lane() == 0) {
@@ -446,7 +486,7 @@ __device__ __forceinline__ void column_sums(const GnArgs& A, int block, double* 
     double s = 0.0;
     if (c < 2 * A.d)
 #pragma unroll 8
-        for (int64_t i = threadIdx.x >> 5; i < A.chunks; i += GN_THREADS / 32) s += (double)A.columns[i * 2 * A.d + c];
+        for (int64_t i = threadIdx.x >> 5; i < A.chunks + A.workers; i += GN_THREADS / 32) s += (double)A.columns[i * 2 * A.d + c];
     red[threadIdx.x] = s;
     __syncthreads();
     if (threadIdx.x < 32 && c < 2 * A.d) {
@@ -460,9 +500,9 @@ template <int T_, bool BACKWARD>
 __global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
     __shared__ double red[BACKWARD ? GN_THREADS : 1];
     if (BACKWARD && (int)blockIdx.x >= A.joins) return column_sums(A, (int)blockIdx.x - A.joins, red);
-    const int per_chunk = (A.blocks + GN_WAVES - 1) / GN_WAVES;
+    const int per_chunk = (A.blocks + GN_THREADS / 64 - 1) / (GN_THREADS / 64);
     const unsigned int chunk = blockIdx.x / per_chunk;
-    const int j = (int)(blockIdx.x % per_chunk) * GN_WAVES + fg_wave();
+    const int j = (int)(blockIdx.x % per_chunk) * (GN_THREADS / 64) + fg_wave();
     const int g = A.info[chunk * 2 + 1];
     if (g < 0 || j >= A.blocks) return;
     float a, b;
@@ -472,8 +512,8 @@ __global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
 
 // a chunk's parts of split groups: f(group, first entry, end) with what their parts come to in S.stats
 template <int T_, bool BACKWARD, typename F>
-__device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scratch& S, const F& f) {
-    const unsigned int chunk = gridDim.x - 1 - blockIdx.x, c0 = chunk * A.rows, c1 = c0 + A.rows;      // the last chunks' rows are the likeliest to be cached
+__device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scratch<GN_THREADS>& S, const F& f) {
+    const unsigned int chunk = A.chunks - 1 - blockIdx.y, c0 = chunk * A.rows, c1 = c0 + A.rows;      // the last chunks' rows are the likeliest to be cached
     for (int which = 0; which < 2; ++which) {
         const int g = A.info[chunk * 2 + which];
         if (g < 0) continue;
@@ -484,7 +524,7 @@ __device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scra
                 S.stats[j][0] = p[0], S.stats[j][1] = p[1];
             }
         } else {
-            for (int j = fg_wave(); j < T.n_blocks; j += GN_WAVES) {
+            for (int j = fg_wave(); j < T.n_blocks; j += GN_THREADS / 64) {
                 float a, b;
                 joined<T_, BACKWARD>(A, g, begin, T.block0 + j, which == 1, a, b);
                 if (fg_lane() == 0) S.stats[j][0] = a, S.stats[j][1] = b;
@@ -497,12 +537,12 @@ __device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scra
 }
 template <int T_, bool MANY>
 __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs A) {
-    __shared__ Scratch S;
-    const Tile T = tile_of(A);
+    __shared__ Scratch<GN_THREADS> S;
+    const Tile T = tile_of<GN_THREADS>(A);
     split_parts<T_, false>(A, T, S, [&](int, unsigned int k0, unsigned int k1) {
         int now[GN_AHEAD];
         fg_piece<T_> v[GN_AHEAD];
-        normalise<T_, MANY>(A, T, S, k0, k1, false, now, v);
+        normalise<GN_THREADS, T_, MANY>(A, T, S, k0, k1, false, now, v);
     });
 }
 
@@ -517,7 +557,7 @@ __device__ __forceinline__ void grad_columns(const GnArgs& A, const Tile& T, int
     affine(A, T, c, C.w, C.b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY ? (c + e) / A.block : 0);
+        const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY ? block_of(A, c + e) : 0);
         C.mean[e] = A.mean[at], C.rstd[e] = A.rstd[at];
     }
 }
@@ -562,8 +602,8 @@ __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, in
     }
 }
 // dx of the entries [k0, k1) with the blocks' two means in S.stats
-template <int X, int G, bool MANY>
-__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch& S, int g, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R) {
+template <int TH, int X, int G, bool MANY>
+__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch<TH>& S, int g, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R) {
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
         if (!P.there) break;
@@ -572,7 +612,7 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
         float m1[8], m2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = MANY ? (P.c + e) / A.block : 0;
+            const int j = MANY ? block_of(A, P.c + e) : 0;
             m1[e] = S.stats[j][0], m2[e] = S.stats[j][1];
         }
         gradient_rows<X, G>(A, T, P.c, C, k0, k1, held, R, [&](int r, const float(&xh)[8], float(&t)[8]) {
@@ -586,17 +626,18 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
 // The first pass: a group's sums of t and t * xh by column, which give its two means and dw and db. MANY: the columns' sums over a group's rows
 // meet in LDS, a thread to a column adds them up over the chunk's groups. Else (NP pieces a thread) a thread keeps its columns' sums over all of
 // the chunk's rows, and those of a group over its columns beside them.
-template <int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backward_kernel(GnArgs A) {
-    __shared__ Scratch S;
-    const Tile T = tile_of(A);
-    const unsigned int chunk = blockIdx.x;
+template <int TH, int X, int G, bool MANY, int NP>
+__global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel(GnArgs A) {
+    __shared__ Scratch<TH> S;
+    const Tile T = tile_of<TH>(A);
+    const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
     unsigned int k0, k1;
-    const int mine = (int)threadIdx.x;      // MANY: the column whose sums this thread has
-    double dw = 0.0, db = 0.0;
+    constexpr int MINE = GN_COLUMNS / TH;      // MANY: columns whose sums a thread has
+    double dw[MINE] = {}, db[MINE] = {};
     float dw_piece[MANY ? 1 : NP][8] = {}, db_piece[MANY ? 1 : NP][8] = {};
-    for (Walk W(A, chunk); W.next(g, k0, k1, which, [](int) {});) {
+    for (Walk W(A, blockIdx.y); W.next(g, k0, k1, which);) {
+        if (k0 == k1) continue;
         GradRows<X, G> R;
         const bool held = k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
 #pragma unroll
@@ -614,7 +655,7 @@ __global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backwar
                     for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * xh[e];
                 });
             }
-            leave_sums<true>(A, T, S, s, q, rows);
+            leave_sums<TH, true>(A, T, S, s, q, rows);
         } else {
             double s[1] = {}, q[1] = {};
 #pragma unroll
@@ -634,14 +675,19 @@ __global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backwar
                     });
                 }
             }
-            leave_sums<false>(A, T, S, s, q, rows);
+            leave_sums<TH, false>(A, T, S, s, q, rows);
         }
         __syncthreads();
         rows = rows_of(A, S);
-        if (MANY && mine < T.cols)
+        if constexpr (MANY)
 #pragma unroll
-            for (int w = 0; w < GN_WAVES; ++w) db += S.wave[w][mine], dw += S.wave[w][GN_COLUMNS + mine];
-        block_sums<MANY>(
+            for (int i = 0; i < MINE; ++i) {
+                const int c = (int)threadIdx.x + TH * i;
+                if (c < T.cols)
+#pragma unroll
+                    for (int w = 0; w < TH / 64; ++w) db[i] += S.wave[w][c], dw[i] += S.wave[w][GN_COLUMNS + c];
+            }
+        block_sums<TH, MANY>(
             A, T, S,
             [&](int c, double& a, double& b) {
                 if constexpr (MANY) {
@@ -651,23 +697,27 @@ __global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backwar
             },
             [&](int j, double a, double b) {
                 if (which != GN_WHOLE) return write_part(A, T, chunk, which, j, a, b, rows);
-                const double size = rows > 0 ? (double)rows * A.block : 1.0;
-                S.stats[j][0] = (float)(a / size), S.stats[j][1] = (float)(b / size);
+                const double per = reciprocal(rows > 0 ? (double)rows * A.block : 1.0);
+                S.stats[j][0] = (float)(a * per), S.stats[j][1] = (float)(b * per);
             });
         __syncthreads();
         if (which == GN_WHOLE)
-            input_gradient<X, G, MANY>(A, T, S, g, k0, k1, held, R);
+            input_gradient<TH, X, G, MANY>(A, T, S, g, k0, k1, held, R);
         else
             (which == GN_BEGINS ? begins : goes_on) = g;
     }
     note(A, chunk, goes_on, begins);
     if (!A.columns) return;
-    float* const to = A.columns + (int64_t)chunk * 2 * A.d + T.c0;
+    float* const to = A.columns + (int64_t)blockIdx.y * 2 * A.d + T.c0;
     if constexpr (MANY) {
-        if (mine < T.cols) to[mine] = (float)dw, to[A.d + mine] = (float)db;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int c = (int)threadIdx.x + TH * i;
+            if (c < T.cols) to[c] = (float)dw[i], to[A.d + c] = (float)db[i];
+        }
     } else {
         float* const meet = (float*)S.wave;      // [side][width * 8]
-        static_assert(sizeof(S.wave) >= GN_THREADS * 8 * sizeof(float), "eight columns of every thread");
+        static_assert(sizeof(S.wave) >= TH * 8 * sizeof(float), "eight columns of every thread");
 #pragma unroll
         for (int which_sum = 0; which_sum < 2; ++which_sum) {
             if (T.sides == 1) {
@@ -683,7 +733,7 @@ __global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backwar
                 for (int e = 0; e < 8; ++e)
                     if (e >= P.twice) meet[T.side * A.width * 8 + P.c + e] = which_sum ? db_piece[0][e] : dw_piece[0][e];
                 __syncthreads();
-                for (int c = threadIdx.x; c < T.cols; c += GN_THREADS) {
+                for (int c = threadIdx.x; c < T.cols; c += TH) {
                     float v = 0.f;
                     for (int i = 0; i < T.sides; ++i) v += meet[i * A.width * 8 + c];
                     to[which_sum * A.d + c] = v;
@@ -695,23 +745,24 @@ __global__ __launch_bounds__(GN_THREADS, NP > 1 ? 1 : 3) void group_norm_backwar
 // The second pass, on split groups
 template <int X, int G, bool MANY>
 __global__ __launch_bounds__(GN_THREADS, 3) void group_norm_backward_apply_kernel(GnArgs A) {
-    __shared__ Scratch S;
-    const Tile T = tile_of(A);
+    __shared__ Scratch<GN_THREADS> S;
+    const Tile T = tile_of<GN_THREADS>(A);
     split_parts<X, true>(A, T, S, [&](int g, unsigned int k0, unsigned int k1) {
         GradRows<X, G> R;
-        input_gradient<X, G, MANY>(A, T, S, g, k0, k1, false, R);
+        input_gradient<GN_THREADS, X, G, MANY>(A, T, S, g, k0, k1, false, R);
     });
 }
 
-// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block; chunks of rows, with two rows a thread at least, so that
-// all workgroups are on the chip at once, three to a compute unit (a fourth of them in a second turn took as long as all the others). Where that leaves
-// compute units without work, tiles of fewer blocks, and a chunk to each of them. A group whose values in a tile are up to GN_FEW_VALUES is not split.
+// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block. A group whose values in a tile are up to GN_FEW_VALUES is not split.
+// Chunks of rows for the others, with two rows a thread at least, so that all workgroups are on the chip at once, three to a compute unit (a fourth of them in a second
+// turn took as long as all the others). Where there are few groups and rows, tiles of fewer blocks. One wavefront to a workgroup where an average group's rows are up to
+// GN_SMALL_STEPS steps of one.
 struct Plan {
-    int tiles, tile_blocks, width, pieces;
-    int64_t rows, chunks, long_rows;
-    bool split, join_there;
+    int tiles, tile_blocks, width, pieces, threads, workers;
+    int64_t rows, chunks, long_rows;      // chunks 0: no group can be so large that it is split
+    bool join_there;
 };
-Plan plan_of(int64_t max_rows, int d, int blocks) {
+Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks) {
     Plan P;
     const int block = d / blocks, per_tile = GN_COLUMNS / block;
     P.tiles = (int)fg_ceil_div(blocks, per_tile < 1 ? 1 : per_tile);
@@ -723,16 +774,15 @@ Plan plan_of(int64_t max_rows, int d, int blocks) {
         P.width = 1;
         while (P.width < pieces && P.width < GN_THREADS) P.width *= 2;
         places = GN_PLACES / P.tiles, least = 2 * (GN_THREADS / P.width);
-        if (P.tiles * 2 > blocks || blocks / (P.tiles * 2) * block < 8 || (max_rows / least + 1) * P.tiles > GN_FEW_WORKGROUPS) break;
+        if (P.tiles * 2 > blocks || blocks / (P.tiles * 2) * block < 8 || (max_rows / least + n_groups) * P.tiles > GN_FEW_WORKGROUPS) break;
     }
     P.pieces = (int)fg_ceil_div(pieces, P.width);
-    const int64_t even = max_rows / places + 1;
+    const int64_t even = max_rows / places + 1, most = GN_MOST_WORKERS / P.tiles;
     P.rows = even > least ? even : least;
-    const int64_t spread = max_rows * P.tiles / 256 + 2;      // few rows: the groups' beginnings spread over the chip
-    if (spread < P.rows) P.rows = spread;
-    P.chunks = max_rows / P.rows + 1;
     P.long_rows = P.rows > GN_FEW_VALUES / cols ? P.rows : GN_FEW_VALUES / cols;
-    P.split = P.long_rows < max_rows;
+    P.chunks = P.long_rows < max_rows ? max_rows / P.rows + 1 : 0;
+    P.threads = P.width <= 64 && P.pieces == 1 && max_rows / n_groups * P.width <= 64 * GN_SMALL_STEPS ? 64 : GN_THREADS;
+    P.workers = (int)(n_groups < most ? n_groups : most);
     P.join_there = P.chunks * P.tile_blocks > GN_JOIN_HERE;
     return P;
 }
@@ -743,13 +793,13 @@ struct Space {
     size_t part, info, joined, columns;
     size_t total() const { return part + info + joined + columns + 16; }
 };
-Space space_of(int64_t max_rows, int d, int blocks, bool backward) {
+Space space_of(int64_t max_rows, int n_groups, int d, int blocks, bool backward) {
     const int64_t chunks = max_rows < GN_PLACES ? max_rows + 1 : GN_PLACES;      // (two rows to a chunk at least, and no more chunks than places)
     Space W = {};
     W.part = fg_align_up((size_t)chunks * 2 * blocks * 3 * 8, 256);
     W.info = fg_align_up((size_t)chunks * 2 * 4, 256);
     W.joined = fg_align_up((size_t)chunks * blocks * 2 * 4, 256);
-    if (backward) W.columns = (size_t)chunks * 2 * d * 4;
+    if (backward) W.columns = (size_t)(chunks + (n_groups < GN_MOST_WORKERS ? n_groups : GN_MOST_WORKERS)) * 2 * d * 4;
     return W;
 }
 
@@ -777,31 +827,38 @@ GnArgs args_of(const Plan& P, const Space& W, const int32_t* order_dev, const in
     A.n_groups = n_groups, A.d = d, A.block = d / blocks, A.blocks = blocks, A.width = P.width, A.pieces = P.pieces;
     char* ws = (char*)ws_dev;
     A.part = (double*)ws;
-    A.info = P.split ? (int32_t*)(ws + W.part) : nullptr;
-    A.chunks = P.chunks;
+    A.info = (int32_t*)(ws + W.part);
+    A.chunks = (int)P.chunks, A.workers = P.workers;
+    A.block_inverse = (unsigned int)(((1ull << 32) + A.block - 1) / A.block);
     A.joined = (float*)(ws + W.part + W.info);
     A.columns = (float*)(ws + W.part + W.info + W.joined);
     return A;
 }
 
 // workgroups that join the parts of split groups, and those that sum dw and db
-int joins_of(const Plan& P, const GnArgs& A) { return (int)(P.chunks * fg_ceil_div(A.blocks, GN_WAVES)); }
+int joins_of(const Plan& P, const GnArgs& A) { return (int)(P.chunks * fg_ceil_div(A.blocks, GN_THREADS / 64)); }
 int sum_blocks(const GnArgs& A) { return A.columns ? (int)fg_ceil_div(2 * A.d, 32) : 0; }
 
 template <int T, bool MANY>
 void forward(const Plan& P, const GnArgs& A, hipStream_t st) {
-    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles);
-    hipLaunchKernelGGL((group_norm_kernel<T, MANY>), grid, dim3(GN_THREADS), 0, st, A);
-    if (!P.split) return;
+    const dim3 grid((unsigned)P.tiles, (unsigned)(P.chunks + P.workers)), parts((unsigned)P.tiles, (unsigned)P.chunks);      // (the tiles of the same rows side by side)
+    if (P.threads == 64)
+        hipLaunchKernelGGL((group_norm_kernel<64, T, MANY>), grid, dim3(64), 0, st, A);
+    else
+        hipLaunchKernelGGL((group_norm_kernel<GN_THREADS, T, MANY>), grid, dim3(GN_THREADS), 0, st, A);
+    if (P.chunks == 0) return;
     if (A.joins) hipLaunchKernelGGL((group_norm_join_kernel<T, false>), dim3((unsigned)A.joins), dim3(GN_THREADS), 0, st, A);
-    hipLaunchKernelGGL((group_norm_apply_kernel<T, MANY>), grid, dim3(GN_THREADS), 0, st, A);
+    hipLaunchKernelGGL((group_norm_apply_kernel<T, MANY>), parts, dim3(GN_THREADS), 0, st, A);
 }
 template <int X, int G, bool MANY, int NP>
 void backward_pass(const Plan& P, const GnArgs& A, hipStream_t st) {
-    const dim3 grid((unsigned)P.chunks, (unsigned)P.tiles);
-    hipLaunchKernelGGL((group_norm_backward_kernel<X, G, MANY, NP>), grid, dim3(GN_THREADS), 0, st, A);
+    const dim3 grid((unsigned)P.tiles, (unsigned)(P.chunks + P.workers)), parts((unsigned)P.tiles, (unsigned)P.chunks);
+    if (NP == 1 && P.threads == 64)
+        hipLaunchKernelGGL((group_norm_backward_kernel<64, X, G, MANY, 1>), grid, dim3(64), 0, st, A);
+    else
+        hipLaunchKernelGGL((group_norm_backward_kernel<GN_THREADS, X, G, MANY, NP>), grid, dim3(GN_THREADS), 0, st, A);
     if (const int sums = A.joins + sum_blocks(A)) hipLaunchKernelGGL((group_norm_join_kernel<X, true>), dim3((unsigned)sums), dim3(GN_THREADS), 0, st, A);
-    if (P.split) hipLaunchKernelGGL((group_norm_backward_apply_kernel<X, G, MANY>), grid, dim3(GN_THREADS), 0, st, A);
+    if (P.chunks) hipLaunchKernelGGL((group_norm_backward_apply_kernel<X, G, MANY>), parts, dim3(GN_THREADS), 0, st, A);
 }
 template <int X, int G>
 void backward(const Plan& P, const GnArgs& A, hipStream_t st) {
@@ -819,7 +876,7 @@ extern "C" size_t fg_group_norm_workspace_bytes(int64_t max_rows, int32_t n_grou
     if (max_rows < 0 || max_rows > INT32_MAX || n_groups < 1 || n_groups > FG_MAX_NORM_GROUPS || d < 8 || d > FG_MAX_NORM_DIM || channel_groups < 1 || channel_groups > d ||
         d % channel_groups)
         return 0;
-    return space_of(max_rows, d, channel_groups, false).total();
+    return space_of(max_rows, n_groups, d, channel_groups, false).total();
 }
 
 extern "C" fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows,
@@ -838,14 +895,14 @@ extern "C" fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t
     if (x == y && x && (y_dtype != dtype || y_stride != x_stride)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: y over x has its type and stride", who);
     if (((uintptr_t)weight | (uintptr_t)bias | (uintptr_t)mean_out | (uintptr_t)rstd_out) & 3)
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: weight, bias, mean or rstd is not aligned", who);
-    const Space W = space_of(max_rows, d, channel_groups, false);
+    const Space W = space_of(max_rows, n_groups, d, channel_groups, false);
     FG_TRY(check_space(who, ws_dev, ws_bytes, W.total()));
     fg_clear_error();
-    const Plan P = plan_of(max_rows, d, channel_groups);
+    const Plan P = plan_of(max_rows, n_groups, d, channel_groups);
     GnArgs A = args_of(P, W, order_dev, offsets_dev, max_rows, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.out = (char*)y, A.out_stride = y_stride, A.out_type = y_dtype, A.weight = weight, A.bias = bias, A.eps = eps, A.act = act;
     A.mean = mean_out, A.rstd = rstd_out;
-    A.join_there = P.join_there, A.joins = P.split && P.join_there ? joins_of(P, A) : 0;
+    A.join_there = P.join_there, A.joins = P.join_there ? joins_of(P, A) : 0;
     const hipStream_t st = (hipStream_t)stream;
     const bool many = P.tile_blocks > 1;
     if (dtype == FG_F32)
@@ -860,7 +917,7 @@ extern "C" fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t
 
 extern "C" size_t fg_group_norm_backward_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups) {
     if (fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups) == 0) return 0;
-    return space_of(max_rows, d, channel_groups, true).total();
+    return space_of(max_rows, n_groups, d, channel_groups, true).total();
 }
 
 extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* x, int64_t x_stride, fg_dtype_t dtype,
@@ -870,7 +927,8 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
                                               size_t ws_bytes, void* stream) {
     const char* who = "fg_group_norm_backward";
     const int e = fg_dtype_size(dtype), ge = fg_dtype_size(grad_dtype);
-    if (!e || !ge) FG_FAIL(FG_ERR_DTYPE, "%s: unknown element type", who);
+    if (!e) FG_FAIL(FG_ERR_DTYPE, "%s: unknown element type %d", who, (int)dtype);
+    if (grad_dtype != dtype && grad_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: the gradients are of the type of x or fp32", who);
     FG_TRY(check_norm(who, order_dev, offsets_dev, max_rows, n_groups, n, d, channel_groups, act));
     const bool work = max_rows > 0 && n > 0;
     if (work && (!dy || !x || !mean || !rstd || !dx)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: dy, x, mean, rstd and dx must not be NULL", who);
@@ -880,29 +938,27 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     if (dx == dy && dx && dx_stride != dy_stride) FG_FAIL(FG_ERR_INVALID_ARG, "%s: dx over dy has its stride", who);
     if (((uintptr_t)weight | (uintptr_t)bias | (uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dw_dev | (uintptr_t)db_dev) & 3)
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: weight, bias, mean, rstd, dw or db is not aligned", who);
-    const Space W = space_of(max_rows, d, channel_groups, true);
+    const Space W = space_of(max_rows, n_groups, d, channel_groups, true);
     FG_TRY(check_space(who, ws_dev, ws_bytes, W.total()));
     fg_clear_error();
-    const Plan P = plan_of(max_rows, d, channel_groups);
+    const Plan P = plan_of(max_rows, n_groups, d, channel_groups);
     GnArgs A = args_of(P, W, order_dev, offsets_dev, work ? max_rows : 0, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.dy = (const char*)dy, A.dy_stride = dy_stride, A.out = (char*)dx, A.out_stride = dx_stride, A.weight = weight, A.bias = bias;
     A.act = act, A.mean = const_cast<float*>(mean), A.rstd = const_cast<float*>(rstd);
     A.dw = dw_dev, A.db = db_dev;
     if (!dw_dev && !db_dev) A.columns = nullptr;
-    A.join_there = 1, A.joins = work && P.split ? joins_of(P, A) : 0;      // (beside the sums of dw and db)
-    if (!work) A.chunks = 0;
+    A.join_there = 1, A.joins = work ? joins_of(P, A) : 0;      // (beside the sums of dw and db)
+    if (!work) A.chunks = A.workers = 0;
     const hipStream_t st = (hipStream_t)stream;
-#define FG_GN(X) (grad_dtype == FG_F32 ? backward<X, FG_F32>(P, A, st) : grad_dtype == FG_F16 ? backward<X, FG_F16>(P, A, st) : backward<X, FG_BF16>(P, A, st))
     if (work) {
         if (dtype == FG_F32)
-            FG_GN(FG_F32);
+            backward<FG_F32, FG_F32>(P, A, st);
         else if (dtype == FG_F16)
-            FG_GN(FG_F16);
+            grad_dtype == FG_F32 ? backward<FG_F16, FG_F32>(P, A, st) : backward<FG_F16, FG_F16>(P, A, st);
         else
-            FG_GN(FG_BF16);
+            grad_dtype == FG_F32 ? backward<FG_BF16, FG_F32>(P, A, st) : backward<FG_BF16, FG_BF16>(P, A, st);
         FG_LAUNCH_CHECK("group_norm_backward_kernel");
     }
-#undef FG_GN
     if (!work && A.columns) {
         hipLaunchKernelGGL((group_norm_join_kernel<FG_F32, true>), dim3((unsigned)sum_blocks(A)), dim3(GN_THREADS), 0, st, A);
         FG_LAUNCH_CHECK("group_norm_join_kernel");

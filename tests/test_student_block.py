@@ -111,7 +111,7 @@ def test_group_norm_refusals(B):
                                                         act=B.FG_ACT_SILU, order=None, offsets=P, max_rows=10, n_groups=4, n=10, d=64, channel_groups=8, dx=P + 4096,
                                                         dx_stride=256, dw=P, db=P, ws=P, ws_bytes=1 << 40), **k})
     for bad, want in ((dict(dy=None), 1), (dict(x=None), 1), (dict(mean=None), 1), (dict(rstd=None), 1), (dict(dx=None), 1), (dict(offsets=None), 1), (dict(ws=None), 1),
-                      (dict(ws_bytes=64), 2), (dict(grad_dtype=3), 3), (dict(dtype=4), 3), (dict(channel_groups=5), 2), (dict(dy_stride=4), 2), (dict(dx_stride=128), 2),
+                      (dict(ws_bytes=64), 2), (dict(grad_dtype=3), 3), (dict(grad_dtype=B.FG_BF16), 3), (dict(dtype=4), 3), (dict(channel_groups=5), 2), (dict(dy_stride=4), 2), (dict(dx_stride=128), 2),
                       (dict(dw=P + 1), 1), (dict(mean=P + 2), 1), (dict(dx=P, dx_stride=512), 1), (dict(act=-2), 1), (dict(n_groups=-1), 1)):
         assert refused(B, bw, **bad) == want, bad
     for need in (B.fg_group_norm_workspace_bytes, B.fg_group_norm_backward_workspace_bytes):
@@ -454,7 +454,7 @@ def test_group_norm(B, dtype, out, n, n_groups, d, blocks, name, options):
 @pytest.mark.parametrize("dtype, out, n, n_groups, d, blocks, name, options", NORM)
 def test_group_norm_backward(B, dtype, out, n, n_groups, d, blocks, name, options, grad):
     if grad == "same":
-        grad = dtype if dtype != "f32" else "bf16"
+        grad = dtype
     r, pad, order, offsets, x, w, b = norm_inputs(dtype, n, n_groups, d, options)
     dy = values(r, n, d, grad, pad)
     parts = R.members(order, offsets.tolist(), n)
