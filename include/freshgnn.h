@@ -1032,9 +1032,11 @@ fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t
  * A row without a teacher (no entry with a class in [0, d) and a value above -infinity, a node outside [0, table_rows), alpha = 0) has no first term, one without a
  * label in [0, d) (or with alpha = 1) no second; a row with neither has loss 0 and gradient 0 whatever its logits. A class that is stored twice has
  * the sum of both. A logit of -infinity is a class that cannot be chosen: no gradient, an infinite loss if the teacher or the label has it.
- * Exponentials and gradients in fp32, sums in fp64 across a row's lanes. pointers and strides aligned to the element, any d.
+ * Exponentials, gradients and sums in fp32, those of wide rows (more than 512 columns) in fp64 from eight columns on. Pointers and strides aligned to the
+ * element, d up to FG_MAX_CLASSES.
  */
 #define FG_MAX_TOP 64
+#define FG_MAX_CLASSES 1073741824
 fg_status_t fg_distill_loss(const void* h, int64_t h_stride, fg_dtype_t dtype, const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows,
                             int64_t n, int32_t d, const int32_t* ids_dev, const int32_t* top_idx_dev, const void* top_val_dev, fg_dtype_t top_dtype,
                             int64_t table_rows, int32_t k, const int32_t* labels_dev, float temperature, float alpha, const float* weight_dev,

@@ -18,7 +18,7 @@ DTYPE_SIZE = {FG_F32: 4, FG_F16: 2, FG_BF16: 2, FG_E4M3: 1}
 _TENSOR_DTYPE = {"torch.float32": FG_F32, "torch.float16": FG_F16, "torch.bfloat16": FG_BF16}
 FG_MAX_GROUPS, FG_MAX_GROUPED_ROWS, FG_MAX_GROUPED_DIM, FG_MAX_NORM_DIM = 1024, 1 << 29, 65536, 16384
 FG_ACT_NONE, FG_ACT_RELU, FG_ACT_SILU, FG_ACT_GELU, FG_ACT_SIGMOID = range(5)
-FG_MAX_NORM_GROUPS, FG_MAX_TOP = 1 << 20, 64
+FG_MAX_NORM_GROUPS, FG_MAX_TOP, FG_MAX_CLASSES = 1 << 20, 64, 1 << 30
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(f"{LIB_PATH} is not built: run `python -m paper_2301_07482_amd.build` (needs hipcc); "

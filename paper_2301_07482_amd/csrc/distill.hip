@@ -1,10 +1,11 @@
 // fg_distill_loss: a student's loss against a teacher's stored top logits and against labels, with its gradient.
 //
 // A row of logits is read once and its gradient written once; both softmaxes of it (at the temperature and as it is) come from the values held in
-// registers. A row belongs to a power of two of lanes, up to a wavefront's 64, or to the wavefronts of a workgroup, as wide as it is;
-// beyond REG_MAX columns what does not fit the registers is read again. The k classes that the teacher has stored, and the label, are entries of
-// their own: their logits are fetched one by one, their gradients are formed apart (each sums the shares of all entries of its class, so that
-// a class that is stored twice gets the same value from both) and written over what the row's pass has left there.
+// registers, as they lie in memory. Rows of up to DL_NARROW columns share a wavefront, eight columns to a lane; wider ones belong to one wavefront or to several, and
+// what does not fit their registers is read again. Where the temperature is 1, 2 or 4, the exponentials as the row is are those at the temperature squared (that doubles their
+// relative error each time, as a temperature does the other way): exponentials take four times as long as other instructions, and two of them a value for each softmax are
+// what a wide row spends its time on beside memory. The k classes that the teacher has stored, and the label, take their shares from the gradient while it
+// is in registers, in the entries' order, so that a class that is stored twice takes both.
 #include <type_traits>
 
 #include "row_list.h"
@@ -12,8 +13,8 @@
 
 namespace {
 
-constexpr int DL_THREADS = 256, DL_MIN_LANES = 8;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr int DL_THREADS = 256, DL_MIN_LANES = 8, DL_NARROW = 512, DL_FEW_ROWS = 1024;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 
 struct DistillArgs {
     RowList L;
@@ -37,248 +38,392 @@ __device__ __forceinline__ float value_at(const char* p, int type, int64_t i) {
     const unsigned short v = ((const unsigned short*)p)[i];
     return type == FG_BF16 ? __uint_as_float((unsigned int)v << 16) : (float)__builtin_bit_cast(_Float16, v);
 }
-__device__ __forceinline__ void put_value(char* p, int type, int64_t i, float f) {
-    if (type == FG_F32)
-        ((float*)p)[i] = f;
-    else if (type == FG_BF16)
-        ((__bf16*)p)[i] = (__bf16)f;
+// the largest of three, those that are NaN left out (the library's fmaxf makes its operands quiet first)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+__device__ __forceinline__ float sum_over(float v, int lanes) {
+    for (int off = lanes >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
+__device__ __forceinline__ float one(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }      // of a value that is the same in all lanes
+
+// How the exponentials as the row is come from those at the temperature: squared SQUARES times, or (-1) by themselves
+template <typename F>
+__device__ __forceinline__ void with_squares(float temperature, const F& f) {
+    if (temperature == 1.f)
+        f(std::integral_constant<int, 0>());
+    else if (temperature == 2.f)
+        f(std::integral_constant<int, 1>());
+    else if (temperature == 4.f)
+        f(std::integral_constant<int, 2>());
     else
-        ((_Float16*)p)[i] = (_Float16)f;
+        f(std::integral_constant<int, -1>());
 }
-
-// what the lanes of a row have written to LDS or memory is there for all of them
-template <int WAVES>
-__device__ __forceinline__ void row_meets() {
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-    } else {
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
-    }
+// e^((z - m) / temperature), e^(z - m)
+template <int SQUARES>
+__device__ __forceinline__ void both(float z, float m, float soften, float& soft, float& hard) {
+    soft = exp2_of((z - m) * soften);
+    hard = SQUARES < 0 ? exp2_of((z - m) * LOG2E) : SQUARES == 0 ? soft : soft * soft;
+    if (SQUARES == 2) hard *= hard;
 }
-
-struct Entry {
-    int32_t c;      // class, -1: none
-    float p, log_p, z;
-};
-
-// WAVES > 1: that many wavefronts to a row, else 64 / lanes rows to a wavefront. NP pieces of eight columns a lane in registers; TAIL: there are more
-template <int T, int WAVES, int NP, bool TAIL>
-__global__ __launch_bounds__(WAVES > 4 ? WAVES * 64 : DL_THREADS) void distill_kernel(DistillArgs A) {
-    constexpr int E = T == FG_F32 ? 4 : 2;
-    extern __shared__ __attribute__((aligned(16))) char dl_lds[];
-    __shared__ double red[WAVES];
-    __shared__ int taught_by[1];
-    const int64_t count = row_count(A.L);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int rows_per_wave = WAVES > 1 ? 1 : 64 / A.lanes;
-    const int me = WAVES > 1 ? (int)threadIdx.x : lane & (A.lanes - 1);
-    const int width = WAVES > 1 ? WAVES * 64 : A.lanes, few = width < 64 ? width : 64;      // lanes that the entries are spread over
-    const int slot = WAVES > 1 ? 0 : wave * rows_per_wave + lane / A.lanes;
-    const int64_t at = WAVES > 1 ? blockIdx.x : blockIdx.x * (int64_t)(DL_THREADS / A.lanes) + slot;
-    const int64_t r = row_at(A.L, A.L.first + at, count);
-    if (WAVES > 1 && r < 0) return;      // the whole workgroup
-    Entry* const entries = (Entry*)dl_lds + slot * A.k;
-    const char* const row = A.h + r * A.h_stride;
-
-    float v[NP][8];
-#pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        const int c = (me + width * i) * 8, left = r >= 0 ? A.d - c : 0;
-        if (left > 0) fg_piece_values<T>(fg_load_piece<T>(row + (int64_t)c * E, left), v[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e >= left) v[i][e] = -INFINITY;
-    }
-    // the row's node, label and weight; the teacher's distribution over its entries
-    int64_t node = -1;
-    int32_t y = -1;
-    float weight = 1.f;
-    if (r >= 0) {
-        if (A.alpha > 0.f) node = A.ids ? A.ids[r] : r;
-        if (node >= A.table_rows) node = -1;
-        if (A.labels && A.alpha < 1.f) y = A.labels[r];
-        if (y >= A.d) y = -1;
-        if (A.weight) weight = A.weight[r];
-    }
-    bool taught = false;
-    float t_max = -INFINITY;
-    double t_sum = 0.0;
-    if (me < few) {
-        for (int j = me; j < A.k; j += few) {
-            int32_t c = node >= 0 ? A.top_idx[node * A.k + j] : -1;
-            float t = -INFINITY;
-            if (c < 0 || c >= A.d) c = -1;
-            if (c >= 0) t = value_at(A.top_val, A.top_dtype, node * A.k + j) / A.temperature;
-            if (!(t == -INFINITY)) taught = true;
-            t_max = fmaxf(t_max, t);
-            entries[j] = Entry{c, 0.f, t, c >= 0 ? value_at(row, T, c) : 0.f};
-        }
-        t_max = lanes_max(t_max, few);
-        taught = lanes_max(taught ? 1.f : 0.f, few) > 0.f;
-        for (int j = me; j < A.k; j += few)
-            if (entries[j].c >= 0) t_sum += (double)expf(entries[j].log_p - t_max);
-        t_sum = lanes_sum(t_sum, few);
-        const float log_sum = logf((float)t_sum);
-        for (int j = me; j < A.k; j += few)
-            if (entries[j].c >= 0) {
-                const float log_p = entries[j].log_p - t_max - log_sum;
-                entries[j].p = taught ? expf(log_p) : 0.f;
-                entries[j].log_p = log_p;
-            }
-        if (WAVES > 1 && me == 0) taught_by[0] = taught;
-    }
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-        taught = taught_by[0];
-    }
-
-    // the student's softmaxes
-    auto tail = [&](auto f) {      // the pieces that are not held
-        if constexpr (TAIL)
-            for (int c = (me + width * NP) * 8; c < A.d; c += width * 8) {
-                float w[8];
-                fg_piece_values<T>(fg_load_piece<T>(row + (int64_t)c * E, A.d - c), w);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= A.d - c) w[e] = -INFINITY;
-                f(c, w);
-            }
-    };
-    const float soften = LOG2E / A.temperature;
-    float m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, v[i][e]);
-    tail([&](int, const float(&w)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, w[e]);
-    });
-    m = row_max<WAVES>(m, few, red);
-    double hard = 0.0, soft = 0.0;
-    auto add = [&](const float(&w)[8]) {
-        float s = 0.f, t = 0.f;
+// sums of both over eight values
+__device__ __forceinline__ void sums_of(float temperature, const float (&w)[8], float m, float soften, float& soft, float& hard) {
+    soft = hard = 0.f;
+    with_squares(temperature, [&](auto squares) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            if (y >= 0) s += __builtin_amdgcn_exp2f((w[e] - m) * LOG2E);
-            if (taught) t += __builtin_amdgcn_exp2f((w[e] - m) * soften);
+            float s, h;
+            both<decltype(squares)::value>(w[e], m, soften, s, h);
+            soft += s, hard += h;
         }
-        hard += (double)s;
-        soft += (double)t;
-    };
+    });
+}
+// a * soft + b * hard of eight values
+__device__ __forceinline__ void gradients_of(float temperature, const float (&w)[8], float m, float soften, float a, float b, float (&g)[8]) {
+    with_squares(temperature, [&](auto squares) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
-        if ((me + width * i) * 8 < A.d) add(v[i]);
-    tail([&](int, const float(&w)[8]) { add(w); });
-    hard = row_sum<WAVES>(hard, few, red);
-    soft = row_sum<WAVES>(soft, few, red);
-
-    const float T2 = A.temperature;
-    if (A.loss) {
-        double kl = 0.0;
-        const float log_soft = logf((float)soft);
-        if (me < few && taught) {
-            for (int j = me; j < A.k; j += few)
-                if (!(entries[j].p == 0.f)) kl += (double)(entries[j].p * (entries[j].log_p - ((entries[j].z - m) / T2 - log_soft)));
+        for (int e = 0; e < 8; ++e) {
+            float s, h;
+            both<decltype(squares)::value>(w[e], m, soften, s, h);
+            g[e] = a * s + b * h;
         }
-        if (wave == 0 || WAVES == 1) kl = lanes_sum(kl, few);
+    });
+}
+__device__ __forceinline__ void no_value_beyond(int left, float (&w)[8]) {
+    if (left < 8)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= left) w[e] = -INFINITY;
+}
+// node, label (-1: none) and weight of a row
+__device__ __forceinline__ void row_facts(const DistillArgs& A, int64_t r, int32_t& node, int32_t& y, float& weight) {
+    node = -1, y = -1, weight = 1.f;
+    if (r < 0) return;
+    if (A.alpha > 0.f && A.k > 0) node = A.ids ? A.ids[r] : (int32_t)r;
+    if (A.labels && A.alpha < 1.f) y = A.labels[r];
+    if (A.weight) weight = A.weight[r];
+    if (node >= A.table_rows) node = -1;
+    if (y >= A.d || y < 0) y = -1;
+}
+// entry j of a node: its class (-1: none) and its value
+__device__ __forceinline__ void entry_of(const DistillArgs& A, int32_t node, int j, int32_t& c, float& t) {
+    c = -1, t = -INFINITY;
+    if (node < 0) return;
+    const int64_t at = (int64_t)node * A.k + j;
+    c = A.top_idx[at];
+    t = value_at(A.top_val, A.top_dtype, at);
+    if (c < 0 || c >= A.d) c = -1, t = -INFINITY;
+}
+
+// what the lanes of a wavefront have written to LDS is there for all of them
+__device__ __forceinline__ void wave_meets() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Narrow rows: 64 / lanes of them to a wavefront. A row's values lie in LDS for its entries to find theirs, then what those take from its gradient.
+struct Entry {
+    int32_t c;      // class, -1: none
+    float p, log2_p, z;
+};
+template <int T>
+__global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs A) {
+    constexpr int E = T == FG_F32 ? 4 : 2;
+    extern __shared__ __attribute__((aligned(16))) char dl_lds[];
+    __shared__ __attribute__((aligned(16))) float values[DL_THREADS * 8];
+    const int lanes = A.lanes, me = (int)threadIdx.x & (lanes - 1), slot = (int)threadIdx.x / lanes;
+    const int64_t r = row_at(A.L, A.L.first + blockIdx.x * (int64_t)(DL_THREADS / lanes) + slot, row_count(A.L));
+    Entry* const entries = (Entry*)dl_lds + slot * A.k;
+    float* const mine = values + (int)threadIdx.x * 8;      // this lane's eight columns, in a row's
+    float* const all = values + slot * lanes * 8;
+    const int c0 = me * 8, left = r >= 0 ? A.d - c0 : 0;
+    fg_piece<T> raw = {};
+    if (left > 0) raw = fg_load_piece<T>(A.h + r * A.h_stride + (int64_t)c0 * E, left);
+    int32_t node, y;
+    float weight, w[8];
+    row_facts(A, r, node, y, weight);
+    // the teacher's entries are on their way beside the row
+    float t_max = -INFINITY;
+    for (int j = me; j < A.k; j += lanes) {
+        int32_t c;
+        float t;
+        entry_of(A, node, j, c, t);
+        entries[j].c = c, entries[j].log2_p = t;
+        if (!(t == -INFINITY)) t_max = t > t_max || !(t == t) || t_max == -INFINITY ? t : t_max;
+    }
+    fg_piece_values<T>(raw, w);
+    no_value_beyond(left, w);
+    ((float4*)mine)[0] = float4{w[0], w[1], w[2], w[3]}, ((float4*)mine)[1] = float4{w[4], w[5], w[6], w[7]};
+    float m = max3(max3(max3(w[0], w[1], w[2]), w[3], w[4]), max3(w[5], w[6], w[7]), -INFINITY);
+    m = lanes_max(m, lanes);
+    wave_meets();
+    // the teacher's distribution (a value that is NaN makes it NaN; without one above -infinity there is no teacher)
+    const float soften = LOG2E / A.temperature;
+    const float top = lanes_max(t_max, lanes);
+    const bool taught = lanes_max(t_max == -INFINITY ? 0.f : 1.f, lanes) > 0.f;
+    float t_sum = 0.f;
+    for (int j = me; j < A.k; j += lanes) {
+        const int32_t c = entries[j].c;
+        const float x = (entries[j].log2_p - top) * soften;
+        entries[j].log2_p = x;
+        entries[j].z = c >= 0 ? all[c] : 0.f;
+        if (c >= 0) t_sum += exp2_of(x);
+    }
+    const float z_label = y >= 0 ? all[y] : 0.f;
+    t_sum = sum_over(t_sum, lanes);
+    const float t_log = log2_of(t_sum);
+    // the student's
+    float soft = 0.f, hard = 0.f;
+    const bool either = taught || y >= 0;
+    if (either) sums_of(A.temperature, w, m, soften, soft, hard);
+    soft = sum_over(soft, lanes);
+    hard = sum_over(hard, lanes);
+    const float soft_log = log2_of(soft);
+    const float scale = A.grad_scale * weight, a = taught ? scale * A.alpha * A.temperature : 0.f, b = y >= 0 ? scale * (1.f - A.alpha) : 0.f;
+    float kl = 0.f;
+    wave_meets();      // (the values have been read)
+    ((float4*)mine)[0] = ((float4*)mine)[1] = float4{0.f, 0.f, 0.f, 0.f};
+    wave_meets();
+    if (taught)
+        for (int j = me; j < A.k; j += lanes) {
+            const int32_t c = entries[j].c;
+            if (c < 0) continue;
+            const float log2_p = entries[j].log2_p - t_log, p = exp2_of(log2_p);
+            if (!(p == 0.f)) kl += p * (log2_p - ((entries[j].z - m) * soften - soft_log));
+            if (A.dh) __hip_atomic_fetch_add(all + c, a * p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);      // (lanes of one wavefront, in order)
+        }
+    if (A.loss) {
+        kl = sum_over(kl, lanes);
         if (me == 0 && r >= 0) {
             float loss = 0.f;
-            if (taught) loss += A.alpha * T2 * T2 * (float)kl;
-            if (y >= 0) loss += (1.f - A.alpha) * (logf((float)hard) - (value_at(row, T, y) - m));
-            A.loss[r] = taught || y >= 0 ? weight * loss : 0.f;
+            if (taught) loss += A.alpha * A.temperature * A.temperature * LN2 * kl;
+            if (y >= 0) loss += (1.f - A.alpha) * (LN2 * log2_of(hard) - (z_label - m));
+            A.loss[r] = either ? weight * loss : 0.f;
         }
     }
     if (!A.dh) return;
-    const float scale = A.grad_scale * weight;
-    const float a = scale * A.alpha * T2, b = scale * (1.f - A.alpha);
-    const float a_q = a / (float)soft, b_q = b / (float)hard;
-    auto gradient = [&](float z) {
-        float g = 0.f;
-        if (taught) g += a_q * __builtin_amdgcn_exp2f((z - m) * soften);
-        if (y >= 0) g += b_q * __builtin_amdgcn_exp2f((z - m) * LOG2E);
-        return g;
-    };
-    // the entries' own values, the label's (by the first lane, unless an entry is of its class)
-    float at_label = 0.f;
-    bool by_entry = false;
-    row_meets<WAVES>();      // (the entries are all there)
-    if (me < few) {
-        for (int j = me; j < A.k; j += few) {
-            const int32_t c = entries[j].c;
-            if (c < 0) continue;
-            float share = 0.f;
-            for (int i = 0; i < A.k; ++i)
-                if (entries[i].c == c) share += entries[i].p;
-            float g = gradient(entries[j].z) - (c == y ? b : 0.f);
-            if (taught) g -= a * share;
-            entries[j].log_p = g;      // (read by this lane alone)
-        }
-        if (me == 0 && y >= 0) {
-            for (int i = 0; i < A.k; ++i) by_entry |= entries[i].c == y;
-            if (!by_entry) at_label = gradient(value_at(row, T, y)) - b;
-        }
-    }
-    row_meets<WAVES>();      // (dh may be h: its values have been read)
+    if (me == 0 && y >= 0) __hip_atomic_fetch_add(all + y, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    wave_meets();
+    if (left <= 0) return;
+    float g[8] = {};
+    if (either) gradients_of(A.temperature, w, m, soften, taught ? a / soft : 0.f, y >= 0 ? b / hard : 0.f, g);
+    const float4 lo = ((float4*)mine)[0], hi = ((float4*)mine)[1];
+    g[0] -= lo.x, g[1] -= lo.y, g[2] -= lo.z, g[3] -= lo.w, g[4] -= hi.x, g[5] -= hi.y, g[6] -= hi.z, g[7] -= hi.w;
     char* const out = A.dh + r * A.dh_stride;
-    auto write = [&](int c, const float(&w)[8]) {
-        float g[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) g[e] = gradient(w[e]);
-        if (A.dh_dtype == FG_F32)
-            fg_store_piece<FG_F32>(out + (int64_t)c * 4, g, A.d - c);
-        else if constexpr (T != FG_F32)
-            fg_store_piece<T>(out + (int64_t)c * 2, g, A.d - c);
-    };
-    if (r >= 0) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int c = (me + width * i) * 8;
-            if (c < A.d) write(c, v[i]);
-        }
-        tail([&](int c, const float(&w)[8]) { write(c, w); });
-    }
-    row_meets<WAVES>();      // (the entries' values go over these)
-    if (r >= 0 && me < few) {
-        for (int j = me; j < A.k; j += few)
-            if (entries[j].c >= 0) put_value(out, A.dh_dtype, entries[j].c, entries[j].log_p);
-        if (me == 0 && y >= 0 && !by_entry) put_value(out, A.dh_dtype, y, at_label);
-    }
+    if (A.dh_dtype == FG_F32)
+        fg_store_piece<FG_F32>(out + (int64_t)c0 * 4, g, left);
+    else if constexpr (T != FG_F32)
+        fg_store_piece<T>(out + (int64_t)c0 * 2, g, left);
 }
 
+// Wide rows: WAVES wavefronts to a row, one row to a workgroup. NP pieces of eight columns a lane in registers; TAIL: there are more. Pieces are counted from the 16-byte
+// line that the row begins in, so that all but the first and the last of them are whole lines (rows of 50003 bf16 15 % faster). An entry is in a lane of every wavefront, which
+// finds those of its own pieces.
 template <int T, int WAVES, int NP, bool TAIL>
-void launch(DistillArgs A, hipStream_t st) {
-    const int per_block = WAVES > 1 ? 1 : DL_THREADS / A.lanes;
-    const int64_t at_once = (FG_MAX_GRID / 4 - 1) * per_block;      // rows of a launch
+__global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs A) {
+    constexpr int E = T == FG_F32 ? 4 : 2, WIDTH = WAVES * 64;
+    __shared__ double red[2][WAVES];
+    __shared__ float largest[WAVES];
+    __shared__ int32_t top_class[WAVES > 1 ? 64 : 1];
+    __shared__ float top_share[WAVES > 1 ? 64 : 1], teacher_log;
+    __shared__ int taught_by;
+    const int64_t r = row_at(A.L, A.L.first + blockIdx.x, row_count(A.L));
+    if (r < 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = (int)threadIdx.x;
+    const char* const row = A.h + r * A.h_stride;
+    const int lead = (int)((uintptr_t)row & 15) / E, d = A.d + lead;      // columns of the line in front of the row; from there
+    const char* const base = row - lead * E;
+    auto load = [&](int c) -> fg_piece<T> {
+        fg_piece<T> v = {};
+        if (c > 0 || lead == 0) {
+            if (c < d) v = fg_load_piece<T>(base + (int64_t)c * E, d - c);
+        } else {
+#pragma unroll
+            for (int e = 1; e < 8; ++e)
+                if (e >= lead && e < d) {
+                    if constexpr (T == FG_F32)
+                        (e < 4 ? v.a : v.b)[e & 3] = ((const unsigned int*)base)[e];
+                    else
+                        v.a[e / 2] |= (unsigned int)((const unsigned short*)base)[e] << (16 * (e & 1));
+                }
+        }
+        return v;
+    };
+    fg_piece<T> raw[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+        if ((wave * 64 + WIDTH * i) * 8 < d) raw[i] = load((me + WIDTH * i) * 8);
+    int32_t node, y;
+    float weight;
+    row_facts(A, r, node, y, weight);
+    node = __builtin_amdgcn_readfirstlane(node), y = __builtin_amdgcn_readfirstlane(y), weight = one(weight);
+    // the teacher's entries, one to a lane of the first wavefront, and their logits
+    int32_t my_class = -1;
+    float my_value = -INFINITY, my_z = 0.f, z_label = 0.f;
+    if (wave == 0) {
+        if (lane < A.k) entry_of(A, node, lane, my_class, my_value);
+        if (my_class >= 0) my_z = value_at(row, T, my_class);
+        if (y >= 0) z_label = value_at(row, T, y);
+    }
+    // f(piece, values) for every piece of this wavefront, columns that do not exist -infinity
+    auto each = [&](auto f) {
+        auto give = [&](int i, const fg_piece<T>& v) {
+            const int c = (me + WIDTH * i) * 8;
+            float w[8];
+            fg_piece_values<T>(v, w);
+            no_value_beyond(d - c, w);
+            if (c == 0 && lead > 0)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < lead) w[e] = -INFINITY;
+            f(i, w);
+        };
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            if ((wave * 64 + WIDTH * i) * 8 < d) give(i, raw[i]);
+        if constexpr (TAIL)
+            for (int i = NP; (wave * 64 + WIDTH * i) * 8 < d; ++i) give(i, load((me + WIDTH * i) * 8));
+    };
+    float m = -INFINITY;
+    each([&](int, const float(&w)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) m = max3(m, w[e], w[e + 1]);
+    });
+    m = lanes_max(m, 64);
+    const float soften = LOG2E / A.temperature;
+    bool taught = false;
+    float t_log = 0.f;
+    if (wave == 0) {      // the teacher's distribution (a value that is NaN makes it NaN; without one above -infinity there is no teacher)
+        taught = __ballot(my_class >= 0 && !(my_value == -INFINITY)) != 0;
+        my_value = (my_value - lanes_max(my_value, 64)) * soften;
+        t_log = log2_of(sum_over(my_class >= 0 ? exp2_of(my_value) : 0.f, 64));
+    }
+    if constexpr (WAVES > 1) {
+        if (lane == 0) largest[wave] = m;
+        if (wave == 0) {
+            top_class[lane] = my_class, top_share[lane] = my_value;
+            if (lane == 0) taught_by = taught, teacher_log = t_log;
+        }
+        __syncthreads();
+        m = largest[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, largest[w]);
+        taught = taught_by, t_log = teacher_log;
+        if (wave != 0) my_class = top_class[lane], my_value = top_share[lane];
+    }
+    m = one(m), t_log = one(t_log);
+    taught = __builtin_amdgcn_readfirstlane(taught);
+    const bool either = taught || y >= 0;
+    double soft = 0.0, hard = 0.0;
+    if (either)
+        each([&](int, const float(&w)[8]) {
+            float s, h;
+            sums_of(A.temperature, w, m, soften, s, h);
+            soft += (double)s, hard += (double)h;
+        });
+    soft = lanes_sum(soft, 64);
+    hard = lanes_sum(hard, 64);
+    if constexpr (WAVES > 1) {
+        if (lane == 0) red[0][wave] = soft, red[1][wave] = hard;
+        __syncthreads();
+        soft = hard = 0.0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) soft += red[0][w], hard += red[1][w];
+    }
+    const float soft_sum = one((float)soft), hard_sum = one((float)hard);
+    const float log2_p = my_value - t_log, p = taught && my_class >= 0 ? exp2_of(log2_p) : 0.f;
+    if (A.loss && wave == 0) {
+        const float kl = sum_over(p == 0.f ? 0.f : p * (log2_p - ((my_z - m) * soften - log2_of(soft_sum))), 64);
+        if (lane == 0) {
+            float loss = 0.f;
+            if (taught) loss += A.alpha * A.temperature * A.temperature * LN2 * kl;
+            if (y >= 0) loss += (1.f - A.alpha) * (LN2 * log2_of(hard_sum) - (z_label - m));
+            A.loss[r] = either ? weight * loss : 0.f;
+        }
+    }
+    if (!A.dh) return;
+    const float scale = A.grad_scale * weight, a = taught ? scale * A.alpha * A.temperature : 0.f, b = y >= 0 ? scale * (1.f - A.alpha) : 0.f;
+    const float a_q = taught ? a / soft_sum : 0.f, b_q = y >= 0 ? b / hard_sum : 0.f, my_share = a * p;
+    const int32_t my_place = taught && my_class >= 0 ? my_class + lead : -1, label_place = y >= 0 ? y + lead : -1;
+    char* const out = A.dh + r * A.dh_stride;
+    each([&](int i, const float(&w)[8]) {      // (all lanes of a wavefront together)
+        float g[8] = {};
+        if (either) gradients_of(A.temperature, w, m, soften, a_q, b_q, g);
+        // entries whose class lies in the wavefront's pieces: 512 columns from here
+        const int first = (wave * 64 + WIDTH * i) * 8, c = first + lane * 8;
+        auto take = [&](int32_t k, float share) {      // (the same in all lanes)
+            const float mine = (k - first) >> 3 == lane ? share : 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((k & 7) == e) g[e] -= mine;
+        };
+        unsigned long long there = __ballot(my_place >= first && my_place < first + 512);
+        while (there) {
+            const int l = __ffsll((long long)there) - 1;
+            there &= there - 1;
+            take(__builtin_amdgcn_readlane(my_place, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_share), l)));
+        }
+        if (label_place >= first && label_place < first + 512) take(label_place, b);
+        if (c >= d) return;
+        auto put = [&](auto type) {
+            constexpr int O = decltype(type)::value, OE = O == FG_F32 ? 4 : 2;
+            char* const to = out + (int64_t)(c - lead) * OE;
+            if (c > 0 || lead == 0) return fg_store_piece<O>(to, g, d - c);
+            const fg_piece<O> v = fg_to_piece<O>(g);
+#pragma unroll
+            for (int e = 1; e < 8; ++e)
+                if (e >= lead && e < d) {
+                    if constexpr (O == FG_F32)
+                        ((float*)to)[e] = g[e];
+                    else
+                        ((unsigned short*)to)[e] = (unsigned short)(v.a[e / 2] >> (16 * (e & 1)));
+                }
+        };
+        if (A.dh_dtype == FG_F32)
+            put(std::integral_constant<int, FG_F32>());
+        else if constexpr (T != FG_F32)
+            put(std::integral_constant<int, T>());
+    });
+}
+
+template <int T>
+void launch_narrow(DistillArgs A, hipStream_t st) {
+    A.lanes = DL_MIN_LANES;
+    while (A.lanes * 8 < A.d) A.lanes *= 2;
+    const int per_block = DL_THREADS / A.lanes;
+    const int64_t at_once = (FG_MAX_GRID - 1) * per_block;      // rows of a launch
     for (; A.L.first < A.L.max_rows; A.L.first += at_once) {
         const int64_t rows = A.L.max_rows - A.L.first < at_once ? A.L.max_rows - A.L.first : at_once;
-        hipLaunchKernelGGL((distill_kernel<T, WAVES, NP, TAIL>), dim3((unsigned)fg_ceil_div(rows, per_block)), dim3(WAVES > 1 ? WAVES * 64 : DL_THREADS),
-                           (size_t)per_block * A.k * sizeof(Entry), st, A);
+        hipLaunchKernelGGL((distill_narrow_kernel<T>), dim3((unsigned)fg_ceil_div(rows, per_block)), dim3(DL_THREADS), (size_t)per_block * A.k * sizeof(Entry), st, A);
+    }
+}
+template <int T, int WAVES, int NP, bool TAIL>
+void launch_wide(DistillArgs A, hipStream_t st) {
+    const int64_t at_once = FG_MAX_GRID / WAVES - 1;
+    for (; A.L.first < A.L.max_rows; A.L.first += at_once) {
+        const int64_t rows = A.L.max_rows - A.L.first < at_once ? A.L.max_rows - A.L.first : at_once;
+        hipLaunchKernelGGL((distill_wide_kernel<T, WAVES, NP, TAIL>), dim3((unsigned)rows), dim3(WAVES * 64), 0, st, A);
     }
 }
 template <int T>
-void distill(DistillArgs A, hipStream_t st) {
-    const int pieces = (int)fg_ceil_div(A.d, 8);
-    A.lanes = 64;
-    if (pieces <= 64) {
-        A.lanes = DL_MIN_LANES;
-        while (A.lanes < pieces) A.lanes *= 2;
-        launch<T, 1, 1, false>(A, st);
-    } else if (pieces <= 128) {
-        launch<T, 1, 2, false>(A, st);
-    } else if (pieces <= 256) {
-        launch<T, 1, 4, false>(A, st);
-    } else if (pieces <= 1024) {
-        launch<T, 4, 4, false>(A, st);
-    } else if (pieces <= 2048) {
-        launch<T, 8, 4, false>(A, st);
-    } else if (pieces <= 8192) {
-        launch<T, 16, 8, false>(A, st);
-    } else {
-        launch<T, 16, 8, true>(A, st);
-    }
+void distill(const DistillArgs& A, hipStream_t st) {
+    const int pieces = (int)fg_ceil_div(A.d, 8) + 1;      // (a row begins anywhere in its first line)
+    if (A.d <= DL_NARROW) return launch_narrow<T>(A, st);
+    // as few wavefronts as hold the row (what they do beside its values is not for each value), more where there are few rows
+    constexpr int MOST = T == FG_F32 ? 8 : 16;
+    const bool few = A.L.max_rows < DL_FEW_ROWS;
+    if (pieces <= 256 && !few) return launch_wide<T, 1, 4, false>(A, st);
+    if (pieces <= 64 * MOST && !few) return launch_wide<T, 1, MOST, false>(A, st);
+    if (pieces <= 512) return launch_wide<T, 4, 2, false>(A, st);
+    if (pieces <= 256 * MOST) return launch_wide<T, 4, MOST, false>(A, st);
+    if (pieces <= 8192) return launch_wide<T, 128 / MOST, MOST, false>(A, st);
+    launch_wide<T, 128 / MOST, MOST, true>(A, st);
 }
 
 }  // namespace
@@ -292,6 +437,7 @@ extern "C" fg_status_t fg_distill_loss(const void* h, int64_t h_stride, fg_dtype
     if (!e || (k != 0 && !fg_dtype_size(top_dtype))) FG_FAIL(FG_ERR_DTYPE, "%s: unknown element type", who);
     if (dh && dh_dtype != dtype && dh_dtype != FG_F32) FG_FAIL(FG_ERR_DTYPE, "%s: dh is of the type of h or fp32", who);
     FG_TRY(check_rows(who, rows_dev, n_rows_dev, max_rows, n, d));
+    if (d > FG_MAX_CLASSES) FG_FAIL(FG_ERR_SHAPE, "%s: d = %d is more than %d", who, d, FG_MAX_CLASSES);
     if (k < 0 || k > FG_MAX_TOP) FG_FAIL(FG_ERR_SHAPE, "%s: k = %d is not in 0..%d", who, k, FG_MAX_TOP);
     if (table_rows < 0 || table_rows > INT32_MAX) FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
     if (!(temperature > 0.f && temperature < INFINITY)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: temperature = %g must be positive", who, (double)temperature);

@@ -12,8 +12,8 @@
 namespace {
 
 constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 768, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
-constexpr int GN_AHEAD = 4, GN_AHEAD_BW = 2;      // rows whose reads are on their way together
+constexpr int GN_PLACES = 1024, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
+constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;      // rows whose reads are on their way together
 
 struct GnArgs {
     const int32_t* order;      // NULL: position k itself
@@ -60,17 +60,16 @@ __device__ __forceinline__ int near(const GnArgs& A, unsigned int target) {
 enum { GN_WHOLE, GN_GOES_ON, GN_BEGINS };
 // What a workgroup of a tile has to do: the parts of split groups in its chunk (of one that began before it, of one that begins in it), or every so many-th group
 // that is not split. The same in all wavefronts.
+template <bool PARTS>
 struct Walk {
     const GnArgs& A;
-    bool by_chunk;
     unsigned int c0, c1, from, to;      // entries of the chunk; of the group that this lane looks at, or of the next group
     int base;                           // the first lane's group, or the next group
     unsigned long long mask;            // lanes whose groups are still to come
     __device__ __forceinline__ Walk(const GnArgs& args, int number) : A(args) {
-        by_chunk = number >= A.workers;
         mask = 0;
         from = to = 0;
-        if (by_chunk) {
+        if constexpr (PARTS) {
             c0 = (number - A.workers) * A.rows;
             c1 = c0 + A.rows;
             base = near(A, c0) - 64;
@@ -86,7 +85,7 @@ struct Walk {
     }
     // The next part: group, first entry and end, which of the three
     __device__ __forceinline__ bool next(int& g, unsigned int& k0, unsigned int& k1, int& which) {
-        if (!by_chunk) {
+        if constexpr (!PARTS) {
             for (;;) {
                 if (base >= A.n_groups) return false;
                 g = base, k0 = from, k1 = to > from ? to : from;
@@ -95,27 +94,28 @@ struct Walk {
                 which = GN_WHOLE;
                 if (k1 - k0 <= A.long_rows) return true;
             }
-        }
-        while (!mask) {
-            if (__ballot(from >= c1)) return false;
-            base += 64;
-            if (base >= A.n_groups) return false;
-            const int i = base + fg_lane();
-            from = c1, to = 0;
-            if (i < A.n_groups) {
-                from = offset_of(A, i);
-                to = offset_of(A, i + 1);
+        } else {
+            while (!mask) {
+                if (__ballot(from >= c1)) return false;
+                base += 64;
+                if (base >= A.n_groups) return false;
+                const int i = base + fg_lane();
+                from = c1, to = 0;
+                if (i < A.n_groups) {
+                    from = offset_of(A, i);
+                    to = offset_of(A, i + 1);
+                }
+                mask = __ballot(from < c1 && to > c0 && to > from && to - from > A.long_rows);
             }
-            mask = __ballot(from < c1 && to > c0 && to > from && to - from > A.long_rows);
+            const int l = __ffsll((long long)mask) - 1;
+            mask &= mask - 1;
+            g = base + l;
+            const unsigned int first = (unsigned int)__builtin_amdgcn_readlane((int)from, l), end = (unsigned int)__builtin_amdgcn_readlane((int)to, l);
+            which = first < c0 ? GN_GOES_ON : GN_BEGINS;
+            k0 = first < c0 ? c0 : first;
+            k1 = end < c1 ? end : c1;
+            return true;
         }
-        const int l = __ffsll((long long)mask) - 1;
-        mask &= mask - 1;
-        g = base + l;
-        const unsigned int first = (unsigned int)__builtin_amdgcn_readlane((int)from, l), end = (unsigned int)__builtin_amdgcn_readlane((int)to, l);
-        which = first < c0 ? GN_GOES_ON : GN_BEGINS;
-        k0 = first < c0 ? c0 : first;
-        k1 = end < c1 ? end : c1;
-        return true;
     }
 };
 __device__ __forceinline__ int position(const GnArgs& A, unsigned int k) {
@@ -373,15 +373,16 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
     }
 }
 
-template <int TH, int T_, bool MANY>
-__global__ __launch_bounds__(TH, 3) void group_norm_kernel(GnArgs A) {
+// PARTS: the workgroup's work is a chunk's parts of split groups, else whole groups (one kernel for both, so that neither waits for the other; two bodies, so
+// that the first is not short of registers for what the second holds)
+template <int TH, int T_, bool MANY, bool PARTS>
+__device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
     constexpr int N = MANY ? 8 : 1;
-    __shared__ Scratch<TH> S;
     const Tile T = tile_of<TH>(A);
     const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
     unsigned int k0, k1;
-    for (Walk W(A, blockIdx.y); W.next(g, k0, k1, which);) {
+    for (Walk<PARTS> W(A, blockIdx.y); W.next(g, k0, k1, which);) {
         if (k0 == k1) {      // a group without rows
             for (int j = threadIdx.x; j < T.n_blocks; j += TH) put_statistics(A, T, g, j, 0.f, (float)reciprocal_root((double)A.eps));
             continue;
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(TH, 3) void group_norm_kernel(GnArgs A) {
         double s[N] = {}, q[N] = {};
         int rows = 0, now[GN_AHEAD];
         fg_piece<T_> v[GN_AHEAD];
-        const bool held = k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);      // (all of a group's rows at once: they are read once)
+        const bool held = !PARTS && k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);      // (all of a group's rows at once: they are read once)
 #pragma unroll
         for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
         // a column's values are measured from its first one (MANY), all columns' from the block's
@@ -435,19 +436,27 @@ __global__ __launch_bounds__(TH, 3) void group_norm_kernel(GnArgs A) {
                 }
             },
             [&](int j, double a, double b) {
-                if (which != GN_WHOLE) return write_part(A, T, chunk, which, j, a, b, rows);
+                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows);
                 float mean, rstd;
                 mean_rstd(A, MANY ? S.from[j * A.block] : common, a, b, (double)rows, mean, rstd);
                 S.stats[j][0] = mean, S.stats[j][1] = rstd;
                 put_statistics(A, T, g, j, mean, rstd);
             });
         __syncthreads();      // (the sums have been read: the next group's may be left there, and its statistics behind the next barrier)
-        if (which == GN_WHOLE)
+        if constexpr (!PARTS)
             normalise<TH, T_, MANY>(A, T, S, k0, k1, held, now, v);
         else
             (which == GN_BEGINS ? begins : goes_on) = g;
     }
-    note(A, chunk, goes_on, begins);
+    if constexpr (PARTS) note(A, chunk, goes_on, begins);
+}
+template <int TH, int T_, bool MANY>
+__global__ __launch_bounds__(TH, 4) void group_norm_kernel(GnArgs A) {
+    __shared__ Scratch<TH> S;
+    if ((int)blockIdx.y < A.workers)
+        norm_body<TH, T_, MANY, false>(A, S);
+    else
+        norm_body<TH, T_, MANY, true>(A, S);
 }
 
 // the sums of all parts of the split group that begins in a chunk, in order: lanes of a wavefront together
@@ -552,13 +561,15 @@ __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs 
 struct GradColumns {
     float mean[8], rstd[8], w[8], b[8];
 };
-template <bool MANY>
+// FOLDED: rstd * w in place of w, so that rstd is not needed beside them
+template <bool MANY, bool FOLDED>
 __device__ __forceinline__ void grad_columns(const GnArgs& A, const Tile& T, int g, int c, GradColumns& C) {
     affine(A, T, c, C.w, C.b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY ? block_of(A, c + e) : 0);
         C.mean[e] = A.mean[at], C.rstd[e] = A.rstd[at];
+        if (FOLDED) C.w[e] *= C.rstd[e];
     }
 }
 // rows on their way, or held
@@ -568,8 +579,8 @@ struct GradRows {
     fg_piece<X> x[GN_AHEAD_BW];
     fg_piece<G> dy[GN_AHEAD_BW];
 };
-// use(row, xh, t) for every row of the entries [k0, k1) that this thread has; held: R has all of them already
-template <int X, int G, typename Use>
+// use(row, xh, t) for every row of the entries [k0, k1) that this thread has (FOLDED: use(row, x - mean, t)); held: R has all of them already
+template <int X, int G, bool FOLDED, typename Use>
 __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, int c, const GradColumns& C, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R,
                                               const Use& use) {
     const auto terms = [&](int u, int r) {
@@ -578,7 +589,8 @@ __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, in
         fg_piece_values<G>(R.dy[u], t);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            xh[e] = (xh[e] - C.mean[e]) * C.rstd[e];
+            xh[e] -= C.mean[e];
+            if (!FOLDED) xh[e] *= C.rstd[e];
             slope[e] = xh[e] * C.w[e] + C.b[e];
         }
         slopes(A.act, slope);
@@ -608,14 +620,14 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
         const Piece P = piece_of(A, T, i);
         if (!P.there) break;
         GradColumns C;
-        grad_columns<MANY>(A, T, g, P.c, C);
+        grad_columns<MANY, false>(A, T, g, P.c, C);
         float m1[8], m2[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int j = MANY ? block_of(A, P.c + e) : 0;
             m1[e] = S.stats[j][0], m2[e] = S.stats[j][1];
         }
-        gradient_rows<X, G>(A, T, P.c, C, k0, k1, held, R, [&](int r, const float(&xh)[8], float(&t)[8]) {
+        gradient_rows<X, G, false>(A, T, P.c, C, k0, k1, held, R, [&](int r, const float(&xh)[8], float(&t)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) t[e] = C.rstd[e] * (t[e] * C.w[e] - m1[e] - xh[e] * m2[e]);
             store_piece<G>(A.out + (int64_t)r * A.out_stride + T.c0 * (G == FG_F32 ? 4 : 2), P, t);
@@ -626,9 +638,8 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
 // The first pass: a group's sums of t and t * xh by column, which give its two means and dw and db. MANY: the columns' sums over a group's rows
 // meet in LDS, a thread to a column adds them up over the chunk's groups. Else (NP pieces a thread) a thread keeps its columns' sums over all of
 // the chunk's rows, and those of a group over its columns beside them.
-template <int TH, int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel(GnArgs A) {
-    __shared__ Scratch<TH> S;
+template <int TH, int X, int G, bool MANY, int NP, bool PARTS>
+__device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
     const Tile T = tile_of<TH>(A);
     const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
@@ -636,10 +647,10 @@ __global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel
     constexpr int MINE = GN_COLUMNS / TH;      // MANY: columns whose sums a thread has
     double dw[MINE] = {}, db[MINE] = {};
     float dw_piece[MANY ? 1 : NP][8] = {}, db_piece[MANY ? 1 : NP][8] = {};
-    for (Walk W(A, blockIdx.y); W.next(g, k0, k1, which);) {
+    for (Walk<PARTS> W(A, blockIdx.y); W.next(g, k0, k1, which);) {
         if (k0 == k1) continue;
         GradRows<X, G> R;
-        const bool held = k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
+        const bool held = !PARTS && k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
 #pragma unroll
         for (int u = 0; u < GN_AHEAD_BW; ++u) R.now[u] = -1;
         int rows = 0;
@@ -649,11 +660,13 @@ __global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel
             const Piece P = piece_of(A, T, 0);
             if (P.there) {
                 GradColumns C;
-                grad_columns<true>(A, T, g, P.c, C);
-                gradient_rows<X, G>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
+                grad_columns<true, true>(A, T, g, P.c, C);
+                gradient_rows<X, G, true>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&x)[8], const float(&t)[8]) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * xh[e];
+                    for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * x[e];
                 });
+#pragma unroll
+                for (int e = 0; e < 8; ++e) q[e] *= A.rstd[(int64_t)g * A.blocks + T.block0 + block_of(A, P.c + e)];
             }
             leave_sums<TH, true>(A, T, S, s, q, rows);
         } else {
@@ -663,8 +676,8 @@ __global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel
                 const Piece P = piece_of(A, T, i);
                 if (P.there) {
                     GradColumns C;
-                    grad_columns<false>(A, T, g, P.c, C);
-                    gradient_rows<X, G>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
+                    grad_columns<false, false>(A, T, g, P.c, C);
+                    gradient_rows<X, G, false>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             if (e < P.twice) continue;
@@ -696,17 +709,17 @@ __global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel
                 }
             },
             [&](int j, double a, double b) {
-                if (which != GN_WHOLE) return write_part(A, T, chunk, which, j, a, b, rows);
+                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows);
                 const double per = reciprocal(rows > 0 ? (double)rows * A.block : 1.0);
                 S.stats[j][0] = (float)(a * per), S.stats[j][1] = (float)(b * per);
             });
         __syncthreads();
-        if (which == GN_WHOLE)
+        if constexpr (!PARTS)
             input_gradient<TH, X, G, MANY>(A, T, S, g, k0, k1, held, R);
         else
             (which == GN_BEGINS ? begins : goes_on) = g;
     }
-    note(A, chunk, goes_on, begins);
+    if constexpr (PARTS) note(A, chunk, goes_on, begins);
     if (!A.columns) return;
     float* const to = A.columns + (int64_t)blockIdx.y * 2 * A.d + T.c0;
     if constexpr (MANY) {
@@ -742,9 +755,17 @@ __global__ __launch_bounds__(TH, NP > 1 ? 1 : 3) void group_norm_backward_kernel
         }
     }
 }
+template <int TH, int X, int G, bool MANY, int NP>
+__global__ __launch_bounds__(TH, NP > 1 ? 1 : 4) void group_norm_backward_kernel(GnArgs A) {
+    __shared__ Scratch<TH> S;
+    if ((int)blockIdx.y < A.workers)
+        gradient_body<TH, X, G, MANY, NP, false>(A, S);
+    else
+        gradient_body<TH, X, G, MANY, NP, true>(A, S);
+}
 // The second pass, on split groups
 template <int X, int G, bool MANY>
-__global__ __launch_bounds__(GN_THREADS, 3) void group_norm_backward_apply_kernel(GnArgs A) {
+__global__ __launch_bounds__(GN_THREADS, 4) void group_norm_backward_apply_kernel(GnArgs A) {
     __shared__ Scratch<GN_THREADS> S;
     const Tile T = tile_of<GN_THREADS>(A);
     split_parts<X, true>(A, T, S, [&](int g, unsigned int k0, unsigned int k1) {
@@ -754,8 +775,8 @@ __global__ __launch_bounds__(GN_THREADS, 3) void group_norm_backward_apply_kerne
 }
 
 // How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block. A group whose values in a tile are up to GN_FEW_VALUES is not split.
-// Chunks of rows for the others, with two rows a thread at least, so that all workgroups are on the chip at once, three to a compute unit (a fourth of them in a second
-// turn took as long as all the others). Where there are few groups and rows, tiles of fewer blocks. One wavefront to a workgroup where an average group's rows are up to
+// Chunks of rows for the others, with two rows a thread at least, so that all workgroups are on the chip at once, four to a compute unit (a few of them in a second
+// turn take as long as all the others). Where there are few groups and rows, tiles of fewer blocks. One wavefront to a workgroup where an average group's rows are up to
 // GN_SMALL_STEPS steps of one.
 struct Plan {
     int tiles, tile_blocks, width, pieces, threads, workers;

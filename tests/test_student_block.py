@@ -126,7 +126,7 @@ def test_distill_refusals(B):
                                                    top_dtype=B.FG_F16, table_rows=10, k=4, labels=None, temperature=2.0, alpha=0.5, weight=None, grad_scale=1.0,
                                                    loss_out=P, dh=P + 4096, dh_stride=256, dh_dtype=B.FG_F32), **k})
     for bad, want in ((dict(h=None), 1), (dict(top_idx=None), 1), (dict(top_val=None), 1), (dict(loss_out=None, dh=None), 1), (dict(max_rows=-1), 1), (dict(max_rows=11), 2),
-                      (dict(n=1 << 31, rows=P), 1), (dict(d=0), 2), (dict(k=-1), 2), (dict(k=B.FG_MAX_TOP + 1), 2), (dict(table_rows=-1), 1), (dict(table_rows=1 << 31), 1),
+                      (dict(n=1 << 31, rows=P), 1), (dict(d=0), 2), (dict(d=B.FG_MAX_CLASSES + 1, h_stride=1 << 34, dh_stride=1 << 34), 2), (dict(k=-1), 2), (dict(k=B.FG_MAX_TOP + 1), 2), (dict(table_rows=-1), 1), (dict(table_rows=1 << 31), 1),
                       (dict(temperature=0.0), 1), (dict(temperature=-1.0), 1), (dict(temperature=float("nan")), 1), (dict(temperature=float("inf")), 1),
                       (dict(alpha=-0.1), 1), (dict(alpha=1.5), 1), (dict(alpha=float("nan")), 1), (dict(dtype=3), 3), (dict(top_dtype=3), 3), (dict(dh_dtype=B.FG_BF16), 3),
                       (dict(h_stride=252), 2), (dict(dh_stride=128), 2), (dict(h=P + 2), 1), (dict(dh=P + 1), 1), (dict(dh=P, dh_stride=512), 1),
