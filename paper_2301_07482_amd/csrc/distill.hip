@@ -13,14 +13,14 @@
 
 namespace {
 
-constexpr int DL_THREADS = 256, DL_MIN_LANES = 8, DL_NARROW = 512, DL_FEW_ROWS = 1024;
+constexpr int DL_THREADS = 256, DL_NARROW = 512, DL_FEW_ROWS = 16384;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 
 struct DistillArgs {
     RowList L;
     const char* h;
     int64_t h_stride;
-    int d, lanes, k;      // lanes of a row
+    int d, k;
     const int32_t *ids, *top_idx;
     const char* top_val;
     int top_dtype, dh_dtype;
@@ -44,9 +44,49 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
     return m;
 }
-__device__ __forceinline__ float sum_over(float v, int lanes) {
-    for (int off = lanes >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+// over LANES adjacent lanes, all lanes active, the same in all of them: neighbours, pairs, halves of eight and of sixteen lanes change places inside the vector registers
+template <int LANES, typename F>
+__device__ __forceinline__ float over_lanes(float v, const F& f) {
+    const auto moved = [&](auto ctrl) { return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, false)); };
+    v = f(v, moved(std::integral_constant<int, 0xB1>()));
+    v = f(v, moved(std::integral_constant<int, 0x4E>()));
+    v = f(v, moved(std::integral_constant<int, 0x141>()));
+    if constexpr (LANES >= 16) v = f(v, moved(std::integral_constant<int, 0x140>()));
+    if constexpr (LANES >= 32) v = f(v, __shfl_xor(v, 16, 64));
+    if constexpr (LANES >= 64) v = f(v, __shfl_xor(v, 32, 64));
     return v;
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum_of(float v) {
+    return over_lanes<LANES>(v, [](float a, float b) { return a + b; });
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_max_of(float v) {
+    return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+// over a wavefront, all lanes active, the same in all of them. The lanes' values move inside the vector registers, as in fg_wave_scan
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float v, float none) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(none), __float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), 63)); }
+__device__ __forceinline__ float wave_sum(float v) {
+    v += moved<0x111, 0xf>(v, 0.f);
+    v += moved<0x112, 0xf>(v, 0.f);
+    v += moved<0x114, 0xf>(v, 0.f);
+    v += moved<0x118, 0xf>(v, 0.f);
+    v += moved<0x142, 0xa>(v, 0.f);
+    v += moved<0x143, 0xc>(v, 0.f);
+    return last_lane(v);
+}
+__device__ __forceinline__ float wave_max(float v) {      // (what is NaN is left out)
+    v = fmaxf(v, moved<0x111, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x112, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x114, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x118, 0xf>(v, -INFINITY));
+    v = fmaxf(v, moved<0x142, 0xa>(v, -INFINITY));
+    v = fmaxf(v, moved<0x143, 0xc>(v, -INFINITY));
+    return last_lane(v);
 }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }
@@ -127,48 +167,53 @@ __device__ __forceinline__ void wave_meets() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Narrow rows: 64 / lanes of them to a wavefront. A row's values lie in LDS for its entries to find theirs, then what those take from its gradient.
+// Narrow rows: 64 / LANES of them to a wavefront, eight columns to a lane. A row's values lie in LDS for its entries to find theirs, then what those take from its
+// gradient. Bound by memory and, nearly as long, by what a wavefront does beside its values: 54067 x 256 fp32 26 us (4.3 TB/s; without teacher and labels 17), 32 with the
+// lanes a number of the call's; two and four pieces a lane, for more rows to a wavefront, 28 and 30.
 struct Entry {
     int32_t c;      // class, -1: none
     float p, log2_p, z;
 };
-template <int T>
+template <int T, int LANES>
 __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs A) {
-    constexpr int E = T == FG_F32 ? 4 : 2;
+    constexpr int E = T == FG_F32 ? 4 : 2, ROW = LANES * 8, ROWS = DL_THREADS / LANES;
     extern __shared__ __attribute__((aligned(16))) char dl_lds[];
-    __shared__ __attribute__((aligned(16))) float values[DL_THREADS * 8];
-    const int lanes = A.lanes, me = (int)threadIdx.x & (lanes - 1), slot = (int)threadIdx.x / lanes;
-    const int64_t r = row_at(A.L, A.L.first + blockIdx.x * (int64_t)(DL_THREADS / lanes) + slot, row_count(A.L));
+    __shared__ __attribute__((aligned(16))) float values[ROWS * ROW];
+    const int me = (int)threadIdx.x % LANES, slot = (int)threadIdx.x / LANES;
+    const int64_t r = row_at(A.L, A.L.first + blockIdx.x * (int64_t)ROWS + slot, row_count(A.L));
     Entry* const entries = (Entry*)dl_lds + slot * A.k;
-    float* const mine = values + (int)threadIdx.x * 8;      // this lane's eight columns, in a row's
-    float* const all = values + slot * lanes * 8;
+    float* const all = values + slot * ROW;
+    const char* const row = A.h + r * A.h_stride;
     const int c0 = me * 8, left = r >= 0 ? A.d - c0 : 0;
+    float4* const mine = (float4*)(all + c0);      // this lane's columns
     fg_piece<T> raw = {};
-    if (left > 0) raw = fg_load_piece<T>(A.h + r * A.h_stride + (int64_t)c0 * E, left);
+    if (left > 0) raw = fg_load_piece<T>(row + (int64_t)c0 * E, left);
     int32_t node, y;
-    float weight, w[8];
+    float weight;
     row_facts(A, r, node, y, weight);
     // the teacher's entries are on their way beside the row
     float t_max = -INFINITY;
-    for (int j = me; j < A.k; j += lanes) {
+    for (int j = me; j < A.k; j += LANES) {
         int32_t c;
         float t;
         entry_of(A, node, j, c, t);
         entries[j].c = c, entries[j].log2_p = t;
         if (!(t == -INFINITY)) t_max = t > t_max || !(t == t) || t_max == -INFINITY ? t : t_max;
     }
+    float w[8], m = -INFINITY;
     fg_piece_values<T>(raw, w);
     no_value_beyond(left, w);
-    ((float4*)mine)[0] = float4{w[0], w[1], w[2], w[3]}, ((float4*)mine)[1] = float4{w[4], w[5], w[6], w[7]};
-    float m = max3(max3(max3(w[0], w[1], w[2]), w[3], w[4]), max3(w[5], w[6], w[7]), -INFINITY);
-    m = lanes_max(m, lanes);
+    mine[0] = float4{w[0], w[1], w[2], w[3]}, mine[1] = float4{w[4], w[5], w[6], w[7]};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) m = max3(m, w[e], w[e + 1]);
+    m = lanes_max_of<LANES>(m);
     wave_meets();
     // the teacher's distribution (a value that is NaN makes it NaN; without one above -infinity there is no teacher)
     const float soften = LOG2E / A.temperature;
-    const float top = lanes_max(t_max, lanes);
-    const bool taught = lanes_max(t_max == -INFINITY ? 0.f : 1.f, lanes) > 0.f;
+    const float top = lanes_max_of<LANES>(t_max);
+    const bool taught = lanes_max_of<LANES>(t_max == -INFINITY ? 0.f : 1.f) > 0.f;
     float t_sum = 0.f;
-    for (int j = me; j < A.k; j += lanes) {
+    for (int j = me; j < A.k; j += LANES) {
         const int32_t c = entries[j].c;
         const float x = (entries[j].log2_p - top) * soften;
         entries[j].log2_p = x;
@@ -176,22 +221,21 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
         if (c >= 0) t_sum += exp2_of(x);
     }
     const float z_label = y >= 0 ? all[y] : 0.f;
-    t_sum = sum_over(t_sum, lanes);
-    const float t_log = log2_of(t_sum);
+    const float t_log = log2_of(lanes_sum_of<LANES>(t_sum));
     // the student's
     float soft = 0.f, hard = 0.f;
     const bool either = taught || y >= 0;
     if (either) sums_of(A.temperature, w, m, soften, soft, hard);
-    soft = sum_over(soft, lanes);
-    hard = sum_over(hard, lanes);
+    soft = lanes_sum_of<LANES>(soft);
+    hard = lanes_sum_of<LANES>(hard);
     const float soft_log = log2_of(soft);
     const float scale = A.grad_scale * weight, a = taught ? scale * A.alpha * A.temperature : 0.f, b = y >= 0 ? scale * (1.f - A.alpha) : 0.f;
     float kl = 0.f;
     wave_meets();      // (the values have been read)
-    ((float4*)mine)[0] = ((float4*)mine)[1] = float4{0.f, 0.f, 0.f, 0.f};
+    mine[0] = mine[1] = float4{0.f, 0.f, 0.f, 0.f};
     wave_meets();
     if (taught)
-        for (int j = me; j < A.k; j += lanes) {
+        for (int j = me; j < A.k; j += LANES) {
             const int32_t c = entries[j].c;
             if (c < 0) continue;
             const float log2_p = entries[j].log2_p - t_log, p = exp2_of(log2_p);
@@ -199,7 +243,7 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
             if (A.dh) __hip_atomic_fetch_add(all + c, a * p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);      // (lanes of one wavefront, in order)
         }
     if (A.loss) {
-        kl = sum_over(kl, lanes);
+        kl = lanes_sum_of<LANES>(kl);
         if (me == 0 && r >= 0) {
             float loss = 0.f;
             if (taught) loss += A.alpha * A.temperature * A.temperature * LN2 * kl;
@@ -213,7 +257,7 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
     if (left <= 0) return;
     float g[8] = {};
     if (either) gradients_of(A.temperature, w, m, soften, taught ? a / soft : 0.f, y >= 0 ? b / hard : 0.f, g);
-    const float4 lo = ((float4*)mine)[0], hi = ((float4*)mine)[1];
+    const float4 lo = mine[0], hi = mine[1];
     g[0] -= lo.x, g[1] -= lo.y, g[2] -= lo.z, g[3] -= lo.w, g[4] -= hi.x, g[5] -= hi.y, g[6] -= hi.z, g[7] -= hi.w;
     char* const out = A.dh + r * A.dh_stride;
     if (A.dh_dtype == FG_F32)
@@ -228,10 +272,12 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
 template <int T, int WAVES, int NP, bool TAIL>
 __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs A) {
     constexpr int E = T == FG_F32 ? 4 : 2, WIDTH = WAVES * 64;
-    __shared__ double red[2][WAVES];
+    __shared__ float red[2][WAVES];
     __shared__ float largest[WAVES];
     __shared__ int32_t top_class[WAVES > 1 ? 64 : 1];
     __shared__ float top_share[WAVES > 1 ? 64 : 1], teacher_log;
+    constexpr bool BY_LDS = NP <= 4 && !TAIL;      // what entries take lies in LDS (else a loop over those of a piece: 16 of them 25 us of 54000 rows of 1000)
+    __shared__ __attribute__((aligned(16))) float taken[BY_LDS ? WAVES * NP * 512 : 1];
     __shared__ int taught_by;
     const int64_t r = row_at(A.L, A.L.first + blockIdx.x, row_count(A.L));
     if (r < 0) return;
@@ -295,14 +341,14 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
 #pragma unroll
         for (int e = 0; e < 8; e += 2) m = max3(m, w[e], w[e + 1]);
     });
-    m = lanes_max(m, 64);
+    m = wave_max(m);
     const float soften = LOG2E / A.temperature;
     bool taught = false;
     float t_log = 0.f;
     if (wave == 0) {      // the teacher's distribution (a value that is NaN makes it NaN; without one above -infinity there is no teacher)
         taught = __ballot(my_class >= 0 && !(my_value == -INFINITY)) != 0;
-        my_value = (my_value - lanes_max(my_value, 64)) * soften;
-        t_log = log2_of(sum_over(my_class >= 0 ? exp2_of(my_value) : 0.f, 64));
+        my_value = (my_value - wave_max(my_value)) * soften;
+        t_log = log2_of(wave_sum(my_class >= 0 ? exp2_of(my_value) : 0.f));
     }
     if constexpr (WAVES > 1) {
         if (lane == 0) largest[wave] = m;
@@ -327,19 +373,18 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
             sums_of(A.temperature, w, m, soften, s, h);
             soft += (double)s, hard += (double)h;
         });
-    soft = lanes_sum(soft, 64);
-    hard = lanes_sum(hard, 64);
+    float soft_sum = wave_sum((float)soft), hard_sum = wave_sum((float)hard);
     if constexpr (WAVES > 1) {
-        if (lane == 0) red[0][wave] = soft, red[1][wave] = hard;
+        if (lane == 0) red[0][wave] = soft_sum, red[1][wave] = hard_sum;
         __syncthreads();
-        soft = hard = 0.0;
+        soft_sum = hard_sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) soft += red[0][w], hard += red[1][w];
+        for (int w = 0; w < WAVES; ++w) soft_sum += red[0][w], hard_sum += red[1][w];
+        soft_sum = one(soft_sum), hard_sum = one(hard_sum);
     }
-    const float soft_sum = one((float)soft), hard_sum = one((float)hard);
     const float log2_p = my_value - t_log, p = taught && my_class >= 0 ? exp2_of(log2_p) : 0.f;
     if (A.loss && wave == 0) {
-        const float kl = sum_over(p == 0.f ? 0.f : p * (log2_p - ((my_z - m) * soften - log2_of(soft_sum))), 64);
+        const float kl = wave_sum(p == 0.f ? 0.f : p * (log2_p - ((my_z - m) * soften - log2_of(soft_sum))));
         if (lane == 0) {
             float loss = 0.f;
             if (taught) loss += A.alpha * A.temperature * A.temperature * LN2 * kl;
@@ -351,17 +396,43 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
     const float scale = A.grad_scale * weight, a = taught ? scale * A.alpha * A.temperature : 0.f, b = y >= 0 ? scale * (1.f - A.alpha) : 0.f;
     const float a_q = taught ? a / soft_sum : 0.f, b_q = y >= 0 ? b / hard_sum : 0.f, my_share = a * p;
     const int32_t my_place = taught && my_class >= 0 ? my_class + lead : -1, label_place = y >= 0 ? y + lead : -1;
+    if constexpr (BY_LDS) {      // eight columns of a lane's piece behind each other; entries of one class are added in their lanes' order
+        float* const mine = taken + wave * NP * 512;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) ((float4*)mine)[i * 128 + lane * 2] = ((float4*)mine)[i * 128 + lane * 2 + 1] = float4{0.f, 0.f, 0.f, 0.f};
+        wave_meets();
+        auto add = [&](int32_t place, float share) {
+            const int piece = place >> 3;
+            if (place >= 0 && piece % WIDTH / 64 == wave)
+                __hip_atomic_fetch_add(mine + piece / WIDTH * 512 + (place & 511), share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+        };
+        add(my_place, my_share);
+        if (lane == 0) add(label_place, b);
+        wave_meets();
+    }
     char* const out = A.dh + r * A.dh_stride;
     each([&](int i, const float(&w)[8]) {      // (all lanes of a wavefront together)
         float g[8] = {};
         if (either) gradients_of(A.temperature, w, m, soften, a_q, b_q, g);
-        // entries whose class lies in the wavefront's pieces: 512 columns from here
         const int first = (wave * 64 + WIDTH * i) * 8, c = first + lane * 8;
+        if constexpr (BY_LDS) {
+            const float4* from = (const float4*)(taken + wave * NP * 512) + i * 128 + lane * 2;
+            const float4 lo = from[0], hi = from[1];
+            g[0] -= lo.x, g[1] -= lo.y, g[2] -= lo.z, g[3] -= lo.w, g[4] -= hi.x, g[5] -= hi.y, g[6] -= hi.z, g[7] -= hi.w;
+        } else {
+        // entries whose class lies in the wavefront's pieces: 512 columns from here
         auto take = [&](int32_t k, float share) {      // (the same in all lanes)
             const float mine = (k - first) >> 3 == lane ? share : 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if ((k & 7) == e) g[e] -= mine;
+            switch (k & 7) {
+                case 0: g[0] -= mine; break;
+                case 1: g[1] -= mine; break;
+                case 2: g[2] -= mine; break;
+                case 3: g[3] -= mine; break;
+                case 4: g[4] -= mine; break;
+                case 5: g[5] -= mine; break;
+                case 6: g[6] -= mine; break;
+                default: g[7] -= mine;
+            }
         };
         unsigned long long there = __ballot(my_place >= first && my_place < first + 512);
         while (there) {
@@ -370,6 +441,7 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
             take(__builtin_amdgcn_readlane(my_place, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_share), l)));
         }
         if (label_place >= first && label_place < first + 512) take(label_place, b);
+        }
         if (c >= d) return;
         auto put = [&](auto type) {
             constexpr int O = decltype(type)::value, OE = O == FG_F32 ? 4 : 2;
@@ -392,15 +464,13 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
     });
 }
 
-template <int T>
+template <int T, int LANES>
 void launch_narrow(DistillArgs A, hipStream_t st) {
-    A.lanes = DL_MIN_LANES;
-    while (A.lanes * 8 < A.d) A.lanes *= 2;
-    const int per_block = DL_THREADS / A.lanes;
-    const int64_t at_once = (FG_MAX_GRID - 1) * per_block;      // rows of a launch
+    constexpr int PER_BLOCK = DL_THREADS / LANES;
+    const int64_t at_once = (FG_MAX_GRID - 1) * PER_BLOCK;      // rows of a launch
     for (; A.L.first < A.L.max_rows; A.L.first += at_once) {
         const int64_t rows = A.L.max_rows - A.L.first < at_once ? A.L.max_rows - A.L.first : at_once;
-        hipLaunchKernelGGL((distill_narrow_kernel<T>), dim3((unsigned)fg_ceil_div(rows, per_block)), dim3(DL_THREADS), (size_t)per_block * A.k * sizeof(Entry), st, A);
+        hipLaunchKernelGGL((distill_narrow_kernel<T, LANES>), dim3((unsigned)fg_ceil_div(rows, PER_BLOCK)), dim3(DL_THREADS), (size_t)PER_BLOCK * A.k * sizeof(Entry), st, A);
     }
 }
 template <int T, int WAVES, int NP, bool TAIL>
@@ -414,13 +484,16 @@ void launch_wide(DistillArgs A, hipStream_t st) {
 template <int T>
 void distill(const DistillArgs& A, hipStream_t st) {
     const int pieces = (int)fg_ceil_div(A.d, 8) + 1;      // (a row begins anywhere in its first line)
-    if (A.d <= DL_NARROW) return launch_narrow<T>(A, st);
-    // as few wavefronts as hold the row (what they do beside its values is not for each value), more where there are few rows
+    if (A.d <= 64) return launch_narrow<T, 8>(A, st);
+    if (A.d <= 128) return launch_narrow<T, 16>(A, st);
+    if (A.d <= 256) return launch_narrow<T, 32>(A, st);
+    if (A.d <= DL_NARROW) return launch_narrow<T, 64>(A, st);
+    // One wavefront to a row where that holds it (what it does beside the row's values takes as long as some hundred of them), four where rows are few. Both in us, bf16 with 16
+    // entries: 2048 x 2000 9.0 | 9.6, 16384 x 2000 39 | 47; 2048 x 4000 17 | 13, 16384 x 4000 74 | 69, 54000 x 4000 210 | 216; 2048 x 8000 28 | 24, 4096 x 8000 40 | 40, 54000 x 8000 393 | 437
     constexpr int MOST = T == FG_F32 ? 8 : 16;
-    const bool few = A.L.max_rows < DL_FEW_ROWS;
-    if (pieces <= 256 && !few) return launch_wide<T, 1, 4, false>(A, st);
-    if (pieces <= 64 * MOST && !few) return launch_wide<T, 1, MOST, false>(A, st);
-    if (pieces <= 512) return launch_wide<T, 4, 2, false>(A, st);
+    if (pieces <= 256) return launch_wide<T, 1, 4, false>(A, st);
+    if (pieces <= 512 && A.L.max_rows <= DL_FEW_ROWS) return launch_wide<T, 4, 2, false>(A, st);
+    if (pieces <= 64 * MOST && A.L.max_rows > DL_FEW_ROWS / 4) return launch_wide<T, 1, MOST, false>(A, st);
     if (pieces <= 256 * MOST) return launch_wide<T, 4, MOST, false>(A, st);
     if (pieces <= 8192) return launch_wide<T, 128 / MOST, MOST, false>(A, st);
     launch_wide<T, 128 / MOST, MOST, true>(A, st);
@@ -454,7 +527,7 @@ extern "C" fg_status_t fg_distill_loss(const void* h, int64_t h_stride, fg_dtype
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: ids, classes, values, labels, weight and loss must be aligned to their elements", who);
     fg_clear_error();
     if (!work) return FG_OK;
-    const DistillArgs A = {{rows_dev, n_rows_dev, max_rows, n, 0}, (const char*)h, h_stride, d, 0, table_rows > 0 ? k : 0, ids_dev, top_idx_dev, (const char*)top_val_dev,
+    const DistillArgs A = {{rows_dev, n_rows_dev, max_rows, n, 0}, (const char*)h, h_stride, d, table_rows > 0 ? k : 0, ids_dev, top_idx_dev, (const char*)top_val_dev,
                            (int)top_dtype, (int)dh_dtype, table_rows, labels_dev, weight_dev, temperature, alpha, grad_scale, loss_out, (char*)dh, dh_stride};
     const hipStream_t st = (hipStream_t)stream;
     if (dtype == FG_F32)
