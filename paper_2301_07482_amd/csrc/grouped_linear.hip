@@ -149,6 +149,13 @@ __device__ __forceinline__ void arrived() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The same for this wavefront alone; all that it has read from LDS is in its registers
+template <int N>
+__device__ __forceinline__ void own_arrived() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void own_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // 8-bit values become bf16, which holds every one of them, and are multiplied as such (two instructions to an operand's 16 bytes), with sums in fp32
 // throughout. The 8-bit matrix instructions are not used: they add groups of eight adjacent products with 13 bits below the largest of the group
 // (measured: of 2^16 and 1 in one group the 1 is lost), so that of a row with a large value in every eight the others are lost, and where the large
@@ -711,6 +718,195 @@ fg_status_t tile_product(GlArgs& A, hipStream_t st) {
     if (mid >= 256 && A.N > 64 && A.G.max_rows > 64 * groups) return tile_launch<T, 128, 128, 2, 2, 2, B_KN, GATED>(A, st);
     if constexpr (GATED) return tile_launch<T, 64, 64, 2, 1, 4, B_KN, GATED>(A, st);
     return tile_launch<T, 64, 64, 2, 2, 4, B_KN>(A, st);
+}
+
+// Gated layers of few rows: what counts is how long a workgroup takes for its tile, the weights' way from memory to LDS above all. A tile has 32 rows and 32 outputs. The
+// contraction is split over the four wavefronts, each of which takes every fourth step, loads all of the step's operands itself into buffers of its own, three of them on their
+// way at a time, and waits for nobody; their sums meet in LDS. (Steps that all four load and share took 9.7 us instead of 7.6 for 16 x 1024 x 1024 bf16 and 26.8 instead of
+// 13.1 fp32: a barrier a step.) What bounds it is how few workgroups there are: 64 for 1 x 4096 x 2048, whose weights of 33.5 MB arrive at 1.6 TB/s (20.9 us; fp32 39.6).
+constexpr int GR_THREADS = 256, GR_WAVES = GR_THREADS / 64, GR_ROWS = 32, GR_OUT = 32, GR_AHEAD = 3, GR_STAGE = (GR_ROWS + 2 * GR_OUT) * GL_STEP, GR_SUM_ROW = 36;
+static_assert(GR_STAGE >= 2 * GR_ROWS * GR_SUM_ROW * 4, "the sums lie where the operands did");
+template <int T>
+__global__ __launch_bounds__(GR_THREADS) void gated_few_kernel(GlArgs A, int stages) {
+    constexpr int E = T == FG_F32 ? 4 : 2, BK = GL_STEP / E, DEEP = T == FG_F32 ? 2 : 1, SUB = GL_STEP / 32 / DEEP;
+    constexpr int B_ROW = 2 * GR_OUT * E, B_PIECES = B_ROW / 16, B_ROWS = 64 / B_PIECES, A_LOADS = GR_ROWS / GL_ROWS, B_LOADS = BK / B_ROWS, LOADS = A_LOADS + B_LOADS;
+    static_assert((GR_AHEAD - 1) * LOADS < 64, "as many as can be counted");
+    extern __shared__ __attribute__((aligned(16))) char gl_lds[];
+    __shared__ int32_t pos[GR_ROWS], src[GR_ROWS];
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l32 = lane & 31, half = lane >> 5;
+    const int K = A.K, N = A.N, D = N / 2, n0 = (int)(blockIdx.x % A.tiles_n) * GR_OUT, steps = (K + BK - 1) / BK;
+    int g;
+    int64_t k0, k1;
+    if (!find_tile(A.G, blockIdx.x / A.tiles_n, GR_ROWS, g, k0, k1)) return;
+    g = __builtin_amdgcn_readfirstlane(g);
+    if (t < GR_ROWS) entry(A, k0 + t, k1, pos[t], src[t]);
+    __syncthreads();
+    // this lane's loads (rows, columns, exchanges and what is read beyond K as in grouped_tile_kernel)
+    const char* const zero = (const char*)gl_zero;
+    const char* pa[A_LOADS];
+    auto a_piece = [&](int i) { return (lane % GL_PIECES) ^ (((GL_ROWS * i + lane / GL_PIECES) >> 1) & (GL_PIECES - 1)); };
+#pragma unroll
+    for (int i = 0; i < A_LOADS; ++i) {
+        const int32_t row = src[GL_ROWS * i + lane / GL_PIECES];
+        pa[i] = A.a + (int64_t)(row >= 0 ? row : 0) * A.a_stride + wave * GL_STEP + a_piece(i) * 16;
+    }
+    const char* w_at = A.W + ((int64_t)g * K + wave * BK) * N * E;
+    auto b_window = [](int k) { return T == FG_F32 ? (k >> 2) & 1 : (k >> 1) & 1; };
+    unsigned int pb[2];      // of even and odd loads
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int k = lane / B_PIECES, slot = lane % B_PIECES, w = b_window(B_ROWS * i + k);
+        const int c = T == FG_F32 ? (((slot >> 3) ^ w) * 8 + (slot & 7)) * 4 : (((slot >> 2) ^ w) * 4 + (slot & 3)) * 8, o = n0 + c % GR_OUT;
+        pb[i] = (unsigned int)(k * N + (o < D ? o + (c < GR_OUT ? 0 : D) : 0)) * E;
+    }
+    const unsigned int lds0 = (unsigned int)(uintptr_t)(__attribute__((address_space(3))) char*)gl_lds + wave * stages * GR_STAGE;
+    int to_load = wave, to_slot = 0;
+    auto load_next = [&]() {
+        const unsigned int to = __builtin_amdgcn_readfirstlane(lds0 + to_slot * GR_STAGE);
+        const int left = K - to_load * BK;
+        const char* const w = uniform(w_at);
+        if (left >= BK) {
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) load_to_lds(pa[i], to + i * 1024);
+#pragma unroll
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds(w, pb[i & 1] + (unsigned int)(i * B_ROWS * N * E), to + GR_ROWS * GL_STEP + i * 1024);
+        } else {
+#pragma unroll
+            for (int i = 0; i < A_LOADS; ++i) load_to_lds(a_piece(i) * (16 / E) < left ? pa[i] : zero, to + i * 1024);
+#pragma unroll
+            for (int i = 0; i < B_LOADS; ++i)
+                load_to_lds(B_ROWS * i + lane / B_PIECES < left ? w + pb[i & 1] + (unsigned int)(i * B_ROWS * N * E) : zero, to + GR_ROWS * GL_STEP + i * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < A_LOADS; ++i) pa[i] += GR_WAVES * GL_STEP;
+        w_at += (int64_t)GR_WAVES * BK * N * E;
+        to_slot = to_slot + 1 == stages ? 0 : to_slot + 1;
+        to_load += GR_WAVES;
+    };
+    gl_f32x16 acc[2], rest[T == FG_F32 ? 2 : 1];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        acc[0][e] = acc[1][e] = 0.f;
+        if constexpr (T == FG_F32) rest[0][e] = rest[1][e] = 0.f;
+    }
+    const int swap = ((l32 >> 1) & (GL_PIECES - 1)) << 4, place = (lane >> 2) & 3;
+    const int b_in = (8 * half + place) * B_ROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto multiply = [&](const char* As, int kk) {
+        const char* Bs = As + GR_ROWS * GL_STEP;
+        fg_u32x4 a[DEEP], b[2][DEEP];
+#pragma unroll
+        for (int q = 0; q < DEEP; ++q) a[q] = *(const fg_u32x4*)(As + l32 * GL_STEP + ((((kk * DEEP + q) * 2 + half) << 4) ^ swap));
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) {
+            if constexpr (T == FG_F32) {
+                const char* from = Bs + (kk * 16 + 4 * half) * B_ROW + ((nb ^ half) << 7) + l32 * 4;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b[nb][e >> 2][e & 3] = *(const unsigned int*)(from + (e + (e & 4)) * B_ROW);
+            } else {
+                typedef __attribute__((address_space(3))) gl_s16x4* lds_s16x4;
+                const char* from = Bs + kk * 16 * B_ROW + b_in + ((nb ^ b_window(place)) << 6);
+                const gl_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from);
+                const gl_s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 4 * B_ROW));
+                b[nb][0] = __builtin_bit_cast(fg_u32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+        }
+        if constexpr (T == FG_F32) {
+            constexpr int TA[5] = {2, 0, 1, 1, 0}, TB[5] = {0, 2, 1, 0, 1};      // smallest products first
+            fg_u32x4 sa[3];
+            split8(a, sa);
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) {
+                fg_u32x4 sb[3];
+                split8(b[nb], sb);
+#pragma unroll
+                for (int e = 0; e < 5; ++e) rest[nb] = mfma<FG_BF16>(&sb[TB[e]], &sa[TA[e]], rest[nb]);
+                acc[nb] = mfma<FG_BF16>(&sb[0], &sa[0], acc[nb]);
+            }
+        } else {
+#pragma unroll
+            for (int nb = 0; nb < 2; ++nb) acc[nb] = mfma<T>(b[nb], a, acc[nb]);
+        }
+    };
+    for (int i = 0; i < stages && to_load < steps; ++i) load_next();
+    int slot = 0;
+    for (int s = wave; s < steps; s += GR_WAVES) {
+        // this step's loads have arrived, those of the steps behind it stay on their way
+        const int behind = (to_load - s) / GR_WAVES - 1;
+        if (behind == 2)
+            own_arrived<2 * LOADS>();
+        else if (behind == 1)
+            own_arrived<LOADS>();
+        else
+            own_arrived<0>();
+#pragma unroll
+        for (int kk = 0; kk < SUB; ++kk) multiply(gl_lds + (wave * stages + slot) * GR_STAGE, kk);
+        if (to_load < steps) {
+            own_read();
+            load_next();
+        }
+        slot = slot + 1 == stages ? 0 : slot + 1;
+    }
+    __syncthreads();
+    float* const sums = (float*)gl_lds;      // [wave][projection][row][GR_SUM_ROW]
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            float4 v;
+            if constexpr (T == FG_F32)
+                v = float4{acc[nb][4 * q] + rest[nb][4 * q], acc[nb][4 * q + 1] + rest[nb][4 * q + 1], acc[nb][4 * q + 2] + rest[nb][4 * q + 2], acc[nb][4 * q + 3] + rest[nb][4 * q + 3]};
+            else
+                v = float4{acc[nb][4 * q], acc[nb][4 * q + 1], acc[nb][4 * q + 2], acc[nb][4 * q + 3]};
+            *(float4*)(sums + ((wave * 2 + nb) * GR_ROWS + l32) * GR_SUM_ROW + 8 * q + 4 * half) = v;
+        }
+    __syncthreads();
+    static_assert(GR_THREADS * 4 == GR_ROWS * GR_OUT, "four outputs a thread");
+    const int m = t >> 3, c = (t & 7) * 4;
+    const int32_t r = pos[m];
+    if (r < 0 || n0 + c >= D) return;      // (D is a multiple of four)
+    float z[2][4], h[4];
+#pragma unroll
+    for (int nb = 0; nb < 2; ++nb) {
+        float4 v = {0.f, 0.f, 0.f, 0.f};
+        const float* const bias = A.bias + (int64_t)g * N + nb * D + n0 + c;
+        if (A.bias) v = float4{bias[0], bias[1], bias[2], bias[3]};
+#pragma unroll
+        for (int w = 0; w < GR_WAVES; ++w) {
+            const float4 p = *(const float4*)(sums + ((w * 2 + nb) * GR_ROWS + m) * GR_SUM_ROW + c);
+            v.x += p.x, v.y += p.y, v.z += p.z, v.w += p.w;
+        }
+        z[nb][0] = v.x, z[nb][1] = v.y, z[nb][2] = v.z, z[nb][3] = v.w;
+    }
+    auto put = [&](char* to, int type, const float (&v)[4]) {
+        if (type == FG_F32)
+            *(fg_u32x4*)(to + (int64_t)(n0 + c) * 4) = fg_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else
+            *(fg_u32x2*)(to + (int64_t)(n0 + c) * 2) = type == FG_BF16 ? fg_to_words<FG_BF16>(v) : fg_to_words<FG_F16>(v);
+    };
+    if (A.z)
+#pragma unroll
+        for (int nb = 0; nb < 2; ++nb) put(A.z + r * A.z_stride + (int64_t)nb * D * E, T, z[nb]);
+    fg_with_act(A.act, [&](auto act) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = fg_act<decltype(act)::value>(z[0][e]) * z[1][e];
+    });
+    put(A.out + r * A.out_stride, A.out_type, h);
+}
+// As many of these tiles as the chip holds at once, or little more; fp32, whose large tiles hold a compute unit for longer, up to twice that. Both sides (this | large tiles):
+// 16 bits, 16 x 1024 x 1024 7.6 | 11.1 us, 256 rows 7.6 | 11.7, 512 rows 12.7 | 11.9, 1024 rows 22.7 | 13.9, 1 x 4096 x 2048 20.9 | 39.3; fp32, 16 rows 13.1 | 37.2,
+// 256 rows 15.3 | 38.2, 512 rows 27.6 | 38.6, 2048 rows 98 | 60, 16 x 256 x 256 7.1 | 12.1 (7 us is what calls in a row cost at least)
+template <int T>
+constexpr int64_t gr_most_tiles = T == FG_F32 ? 640 : 384;
+template <int T>
+fg_status_t gated_product(GlArgs& A, hipStream_t st) {
+    const int64_t rows = A.G.max_rows / GR_ROWS + (A.G.n_groups < A.G.max_rows ? A.G.n_groups : A.G.max_rows);
+    A.tiles_n = (int)fg_ceil_div(A.N / 2, GR_OUT);
+    if (rows * A.tiles_n > gr_most_tiles<T>) return tile_product<T, true, true>(A, st);
+    const int64_t rounds = fg_ceil_div(A.K, GR_WAVES * GL_STEP / (T == FG_F32 ? 4 : 2));      // steps of a wavefront
+    const int stages = rounds < GR_AHEAD ? (int)rounds : GR_AHEAD;
+    hipLaunchKernelGGL((gated_few_kernel<T>), dim3((unsigned)(rows * A.tiles_n)), dim3(GR_THREADS), (size_t)GR_WAVES * stages * GR_STAGE, st, A, stages);
+    FG_LAUNCH_CHECK("gated_few_kernel");
+    return FG_OK;
 }
 
 // ---- gradients ----
@@ -1552,9 +1748,9 @@ extern "C" fg_status_t fg_gated_linear_grouped(const void* x, int64_t x_rows, in
     A.x = A.a = (const char*)x, A.x_rows = x_rows, A.x_stride = A.a_stride = x_stride, A.a_by = GL_A_SOURCE, A.W = (const char*)W, A.bias = bias, A.src_ids = src_ids_dev;
     A.n = n_out, A.out = (char*)h_out, A.out_stride = out_stride, A.out_type = out_dtype, A.z = (char*)z_out, A.z_stride = z_stride, A.act = act;
     A.d_in = A.K = d_in, A.d_out = A.N = 2 * d_out;
-    if (dtype == FG_BF16) return tile_product<FG_BF16, true, true>(A, (hipStream_t)stream);
-    if (dtype == FG_F16) return tile_product<FG_F16, true, true>(A, (hipStream_t)stream);
-    return tile_product<FG_F32, true, true>(A, (hipStream_t)stream);
+    if (dtype == FG_BF16) return gated_product<FG_BF16>(A, (hipStream_t)stream);
+    if (dtype == FG_F16) return gated_product<FG_F16>(A, (hipStream_t)stream);
+    return gated_product<FG_F32>(A, (hipStream_t)stream);
 }
 
 extern "C" size_t fg_gated_linear_grouped_backward_workspace_bytes(fg_dtype_t dtype, int64_t max_rows, int32_t n_groups, int32_t d_in, int32_t d_out) {
