@@ -202,6 +202,10 @@ GATED = [  # dtype, out, n, groups, d_in, d_out, act, options
     ("bf16", "bf16", 130, 4, 72, 136, "relu", "keep src pad empty"), ("f16", "f16", 64, 2, 128, 32, "silu", "nobias"), ("f16", "f32", 200, 5, 40, 264, "sigmoid", "keep src"),
     ("f16", "f16", 1000, 3, 200, 72, "gelu", "keep order0"), ("bf16", "bf16", 3, 3, 2048, 64, "silu", "keep"), ("f16", "f16", 31, 31, 96, 96, "silu", "keep empty pad"),
     ("f32", "f32", 1000, 1024, 32, 64, "silu", "src"),
+    # few rows, the contraction split: none, one and several steps to a share of it, the last of them partly filled
+    ("f32", "f32", 40, 1, 2052, 20, "silu", "keep src"), ("f32", "f32", 35, 2, 388, 132, "gelu", "keep pad"), ("bf16", "bf16", 33, 1, 1096, 24, "gelu", "keep pad"),
+    ("f16", "f32", 64, 2, 520, 72, "silu", "keep empty"), ("bf16", "f32", 2, 1, 4096, 8, "silu", "src"), ("f16", "f16", 250, 1, 776, 1000, "silu", ""),
+    ("f32", "f32", 12_000, 5, 100, 36, "silu", "keep"), ("bf16", "bf16", 9000, 7, 136, 72, "gelu", "keep src"), ("f16", "f32", 5000, 2, 72, 200, "silu", "keep"),
 ]
 
 
