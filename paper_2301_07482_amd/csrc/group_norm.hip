@@ -30,7 +30,7 @@ struct GnArgs {
     int act, out_type;
     char* out;
     float *mean, *rstd;      // [n_groups x blocks]; the forward call's may be NULL
-    double* part;            // [chunks][2][blocks][3]: the sums of a chunk's parts of a group that began before it, and of one that begins in it
+    double* part;            // [chunks][2][blocks][4]: the sums of a chunk's parts of a group that began before it, and of one that begins in it, rows and level
     int32_t* info;           // [chunks][2]: those groups, -1: none
     float* joined;           // [chunks][blocks][2]: what the parts of the group that begins in the chunk come to
     int join_there;          // ... has been left there by a launch of its own
@@ -244,9 +244,9 @@ __device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const
         done(0, a, b);
     }
 }
-__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, int chunk, int which, int j, double s, double q, int rows) {
-    double* to = A.part + ((int64_t)(chunk * 2 + (which == GN_BEGINS)) * A.blocks + T.block0 + j) * 3;
-    to[0] = s, to[1] = q, to[2] = (double)rows;
+__device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, int chunk, int which, int j, double s, double q, int rows, float level) {
+    double* to = A.part + ((int64_t)(chunk * 2 + (which == GN_BEGINS)) * A.blocks + T.block0 + j) * 4;
+    to[0] = s, to[1] = q, to[2] = (double)rows, to[3] = (double)level;
 }
 __device__ __forceinline__ void note(const GnArgs& A, int chunk, int goes_on, int begins) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && chunk >= 0) A.info[chunk * 2] = goes_on, A.info[chunk * 2 + 1] = begins;
@@ -258,11 +258,6 @@ __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
 }
 // the block of a tile's column
 __device__ __forceinline__ int block_of(const GnArgs& A, int c) { return A.block == 1 ? c : (int)__umulhi((unsigned int)c, A.block_inverse); }
-// what a block's values are measured from: its first value in the group's first row (0 where that row does not exist)
-__device__ __forceinline__ float level(const GnArgs& A, int type, int g, int block) {
-    const int r = position(A, offset_of(A, g));
-    return r >= 0 ? element(A.x + (int64_t)r * A.x_stride, type, (int64_t)block * A.block) : 0.f;
-}
 // 1 / x and 1 / sqrt(x) to within a few steps of 2^-52: the hardware's estimates and Newton's steps (a division and a root take longer than the rest of a
 // small group's statistics)
 __device__ __forceinline__ double reciprocal(double x) {
@@ -436,9 +431,10 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
                 }
             },
             [&](int j, double a, double b) {
-                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows);
+                const float level = MANY ? S.from[j * A.block] : common;
+                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows, level);
                 float mean, rstd;
-                mean_rstd(A, MANY ? S.from[j * A.block] : common, a, b, (double)rows, mean, rstd);
+                mean_rstd(A, level, a, b, (double)rows, mean, rstd);
                 S.stats[j][0] = mean, S.stats[j][1] = rstd;
                 put_statistics(A, T, g, j, mean, rstd);
             });
@@ -460,13 +456,15 @@ __global__ __launch_bounds__(TH, 4) void group_norm_kernel(GnArgs A) {
 }
 
 // the sums of all parts of the split group that begins in a chunk, in order: lanes of a wavefront together
-__device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin, int block, double& s, double& q, double& rows) {
+__device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin, int block, double& s, double& q, double& rows, double& level) {
     const unsigned int last = (offset_of(A, g + 1) - 1) / A.rows;
-    s = q = rows = 0.0;
+    s = q = rows = level = 0.0;
     for (unsigned int c = begin + fg_lane(); c <= last; c += 64) {
-        const double* p = A.part + ((int64_t)(c * 2 + (c == begin)) * A.blocks + block) * 3;
+        const double* p = A.part + ((int64_t)(c * 2 + (c == begin)) * A.blocks + block) * 4;
         s += p[0], q += p[1], rows += p[2];
+        if (c == begin) level = p[3];
     }
+    level = __shfl(level, 0, 64);
     for (int off = 32; off > 0; off >>= 1) {
         s += __shfl_xor(s, off, 64);
         q += __shfl_xor(q, off, 64);
@@ -476,13 +474,13 @@ __device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin,
 // what the parts come to, and the forward call's results
 template <int T_, bool BACKWARD>
 __device__ __forceinline__ void joined(const GnArgs& A, int g, unsigned int begin, int block, bool write, float& a, float& b) {
-    double s, q, rows;
-    join(A, g, begin, block, s, q, rows);
+    double s, q, rows, level;
+    join(A, g, begin, block, s, q, rows, level);
     if constexpr (BACKWARD) {
         const double per = reciprocal(rows > 0.0 ? rows * A.block : 1.0);
         a = (float)(s * per), b = (float)(q * per);
     } else {
-        mean_rstd(A, level(A, T_, g, block), s, q, rows, a, b);
+        mean_rstd(A, (float)level, s, q, rows, a, b);      // (as it was left with the sums: y may be written over x meanwhile)
         if (write && fg_lane() == 0) {
             if (A.mean) A.mean[(int64_t)g * A.blocks + block] = a;
             if (A.rstd) A.rstd[(int64_t)g * A.blocks + block] = b;
@@ -709,7 +707,7 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
                 }
             },
             [&](int j, double a, double b) {
-                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows);
+                if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows, 0.f);
                 const double per = reciprocal(rows > 0 ? (double)rows * A.block : 1.0);
                 S.stats[j][0] = (float)(a * per), S.stats[j][1] = (float)(b * per);
             });
@@ -817,7 +815,7 @@ struct Space {
 Space space_of(int64_t max_rows, int n_groups, int d, int blocks, bool backward) {
     const int64_t chunks = max_rows < GN_PLACES ? max_rows + 1 : GN_PLACES;      // (two rows to a chunk at least, and no more chunks than places)
     Space W = {};
-    W.part = fg_align_up((size_t)chunks * 2 * blocks * 3 * 8, 256);
+    W.part = fg_align_up((size_t)chunks * 2 * blocks * 4 * 8, 256);
     W.info = fg_align_up((size_t)chunks * 2 * 4, 256);
     W.joined = fg_align_up((size_t)chunks * blocks * 2 * 4, 256);
     if (backward) W.columns = (size_t)(chunks + (n_groups < GN_MOST_WORKERS ? n_groups : GN_MOST_WORKERS)) * 2 * d * 4;

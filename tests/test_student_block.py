@@ -554,6 +554,26 @@ def test_group_norm_leaves_out_what_is_out_of_range(B):
         assert bool((y.cpu()[~taken] == -77).all()) and bool((dx.cpu()[~taken] == -77).all())
 
 
+@gpu
+@pytest.mark.parametrize("dtype, n, d, blocks", [("f32", 40_000, 256, 8), ("bf16", 300_000, 64, 8), ("f32", 20_000, 64, 2), ("f16", 30_000, 512, 1), ("bf16", 9000, 1024, 32)])
+def test_group_norm_of_split_groups_over_their_own_rows(B, dtype, n, d, blocks):
+    """Rows of groups that many workgroups share are overwritten while others still form the statistics: the same bits as beside them, every time."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = (torch.randn(n, d, device="cuda", generator=g) + 5 * torch.randn(d, device="cuda", generator=g)).to(T[dtype])
+    off = torch.tensor([0, n // 3, n], device="cuda")
+    ws = torch.zeros(B.fg_group_norm_workspace_bytes(n, 2, d, blocks), dtype=torch.uint8, device="cuda")
+    y = torch.empty_like(x)
+
+    def call(x, y):
+        B.fg_group_norm(x, stride(x), code(B, dtype), None, off, n, 2, n, d, blocks, None, None, 1e-5, B.FG_ACT_NONE, y, stride(y), code(B, dtype), None, None, ws, len(ws))
+
+    call(x, y)
+    for _ in range(20):
+        over = x.clone()
+        call(over, over)
+        assert torch.equal(over, y)
+
+
 # ---- distillation ----
 
 DISTILL = [  # dtype, dh, n, d, k, top, T, alpha, options
