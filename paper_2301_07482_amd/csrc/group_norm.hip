@@ -12,8 +12,11 @@
 namespace {
 
 constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 1024, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
+constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_LEAST_VALUES = 16384, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
 constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;      // rows whose reads are on their way together
+
+// workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them
+constexpr int gn_per_unit(int type, bool many, bool backward) { return type == FG_F32 && many != backward ? 3 : 4; }
 
 struct GnArgs {
     const int32_t* order;      // NULL: position k itself
@@ -181,30 +184,66 @@ struct Scratch {
     float stats[GN_COLUMNS][2];                 // of a block: mean and rstd, or the gradient's two means
     int rows[TH / 64];
 };
+// Lanes l and l + HALF (of 64 for HALF = 32, of every 32 for 16) add up a and b between them: the first has a's sum, the other b's
+template <int HALF>
+__device__ __forceinline__ float half_sums(float a, float b) {
+    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
+    const unsigned int x = __float_as_uint(a), y = __float_as_uint(b);
+    const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int HALF>
+__device__ __forceinline__ double half_sums(double a, double b) {
+    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
+    const fg_u32x2 x = __builtin_bit_cast(fg_u32x2, a), y = __builtin_bit_cast(fg_u32x2, b);
+    fg_u32x2 first, second;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false) : __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
+        first[i] = r[0], second[i] = r[1];
+    }
+    return __builtin_bit_cast(double, first) + __builtin_bit_cast(double, second);
+}
 // The sums s[e], q[e] of a thread's columns (MANY) or s[0], q[0] of all it has seen, over the rows that a wavefront has side by side, and the number of rows;
-// they are there after the workgroup's next barrier.
+// they are there after the workgroup's next barrier. Halves of the wavefront exchange half of their sums each: 16 fp64 sums over four rows take 24 exchanges between
+// registers instead of 64 through LDS.
 template <int TH, bool MANY, typename V>
 __device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch<TH>& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows) {
-    constexpr int N = MANY ? 8 : 1;
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-        for (int off = MANY ? A.width : 1; off < 64; off <<= 1) {
-            s[e] += __shfl_xor(s[e], off, 64);
-            q[e] += __shfl_xor(q[e], off, 64);
-        }
-    for (int off = 32; off > 0; off >>= 1) rows += __shfl_xor(rows, off, 64);
+    for (int off = A.width; off < 64; off <<= 1) rows += __shfl_xor(rows, off, 64);
     if (fg_lane() == 0) S.rows[fg_wave()] = rows;
     if constexpr (MANY) {
         const Piece P = piece_of(A, T, 0);
-        if (fg_lane() < A.width)
+        double* const to = S.wave[fg_wave()] + P.c;
+        if (A.width >= 64) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e >= P.twice) {
-                    S.wave[fg_wave()][P.c + e] = (double)s[e];
-                    S.wave[fg_wave()][GN_COLUMNS + P.c + e] = (double)q[e];
-                }
-    } else if (fg_lane() == 0) {
-        S.wave[fg_wave()][0] = (double)s[0], S.wave[fg_wave()][GN_COLUMNS] = (double)q[0];
+                if (e >= P.twice) to[e] = (double)s[e], to[GN_COLUMNS + e] = (double)q[e];
+            return;
+        }
+        V v[8];      // of s in the first half of the wavefront, of q in the second
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = half_sums<32>(s[e], q[e]);
+        const int base = fg_lane() < 32 ? 0 : GN_COLUMNS;
+        if (A.width == 32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= P.twice) to[base + e] = (double)v[e];
+            return;
+        }
+        const int e0 = fg_lane() & 16 ? 4 : 0;      // four columns of the piece
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = half_sums<16>(v[e], v[e + 4]);
+            for (int off = A.width; off < 16; off <<= 1) v[e] += __shfl_xor(v[e], off, 64);
+        }
+        if ((fg_lane() & 15) < A.width)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (e0 + e >= P.twice) to[base + e0 + e] = (double)v[e];
+    } else {
+        V v = half_sums<32>(s[0], q[0]);
+        for (int off = 1; off < 32; off <<= 1) v += __shfl_xor(v, off, 64);
+        if ((fg_lane() & 31) == 0) S.wave[fg_wave()][fg_lane() ? GN_COLUMNS : 0] = (double)v;
     }
 }
 template <int TH>
@@ -212,7 +251,7 @@ __device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch<TH>& S) {
     int all = 0;
 #pragma unroll
     for (int w = 0; w < TH / 64; ++w) all += S.rows[w];
-    return all / A.width;      // (every lane of a row has counted it)
+    return A.width > 64 ? all / (A.width / 64) : all;      // (every wavefront of a row has counted it)
 }
 // done(block of the tile, s, q) by one thread of every block, of the sums over its columns; column(c, s, q) makes of a column's what is to be added
 template <int TH, bool MANY, typename Column, typename Done>
@@ -258,6 +297,15 @@ __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
 }
 // the block of a tile's column
 __device__ __forceinline__ int block_of(const GnArgs& A, int c) { return A.block == 1 ? c : (int)__umulhi((unsigned int)c, A.block_inverse); }
+// the two values of S.stats for each of a piece's columns
+template <int TH, bool MANY>
+__device__ __forceinline__ void stats_of(const GnArgs& A, const Scratch<TH>& S, int c, float (&first)[8], float (&second)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int j = MANY ? block_of(A, c + e) : 0;
+        first[e] = S.stats[j][0], second[e] = S.stats[j][1];
+    }
+}
 // 1 / x and 1 / sqrt(x) to within a few steps of 2^-52: the hardware's estimates and Newton's steps (a division and a root take longer than the rest of a
 // small group's statistics)
 __device__ __forceinline__ double reciprocal(double x) {
@@ -334,13 +382,11 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
         if (!P.there) break;
-        float w[8], b[8], mean[8];
+        float w[8], b[8], mean[8], rstd[8];
         affine(A, T, P.c, w, b);
+        stats_of<TH, MANY>(A, S, P.c, mean, rstd);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = MANY ? block_of(A, P.c + e) : 0;
-            mean[e] = S.stats[j][0], w[e] *= S.stats[j][1];
-        }
+        for (int e = 0; e < 8; ++e) w[e] *= rstd[e];
         const auto finish = [&](int u, int r) {
             float f[8];
             fg_piece_values<T_>(v[u], f);
@@ -447,7 +493,7 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
     if constexpr (PARTS) note(A, chunk, goes_on, begins);
 }
 template <int TH, int T_, bool MANY>
-__global__ __launch_bounds__(TH, 4) void group_norm_kernel(GnArgs A) {
+__global__ __launch_bounds__(TH, gn_per_unit(T_, MANY, false)) void group_norm_kernel(GnArgs A) {
     __shared__ Scratch<TH> S;
     if ((int)blockIdx.y < A.workers)
         norm_body<TH, T_, MANY, false>(A, S);
@@ -620,11 +666,7 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
         GradColumns C;
         grad_columns<MANY, false>(A, T, g, P.c, C);
         float m1[8], m2[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = MANY ? block_of(A, P.c + e) : 0;
-            m1[e] = S.stats[j][0], m2[e] = S.stats[j][1];
-        }
+        stats_of<TH, MANY>(A, S, P.c, m1, m2);
         gradient_rows<X, G, false>(A, T, P.c, C, k0, k1, held, R, [&](int r, const float(&xh)[8], float(&t)[8]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) t[e] = C.rstd[e] * (t[e] * C.w[e] - m1[e] - xh[e] * m2[e]);
@@ -754,7 +796,7 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
     }
 }
 template <int TH, int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(TH, NP > 1 ? 1 : 4) void group_norm_backward_kernel(GnArgs A) {
+__global__ __launch_bounds__(TH, NP > 1 ? 1 : gn_per_unit(X, MANY, true)) void group_norm_backward_kernel(GnArgs A) {
     __shared__ Scratch<TH> S;
     if ((int)blockIdx.y < A.workers)
         gradient_body<TH, X, G, MANY, NP, false>(A, S);
@@ -781,7 +823,7 @@ struct Plan {
     int64_t rows, chunks, long_rows;      // chunks 0: no group can be so large that it is split
     bool join_there;
 };
-Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks) {
+Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks, int type, bool backward) {
     Plan P;
     const int block = d / blocks, per_tile = GN_COLUMNS / block;
     P.tiles = (int)fg_ceil_div(blocks, per_tile < 1 ? 1 : per_tile);
@@ -792,20 +834,23 @@ Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks) {
         cols = P.tile_blocks * block, pieces = (int)fg_ceil_div(cols, 8);
         P.width = 1;
         while (P.width < pieces && P.width < GN_THREADS) P.width *= 2;
-        places = GN_PLACES / P.tiles, least = 2 * (GN_THREADS / P.width);
+        places = GN_UNITS * gn_per_unit(type, P.tile_blocks > 1, backward) / P.tiles, least = 2 * (GN_THREADS / P.width);
         if (P.tiles * 2 > blocks || blocks / (P.tiles * 2) * block < 8 || (max_rows / least + n_groups) * P.tiles > GN_FEW_WORKGROUPS) break;
     }
     P.pieces = (int)fg_ceil_div(pieces, P.width);
     const int64_t even = max_rows / places + 1, most = GN_MOST_WORKERS / P.tiles;
     P.rows = even > least ? even : least;
-    P.long_rows = P.rows > GN_FEW_VALUES / cols ? P.rows : GN_FEW_VALUES / cols;
+    const int64_t whole = (int64_t)n_groups * P.tiles, few = whole >= GN_UNITS ? GN_FEW_VALUES : GN_FEW_VALUES * whole / GN_UNITS;
+    const int64_t few_rows = (few > GN_LEAST_VALUES ? few : GN_LEAST_VALUES) / cols;
+    P.long_rows = P.rows > few_rows ? P.rows : few_rows;
     P.chunks = P.long_rows < max_rows ? max_rows / P.rows + 1 : 0;
     P.threads = P.width <= 64 && P.pieces == 1 && max_rows / n_groups * P.width <= 64 * GN_SMALL_STEPS ? 64 : GN_THREADS;
     P.workers = (int)(n_groups < most ? n_groups : most);
     P.join_there = P.chunks * P.tile_blocks > GN_JOIN_HERE;
     return P;
 }
-static_assert(FG_MAX_NORM_DIM <= GN_THREADS * 8 * GN_MAX_PIECES && FG_MAX_NORM_DIM / GN_COLUMNS * 2 <= GN_PLACES, "pieces of a row; tiles");
+static_assert(FG_MAX_NORM_DIM <= GN_THREADS * 8 * GN_MAX_PIECES && FG_MAX_NORM_DIM / GN_COLUMNS * 2 <= GN_UNITS * 3, "pieces of a row; tiles");
+static_assert(GN_UNITS * 4 <= GN_PLACES, "what a workspace is measured for");
 
 // A workspace for max_rows serves fewer rows too: by the most chunks that a call can have
 struct Space {
@@ -917,7 +962,7 @@ extern "C" fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t
     const Space W = space_of(max_rows, n_groups, d, channel_groups, false);
     FG_TRY(check_space(who, ws_dev, ws_bytes, W.total()));
     fg_clear_error();
-    const Plan P = plan_of(max_rows, n_groups, d, channel_groups);
+    const Plan P = plan_of(max_rows, n_groups, d, channel_groups, dtype, false);
     GnArgs A = args_of(P, W, order_dev, offsets_dev, max_rows, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.out = (char*)y, A.out_stride = y_stride, A.out_type = y_dtype, A.weight = weight, A.bias = bias, A.eps = eps, A.act = act;
     A.mean = mean_out, A.rstd = rstd_out;
@@ -960,7 +1005,7 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     const Space W = space_of(max_rows, n_groups, d, channel_groups, true);
     FG_TRY(check_space(who, ws_dev, ws_bytes, W.total()));
     fg_clear_error();
-    const Plan P = plan_of(max_rows, n_groups, d, channel_groups);
+    const Plan P = plan_of(max_rows, n_groups, d, channel_groups, dtype, true);
     GnArgs A = args_of(P, W, order_dev, offsets_dev, work ? max_rows : 0, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.dy = (const char*)dy, A.dy_stride = dy_stride, A.out = (char*)dx, A.out_stride = dx_stride, A.weight = weight, A.bias = bias;
     A.act = act, A.mean = const_cast<float*>(mean), A.rstd = const_cast<float*>(rstd);
