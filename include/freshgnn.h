@@ -1017,7 +1017,7 @@ fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t
                                    void* stream);
 
 /*
- * Loss of a student against a teacher's stored top logits and against labels, and its gradient, for the rows listed (r = rows[k]; NULL: r = k):
+ * Loss of a student against a teacher's stored top logits and against labels, and its gradient, for the rows listed (r = rows[k], no row twice; NULL: r = k):
  *   p = softmax of top_val[v, j] / temperature over the k stored entries of node v = ids[r] (NULL: v = r) whose class top_idx[v, j] lies in [0, d)
  *   q_T = softmax(h[r, :] / temperature), q = softmax(h[r, :])
  *   loss[r] = weight[r] * (alpha * temperature^2 * sum_j p_j * (log p_j - log q_T[c_j]) - (1 - alpha) * log q[labels[r]])

@@ -4,6 +4,9 @@
 // from registers where the group is small enough, else from the caches. A group of many rows is split: the entries of all groups are a line that is cut into
 // chunks of rows, every chunk's workgroup leaves the sums of its part, a second launch goes over the rows again with what all parts come to. A workgroup takes a tile of
 // whole blocks of columns; a thread has pieces of eight adjacent columns (whole ones: the last of a tile overlaps the one before it) and every so many-th row.
+// Bound by memory where rows are many: 58982 listed rows x 1024 bf16 in 4 groups 98 us (sums 29, result 49, both of what a copy would take), gradients 166 (73, sums 5, 72).
+// Many small groups are bound by what their reductions take beside their values (31744 x 100 fp32 in 1024 groups 17 us, 29 with cold caches, of 5 for the bytes), few rows by the
+// latency of reads that depend on each other (777 x 88 6.0, gradients 11.8).
 #include "activation.h"
 #include "row_list.h"
 #include "row_types.h"
@@ -12,11 +15,15 @@
 namespace {
 
 constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 131072, GN_LEAST_VALUES = 16384, GN_JOIN_HERE = 8192, GN_MAX_PIECES = 8;
-constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;      // rows whose reads are on their way together
+constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 65536, GN_LEAST_VALUES = 24576, GN_JOIN_HERE = 4000, GN_MAX_PIECES = 8;
+// Rows of a thread whose reads are on their way together. Two | one: forward 17.2 | 18.3 us for 31744 x 100 in 1024 groups, 24.6 | 26.5 for 100000 x 40 in 10000 groups,
+// 27.6 | 25.6 for 65536 x 128 in 4096 groups; gradients, which have two arrays to read, 39.7 | 37.0 and 71 | 62 for the first two
+constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;
 
-// workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them
-constexpr int gn_per_unit(int type, bool many, bool backward) { return type == FG_F32 && many != backward ? 3 : 4; }
+// Workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them. Three | four, fp32: 31744 x 100 in 1024
+// groups 17.2 | 22.5 us, its gradients 36.6 | 48.6, those of 777 x 88 in 9 groups 11.8 | 13.5, of 65536 x 1024 in 4 groups 281 | 295, of 100000 x 40 in 10000 groups 62 | 104;
+// rows of one block forward 30.7 | 28.2 (65536 x 128 in 4096 groups); bf16 gradients of 58982 listed rows x 1024 in 4 groups 172 | 166
+constexpr int gn_per_unit(int type, bool many, bool backward) { return type == FG_F32 && (backward || many) ? 3 : 4; }
 
 struct GnArgs {
     const int32_t* order;      // NULL: position k itself
@@ -814,10 +821,16 @@ __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_backward_apply_kerne
     });
 }
 
-// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block. A group whose values in a tile are up to GN_FEW_VALUES is not split.
-// Chunks of rows for the others, with two rows a thread at least, so that all workgroups are on the chip at once, four to a compute unit (a few of them in a second
-// turn take as long as all the others). Where there are few groups and rows, tiles of fewer blocks. One wavefront to a workgroup where an average group's rows are up to
-// GN_SMALL_STEPS steps of one.
+// How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block. Where there are few groups and rows (fewer than GN_FEW_WORKGROUPS workgroups), tiles
+// of fewer blocks (777 x 88 in 9 groups, 8 blocks: 6.0 us, 11.3 without; 2000 rows 6.4, 16.4).
+// A group is not split as long as its workgroup, alone with its tile, ends with the others: up to GN_FEW_VALUES values in a tile where the groups fill the chip, fewer where
+// they do not, down to GN_LEAST_VALUES (with | without: 5000 x 88 in 9 groups 16 | 32 us, gradients 19 | 53; 20000 x 256 in 40 groups 25 | 61, gradients 38 | 117; a
+// limit of 16384 values has 2000 x 88 in 9 groups wait for launches that have nothing to do, 8.8 against 6.4). If no group of max_rows rows can be split, the launches for the parts are left out.
+// Chunks of rows for the split groups, with two rows a thread at least, so that all workgroups are on the chip at once (a few of them in a second turn take as long as all
+// the others). Their sums are joined in a launch of its own from GN_JOIN_HERE chunks and blocks on, else by every workgroup of the second pass for itself: 8000 x 2048
+// bf16 in 256 blocks 30 us against 44, 65536 x 256 in 8 blocks 43 against 46; 31744 x 100 in 5 blocks 18.8 against 17.2, 65536 x 256 in one block 40.9 against 38.6.
+// One wavefront to a workgroup where an average group's rows are up to GN_SMALL_STEPS steps of one: 50000 x 32 in 20000 groups 35 us against 125, gradients 67 against 166;
+// at eight steps (31 rows x 100) 53 against 25.
 struct Plan {
     int tiles, tile_blocks, width, pieces, threads, workers;
     int64_t rows, chunks, long_rows;      // chunks 0: no group can be so large that it is split
