@@ -1031,7 +1031,8 @@ fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t
  *   dh, dh_dtype                        n rows by position, `dtype` or FG_F32; NULL: not wanted; dh may be h (of one type)
  * A row without a teacher (no entry with a class in [0, d) and a value above -infinity, a node outside [0, table_rows), alpha = 0) has no first term, one without a
  * label in [0, d) (or with alpha = 1) no second; a row with neither has loss 0 and gradient 0 whatever its logits. A class that is stored twice has
- * the sum of both. A logit of -infinity is a class that cannot be chosen: no gradient, an infinite loss if the teacher or the label has it.
+ * the sum of both. A logit of -infinity is a class that cannot be chosen: no gradient, an infinite loss if the teacher or the label has it. Where no
+ * class of a row with a teacher or a label can be chosen, and where a logit is +infinity or NaN, the row's loss and gradient are NaN.
  * Exponentials, gradients and sums in fp32, those of wide rows (more than 512 columns) in fp64 from eight columns on. Pointers and strides aligned to the
  * element, d up to FG_MAX_CLASSES.
  */

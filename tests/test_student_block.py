@@ -682,6 +682,30 @@ def test_distill_loss_of_masked_classes(B, dtype, d):
 
 
 @gpu
+@pytest.mark.parametrize("d", [1, 40, 500, 3000, 20_000])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_distill_loss_of_rows_without_a_class_to_choose(B, dtype, d):
+    """All classes masked: NaN where there is a teacher or a label, nothing where there is neither; the rows beside them as if they were not there."""
+    h = torch.randn(5, d, generator=torch.Generator().manual_seed(2)).to(T[dtype])
+    h[:3] = -math.inf
+    h[3, d // 2] = math.inf
+    idx, val = torch.tensor([[0], [-1], [-1], [0], [d - 1]], dtype=torch.int32), torch.zeros(5, 1)
+    label = torch.tensor([-1, 0, -1, -1, 0], dtype=torch.int32)
+    for temperature in (1.0, 2.0, 3.0):
+        loss, dh = torch.full((5,), -77.0, device="cuda"), torch.full((5, d), -77.0, dtype=T[dtype], device="cuda")
+        B.fg_distill_loss(h.cuda(), stride(h), code(B, dtype), None, None, 5, 5, d, None, idx.cuda(), val.cuda(), B.FG_F32, 5, 1, label.cuda(), temperature, 0.5, None, 1.0, loss, dh,
+                          stride(dh), code(B, dtype))
+        torch.cuda.synchronize()
+        loss, dh = loss.cpu(), dh.cpu()
+        for i in (0, 1, 3):
+            assert bool(torch.isnan(loss[i])) and bool(torch.isnan(dh[i]).all()), i
+        assert float(loss[2]) == 0 and not bool(dh[2].any())
+        want, off, grad, grad_off = R.distill(h[4:], idx[4:], val[4:], label[4:], temperature, 0.5, None, 1.0)
+        close(loss[4:], want, off + 2.0 ** -24 * want.abs(), "loss")
+        close(dh[4:], grad, grad_off + HALF[dtype] * grad.abs() + TINY[dtype], "dh")
+
+
+@gpu
 def test_distill_loss_of_no_rows(B):
     h, loss = torch.ones(3, 8, device="cuda"), torch.full((3,), -77.0, device="cuda")
     count = torch.zeros(1, dtype=torch.int64, device="cuda")
