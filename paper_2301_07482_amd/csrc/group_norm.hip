@@ -15,7 +15,8 @@
 namespace {
 
 constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
-constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 3072, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 65536, GN_LEAST_VALUES = 24576, GN_JOIN_HERE = 4000, GN_MAX_PIECES = 8;
+constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 12 * GN_UNITS, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 65536, GN_LEAST_VALUES = 24576;
+constexpr int GN_JOIN_HERE = 4000, GN_MAX_PIECES = 8;
 // Rows of a thread whose reads are on their way together. Two | one: forward 17.2 | 18.3 us for 31744 x 100 in 1024 groups, 24.6 | 26.5 for 100000 x 40 in 10000 groups,
 // 27.6 | 25.6 for 65536 x 128 in 4096 groups; gradients, which have two arrays to read, 39.7 | 37.0 and 71 | 62 for the first two
 constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;

@@ -574,6 +574,46 @@ def test_group_norm_of_split_groups_over_their_own_rows(B, dtype, n, d, blocks):
         assert torch.equal(over, y)
 
 
+@gpu
+@pytest.mark.parametrize("n", [300, 60_000])
+def test_group_norm_of_the_most_groups(B, n):
+    """2^20 groups, nearly all of them without rows, one of half of the rows among them; forward and back."""
+    G, d, blocks = B.FG_MAX_NORM_GROUPS, 16, 2
+    r = np.random.default_rng(n)
+    group = r.integers(0, G, n)
+    group[:n // 2] = G // 3
+    group[-1] = G - 1
+    group = np.sort(group)
+    off = torch.from_numpy(np.searchsorted(group, np.arange(G + 1))).cuda()
+    x, dy = values(r, n, d, "f32"), values(r, n, d, "f32")
+    y, dx, mean, rstd = (torch.full(s, -77.0, device="cuda") for s in ((n, d), (n, d), (G, blocks), (G, blocks)))
+    dw, db = torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+    ws = torch.full((B.fg_group_norm_backward_workspace_bytes(n, G, d, blocks),), 255, dtype=torch.uint8, device="cuda")
+    xd, gd = x.cuda(), dy.cuda()
+    B.fg_group_norm(xd, d * 4, B.FG_F32, None, off, n, G, n, d, blocks, None, None, 0.25, B.FG_ACT_SILU, y, d * 4, B.FG_F32, mean, rstd, ws, len(ws))
+    B.fg_group_norm_backward(gd, d * 4, B.FG_F32, xd, d * 4, B.FG_F32, mean, rstd, None, None, B.FG_ACT_SILU, None, off, n, G, n, d, blocks, dx, d * 4, dw, db, ws, len(ws))
+    torch.cuda.synchronize()
+    y, dx, mean, rstd, dw, db = (t.cpu() for t in (y, dx, mean, rstd, dw, db))
+    there = np.unique(group)
+    none = np.setdiff1d(np.arange(G), there)
+    assert bool((mean[none] == 0).all()) and bool((rstd[none] == 2).all())
+    sums = [torch.zeros(d, dtype=torch.float64) for _ in range(4)]
+    for g in there if n < 1000 else there[:40].tolist() + [G // 3, G - 1]:
+        pos = torch.from_numpy(np.flatnonzero(group == g))
+        m, s = R.norm_statistics(x[pos], blocks, 0.25)
+        close(mean[g], m, 2.0 ** -24 * m.abs() + 2.0 ** -40 * x[pos].double().abs().max(), "mean")
+        close(rstd[g], s, 2.0 ** -23 * s, "rstd")
+        want, tol, _, _ = R.norm_rows(x[pos], m, s, None, None, "silu")
+        close(y[pos], want, tol + 2.0 ** -24 * want.abs(), "y")
+        (want, tol), (gw, gw_off), (gb, gb_off), _ = R.norm_backward(x[pos], dy[pos], mean[g], rstd[g], None, None, "silu")
+        close(dx[pos], want, tol + 2.0 ** -24 * want.abs(), "dx")
+        for t, v in zip(sums, (gw, gw_off, gb, gb_off)):
+            t += v
+    if n < 1000:
+        close(dw, sums[0], sums[1] + 2.0 ** -23 * sums[0].abs(), "dw")
+        close(db, sums[2], sums[3] + 2.0 ** -23 * sums[2].abs(), "db")
+
+
 # ---- distillation ----
 
 DISTILL = [  # dtype, dh, n, d, k, top, T, alpha, options
