@@ -322,8 +322,6 @@ def _own_gnorm_bw(s):
     B, T, A = _lib()
     c = s.case
     d, e, t, parts, groups = c["d"], _SIZE[c["dtype"]], T[c["dtype"]], c["parts"], c["channel_groups"]
-    if s.ws is None:      # the call takes the statistics as the forward call writes them: a part's behind each other
-        s.mean, s.rstd = s.mean.contiguous(), s.rstd.contiguous()
     ws, ws_bytes = _workspace(s, lambda: B.fg_group_norm_backward_workspace_bytes(s.n, parts, d, groups))
     B.fg_group_norm_backward(s.dy, d * e, t, s.x, d * e, t, s.mean, s.rstd, s.w, s.b, A[c["act"]], s.order, s.offsets, s.n, parts, s.n, d, groups,
                              s.dx, d * e, s.dw, s.db, ws, ws_bytes, _stream())
