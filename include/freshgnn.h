@@ -1005,16 +1005,18 @@ fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, con
  *   dx[r, c] = rstd[g, j] * (t * weight[c] - m1 - xh * m2),  m1, m2 = the means of t * weight and t * weight * xh over the group's rows and block j
  *   dw[c] = sum over all groups' rows of t * xh,  db[c] = that of t      ([d] float; NULL: not wanted)
  *   dy, dx, grad_dtype                  n rows of d values by position, FG_F32 or `dtype`; dx may be dy
- *   x, mean, rstd, ...                  as in the forward call (mean, rstd its mean_out, rstd_out)
+ *   mean, rstd, stat_stride, stat_step  the forward call's mean_out, rstd_out, or what a program has of them in another layout: group g and block j at
+ *                                       g * stat_stride + j * stat_step floats (channel_groups and 1 as the forward call leaves them); not negative, stat_step up to 2 * FG_MAX_NORM_GROUPS
+ *   x, ...                              as in the forward call
  *   ws_dev, ws_bytes                    >= fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
  * Means in fp64; dw and db in fp32 within and fp64 across ranges of rows; results do not depend on scheduling.
  */
 size_t fg_group_norm_backward_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups);
 fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* x, int64_t x_stride, fg_dtype_t dtype,
-                                   const float* mean, const float* rstd, const float* weight, const float* bias, fg_act_t act,
-                                   const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int64_t n, int32_t d,
-                                   int32_t channel_groups, void* dx, int64_t dx_stride, float* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes,
-                                   void* stream);
+                                   const float* mean, const float* rstd, int64_t stat_stride, int64_t stat_step, const float* weight,
+                                   const float* bias, fg_act_t act, const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows,
+                                   int32_t n_groups, int64_t n, int32_t d, int32_t channel_groups, void* dx, int64_t dx_stride, float* dw_dev,
+                                   float* db_dev, void* ws_dev, size_t ws_bytes, void* stream);
 
 /*
  * Loss of a student against a teacher's stored top logits and against labels, and its gradient, for the rows listed (r = rows[k], no row twice; NULL: r = k):

@@ -108,8 +108,8 @@ SIGNATURES = {
     "fg_group_norm_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
     "fg_group_norm": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i32, _i64, _i32, _i32, _p, _p, _f, _i32, _p, _i64, _i32, _p, _p, _p, _sz, _p]),
     "fg_group_norm_backward_workspace_bytes": (_sz, [_i64, _i32, _i32, _i32]),
-    "fg_group_norm_backward": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _p, _p, _i32, _p, _p, _i64, _i32, _i64, _i32, _i32, _p, _i64, _p, _p, _p,
-                                      _sz, _p]),
+    "fg_group_norm_backward": (_i32, [_p, _i64, _i32, _p, _i64, _i32, _p, _p, _i64, _i64, _p, _p, _i32, _p, _p, _i64, _i32, _i64, _i32, _i32, _p, _i64,
+                                      _p, _p, _p, _sz, _p]),
     "fg_distill_loss": (_i32, [_p, _i64, _i32, _p, _p, _i64, _i64, _i32, _p, _p, _p, _i32, _i64, _i32, _p, _f, _f, _p, _f, _p, _p, _i64, _i32, _p]),
 }
 
@@ -605,10 +605,28 @@ def fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups
     return int(_lib.fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups))
 
 
+def _statistics_strides(mean, rstd, n_groups, channel_groups):
+    """Of mean and rstd, in elements: those of the tensors; of addresses, as fg_group_norm writes them."""
+    def of(t):
+        if t is None or isinstance(t, int) or t.is_contiguous():
+            return channel_groups, 1
+        if tuple(t.shape) != (n_groups, channel_groups):
+            raise FgError(FG_ERR_SHAPE, f"fg_group_norm_backward: mean and rstd of the shape {tuple(t.shape)} neither lie behind each other nor are [n_groups, channel_groups]")
+        return t.stride(0) if n_groups > 1 else channel_groups, t.stride(1) if channel_groups > 1 else 1
+
+    strides = of(mean)
+    if of(rstd) != strides:
+        raise FgError(FG_ERR_SHAPE, "fg_group_norm_backward: mean and rstd have different strides")
+    return strides
+
+
 def fg_group_norm_backward(dy, dy_stride, grad_dtype, x, x_stride, dtype, mean, rstd, weight, bias, act, order, offsets, max_rows, n_groups, n, d,
-                           channel_groups, dx, dx_stride, dw, db, ws, ws_bytes, stream=None):
-    _check(_lib.fg_group_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(x), x_stride, dtype, ptr(mean), ptr(rstd), ptr(weight), ptr(bias), act,
-                                       ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(dx), dx_stride, ptr(dw), ptr(db),
+                           channel_groups, dx, dx_stride, dw, db, ws, ws_bytes, stream=None, stat_strides=None):
+    """stat_strides None: those of the tensors mean and rstd, of addresses (channel_groups, 1)."""
+    if stat_strides is None:
+        stat_strides = _statistics_strides(mean, rstd, n_groups, channel_groups)
+    _check(_lib.fg_group_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(x), x_stride, dtype, ptr(mean), ptr(rstd), *stat_strides, ptr(weight), ptr(bias),
+                                       act, ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(dx), dx_stride, ptr(dw), ptr(db),
                                        ptr(ws), ws_bytes, stream))
 
 

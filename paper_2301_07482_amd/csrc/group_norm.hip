@@ -41,6 +41,8 @@ struct GnArgs {
     int act, out_type;
     char* out;
     float *mean, *rstd;      // [n_groups x blocks]; the forward call's may be NULL
+    int64_t stat_stride;     // ... the gradients': group g, block j at g * stat_stride + j * stat_step
+    unsigned int stat_step;
     double* part;            // [chunks][2][blocks][4]: the sums of a chunk's parts of a group that began before it, and of one that begins in it, rows and level
     int32_t* info;           // [chunks][2]: those groups, -1: none
     float* joined;           // [chunks][blocks][2]: what the parts of the group that begins in the chunk come to
@@ -609,6 +611,12 @@ __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs 
 
 // ---- gradients ----
 
+// mean or rstd of a group and a block of the tile (the gradients'; the offset within a tile is one multiplication of 24 bits: with 64-bit addresses
+// fp32 gradients of many small groups took 8 to 11 % longer)
+__device__ __forceinline__ float given(const GnArgs& A, const Tile& T, const float* all, int g, int j) {
+    const char* tile = (const char*)(all + (int64_t)g * A.stat_stride + (int64_t)T.block0 * A.stat_step);
+    return *(const float*)(tile + __umul24((unsigned int)j, A.stat_step * 4));
+}
 // A thread's piece of the columns: what the gradients need of them
 struct GradColumns {
     float mean[8], rstd[8], w[8], b[8];
@@ -617,10 +625,11 @@ struct GradColumns {
 template <bool MANY, bool FOLDED>
 __device__ __forceinline__ void grad_columns(const GnArgs& A, const Tile& T, int g, int c, GradColumns& C) {
     affine(A, T, c, C.w, C.b);
+    if (MANY) asm volatile("" : "+v"(c));      // (what the columns' blocks come to is formed here: held over the groups it takes registers that are not there)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const int64_t at = (int64_t)g * A.blocks + T.block0 + (MANY ? block_of(A, c + e) : 0);
-        C.mean[e] = A.mean[at], C.rstd[e] = A.rstd[at];
+        const int j = MANY ? block_of(A, c + e) : 0;
+        C.mean[e] = given(A, T, A.mean, g, j), C.rstd[e] = given(A, T, A.rstd, g, j);
         if (FOLDED) C.w[e] *= C.rstd[e];
     }
 }
@@ -713,8 +722,6 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * x[e];
                 });
-#pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] *= A.rstd[(int64_t)g * A.blocks + T.block0 + block_of(A, P.c + e)];
             }
             leave_sums<TH, true>(A, T, S, s, q, rows);
         } else {
@@ -740,13 +747,15 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
         }
         __syncthreads();
         rows = rows_of(A, S);
-        if constexpr (MANY)
+        if constexpr (MANY)      // (rstd is still missing from the sums of t * xh)
 #pragma unroll
             for (int i = 0; i < MINE; ++i) {
                 const int c = (int)threadIdx.x + TH * i;
-                if (c < T.cols)
+                if (c >= T.cols) continue;
+                double s = 0.0, q = 0.0;
 #pragma unroll
-                    for (int w = 0; w < TH / 64; ++w) db[i] += S.wave[w][c], dw[i] += S.wave[w][GN_COLUMNS + c];
+                for (int w = 0; w < TH / 64; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
+                db[i] += s, dw[i] += q * (double)given(A, T, A.rstd, g, block_of(A, c));
             }
         block_sums<TH, MANY>(
             A, T, S,
@@ -757,6 +766,7 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
                 }
             },
             [&](int j, double a, double b) {
+                if (MANY) b *= (double)given(A, T, A.rstd, g, j);
                 if (PARTS) return write_part(A, T, chunk, which, j, a, b, rows, 0.f);
                 const double per = reciprocal(rows > 0 ? (double)rows * A.block : 1.0);
                 S.stats[j][0] = (float)(a * per), S.stats[j][1] = (float)(b * per);
@@ -999,10 +1009,10 @@ extern "C" size_t fg_group_norm_backward_workspace_bytes(int64_t max_rows, int32
 }
 
 extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* x, int64_t x_stride, fg_dtype_t dtype,
-                                              const float* mean, const float* rstd, const float* weight, const float* bias, fg_act_t act,
-                                              const int32_t* order_dev, const int64_t* offsets_dev, int64_t max_rows, int32_t n_groups, int64_t n, int32_t d,
-                                              int32_t channel_groups, void* dx, int64_t dx_stride, float* dw_dev, float* db_dev, void* ws_dev,
-                                              size_t ws_bytes, void* stream) {
+                                              const float* mean, const float* rstd, int64_t stat_stride, int64_t stat_step, const float* weight,
+                                              const float* bias, fg_act_t act, const int32_t* order_dev, const int64_t* offsets_dev,
+                                              int64_t max_rows, int32_t n_groups, int64_t n, int32_t d, int32_t channel_groups, void* dx, int64_t dx_stride,
+                                              float* dw_dev, float* db_dev, void* ws_dev, size_t ws_bytes, void* stream) {
     const char* who = "fg_group_norm_backward";
     const int e = fg_dtype_size(dtype), ge = fg_dtype_size(grad_dtype);
     if (!e) FG_FAIL(FG_ERR_DTYPE, "%s: unknown element type %d", who, (int)dtype);
@@ -1013,6 +1023,9 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     FG_TRY(check_array(who, "dy", dy, dy_stride, ge, d));
     FG_TRY(check_array(who, "x", x, x_stride, e, d));
     FG_TRY(check_array(who, "dx", dx, dx_stride, ge, d));
+    static_assert(GN_COLUMNS <= 1 << 24 && (int64_t)GN_COLUMNS * FG_MAX_NORM_GROUPS * 2 * 4 <= 1ll << 31 && FG_MAX_NORM_GROUPS * 2 * 4 < 1 << 24, "offsets within a tile");
+    if (stat_stride < 0 || stat_step < 0 || stat_stride > INT32_MAX || stat_step > 2 * FG_MAX_NORM_GROUPS)
+        FG_FAIL(FG_ERR_SHAPE, "%s: a stride of mean and rstd is negative or too large", who);
     if (dx == dy && dx && dx_stride != dy_stride) FG_FAIL(FG_ERR_INVALID_ARG, "%s: dx over dy has its stride", who);
     if (((uintptr_t)weight | (uintptr_t)bias | (uintptr_t)mean | (uintptr_t)rstd | (uintptr_t)dw_dev | (uintptr_t)db_dev) & 3)
         FG_FAIL(FG_ERR_INVALID_ARG, "%s: weight, bias, mean, rstd, dw or db is not aligned", who);
@@ -1023,6 +1036,7 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     GnArgs A = args_of(P, W, order_dev, offsets_dev, work ? max_rows : 0, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.dy = (const char*)dy, A.dy_stride = dy_stride, A.out = (char*)dx, A.out_stride = dx_stride, A.weight = weight, A.bias = bias;
     A.act = act, A.mean = const_cast<float*>(mean), A.rstd = const_cast<float*>(rstd);
+    A.stat_stride = stat_stride, A.stat_step = (unsigned int)stat_step;
     A.dw = dw_dev, A.db = db_dev;
     if (!dw_dev && !db_dev) A.columns = nullptr;
     A.join_there = 1, A.joins = work ? joins_of(P, A) : 0;      // (beside the sums of dw and db)
