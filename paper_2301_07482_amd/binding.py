@@ -235,6 +235,21 @@ def ptr(t):
     return t.data_ptr()
 
 
+def flat(t):
+    """`ptr` of what a call takes without a stride (lists, weights, sums, workspaces): a tensor whose elements do not lie behind each other is refused."""
+    if t is None or isinstance(t, int) or t.is_contiguous():
+        return ptr(t)
+    raise FgError(FG_ERR_INVALID_ARG, f"a tensor of the shape {tuple(t.shape)} and the strides {t.stride()}, for which the call has no stride, must be "
+                                      "contiguous")
+
+
+def rows_of(t):
+    """`ptr` of rows, for which a call has the stride from one to the next: a tensor whose rows' elements do not lie behind each other is refused."""
+    if t is None or isinstance(t, int) or t.dim() < 2 or t.shape[-1] == 1 or t.stride(-1) == 1:
+        return ptr(t)
+    raise FgError(FG_ERR_INVALID_ARG, f"rows whose elements are {t.stride(-1)} apart: they must lie behind each other")
+
+
 def fg_version():
     return _lib.fg_version()
 
@@ -525,14 +540,14 @@ def fg_group_rows_workspace_bytes(max_rows, n_groups):
 
 
 def fg_group_rows(groups, n_table, ids, n_positions, rows, n_rows, max_rows, n_groups, order, offsets, ws, ws_bytes, stream=None):
-    _check(_lib.fg_group_rows(ptr(groups), n_table, ptr(ids), n_positions, ptr(rows), ptr(n_rows), max_rows, n_groups, ptr(order), ptr(offsets),
-                              ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_group_rows(flat(groups), n_table, flat(ids), n_positions, flat(rows), flat(n_rows), max_rows, n_groups, flat(order), flat(offsets),
+                              flat(ws), ws_bytes, stream))
 
 
 def fg_linear_grouped(x, x_rows, x_stride, dtype, x_scale, src_ids, order, offsets, max_rows, n_groups, d_in, d_out, W, w_scale, bias, relu, h_out,
                       n_out, out_stride, out_dtype, stream=None):
-    _check(_lib.fg_linear_grouped(ptr(x), x_rows, x_stride, dtype, ptr(x_scale), ptr(src_ids), ptr(order), ptr(offsets), max_rows, n_groups, d_in,
-                                  d_out, ptr(W), ptr(w_scale), ptr(bias), relu, ptr(h_out), n_out, out_stride, out_dtype, stream))
+    _check(_lib.fg_linear_grouped(rows_of(x), x_rows, x_stride, dtype, flat(x_scale), flat(src_ids), flat(order), flat(offsets), max_rows, n_groups, d_in,
+                                  d_out, flat(W), flat(w_scale), flat(bias), relu, rows_of(h_out), n_out, out_stride, out_dtype, stream))
 
 
 def fg_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out):
@@ -544,19 +559,19 @@ def fg_linear_grouped_backward(x, x_rows, x_stride, dtype, src_ids, dh, dh_strid
     """h_dtype None: the type of the tensor h, of an address that of the rows."""
     if h_dtype is None:
         h_dtype = _TENSOR_DTYPE.get(str(getattr(h, "dtype", "")), dtype)
-    _check(_lib.fg_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(h), h_stride,
-                                           h_dtype, n, ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), ptr(dx), dx_stride, dx_dtype, ptr(dw),
-                                           ptr(db), ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_linear_grouped_backward(rows_of(x), x_rows, x_stride, dtype, flat(src_ids), rows_of(dh), dh_stride, dh_dtype, rows_of(h), h_stride,
+                                           h_dtype, n, flat(order), flat(offsets), max_rows, n_groups, d_in, d_out, flat(W), rows_of(dx), dx_stride,
+                                           dx_dtype, flat(dw), flat(db), flat(ws), ws_bytes, stream))
 
 
 def fg_dropout(x, x_stride, dtype, rows, n_rows, max_rows, n, d, p, key, out, out_stride, stream=None):
-    _check(_lib.fg_dropout(ptr(x), x_stride, dtype, ptr(rows), ptr(n_rows), max_rows, n, d, p, key, ptr(out), out_stride, stream))
+    _check(_lib.fg_dropout(rows_of(x), x_stride, dtype, flat(rows), flat(n_rows), max_rows, n, d, p, key, rows_of(out), out_stride, stream))
 
 
 def fg_residual_norm(x, x_stride, dtype, residual, residual_stride, sum_dtype, rows, n_rows, max_rows, n, d, p, key, weight, eps, sum_out, sum_stride,
                      y, y_stride, y_dtype, y_scale, rstd_out, stream=None):
-    _check(_lib.fg_residual_norm(ptr(x), x_stride, dtype, ptr(residual), residual_stride, sum_dtype, ptr(rows), ptr(n_rows), max_rows, n, d, p, key,
-                                 ptr(weight), eps, ptr(sum_out), sum_stride, ptr(y), y_stride, y_dtype, ptr(y_scale), ptr(rstd_out), stream))
+    _check(_lib.fg_residual_norm(rows_of(x), x_stride, dtype, rows_of(residual), residual_stride, sum_dtype, flat(rows), flat(n_rows), max_rows, n, d, p, key,
+                                 flat(weight), eps, rows_of(sum_out), sum_stride, rows_of(y), y_stride, y_dtype, flat(y_scale), flat(rstd_out), stream))
 
 
 def fg_residual_norm_backward_workspace_bytes(max_rows, d):
@@ -565,19 +580,19 @@ def fg_residual_norm_backward_workspace_bytes(max_rows, d):
 
 def fg_residual_norm_backward(dy, dy_stride, grad_dtype, sum_, sum_stride, sum_dtype, rstd, weight, dsum_in, dsum_in_stride, rows, n_rows, max_rows, n,
                               d, p, key, dsum_out, dsum_stride, dx, dx_stride, dw, ws, ws_bytes, stream=None):
-    _check(_lib.fg_residual_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(sum_), sum_stride, sum_dtype, ptr(rstd), ptr(weight), ptr(dsum_in),
-                                          dsum_in_stride, ptr(rows), ptr(n_rows), max_rows, n, d, p, key, ptr(dsum_out), dsum_stride, ptr(dx),
-                                          dx_stride, ptr(dw), ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_residual_norm_backward(rows_of(dy), dy_stride, grad_dtype, rows_of(sum_), sum_stride, sum_dtype, flat(rstd), flat(weight), rows_of(dsum_in),
+                                          dsum_in_stride, flat(rows), flat(n_rows), max_rows, n, d, p, key, rows_of(dsum_out), dsum_stride, rows_of(dx),
+                                          dx_stride, flat(dw), flat(ws), ws_bytes, stream))
 
 
 def fg_quantize_rows(x, x_stride, dtype, n_rows, d, q, q_stride, scale, stream=None):
-    _check(_lib.fg_quantize_rows(ptr(x), x_stride, dtype, n_rows, d, ptr(q), q_stride, ptr(scale), stream))
+    _check(_lib.fg_quantize_rows(rows_of(x), x_stride, dtype, n_rows, d, rows_of(q), q_stride, flat(scale), stream))
 
 
 def fg_gated_linear_grouped(x, x_rows, x_stride, dtype, src_ids, order, offsets, max_rows, n_groups, d_in, d_out, W, bias, act, h_out, n_out, out_stride,
                             out_dtype, z_out, z_stride, stream=None):
-    _check(_lib.fg_gated_linear_grouped(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W),
-                                        ptr(bias), act, ptr(h_out), n_out, out_stride, out_dtype, ptr(z_out), z_stride, stream))
+    _check(_lib.fg_gated_linear_grouped(rows_of(x), x_rows, x_stride, dtype, flat(src_ids), flat(order), flat(offsets), max_rows, n_groups, d_in, d_out, flat(W),
+                                        flat(bias), act, rows_of(h_out), n_out, out_stride, out_dtype, rows_of(z_out), z_stride, stream))
 
 
 def fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, d_in, d_out):
@@ -586,9 +601,9 @@ def fg_gated_linear_grouped_backward_workspace_bytes(dtype, max_rows, n_groups, 
 
 def fg_gated_linear_grouped_backward(x, x_rows, x_stride, dtype, src_ids, dh, dh_stride, dh_dtype, z, z_stride, n, order, offsets, max_rows, n_groups, d_in,
                                      d_out, W, act, dx, dx_stride, dx_dtype, dw, dw_dtype, db, ws, ws_bytes, stream=None):
-    _check(_lib.fg_gated_linear_grouped_backward(ptr(x), x_rows, x_stride, dtype, ptr(src_ids), ptr(dh), dh_stride, dh_dtype, ptr(z), z_stride, n,
-                                                 ptr(order), ptr(offsets), max_rows, n_groups, d_in, d_out, ptr(W), act, ptr(dx), dx_stride, dx_dtype,
-                                                 ptr(dw), dw_dtype, ptr(db), ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_gated_linear_grouped_backward(rows_of(x), x_rows, x_stride, dtype, flat(src_ids), rows_of(dh), dh_stride, dh_dtype, rows_of(z), z_stride, n,
+                                                 flat(order), flat(offsets), max_rows, n_groups, d_in, d_out, flat(W), act, rows_of(dx), dx_stride, dx_dtype,
+                                                 flat(dw), dw_dtype, flat(db), flat(ws), ws_bytes, stream))
 
 
 def fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups):
@@ -597,8 +612,8 @@ def fg_group_norm_workspace_bytes(max_rows, n_groups, d, channel_groups):
 
 def fg_group_norm(x, x_stride, dtype, order, offsets, max_rows, n_groups, n, d, channel_groups, weight, bias, eps, act, y, y_stride, y_dtype, mean_out,
                   rstd_out, ws, ws_bytes, stream=None):
-    _check(_lib.fg_group_norm(ptr(x), x_stride, dtype, ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(weight), ptr(bias), eps,
-                              act, ptr(y), y_stride, y_dtype, ptr(mean_out), ptr(rstd_out), ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_group_norm(rows_of(x), x_stride, dtype, flat(order), flat(offsets), max_rows, n_groups, n, d, channel_groups, flat(weight), flat(bias), eps,
+                              act, rows_of(y), y_stride, y_dtype, flat(mean_out), flat(rstd_out), flat(ws), ws_bytes, stream))
 
 
 def fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups):
@@ -611,7 +626,8 @@ def _statistics_strides(mean, rstd, n_groups, channel_groups):
         if t is None or isinstance(t, int) or t.is_contiguous():
             return channel_groups, 1
         if tuple(t.shape) != (n_groups, channel_groups):
-            raise FgError(FG_ERR_SHAPE, f"fg_group_norm_backward: mean and rstd of the shape {tuple(t.shape)} neither lie behind each other nor are [n_groups, channel_groups]")
+            raise FgError(FG_ERR_SHAPE, f"fg_group_norm_backward: mean and rstd of the shape {tuple(t.shape)} neither lie behind each other nor are "
+                                        "[n_groups, channel_groups]")
         return t.stride(0) if n_groups > 1 else channel_groups, t.stride(1) if channel_groups > 1 else 1
 
     strides = of(mean)
@@ -625,15 +641,15 @@ def fg_group_norm_backward(dy, dy_stride, grad_dtype, x, x_stride, dtype, mean, 
     """stat_strides None: those of the tensors mean and rstd, of addresses (channel_groups, 1)."""
     if stat_strides is None:
         stat_strides = _statistics_strides(mean, rstd, n_groups, channel_groups)
-    _check(_lib.fg_group_norm_backward(ptr(dy), dy_stride, grad_dtype, ptr(x), x_stride, dtype, ptr(mean), ptr(rstd), *stat_strides, ptr(weight), ptr(bias),
-                                       act, ptr(order), ptr(offsets), max_rows, n_groups, n, d, channel_groups, ptr(dx), dx_stride, ptr(dw), ptr(db),
-                                       ptr(ws), ws_bytes, stream))
+    _check(_lib.fg_group_norm_backward(rows_of(dy), dy_stride, grad_dtype, rows_of(x), x_stride, dtype, ptr(mean), ptr(rstd), *stat_strides,
+                                       flat(weight), flat(bias), act, flat(order), flat(offsets), max_rows, n_groups, n, d, channel_groups, rows_of(dx), dx_stride, flat(dw), flat(db),
+                                       flat(ws), ws_bytes, stream))
 
 
 def fg_distill_loss(h, h_stride, dtype, rows, n_rows, max_rows, n, d, ids, top_idx, top_val, top_dtype, table_rows, k, labels, temperature, alpha, weight,
                     grad_scale, loss_out, dh, dh_stride, dh_dtype, stream=None):
-    _check(_lib.fg_distill_loss(ptr(h), h_stride, dtype, ptr(rows), ptr(n_rows), max_rows, n, d, ptr(ids), ptr(top_idx), ptr(top_val), top_dtype,
-                                table_rows, k, ptr(labels), temperature, alpha, ptr(weight), grad_scale, ptr(loss_out), ptr(dh), dh_stride, dh_dtype,
+    _check(_lib.fg_distill_loss(rows_of(h), h_stride, dtype, flat(rows), flat(n_rows), max_rows, n, d, flat(ids), flat(top_idx), flat(top_val), top_dtype,
+                                table_rows, k, flat(labels), temperature, alpha, flat(weight), grad_scale, flat(loss_out), rows_of(dh), dh_stride, dh_dtype,
                                 stream))
 
 

@@ -73,3 +73,43 @@ def test_statistics_whose_layout_no_stride_can_say(B):
     assert bw(t[:3], t[:3]) == B.FG_ERR_SHAPE and bw(torch.ones(64)[::2], torch.ones(64)[::2]) == B.FG_ERR_SHAPE
     for bad in ((-1, 1), (8, -1), (1 << 31, 1), (8, 2 * B.FG_MAX_NORM_GROUPS + 1)):
         assert bw(P, P, stat_strides=bad) == B.FG_ERR_SHAPE, bad
+
+
+P = 4096
+CALLS = {  # every array that a call takes without a stride, and (after "/") every one of rows that lie a stride apart
+    "fg_group_rows": "groups ids rows n_rows order offsets ws /",
+    "fg_linear_grouped": "x_scale src_ids order offsets W w_scale bias / x h_out",
+    "fg_linear_grouped_backward": "src_ids order offsets W dw db ws / x dh h dx",
+    "fg_dropout": "rows n_rows / x out",
+    "fg_residual_norm": "rows n_rows weight y_scale rstd_out / x residual sum_out y",
+    "fg_residual_norm_backward": "rstd weight rows n_rows dw ws / dy sum_ dsum_in dsum_out dx",
+    "fg_quantize_rows": "scale / x q",
+    "fg_gated_linear_grouped": "src_ids order offsets W bias / x h_out z_out",
+    "fg_gated_linear_grouped_backward": "src_ids order offsets W dw db ws / x dh z dx",
+    "fg_group_norm": "order offsets weight bias mean_out rstd_out ws / x y",
+    "fg_group_norm_backward": "weight bias order offsets dw db ws / dy x dx",
+    "fg_distill_loss": "rows n_rows ids top_idx top_val labels weight loss_out / h dh",
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_layouts_that_a_call_has_no_stride_for(B, name):
+    """Refused by the binding, an array at a time; the same arrays behind each other go on to the library, which refuses what is asked for here (nothing is launched)."""
+    import inspect
+    flat, rows = (part.split() for part in CALLS[name].split("/"))
+    fn = getattr(B, name)
+    call = {p: 0 for p in inspect.signature(fn).parameters if p not in ("stream", "stat_strides")}
+    assert set(flat + rows) | ({"mean", "rstd"} if name == "fg_group_norm_backward" else set()) <= set(call)
+    call.update({a: P for a in flat + rows}, max_rows=-1, n_rows=-1 if name == "fg_quantize_rows" else P)
+    call = {p: v for p, v in call.items() if p in inspect.signature(fn).parameters}
+    apart = [torch.ones(6, 8).T, torch.ones(4, 3, 8)[:, 1, ::2]]                                                    # a row's elements are
+    strided = [torch.ones(4, 6)[:, :4], torch.ones(3, 2)[:, :1]]                                                     # the rows are
+    for array in flat + rows:
+        for t in apart + ([*strided, torch.ones(20)[::2], torch.ones(1).expand(9)] if array in flat else []):
+            with pytest.raises(B.FgError, match="contiguous|behind each other") as e:
+                fn(**{**call, array: t})
+            assert e.value.code == B.FG_ERR_INVALID_ARG, array
+        for t in [torch.ones(4, 8), torch.ones(5), torch.ones(1, 8)] + (strided if array in rows else []):
+            with pytest.raises(B.FgError) as e:
+                fn(**{**call, array: t})
+            assert "contiguous" not in str(e.value) and "behind each other" not in str(e.value), array
