@@ -237,17 +237,31 @@ def ptr(t):
 
 def flat(t):
     """`ptr` of what a call takes without a stride (lists, weights, sums, workspaces): a tensor whose elements do not lie behind each other is refused."""
-    if t is None or isinstance(t, int) or t.is_contiguous():
-        return ptr(t)
-    raise FgError(FG_ERR_INVALID_ARG, f"a tensor of the shape {tuple(t.shape)} and the strides {t.stride()}, for which the call has no stride, must be "
-                                      "contiguous")
+    if t is None:
+        return None
+    try:      # (an address is the rarer case)
+        return t.data_ptr() if t.is_contiguous() else _apart(t, False)
+    except AttributeError:
+        return t
 
 
 def rows_of(t):
     """`ptr` of rows, for which a call has the stride from one to the next: a tensor whose rows' elements do not lie behind each other is refused."""
-    if t is None or isinstance(t, int) or t.dim() < 2 or t.shape[-1] == 1 or t.stride(-1) == 1:
-        return ptr(t)
-    raise FgError(FG_ERR_INVALID_ARG, f"rows whose elements are {t.stride(-1)} apart: they must lie behind each other")
+    if t is None:
+        return None
+    try:
+        return t.data_ptr() if t.is_contiguous() else _apart(t, True)
+    except AttributeError:
+        return t
+
+
+def _apart(t, rows):
+    if not rows:
+        raise FgError(FG_ERR_INVALID_ARG, f"a tensor of the shape {tuple(t.shape)} and the strides {t.stride()}, for which the call has no stride, must be "
+                                          "contiguous")
+    if t.dim() >= 2 and t.shape[-1] != 1 and t.stride(-1) != 1:
+        raise FgError(FG_ERR_INVALID_ARG, f"rows whose elements are {t.stride(-1)} apart: they must lie behind each other")
+    return t.data_ptr()
 
 
 def fg_version():
