@@ -136,6 +136,17 @@ __device__ __forceinline__ int position(const GnArgs& A, unsigned int k) {
     return r < 0 || r >= A.n ? -1 : r;
 }
 
+// The row of the first of the entries [k0, k1) that exists, -1: none does (lanes of a wavefront together; nearly always that of k0)
+__device__ __forceinline__ int first_row(const GnArgs& A, unsigned int k0, unsigned int k1) {
+    int r = uniform(position(A, k0));
+    for (unsigned int k = k0 + 1; r < 0 && k < k1; k += 64) {
+        const int mine = k + fg_lane() < k1 ? position(A, k + fg_lane()) : -1;
+        const unsigned long long there = __ballot(mine >= 0);
+        if (there) r = __builtin_amdgcn_readlane(mine, __ffsll((long long)there) - 1);
+    }
+    return r;
+}
+
 // this workgroup's tile and this thread's share of it
 struct Tile {
     int c0, cols, block0, n_blocks, p, side, sides;      // columns, blocks; piece and row of the thread, rows side by side
@@ -444,8 +455,8 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
         const bool held = !PARTS && k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);      // (all of a group's rows at once: they are read once)
 #pragma unroll
         for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
-        // a column's values are measured from its first one (MANY), all columns' from the block's
-        const int first = position(A, which == GN_GOES_ON ? offset_of(A, g) : k0);
+        // a column's values are measured from its first one in these entries (MANY), all columns' from the block's
+        const int first = first_row(A, k0, k1);
         const float common = !MANY && first >= 0 ? element(A.x + (int64_t)first * A.x_stride, T_, T.c0) : 0.f;
         for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
             const Piece P = piece_of(A, T, i);
@@ -511,16 +522,30 @@ __global__ __launch_bounds__(TH, gn_per_unit(T_, MANY, false)) void group_norm_k
         norm_body<TH, T_, MANY, true>(A, S);
 }
 
-// the sums of all parts of the split group that begins in a chunk, in order: lanes of a wavefront together
+// The sums of all parts of the split group that begins in a chunk, in order, measured from the level of the first part that has rows: lanes of a wavefront together.
+// (LEVELS: a part's sums are measured from a level of its own)
+template <bool LEVELS>
 __device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin, int block, double& s, double& q, double& rows, double& level) {
     const unsigned int last = (offset_of(A, g + 1) - 1) / A.rows;
     s = q = rows = level = 0.0;
-    for (unsigned int c = begin + fg_lane(); c <= last; c += 64) {
-        const double* p = A.part + ((int64_t)(c * 2 + (c == begin)) * A.blocks + block) * 4;
-        s += p[0], q += p[1], rows += p[2];
-        if (c == begin) level = p[3];
+    bool known = false;
+    for (unsigned int c0 = begin; c0 <= last; c0 += 64) {
+        const unsigned int c = c0 + fg_lane();
+        double part[4] = {0.0, 0.0, 0.0, 0.0};
+        if (c <= last) {
+            const double* p = A.part + ((int64_t)(c * 2 + (c == begin)) * A.blocks + block) * 4;
+#pragma unroll
+            for (int i = 0; i < (LEVELS ? 4 : 3); ++i) part[i] = p[i];
+        }
+        if constexpr (LEVELS) {
+            const unsigned long long there = __ballot(part[2] > 0.0);
+            if (!known && there) level = __shfl(part[3], __ffsll((long long)there) - 1, 64), known = true;
+            const double up = part[2] > 0.0 ? part[3] - level : 0.0, values = part[2] * A.block;
+            part[1] += up * (2.0 * part[0] + values * up);
+            part[0] += values * up;
+        }
+        s += part[0], q += part[1], rows += part[2];
     }
-    level = __shfl(level, 0, 64);
     for (int off = 32; off > 0; off >>= 1) {
         s += __shfl_xor(s, off, 64);
         q += __shfl_xor(q, off, 64);
@@ -531,7 +556,7 @@ __device__ __forceinline__ void join(const GnArgs& A, int g, unsigned int begin,
 template <int T_, bool BACKWARD>
 __device__ __forceinline__ void joined(const GnArgs& A, int g, unsigned int begin, int block, bool write, float& a, float& b) {
     double s, q, rows, level;
-    join(A, g, begin, block, s, q, rows, level);
+    join<!BACKWARD>(A, g, begin, block, s, q, rows, level);
     if constexpr (BACKWARD) {
         const double per = reciprocal(rows > 0.0 ? rows * A.block : 1.0);
         a = (float)(s * per), b = (float)(q * per);

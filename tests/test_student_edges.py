@@ -113,3 +113,54 @@ def test_layouts_that_a_call_has_no_stride_for(B, name):
             with pytest.raises(B.FgError) as e:
                 fn(**{**call, array: t})
             assert "contiguous" not in str(e.value) and "behind each other" not in str(e.value), array
+
+
+# ---- levels ----
+
+@gpu
+@pytest.mark.parametrize("dtype, n, d, blocks", [("f32", 60, 24, 3), ("f32", 60, 600, 2), ("f32", 1000, 16, 16), ("f32", 40_000, 256, 8), ("f32", 40_000, 512, 1), ("f32", 90_000, 24, 24),
+                                                 ("bf16", 50_000, 1024, 32), ("f16", 30_000, 2048, 256)])
+def test_levels_behind_entries_that_do_not_exist(B, dtype, n, d, blocks):
+    """A group's first entries do not exist, and whole runs of entries further on: in groups of one workgroup and in split ones. The level of what is there still takes
+    nothing from the variance: of equal values it is 0, of values about 300 or 10^7 as exact as for a level of 0."""
+    r = np.random.default_rng(n + d)
+    order = r.permutation(n).astype(np.int32)
+    offsets = np.array([0, n // 3, n // 3, n], np.int64)
+    for at in (0, n // 3):
+        order[at:at + 1 + n // 50] = -1
+    order[n // 2:n // 2 + n // 4] = n
+    order[n - 3:] = 2 ** 31 - 1
+    equal = 1e7 + 1 if dtype == "f32" else 300.0
+    o, f = torch.from_numpy(order).cuda(), torch.from_numpy(offsets).cuda()
+    ws = torch.full((B.fg_group_norm_workspace_bytes(n, 3, d, blocks),), 255, dtype=torch.uint8, device="cuda")
+    for level, spread in ((equal, 0.0), (300.0, 1.5), (equal, 5.0)):
+        x = values(r, n, d, dtype, 0, spread, level)
+        y, mean, rstd = sentinel(n, d, "f32").cuda(), full(3, blocks), full(3, blocks)
+        B.fg_group_norm(x.cuda(), d * T[dtype].itemsize, code(B, dtype), o, f, n, 3, n, d, blocks, None, None, 0.25, B.FG_ACT_NONE, y, d * 4, B.FG_F32, mean, rstd, ws, len(ws))
+        torch.cuda.synchronize()
+        taken = torch.zeros(n, dtype=torch.bool)
+        for g, pos, _ in R.members(order, offsets.tolist(), n):
+            taken[pos] = True
+            m, s = R.norm_statistics(x[pos], blocks, 0.25)
+            # fp64 sums of at most 2^26 distances of up to 2^6 (or equal values): 2^-53 * 2^6 * 2^26 of the mean at most
+            close(mean.cpu()[g], m, 2.0 ** -24 * m.abs() + 2.0 ** -21, f"mean of group {g} about {level}")
+            close(rstd.cpu()[g], s, 2.0 ** -23 * s, f"rstd of group {g} about {level}")
+            if len(pos):
+                want, tol, _, _ = R.norm_rows(x[pos], m, s, None, None, "none")
+                close(y.cpu()[pos], want, tol + 2.0 ** -24 * want.abs(), "y")
+        assert bool((y.cpu()[~taken] == -77).all())
+        if spread == 0:
+            assert not bool(y.cpu()[taken].any()) and bool((rstd == 2).all())
+
+
+@gpu
+@pytest.mark.parametrize("n, d", [(100, 16), (50_000, 64)])
+def test_a_group_none_of_whose_entries_exists(B, n, d):
+    order = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, n // 2, n], device="cuda")
+    order[n // 2:] = torch.arange(n // 2, n, device="cuda")
+    x, y, mean, rstd = torch.randn(n, d, device="cuda") + 5, full(n, d), full(2, 4), full(2, 4)
+    ws = torch.zeros(B.fg_group_norm_workspace_bytes(n, 2, d, 4), dtype=torch.uint8, device="cuda")
+    B.fg_group_norm(x, d * 4, B.FG_F32, order, off, n, 2, n, d, 4, None, None, 0.25, B.FG_ACT_NONE, y, d * 4, B.FG_F32, mean, rstd, ws, len(ws))
+    torch.cuda.synchronize()
+    assert bool((mean[0] == 0).all()) and bool((rstd[0] == 2).all()) and bool((y[:n // 2] == -77).all()) and bool((mean[1] > 4).all()) and not bool((y[n // 2:] == -77).any())
