@@ -1009,7 +1009,8 @@ fg_status_t fg_group_norm(const void* x, int64_t x_stride, fg_dtype_t dtype, con
  *                                       g * stat_stride + j * stat_step floats (channel_groups and 1 as the forward call leaves them); not negative, stat_step up to 2 * FG_MAX_NORM_GROUPS
  *   x, ...                              as in the forward call
  *   ws_dev, ws_bytes                    >= fg_group_norm_backward_workspace_bytes(max_rows, n_groups, d, channel_groups), 16-byte aligned
- * Means in fp64; dw and db in fp32 within and fp64 across ranges of rows; results do not depend on scheduling.
+ * Sums in fp32 over up to 128 rows of a thread and the lanes of its wavefront, in fp64 beyond those; the two means of blocks of more than 128 columns in fp64
+ * throughout, dw and db of blocks of more than 2048 in fp32 within a range of rows and fp64 across ranges. Results do not depend on scheduling.
  */
 size_t fg_group_norm_backward_workspace_bytes(int64_t max_rows, int32_t n_groups, int32_t d, int32_t channel_groups);
 fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t grad_dtype, const void* x, int64_t x_stride, fg_dtype_t dtype,

@@ -20,6 +20,8 @@ constexpr int GN_JOIN_HERE = 4000, GN_MAX_PIECES = 8;
 // Rows of a thread whose reads are on their way together. Two | one: forward 17.2 | 18.3 us for 31744 x 100 in 1024 groups, 24.6 | 26.5 for 100000 x 40 in 10000 groups,
 // 27.6 | 25.6 for 65536 x 128 in 4096 groups; gradients, which have two arrays to read, 39.7 | 37.0 and 71 | 62 for the first two
 constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;
+// Rows of a thread whose fp32 sums (the gradients', several blocks to a tile) are joined to fp64 ones: what is lost of them stays below 2^-17 however long a call is
+constexpr int GN_RUN = 128;
 
 // Workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them. Three | four, fp32: 31744 x 100 in 1024
 // groups 17.2 | 22.5 us, its gradients 36.6 | 48.6, those of 777 x 88 in 9 groups 11.8 | 13.5, of 65536 x 1024 in 4 groups 281 | 295, of 100000 x 40 in 10000 groups 62 | 104;
@@ -198,11 +200,12 @@ __device__ __forceinline__ void store_piece(char* row, const Piece& P, const flo
         }
 }
 
-template <int TH>
+template <int TH, bool MANY>
 struct Scratch {
-    double wave[TH / 64][2 * GN_COLUMNS];      // sums of a wavefront's rows, by column
-    float from[GN_COLUMNS];                     // what they are measured from
-    float stats[GN_COLUMNS][2];                 // of a block: mean and rstd, or the gradient's two means
+    static constexpr int COLUMNS = MANY ? GN_COLUMNS : 1;
+    double wave[TH / 64][2 * COLUMNS];      // sums of a wavefront's rows, by column; one block to a tile: of all columns
+    float from[COLUMNS];                    // what they are measured from
+    float stats[COLUMNS][2];                // of a block: mean and rstd, or the gradient's two means
     int rows[TH / 64];
 };
 // Lanes l and l + HALF (of 64 for HALF = 32, of every 32 for 16) add up a and b between them: the first has a's sum, the other b's
@@ -227,18 +230,19 @@ __device__ __forceinline__ double half_sums(double a, double b) {
 }
 // The sums s[e], q[e] of a thread's columns (MANY) or s[0], q[0] of all it has seen, over the rows that a wavefront has side by side, and the number of rows;
 // they are there after the workgroup's next barrier. Halves of the wavefront exchange half of their sums each: 16 fp64 sums over four rows take 24 exchanges between
-// registers instead of 64 through LDS.
+// registers instead of 64 through LDS. `more` (MANY): they are added to what is there.
 template <int TH, bool MANY, typename V>
-__device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch<TH>& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows) {
+__device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scratch<TH, MANY>& S, V (&s)[MANY ? 8 : 1], V (&q)[MANY ? 8 : 1], int rows, bool more = false) {
     for (int off = A.width; off < 64; off <<= 1) rows += __shfl_xor(rows, off, 64);
     if (fg_lane() == 0) S.rows[fg_wave()] = rows;
     if constexpr (MANY) {
         const Piece P = piece_of(A, T, 0);
         double* const to = S.wave[fg_wave()] + P.c;
+        const auto put = [&](int at, V v) { to[at] = more ? to[at] + (double)v : (double)v; };
         if (A.width >= 64) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e >= P.twice) to[e] = (double)s[e], to[GN_COLUMNS + e] = (double)q[e];
+                if (e >= P.twice) put(e, s[e]), put(GN_COLUMNS + e, q[e]);
             return;
         }
         V v[8];      // of s in the first half of the wavefront, of q in the second
@@ -248,7 +252,7 @@ __device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scrat
         if (A.width == 32) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (e >= P.twice) to[base + e] = (double)v[e];
+                if (e >= P.twice) put(base + e, v[e]);
             return;
         }
         const int e0 = fg_lane() & 16 ? 4 : 0;      // four columns of the piece
@@ -260,15 +264,15 @@ __device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scrat
         if ((fg_lane() & 15) < A.width)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (e0 + e >= P.twice) to[base + e0 + e] = (double)v[e];
+                if (e0 + e >= P.twice) put(base + e0 + e, v[e]);
     } else {
         V v = half_sums<32>(s[0], q[0]);
         for (int off = 1; off < 32; off <<= 1) v += __shfl_xor(v, off, 64);
-        if ((fg_lane() & 31) == 0) S.wave[fg_wave()][fg_lane() ? GN_COLUMNS : 0] = (double)v;
+        if ((fg_lane() & 31) == 0) S.wave[fg_wave()][fg_lane() ? 1 : 0] = (double)v;
     }
 }
-template <int TH>
-__device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch<TH>& S) {
+template <int TH, bool MANY>
+__device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch<TH, MANY>& S) {
     int all = 0;
 #pragma unroll
     for (int w = 0; w < TH / 64; ++w) all += S.rows[w];
@@ -276,11 +280,11 @@ __device__ __forceinline__ int rows_of(const GnArgs& A, const Scratch<TH>& S) {
 }
 // done(block of the tile, s, q) by one thread of every block, of the sums over its columns; column(c, s, q) makes of a column's what is to be added
 template <int TH, bool MANY, typename Column, typename Done>
-__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const Scratch<TH>& S, const Column& column, const Done& done) {
+__device__ __forceinline__ void block_sums(const GnArgs& A, const Tile& T, const Scratch<TH, MANY>& S, const Column& column, const Done& done) {
     const auto both = [&](int c, double& a, double& b) {
         double s = 0.0, q = 0.0;
 #pragma unroll
-        for (int w = 0; w < TH / 64; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
+        for (int w = 0; w < TH / 64; ++w) s += S.wave[w][c], q += S.wave[w][S.COLUMNS + c];
         column(c, s, q);
         a += s, b += q;
     };
@@ -320,7 +324,7 @@ __device__ __forceinline__ float element(const char* p, int type, int64_t i) {
 __device__ __forceinline__ int block_of(const GnArgs& A, int c) { return A.block == 1 ? c : (int)__umulhi((unsigned int)c, A.block_inverse); }
 // the two values of S.stats for each of a piece's columns
 template <int TH, bool MANY>
-__device__ __forceinline__ void stats_of(const GnArgs& A, const Scratch<TH>& S, int c, float (&first)[8], float (&second)[8]) {
+__device__ __forceinline__ void stats_of(const GnArgs& A, const Scratch<TH, MANY>& S, int c, float (&first)[8], float (&second)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const int j = MANY ? block_of(A, c + e) : 0;
@@ -398,7 +402,7 @@ __device__ __forceinline__ void for_rows(const GnArgs& A, const Tile& T, unsigne
 
 // y of the entries [k0, k1) with the blocks' mean and rstd in S.stats. held: the sets `now`, v are all of them and there already
 template <int TH, int T_, bool MANY>
-__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch<TH>& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
+__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch<TH, MANY>& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
                                           fg_piece<T_> (&v)[GN_AHEAD]) {
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
@@ -438,7 +442,7 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
 // PARTS: the workgroup's work is a chunk's parts of split groups, else whole groups (one kernel for both, so that neither waits for the other; two bodies, so
 // that the first is not short of registers for what the second holds)
 template <int TH, int T_, bool MANY, bool PARTS>
-__device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
+__device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S) {
     constexpr int N = MANY ? 8 : 1;
     const Tile T = tile_of<TH>(A);
     const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
@@ -515,7 +519,7 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH>& S) {
 }
 template <int TH, int T_, bool MANY>
 __global__ __launch_bounds__(TH, gn_per_unit(T_, MANY, false)) void group_norm_kernel(GnArgs A) {
-    __shared__ Scratch<TH> S;
+    __shared__ Scratch<TH, MANY> S;
     if ((int)blockIdx.y < A.workers)
         norm_body<TH, T_, MANY, false>(A, S);
     else
@@ -599,8 +603,8 @@ __global__ __launch_bounds__(GN_THREADS) void group_norm_join_kernel(GnArgs A) {
 }
 
 // a chunk's parts of split groups: f(group, first entry, end) with what their parts come to in S.stats
-template <int T_, bool BACKWARD, typename F>
-__device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scratch<GN_THREADS>& S, const F& f) {
+template <int T_, bool MANY, bool BACKWARD, typename F>
+__device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scratch<GN_THREADS, MANY>& S, const F& f) {
     const unsigned int chunk = A.chunks - 1 - blockIdx.y, c0 = chunk * A.rows, c1 = c0 + A.rows;      // the last chunks' rows are the likeliest to be cached
     for (int which = 0; which < 2; ++which) {
         const int g = A.info[chunk * 2 + which];
@@ -625,9 +629,9 @@ __device__ __forceinline__ void split_parts(const GnArgs& A, const Tile& T, Scra
 }
 template <int T_, bool MANY>
 __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs A) {
-    __shared__ Scratch<GN_THREADS> S;
+    __shared__ Scratch<GN_THREADS, MANY> S;
     const Tile T = tile_of<GN_THREADS>(A);
-    split_parts<T_, false>(A, T, S, [&](int, unsigned int k0, unsigned int k1) {
+    split_parts<T_, MANY, false>(A, T, S, [&](int, unsigned int k0, unsigned int k1) {
         int now[GN_AHEAD];
         fg_piece<T_> v[GN_AHEAD];
         normalise<GN_THREADS, T_, MANY>(A, T, S, k0, k1, false, now, v);
@@ -701,7 +705,7 @@ __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, in
 }
 // dx of the entries [k0, k1) with the blocks' two means in S.stats
 template <int TH, int X, int G, bool MANY>
-__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch<TH>& S, int g, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R) {
+__device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, const Scratch<TH, MANY>& S, int g, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R) {
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
         if (!P.there) break;
@@ -719,16 +723,47 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
 
 // The first pass: a group's sums of t and t * xh by column, which give its two means and dw and db. MANY: the columns' sums over a group's rows
 // meet in LDS, a thread to a column adds them up over the chunk's groups. Else (NP pieces a thread) a thread keeps its columns' sums over all of
-// the chunk's rows, and those of a group over its columns beside them.
+// the chunk's rows, and those of a group over its columns beside them in fp64. The former are in fp32 for GN_RUN rows at most; with one piece they are added to fp64
+// sums in LDS then, with several, for which LDS has no room, to the range's in fp32 at the end of every group. (All pieces' sums in registers took 400 of them: 30000 x 2500
+// bf16 in 3000 groups 553 us, 236 so; fp32 sums in LDS 251, but 2000 x 16384 fp32 269 instead of 194, as LDS holds one workgroup then.)
 template <int TH, int X, int G, bool MANY, int NP, bool PARTS>
-__device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
+__device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>& S, double* kept) {
     const Tile T = tile_of<TH>(A);
     const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
     unsigned int k0, k1;
     constexpr int MINE = GN_COLUMNS / TH;      // MANY: columns whose sums a thread has
     double dw[MINE] = {}, db[MINE] = {};
-    float dw_piece[MANY ? 1 : NP][8] = {}, db_piece[MANY ? 1 : NP][8] = {};
+    constexpr int KEPT = TH + 8;      // (a thread's sums lie so far apart; eight more, so that a column's reader finds its neighbours' in other banks)
+    float dw_piece[8] = {}, db_piece[8] = {};
+    int since = 0;              // rows in them
+    unsigned int there = 0;     // pieces of which something has been kept
+    float* const range = A.columns ? A.columns + (int64_t)blockIdx.y * 2 * A.d + T.c0 : nullptr;
+    // a piece's sums to LDS, or to the range's
+    const auto keep = [&](int i, const Piece& P) {
+        const bool more = there >> i & 1;
+        there |= 1u << i;
+        if constexpr (NP == 1) {
+            double* const at = kept + threadIdx.x;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                at[e * KEPT] = (more ? at[e * KEPT] : 0.0) + (double)dw_piece[e];
+                at[(8 + e) * KEPT] = (more ? at[(8 + e) * KEPT] : 0.0) + (double)db_piece[e];
+            }
+        } else if (range) {
+#pragma unroll
+            for (int sum = 0; sum < 2; ++sum) {
+                char* const at = (char*)(range + sum * A.d);
+                float f[8] = {};
+                if (more) fg_piece_values<FG_F32>(load_piece<FG_F32>(at, P.c), f);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) f[e] += sum ? db_piece[e] : dw_piece[e];
+                store_piece<FG_F32>(at, P, f);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dw_piece[e] = db_piece[e] = 0.f;
+    };
     for (Walk<PARTS> W(A, blockIdx.y); W.next(g, k0, k1, which);) {
         if (k0 == k1) continue;
         GradRows<X, G> R;
@@ -738,34 +773,46 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
         int rows = 0;
         for (unsigned int k = k0 + T.side; k < k1; k += T.sides) rows += position(A, k) >= 0;
         if constexpr (MANY) {
-            float s[8] = {}, q[8] = {};
-            const Piece P = piece_of(A, T, 0);
-            if (P.there) {
-                GradColumns C;
-                grad_columns<true, true>(A, T, g, P.c, C);
-                gradient_rows<X, G, true>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&x)[8], const float(&t)[8]) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * x[e];
-                });
-            }
-            leave_sums<TH, true>(A, T, S, s, q, rows);
-        } else {
-            double s[1] = {}, q[1] = {};
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const Piece P = piece_of(A, T, i);
+            for (unsigned int from = k0, to; from < k1; from = to) {
+                to = k1 - from > (unsigned int)(GN_RUN * T.sides) ? from + GN_RUN * T.sides : k1;
+                float s[8] = {}, q[8] = {};
+                const Piece P = piece_of(A, T, 0);
                 if (P.there) {
                     GradColumns C;
-                    grad_columns<false, false>(A, T, g, P.c, C);
-                    gradient_rows<X, G, false>(A, T, P.c, C, k0, k1, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
+                    grad_columns<true, true>(A, T, g, P.c, C);
+                    gradient_rows<X, G, true>(A, T, P.c, C, from, to, false, R, [&](int, const float(&x)[8], const float(&t)[8]) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) s[e] += t[e], q[e] += t[e] * x[e];
+                    });
+                }
+                leave_sums<TH, true>(A, T, S, s, q, rows, from != k0);
+            }
+        } else {
+            double s[1] = {}, q[1] = {};
+            const int mine = (int)((k1 - k0 + T.sides - 1) / T.sides);      // a thread's rows
+            if (NP == 1 && since + mine > GN_RUN) {
+                keep(0, piece_of(A, T, 0));
+                since = 0;
+            }
+            since = mine < GN_RUN ? since + mine : GN_RUN;
+            for (int i = 0; i < (NP == 1 ? 1 : A.pieces); ++i) {
+                const Piece P = piece_of(A, T, i);
+                if (!P.there) break;
+                GradColumns C;
+                grad_columns<false, false>(A, T, g, P.c, C);
+                for (unsigned int from = k0, to; from < k1; from = to) {
+                    to = k1 - from > (unsigned int)(GN_RUN * T.sides) ? from + GN_RUN * T.sides : k1;
+                    if (NP == 1 && from != k0) keep(0, P);
+                    gradient_rows<X, G, false>(A, T, P.c, C, from, to, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             if (e < P.twice) continue;
                             const double a = (double)(t[e] * C.w[e]);
                             s[0] += a, q[0] += a * (double)xh[e];
-                            dw_piece[i][e] += t[e] * xh[e], db_piece[i][e] += t[e];
+                            dw_piece[e] += t[e] * xh[e], db_piece[e] += t[e];
                         }
                     });
+                    if (NP > 1) keep(i, P);
                 }
             }
             leave_sums<TH, false>(A, T, S, s, q, rows);
@@ -803,55 +850,47 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH>& S) {
             (which == GN_BEGINS ? begins : goes_on) = g;
     }
     if constexpr (PARTS) note(A, chunk, goes_on, begins);
-    if (!A.columns) return;
-    float* const to = A.columns + (int64_t)blockIdx.y * 2 * A.d + T.c0;
+    if (!range) return;
     if constexpr (MANY) {
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             const int c = (int)threadIdx.x + TH * i;
-            if (c < T.cols) to[c] = (float)dw[i], to[A.d + c] = (float)db[i];
+            if (c < T.cols) range[c] = (float)dw[i], range[A.d + c] = (float)db[i];
         }
     } else {
-        float* const meet = (float*)S.wave;      // [side][width * 8]
-        static_assert(sizeof(S.wave) >= TH * 8 * sizeof(float), "eight columns of every thread");
-#pragma unroll
-        for (int which_sum = 0; which_sum < 2; ++which_sum) {
-            if (T.sides == 1) {
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    const Piece P = piece_of(A, T, i);
-                    if (P.there) store_piece<FG_F32>((char*)(to + which_sum * A.d), P, which_sum ? db_piece[i] : dw_piece[i]);
-                }
-            } else {      // rows side by side (NP is 1 then): their sums meet in LDS
-                const Piece P = piece_of(A, T, 0);
-                __syncthreads();
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e >= P.twice) meet[T.side * A.width * 8 + P.c + e] = which_sum ? db_piece[0][e] : dw_piece[0][e];
-                __syncthreads();
-                for (int c = threadIdx.x; c < T.cols; c += TH) {
-                    float v = 0.f;
-                    for (int i = 0; i < T.sides; ++i) v += meet[i * A.width * 8 + c];
-                    to[which_sum * A.d + c] = v;
-                }
+        if constexpr (NP > 1) {
+            for (int i = 0; i < A.pieces; ++i) {
+                const Piece P = piece_of(A, T, i);
+                if (P.there && !(there >> i & 1)) keep(i, P);
             }
+            return;
+        }
+        keep(0, piece_of(A, T, 0));
+        __syncthreads();
+        for (int c = threadIdx.x; c < T.cols; c += TH) {      // rows side by side: their sums meet
+            const int p = c / 8, e = c - (p * 8 + 8 <= T.cols ? p * 8 : T.cols - 8);
+            const double* at = kept + e * KEPT + p;
+            double w = 0.0, b = 0.0;
+            for (int i = 0; i < T.sides; ++i) w += at[i * A.width], b += at[8 * KEPT + i * A.width];
+            range[c] = (float)w, range[A.d + c] = (float)b;
         }
     }
 }
 template <int TH, int X, int G, bool MANY, int NP>
 __global__ __launch_bounds__(TH, NP > 1 ? 1 : gn_per_unit(X, MANY, true)) void group_norm_backward_kernel(GnArgs A) {
-    __shared__ Scratch<TH> S;
+    __shared__ Scratch<TH, MANY> S;
+    __shared__ double kept[MANY || NP > 1 ? 1 : 16 * (TH + 8)];
     if ((int)blockIdx.y < A.workers)
-        gradient_body<TH, X, G, MANY, NP, false>(A, S);
+        gradient_body<TH, X, G, MANY, NP, false>(A, S, kept);
     else
-        gradient_body<TH, X, G, MANY, NP, true>(A, S);
+        gradient_body<TH, X, G, MANY, NP, true>(A, S, kept);
 }
 // The second pass, on split groups
 template <int X, int G, bool MANY>
 __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_backward_apply_kernel(GnArgs A) {
-    __shared__ Scratch<GN_THREADS> S;
+    __shared__ Scratch<GN_THREADS, MANY> S;
     const Tile T = tile_of<GN_THREADS>(A);
-    split_parts<X, true>(A, T, S, [&](int g, unsigned int k0, unsigned int k1) {
+    split_parts<X, MANY, true>(A, T, S, [&](int g, unsigned int k0, unsigned int k1) {
         GradRows<X, G> R;
         input_gradient<GN_THREADS, X, G, MANY>(A, T, S, g, k0, k1, false, R);
     });

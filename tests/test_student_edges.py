@@ -164,3 +164,39 @@ def test_a_group_none_of_whose_entries_exists(B, n, d):
     B.fg_group_norm(x, d * 4, B.FG_F32, order, off, n, 2, n, d, 4, None, None, 0.25, B.FG_ACT_NONE, y, d * 4, B.FG_F32, mean, rstd, ws, len(ws))
     torch.cuda.synchronize()
     assert bool((mean[0] == 0).all()) and bool((rstd[0] == 2).all()) and bool((y[:n // 2] == -77).all()) and bool((mean[1] > 4).all()) and not bool((y[n // 2:] == -77).any())
+
+
+# ---- long sums ----
+
+@gpu
+@pytest.mark.parametrize("n, n_groups, d, blocks", [(16_400_000, 1, 256, 256), (16_400_000, 2, 256, 8), (8_200_000, 1, 512, 1), (2_050_000, 1, 4096, 1), (16_000_000, 100_000, 512, 1)])
+def test_gradients_of_groups_whose_threads_have_thousands_of_rows(B, n, n_groups, d, blocks):
+    """Terms that are all the same within a column: fp32 sums that went on for 2000 of them would be off by up to 2000 / 2^25 of the sum, always to one side."""
+    g = torch.Generator().manual_seed(d)
+    w, b = (0.5 + torch.rand(d, generator=g) for _ in range(2))
+    off = torch.linspace(0, n, n_groups + 1, dtype=torch.float64).long().cuda()
+    x = torch.ones(n, d, dtype=torch.bfloat16, device="cuda")
+    dy = torch.empty_like(x)
+    ws = torch.empty(B.fg_group_norm_backward_workspace_bytes(n, n_groups, d, blocks), dtype=torch.uint8, device="cuda")
+    rstd = torch.ones(n_groups, blocks, device="cuda")
+    wd, bd = w.cuda(), b.cuda()
+    u = 2.0 ** -24
+    # up to 128 rows of a thread in fp32, 8 sums over lanes, the joins' rounding, and what 2000 / 128 sums of those lose in fp32 (rows of more than 2048 columns)
+    steps = 128 + 8 + 4 + 16
+    for level in (0.0, 1.0):      # xh is 1 or 0
+        dy.fill_(1)
+        dw, db, mean = full(d), full(d), torch.full((n_groups, blocks), level, device="cuda")
+        B.fg_group_norm_backward(dy, 2 * d, B.FG_BF16, x, 2 * d, B.FG_BF16, mean, rstd, wd, bd, B.FG_ACT_SILU, None, off, n, n_groups, n, d, blocks, dy, 2 * d, dw, db, ws, len(ws))
+        torch.cuda.synchronize()
+        xh = 1.0 - level
+        arg = w.double() * xh + b.double()
+        t = R.slope("silu", arg)
+        t_off = R.slope_off("silu", arg) + 0.5 * 4 * u * arg.abs() + u * t
+        close(db.cpu(), n * t, n * (t_off + steps * u * t), f"db, xh {xh}")
+        close(dw.cpu(), n * t * xh, xh * n * (t_off + steps * u * t), f"dw, xh {xh}")
+        tw, tw_off = (t * w.double()).view(blocks, -1), ((t_off + u * t) * w.double()).view(blocks, -1)
+        m1 = tw.mean(1, keepdim=True)
+        want = (tw - m1 - xh * xh * m1).flatten()
+        tolerance = (tw_off + (1 + xh) * (tw_off.mean(1, keepdim=True) + steps * u * m1) + 8 * u * (tw + 2 * m1)).flatten() + HALF["bf16"] * want.abs()
+        for rows in (dy[:64], dy[n // 2:n // 2 + 64], dy[-64:]):
+            close(rows.cpu(), want.expand(64, -1), tolerance.expand(64, -1), f"dx, xh {xh}")
