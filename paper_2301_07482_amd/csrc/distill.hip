@@ -79,6 +79,25 @@ __device__ __forceinline__ float wave_sum(float v) {
     v += moved<0x143, 0xc>(v, 0.f);
     return last_lane(v);
 }
+// of two values at once: halves of the wavefront exchange them first
+__device__ __forceinline__ void wave_sums(double& a, double& b) {
+    double v = half_sums<32>(a, b);
+    const auto moved = [&](auto ctrl) {
+        const fg_u32x2 w = __builtin_bit_cast(fg_u32x2, v);
+        return __builtin_bit_cast(double, fg_u32x2{(unsigned int)__builtin_amdgcn_mov_dpp((int)w[0], decltype(ctrl)::value, 0xf, 0xf, false),
+                                                   (unsigned int)__builtin_amdgcn_mov_dpp((int)w[1], decltype(ctrl)::value, 0xf, 0xf, false)});
+    };
+    v += moved(std::integral_constant<int, 0xB1>());
+    v += moved(std::integral_constant<int, 0x4E>());
+    v += moved(std::integral_constant<int, 0x141>());
+    v += moved(std::integral_constant<int, 0x140>());
+    v = half_sums<16>(v, v);
+    const fg_u32x2 w = __builtin_bit_cast(fg_u32x2, v);
+    const auto of = [&](int lane) {
+        return __builtin_bit_cast(double, fg_u32x2{(unsigned int)__builtin_amdgcn_readlane((int)w[0], lane), (unsigned int)__builtin_amdgcn_readlane((int)w[1], lane)});
+    };
+    a = of(0), b = of(32);
+}
 __device__ __forceinline__ float wave_max(float v) {      // (what is NaN is left out)
     v = fmaxf(v, moved<0x111, 0xf>(v, -INFINITY));
     v = fmaxf(v, moved<0x112, 0xf>(v, -INFINITY));
@@ -268,11 +287,13 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
 
 // Wide rows: WAVES wavefronts to a row, one row to a workgroup. NP pieces of eight columns a lane in registers; TAIL: there are more. Pieces are counted from the 16-byte
 // line that the row begins in, so that all but the first and the last of them are whole lines (rows of 50003 bf16 15 % faster). An entry is in a lane of every wavefront, which
-// finds those of its own pieces.
+// finds those of its own pieces. Sums are in fp64 from a lane's pieces on (exchanged between registers, both softmaxes' at once). Five wavefronts to a SIMD where a 16-bit row's
+// pieces leave room, both in us (five | four): 20000 x 16384 271 | 291, 4096 x 8000 41.7 | 42.6, 8192 x 50003 456 to 465 | 459 to 463; losses alone the other way, 225 | 163 for
+// 8192 x 50000.
 template <int T, int WAVES, int NP, bool TAIL>
-__global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs A) {
+__global__ __launch_bounds__(WAVES * 64, T != FG_F32 && !TAIL ? 5 : 4) void distill_wide_kernel(DistillArgs A) {
     constexpr int E = T == FG_F32 ? 4 : 2, WIDTH = WAVES * 64;
-    __shared__ float red[2][WAVES];
+    __shared__ double red[2][WAVES];
     __shared__ float largest[WAVES];
     __shared__ int32_t top_class[WAVES > 1 ? 64 : 1];
     __shared__ float top_share[WAVES > 1 ? 64 : 1], teacher_log;
@@ -373,15 +394,15 @@ __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs
             sums_of(A.temperature, w, m, soften, s, h);
             soft += (double)s, hard += (double)h;
         });
-    float soft_sum = wave_sum((float)soft), hard_sum = wave_sum((float)hard);
+    wave_sums(soft, hard);
     if constexpr (WAVES > 1) {
-        if (lane == 0) red[0][wave] = soft_sum, red[1][wave] = hard_sum;
+        if (lane == 0) red[0][wave] = soft, red[1][wave] = hard;
         __syncthreads();
-        soft_sum = hard_sum = 0.f;
+        soft = hard = 0.0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) soft_sum += red[0][w], hard_sum += red[1][w];
-        soft_sum = one(soft_sum), hard_sum = one(hard_sum);
+        for (int w = 0; w < WAVES; ++w) soft += red[0][w], hard += red[1][w];
     }
+    const float soft_sum = one((float)soft), hard_sum = one((float)hard);
     const float log2_p = my_value - t_log, p = taught && my_class >= 0 ? exp2_of(log2_p) : 0.f;
     if (A.loss && wave == 0) {
         const float kl = wave_sum(p == 0.f ? 0.f : p * (log2_p - ((my_z - m) * soften - log2_of(soft_sum))));

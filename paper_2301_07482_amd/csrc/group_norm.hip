@@ -208,26 +208,6 @@ struct Scratch {
     float stats[COLUMNS][2];                // of a block: mean and rstd, or the gradient's two means
     int rows[TH / 64];
 };
-// Lanes l and l + HALF (of 64 for HALF = 32, of every 32 for 16) add up a and b between them: the first has a's sum, the other b's
-template <int HALF>
-__device__ __forceinline__ float half_sums(float a, float b) {
-    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
-    const unsigned int x = __float_as_uint(a), y = __float_as_uint(b);
-    const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-template <int HALF>
-__device__ __forceinline__ double half_sums(double a, double b) {
-    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
-    const fg_u32x2 x = __builtin_bit_cast(fg_u32x2, a), y = __builtin_bit_cast(fg_u32x2, b);
-    fg_u32x2 first, second;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false) : __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
-        first[i] = r[0], second[i] = r[1];
-    }
-    return __builtin_bit_cast(double, first) + __builtin_bit_cast(double, second);
-}
 // The sums s[e], q[e] of a thread's columns (MANY) or s[0], q[0] of all it has seen, over the rows that a wavefront has side by side, and the number of rows;
 // they are there after the workgroup's next barrier. Halves of the wavefront exchange half of their sums each: 16 fp64 sums over four rows take 24 exchanges between
 // registers instead of 64 through LDS. `more` (MANY): they are added to what is there.

@@ -1,6 +1,6 @@
 // What the calls on listed rows share: the list, sums over the lanes of a row, checks of their arguments.
 #pragma once
-#include "common.h"
+#include "row_types.h"
 
 // rows listed
 struct RowList {
@@ -53,6 +53,27 @@ __device__ __forceinline__ float row_max(float v, int lanes, double* lds) {
         for (int w = 1; w < WAVES; ++w) v = fmaxf(v, (float)lds[w]);
     }
     return v;
+}
+
+// Lanes l and l + HALF (of 64 for HALF = 32, of every 32 for 16) add up a and b between them: the first has a's sum, the other b's
+template <int HALF>
+__device__ __forceinline__ float half_sums(float a, float b) {
+    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
+    const unsigned int x = __float_as_uint(a), y = __float_as_uint(b);
+    const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x, y, false, false) : __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+template <int HALF>
+__device__ __forceinline__ double half_sums(double a, double b) {
+    static_assert(HALF == 32 || HALF == 16, "lanes that can be exchanged");
+    const fg_u32x2 x = __builtin_bit_cast(fg_u32x2, a), y = __builtin_bit_cast(fg_u32x2, b);
+    fg_u32x2 first, second;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto r = HALF == 32 ? __builtin_amdgcn_permlane32_swap(x[i], y[i], false, false) : __builtin_amdgcn_permlane16_swap(x[i], y[i], false, false);
+        first[i] = r[0], second[i] = r[1];
+    }
+    return __builtin_bit_cast(double, first) + __builtin_bit_cast(double, second);
 }
 
 static inline fg_status_t check_rows(const char* who, const int32_t* rows_dev, const int64_t* n_rows_dev, int64_t max_rows, int64_t n, int32_t d) {

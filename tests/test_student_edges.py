@@ -200,3 +200,35 @@ def test_gradients_of_groups_whose_threads_have_thousands_of_rows(B, n, n_groups
         tolerance = (tw_off + (1 + xh) * (tw_off.mean(1, keepdim=True) + steps * u * m1) + 8 * u * (tw + 2 * m1)).flatten() + HALF["bf16"] * want.abs()
         for rows in (dy[:64], dy[n // 2:n // 2 + 64], dy[-64:]):
             close(rows.cpu(), want.expand(64, -1), tolerance.expand(64, -1), f"dx, xh {xh}")
+
+
+# ---- the loss ----
+
+@gpu
+@pytest.mark.parametrize("lead", [0, 1])
+@pytest.mark.parametrize("dtype, d", [("f32", 600), ("f32", 3000), ("f32", 20_000), ("f32", 140_000), ("bf16", 1000), ("bf16", 50_000)])
+def test_sums_of_wide_rows_to_the_last_step(B, dtype, d, lead):
+    """One class of 1 and groups of classes that come to just under half a step of 1 each: added to it in fp32 one after the other, every one of them is lost. The largest class's share
+    is 1 / sum: half a step for the sum in fp32 (2^-24 above 1), half for the quotient (2^-25 below 1), and what the exponentials of the small ones are off."""
+    n, rows = 64, d + 5
+    want = []
+    h = torch.full((n, rows), -math.inf, dtype=T[dtype])
+    r = np.random.default_rng(d)
+    for i in range(n):
+        top = int(r.integers(0, d))
+        h[i, lead + top] = 0
+        groups = [r.integers(0, d, 2 ** int(r.integers(0, 5))) for _ in range(7)]
+        for at in groups:
+            h[i, lead + at] = torch.tensor(math.log(0.96 * 2.0 ** -24 / len(at)), dtype=torch.float64).to(T[dtype])
+        h[i, lead + top] = 0
+        want.append((top, float(torch.exp(h[i, lead:lead + d].double()).sum())))
+    hd = h.cuda()
+    dh = full(n, d)
+    label = torch.tensor([(top + 1) % d for top, _ in want], dtype=torch.int32, device="cuda")
+    e = T[dtype].itemsize
+    B.fg_distill_loss(hd.data_ptr() + lead * e, rows * e, code(B, dtype), None, None, n, n, d, None, None, None, B.FG_F32, 0, 0, label, 1.0, 0.0, None, 1.0, None, dh, 4 * d, B.FG_F32)
+    torch.cuda.synchronize()
+    for i, (top, total) in enumerate(want):
+        got = float(dh[i, top])
+        # (the exponentials: 7 * 2^-24 of them, each to 2^-18 of itself)
+        assert abs(got - 1 / total) <= (2.0 ** -24 + 2.0 ** -25 + 2.0 ** -38) / total, (i, got, 1 / total)
