@@ -186,12 +186,39 @@ __device__ __forceinline__ void wave_meets() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// all[at] = a wavefront's shares (at < 0: none), of zeros. Every lane leaves its number at its place; who finds another's marks the place as shared, and the shares of such a
+// place are added one after the other, in the lanes' order. (Nearly always no place is: a teacher's classes differ.)
+constexpr float SHARED = -1.f;
+__device__ __forceinline__ void share_out(float* all, int at, float share, int lane) {
+    if (at >= 0) all[at] = (float)lane;
+    wave_meets();
+    const bool other = at >= 0 && all[at] != (float)lane;
+    const bool any = __ballot(other) != 0;
+    wave_meets();
+    if (any) {
+        if (other) all[at] = SHARED;
+        wave_meets();
+        const bool shared = at >= 0 && all[at] == SHARED;
+        wave_meets();
+        if (shared) all[at] = 0.f;
+        wave_meets();
+        for (unsigned long long left = __ballot(shared); left; left &= left - 1) {
+            const int l = __ffsll((long long)left) - 1, place = __builtin_amdgcn_readlane(at, l);
+            const float v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), l));
+            if (lane == 0) all[place] += v;
+        }
+        if (shared) at = -1;
+    }
+    if (at >= 0) all[at] = share;
+    wave_meets();
+}
+
 // Narrow rows: 64 / LANES of them to a wavefront, eight columns to a lane. A row's values lie in LDS for its entries to find theirs, then what those take from its
 // gradient. Bound by memory and, nearly as long, by what a wavefront does beside its values: 54067 x 256 fp32 26 us (4.3 TB/s; without teacher and labels 17), 32 with the
 // lanes a number of the call's; two and four pieces a lane, for more rows to a wavefront, 28 and 30.
 struct Entry {
     int32_t c;      // class, -1: none
-    float p, log2_p, z;
+    float p, log2_p, z;      // p: its share of the gradient; z: its logit, then whether its class is another's too
 };
 template <int T, int LANES>
 __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs A) {
@@ -259,7 +286,8 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
             if (c < 0) continue;
             const float log2_p = entries[j].log2_p - t_log, p = exp2_of(log2_p);
             if (!(p == 0.f)) kl += p * (log2_p - ((entries[j].z - m) * soften - soft_log));
-            if (A.dh) __hip_atomic_fetch_add(all + c, a * p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);      // (lanes of one wavefront, in order)
+            entries[j].p = a * p;
+            all[c] = (float)j;
         }
     if (A.loss) {
         kl = lanes_sum_of<LANES>(kl);
@@ -271,7 +299,45 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
         }
     }
     if (!A.dh) return;
-    if (me == 0 && y >= 0) __hip_atomic_fetch_add(all + y, b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+    // as in share_out, with the entries' numbers (54067 x 256 fp32 with 64 entries: 30 us where all classes differ, 44 where most of a row's are stored twice; 38 with
+    // atomic additions, whose order in one instruction nothing says)
+    wave_meets();
+    bool other = false;
+    if (taught)
+        for (int j = me; j < A.k; j += LANES)
+            if (entries[j].c >= 0 && all[entries[j].c] != (float)j) other = true, entries[j].z = SHARED;
+            else entries[j].z = 0.f;
+    const bool any = __ballot(other) != 0;      // (in any row of the wavefront)
+    wave_meets();
+    if (any) {
+        if (other)
+            for (int j = me; j < A.k; j += LANES)
+                if (entries[j].z == SHARED) all[entries[j].c] = SHARED;
+        wave_meets();
+        if (taught)
+            for (int j = me; j < A.k; j += LANES)
+                if (entries[j].c >= 0 && all[entries[j].c] == SHARED) entries[j].z = SHARED;
+        wave_meets();
+        if (taught)
+            for (int j = me; j < A.k; j += LANES)
+                if (entries[j].c >= 0 && entries[j].z == SHARED) all[entries[j].c] = 0.f;
+        wave_meets();
+        for (int j0 = 0; j0 < A.k; j0 += LANES) {
+            const int j = j0 + me;
+            unsigned long long left = __ballot(taught && j < A.k && entries[j].c >= 0 && entries[j].z == SHARED) >> ((threadIdx.x & 63) - me);
+            if constexpr (LANES < 64) left &= (1ull << LANES) - 1;
+            if (me == 0)
+                for (; left; left &= left - 1) {
+                    const Entry& shared = entries[j0 + __ffsll((long long)left) - 1];
+                    all[shared.c] += shared.p;
+                }
+        }
+    }
+    if (taught)
+        for (int j = me; j < A.k; j += LANES)
+            if (entries[j].c >= 0 && entries[j].z != SHARED) all[entries[j].c] = entries[j].p;
+    wave_meets();
+    if (me == 0 && y >= 0) all[y] += b;
     wave_meets();
     if (left <= 0) return;
     float g[8] = {};
@@ -417,18 +483,16 @@ __global__ __launch_bounds__(WAVES * 64, T != FG_F32 && !TAIL ? 5 : 4) void dist
     const float scale = A.grad_scale * weight, a = taught ? scale * A.alpha * A.temperature : 0.f, b = y >= 0 ? scale * (1.f - A.alpha) : 0.f;
     const float a_q = taught ? a / soft_sum : 0.f, b_q = y >= 0 ? b / hard_sum : 0.f, my_share = a * p;
     const int32_t my_place = taught && my_class >= 0 ? my_class + lead : -1, label_place = y >= 0 ? y + lead : -1;
-    if constexpr (BY_LDS) {      // eight columns of a lane's piece behind each other; entries of one class are added in their lanes' order
+    if constexpr (BY_LDS) {      // eight columns of a lane's piece behind each other
         float* const mine = taken + wave * NP * 512;
 #pragma unroll
         for (int i = 0; i < NP; ++i) ((float4*)mine)[i * 128 + lane * 2] = ((float4*)mine)[i * 128 + lane * 2 + 1] = float4{0.f, 0.f, 0.f, 0.f};
         wave_meets();
-        auto add = [&](int32_t place, float share) {
-            const int piece = place >> 3;
-            if (place >= 0 && piece % WIDTH / 64 == wave)
-                __hip_atomic_fetch_add(mine + piece / WIDTH * 512 + (place & 511), share, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
-        };
-        add(my_place, my_share);
-        if (lane == 0) add(label_place, b);
+        // where a column's share lies if it is in this wavefront's pieces, -1: it is not
+        const auto at = [&](int32_t place) { return place >= 0 && (place >> 3) % WIDTH / 64 == wave ? (place >> 3) / WIDTH * 512 + (place & 511) : -1; };
+        const int my_at = at(my_place), label_at = at(label_place);
+        share_out(mine, my_at, my_share, lane);
+        if (lane == 0 && label_at >= 0) mine[label_at] += b;
         wave_meets();
     }
     char* const out = A.dh + r * A.dh_stride;
@@ -441,27 +505,27 @@ __global__ __launch_bounds__(WAVES * 64, T != FG_F32 && !TAIL ? 5 : 4) void dist
             const float4 lo = from[0], hi = from[1];
             g[0] -= lo.x, g[1] -= lo.y, g[2] -= lo.z, g[3] -= lo.w, g[4] -= hi.x, g[5] -= hi.y, g[6] -= hi.z, g[7] -= hi.w;
         } else {
-        // entries whose class lies in the wavefront's pieces: 512 columns from here
-        auto take = [&](int32_t k, float share) {      // (the same in all lanes)
-            const float mine = (k - first) >> 3 == lane ? share : 0.f;
-            switch (k & 7) {
-                case 0: g[0] -= mine; break;
-                case 1: g[1] -= mine; break;
-                case 2: g[2] -= mine; break;
-                case 3: g[3] -= mine; break;
-                case 4: g[4] -= mine; break;
-                case 5: g[5] -= mine; break;
-                case 6: g[6] -= mine; break;
-                default: g[7] -= mine;
+            // entries whose class lies in the wavefront's pieces: 512 columns from here
+            auto take = [&](int32_t k, float share) {      // (the same in all lanes)
+                const float mine = (k - first) >> 3 == lane ? share : 0.f;
+                switch (k & 7) {
+                    case 0: g[0] -= mine; break;
+                    case 1: g[1] -= mine; break;
+                    case 2: g[2] -= mine; break;
+                    case 3: g[3] -= mine; break;
+                    case 4: g[4] -= mine; break;
+                    case 5: g[5] -= mine; break;
+                    case 6: g[6] -= mine; break;
+                    default: g[7] -= mine;
+                }
+            };
+            unsigned long long there = __ballot(my_place >= first && my_place < first + 512);
+            while (there) {
+                const int l = __ffsll((long long)there) - 1;
+                there &= there - 1;
+                take(__builtin_amdgcn_readlane(my_place, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_share), l)));
             }
-        };
-        unsigned long long there = __ballot(my_place >= first && my_place < first + 512);
-        while (there) {
-            const int l = __ffsll((long long)there) - 1;
-            there &= there - 1;
-            take(__builtin_amdgcn_readlane(my_place, l), __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(my_share), l)));
-        }
-        if (label_place >= first && label_place < first + 512) take(label_place, b);
+            if (label_place >= first && label_place < first + 512) take(label_place, b);
         }
         if (c >= d) return;
         auto put = [&](auto type) {

@@ -232,3 +232,47 @@ def test_sums_of_wide_rows_to_the_last_step(B, dtype, d, lead):
         got = float(dh[i, top])
         # (the exponentials: 7 * 2^-24 of them, each to 2^-18 of itself)
         assert abs(got - 1 / total) <= (2.0 ** -24 + 2.0 ** -25 + 2.0 ** -38) / total, (i, got, 1 / total)
+
+
+@gpu
+@pytest.mark.parametrize("dtype, d, bound", [("f32", 40, 0), ("f32", 120, 0), ("bf16", 256, 0), ("f32", 500, 0), ("f16", 1500, 0), ("bf16", 3000, 0), ("f32", 3000, 20_000), ("bf16", 8000, 5000), ("f32", 20_000, 0),
+                                             ("bf16", 90_000, 0)])
+def test_shares_of_one_class_are_added_in_the_entries_order(B, dtype, d, bound):
+    """The entries' shares as a row of different classes shows them, each by itself where no logit can be chosen; then rows whose entries share classes: the fp32 sums of
+    those shares, one after the other, to the bit, and the label's behind them."""
+    n, k, r = 40, 50, np.random.default_rng(d)
+    k = min(k, d - 1)
+    h = torch.full((n, d), -math.inf, dtype=T[dtype])
+    h[:, d - 1] = 0      # the one class that can be
+    val = (3 * torch.randn(1, k, generator=torch.Generator().manual_seed(d))).repeat(n, 1)
+    idx = np.empty((n, k), np.int32)
+    for i in range(n):      # row 0: all different; the others: more and more alike
+        idx[i] = r.permutation(d - 1)[:k] if i == 0 else r.integers(0, d - 1, max(1, k - i))[r.integers(0, max(1, k - i), k)]
+    idx[3] = idx[3, 0]
+    label = np.full(n, -1, np.int32)
+    label[4::3] = idx[4::3, 7]
+    rows = torch.full((max(bound, n),), -1, dtype=torch.int32, device="cuda")
+    rows[:n] = torch.arange(n)
+    count = torch.full((1,), n, device="cuda")
+    dev = h.cuda(), torch.from_numpy(idx).cuda(), val.cuda(), torch.from_numpy(label).cuda()
+
+    def call(label):
+        dh = full(n, d)
+        B.fg_distill_loss(dev[0], stride(h), code(B, dtype), rows, count, len(rows), n, d, None, dev[1], dev[2], B.FG_F32, n, k, label, 1.0, 0.75, None, 1.0, None, dh, 4 * d, B.FG_F32)
+        torch.cuda.synchronize()
+        return dh.cpu().numpy()
+
+    plain = call(None)
+    share = -plain[0, idx[0]]
+    assert (share > 0).all() and abs(float(share.astype(np.float64).sum()) - 0.75) < 1e-5
+    got = call(dev[3])
+    for i in range(1, n):
+        want = np.zeros(d, np.float32)
+        for j in range(k):
+            want[idx[i, j]] += share[j]
+        assert np.array_equal(plain[i, :d - 1], -want[:d - 1]), i
+        if label[i] >= 0:
+            want[label[i]] += np.float32(0.25)
+        assert np.array_equal(got[i, :d - 1], -want[:d - 1]), i
+    for _ in range(3):
+        assert np.array_equal(call(dev[3]), got)
