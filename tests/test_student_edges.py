@@ -276,3 +276,56 @@ def test_shares_of_one_class_are_added_in_the_entries_order(B, dtype, d, bound):
         assert np.array_equal(got[i, :d - 1], -want[:d - 1]), i
     for _ in range(3):
         assert np.array_equal(call(dev[3]), got)
+
+
+def distill_case(B, dtype, dh_type, n, d, k, bound, pad, seed, temp=2.0, alpha=0.6, over=False):
+    """n rows of a list whose bound is `bound`, a count on the device; against the statement."""
+    r = np.random.default_rng(seed)
+    h = values(r, n, d, dtype, pad, 3.0)
+    idx = np.stack([r.permutation(d)[:k] for _ in range(n)]).astype(np.int32)
+    idx[r.random(idx.shape) < 0.1] = -1
+    idx[::3, 1] = idx[::3, 0]
+    idx[1], idx[2, 0] = -1, d - 1
+    val = torch.from_numpy(4 * r.standard_normal((n, k))).to(torch.float16)
+    label = r.integers(-1, d, n).astype(np.int32)
+    label[1], label[2] = -1, d - 1
+    h[4, :d] = -math.inf      # no class to choose
+    label[4] = 0
+    h[5, :d] = -math.inf
+    idx[5], label[5] = -1, -1
+    h[6, 0] = math.nan
+    rows = torch.full((bound,), -1, dtype=torch.int32)
+    order = r.permutation(n).astype(np.int32)
+    rows[:n] = torch.from_numpy(order)
+    hd, loss, dh = h.cuda(), full(n), sentinel(n, d, dh_type, pad).cuda()
+    out = hd if over else dh
+    B.fg_distill_loss(hd, stride(hd), code(B, dtype), rows.cuda(), torch.full((1,), n, device="cuda"), bound, n, d, None, torch.from_numpy(idx).cuda(), val.cuda(), B.FG_F16, n, k,
+                      torch.from_numpy(label).cuda(), temp, alpha, None, 0.5, loss, out, stride(out), code(B, dh_type))
+    torch.cuda.synchronize()
+    loss, got = loss.cpu(), out.cpu()
+    assert bool((dh.cpu()[:, d:] == -77).all()) and (not over or bool(torch.isnan(got[:, d:]).all()))
+    for i in (4, 6):
+        if i == 4 or label[6] >= 0 or (idx[6] >= 0).any():
+            assert bool(torch.isnan(loss[i])) and bool(torch.isnan(got[i, :d]).all()), i
+    for i in (1, 5):
+        assert float(loss[i]) == 0 and not bool(got[i, :d].any())
+    rest = [i for i in range(n) if i not in (4, 6)]
+    want, off, grad, grad_off = R.distill(h[rest, :d], torch.from_numpy(idx[rest]), val[rest], label[rest], temp, alpha, None, 0.5)
+    close(loss[rest], want, off + 2.0 ** -24 * want.abs(), "loss")
+    close(got[rest, :d], grad, grad_off + HALF[dh_type] * grad.abs() + TINY[dh_type], "dh")
+
+
+@gpu
+@pytest.mark.parametrize("over", [False, True])
+@pytest.mark.parametrize("dtype, d, bound, pad", [("f32", 2100, 5000, 0), ("f32", 4000, 5000, 3), ("f32", 4080, 17_000, 1), ("f32", 2500, 17_000, 5), ("bf16", 3000, 17_000, 1), ("bf16", 4081, 17_000, 3),
+                                                   ("bf16", 5000, 5000, 0), ("bf16", 8000, 5000, 3), ("f16", 8176, 20_000, 5), ("f16", 4100, 4097, 2)])
+def test_wide_rows_one_to_a_wavefront(B, dtype, d, bound, pad, over):
+    """More rows may be listed than rows of one wavefront need: those of up to 4088 columns, in 16 bits 8184, at strides that are no multiples of a line."""
+    distill_case(B, dtype, dtype, 12, d, 30, bound, pad, d, over=over)
+
+
+@gpu
+@pytest.mark.parametrize("temp", [1.0, 2.5, 4.0])
+def test_wide_rows_one_to_a_wavefront_at_other_temperatures(B, temp):
+    distill_case(B, "bf16", "f32", 10, 6001, 64, 4500, 1, 7, temp, 1.0)
+    distill_case(B, "f32", "f32", 10, 3001, 64, 4500, 1, 8, temp, 0.0)
