@@ -329,3 +329,160 @@ def test_wide_rows_one_to_a_wavefront(B, dtype, d, bound, pad, over):
 def test_wide_rows_one_to_a_wavefront_at_other_temperatures(B, temp):
     distill_case(B, "bf16", "f32", 10, 6001, 64, 4500, 1, 7, temp, 1.0)
     distill_case(B, "f32", "f32", 10, 3001, 64, 4500, 1, 8, temp, 0.0)
+
+
+# ---- far arguments, infinities, NaN ----
+
+def far_arguments(name, count):
+    """Arguments of an activation: near zero, through its bend, into both tails to where they leave fp32, and the largest numbers."""
+    u = torch.cat([torch.linspace(-20, 20, count // 2), torch.linspace(-120, 120, count // 4), torch.tensor([0.0, -0.0, 1e-30, -1e-30, 2.0 ** -126, 1e-40, -1e-40, 1e30, -1e30, 3e38, -3e38]),
+                   torch.linspace(-104, -86, 40), torch.linspace(86, 104, 40), torch.linspace(-15, -12, 60)])
+    return torch.cat([u, torch.linspace(-1, 1, count - len(u))])
+
+
+def act_at(name, u):
+    """R.act, with the lower tail of the normal distribution function as it is (1 + erf(x) leaves nothing of it below -8)."""
+    return u * 0.5 * torch.special.erfc(-u * math.sqrt(0.5)) if name == "gelu" else R.act(name, u)
+
+
+def far_off(name, u):
+    """act_off and slope_off; beyond where a tail has left fp32 an argument's size adds nothing: act(u) is u or 1 there, and its slope 1 or 0."""
+    near = u.double().clamp(-104, 104) if name != "gelu" else u.double().clamp(-15, 15)
+    steps = (16 + near.abs() + (near * near if name == "gelu" else 0)) * 2.0 ** -24
+    f = act_at(name, u.double()).abs()
+    return (f * steps if name not in ("none", "relu") else 0 * f) + 2.0 ** -100, R.slope_off(name, near) + 0 * f
+
+
+def slope_at(name, u):
+    if name != "gelu" and name != "silu":
+        return R.slope(name, u)
+    return torch.where(u.abs() > 200, (u > 0).double(), R.slope(name, u.clamp(-200, 200)))      # (0 * infinity in the statement)
+
+
+@gpu
+@pytest.mark.parametrize("name", R.ACTS)
+@pytest.mark.parametrize("rows", [3, 40_000])
+def test_far_arguments_of_the_gated_layer(B, name, rows):
+    """z is the bias (x is 0), the other projection 1: h is the activation, and with dh = 1 db is its slope. Few rows and many, which are kernels of their own."""
+    b, a = 2048, 8
+    u = far_arguments(name, b)
+    bias = torch.cat([u, torch.ones(b)])[None]
+    x, W = torch.zeros(rows, a, device="cuda"), torch.ones(1, a, 2 * b, device="cuda")
+    h, z, off = torch.empty(rows, b, device="cuda"), torch.empty(rows, 2 * b, device="cuda"), torch.tensor([0, rows], device="cuda")
+    B.fg_gated_linear_grouped(x, rows, 4 * a, B.FG_F32, None, None, off, rows, 1, a, b, W, bias.cuda(), act_code(B, name), h, rows, 4 * b, B.FG_F32, z, 8 * b)
+    f_off, s_off = far_off(name, u)
+    for r in (0, rows - 1):
+        assert torch.equal(z[r].cpu() + 0.0, bias[0] + 0.0)
+        close(h[r].cpu(), act_at(name, u.double()), f_off, "h")
+    assert torch.equal(h[1:], h[:1].expand(rows - 1, -1))
+    need = B.fg_gated_linear_grouped_backward_workspace_bytes(B.FG_F32, 1, 1, a, b)
+    ws, db, one = torch.empty(need, dtype=torch.uint8, device="cuda"), full(1, 2 * b), torch.tensor([0, 1], device="cuda")
+    B.fg_gated_linear_grouped_backward(x, rows, 4 * a, B.FG_F32, None, torch.ones(rows, b, device="cuda"), 4 * b, B.FG_F32, z, 8 * b, rows, None, one, 1, 1, a, b, W, act_code(B, name), None, 0,
+                                       B.FG_F32, None, B.FG_F32, db, ws, need)
+    torch.cuda.synchronize()
+    s = torch.where(u == 0, torch.zeros(()).double(), slope_at(name, u.double())) if name == "relu" else slope_at(name, u.double())
+    close(db[0, :b].cpu(), s, s_off, "slope")
+    close(db[0, b:].cpu(), act_at(name, u.double()), f_off, "act")
+
+
+@gpu
+@pytest.mark.parametrize("name", R.ACTS)
+@pytest.mark.parametrize("rows, blocks", [(5, 64), (5, 1), (3000, 64)])
+def test_far_arguments_of_the_group_norm(B, name, rows, blocks):
+    """Rows that are all alike: y is the activation of the bias, db the rows' number times its slope."""
+    d = 2048
+    u = far_arguments(name, d)
+    x, y, off = torch.full((rows, d), 3.0, device="cuda"), torch.empty(rows, d, device="cuda"), torch.tensor([0, rows], device="cuda")
+    mean, rstd, bias = full(1, blocks), full(1, blocks), u.cuda()
+    ws = torch.empty(B.fg_group_norm_backward_workspace_bytes(rows, 1, d, blocks), dtype=torch.uint8, device="cuda")
+    B.fg_group_norm(x, 4 * d, B.FG_F32, None, off, rows, 1, rows, d, blocks, None, bias, 0.25, act_code(B, name), y, 4 * d, B.FG_F32, mean, rstd, ws, len(ws))
+    dx, dw, db = full(rows, d), full(d), full(d)
+    B.fg_group_norm_backward(torch.ones_like(x), 4 * d, B.FG_F32, x, 4 * d, B.FG_F32, mean, rstd, None, bias, act_code(B, name), None, off, rows, 1, rows, d, blocks, dx, 4 * d, dw, db, ws,
+                             len(ws))
+    torch.cuda.synchronize()
+    assert bool((mean == 3).all()) and bool((rstd == 2).all()) and bool((dw == 0).all()) and bool(torch.isfinite(dx).all())
+    f_off, s_off = far_off(name, u)
+    close(y[0].cpu(), act_at(name, u.double()), f_off, "y")
+    assert torch.equal(y, y[:1].expand(rows, -1))
+    s = slope_at(name, u.double())
+    close(db.cpu(), rows * s, rows * (s_off + 160 * 2.0 ** -24 * s.abs()) + 2.0 ** -100, "db")
+
+
+@gpu
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("n, a, b", [(9, 64, 40), (40_000, 72, 264)])
+def test_the_gated_layer_keeps_what_is_not_finite_in_its_row(B, dtype, n, a, b, bad):
+    c, e = code(B, dtype), T[dtype].itemsize
+    g = torch.Generator(device="cuda").manual_seed(n)
+    kw = dict(device="cuda", generator=g)
+    x, W = torch.randn(n, a, **kw).to(T[dtype]), (torch.randn(2, a, 2 * b, **kw) / 8).to(T[dtype])
+    dh, off = torch.randn(n, b, **kw).to(T[dtype]), torch.tensor([0, n // 3, n], device="cuda")
+    need = B.fg_gated_linear_grouped_backward_workspace_bytes(c, n, 2, a, b)
+
+    def run(x, dh, z=None):
+        h, own_z = torch.empty(n, b, dtype=T[dtype], device="cuda"), torch.empty(n, 2 * b, dtype=T[dtype], device="cuda")
+        B.fg_gated_linear_grouped(x, n, a * e, c, None, None, off, n, 2, a, b, W, None, B.FG_ACT_SILU, h, n, b * e, c, own_z, 2 * b * e)
+        z = own_z if z is None else z
+        dx, dw, db = torch.empty(n, a, dtype=T[dtype], device="cuda"), full(2, a, 2 * b), full(2, 2 * b)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        B.fg_gated_linear_grouped_backward(x, n, a * e, c, None, dh, b * e, c, z, 2 * b * e, n, None, off, n, 2, a, b, W, B.FG_ACT_SILU, dx, a * e, c, dw, B.FG_F32, db, ws, need)
+        torch.cuda.synchronize()
+        return h, dx, dw, db, z
+
+    want = run(x, dh)
+    row = n // 3 + 2      # of the second group
+    others = torch.arange(n, device="cuda") != row
+    xb, dhb = x.clone(), dh.clone()
+    xb[row, 5], dhb[row, 7] = bad, bad
+    h, dx, dw, db, _ = run(xb, dhb, want[4])      # (the gradients with the projections of the rows as they were)
+    assert not bool(torch.isfinite(h[row]).any()) and not bool(torch.isfinite(dx[row]).any())
+    assert torch.equal(h[others], want[0][others]) and torch.equal(dx[others], want[1][others])
+    assert torch.equal(dw[0], want[2][0]) and torch.equal(db[0], want[3][0])
+    bad_columns = torch.zeros(2 * b, dtype=torch.bool, device="cuda")
+    bad_columns[[7, b + 7]] = True
+    assert not bool(torch.isfinite(db[1][bad_columns]).any()) and torch.equal(db[1][~bad_columns], want[3][1][~bad_columns])
+    assert not bool(torch.isfinite(dw[1][:, bad_columns]).any()) and not bool(torch.isfinite(dw[1][5]).any())
+    there = torch.arange(a, device="cuda") != 5
+    assert torch.equal(dw[1][there][:, ~bad_columns], want[2][1][there][:, ~bad_columns])
+
+
+@gpu
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("dtype, n, n_groups, d, blocks", [("f32", 300, 3, 88, 8), ("bf16", 50_000, 3, 256, 8), ("f32", 30_000, 2, 512, 1), ("f16", 600, 30, 96, 96), ("bf16", 300, 2, 4096, 1),
+                                                         ("f32", 4000, 1000, 40, 2)])
+def test_the_group_norm_keeps_what_is_not_finite_in_its_block(B, dtype, n, n_groups, d, blocks, bad):
+    c, e = code(B, dtype), T[dtype].itemsize
+    g = torch.Generator(device="cuda").manual_seed(n)
+    kw = dict(device="cuda", generator=g)
+    x, dy, off = torch.randn(n, d, **kw).to(T[dtype]), torch.randn(n, d, **kw).to(T[dtype]), torch.linspace(0, n, n_groups + 1, dtype=torch.float64).long().cuda()
+    ws = torch.empty(B.fg_group_norm_backward_workspace_bytes(n, n_groups, d, blocks), dtype=torch.uint8, device="cuda")
+    mean, rstd = torch.zeros(n_groups, blocks, device="cuda"), torch.ones(n_groups, blocks, device="cuda")
+
+    def run(x, dy):
+        y, m, r, dx, dw, db = torch.empty_like(x), full(n_groups, blocks), full(n_groups, blocks), torch.empty_like(x), full(d), full(d)
+        B.fg_group_norm(x, d * e, c, None, off, n, n_groups, n, d, blocks, None, None, 1e-5, B.FG_ACT_SILU, y, d * e, c, m, r, ws, len(ws))
+        B.fg_group_norm_backward(dy, d * e, c, x, d * e, c, mean, rstd, None, None, B.FG_ACT_SILU, None, off, n, n_groups, n, d, blocks, dx, d * e, dw, db, ws, len(ws))
+        torch.cuda.synchronize()
+        return y, m, r, dx, dw, db
+
+    good = run(x, dy)
+    group, column = n_groups - 1, d - 3
+    block, size = column // (d // blocks), d // blocks
+    for row in (int(off[group]), int(off[group]) + int(off[group + 1] - off[group]) // 2):      # the group's first, whose values are the level; another
+        for of_x in (True, False):
+            xb, dyb = x.clone(), dy.clone()
+            (xb if of_x else dyb)[row, column] = bad
+            y, m, r, dx, dw, db = run(xb, dyb)
+            inside = torch.zeros(n, d, dtype=torch.bool, device="cuda")
+            inside[off[group]:off[group + 1], block * size:(block + 1) * size] = True
+            one = torch.zeros(d, dtype=torch.bool, device="cuda")
+            one[column] = True
+            if of_x:
+                assert not bool(torch.isfinite(y[inside]).any()) and not bool(torch.isfinite(r[group, block])) and not bool(torch.isfinite(m[group, block]))
+                m[group, block], r[group, block] = good[1][group, block], good[2][group, block]
+            else:
+                assert torch.equal(y, good[0])
+            assert torch.equal(y[~inside], good[0][~inside]) and torch.equal(m, good[1]) and torch.equal(r, good[2])
+            assert torch.equal(dx[~inside], good[3][~inside]) and torch.equal(dw[~one], good[4][~one]) and torch.equal(db[~one], good[5][~one])
+            assert not bool(torch.isfinite(dx[inside]).any()) and not bool(torch.isfinite(dw[column])), (row, of_x)
