@@ -1036,8 +1036,8 @@ fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride, fg_dtype_t
  * label in [0, d) (or with alpha = 1) no second; a row with neither has loss 0 and gradient 0 whatever its logits. A class that is stored twice has
  * the sum of both. A logit of -infinity is a class that cannot be chosen: no gradient, an infinite loss if the teacher or the label has it. Where no
  * class of a row with a teacher or a label can be chosen, and where a logit is +infinity or NaN, the row's loss and gradient are NaN.
- * Exponentials, gradients and sums in fp32, those of wide rows (more than 512 columns) in fp64 from eight columns on. Pointers and strides aligned to the
- * element, d up to FG_MAX_CLASSES.
+ * Exponentials, gradients and sums in fp32, those of wide rows (more than 512 columns) in fp64 from eight columns on; the shares of a class that is stored
+ * several times are added in the entries' order. Pointers and strides aligned to the element, d up to FG_MAX_CLASSES, temperature from 2^-60 to 2^60.
  */
 #define FG_MAX_TOP 64
 #define FG_MAX_CLASSES 1073741824

@@ -598,7 +598,8 @@ extern "C" fg_status_t fg_distill_loss(const void* h, int64_t h_stride, fg_dtype
     if (d > FG_MAX_CLASSES) FG_FAIL(FG_ERR_SHAPE, "%s: d = %d is more than %d", who, d, FG_MAX_CLASSES);
     if (k < 0 || k > FG_MAX_TOP) FG_FAIL(FG_ERR_SHAPE, "%s: k = %d is not in 0..%d", who, k, FG_MAX_TOP);
     if (table_rows < 0 || table_rows > INT32_MAX) FG_FAIL(FG_ERR_INVALID_ARG, "%s: a number of rows is negative or too large", who);
-    if (!(temperature > 0.f && temperature < INFINITY)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: temperature = %g must be positive", who, (double)temperature);
+    if (!(temperature >= 0x1p-60f && temperature <= 0x1p60f))      // (its square and its reciprocal are fp32 numbers)
+        FG_FAIL(FG_ERR_INVALID_ARG, "%s: temperature = %g is not in 2^-60..2^60", who, (double)temperature);
     if (!(alpha >= 0.f && alpha <= 1.f)) FG_FAIL(FG_ERR_INVALID_ARG, "%s: alpha = %g is not in [0, 1]", who, (double)alpha);
     if (!loss_out && !dh) FG_FAIL(FG_ERR_INVALID_ARG, "%s: neither loss nor gradient is wanted", who);
     const bool work = max_rows > 0 && n > 0;

@@ -486,3 +486,28 @@ def test_the_group_norm_keeps_what_is_not_finite_in_its_block(B, dtype, n, n_gro
             assert torch.equal(y[~inside], good[0][~inside]) and torch.equal(m, good[1]) and torch.equal(r, good[2])
             assert torch.equal(dx[~inside], good[3][~inside]) and torch.equal(dw[~one], good[4][~one]) and torch.equal(db[~one], good[5][~one])
             assert not bool(torch.isfinite(dx[inside]).any()) and not bool(torch.isfinite(dw[column])), (row, of_x)
+
+
+def test_temperatures_beyond_what_fp32_can_square(B):
+    """1e-39 gave NaN (0 times the infinite reciprocal), 1e20 an infinite loss."""
+    for t in (1e-39, 2.0 ** -61, 1e20, 2.0 ** 61, 0.0, -1.0, math.inf, math.nan):
+        assert refused(B, B.fg_distill_loss, P, 256, B.FG_F32, None, None, 10, 10, 64, None, P, P, B.FG_F16, 10, 4, None, t, 0.5, None, 1.0, P, P + 4096, 256, B.FG_F32) == B.FG_ERR_INVALID_ARG, t
+
+
+@gpu
+@pytest.mark.parametrize("d", [40, 600, 9000])
+def test_the_least_and_the_largest_temperature(B, d):
+    """At 2^-60 the softmax is the largest logit's alone, at 2^60 all classes are alike."""
+    h = torch.zeros(1, d)
+    h[0, 3] = 1.0
+    idx, val = torch.tensor([[3, 7]], dtype=torch.int32, device="cuda"), torch.tensor([[1.0, 0.0]], device="cuda")
+    for t, q, p in ((2.0 ** -60, 1.0, (1.0, 0.0)), (2.0 ** 60, 1.0 / d, (0.5, 0.5))):
+        loss, dh = full(1), full(1, d)
+        B.fg_distill_loss(h.cuda(), 4 * d, B.FG_F32, None, None, 1, 1, d, None, idx, val, B.FG_F32, 1, 2, None, t, 1.0, None, 1.0, loss, dh, 4 * d, B.FG_F32)
+        torch.cuda.synchronize()
+        got = dh.cpu().double()[0] / t
+        want = torch.full((d,), 0.0 if t < 1 else 1.0 / d, dtype=torch.float64)
+        want[3] = q
+        want[3] -= p[0]
+        want[7] -= p[1]
+        assert bool(torch.isfinite(loss).all()) and bool(((got - want).abs() <= 2.0 ** -20).all()), t
