@@ -33,11 +33,6 @@ struct DistillArgs {
     int64_t dh_stride;
 };
 
-__device__ __forceinline__ float value_at(const char* p, int type, int64_t i) {
-    if (type == FG_F32) return ((const float*)p)[i];
-    const unsigned short v = ((const unsigned short*)p)[i];
-    return type == FG_BF16 ? __uint_as_float((unsigned int)v << 16) : (float)__builtin_bit_cast(_Float16, v);
-}
 // the largest of three, those that are NaN left out (the library's fmaxf makes its operands quiet first)
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float m;
@@ -175,7 +170,7 @@ __device__ __forceinline__ void entry_of(const DistillArgs& A, int32_t node, int
     if (node < 0) return;
     const int64_t at = (int64_t)node * A.k + j;
     c = A.top_idx[at];
-    t = value_at(A.top_val, A.top_dtype, at);
+    t = fg_element(A.top_val, A.top_dtype, at);
     if (c < 0 || c >= A.d) c = -1, t = -INFINITY;
 }
 
@@ -401,8 +396,8 @@ __global__ __launch_bounds__(WAVES * 64, T != FG_F32 && !TAIL ? 5 : 4) void dist
     float my_value = -INFINITY, my_z = 0.f, z_label = 0.f;
     if (wave == 0) {
         if (lane < A.k) entry_of(A, node, lane, my_class, my_value);
-        if (my_class >= 0) my_z = value_at(row, T, my_class);
-        if (y >= 0) z_label = value_at(row, T, y);
+        if (my_class >= 0) my_z = fg_element(row, T, my_class);
+        if (y >= 0) z_label = fg_element(row, T, y);
     }
     // f(piece, values) for every piece of this wavefront, columns that do not exist -infinity
     auto each = [&](auto f) {

@@ -219,12 +219,7 @@ __device__ __forceinline__ void leave_sums(const GnArgs& A, const Tile& T, Scrat
         const Piece P = piece_of(A, T, 0);
         double* const to = S.wave[fg_wave()] + P.c;
         const auto put = [&](int at, V v) { to[at] = more ? to[at] + (double)v : (double)v; };
-        if (A.width >= 64) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e >= P.twice) put(e, s[e]), put(GN_COLUMNS + e, q[e]);
-            return;
-        }
+        static_assert(GN_COLUMNS / 8 <= 32, "a tile of several blocks has rows side by side in a wavefront");
         V v[8];      // of s in the first half of the wavefront, of q in the second
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = half_sums<32>(s[e], q[e]);
@@ -294,11 +289,6 @@ __device__ __forceinline__ void write_part(const GnArgs& A, const Tile& T, int c
 }
 __device__ __forceinline__ void note(const GnArgs& A, int chunk, int goes_on, int begins) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && chunk >= 0) A.info[chunk * 2] = goes_on, A.info[chunk * 2 + 1] = begins;
-}
-__device__ __forceinline__ float element(const char* p, int type, int64_t i) {
-    if (type == FG_F32) return ((const float*)p)[i];
-    const unsigned short v = ((const unsigned short*)p)[i];
-    return type == FG_BF16 ? __uint_as_float((unsigned int)v << 16) : (float)__builtin_bit_cast(_Float16, v);
 }
 // the block of a tile's column
 __device__ __forceinline__ int block_of(const GnArgs& A, int c) { return A.block == 1 ? c : (int)__umulhi((unsigned int)c, A.block_inverse); }
@@ -441,7 +431,7 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S)
         for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
         // a column's values are measured from its first one in these entries (MANY), all columns' from the block's
         const int first = first_row(A, k0, k1);
-        const float common = !MANY && first >= 0 ? element(A.x + (int64_t)first * A.x_stride, T_, T.c0) : 0.f;
+        const float common = !MANY && first >= 0 ? fg_element(A.x + (int64_t)first * A.x_stride, T_, T.c0) : 0.f;
         for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
             const Piece P = piece_of(A, T, i);
             float from[8];

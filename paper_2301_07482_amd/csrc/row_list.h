@@ -1,4 +1,4 @@
-// What the calls on listed rows share: the list, sums over the lanes of a row, checks of their arguments.
+// What the calls on listed rows share: the list, sums that halves of a wavefront exchange, checks of their arguments.
 #pragma once
 #include "row_types.h"
 
@@ -16,43 +16,6 @@ __device__ __forceinline__ int64_t row_at(const RowList& L, int64_t k, int64_t c
     if (k >= count) return -1;
     const int64_t r = L.rows ? L.rows[k] : k;
     return r < 0 || r >= L.n ? -1 : r;
-}
-
-// sum or maximum over the lanes of a row
-__device__ __forceinline__ double lanes_sum(double v, int lanes) {
-    for (int off = lanes >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-}
-__device__ __forceinline__ float lanes_max(float v, int lanes) {
-    for (int off = lanes >> 1; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
-}
-// the same over the wavefronts of a workgroup that share a row
-template <int WAVES>
-__device__ __forceinline__ double row_sum(double v, int lanes, double* lds) {
-    v = lanes_sum(v, lanes);
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = 0.0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += lds[w];
-    }
-    return v;
-}
-template <int WAVES>
-__device__ __forceinline__ float row_max(float v, int lanes, double* lds) {
-    v = lanes_max(v, lanes);
-    if constexpr (WAVES > 1) {
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = (float)lds[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, (float)lds[w]);
-    }
-    return v;
 }
 
 // Lanes l and l + HALF (of 64 for HALF = 32, of every 32 for 16) add up a and b between them: the first has a's sum, the other b's

@@ -54,6 +54,43 @@ __global__ __launch_bounds__(ROW_THREADS) void dropout_kernel(RowList L, int64_t
     fg_store_piece<T>(out + r * out_stride + (int64_t)c * E, f, d - c);
 }
 
+// sum or maximum over the lanes of a row
+__device__ __forceinline__ double lanes_sum(double v, int lanes) {
+    for (int off = lanes >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+}
+__device__ __forceinline__ float lanes_max(float v, int lanes) {
+    for (int off = lanes >> 1; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+}
+// the same over the wavefronts of a workgroup that share a row
+template <int WAVES>
+__device__ __forceinline__ double row_sum(double v, int lanes, double* lds) {
+    v = lanes_sum(v, lanes);
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v += lds[w];
+    }
+    return v;
+}
+template <int WAVES>
+__device__ __forceinline__ float row_max(float v, int lanes, double* lds) {
+    v = lanes_max(v, lanes);
+    if constexpr (WAVES > 1) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = (float)lds[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) v = fmaxf(v, (float)lds[w]);
+    }
+    return v;
+}
+
 struct NormArgs {
     RowList L;
     const char *x, *residual;

@@ -128,6 +128,12 @@ __device__ __forceinline__ void fg_store_piece(char* p, const float (&f)[8], int
         }
     }
 }
+// value i of a row that is known by its type's number
+__device__ __forceinline__ float fg_element(const char* p, int type, int64_t i) {
+    if (type == FG_F32) return ((const float*)p)[i];
+    const unsigned short v = ((const unsigned short*)p)[i];
+    return type == FG_BF16 ? __uint_as_float((unsigned int)v << 16) : (float)__builtin_bit_cast(_Float16, v);
+}
 // eight values of at most 448 in magnitude (or NaN) to 8 bits
 __device__ __forceinline__ void fg_store_piece_e4m3(char* p, const float (&f)[8], int left) {
     fg_u32x2 q;
