@@ -1158,7 +1158,8 @@ __device__ __forceinline__ unsigned short narrow(int type, float v) {
     return type == FG_BF16 ? __builtin_bit_cast(unsigned short, (__bf16)v) : __builtin_bit_cast(unsigned short, (_Float16)v);
 }
 
-template <int T, int BM, int BN, int WAVES_M, int WAVES_N>
+// DW: the type of dw (known when this is compiled: a branch at every store: 64 x 256 x 256 in 4 groups 23.7 us instead of 22.6)
+template <int T, int DW, int BM, int BN, int WAVES_M, int WAVES_N>
 __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(GlArgs A) {
     constexpr int WAVES = WAVES_M * WAVES_N, THREADS = 64 * WAVES;
     constexpr int STAGE = GW_ROWS * (BM + BN) * 2, LOADS = GW_ROWS * BM * 2 / 1024 / WAVES;      // of either operand
@@ -1285,8 +1286,8 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
         }
         const bool whole = W.first == 0 && W.last == W.steps_g;
         float* to_part = A.dw_part + ((int64_t)(2 * range + (W.at == range * S.per ? 0 : 1)) * tiles + tile) * BM * BN;
-        float* to_dw = (float*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
-        unsigned short* to_narrow = (unsigned short*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
+        typedef std::conditional_t<DW == FG_F32, float, unsigned short> dw_t;
+        dw_t* to_dw = (dw_t*)A.dw + (int64_t)W.g * A.d_in * A.d_out;
         int m_first = wm + 4 * half, c_first = wn + l32;      // (addresses are formed here: hoisted out of the loops they take registers those have not got)
         asm volatile("" : "+v"(m_first), "+v"(c_first));
 #pragma unroll
@@ -1300,11 +1301,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_dw_kernel(G
                     if (!whole)
                         to_part[m * BN + c] = acc[mb][nb][i];
                     else if (m0 + m < A.d_in && n0 + c < A.d_out) {
-                        const int64_t at = (int64_t)(m0 + m) * A.d_out + n0 + c;
-                        if (A.dw_type == FG_F32)
-                            to_dw[at] = acc[mb][nb][i];
+                        if constexpr (DW == FG_F32)
+                            to_dw[(int64_t)(m0 + m) * A.d_out + n0 + c] = acc[mb][nb][i];
                         else
-                            to_narrow[at] = narrow(T, acc[mb][nb][i]);
+                            to_dw[(int64_t)(m0 + m) * A.d_out + n0 + c] = narrow(T, acc[mb][nb][i]);
                     }
                 }
             }
@@ -1602,6 +1602,10 @@ template <int T, int D>
 void launch_gated_dz(const GlArgs& A, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((grouped_gated_dz_kernel<T, D>), grid, dim3(GZ_THREADS), 0, st, A);
 }
+template <int T, int DW, int BM, int BN, int WM, int WN>
+void launch_dw(const GlArgs& A, dim3 grid, hipStream_t st) {
+    hipLaunchKernelGGL((grouped_dw_kernel<T, DW, BM, BN, WM, WN>), grid, dim3(64 * WM * WN), 2 * GW_ROWS * (BM + BN) * 2 + GW_LIST * 4, st, A);
+}
 template <int BM, int ROWS, int VALUES>
 void launch_sum(const GlArgs& A, dim3 grid, hipStream_t st) {
     hipLaunchKernelGGL((grouped_dw_sum_kernel<BM, BM, ROWS, VALUES>), grid, dim3(GZ_THREADS), 0, st, A);
@@ -1647,10 +1651,10 @@ fg_status_t backward(const char* who, GlArgs& A, bool work, hipStream_t st, void
         if (A.dw) hipLaunchKernelGGL(grouped_f32_dw_kernel, grid, dim3(GF_THREADS), GF_LDS_BYTES + GW_LIST * 4, st, A);
         many ? launch_sum<128, GF_K, DS_MANY>(A, sum_grid, st) : launch_sum<128, GF_K, DS_FEW>(A, sum_grid, st);
     } else if (P.bm == 256) {
-        if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 256, 256, 2, 4>), grid, dim3(512), 2 * GW_ROWS * 512 * 2 + GW_LIST * 4, st, A);
+        if (A.dw) A.dw_type == T ? launch_dw<T, T, 256, 256, 2, 4>(A, grid, st) : launch_dw<T, FG_F32, 256, 256, 2, 4>(A, grid, st);
         many ? launch_sum<256, GW_ROWS, DS_MANY>(A, sum_grid, st) : launch_sum<256, GW_ROWS, DS_FEW>(A, sum_grid, st);
     } else {
-        if (A.dw) hipLaunchKernelGGL((grouped_dw_kernel<T, 128, 128, 2, 2>), grid, dim3(256), 2 * GW_ROWS * 256 * 2 + GW_LIST * 4, st, A);
+        if (A.dw) A.dw_type == T ? launch_dw<T, T, 128, 128, 2, 2>(A, grid, st) : launch_dw<T, FG_F32, 128, 128, 2, 2>(A, grid, st);
         many ? launch_sum<128, GW_ROWS, DS_MANY>(A, sum_grid, st) : launch_sum<128, GW_ROWS, DS_FEW>(A, sum_grid, st);
     }
     FG_LAUNCH_CHECK("grouped_dw_kernel");
