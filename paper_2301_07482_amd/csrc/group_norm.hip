@@ -26,7 +26,8 @@ constexpr int GN_RUN = 128;
 // Workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them. Three | four, fp32: 31744 x 100 in 1024
 // groups 17.2 | 22.5 us, its gradients 36.6 | 48.6, those of 777 x 88 in 9 groups 11.8 | 13.5, of 65536 x 1024 in 4 groups 281 | 295, of 100000 x 40 in 10000 groups 62 | 104;
 // rows of one block forward 30.7 | 28.2 (65536 x 128 in 4096 groups); bf16 gradients of 58982 listed rows x 1024 in 4 groups 172 | 166
-constexpr int gn_per_unit(int type, bool many, bool backward) { return type == FG_F32 && (backward || many) ? 3 : 4; }
+// (16-bit rows with fp32 gradients and several blocks: four would leave them four registers short)
+constexpr int gn_per_unit(int type, bool many, bool backward, bool mixed = false) { return (type == FG_F32 && (backward || many)) || (mixed && many) ? 3 : 4; }
 
 struct GnArgs {
     const int32_t* order;      // NULL: position k itself
@@ -324,10 +325,16 @@ __device__ __forceinline__ void put_statistics(const GnArgs& A, const Tile& T, i
     if (A.mean) A.mean[at] = mean;
     if (A.rstd) A.rstd[at] = rstd;
 }
+// Eight values' instructions are not all mixed with each other: what they hold at once would not fit the registers. A register that is spilled to memory is more than slow here:
+// the compiler has stored one inside a branch for the lanes that took it, and read it behind the branch for all
+__device__ __forceinline__ void part_of_eight() { __builtin_amdgcn_sched_barrier(0); }
 __device__ __forceinline__ void activate(int act, float (&u)[8]) {
     fg_with_act(act, [&](auto which) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = fg_act<decltype(which)::value>(u[e]);
+        for (int e = 0; e < 8; ++e) {
+            if (e == 4) part_of_eight();
+            u[e] = fg_act<decltype(which)::value>(u[e]);
+        }
     });
 }
 // slopes in place of the arguments
@@ -335,6 +342,7 @@ __device__ __forceinline__ void slopes(int act, float (&u)[8]) {
     fg_with_act(act, [&](auto which) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            if (e == 4) part_of_eight();
             float f;
             fg_act_slope<decltype(which)::value>(u[e], f, u[e]);
         }
@@ -426,7 +434,8 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S)
         double s[N] = {}, q[N] = {};
         int rows = 0, now[GN_AHEAD];
         fg_piece<T_> v[GN_AHEAD];
-        const bool held = !PARTS && k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);      // (all of a group's rows at once: they are read once)
+        // all of a group's rows at once: they are read once (not fp32 ones of one block, for which there are no registers)
+        const bool held = !PARTS && (MANY || T_ != FG_F32) && k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);
 #pragma unroll
         for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
         // a column's values are measured from its first one in these entries (MANY), all columns' from the block's
@@ -453,6 +462,7 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S)
                     fg_piece_values<T_>(v[u], f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
+                        if (e % 2 == 0) part_of_eight();
                         const double x = MANY || e >= P.twice ? (double)f[e] - (double)from[e] : 0.0;      // (MANY: a neighbour's columns are not left in the sums)
                         s[MANY ? e : 0] += x;
                         q[MANY ? e : 0] += x * x;
@@ -693,32 +703,30 @@ __device__ __forceinline__ void input_gradient(const GnArgs& A, const Tile& T, c
 
 // The first pass: a group's sums of t and t * xh by column, which give its two means and dw and db. MANY: the columns' sums over a group's rows
 // meet in LDS, a thread to a column adds them up over the chunk's groups. Else (NP pieces a thread) a thread keeps its columns' sums over all of
-// the chunk's rows, and those of a group over its columns beside them in fp64. The former are in fp32 for GN_RUN rows at most; with one piece they are added to fp64
-// sums in LDS then, with several, for which LDS has no room, to the range's in fp32 at the end of every group. (All pieces' sums in registers took 400 of them: 30000 x 2500
-// bf16 in 3000 groups 553 us, 236 so; fp32 sums in LDS 251, but 2000 x 16384 fp32 269 instead of 194, as LDS holds one workgroup then.)
+// the chunk's rows, and those of a group over its columns beside them in fp64. The former are in fp32 for GN_RUN rows of a part at most; with one piece they are added to
+// fp64 sums in LDS then, with several, for which LDS has no room, to the range's in fp32. (All pieces' sums in registers took 400 of them: 30000 x 2500 bf16 in 3000 groups
+// 553 us, 236 so; fp32 sums in LDS 251, but 2000 x 16384 fp32 269 instead of 194, as LDS holds one workgroup then.)
 template <int TH, int X, int G, bool MANY, int NP, bool PARTS>
 __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>& S, double* kept) {
     const Tile T = tile_of<TH>(A);
     const int chunk = (int)blockIdx.y - A.workers;      // (below 0: whole groups)
     int goes_on = -1, begins = -1, g, which;
     unsigned int k0, k1;
-    constexpr int MINE = GN_COLUMNS / TH;      // MANY: columns whose sums a thread has
-    double dw[MINE] = {}, db[MINE] = {};
+    if constexpr (MANY)      // a thread has every TH-th column (in registers they would be spilled)
+        for (int c = threadIdx.x; c < GN_COLUMNS; c += TH) kept[c] = kept[GN_COLUMNS + c] = 0.0;
     constexpr int KEPT = TH + 8;      // (a thread's sums lie so far apart; eight more, so that a column's reader finds its neighbours' in other banks)
-    float dw_piece[8] = {}, db_piece[8] = {};
-    int since = 0;              // rows in them
     unsigned int there = 0;     // pieces of which something has been kept
     float* const range = A.columns ? A.columns + (int64_t)blockIdx.y * 2 * A.d + T.c0 : nullptr;
     // a piece's sums to LDS, or to the range's
-    const auto keep = [&](int i, const Piece& P) {
+    const auto keep = [&](int i, const Piece& P, const float (&dw)[8], const float (&db)[8]) {
         const bool more = there >> i & 1;
         there |= 1u << i;
         if constexpr (NP == 1) {
             double* const at = kept + threadIdx.x;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                at[e * KEPT] = (more ? at[e * KEPT] : 0.0) + (double)dw_piece[e];
-                at[(8 + e) * KEPT] = (more ? at[(8 + e) * KEPT] : 0.0) + (double)db_piece[e];
+                at[e * KEPT] = (more ? at[e * KEPT] : 0.0) + (double)dw[e];
+                at[(8 + e) * KEPT] = (more ? at[(8 + e) * KEPT] : 0.0) + (double)db[e];
             }
         } else if (range) {
 #pragma unroll
@@ -727,17 +735,15 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
                 float f[8] = {};
                 if (more) fg_piece_values<FG_F32>(load_piece<FG_F32>(at, P.c), f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] += sum ? db_piece[e] : dw_piece[e];
+                for (int e = 0; e < 8; ++e) f[e] += sum ? db[e] : dw[e];
                 store_piece<FG_F32>(at, P, f);
             }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) dw_piece[e] = db_piece[e] = 0.f;
     };
     for (Walk<PARTS> W(A, blockIdx.y); W.next(g, k0, k1, which);) {
         if (k0 == k1) continue;
         GradRows<X, G> R;
-        const bool held = !PARTS && k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
+        const bool held = X == G && !PARTS && k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
 #pragma unroll
         for (int u = 0; u < GN_AHEAD_BW; ++u) R.now[u] = -1;
         int rows = 0;
@@ -759,12 +765,6 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
             }
         } else {
             double s[1] = {}, q[1] = {};
-            const int mine = (int)((k1 - k0 + T.sides - 1) / T.sides);      // a thread's rows
-            if (NP == 1 && since + mine > GN_RUN) {
-                keep(0, piece_of(A, T, 0));
-                since = 0;
-            }
-            since = mine < GN_RUN ? since + mine : GN_RUN;
             for (int i = 0; i < (NP == 1 ? 1 : A.pieces); ++i) {
                 const Piece P = piece_of(A, T, i);
                 if (!P.there) break;
@@ -772,17 +772,17 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
                 grad_columns<false, false>(A, T, g, P.c, C);
                 for (unsigned int from = k0, to; from < k1; from = to) {
                     to = k1 - from > (unsigned int)(GN_RUN * T.sides) ? from + GN_RUN * T.sides : k1;
-                    if (NP == 1 && from != k0) keep(0, P);
+                    float dw[8] = {}, db[8] = {};
                     gradient_rows<X, G, false>(A, T, P.c, C, from, to, false, R, [&](int, const float(&xh)[8], const float(&t)[8]) {
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             if (e < P.twice) continue;
                             const double a = (double)(t[e] * C.w[e]);
                             s[0] += a, q[0] += a * (double)xh[e];
-                            dw_piece[e] += t[e] * xh[e], db_piece[e] += t[e];
+                            dw[e] += t[e] * xh[e], db[e] += t[e];
                         }
                     });
-                    if (NP > 1) keep(i, P);
+                    keep(i, P, dw, db);
                 }
             }
             leave_sums<TH, false>(A, T, S, s, q, rows);
@@ -790,14 +790,11 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
         __syncthreads();
         rows = rows_of(A, S);
         if constexpr (MANY)      // (rstd is still missing from the sums of t * xh)
-#pragma unroll
-            for (int i = 0; i < MINE; ++i) {
-                const int c = (int)threadIdx.x + TH * i;
-                if (c >= T.cols) continue;
+            for (int c = threadIdx.x; c < T.cols; c += TH) {
                 double s = 0.0, q = 0.0;
 #pragma unroll
                 for (int w = 0; w < TH / 64; ++w) s += S.wave[w][c], q += S.wave[w][GN_COLUMNS + c];
-                db[i] += s, dw[i] += q * (double)given(A, T, A.rstd, g, block_of(A, c));
+                kept[GN_COLUMNS + c] += s, kept[c] += q * (double)given(A, T, A.rstd, g, block_of(A, c));
             }
         block_sums<TH, MANY>(
             A, T, S,
@@ -822,20 +819,14 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
     if constexpr (PARTS) note(A, chunk, goes_on, begins);
     if (!range) return;
     if constexpr (MANY) {
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-            const int c = (int)threadIdx.x + TH * i;
-            if (c < T.cols) range[c] = (float)dw[i], range[A.d + c] = (float)db[i];
-        }
+        for (int c = threadIdx.x; c < T.cols; c += TH) range[c] = (float)kept[c], range[A.d + c] = (float)kept[GN_COLUMNS + c];
     } else {
-        if constexpr (NP > 1) {
-            for (int i = 0; i < A.pieces; ++i) {
-                const Piece P = piece_of(A, T, i);
-                if (P.there && !(there >> i & 1)) keep(i, P);
-            }
-            return;
+        const float none[8] = {};
+        for (int i = 0; i < A.pieces; ++i) {
+            const Piece P = piece_of(A, T, i);
+            if ((NP == 1 || P.there) && !(there >> i & 1)) keep(i, P, none, none);
         }
-        keep(0, piece_of(A, T, 0));
+        if constexpr (NP > 1) return;
         __syncthreads();
         for (int c = threadIdx.x; c < T.cols; c += TH) {      // rows side by side: their sums meet
             const int p = c / 8, e = c - (p * 8 + 8 <= T.cols ? p * 8 : T.cols - 8);
@@ -847,9 +838,9 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
     }
 }
 template <int TH, int X, int G, bool MANY, int NP>
-__global__ __launch_bounds__(TH, NP > 1 ? 1 : gn_per_unit(X, MANY, true)) void group_norm_backward_kernel(GnArgs A) {
+__global__ __launch_bounds__(TH, NP > 1 ? 1 : gn_per_unit(X, MANY, true, X != G)) void group_norm_backward_kernel(GnArgs A) {
     __shared__ Scratch<TH, MANY> S;
-    __shared__ double kept[MANY || NP > 1 ? 1 : 16 * (TH + 8)];
+    __shared__ double kept[MANY ? 2 * GN_COLUMNS : NP > 1 ? 1 : 16 * (TH + 8)];
     if ((int)blockIdx.y < A.workers)
         gradient_body<TH, X, G, MANY, NP, false>(A, S, kept);
     else
@@ -881,7 +872,7 @@ struct Plan {
     int64_t rows, chunks, long_rows;      // chunks 0: no group can be so large that it is split
     bool join_there;
 };
-Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks, int type, bool backward) {
+Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks, int type, bool backward, bool mixed = false) {
     Plan P;
     const int block = d / blocks, per_tile = GN_COLUMNS / block;
     P.tiles = (int)fg_ceil_div(blocks, per_tile < 1 ? 1 : per_tile);
@@ -892,7 +883,7 @@ Plan plan_of(int64_t max_rows, int n_groups, int d, int blocks, int type, bool b
         cols = P.tile_blocks * block, pieces = (int)fg_ceil_div(cols, 8);
         P.width = 1;
         while (P.width < pieces && P.width < GN_THREADS) P.width *= 2;
-        places = GN_UNITS * gn_per_unit(type, P.tile_blocks > 1, backward) / P.tiles, least = 2 * (GN_THREADS / P.width);
+        places = GN_UNITS * gn_per_unit(type, P.tile_blocks > 1, backward, mixed) / P.tiles, least = 2 * (GN_THREADS / P.width);
         if (P.tiles * 2 > blocks || blocks / (P.tiles * 2) * block < 8 || (max_rows / least + n_groups) * P.tiles > GN_FEW_WORKGROUPS) break;
     }
     P.pieces = (int)fg_ceil_div(pieces, P.width);
@@ -1066,7 +1057,7 @@ extern "C" fg_status_t fg_group_norm_backward(const void* dy, int64_t dy_stride,
     const Space W = space_of(max_rows, n_groups, d, channel_groups, true);
     FG_TRY(check_space(who, ws_dev, ws_bytes, W.total()));
     fg_clear_error();
-    const Plan P = plan_of(max_rows, n_groups, d, channel_groups, dtype, true);
+    const Plan P = plan_of(max_rows, n_groups, d, channel_groups, dtype, true, grad_dtype != dtype);
     GnArgs A = args_of(P, W, order_dev, offsets_dev, work ? max_rows : 0, n_groups, n, d, channel_groups, ws_dev);
     A.x = (const char*)x, A.x_stride = x_stride, A.dy = (const char*)dy, A.dy_stride = dy_stride, A.out = (char*)dx, A.out_stride = dx_stride, A.weight = weight, A.bias = bias;
     A.act = act, A.mean = const_cast<float*>(mean), A.rstd = const_cast<float*>(rstd);
