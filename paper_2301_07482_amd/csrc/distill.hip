@@ -348,11 +348,10 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
 
 // Wide rows: WAVES wavefronts to a row, one row to a workgroup. NP pieces of eight columns a lane in registers; TAIL: there are more. Pieces are counted from the 16-byte
 // line that the row begins in, so that all but the first and the last of them are whole lines (rows of 50003 bf16 15 % faster). An entry is in a lane of every wavefront, which
-// finds those of its own pieces. Sums are in fp64 from a lane's pieces on (exchanged between registers, both softmaxes' at once). Five wavefronts to a SIMD where a 16-bit row's
-// pieces leave room, both in us (five | four): 20000 x 16384 271 | 291, 4096 x 8000 41.7 | 42.6, 8192 x 50003 456 to 465 | 459 to 463; losses alone the other way, 225 | 163 for
-// 8192 x 50000.
+// finds those of its own pieces. Sums are in fp64 from a lane's pieces on (exchanged between registers, both softmaxes' at once).
+// Four wavefronts to a SIMD: with five, 16-bit rows of several wavefronts had to spill registers (20000 x 16384 271 us, four 290; 4096 x 32000 154, four 139).
 template <int T, int WAVES, int NP, bool TAIL>
-__global__ __launch_bounds__(WAVES * 64, T != FG_F32 && !TAIL ? 5 : 4) void distill_wide_kernel(DistillArgs A) {
+__global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs A) {
     constexpr int E = T == FG_F32 ? 4 : 2, WIDTH = WAVES * 64;
     __shared__ double red[2][WAVES];
     __shared__ float largest[WAVES];

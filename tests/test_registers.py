@@ -52,7 +52,7 @@ def spilled():
     return found
 
 
-@pytest.mark.parametrize("part", ["group_norm"])
+@pytest.mark.parametrize("part", ["group_norm", "distill"])
 def test_no_kernel_spills_vector_registers(spilled, part):
     of_part = {name: n for name, n in spilled.items() if part in name}
     assert of_part
