@@ -324,21 +324,26 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
     // different banks
     auto b_window = [](int row) { return T == FG_F32 ? (row >> 2) & 1 : BN >= 128 ? row & 3 : (row >> 1) & 1; };
     auto begin = [&](const Tile& F, const TileData& D) {
+        // (the lane's own places in a step are formed here and in `load_step`'s last one: held over the tiles, as the compiler would do, they take
+        // registers that fp32 has not got)
+        int own = lane;
+        if constexpr (T == FG_F32) asm volatile("" : "+v"(own));
+        const int own_row = GL_ROWS * wave + own / GL_PIECES, own_piece = (own % GL_PIECES) ^ exchanged(own_row);
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) {
-            const int32_t r = D.src[a_row + GL_ROWS * WAVES * i];
-            pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + a_piece * 16;
+            const int32_t r = D.src[own_row + GL_ROWS * WAVES * i];
+            pa[i] = A.a + (int64_t)(r >= 0 ? r : 0) * A.a_stride + own_piece * 16;
         }
         w_at = A.W + ((int64_t)F.g * N + (B_KN ? 0 : F.n0)) * K * E;      // (a column tile begins below N)
 #pragma unroll
         for (int i = 0; i < B_LOADS; ++i) {
             if constexpr (B_KN) {
-                const int at = 64 * (wave + WAVES * i) + lane, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
+                const int at = 64 * (wave + WAVES * i) + own, row = at / B_ROW_PIECES, slot = at % B_ROW_PIECES;
                 const int c = T == FG_F32 ? (((slot >> 3) ^ b_window(row)) * 8 + (slot & 7)) * 4 : (((slot >> 2) ^ b_window(row)) * 4 + (slot & 3)) * 8;
                 pb[i] = (unsigned int)(row * N + column(F, c, 0)) * E;
             } else {
-                const int c = F.n0 + a_row + GL_ROWS * WAVES * i;
-                pb[i] = (unsigned int)(c < N ? c - F.n0 : 0) * K * E + a_piece * 16;
+                const int c = F.n0 + own_row + GL_ROWS * WAVES * i;
+                pb[i] = (unsigned int)(c < N ? c - F.n0 : 0) * K * E + own_piece * 16;
             }
         }
     };
@@ -355,10 +360,12 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
 #pragma unroll
             for (int i = 0; i < B_LOADS; ++i) load_to_lds(w, pb[i], to + BM * GL_STEP + i * WAVES * 1024);
         } else {
+            int own = lane;
+            if constexpr (T == FG_F32 && B_KN) asm volatile("" : "+v"(own));
 #pragma unroll
             for (int i = 0; i < A_LOADS; ++i) load_to_lds(ka < left ? pa[i] : zero, to + i * WAVES * 1024);
 #pragma unroll
-            for (int i = 0; i < B_LOADS; ++i) load_to_lds((B_KN ? (64 * (wave + WAVES * i) + lane) / B_ROW_PIECES : ka) < left ? w_at + pb[i] : zero, to + BM * GL_STEP + i * WAVES * 1024);
+            for (int i = 0; i < B_LOADS; ++i) load_to_lds((B_KN ? (64 * (wave + WAVES * i) + own) / B_ROW_PIECES : ka) < left ? w_at + pb[i] : zero, to + BM * GL_STEP + i * WAVES * 1024);
         }
 #pragma unroll
         for (int i = 0; i < A_LOADS; ++i) pa[i] += GL_STEP;
