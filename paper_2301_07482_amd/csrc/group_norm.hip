@@ -4,9 +4,9 @@
 // from registers where the group is small enough, else from the caches. A group of many rows is split: the entries of all groups are a line that is cut into
 // chunks of rows, every chunk's workgroup leaves the sums of its part, a second launch goes over the rows again with what all parts come to. A workgroup takes a tile of
 // whole blocks of columns; a thread has pieces of eight adjacent columns (whole ones: the last of a tile overlaps the one before it) and every so many-th row.
-// Bound by memory where rows are many: 58982 listed rows x 1024 bf16 in 4 groups 98 us (sums 29, result 49, both of what a copy would take), gradients 166 (73, sums 5, 72).
-// Many small groups are bound by what their reductions take beside their values (31744 x 100 fp32 in 1024 groups 17 us, 29 with cold caches, of 5 for the bytes), few rows by the
-// latency of reads that depend on each other (777 x 88 6.0, gradients 11.8).
+// Bound by memory where rows are many: 58982 listed rows x 1024 bf16 in 4 groups 76 us between calls of the same rows (48 for the bytes; statistics come before results, so the
+// rows are read twice), gradients 130 of 73; 65536 x 1024 fp32 168 and 280. Many small groups are bound by what their reductions take beside their values (31744 x 100 fp32 in
+// 1024 groups 16 us, 29 with cold caches, of 5 for the bytes), few rows by the latency of reads that depend on each other (777 x 88 6, gradients 10.8).
 #include "activation.h"
 #include "row_list.h"
 #include "row_types.h"
@@ -17,15 +17,14 @@ namespace {
 constexpr int GN_THREADS = 256, GN_COLUMNS = 256;      // columns of a tile that has several blocks
 constexpr int GN_PLACES = 1024, GN_UNITS = 256, GN_MOST_WORKERS = 12 * GN_UNITS, GN_FEW_WORKGROUPS = 128, GN_SMALL_STEPS = 2, GN_FEW_VALUES = 65536, GN_LEAST_VALUES = 24576;
 constexpr int GN_JOIN_HERE = 4000, GN_MAX_PIECES = 8;
-// Rows of a thread whose reads are on their way together. Two | one: forward 17.2 | 18.3 us for 31744 x 100 in 1024 groups, 24.6 | 26.5 for 100000 x 40 in 10000 groups,
-// 27.6 | 25.6 for 65536 x 128 in 4096 groups; gradients, which have two arrays to read, 39.7 | 37.0 and 71 | 62 for the first two
-constexpr int GN_AHEAD = 2, GN_AHEAD_BW = 1;
 // Rows of a thread whose fp32 sums (the gradients', several blocks to a tile) are joined to fp64 ones: what is lost of them stays below 2^-17 however long a call is
 constexpr int GN_RUN = 128;
 
-// Workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them. Three | four, fp32: 31744 x 100 in 1024
-// groups 17.2 | 22.5 us, its gradients 36.6 | 48.6, those of 777 x 88 in 9 groups 11.8 | 13.5, of 65536 x 1024 in 4 groups 281 | 295, of 100000 x 40 in 10000 groups 62 | 104;
-// rows of one block forward 30.7 | 28.2 (65536 x 128 in 4096 groups); bf16 gradients of 58982 listed rows x 1024 in 4 groups 172 | 166
+// Workgroups of the first pass that a compute unit holds: three of those that need more registers than a fourth one would leave them. Three | four, us. fp32, several blocks:
+// 31744 x 100 in 1024 groups 17.4 | 20.3, 100000 x 40 in 10000 groups 26 | 31, 200000 x 64 in 20000 groups 42 | 56, but 20000 x 256 in 40 groups 24 | 22; its gradients 36.2 | 35.7,
+// 59 | 63, 84 | 92 and 35 | 33, of 65536 x 1024 in 4 groups 280 | 277; forward with one block 26 | 26 (65536 x 128 in 4096 groups). 16 bits: 65536 x 1024 in 4 groups 82 | 78, gathered
+// 89 | 82, with one block 77 | 75, 8000 x 2048 in 256 blocks 48 | 31, but 31744 x 100 16 | 17 and 100000 x 40 25 | 27; gradients 146 | 143, gathered 170 | 155, with one block
+// 164 | 153, 8000 x 2048 44 | 43, 100000 x 40 57 | 62.
 // (16-bit rows with fp32 gradients and several blocks: four would leave them four registers short)
 constexpr int gn_per_unit(int type, bool many, bool backward, bool mixed = false) { return (type == FG_F32 && (backward || many)) || (mixed && many) ? 3 : 4; }
 
@@ -355,33 +354,25 @@ __device__ __forceinline__ void affine(const GnArgs& A, const Tile& T, int c, fl
     if (A.bias) fg_piece_values<FG_F32>(load_piece<FG_F32>((const char*)A.bias, T.c0 + c), b);
 }
 
-// The rows of the entries [k0, k1) that this thread has, AHEAD at a time: load(set, row or -1) for all of them, then use(set, row) for each that exists; `now`: the rows of the last sets.
-// The next positions are fetched beside the rows.
-template <int AHEAD, typename Load, typename Use>
-__device__ __forceinline__ void for_rows(const GnArgs& A, const Tile& T, unsigned int k0, unsigned int k1, int (&now)[AHEAD], const Load& load, const Use& use) {
-    int r[AHEAD];
-    const auto fetch = [&](unsigned int k) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) r[u] = k + u * T.sides < k1 ? position(A, k + u * T.sides) : -1;
-    };
-    fetch(k0 + T.side);
-    for (unsigned int k = k0 + T.side; k < k1; k += AHEAD * T.sides) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            now[u] = r[u];
-            load(u, now[u]);
-        }
-        fetch(k + AHEAD * T.sides);
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (now[u] >= 0) use(u, now[u]);
+// The rows of the entries [k0, k1) that this thread has: load(row or -1), then use(row) if it exists; `now`: the last one. The next position is fetched beside the row.
+// (Two rows on their way: forward 17.5 us for 31744 x 100 fp32 in 1024 groups, one 16.0; 65536 listed rows x 1024 bf16 in 4 groups 82 | 80, with one block 81 | 76; only
+// 200000 x 64 fp32 in 20000 groups 42 | 44; gradients of the first three 37.0 | 36.0, 163 | 155, 167 | 161.)
+template <typename Load, typename Use>
+__device__ __forceinline__ void for_rows(const GnArgs& A, const Tile& T, unsigned int k0, unsigned int k1, int& now, const Load& load, const Use& use) {
+    const auto fetch = [&](unsigned int k) { return k < k1 ? position(A, k) : -1; };
+    int next = fetch(k0 + T.side);
+    for (unsigned int k = k0 + T.side; k < k1; k += T.sides) {
+        now = next;
+        load(now);
+        next = fetch(k + T.sides);
+        if (now >= 0) use(now);
     }
 }
 
-// y of the entries [k0, k1) with the blocks' mean and rstd in S.stats. held: the sets `now`, v are all of them and there already
+// y of the entries [k0, k1) with the blocks' mean and rstd in S.stats. held: `now`, v are all of them and there already
 template <int TH, int T_, bool MANY>
-__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch<TH, MANY>& S, unsigned int k0, unsigned int k1, bool held, int (&now)[GN_AHEAD],
-                                          fg_piece<T_> (&v)[GN_AHEAD]) {
+__device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const Scratch<TH, MANY>& S, unsigned int k0, unsigned int k1, bool held, int& now,
+                                          fg_piece<T_>& v) {
     for (int i = 0; i < (MANY ? 1 : A.pieces); ++i) {
         const Piece P = piece_of(A, T, i);
         if (!P.there) break;
@@ -390,9 +381,9 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
         stats_of<TH, MANY>(A, S, P.c, mean, rstd);
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] *= rstd[e];
-        const auto finish = [&](int u, int r) {
+        const auto finish = [&](int r) {
             float f[8];
-            fg_piece_values<T_>(v[u], f);
+            fg_piece_values<T_>(v, f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = (f[e] - mean[e]) * w[e] + b[e];
             activate(A.act, f);
@@ -403,14 +394,12 @@ __device__ __forceinline__ void normalise(const GnArgs& A, const Tile& T, const 
                 store_piece<T_>(to + T.c0 * 2, P, f);
         };
         if (held) {
-#pragma unroll
-            for (int u = 0; u < GN_AHEAD; ++u)
-                if (now[u] >= 0) finish(u, now[u]);
+            if (now >= 0) finish(now);
         } else {
-            for_rows<GN_AHEAD>(
+            for_rows(
                 A, T, k0, k1, now,
-                [&](int u, int r) {
-                    if (r >= 0) v[u] = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
+                [&](int r) {
+                    if (r >= 0) v = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
                 },
                 finish);
         }
@@ -432,12 +421,10 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S)
             continue;
         }
         double s[N] = {}, q[N] = {};
-        int rows = 0, now[GN_AHEAD];
-        fg_piece<T_> v[GN_AHEAD];
+        int rows = 0, now = -1;
+        fg_piece<T_> v;
         // all of a group's rows at once: they are read once (not fp32 ones of one block, for which there are no registers)
-        const bool held = !PARTS && (MANY || T_ != FG_F32) && k1 - k0 <= GN_AHEAD * T.sides && (MANY || A.pieces == 1);
-#pragma unroll
-        for (int u = 0; u < GN_AHEAD; ++u) now[u] = -1;
+        const bool held = !PARTS && (MANY || T_ != FG_F32) && k1 - k0 <= (unsigned int)T.sides && (MANY || A.pieces == 1);
         // a column's values are measured from its first one in these entries (MANY), all columns' from the block's
         const int first = first_row(A, k0, k1);
         const float common = !MANY && first >= 0 ? fg_element(A.x + (int64_t)first * A.x_stride, T_, T.c0) : 0.f;
@@ -451,15 +438,15 @@ __device__ __forceinline__ void norm_body(const GnArgs& A, Scratch<TH, MANY>& S)
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if (e >= P.twice) S.from[P.c + e] = from[e];
-            for_rows<GN_AHEAD>(
+            for_rows(
                 A, T, k0, k1, now,
-                [&](int u, int r) {
+                [&](int r) {
                     rows += r >= 0 && i == 0;
-                    if (r >= 0) v[u] = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
+                    if (r >= 0) v = load_piece<T_>(A.x + (int64_t)r * A.x_stride, T.c0 + P.c);
                 },
-                [&](int u, int) {
+                [&](int) {
                     float f[8];
-                    fg_piece_values<T_>(v[u], f);
+                    fg_piece_values<T_>(v, f);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         if (e % 2 == 0) part_of_eight();
@@ -612,8 +599,8 @@ __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_apply_kernel(GnArgs 
     __shared__ Scratch<GN_THREADS, MANY> S;
     const Tile T = tile_of<GN_THREADS>(A);
     split_parts<T_, MANY, false>(A, T, S, [&](int, unsigned int k0, unsigned int k1) {
-        int now[GN_AHEAD];
-        fg_piece<T_> v[GN_AHEAD];
+        int now = -1;
+        fg_piece<T_> v;
         normalise<GN_THREADS, T_, MANY>(A, T, S, k0, k1, false, now, v);
     });
 }
@@ -642,21 +629,21 @@ __device__ __forceinline__ void grad_columns(const GnArgs& A, const Tile& T, int
         if (FOLDED) C.w[e] *= C.rstd[e];
     }
 }
-// rows on their way, or held
+// a row on its way, or held
 template <int X, int G>
 struct GradRows {
-    int now[GN_AHEAD_BW];
-    fg_piece<X> x[GN_AHEAD_BW];
-    fg_piece<G> dy[GN_AHEAD_BW];
+    int now = -1;
+    fg_piece<X> x;
+    fg_piece<G> dy;
 };
 // use(row, xh, t) for every row of the entries [k0, k1) that this thread has (FOLDED: use(row, x - mean, t)); held: R has all of them already
 template <int X, int G, bool FOLDED, typename Use>
 __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, int c, const GradColumns& C, unsigned int k0, unsigned int k1, bool held, GradRows<X, G>& R,
                                               const Use& use) {
-    const auto terms = [&](int u, int r) {
+    const auto terms = [&](int r) {
         float xh[8], t[8], slope[8];
-        fg_piece_values<X>(R.x[u], xh);
-        fg_piece_values<G>(R.dy[u], t);
+        fg_piece_values<X>(R.x, xh);
+        fg_piece_values<G>(R.dy, t);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             xh[e] -= C.mean[e];
@@ -669,16 +656,14 @@ __device__ __forceinline__ void gradient_rows(const GnArgs& A, const Tile& T, in
         use(r, xh, t);
     };
     if (held) {
-#pragma unroll
-        for (int u = 0; u < GN_AHEAD_BW; ++u)
-            if (R.now[u] >= 0) terms(u, R.now[u]);
+        if (R.now >= 0) terms(R.now);
     } else {
-        for_rows<GN_AHEAD_BW>(
+        for_rows(
             A, T, k0, k1, R.now,
-            [&](int u, int r) {
+            [&](int r) {
                 if (r < 0) return;
-                R.x[u] = load_piece<X>(A.x + (int64_t)r * A.x_stride, T.c0 + c);
-                R.dy[u] = load_piece<G>(A.dy + (int64_t)r * A.dy_stride, T.c0 + c);
+                R.x = load_piece<X>(A.x + (int64_t)r * A.x_stride, T.c0 + c);
+                R.dy = load_piece<G>(A.dy + (int64_t)r * A.dy_stride, T.c0 + c);
             },
             terms);
     }
@@ -743,9 +728,7 @@ __device__ __forceinline__ void gradient_body(const GnArgs& A, Scratch<TH, MANY>
     for (Walk<PARTS> W(A, blockIdx.y); W.next(g, k0, k1, which);) {
         if (k0 == k1) continue;
         GradRows<X, G> R;
-        const bool held = X == G && !PARTS && k1 - k0 <= GN_AHEAD_BW * T.sides && (MANY || A.pieces == 1);
-#pragma unroll
-        for (int u = 0; u < GN_AHEAD_BW; ++u) R.now[u] = -1;
+        const bool held = X == G && !PARTS && k1 - k0 <= (unsigned int)T.sides && (MANY || A.pieces == 1);
         int rows = 0;
         for (unsigned int k = k0 + T.side; k < k1; k += T.sides) rows += position(A, k) >= 0;
         if constexpr (MANY) {
@@ -858,15 +841,20 @@ __global__ __launch_bounds__(GN_THREADS, 4) void group_norm_backward_apply_kerne
 }
 
 // How a call is cut: whole blocks of up to GN_COLUMNS columns to a tile, or one wider block. Where there are few groups and rows (fewer than GN_FEW_WORKGROUPS workgroups), tiles
-// of fewer blocks (777 x 88 in 9 groups, 8 blocks: 6.0 us, 11.3 without; 2000 rows 6.4, 16.4).
+// of fewer blocks (limits of 32 | 128 | 512: 777 x 88 fp32 in 9 groups 11.5 | 6.1 | 5.9 us, 2000 x 88 17.5 | 6.6 | 6.5, 500 x 512 bf16 in 4 groups 20 | 6 | 6, 2000 x 256 in 2 groups
+// 15.8 | 15.2 | 13.1; their gradients 17.6 | 10.8 | 10.8, 26 | 12.6 | 12.6, 19 | 11 | 11, 17.5 | 19.2 | 17.8; those of 5000 x 88 19.1 | 19.1 | 20.4).
+// Up to GN_MOST_WORKERS workgroups take whole groups in turn, four times as many as are on the chip (6 | 12 | 24 times the units: 100000 x 40 fp32 in 10000 groups 37 | 26 | 26 us,
+// 300000 x 32 in 50000 groups 147 | 85 | 85, 200000 x 64 in 20000 groups 70 | 42 | 44; gradients, for which each leaves sums of dw and db, 66 | 59 | 77, 192 | 127 | 146, 112 | 84 | 104;
+// those of 65536 x 128 in one block and 4096 groups 52 | 62 | 69).
 // A group is not split as long as its workgroup, alone with its tile, ends with the others: up to GN_FEW_VALUES values in a tile where the groups fill the chip, fewer where
-// they do not, down to GN_LEAST_VALUES (with | without: 5000 x 88 in 9 groups 16 | 32 us, gradients 19 | 53; 20000 x 256 in 40 groups 25 | 61, gradients 38 | 117; a
-// limit of 16384 values has 2000 x 88 in 9 groups wait for launches that have nothing to do, 8.8 against 6.4). If no group of max_rows rows can be split, the launches for the parts are left out.
+// they do not, down to GN_LEAST_VALUES. Split | whole: 5000 x 88 in 9 groups 16 | 32 us, gradients 19 | 53; 20000 x 256 in 40 groups 24 | 61, gradients 35 | 117. With no limit 777 x 88
+// in 9 groups, whose launches for the parts then have nothing to do, takes 8.8 us instead of 6.1, gradients 12.7 instead of 10.8; with one of 16384 values 2000 x 88 8.6 instead of
+// 6.6. If no group of max_rows rows can be split, the launches for the parts are left out.
 // Chunks of rows for the split groups, with two rows a thread at least, so that all workgroups are on the chip at once (a few of them in a second turn take as long as all
 // the others). Their sums are joined in a launch of its own from GN_JOIN_HERE chunks and blocks on, else by every workgroup of the second pass for itself: 8000 x 2048
-// bf16 in 256 blocks 30 us against 44, 65536 x 256 in 8 blocks 43 against 46; 31744 x 100 in 5 blocks 18.8 against 17.2, 65536 x 256 in one block 40.9 against 38.6.
-// One wavefront to a workgroup where an average group's rows are up to GN_SMALL_STEPS steps of one: 50000 x 32 in 20000 groups 35 us against 125, gradients 67 against 166;
-// at eight steps (31 rows x 100) 53 against 25.
+// bf16 in 256 blocks 31 us against 46, 65536 x 256 in 8 blocks 32.6 against 36; 31744 x 100 in 5 blocks 19.1 against 17.5, 65536 x 256 in one block 41.4 against 39.5.
+// One wavefront to a workgroup where an average group's rows are up to GN_SMALL_STEPS steps of one: 50000 x 32 in 20000 groups 35 us against 122, gradients 63 against 174;
+// up to eight steps: 65536 x 128 in one block and 4096 groups 21 against 26, gradients 58 against 62, but 2000 x 88 in 9 groups 9.5 against 6.6, gradients 17 against 12.6.
 struct Plan {
     int tiles, tile_blocks, width, pieces, threads, workers;
     int64_t rows, chunks, long_rows;      // chunks 0: no group can be so large that it is split
