@@ -567,12 +567,16 @@ void distill(const DistillArgs& A, hipStream_t st) {
     if (A.d <= 128) return launch_narrow<T, 16>(A, st);
     if (A.d <= 256) return launch_narrow<T, 32>(A, st);
     if (A.d <= DL_NARROW) return launch_narrow<T, 64>(A, st);
-    // One wavefront to a row where that holds it (what it does beside the row's values takes as long as some hundred of them), four where rows are few. Both in us, bf16 with 16
-    // entries: 2048 x 2000 9.0 | 9.6, 16384 x 2000 39 | 47; 2048 x 4000 17 | 13, 16384 x 4000 74 | 69, 54000 x 4000 210 | 216; 2048 x 8000 28 | 24, 4096 x 8000 40 | 40, 54000 x 8000 393 | 437
+    // One wavefront to a row where that holds it (what it does beside the row's values takes as long as some hundred of them), four where rows are few. One | four, us with 16
+    // entries, bf16: 2048 x 2000 9.0 | 9.8, 16384 x 2000 38 | 48; 2048 x 4000 17 | 13, 16384 x 4000 74 | 70, 54000 x 4000 211 | 216; 2048 x 8000 27 | 25, 4096 x 8000 40 | 40,
+    // 8192 x 8000 76 | 83. fp32: 2048 x 1000 8.2 | 9.6, 54000 x 1000 91 | 148, 2048 x 2000 11.5 | 11.8, 54000 x 2000 168 | 186; 2048 x 4000 19 | 17, 16384 x 3000 89 | 82,
+    // 54000 x 3000 260 | 254, x 4000 341 | 320: four as soon as a row takes more than four pieces a lane. Sixteen for what four do not hold: four | sixteen, fp32: 8192 x 8000 103 | 184,
+    // x 16000 203 | 260; bf16 8192 x 16000 128 | 152.
     constexpr int MOST = T == FG_F32 ? 8 : 16;
     if (pieces <= 256) return launch_wide<T, 1, 4, false>(A, st);
-    if (pieces <= 512 && A.L.max_rows <= DL_FEW_ROWS) return launch_wide<T, 4, 2, false>(A, st);
-    if (pieces <= 64 * MOST && A.L.max_rows > DL_FEW_ROWS / 4) return launch_wide<T, 1, MOST, false>(A, st);
+    if (pieces <= 512 && (T == FG_F32 || A.L.max_rows <= DL_FEW_ROWS)) return launch_wide<T, 4, 2, false>(A, st);
+    if constexpr (T != FG_F32)
+        if (pieces <= 64 * MOST && A.L.max_rows > DL_FEW_ROWS / 4) return launch_wide<T, 1, MOST, false>(A, st);
     if (pieces <= 256 * MOST) return launch_wide<T, 4, MOST, false>(A, st);
     if (pieces <= 8192) return launch_wide<T, 128 / MOST, MOST, false>(A, st);
     launch_wide<T, 128 / MOST, MOST, true>(A, st);
