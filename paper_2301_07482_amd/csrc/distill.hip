@@ -209,7 +209,7 @@ __device__ __forceinline__ void share_out(float* all, int at, float share, int l
 }
 
 // Narrow rows: 64 / LANES of them to a wavefront, eight columns to a lane. A row's values lie in LDS for its entries to find theirs, then what those take from its
-// gradient. Bound by memory and, nearly as long, by what a wavefront does beside its values: 54067 x 256 fp32 26 us (4.3 TB/s; without teacher and labels 17), 32 with the
+// gradient. Bound by memory and, nearly as long, by what a wavefront does beside its values: 54067 x 256 fp32 24 us (4.6 TB/s; without teacher and labels 17; bf16 21, 54067 x 512 bf16 37), 32 with the
 // lanes a number of the call's; two and four pieces a lane, for more rows to a wavefront, 28 and 30.
 struct Entry {
     int32_t c;      // class, -1: none
@@ -349,6 +349,7 @@ __global__ __launch_bounds__(DL_THREADS) void distill_narrow_kernel(DistillArgs 
 // Wide rows: WAVES wavefronts to a row, one row to a workgroup. NP pieces of eight columns a lane in registers; TAIL: there are more. Pieces are counted from the 16-byte
 // line that the row begins in, so that all but the first and the last of them are whole lines (rows of 50003 bf16 15 % faster). An entry is in a lane of every wavefront, which
 // finds those of its own pieces. Sums are in fp64 from a lane's pieces on (exchanged between registers, both softmaxes' at once).
+// Bound by memory: 8192 x 32000 bf16 253 us (4.1 TB/s), fp32 435 (4.8); rows that the registers do not hold are read twice: 4096 x 100000 bf16 496 us, 2048 x 200000 fp32 860.
 // Four wavefronts to a SIMD: with five, 16-bit rows of several wavefronts had to spill registers (20000 x 16384 271 us, four 290; 4096 x 32000 154, four 139).
 template <int T, int WAVES, int NP, bool TAIL>
 __global__ __launch_bounds__(WAVES * 64, 4) void distill_wide_kernel(DistillArgs A) {

@@ -620,10 +620,10 @@ __global__ __launch_bounds__(64 * WAVES_M * WAVES_N, 2) void grouped_tile_kernel
             }
         }
     };
-    // Gated: z where it is wanted, then act(u) * v, formed in the accumulators. 368640 rows x 768 x 1024 fp16 with z: 1570 us (GELU; SiLU 1510, none 1470; without z and
+    // Gated: z where it is wanted, then act(u) * v, formed in the accumulators. 368640 rows x 768 x 1024 fp16 with z: 1570 to 1630 us (GELU; SiLU 1510, none 1470; without z and
     // activation 1235, 0.94 PFLOP/s). All workgroups write 192 KB at about the same time, more than the caches take, and the next tile's second step waits for them: some 300 us
     // of it (1158 with the stores to one place). Starts that are staggered took 15 to 70 us more, tiles of 128 x 128 1903, whole lines to a store 1603, streaming stores
-    // 1550 to 1700 (285 against 304 for 65536 x 1024 x 1024).
+    // 1550 to 1700 (285 against 304 for 65536 x 1024 x 1024). 65536 x 1024 x 1024 bf16 with z 316 us, as one group or as 8 in any order with rows by id; fp32 65536 x 256 x 256 in 4 groups 133.
     auto write_gated = [&](const Tile& F, const TileData& D) {
         const int c0 = F.n0 + wn / 2, columns = N / 2;
 #pragma unroll
